@@ -38,8 +38,8 @@
  *    but the status word, which kernels update atomically).  A context is not
  *    thread-safe.
  *  - Device memory is allocated by hx_ctx_create and hx_dag_reserve, and by
- *    hx_decode_score and hx_rank (beyond 28672 calls) the first time they meet
- *    a larger problem than before; every other call only launches kernels and
+ *    hx_decode_score, hx_rank (beyond 28672 calls), hx_kv_*, hx_attend and
+ *    hx_sample the first time they meet a larger problem than before; every other call only launches kernels and
  *    can be captured in a HIP graph (hx_validate_round and hx_stream_status
  *    wait for the stream and cannot).
  */
@@ -588,6 +588,188 @@ int hx_decode_plan_greedy(hx_ctx *ctx, const hx_model *model, const hx_calls *qu
                           const float *tail, const float *horizon, int32_t n_nodes, int32_t n_wf,
                           int32_t *best_d, float *best_start, float *best_cost, float *ratio, int32_t *rank,
                           void *stream);
+
+/* ---- the serving step of a decode instance ------------------------------- */
+
+/*
+ * What a decode instance does with the calls placed on it, on the same card:
+ * the pages of its KV cache (the tokens that used_tok and cap_tok count), the
+ * attention that reads them, and the choice of the tokens that answer a call.
+ *
+ * The cache is a pool of pages of page_tokens tokens.  A page holds the keys
+ * and the values of its tokens in every layer and KV head; ref counts the
+ * tables that hold it, 0 is a free page.  Sequences are rows of a table: entry
+ * b of a row is the page of positions b*page_tokens .. of its sequence, -1 =
+ * no page (nothing there can be seen).  A row of length 0 holds no page.  Rows
+ * may share pages whose positions are all filled; a page that is being filled
+ * belongs to one row.  All of it is the caller's memory; a pool with
+ * every ref 0 and a table of -1 with lengths 0 is the empty cache.
+ *
+ * Pages are taken lowest number first, in the order of the rows in the call.
+ * Rows in error (out of range, listed twice -- the first counts --, lengths or
+ * pages out of range) are left as they are and raise HX_ERR_INDEX in the stream
+ * status; rows for which no page is left raise HX_ERR_CAPACITY and are left as
+ * they are too.  Scratch: these calls allocate the first time they meet a
+ * larger problem than before, in bytes that follow n_pages and the rows of the
+ * call; what they allocated before stays until the context ends, so graphs
+ * captured earlier stay valid.
+ */
+#define HX_F32   1     /* types of stored numbers */
+#define HX_BF16  2
+#define HX_F16   3
+#define HX_E4M3  4     /* 8 bits: 4 of exponent, 3 of mantissa, no infinity, 448 the largest */
+
+#define HX_MAX_PAGE_TOKENS 1024
+#define HX_MAX_DRAFTS      256       /* drafted tokens of a sequence in hx_attend, as a tree */
+#define HX_MAX_VOCAB       524288    /* logits of a row in hx_sample                        */
+
+typedef struct {
+    int32_t n_layers, n_pages, n_heads;   /* n_heads: KV heads                                  */
+    int32_t page_tokens;      /* a power of two, 1..HX_MAX_PAGE_TOKENS                          */
+    int32_t head_dim;         /* hx_attend: 64, 128 or 256; the others: any multiple of 16      */
+    int32_t dtype;            /* HX_BF16, HX_F16 or HX_E4M3                                     */
+    void *k, *v;              /* device [n_layers][n_pages][n_heads][page_tokens][head_dim], 16-byte aligned */
+    int32_t *ref;             /* device [n_pages]                                               */
+    const float *k_scale;     /* device [n_layers][n_heads], HX_E4M3 only: a stored number times*/
+    const float *v_scale;     /*   this is the key's (value's); > 0; NULL = 1                   */
+} hx_kv_pool;
+
+typedef struct {
+    int32_t n, max_pages;     /* rows, entries of a row                                         */
+    int32_t *table;           /* device [n][max_pages]                                          */
+    int32_t *len;             /* device [n] tokens of each row                                  */
+} hx_kv_seqs;
+
+/*
+ * Row dst[i], which must be empty, becomes a copy of the first n_tok[i] tokens
+ * of row src[i] (n_tok NULL: all of them), as a workflow's calls start from the
+ * prompt of the call above them.  Filled pages are shared; the tokens
+ * of a last page that the copy fills only in part are copied to a page of its
+ * own, in every layer.  Sources are read as they are before the call (a row is
+ * not a source and a destination of the same call).  At most one page a copy.
+ */
+int hx_kv_fork(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs *seqs, int32_t n,
+               const int32_t *src, const int32_t *dst, const int32_t *n_tok, void *stream);
+
+/*
+ * Room for n_new[i] >= 0 more tokens in row[i], whose length grows by as many;
+ * the keys and values are hx_kv_write's.  From the first row on that finds too
+ * few pages left, rows that need a page get none.
+ */
+int hx_kv_grow(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs *seqs, int32_t n,
+               const int32_t *row, const int32_t *n_new, void *stream);
+
+/*
+ * Keys and values of one layer for the last tok_ptr[i+1] - tok_ptr[i] tokens of
+ * row[i]: token j of the call is k[j*token_stride + h*head_stride ..] (numbers
+ * of type src_dtype: HX_F32, HX_BF16 or HX_F16; strides in numbers; n_tok =
+ * tokens in all).  Rounded to the pool's type, to nearest even; HX_E4M3 holds
+ * number / scale, and what lies beyond +-448 becomes +-448 (NaN stays NaN).  A
+ * page that other rows hold too is not written to (HX_ERR_INDEX).
+ */
+int hx_kv_write(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_kv_seqs *seqs, int32_t n,
+                const int32_t *row, const int32_t *tok_ptr, int32_t n_tok, int32_t src_dtype,
+                const void *k, const void *v, int64_t token_stride, int64_t head_stride, void *stream);
+
+/*
+ * Of the last n_draft[i] tokens of row[i] those with the numbers keep[j], j =
+ * keep_ptr[i] .. keep_ptr[i+1]-1 (rising, 0..n_draft[i]-1), stay and move
+ * together, in every layer; the row's length follows and pages past it are
+ * given back.  n_keep = length of keep.  Without any number the drafts are
+ * dropped.  A row whose tokens would move within a page that other rows hold,
+ * or whose page being filled would then be one, is left as it is (HX_ERR_INDEX).
+ */
+int hx_kv_keep(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs *seqs, int32_t n, const int32_t *row,
+               const int32_t *n_draft, const int32_t *keep_ptr, const int32_t *keep, int32_t n_keep, void *stream);
+
+/*
+ * first, last NULL: row[i] gives all its pages back and is empty (a call that
+ * is done).  Else only pages whose positions all lie in first[i] ..
+ * last[i]-1 and are filled are given back (what a sliding window has left
+ * behind); the length stays.  A row may be listed more than once.
+ */
+int hx_kv_free(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs *seqs, int32_t n, const int32_t *row,
+               const int32_t *first, const int32_t *last, void *stream);
+
+/*
+ * Moves pages so that those in use are 0 .. *n_used-1: pages in use beyond that,
+ * rising, go to the free ones below, rising; every table entry of `seqs`
+ * follows.  n_used: device [1] out, or NULL; moved: device [n_pages] out, the
+ * new number of each page (-1: it was free), for tables kept elsewhere, or NULL.
+ */
+int hx_kv_compact(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs *seqs, int32_t *n_used, int32_t *moved,
+                  void *stream);
+
+/*
+ * Attention of the queries of n sequences over their cached keys and values.
+ * Query j, q_ptr[i] <= j < q_ptr[i+1], belongs to the token number j - q_ptr[i]
+ * of the last q_ptr[i+1] - q_ptr[i] tokens of its row, which are in the cache
+ * already.  Query head a reads KV head a / (n_heads / pool n_heads).  With
+ * visible keys y
+ *   s_y = scale * (q . k_y)    lse = log sum_y exp(s_y)    out = sum_y exp(s_y - lse) v_y
+ * and, where no key is visible, out = 0 and lse = -infinity.  Visible are
+ *   without parent: the tokens up to the query's own;
+ *   with parent (device [n_q]): the tokens before the queries' and, of the
+ *     queries' own, the token itself and those above it in a tree of drafts:
+ *     parent[j] = number (below its own) of the token above among the sequence's
+ *     queries, -1 = the last token before them, -2 = left out, as padding (it
+ *     sees nothing, and neither does what is below it).  A token's position
+ *     is that of the last token before the queries + its depth in the tree.  At
+ *     most HX_MAX_DRAFTS queries of a sequence;
+ * of those, with window > 0, the positions below n_sink and the last `window`
+ * positions up to the query's own; and only where the table holds a page.
+ * What is not visible to a query has no part in its result, whatever its bits.
+ * Sums, maxima and outputs are held in 32 bits; the weights exp(s - max) are
+ * rounded to q's type for their product with the values.
+ * A row, q_ptr, page or parent out of range raises HX_ERR_INDEX; its queries
+ * then get out = 0, lse = -infinity, or are not written.
+ */
+typedef struct {
+    int32_t n;                /* sequences                                                      */
+    const int32_t *row;       /* device [n] row of each, NULL = 0..n-1                          */
+    const int32_t *q_ptr;     /* device [n+1], rising from 0 to n_q                             */
+    int32_t n_q;              /* queries in all                                                 */
+    int32_t max_q;            /* most queries of one sequence                                   */
+    int32_t max_len;          /* longest sequence, about: only how the work is divided goes by it */
+    int32_t n_heads;          /* query heads, a multiple of the KV heads                        */
+    int32_t dtype;            /* of q and out: HX_BF16 or HX_F16, the pool's unless that is HX_E4M3 */
+    const void *q;            /* device, strides in numbers, dim contiguous                     */
+    int64_t q_token, q_head;
+    void *out;
+    int64_t out_token, out_head;
+    float *lse;               /* device [n_q][n_heads] or NULL                                  */
+    float scale;              /* finite                                                         */
+    int32_t window;           /* 0 = no window                                                  */
+    int32_t n_sink;
+    const int32_t *parent;
+} hx_attend_args;
+int hx_attend(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_kv_seqs *seqs,
+              const hx_attend_args *args, void *stream);
+
+/*
+ * One token a row from its logits (dtype HX_F32, HX_BF16 or HX_F16; row_stride
+ * in numbers) and a given number u in [0, 1).  With w_i = exp((logit_i - max) /
+ * temperature) and the tokens in falling order of their logits, equal ones in
+ * rising order of their numbers:
+ *   top_k > 0    only the first top_k stay;
+ *   top_p < 1    of those, a token stays if the w before it sum to less than
+ *                top_p times the sum of all those (the first stays always);
+ *   min_p > 0    of those, only w_i >= min_p (the first has w = 1);
+ * then token = the lowest i, in order of the numbers, at which the sum of the w
+ * that stay, up to and with i, exceeds u times their whole sum.  logprob = log of its
+ * share, n_kept = how many stay.  temperature 0 takes the first token of the
+ * order.  NULL for top_k, top_p, min_p: off; for temperature: 1; logprob and
+ * n_kept may be NULL.  The w are held to 2^-42 of the largest or better and added as whole
+ * numbers, so a row's result depends on nothing but its inputs.  -infinity bars a token; where all are
+ * barred token = -1, logprob = -infinity, n_kept = 0.  +infinity takes all the
+ * weight.  A NaN logit counts as -infinity and raises HX_ERR_INVALID_ARG in the stream
+ * status; so does a setting out of range (temperature or min_p below 0, min_p
+ * above 1, any of them or u no number, u outside [0, 1), an infinite temperature), whose row
+ * gets token -1.
+ */
+int hx_sample(hx_ctx *ctx, int32_t n_rows, int32_t n_vocab, int32_t dtype, const void *logits, int64_t row_stride,
+              const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p, const float *u,
+              int32_t *token, float *logprob, int32_t *n_kept, void *stream);
 
 #ifdef __cplusplus
 }

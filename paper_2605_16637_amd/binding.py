@@ -20,7 +20,10 @@ ERRORS = {-1: "HX_ERR_INVALID_ARG", -2: "HX_ERR_SHAPE", -3: "HX_ERR_NOT_DAG", -4
 EXPORTS = ("hx_ctx_create", "hx_ctx_destroy", "hx_last_error", "hx_stream_status", "hx_node_cost",
            "hx_critical_path", "hx_horizons", "hx_dag_reserve", "hx_dag_append", "hx_dag_set_cost", "hx_dag_view",
            "hx_score_placements", "hx_validate_round", "hx_select", "hx_urgency", "hx_commit", "hx_commit_static", "hx_round", "hx_rank", "hx_plan_greedy",
-           "hx_decode_score", "hx_decode_plan_greedy")
+           "hx_decode_score", "hx_decode_plan_greedy",
+           "hx_kv_fork", "hx_kv_grow", "hx_kv_write", "hx_kv_keep", "hx_kv_free", "hx_kv_compact", "hx_attend", "hx_sample")
+
+HX_F32, HX_BF16, HX_F16, HX_E4M3 = 1, 2, 3, 4
 
 
 class HxError(RuntimeError):
@@ -71,6 +74,24 @@ class hx_round_args(C.Structure):
                 ("backlog_tok", C.c_void_p), ("used_tok", C.c_void_p), ("batch", C.c_void_p), ("qd_tok", C.c_void_p),
                 ("drain_prefill", C.c_void_p), ("drain_decode_q", C.c_void_p), ("release_tok", C.c_void_p),
                 ("tokens_per_seq", C.c_int32), ("max_batch", C.c_int32)]
+
+
+class hx_kv_pool(C.Structure):
+    _fields_ = [("n_layers", C.c_int32), ("n_pages", C.c_int32), ("n_heads", C.c_int32), ("page_tokens", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("ref", C.c_void_p),
+                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class hx_kv_seqs(C.Structure):
+    _fields_ = [("n", C.c_int32), ("max_pages", C.c_int32), ("table", C.c_void_p), ("len", C.c_void_p)]
+
+
+class hx_attend_args(C.Structure):
+    _fields_ = [("n", C.c_int32), ("row", C.c_void_p), ("q_ptr", C.c_void_p), ("n_q", C.c_int32), ("max_q", C.c_int32),
+                ("max_len", C.c_int32), ("n_heads", C.c_int32), ("dtype", C.c_int32), ("q", C.c_void_p),
+                ("q_token", C.c_int64), ("q_head", C.c_int64), ("out", C.c_void_p), ("out_token", C.c_int64),
+                ("out_head", C.c_int64), ("lse", C.c_void_p), ("scale", C.c_float), ("window", C.c_int32),
+                ("n_sink", C.c_int32), ("parent", C.c_void_p)]
 
 
 _lib = None
@@ -226,6 +247,51 @@ def make_intervals(iv: dict, D: int) -> hx_intervals:
     k = int(iv["stride"])
     return hx_intervals(k, _ptr(iv["count"], torch.int32, D), _ptr(iv["start"], torch.float32, D * k),
                         _ptr(iv["end"], torch.float32, D * k), _ptr(iv["tok"], torch.int32, D * k))
+
+
+_number_types = None
+
+
+def _number_type(t, *allowed):
+    """HX_* of a tensor's type."""
+    global _number_types
+    if _number_types is None:
+        torch = _torch()
+        _number_types = {torch.float32: HX_F32, torch.bfloat16: HX_BF16, torch.float16: HX_F16, torch.float8_e4m3fn: HX_E4M3}
+    got = _number_types.get(t.dtype)
+    if got not in allowed:
+        raise ValueError(f"tensor of type {t.dtype}")
+    return got
+
+
+def make_kv_pool(p: dict) -> hx_kv_pool:
+    """From k, v [layers, pages, KV heads, page_tokens, head_dim], ref [pages] and, for 8-bit caches, k_scale, v_scale [layers, KV heads]."""
+    torch = _torch()
+    k, v = p["k"], p["v"]
+    if k.dim() != 5 or v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError("expected k and v of one type, [layers, pages, KV heads, page_tokens, head_dim]")
+    n_layers, n_pages, n_heads, tokens, dim = k.shape
+    if tokens != int(p.get("page_tokens", tokens)):
+        raise ValueError(f"pages of {tokens} tokens, not {p['page_tokens']}")
+    return hx_kv_pool(n_layers, n_pages, n_heads, tokens, dim, _number_type(k, HX_BF16, HX_F16, HX_E4M3), _ptr(k), _ptr(v),
+                      _ptr(p["ref"], torch.int32, n_pages), _ptr(p.get("k_scale"), torch.float32, n_layers * n_heads),
+                      _ptr(p.get("v_scale"), torch.float32, n_layers * n_heads))
+
+
+def make_kv_seqs(s: dict) -> hx_kv_seqs:
+    torch = _torch()
+    table = s["table"]
+    n, max_pages = table.shape
+    return hx_kv_seqs(n, max_pages, _ptr(table, torch.int32), _ptr(s["len"], torch.int32, n))
+
+
+def _strided(t, n, heads, dim):
+    """Address, token and head stride of a [n, heads, dim] tensor whose last dimension is contiguous (any strides before it)."""
+    if t.dim() != 3 or t.shape[0] < n or t.shape[1] != heads or t.shape[2] != dim:
+        raise ValueError(f"expected [{n}, {heads}, {dim}], got {list(t.shape)}")
+    if not t.is_cuda or (dim > 1 and t.stride(2) != 1):
+        raise ValueError("expected a tensor in device memory whose last dimension is contiguous")
+    return t.data_ptr(), t.stride(0), t.stride(1)
 
 
 class Context:
@@ -501,6 +567,78 @@ class Context:
             _ptr(tail, f32), _ptr(horizon, f32), int(tail.numel()), int(horizon.numel()),
             _ptr(best_d, i32, cs.n), _ptr(best_start, f32, cs.n), _ptr(best_cost, f32, cs.n), _ptr(ratio, f32, cs.n),
             _ptr(rank, i32, cs.n), _stream(stream))
+
+    def hx_kv_fork(self, pool, seqs, src, dst, n_tok=None, stream=None):
+        torch = _torch()
+        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs), int(src.numel()), torch.int32
+        self._invoke(self.lib.hx_kv_fork, self._ctx, C.byref(kv), C.byref(sq), n, _ptr(src, i32), _ptr(dst, i32, n),
+                     _ptr(n_tok, i32, n), _stream(stream))
+
+    def hx_kv_grow(self, pool, seqs, row, n_new, stream=None):
+        torch = _torch()
+        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs), int(row.numel()), torch.int32
+        self._invoke(self.lib.hx_kv_grow, self._ctx, C.byref(kv), C.byref(sq), n, _ptr(row, i32), _ptr(n_new, i32, n), _stream(stream))
+
+    def hx_kv_write(self, pool, layer, seqs, row, tok_ptr, k, v, stream=None):
+        """k, v [tokens, KV heads, head_dim], of one type and one set of strides."""
+        torch = _torch()
+        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs), int(row.numel()), torch.int32
+        n_tok = int(k.shape[0])
+        kp, token, head = _strided(k, n_tok, kv.n_heads, kv.head_dim)
+        vp, v_token, v_head = _strided(v, n_tok, kv.n_heads, kv.head_dim)
+        if (v_token, v_head) != (token, head) or v.dtype != k.dtype or v.shape != k.shape:
+            raise ValueError("expected k and v of one type, shape and set of strides")
+        self._invoke(self.lib.hx_kv_write, self._ctx, C.byref(kv), int(layer), C.byref(sq), n, _ptr(row, i32), _ptr(tok_ptr, i32, n + 1),
+                     n_tok, _number_type(k, HX_F32, HX_BF16, HX_F16), C.c_void_p(kp), C.c_void_p(vp), C.c_int64(token), C.c_int64(head),
+                     _stream(stream))
+
+    def hx_kv_keep(self, pool, seqs, row, n_draft, keep_ptr, keep, stream=None):
+        torch = _torch()
+        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs), int(row.numel()), torch.int32
+        self._invoke(self.lib.hx_kv_keep, self._ctx, C.byref(kv), C.byref(sq), n, _ptr(row, i32), _ptr(n_draft, i32, n),
+                     _ptr(keep_ptr, i32, n + 1), _ptr(keep, i32), int(keep.numel()), _stream(stream))
+
+    def hx_kv_free(self, pool, seqs, row, first=None, last=None, stream=None):
+        torch = _torch()
+        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs), int(row.numel()), torch.int32
+        self._invoke(self.lib.hx_kv_free, self._ctx, C.byref(kv), C.byref(sq), n, _ptr(row, i32), _ptr(first, i32, n), _ptr(last, i32, n),
+                     _stream(stream))
+
+    def hx_kv_compact(self, pool, seqs, n_used=None, moved=None, stream=None):
+        torch = _torch()
+        kv, sq, i32 = make_kv_pool(pool), make_kv_seqs(seqs), torch.int32
+        self._invoke(self.lib.hx_kv_compact, self._ctx, C.byref(kv), C.byref(sq), _ptr(n_used, i32, 1), _ptr(moved, i32, kv.n_pages),
+                     _stream(stream))
+
+    def hx_attend(self, pool, layer, seqs, q_ptr, q, out, max_q, max_len=None, row=None, scale=None, window=0, n_sink=0, parent=None,
+                  lse=None, stream=None):
+        """q, out [queries, query heads, head_dim] (any strides before the last dimension); scale None: head_dim ** -0.5; max_len None:
+        what the table can hold."""
+        torch = _torch()
+        kv, sq, i32 = make_kv_pool(pool), make_kv_seqs(seqs), torch.int32
+        n, n_q, heads = int(q_ptr.numel()) - 1, int(q.shape[0]), int(q.shape[1])
+        if out.dtype != q.dtype:
+            raise ValueError(f"out of type {out.dtype} for queries of type {q.dtype}")
+        a = hx_attend_args()
+        a.n, a.row, a.q_ptr, a.n_q, a.max_q = n, _ptr(row, i32, n), _ptr(q_ptr, i32), n_q, int(max_q)
+        a.max_len = sq.max_pages * kv.page_tokens if max_len is None else int(max_len)
+        a.n_heads, a.dtype = heads, _number_type(q, HX_BF16, HX_F16)
+        a.q, a.q_token, a.q_head = _strided(q, n_q, heads, kv.head_dim)
+        a.out, a.out_token, a.out_head = _strided(out, n_q, heads, kv.head_dim)
+        a.lse, a.scale = _ptr(lse, torch.float32, n_q * heads), kv.head_dim ** -0.5 if scale is None else float(scale)
+        a.window, a.n_sink, a.parent = int(window), int(n_sink), _ptr(parent, i32, n_q)
+        self._invoke(self.lib.hx_attend, self._ctx, C.byref(kv), int(layer), C.byref(sq), C.byref(a), _stream(stream))
+
+    def hx_sample(self, logits, u, token, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, n_kept=None, stream=None):
+        """logits [rows, vocabulary], the rows any stride apart."""
+        torch = _torch()
+        if logits.dim() != 2 or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
+            raise ValueError("expected [rows, vocabulary] in device memory, each row contiguous")
+        n, v = logits.shape
+        f32, i32 = torch.float32, torch.int32
+        self._invoke(self.lib.hx_sample, self._ctx, n, v, _number_type(logits, HX_F32, HX_BF16, HX_F16), C.c_void_p(logits.data_ptr()),
+                     C.c_int64(logits.stride(0)), _ptr(temperature, f32, n), _ptr(top_k, i32, n), _ptr(top_p, f32, n), _ptr(min_p, f32, n),
+                     _ptr(u, f32, n), _ptr(token, i32, n), _ptr(logprob, f32, n), _ptr(n_kept, i32, n), _stream(stream))
 
 
 def hx_commit_static(calls, best_p, best_d, backlog_tok, used_tok, batch, qd_tok,

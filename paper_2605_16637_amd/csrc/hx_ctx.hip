@@ -17,6 +17,7 @@ int hx_relax_search(hx_ctx *ctx, const hx_model *model, const hx_calls *calls,
                     const HxAppendPlan *walks, bool *merged, void *stream);         // hx_score.hip
 int hx_plan_init();                 // hx_plan.hip
 int hx_decode_init();               // hx_decode.hip
+int hx_attend_init();               // hx_attend.hip
 
 namespace {
 
@@ -402,7 +403,7 @@ extern "C" int hx_ctx_create(hx_ctx **out, int device)
         unsigned long long *p = nullptr;
         e = hx_static_scratch(device, &p);
     }
-    if (e == hipSuccess && (hx_plan_init() != HX_OK || hx_decode_init() != HX_OK)) { what = "hipFuncSetAttribute(LDS size)"; e = hipErrorInvalidValue; }
+    if (e == hipSuccess && (hx_plan_init() != HX_OK || hx_decode_init() != HX_OK || hx_attend_init() != HX_OK)) { what = "hipFuncSetAttribute(LDS size)"; e = hipErrorInvalidValue; }
     if (e == hipSuccess) {
         what = "launch of hx_clear_status_kernel";
         CommitArgs z{};
@@ -437,6 +438,9 @@ extern "C" int hx_ctx_destroy(hx_ctx *ctx)
     if (ctx->d_dtl) (void)hipFree(ctx->d_dtl);
     if (ctx->d_dtab) (void)hipFree(ctx->d_dtab);
     if (ctx->d_rkey) (void)hipFree(ctx->d_rkey);
+    hx_scratch_release(ctx->kv);
+    hx_scratch_release(ctx->att);
+    hx_scratch_release(ctx->smp);
     delete ctx;
     return HX_OK;
 }
@@ -460,8 +464,8 @@ extern "C" int hx_stream_status(hx_ctx *ctx, void *stream_)
         const char *what = code == HX_ERR_NOT_DAG ? "an edge breaks the DAG order, or no fixed point within the sweep limit"
                          : code == HX_ERR_INDEX ? "an index held in a device array is out of range"
                          : code == HX_ERR_OVERFLOW ? "an instance counter exceeded INT32_MAX"
-                         : code == HX_ERR_INVALID_ARG ? "the cost of a node is below 0 or no number"
-                         : code == HX_ERR_CAPACITY ? "a limit was hit on the device: propagation did not finish within max_depth sweeps, or an interval list is full"
+                         : code == HX_ERR_INVALID_ARG ? "the cost of a node is below 0 or no number, or a logit or a sampling setting is none or out of range"
+                         : code == HX_ERR_CAPACITY ? "a limit was hit on the device: propagation did not finish within max_depth sweeps, an interval list is full, or the cache has no page left"
                                                    : "device status";
         return hx_fail(ctx, code, "%s", what);
     }

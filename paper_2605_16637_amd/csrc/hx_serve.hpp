@@ -1,0 +1,56 @@
+// What the serving step's files share: the cache's addresses, its number types, and checks of its descriptors.
+#pragma once
+
+#include "hx_common.hpp"
+
+// The pool and the tables as kernels take them.  T = 1 << shift tokens a page.
+struct KvView {
+    void *k, *v;
+    int32_t *ref;
+    int32_t *table, *len;
+    int32_t *status;
+    int n_layers, n_pages, n_heads, shift, dim;
+    int rows, max_pages;
+};
+
+inline int hx_type_size(int dtype) { return dtype == HX_F32 ? 4 : dtype == HX_E4M3 ? 1 : 2; }
+
+// Fills a view after the checks every call makes.
+inline int hx_kv_view(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs *seqs, KvView *out)
+{
+    HX_REQUIRE(ctx, pool && seqs, HX_ERR_INVALID_ARG, "NULL pool or sequences");
+    HX_REQUIRE(ctx, pool->n_layers > 0 && pool->n_pages >= 0 && pool->n_heads > 0 && pool->head_dim > 0, HX_ERR_INVALID_ARG,
+               "pool of %d layers, %d pages, %d heads of %d", pool->n_layers, pool->n_pages, pool->n_heads, pool->head_dim);
+    HX_REQUIRE(ctx, pool->dtype == HX_BF16 || pool->dtype == HX_F16 || pool->dtype == HX_E4M3, HX_ERR_INVALID_ARG, "pool of type %d", pool->dtype);
+    const int T = pool->page_tokens;
+    HX_REQUIRE(ctx, T >= 1 && T <= HX_MAX_PAGE_TOKENS && (T & (T - 1)) == 0, HX_ERR_SHAPE,
+               "page_tokens %d is no power of two up to %d", T, HX_MAX_PAGE_TOKENS);
+    HX_REQUIRE(ctx, pool->head_dim % 16 == 0 && pool->head_dim <= 1024, HX_ERR_SHAPE, "head_dim %d is no multiple of 16 up to 1024", pool->head_dim);
+    HX_REQUIRE(ctx, pool->n_heads <= 65536 && pool->n_layers <= 65536, HX_ERR_SHAPE, "%d layers of %d heads", pool->n_layers, pool->n_heads);
+    HX_REQUIRE(ctx, pool->n_pages == 0 || (pool->k && pool->v && pool->ref), HX_ERR_INVALID_ARG, "NULL member in pool");
+    HX_REQUIRE(ctx, (((uintptr_t)pool->k | (uintptr_t)pool->v) & 15) == 0, HX_ERR_INVALID_ARG, "the pool's k and v have to be 16-byte aligned");
+    HX_REQUIRE(ctx, pool->dtype == HX_E4M3 || (!pool->k_scale && !pool->v_scale), HX_ERR_INVALID_ARG, "scales are for a pool of HX_E4M3");
+    HX_REQUIRE(ctx, seqs->n >= 0 && seqs->max_pages >= 0, HX_ERR_INVALID_ARG, "negative size of sequences");
+    HX_REQUIRE(ctx, (int64_t)seqs->max_pages * T <= INT32_MAX, HX_ERR_SHAPE, "%d pages of %d tokens a row are beyond int32", seqs->max_pages, T);
+    HX_REQUIRE(ctx, seqs->n == 0 || (seqs->len && (seqs->table || seqs->max_pages == 0)), HX_ERR_INVALID_ARG, "NULL member in sequences");
+    int shift = 0;
+    while ((1 << shift) < T) ++shift;
+    *out = KvView{pool->k, pool->v, pool->ref, seqs->table, seqs->len, ctx->d_status, pool->n_layers, pool->n_pages, pool->n_heads, shift,
+                  pool->head_dim, seqs->n, seqs->max_pages};
+    return HX_OK;
+}
+
+__host__ __device__ inline int hx_pages_of(int tokens, int shift) { return (int)(((int64_t)tokens + (1 << shift) - 1) >> shift); }
+
+// a row of the tables whose length its entries can hold
+__device__ __forceinline__ bool hx_row_ok(const KvView &kv, int r, int len) { return len >= 0 && len <= (int64_t)kv.max_pages << kv.shift; }
+
+__device__ __forceinline__ int32_t *hx_row(const KvView &kv, int r) { return kv.table + (int64_t)r * kv.max_pages; }
+
+// numbers before (page, head, token) of a layer
+__device__ __forceinline__ int64_t hx_kv_at(const KvView &kv, int layer, int page, int head, int tok)
+{
+    return ((((int64_t)layer * kv.n_pages + page) * kv.n_heads + head) << kv.shift) * kv.dim + (int64_t)tok * kv.dim;
+}
+
+__device__ __forceinline__ int hx_sync_load(const int32_t *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
