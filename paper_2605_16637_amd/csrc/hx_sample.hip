@@ -3,7 +3,7 @@
 // Nothing is sorted.  What stays of a row is always a prefix of its order (logit falling, number rising), so a limit is one element, the
 // last that stays: it is found by adding up the row's elements in bins of the logit -- counts for top-k, weights for top-p --, then the
 // elements of the bin where the limit falls, in finer bins where they are many.  The token is found the same way in the
-// order of the numbers.  Weights are whole numbers of 2^-q of the largest (q from 42 to 61 with the row's length, so that a row's sum
+// order of the numbers.  Weights are whole numbers of 2^-q of the largest (q = 42 to 50 by the row's length, so that a row's sum
 // stays below 2^62): sums do not depend on the order they are added in, and no limit on how rounding went.
 #include "hx_serve.hpp"
 
@@ -11,8 +11,11 @@ namespace {
 
 constexpr int SA_THREADS = 1024;
 constexpr int SA_WAVES = SA_THREADS / HX_WAVE;
-constexpr int SA_BINS = 128, SA_COLS = 32;        // a bin's sum lies in 32 places, a lane's by its number: lanes of a wavefront seldom meet
-constexpr int SA_LIST = 256;                      // elements of the limit's bin that are compared with each other
+constexpr int SA_UNROLL = 4;                      // pieces of 16 bytes a lane adds up before the wavefront does
+constexpr int SA_STEP = SA_UNROLL * HX_WAVE;
+constexpr int SA_BINS = 1408, SA_COLS = 4;        // 32 bins to a factor of 2 in weight, 44 factors; a bin's sum lies in 4 places, a lane's by its number
+constexpr int SA_LIST = 1792;                     // elements of the limit's bin that are looked at in LDS
+constexpr int SA_FEW = 128;                       // of them, those that are compared with each other
 
 struct SampleArgs {
     int n_rows, n_vocab, qbits;
@@ -43,26 +46,6 @@ __device__ __forceinline__ uint32_t key_of(float x)
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 constexpr uint32_t KEY_BARRED = 0x007fffffu;       // of -infinity; a NaN's is made the same
 
-// 2^z for z <= 0, to 2^-50 of it: the whole part by the exponent, the rest, |f| <= 1/2, by the series of exp(f ln 2) to f^12
-__device__ __forceinline__ double exp2_neg(double z)
-{
-    const double n = __builtin_rint(z), f = z - n;
-    double p = 2.5678435993488205e-11;                        // ln2^12 / 12!
-    p = __builtin_fma(p, f, 4.4455382718708116e-10);
-    p = __builtin_fma(p, f, 7.0549116208011233e-09);
-    p = __builtin_fma(p, f, 1.0178086009239699e-07);
-    p = __builtin_fma(p, f, 1.3215486790144307e-06);
-    p = __builtin_fma(p, f, 1.5252733804059841e-05);
-    p = __builtin_fma(p, f, 1.5403530393381609e-04);
-    p = __builtin_fma(p, f, 1.3333558146428443e-03);
-    p = __builtin_fma(p, f, 9.6181291076284772e-03);
-    p = __builtin_fma(p, f, 5.5504108664821580e-02);
-    p = __builtin_fma(p, f, 2.4022650695910072e-01);
-    p = __builtin_fma(p, f, 6.9314718055994531e-01);
-    p = __builtin_fma(p, f, 1.0);
-    return n < -1000.0 ? 0.0 : __builtin_ldexp(p, (int)n);
-}
-
 // floor(f * w) for 0 <= f < 1; *rest: whether something was cut off
 __device__ __forceinline__ uint64_t scaled(float f, uint64_t w, bool *rest)
 {
@@ -82,69 +65,151 @@ __device__ __forceinline__ uint64_t scaled(float f, uint64_t w, bool *rest)
 
 struct Shared {
     uint64_t hist[SA_BINS * SA_COLS];          // and the sums of locate()
+    uint32_t lkey[SA_LIST];
+    int lidx[SA_LIST];
+    double tab[32];                            // 2^(j / 32)
     uint64_t wave[SA_WAVES];
-    uint32_t wmin[SA_WAVES], wmax[SA_WAVES];
-    uint32_t key[SA_LIST];
-    int idx[SA_LIST];
-    uint64_t mass[SA_LIST];
+    int wmin[SA_WAVES], wmax[SA_WAVES];
     uint64_t r64[2];
     int r32[4];
 };
 
+template <typename E> struct Raw;
+template <> struct Raw<float> {
+    static constexpr int EACH = 4;
+    static constexpr uint32_t BARRED = 0xff800000u;
+    static constexpr int INF = 0x7f800000;
+    // signed whole numbers in the order of the stored ones
+    static __device__ __forceinline__ void extremes(const uint32_t *w, int &hi, int &lo)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int x = (int)w[i], s = x ^ ((x >> 31) & 0x7fffffff);
+            hi = s > hi ? s : hi;
+            lo = s < lo ? s : lo;
+        }
+    }
+    static __device__ __forceinline__ float of_order(int s) { return __uint_as_float((uint32_t)(s ^ ((s >> 31) & 0x7fffffff))); }
+    static __device__ __forceinline__ float get(const uint32_t *w, int j) { return __uint_as_float(w[j]); }
+};
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+template <typename E> struct Raw16 {
+    static constexpr int EACH = 8;
+    static __device__ __forceinline__ void extremes(const uint32_t *w, int &hi, int &lo)
+    {
+        i16x2 h = __builtin_bit_cast(i16x2, hi), l = __builtin_bit_cast(i16x2, lo);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const i16x2 x = __builtin_bit_cast(i16x2, w[i]), s = x ^ ((x >> 15) & (short)0x7fff);
+            h = __builtin_elementwise_max(h, s);
+            l = __builtin_elementwise_min(l, s);
+        }
+        hi = __builtin_bit_cast(int, h);
+        lo = __builtin_bit_cast(int, l);
+    }
+};
+template <> struct Raw<__bf16> : Raw16<__bf16> {
+    static constexpr uint32_t BARRED = 0xff80ff80u;
+    static constexpr int INF = 0x7f80;
+    static __device__ __forceinline__ float of_order(int s) { return __uint_as_float((uint32_t)(s ^ ((s >> 31) & 0x7fff)) << 16); }
+    static __device__ __forceinline__ float get(const uint32_t *w, int j) { return __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16); }
+};
+template <> struct Raw<_Float16> : Raw16<_Float16> {
+    static constexpr uint32_t BARRED = 0xfc00fc00u;
+    static constexpr int INF = 0x7c00;
+    static __device__ __forceinline__ float of_order(int s) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(s ^ ((s >> 31) & 0x7fff))); }
+    static __device__ __forceinline__ float get(const uint32_t *w, int j) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(w[j / 2] >> (16 * (j & 1)))); }
+};
+
+// A row in pieces of 16 aligned bytes; wavefront w has the pieces w per .. (w + 1) per - 1.
 template <typename E>
 struct Row {
+    using R = Raw<E>;
+    static constexpr int EACH = R::EACH;
     const E *p;
-    int n, skip;              // elements; those of the first 16 bytes that lie before the row
-    int per;                  // pieces of a wavefront, a multiple of 64
-    int pieces;
-    static constexpr int EACH = 16 / sizeof(E);      // elements of a piece
+    int n, skip;              // elements; those of the first piece that lie before the row
+    int per, pieces;
+    bool nans;                // some element is no number
 
     __device__ void set(const E *at, int count)
     {
         p = at;
         n = count;
+        nans = false;
         skip = (int)(((uintptr_t)at & 15) / sizeof(E));
         pieces = (int)(((int64_t)n + skip + EACH - 1) / EACH);
         const int64_t w = ((int64_t)pieces + SA_WAVES - 1) / SA_WAVES;
-        per = (int)((w + HX_WAVE - 1) / HX_WAVE * HX_WAVE);
+        per = (int)((w + SA_STEP - 1) / SA_STEP * SA_STEP);
     }
-    // The elements of piece c: their keys, KEY_BARRED for what is not of the row.
-    __device__ __forceinline__ void keys(int c, uint32_t *k) const
+    // piece c as it is stored; -infinity for what is not of the row, and for a NaN
+    __device__ __forceinline__ void load_any(int c, uint32_t *w) const
     {
         const int64_t first = (int64_t)c * EACH - skip;
-        if (first >= 0 && first + EACH <= n) {
-            struct alignas(16) Piece { E x[EACH]; };
-            const Piece v = *(const Piece *)(p + first);
 #pragma unroll
-            for (int j = 0; j < EACH; ++j) k[j] = key(to_float(v.x[j]));
-        } else {
+        for (int i = 0; i < 4; ++i) w[i] = R::BARRED;
 #pragma unroll
-            for (int j = 0; j < EACH; ++j) k[j] = first + j >= 0 && first + j < n ? key(to_float(p[first + j])) : KEY_BARRED;
-        }
+        for (int j = 0; j < EACH; ++j)
+            if (first + j >= 0 && first + j < n) {
+                const E x = p[first + j];
+                if (is_nan(to_float(x)) && nans) continue;
+                if constexpr (sizeof(E) == 4) w[j] = __float_as_uint(x);
+                else {
+                    const uint32_t y = __builtin_bit_cast(uint16_t, x);
+                    w[j / 2] = j & 1 ? (w[j / 2] & 0xffffu) | y << 16 : (w[j / 2] & 0xffff0000u) | y;
+                }
+            }
     }
-    static __device__ __forceinline__ uint32_t key(float x) { return is_nan(x) ? KEY_BARRED : key_of(x); }
-    __device__ __forceinline__ int index(int c, int j) const { return c * EACH - skip + j; }
-    // f(piece, its keys) for all of this wavefront's, all lanes together
-    template <typename F>
-    __device__ __forceinline__ void each(F f) const
+    // piece at + lane
+    __device__ __forceinline__ uint4 load(int at) const
     {
-        const int lane = threadIdx.x & 63, c0 = (threadIdx.x >> 6) * per;
-        for (int it = 0; it < per; it += HX_WAVE) {
-            const int c = c0 + it + lane;
-            uint32_t k[EACH];
-            if (c < pieces) keys(c, k);
-            else
-#pragma unroll
-                for (int j = 0; j < EACH; ++j) k[j] = KEY_BARRED;
-            f(c, k, it / HX_WAVE);
+        const int lane = threadIdx.x & 63;
+        if ((int64_t)at * EACH >= skip && (int64_t)(at + HX_WAVE) * EACH - skip <= n && !nans)      // the same for all lanes
+            return *((const uint4 *)(p - skip) + at + lane);
+        uint32_t w[4];
+        load_any(at + lane, w);
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    static __device__ __forceinline__ uint32_t key(const uint32_t *w, int j) { return key_of(R::get(w, j)); }
+    __device__ __forceinline__ int index(int c, int j) const { return c * EACH - skip + j; }
+    // f(number of the piece, piece) for all pieces of this wavefront, a lane's next two being asked for meanwhile; done(step) after
+    // each SA_UNROLL of them
+    template <typename F, typename D>
+    __device__ __forceinline__ void each(F f, D done) const
+    {
+        const int lane = threadIdx.x & 63, c0 = (threadIdx.x >> 6) * per, end = c0 + per < pieces ? c0 + per : pieces;
+        uint4 now = make_uint4(0, 0, 0, 0), next = now;
+        if (c0 < end) now = load(c0);
+        if (c0 + HX_WAVE < end) next = load(c0 + HX_WAVE);
+#pragma unroll 1
+        for (int at = c0; at < c0 + per; at += HX_WAVE) {
+            if (at < end) {
+                const uint32_t w[4] = {now.x, now.y, now.z, now.w};
+                now = next;
+                if (at + 2 * HX_WAVE < end) next = load(at + 2 * HX_WAVE);
+                f(at + lane, w);
+            }
+            if ((at - c0) % SA_STEP == SA_STEP - HX_WAVE) done((at - c0) / SA_STEP);
         }
     }
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const { each(f, [](int) {}); }
 };
 
 __device__ __forceinline__ uint64_t wave_sum(uint64_t x)
 {
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+    return x;
+}
+// inclusive
+__device__ __forceinline__ uint64_t wave_scan(uint64_t x)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < HX_WAVE; d <<= 1) {
+        const uint64_t y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
     return x;
 }
 
@@ -155,148 +220,216 @@ struct Limit {
     __device__ __forceinline__ bool holds(uint32_t k, int i) const { return k > key || (k == key && i <= idx); }
 };
 
-// The lowest element at which the sum of `mass` in the order of the numbers exceeds target(total); -1: nowhere.
+// Weights of a row: 2^q exp((x - top) / T) = 2^q 2^(z / 32).  z's whole part picks a number of the table and the exponent, the rest,
+// |f| <= 1/2, goes through the series of exp(f ln 2 / 32) up to f^5: 2^-48 of the weight.
+struct Weights {
+    double top, inv;          // 32 log2(e) / T
+    const double *tab;
+    int q;
+    bool boundless;           // the largest is +infinity, which takes all the weight
+    uint32_t hi;
+
+    __device__ __forceinline__ double reach(uint32_t k) const { return fmax(((double)of_key(k) - top) * inv, -1.0e6); }
+    __device__ __forceinline__ int bin(uint32_t k) const
+    {
+        if (boundless) return k == hi ? 0 : SA_BINS - 1;
+        const int b = -(int)__builtin_bit_cast(uint64_t, reach(k) + 6755399441055744.0);     // 1.5 2^52: the nearest whole number in the low bits
+        return b < SA_BINS - 1 ? b : SA_BINS - 1;
+    }
+    // the weight, and its bin
+    __device__ __forceinline__ double scaled(uint32_t k, int *b) const
+    {
+        if (boundless) {
+            *b = k == hi ? 0 : SA_BINS - 1;
+            return k == hi ? __builtin_ldexp(1.0, q) : 0.0;
+        }
+        const double z = reach(k), t = z + 6755399441055744.0, f = z - (t - 6755399441055744.0);
+        const int n = (int)__builtin_bit_cast(uint64_t, t);
+        double p = 3.9737099845494154e-11;                    // (ln 2 / 32)^5 / 5!
+        p = __builtin_fma(p, f, 9.172562701824643e-09);
+        p = __builtin_fma(p, f, 1.6938509724371819e-06);
+        p = __builtin_fma(p, f, 2.3459619820224677e-04);
+        p = __builtin_fma(p, f, 2.166084939249829e-02);
+        p = __builtin_fma(p, f, 1.0);
+        *b = -n < SA_BINS - 1 ? -n : SA_BINS - 1;
+        return __builtin_ldexp(p * tab[n & 31], (n >> 5) + q);
+    }
+    // to the nearest whole number; it is below 2^51
+    static __device__ __forceinline__ uint64_t whole(double w) { return __builtin_bit_cast(uint64_t, w + 4503599627370496.0) & 0xfffffffffffffull; }
+    __device__ __forceinline__ uint64_t mass(uint32_t k) const { int b; return whole(scaled(k, &b)); }
+};
+
+// The lowest element at which the sum of `mass` in the order of the numbers exceeds target(total); -1: nowhere.  mass(key,
+// number, &in) says whether the element counts, *count how many do.
 template <typename E, typename M, typename W>
-__device__ int locate(const Row<E> &row, Shared &s, M mass, W target, uint64_t *total)
+__device__ __forceinline__ int locate(const Row<E> &row, Shared &s, M mass, W target, uint64_t *total, int *count)
 {
     constexpr int EACH = Row<E>::EACH;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, iters = row.per / HX_WAVE;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, steps = row.per / SA_STEP;
+    int mine = 0;
+    uint64_t x = 0;
     __syncthreads();
-    row.each([&](int c, const uint32_t *k, int it) {
-        uint64_t x = 0;
+    row.each([&](int c, const uint32_t *p) {
 #pragma unroll
-        for (int j = 0; j < EACH; ++j) x += k[j] > KEY_BARRED ? mass(k[j], row.index(c, j)) : 0;
+        for (int j = 0; j < EACH; ++j) {
+            bool in;
+            x += mass(row.key(p, j), row.index(c, j), &in);
+            mine += in;
+        }
+    }, [&](int step) {
         x = wave_sum(x);
-        if (lane == 0) s.hist[w * iters + it] = x;
+        if (lane == 0) s.hist[w * steps + step] = x;
+        x = 0;
     });
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) mine += __shfl_xor(mine, d);
+    if (lane == 0) s.wmin[w] = mine;
     if (tid == 0) s.r32[0] = -1;
     __syncthreads();
-    // the step of 64 pieces at which it is exceeded: by the first wavefront
+    // the step at which it is exceeded, and the element: the first wavefront
     if (w == 0) {
         uint64_t all = 0;
-        for (int i = lane; i < SA_WAVES * iters; i += HX_WAVE) all += s.hist[i];
+        for (int i = lane; i < SA_WAVES * steps; i += HX_WAVE) all += s.hist[i];
         all = wave_sum(all);
         const uint64_t want = target(all);
         uint64_t before = 0;
         int at = -1;
-        for (int i0 = 0; i0 < SA_WAVES * iters && at < 0; i0 += HX_WAVE) {
-            uint64_t x = i0 + lane < SA_WAVES * iters ? s.hist[i0 + lane] : 0, sum = x;
-#pragma unroll
-            for (int d = 1; d < HX_WAVE; d <<= 1) {
-                const uint64_t y = __shfl_up(sum, d);
-                if (lane >= d) sum += y;
-            }
+        for (int i0 = 0; i0 < SA_WAVES * steps && at < 0; i0 += HX_WAVE) {
+            const uint64_t y = i0 + lane < SA_WAVES * steps ? s.hist[i0 + lane] : 0, sum = wave_scan(y);
             const unsigned long long m = __builtin_amdgcn_ballot_w64(before + sum > want);
             if (m) {
                 const int l = __builtin_ctzll(m);
                 at = i0 + l;
-                before += __shfl(sum - x, l);
+                before += __shfl(sum - y, l);
             } else before += __shfl(sum, 63);
         }
         if (at >= 0) {
-            const int c = (at / iters) * row.per + (at % iters) * HX_WAVE + lane;
-            uint32_t k[EACH];
-            uint64_t q[EACH], x = 0;
-            if (c < row.pieces) row.keys(c, k);
-            else
-#pragma unroll
-                for (int j = 0; j < EACH; ++j) k[j] = KEY_BARRED;
-#pragma unroll
-            for (int j = 0; j < EACH; ++j) { q[j] = k[j] > KEY_BARRED ? mass(k[j], row.index(c, j)) : 0; x += q[j]; }
-            uint64_t sum = x;
-#pragma unroll
-            for (int d = 1; d < HX_WAVE; d <<= 1) {
-                const uint64_t y = __shfl_up(sum, d);
-                if (lane >= d) sum += y;
-            }
-            uint64_t run = before + sum - x;
+            const int c0 = (at / steps) * row.per + (at % steps) * SA_STEP;
             int found = -1;
+#pragma unroll 1
+            for (int i = 0; i < SA_UNROLL && found < 0; ++i) {
+                const int c = c0 + i * HX_WAVE + lane;
+                uint32_t p[4];
+                uint64_t q[EACH], y = 0;
+                row.load_any(c, p);
 #pragma unroll
-            for (int j = 0; j < EACH; ++j) {
-                run += q[j];
-                if (found < 0 && run > want) found = row.index(c, j);
+                for (int j = 0; j < EACH; ++j) {
+                    bool in;
+                    q[j] = mass(row.key(p, j), row.index(c, j), &in);
+                    y += q[j];
+                }
+                const uint64_t sum = wave_scan(y);
+                uint64_t run = before + sum - y;
+                int here = -1;
+#pragma unroll
+                for (int j = 0; j < EACH; ++j) {
+                    run += q[j];
+                    if (here < 0 && run > want) here = row.index(c, j);
+                }
+                const unsigned long long m = __builtin_amdgcn_ballot_w64(here >= 0);
+                if (m) found = __shfl(here, __builtin_ctzll(m));
+                before += __shfl(sum, 63);
             }
-            const unsigned long long m = __builtin_amdgcn_ballot_w64(found >= 0);
-            if (m && lane == __builtin_ctzll(m)) s.r32[0] = found;
+            if (lane == 0) s.r32[0] = found;
         }
         if (lane == 0) s.r64[0] = all;
     }
     __syncthreads();
     const int got = s.r32[0];
     *total = s.r64[0];
+    int n = 0;
+    for (int i = 0; i < SA_WAVES; ++i) n += s.wmin[i];
+    *count = n;
     __syncthreads();
     return got;
 }
 
+// Of sums in order, EACH of a thread's beside each other, the one at which the whole exceeds or reaches `limit`: b < limit <= b + x.
+// Its number in s.r32[1] (-1: none), what is before it in s.r64[0].  want(total) gives the limit the first time.
+template <int EACH, typename W>
+__device__ __forceinline__ void crossing(Shared &s, const uint64_t *x, uint64_t before, uint64_t *limit, bool first, W want)
+{
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    uint64_t own = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) own += x[i];
+    const uint64_t sum = wave_scan(own);
+    if (lane == 63) s.wave[w] = sum;
+    if (tid == 0) s.r32[1] = -1;
+    __syncthreads();
+    uint64_t b = before + sum - own, all = 0;
+#pragma unroll
+    for (int i = 0; i < SA_WAVES; ++i) {
+        b += i < w ? s.wave[i] : 0;
+        all += s.wave[i];
+    }
+    if (first) *limit = want(all);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        if (b < *limit && *limit <= b + x[i]) { s.r32[1] = tid * EACH + i; s.r64[0] = b; }
+        b += x[i];
+    }
+    __syncthreads();
+}
+
 // The last element that stays of those for which `in` holds, in the order (logit falling, number rising): the one at which the sum of
-// `mass` reaches want(total).  false: all stay, or none is there.
-template <typename E, typename I, typename M, typename W>
-__device__ bool find_limit(const Row<E> &row, Shared &s, float top, float reach, I in, M mass, W want, Limit *out)
+// their weights (count_them: their number) reaches want(total).  EQUALS: the first *stay of those with the key are the last ones that stay.
+enum Found { ALL_STAY, LAST_FOUND, EQUALS };
+template <typename E, typename W>
+__device__ __forceinline__ Found find_limit(const Row<E> &row, Shared &s, const Weights &wt, bool count_them, const Limit in, W want, Limit *out, uint64_t *stay)
 {
     constexpr int EACH = Row<E>::EACH;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    // first bins: by how far a logit lies below the largest, the last for all that lie beyond `reach`
-    const float unit = reach > 0.0f ? (SA_BINS - 1) / reach : 0.0f;
+    auto mass = [&](uint32_t k) -> uint64_t { return count_them ? 1 : wt.mass(k); };
     uint32_t k_low = KEY_BARRED + 1, k_high = 0xffffffffu;       // keys still in question
-    int shift = -1;                                              // -1: first bins; else bins of (k_high - key) >> shift
+    int shift = -1;                                              // -1: the weights' bins; else bins of (k_high - key) >> shift
     uint64_t before = 0, limit = 0;
-    auto bin_of = [&](uint32_t k) {
-        if (shift >= 0) return (int)((k_high - k) >> shift);
-        const float d = fminf((top - of_key(k)) * unit, (float)(SA_BINS - 1));
-        return of_key(k) == top ? 0 : (int)d;
-    };
     for (bool first = true;; first = false) {
         __syncthreads();
         for (int i = tid; i < SA_BINS * SA_COLS; i += SA_THREADS) s.hist[i] = 0;
-        __syncthreads();
-        row.each([&](int c, const uint32_t *k, int) {
-#pragma unroll
-            for (int j = 0; j < EACH; ++j)
-                if (k[j] >= k_low && k[j] <= k_high && in(k[j], row.index(c, j)))
-                    if (const uint64_t x = mass(k[j])) atomicAdd((unsigned long long *)&s.hist[bin_of(k[j]) * SA_COLS + (lane & (SA_COLS - 1))], (unsigned long long)x);
-        });
-        __syncthreads();
-        // a thread a bin adds its places up, the first wavefront then the bins
-        if (tid < SA_BINS) {
-            uint64_t x = 0;
-            for (int i = 0; i < SA_COLS; ++i) x += s.hist[tid * SA_COLS + ((i + tid) & (SA_COLS - 1))];
-            s.mass[tid] = x;
-        }
-        __syncthreads();
-        if (w == 0) {
-            const uint64_t x0 = s.mass[2 * lane], x1 = s.mass[2 * lane + 1];
-            uint64_t sum = x0 + x1;
-#pragma unroll
-            for (int d = 1; d < HX_WAVE; d <<= 1) {
-                const uint64_t y = __shfl_up(sum, d);
-                if (lane >= d) sum += y;
-            }
-            const uint64_t all = __shfl(sum, 63);
-            uint64_t lim = limit;
-            if (first) lim = want(all);
-            const uint64_t b0 = before + sum - x0 - x1, b1 = b0 + x0;
-            if (lane == 0) { s.r32[1] = -1; s.r64[1] = lim; }
-            if (b0 < lim && lim <= b0 + x0) { s.r32[1] = 2 * lane; s.r64[0] = b0; }
-            if (b1 < lim && lim <= b1 + x1) { s.r32[1] = 2 * lane + 1; s.r64[0] = b1; }
-        }
         if (tid == 0) s.r32[2] = 0;
         __syncthreads();
+        row.each([&](int c, const uint32_t *p) {
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+                const uint32_t k = row.key(p, j);
+                const bool mine = k >= k_low && k <= k_high && in.holds(k, row.index(c, j));
+                if (__builtin_amdgcn_ballot_w64(mine)) {
+                    int b;
+                    uint64_t x = 1;
+                    if (count_them) b = wt.bin(k);
+                    else x = Weights::whole(wt.scaled(k, &b));
+                    if (shift >= 0) b = (int)((k_high - k) >> shift);
+                    if (mine && x) atomicAdd((unsigned long long *)&s.hist[b * SA_COLS + (lane & (SA_COLS - 1))], (unsigned long long)x);
+                }
+            }
+        });
+        __syncthreads();
+        {
+            uint64_t x[2] = {0, 0};
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (2 * tid + i < SA_BINS)
+#pragma unroll
+                    for (int j = 0; j < SA_COLS; ++j) x[i] += s.hist[(2 * tid + i) * SA_COLS + j];
+            crossing<2>(s, x, before, &limit, first, want);
+        }
         const int bin = s.r32[1];
-        limit = s.r64[1];
-        if (bin < 0) return false;
+        if (bin < 0) return ALL_STAY;
         before = s.r64[0];
         // the elements of that bin
         uint32_t lo = 0xffffffffu, hi = 0;
-        row.each([&](int c, const uint32_t *k, int) {
+        row.each([&](int c, const uint32_t *p) {
 #pragma unroll
-            for (int j = 0; j < EACH; ++j)
-                if (k[j] >= k_low && k[j] <= k_high && in(k[j], row.index(c, j)) && bin_of(k[j]) == bin)
-                    if (const uint64_t x = mass(k[j])) {
-                        lo = k[j] < lo ? k[j] : lo;
-                        hi = k[j] > hi ? k[j] : hi;
-                        const int at = atomicAdd(&s.r32[2], 1);
-                        if (at < SA_LIST) { s.key[at] = k[j]; s.idx[at] = row.index(c, j); s.mass[at] = x; }
-                    }
+            for (int j = 0; j < EACH; ++j) {
+                const uint32_t k = row.key(p, j);
+                if (k >= k_low && k <= k_high && (shift >= 0 ? (int)((k_high - k) >> shift) : wt.bin(k)) == bin && in.holds(k, row.index(c, j))) {
+                    lo = k < lo ? k : lo;
+                    hi = k > hi ? k : hi;
+                    const int at = atomicAdd(&s.r32[2], 1);
+                    if (at < SA_LIST) { s.lkey[at] = k; s.lidx[at] = row.index(c, j); }
+                }
+            }
         });
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) {
@@ -304,38 +437,78 @@ __device__ bool find_limit(const Row<E> &row, Shared &s, float top, float reach,
             lo = a < lo ? a : lo;
             hi = b > hi ? b : hi;
         }
-        if (lane == 0) { s.wmin[w] = lo; s.wmax[w] = hi; }
+        if (lane == 0) { s.wmin[w] = (int)lo; s.wmax[w] = (int)hi; }
         __syncthreads();
-        const int count = s.r32[2];
+        int count = s.r32[2];
         for (int i = 0; i < SA_WAVES; ++i) {
-            lo = s.wmin[i] < lo ? s.wmin[i] : lo;
-            hi = s.wmax[i] > hi ? s.wmax[i] : hi;
+            lo = (uint32_t)s.wmin[i] < lo ? (uint32_t)s.wmin[i] : lo;
+            hi = (uint32_t)s.wmax[i] > hi ? (uint32_t)s.wmax[i] : hi;
         }
         if (count <= SA_LIST) {
-            if (tid < count) {
-                const uint32_t k = s.key[tid];
-                const int i = s.idx[tid];
-                uint64_t b = before;
-                for (int j = 0; j < count; ++j) {
-                    const uint32_t kj = s.key[j];
-                    b += kj > k || (kj == k && s.idx[j] < i) ? s.mass[j] : 0;
+            // in finer and finer bins until few are left of the list
+            const int n = count;
+            while (count > SA_FEW && lo != hi) {
+                int sh = 0;
+                while (((hi - lo) >> sh) >= SA_THREADS) ++sh;
+                __syncthreads();
+                s.hist[tid] = 0;
+                if (tid == 0) s.r32[2] = 0;
+                __syncthreads();
+                for (int i = tid; i < n; i += SA_THREADS) {
+                    const uint32_t k = s.lkey[i];
+                    if (k >= lo && k <= hi) atomicAdd((unsigned long long *)&s.hist[(hi - k) >> sh], (unsigned long long)mass(k));
                 }
-                if (b < limit && limit <= b + s.mass[tid]) { s.r32[3] = i; s.r64[0] = k; }
+                __syncthreads();
+                const uint64_t x[1] = {s.hist[tid]};
+                crossing<1>(s, x, before, &limit, false, want);
+                const int b = s.r32[1];
+                before = s.r64[0];
+                const uint32_t top = hi - ((uint32_t)b << sh);
+                const uint64_t floor_ = (uint64_t)((uint32_t)b + 1) << sh;         // of hi - key in the bins up to this one
+                lo = hi - lo >= floor_ ? hi - (uint32_t)floor_ + 1 : lo;
+                hi = top;
+                int mine = 0;
+                for (int i = tid; i < n; i += SA_THREADS) mine += s.lkey[i] >= lo && s.lkey[i] <= hi;
+#pragma unroll
+                for (int d = 32; d > 0; d >>= 1) mine += __shfl_xor(mine, d);
+                if (lane == 0 && mine) atomicAdd(&s.r32[2], mine);
+                __syncthreads();
+                count = s.r32[2];
             }
-            __syncthreads();
-            out->key = (uint32_t)s.r64[0];
-            out->idx = s.r32[3];
-            __syncthreads();
-            return true;
+            if (count <= SA_FEW) {
+                __syncthreads();
+                if (tid == 0) s.r32[2] = 0;
+                __syncthreads();
+                uint64_t *fm = s.hist;
+                uint32_t *fk = (uint32_t *)(s.hist + SA_FEW);
+                int *fi = (int *)(s.hist + 2 * SA_FEW);
+                for (int i = tid; i < n; i += SA_THREADS) {
+                    const uint32_t k = s.lkey[i];
+                    if (k >= lo && k <= hi) {
+                        const int at = atomicAdd(&s.r32[2], 1);
+                        fk[at] = k; fi[at] = s.lidx[i]; fm[at] = mass(k);
+                    }
+                }
+                __syncthreads();
+                if (tid < count) {
+                    const uint32_t k = fk[tid];
+                    const int i = fi[tid];
+                    uint64_t b = before;
+                    for (int j = 0; j < count; ++j) b += fk[j] > k || (fk[j] == k && fi[j] < i) ? fm[j] : 0;
+                    if (b < limit && limit <= b + fm[tid]) { s.r32[3] = i; s.r64[1] = k; }
+                }
+                __syncthreads();
+                out->key = (uint32_t)s.r64[1];
+                out->idx = s.r32[3];
+                __syncthreads();
+                return LAST_FOUND;
+            }
         }
         if (lo == hi) {
-            // all equal: the first so many by their numbers
-            const uint64_t x = mass(lo), stay = (limit - before + x - 1) / x;
-            uint64_t all;
+            const uint64_t x = mass(lo);
+            *stay = (limit - before + x - 1) / x;
             out->key = lo;
-            out->idx = locate(row, s, [&](uint32_t k, int i) -> uint64_t { return k == lo && in(k, i); },
-                              [&](uint64_t) -> uint64_t { return stay - 1; }, &all);
-            return true;
+            return EQUALS;
         }
         k_low = lo;
         k_high = hi;
@@ -347,7 +520,7 @@ __device__ bool find_limit(const Row<E> &row, Shared &s, float top, float reach,
 template <typename E>
 __global__ __launch_bounds__(SA_THREADS) void hx_sample_kernel(SampleArgs a)
 {
-    constexpr int EACH = Row<E>::EACH;
+    using R = Raw<E>;
     __shared__ Shared s;
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     Row<E> row;
@@ -357,43 +530,64 @@ __global__ __launch_bounds__(SA_THREADS) void hx_sample_kernel(SampleArgs a)
     const int k = a.top_k ? a.top_k[r] : 0;
     const bool fine = !is_nan(T) && !is_nan(p) && !is_nan(mp) && !is_nan(u) && T >= 0.0f && __float_as_uint(T) != 0x7f800000u && mp >= 0.0f && mp <= 1.0f &&
                       u >= 0.0f && u < 1.0f;
+    if (tid < 32) s.tab[tid] = exp2((double)tid / 32.0);
 
-    // the largest and the least logit that are not barred
-    uint32_t hi = 0, lo = 0xffffffffu;
-    bool nan = false;
-    row.each([&](int c, const uint32_t *kk, int) {
+    // the largest logit; a NaN of either sign lies beyond the infinities in the order of the bits
+    constexpr bool WIDE = sizeof(E) == 4;
+    int hi = WIDE ? (int)0x80000000 : (int)0x80008000, lo = WIDE ? 0x7fffffff : 0x7fff7fff;
+    row.each([&](int, const uint32_t *piece) { R::extremes(piece, hi, lo); });
+    if constexpr (!WIDE) {
+        const int h0 = (short)hi, h1 = hi >> 16, l0 = (short)lo, l1 = lo >> 16;
+        hi = h0 > h1 ? h0 : h1;
+        lo = l0 < l1 ? l0 : l1;
+    }
+    auto over_all = [&](int &most, int &least) {
 #pragma unroll
-        for (int j = 0; j < EACH; ++j) {
-            hi = kk[j] > hi ? kk[j] : hi;
-            lo = kk[j] > KEY_BARRED && kk[j] < lo ? kk[j] : lo;
+        for (int d = 32; d > 0; d >>= 1) {
+            const int x = __shfl_xor(most, d), y = __shfl_xor(least, d);
+            most = x > most ? x : most;
+            least = y < least ? y : least;
         }
-    });
-    // a NaN is told by its bits
-    {
-        const int lane_c0 = w * row.per + lane;
-        for (int it = 0; it < row.per; it += HX_WAVE) {
-            const int c = lane_c0 + it;
-            for (int j = 0; j < EACH; ++j) {
-                const int i = row.index(c, j);
-                if (c < row.pieces && i >= 0 && i < row.n) nan |= is_nan(to_float(row.p[i]));
+        __syncthreads();
+        if (lane == 0) { s.wmax[w] = most; s.wmin[w] = least; }
+        __syncthreads();
+        for (int i = 0; i < SA_WAVES; ++i) {
+            most = s.wmax[i] > most ? s.wmax[i] : most;
+            least = s.wmin[i] < least ? s.wmin[i] : least;
+        }
+    };
+    over_all(hi, lo);
+    uint32_t top_key;
+    if (hi > R::INF || lo < ~R::INF) {
+        row.nans = true;
+        if (tid == 0) hx_raise(a.status, HX_ERR_INVALID_ARG);
+        int most = 0, least = 0;                             // of the keys, shifted into the signed range
+        row.each([&](int, const uint32_t *piece) {
+#pragma unroll
+            for (int j = 0; j < R::EACH; ++j) {
+                const int x = (int)(row.key(piece, j) >> 1);
+                most = x > most ? x : most;
             }
-        }
-    }
-    if (nan || (!fine && tid == 0)) hx_raise(a.status, HX_ERR_INVALID_ARG);
+        });
+        over_all(most, least);
+        // the last bit is lost: it is the same for all but full-precision logits, where it is looked for
+        uint32_t best = 0;
+        row.each([&](int, const uint32_t *piece) {
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        const uint32_t x = __shfl_xor(hi, d), y = __shfl_xor(lo, d);
-        hi = x > hi ? x : hi;
-        lo = y < lo ? y : lo;
-    }
-    if (lane == 0) { s.wmax[w] = hi; s.wmin[w] = lo; }
+            for (int j = 0; j < R::EACH; ++j) {
+                const uint32_t x = row.key(piece, j);
+                if ((int)(x >> 1) == most && x > best) best = x;
+            }
+        });
+        int odd = (int)(best & 1);
+        if (best == 0) odd = 0;
+        least = 0;
+        over_all(odd, least);
+        top_key = (uint32_t)most << 1 | (uint32_t)odd;
+    } else top_key = key_of(R::of_order(hi));
     __syncthreads();
-    for (int i = 0; i < SA_WAVES; ++i) {
-        hi = s.wmax[i] > hi ? s.wmax[i] : hi;
-        lo = s.wmin[i] < lo ? s.wmin[i] : lo;
-    }
-    __syncthreads();
-    if (!fine || hi <= KEY_BARRED) {
+    if (!fine && tid == 0) hx_raise(a.status, HX_ERR_INVALID_ARG);
+    if (!fine || top_key <= KEY_BARRED) {
         if (tid == 0) {
             a.token[r] = -1;
             if (a.logprob) a.logprob[r] = -__builtin_inff();
@@ -401,10 +595,52 @@ __global__ __launch_bounds__(SA_THREADS) void hx_sample_kernel(SampleArgs a)
         }
         return;
     }
-    const float top = of_key(hi);
+    const Weights wt{(double)of_key(top_key), 46.16624130844683 / (double)T, s.tab, a.qbits, top_key == 0xff800000u, top_key};
+    const double min_w = __builtin_ldexp((double)mp, a.qbits);
+    Limit lim{KEY_BARRED + 1, 0x7fffffff};                 // all that are not barred
     uint64_t all;
+    int kept, t = -1;
+    enum { TOP_K, TOP_P, TOKEN };
+    for (int step = T == 0.0f ? TOKEN : TOP_K;; ++step) {
+        // equal_key: elements of this key count 1 and no others; else the weights of all that stay
+        bool equal = step == TOKEN && T == 0.0f;
+        uint32_t equal_key = top_key;
+        uint64_t stay = 1;
+        if (step != TOKEN) {
+            if (step == TOP_K ? k <= 0 || k >= a.n_vocab : p >= 1.0f) continue;
+            const bool count_them = step == TOP_K;
+            const Found found = find_limit(row, s, wt, count_them, lim, [&](uint64_t n) -> uint64_t {
+                if (count_them) return (uint64_t)k < n ? (uint64_t)k : ~0ull;
+                if (p <= 0.0f) return 1;
+                bool rest;
+                const uint64_t x = scaled(p, n, &rest) + rest;           // rounded up
+                return x ? x : 1;
+            }, &lim, &stay);
+            if (found != EQUALS) continue;
+            equal = true;
+            equal_key = lim.key;
+        }
+        t = locate(row, s, [&](uint32_t kk, int i, bool *in) -> uint64_t {
+            if (equal) { *in = kk == equal_key; return *in; }
+            const bool held = kk > KEY_BARRED && lim.holds(kk, i);
+            *in = false;
+            uint64_t x = 0;
+            if (__builtin_amdgcn_ballot_w64(held)) {
+                int b;
+                const double y = wt.scaled(kk, &b);
+                *in = held && y >= min_w;
+                x = *in ? Weights::whole(y) : 0;
+            }
+            return x;
+        }, [&](uint64_t n) -> uint64_t {
+            if (equal) return stay - 1;
+            bool rest;
+            return scaled(u, n, &rest);
+        }, &all, &kept);
+        if (step == TOKEN) break;
+        lim.idx = t;
+    }
     if (T == 0.0f) {
-        const int t = locate(row, s, [&](uint32_t kk, int) -> uint64_t { return kk == hi; }, [](uint64_t) -> uint64_t { return 0; }, &all);
         if (tid == 0) {
             a.token[r] = t;
             if (a.logprob) a.logprob[r] = 0.0f;
@@ -412,58 +648,12 @@ __global__ __launch_bounds__(SA_THREADS) void hx_sample_kernel(SampleArgs a)
         }
         return;
     }
-    const bool boundless = hi == 0xff800000u;              // +infinity takes all the weight
-    const double inv = 1.4426950408889634 / (double)T, one = __builtin_ldexp(1.0, a.qbits);
-    auto weight = [&](uint32_t kk) -> double {
-        if (boundless) return kk == hi ? 1.0 : 0.0;
-        return exp2_neg(((double)of_key(kk) - (double)top) * inv);
-    };
-    auto whole = [&](double x) -> uint64_t { return (uint64_t)(x * one + 0.5); };
-
-    Limit lim{KEY_BARRED + 1, 0x7fffffff};                 // all that are not barred
-    const float span = top - of_key(lo);
-    if (k > 0)
-        find_limit(row, s, top, fminf(span, 32.0f), [](uint32_t, int) { return true; }, [](uint32_t) -> uint64_t { return 1; },
-                   [&](uint64_t n) -> uint64_t { return (uint64_t)k < n ? (uint64_t)k : ~0ull; }, &lim);
-    if (p < 1.0f) {
-        const Limit of = lim;
-        find_limit(row, s, top, fminf(span, 40.0f * T), [&](uint32_t kk, int i) { return of.holds(kk, i); }, [&](uint32_t kk) { return whole(weight(kk)); },
-                   [&](uint64_t n) -> uint64_t {
-                       if (p <= 0.0f) return 1;
-                       bool rest;
-                       const uint64_t x = scaled(p, n, &rest) + 1;       // one more than the floor ..
-                       const uint64_t up = rest ? x : x - 1;             // .. unless nothing was cut off
-                       return up ? up : 1;
-                   }, &lim);
-    }
-    const double min_w = mp;
-    const int t = locate(row, s, [&](uint32_t kk, int i) -> uint64_t {
-        if (!lim.holds(kk, i)) return 0;
-        const double x = weight(kk);
-        return x >= min_w ? whole(x) : 0;
-    }, [&](uint64_t n) -> uint64_t { bool rest; return scaled(u, n, &rest); }, &all);
-    if (tid == 0) a.token[r] = t;
-    if (a.n_kept || a.logprob) {
-        int mine = 0;
-        if (a.n_kept)
-            row.each([&](int c, const uint32_t *kk, int) {
-#pragma unroll
-                for (int j = 0; j < EACH; ++j) mine += kk[j] > KEY_BARRED && lim.holds(kk[j], row.index(c, j)) && (min_w <= 0.0 || weight(kk[j]) >= min_w);
-            });
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) mine += __shfl_xor(mine, d);
-        __syncthreads();
-        if (lane == 0) s.wmin[w] = (uint32_t)mine;
-        __syncthreads();
-        if (tid == 0) {
-            int n = 0;
-            for (int i = 0; i < SA_WAVES; ++i) n += (int)s.wmin[i];
-            if (a.n_kept) a.n_kept[r] = n;
-            if (a.logprob) {
-                const float x = to_float(row.p[t]);
-                const double d = boundless ? 0.0 : ((double)x - (double)top) / (double)T;
-                a.logprob[r] = (float)(d - (log((double)all) - a.qbits * 0.6931471805599453));
-            }
+    if (tid == 0) {
+        a.token[r] = t;
+        if (a.n_kept) a.n_kept[r] = kept;
+        if (a.logprob) {
+            const double d = wt.boundless ? 0.0 : ((double)to_float(row.p[t]) - wt.top) / (double)T;
+            a.logprob[r] = (float)(d - (log((double)all) - a.qbits * 0.6931471805599453));
         }
     }
 }
@@ -487,7 +677,8 @@ extern "C" int hx_sample(hx_ctx *ctx, int32_t n_rows, int32_t n_vocab, int32_t d
     hipStream_t stream = (hipStream_t)stream_;
     int bits = 0;
     while (((int64_t)1 << bits) < n_vocab) ++bits;
-    SampleArgs a{n_rows, n_vocab, 62 - bits - 1, logits, row_stride, temperature, top_k, top_p, min_p, u, token, logprob, n_kept, ctx->d_status};
+    const int q = 61 - bits < 50 ? 61 - bits : 50;
+    SampleArgs a{n_rows, n_vocab, q, logits, row_stride, temperature, top_k, top_p, min_p, u, token, logprob, n_kept, ctx->d_status};
     if (dtype == HX_F32) hx_sample_kernel<float><<<n_rows, SA_THREADS, 0, stream>>>(a);
     else if (dtype == HX_BF16) hx_sample_kernel<__bf16><<<n_rows, SA_THREADS, 0, stream>>>(a);
     else hx_sample_kernel<_Float16><<<n_rows, SA_THREADS, 0, stream>>>(a);
