@@ -4,6 +4,8 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -56,6 +58,15 @@ def _marshal_command():
 
 
 def _compile(cmd, verbose, out=None) -> str:
+    """Runs a compiler command; one of several HIP sources as a command each, side by side, and one that links them."""
+    sources = [x for x in cmd if x.endswith(".hip")]
+    if len(sources) > 1:
+        with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+            rest = [x for x in cmd if x not in sources and x != "-shared"]
+            at = rest.index("-o")
+            objects = [os.path.join(tmp, os.path.basename(x) + ".o") for x in sources]
+            list(pool.map(lambda so: _compile([*rest[:at], "-c", "-o", so[1], so[0]], verbose), zip(sources, objects)))
+            return _compile([*rest[:at], "-shared", "-o", rest[at + 1], *objects], verbose, out)
     if verbose:
         print(" ".join(cmd))
     run = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)

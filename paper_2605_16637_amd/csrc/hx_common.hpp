@@ -57,7 +57,7 @@ struct hx_ctx {
     size_t dtl_cap = 0;
     float *d_dtab = nullptr;               // decode-stage first-room tables, dtab_cap instances
     int dtab_cap = 0;
-    HxScratch kv, att, smp;                // the serving step: pages (hx_kv.hip), attention (hx_attend.hip), sampling (hx_sample.hip)
+    HxScratch kv, att, att_done, smp;      // the serving step: pages (hx_kv.hip), attention (hx_attend.hip; its counters, 0 between launches), sampling (hx_sample.hip)
     int num_cu = 256;
     HxDagStore dag;
 };

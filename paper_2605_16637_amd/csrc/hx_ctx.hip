@@ -440,6 +440,7 @@ extern "C" int hx_ctx_destroy(hx_ctx *ctx)
     if (ctx->d_rkey) (void)hipFree(ctx->d_rkey);
     hx_scratch_release(ctx->kv);
     hx_scratch_release(ctx->att);
+    hx_scratch_release(ctx->att_done);
     hx_scratch_release(ctx->smp);
     delete ctx;
     return HX_OK;
