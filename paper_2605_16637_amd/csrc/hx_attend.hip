@@ -1,1079 +1,10 @@
-// Attention of a few or many queries over cached pages: sliding windows with sinks, trees of drafted tokens.
-//
-// One pass over the keys with a running maximum and sum.  The products are taken transposed, S^T = K Q^T and O^T = V^T P^T: a
-// lane then holds one query's scores, its maximum needs one exchange between the two halves of the wavefront, the running
-// maximum scales a lane's own accumulators, and the weights leave the first product in the very registers that the second wants them
-// in (the order in which keys are summed is free, so the second product takes them in the first's order and the
-// values are read from LDS in that order, transposed on the way).
-#include "hx_serve.hpp"
-
-#include <type_traits>
-
-namespace {
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-
-template <typename E> struct Types;
-template <> struct Types<__bf16> { using x8 = bf16x8; using x4 = bf16x4; using x2 = bf16x2; };
-template <> struct Types<_Float16> { using x8 = f16x8; using x4 = f16x4; using x2 = f16x2; };
-
-__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
-
-// 4 stored numbers of 8 bits; every e4m3 is a bf16 and an fp16 exactly
-__device__ __forceinline__ void widen(uint32_t w, bf16x2 &a, bf16x2 &b)
-{
-    a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false);
-    b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
-}
-__device__ __forceinline__ void widen(uint32_t w, f16x2 &a, f16x2 &b)
-{
-    a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false);
-    b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true);
-}
-
-constexpr float NEG_INF = -__builtin_inff();
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr float MAX_SLACK = 8.0f;            // a running maximum is raised when a score exceeds it by this many powers of 2
-
-struct AttendArgs {
-    KvView kv;
-    int layer, n;
-    const int32_t *row, *q_ptr;
-    int n_q, max_q, n_heads, group;
-    const void *q;
-    int64_t q_token, q_head;
-    void *out;
-    int64_t out_token, out_head;
-    float *lse;
-    float scale;
-    int window, n_sink;
-    const int32_t *parent;
-    const float *k_scale, *v_scale;
-    bool q_wide, out_wide;       // q can be read 16 bytes at a time, out written 8
-    int row_tiles, splits;       // parts of a row tile's keys, at most
-    int chunk;                   // tiles of keys of a part
-    int *done;                   // [pair][row tile] parts that are written; 0 between launches
-    float *part;                 // [workgroup][rows][dim], when splits > 1
-    float2 *part_ml;             // [workgroup][rows] maximum (of s log2 e) and sum
-};
-
-constexpr int AT_THREADS = 256;
-constexpr int MAX_SPLITS = 64;
-
-// one value of the other half of the wavefront
-__device__ __forceinline__ float other_half(float x)
-{
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(threadIdx.x & 32 ? r[0] : r[1]);
-}
-
-// A sequence and its queries.
-struct Seq {
-    int q0, nq, len, base;       // base: the position of the first query's token
-    bool there, ok;              // queries lie within the call's; the rest is in range too
-    const int32_t *table;
-};
-
-__device__ __forceinline__ Seq sequence(const AttendArgs &a, int i)
-{
-    const KvView &kv = a.kv;
-    Seq s;
-    s.q0 = a.q_ptr[i];
-    const int q1 = a.q_ptr[i + 1], r = a.row ? a.row[i] : i;
-    s.nq = q1 - s.q0;
-    s.there = s.q0 >= 0 && q1 >= s.q0 && q1 <= a.n_q;
-    s.ok = s.there && r >= 0 && r < kv.rows && s.nq <= a.max_q;
-    s.len = s.ok ? kv.len[r] : 0;
-    s.ok = s.ok && hx_row_ok(kv, r, s.len) && s.nq <= s.len;
-    s.base = s.len - s.nq;
-    s.table = hx_row(kv, s.ok ? r : 0);
-    return s;
-}
-
-constexpr int ANC_WORDS = HX_MAX_DRAFTS / 32;
-constexpr int TREE_BYTES = HX_MAX_DRAFTS * 4 * (1 + ANC_WORDS);
-
-// Every draft's depth (-1: left out) and the bits of the drafts above it; s_parent: HX_MAX_DRAFTS words that are free yet.
-__device__ __forceinline__ void plant(const AttendArgs &a, const Seq &q, int *s_parent, int *s_depth, uint32_t *s_anc)
-{
-    const int tid = threadIdx.x;
-    if (tid < q.nq) s_parent[tid] = a.parent[q.q0 + tid];
-    __syncthreads();
-    if (tid < q.nq) {
-        uint32_t mine[ANC_WORDS] = {};
-        int depth = 0, at = tid;
-        while (at >= 0) {
-#pragma unroll
-            for (int w = 0; w < ANC_WORDS; ++w) mine[w] |= at >> 5 == w ? 1u << (at & 31) : 0u;
-            const int up = s_parent[at];
-            if (up >= at || up < -2) { hx_raise(a.kv.status, HX_ERR_INDEX); at = -2; break; }
-            at = up;
-            ++depth;
-        }
-        s_depth[tid] = at == -2 ? -1 : depth - 1;
-#pragma unroll
-        for (int w = 0; w < ANC_WORDS; ++w) s_anc[tid * ANC_WORDS + w] = mine[w];
-    }
-    __syncthreads();
-}
-
-// The tiles of KT keys that some of the queries t_first .. t_last may see: the first sink_tiles, then those from lo_tile on.
-struct Extent {
-    int lo, hi, sink_tiles, lo_tile, n;
-};
-
-template <int KT>
-__device__ __forceinline__ Extent extent(const AttendArgs &a, const Seq &q, int t_first, int t_last)
-{
-    const bool tree = a.parent != nullptr;
-    Extent x{0, 0, 0, 0, 0};
-    if (!q.ok) return x;
-    x.hi = tree ? q.len : q.base + t_last + 1;
-    if (a.window > 0) {
-        const int first_pos = tree ? q.base - 1 : q.base + t_first;         // the least position of a query
-        x.lo = first_pos - a.window + 1;
-        x.lo = x.lo > 0 ? x.lo : 0;
-        if (tree && x.lo > q.base) x.lo = q.base;
-    }
-    x.lo_tile = x.lo / KT;
-    if (x.lo > 0) {
-        const int sinks = a.n_sink < x.lo ? a.n_sink : x.lo;
-        x.sink_tiles = (sinks + KT - 1) / KT;
-        if (x.sink_tiles >= x.lo_tile) { x.sink_tiles = 0; x.lo_tile = 0; }
-    }
-    x.n = x.hi > 0 ? x.sink_tiles + (x.hi + KT - 1) / KT - x.lo_tile : 0;
-    return x;
-}
-
-// Parts of n tiles: of `chunk` each, the last takes what is left.
-__device__ __forceinline__ int parts_of(const AttendArgs &a, int n)
-{
-    const int parts = n > a.chunk ? (n + a.chunk - 1) / a.chunk : 1;
-    return parts < a.splits ? parts : a.splits;
-}
-
-// What a lane's query sees.
-struct Sight {
-    bool tree, alive;
-    int pos, t, base, nq, window, n_sink;
-    const int *s_depth;
-    const uint32_t *s_anc;
-    __device__ __forceinline__ bool sees(int y) const
-    {
-        bool see = alive;
-        int ypos = y;
-        if (tree && y >= base) {
-            const int d = y - base;
-            const bool in = d < nq;
-            see = see && in && ((s_anc[t * ANC_WORDS + ((in ? d : 0) >> 5)] >> (d & 31)) & 1);
-            ypos = base + s_depth[in ? d : 0];
-        }
-        return see && ypos <= pos && (window <= 0 || ypos < n_sink || pos - ypos < window);
-    }
-};
-
-__device__ __forceinline__ Sight sight(const AttendArgs &a, const Seq &q, int t, const int *s_depth, const uint32_t *s_anc)
-{
-    Sight v;
-    v.tree = a.parent != nullptr;
-    v.alive = q.ok && t < q.nq;
-    v.t = v.alive ? t : 0;
-    v.pos = q.base + t;
-    if (v.tree && v.alive) {
-        const int d = s_depth[t];
-        v.alive = d >= 0;
-        v.pos = q.base + d;
-    }
-    v.base = q.base; v.nq = q.nq; v.window = a.window; v.n_sink = a.n_sink; v.s_depth = s_depth; v.s_anc = s_anc;
-    return v;
-}
-
-template <typename E>
-__device__ __forceinline__ void put(E *to, bool wide, float a, float b, float c, float d)
-{
-    typename Types<E>::x4 y;
-    y[0] = (E)a; y[1] = (E)b; y[2] = (E)c; y[3] = (E)d;
-    if (wide) *(typename Types<E>::x4 *)to = y;
-    else
-#pragma unroll
-        for (int j = 0; j < 4; ++j) to[j] = y[j];
-}
-
-// What workgroups leave for each other goes past the caches that they do not share: device-scope stores and loads, of 8 bytes.
-__device__ __forceinline__ void leave(float *to, float x, float y)
-{
-    const uint64_t v = (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x);
-    __hip_atomic_store((uint64_t *)to, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 find(const float *from)
-{
-    const uint64_t v = __hip_atomic_load((const uint64_t *)from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
-}
-
-// The parts of a row tile put together by the workgroup that wrote the last of them.  Each workgroup writes its part, waits until
-// it is written, and counts; who counts last reads all.  s: (2 parts + 1) ROWS floats; the others return.
-template <typename E, int D, int ROWS>
-__device__ __forceinline__ void join(const AttendArgs &a, const Seq &q, int pair, int rt, int parts, float *s)
-{
-    __shared__ int s_last;
-    const int tid = threadIdx.x;
-    const int64_t tile = (int64_t)pair * a.row_tiles + rt;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tid == 0) {
-        const int before = atomicAdd(a.done + tile, 1);
-        s_last = before == parts - 1;
-        if (s_last) __hip_atomic_store(a.done + tile, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    __syncthreads();
-    if (!s_last) return;
-    const int head = pair % a.kv.n_heads;
-    const int64_t slot0 = tile * a.splits * ROWS;
-    const int rows_left = q.nq * a.group - rt * ROWS, rows = rows_left < ROWS ? rows_left : ROWS;
-    const float v_unit = a.v_scale ? a.v_scale[a.layer * a.kv.n_heads + head] : 1.0f;
-    // all parts' maxima and sums at once, then the factor of each part for each row
-    float *s_l = s + (parts + 1) * ROWS;
-    for (int u = tid; u < parts * rows; u += AT_THREADS) {
-        const int p = u / rows, r = u % rows;
-        const float2 ml = find((const float *)(a.part_ml + slot0 + (int64_t)p * ROWS + r));
-        s[p * ROWS + r] = ml.x;
-        s_l[p * ROWS + r] = ml.y;
-    }
-    __syncthreads();
-    for (int r = tid; r < rows; r += AT_THREADS) {
-        float top = NEG_INF, l = 0.0f;
-        for (int p = 0; p < parts; ++p) top = fmaxf(top, s[p * ROWS + r]);
-        const float use = top == NEG_INF ? 0.0f : top;
-        for (int p = 0; p < parts; ++p) {
-            const float y = s_l[p * ROWS + r], f = y > 0.0f ? __builtin_amdgcn_exp2f(s[p * ROWS + r] - use) : 0.0f;
-            s[p * ROWS + r] = f;
-            l += y * f;
-        }
-        s[parts * ROWS + r] = l > 0.0f ? v_unit / l : 0.0f;
-        if (a.lse) {
-            const int row = rt * ROWS + r;
-            a.lse[(int64_t)(q.q0 + row / a.group) * a.n_heads + head * a.group + row % a.group] = l > 0.0f ? (top + __builtin_amdgcn_logf(l)) * LN2 : NEG_INF;
-        }
-    }
-    __syncthreads();
-    for (int u = tid; u < rows * (D / 4); u += AT_THREADS) {
-        const int r = u / (D / 4), d = u % (D / 4) * 4, row = rt * ROWS + r;
-        float4 o = make_float4(0, 0, 0, 0);
-#pragma unroll 4
-        for (int p = 0; p < parts; ++p) {
-            const float *from = a.part + (slot0 + (int64_t)p * ROWS + r) * D + d;
-            const float2 x = find(from), y = find(from + 2);
-            const float f = s[p * ROWS + r];
-            if (f > 0.0f) { o.x += x.x * f; o.y += x.y * f; o.z += y.x * f; o.w += y.y * f; }
-        }
-        const float f = s[parts * ROWS + r];
-        put((E *)a.out + (int64_t)(q.q0 + row / a.group) * a.out_token + (int64_t)(head * a.group + row % a.group) * a.out_head + d, a.out_wide,
-            o.x * f, o.y * f, o.z * f, o.w * f);
-    }
-}
-
-// ---- many rows ---------------------------------------------------------------
-
-// WR wavefronts beside each other take 32 rows each (a row: one query and query head of the KV head), 4 / WR share a tile's keys.
-template <bool FP8, int D, int WR>
-struct Tile {
-    static constexpr int WK = 4 / WR;
-    static constexpr int NK = WR == 4 ? 2 : 1;           // blocks of 32 keys a wavefront takes of a tile
-    static constexpr int KT = WK * NK * 32;              // keys of a tile
-    static constexpr int ROWS = 32 * WR;
-    static constexpr int CH = D / 8;                     // 16-byte pieces of a row in LDS
-    static constexpr int LOADS = KT * CH / AT_THREADS / (FP8 ? 2 : 1);   // of a thread, 16 bytes each, keys or values
-    static constexpr int BUF = 2 * KT * D * 2;           // keys and values of a tile
-    static constexpr int BUFS = BUF <= 32768 ? 2 : 1;    // two tiles where two workgroups' fit a compute unit
-    static constexpr int LDS = BUF * BUFS;
-};
-
-// Where 16-byte piece c of key row r lies in LDS.  Keys are read 32 rows at a time at one piece; the pieces of 8 rows and more fall in
-// different banks.  Values are read as 4 rows x 64 bytes; those rows' pieces, too.  (No bank conflict is counted.)
-template <int CH> __device__ __forceinline__ int k_piece(int r, int c) { return r * CH + (c ^ (r & (CH < 16 ? CH - 1 : 15))); }
-template <int CH> __device__ __forceinline__ int v_piece(int r, int c) { return r * CH + (c ^ (CH >= 16 ? (r & 3) << 2 : ((r >> 1) & 1) << 2)); }
-
-// PAGE16: pages of 16 tokens and more, so that what a wavefront loads at once lies in one page, and its address is a scalar.
-template <typename E, bool FP8, int D, int WR, bool PAGE16>
-__global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : 2) void hx_attend_kernel(AttendArgs a)
-{
-    using X8 = typename Types<E>::x8;
-    using X2 = typename Types<E>::x2;
-    using C = Tile<FP8, D, WR>;
-    constexpr int KT = C::KT, CH = C::CH, LOADS = C::LOADS, NK = C::NK, WK = C::WK;
-    extern __shared__ __align__(16) char smem[];
-    int *s_depth = (int *)(smem + C::LDS);
-    uint32_t *s_anc = (uint32_t *)(s_depth + HX_MAX_DRAFTS);     // [HX_MAX_DRAFTS][ANC_WORDS]
-    __shared__ float s_ml[4][2][32];
-
-    const KvView &kv = a.kv;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, col = lane & 31;
-    const int wr = wave % WR, wk = wave / WR;
-    const int nh = a.n * kv.n_heads;
-    const int pair = blockIdx.x % nh, rest = blockIdx.x / nh;
-    const int split = rest % a.splits, rt = a.row_tiles - 1 - rest / a.splits;
-    const int head = pair % kv.n_heads;
-    const Seq sq = sequence(a, pair / kv.n_heads);
-    if (!sq.there) { if (tid == 0) hx_raise(kv.status, HX_ERR_INDEX); return; }
-    if (rt * C::ROWS >= sq.nq * (int64_t)a.group) return;
-    if (!sq.ok && tid == 0) hx_raise(kv.status, HX_ERR_INDEX);
-    const int base = sq.base;
-    const bool tree = a.parent != nullptr;
-
-    const int t_first = rt * C::ROWS / a.group;
-    int t_last = (rt * C::ROWS + C::ROWS - 1) / a.group;
-    t_last = t_last < sq.nq ? t_last : sq.nq - 1;
-    const Extent ex = extent<KT>(a, sq, t_first, t_last);
-    const int parts = parts_of(a, ex.n);
-    if (split >= parts) return;
-    const int tile0 = split * a.chunk, tile1 = split == parts - 1 ? ex.n : tile0 + a.chunk;
-    if (tree && sq.ok) plant(a, sq, (int *)smem, s_depth, s_anc);
-
-    // this lane's row
-    const int row = rt * C::ROWS + wr * 32 + col, t = row / a.group, qhead = head * a.group + row % a.group;
-    const Sight view = sight(a, sq, t, s_depth, s_anc);
-
-    const float k_unit = a.k_scale ? a.k_scale[a.layer * kv.n_heads + head] : 1.0f;
-    const float sc = a.scale * k_unit * LOG2E;
-    // the score's sign goes into the query, and its factor is no 0: a masked score stays -infinity
-    const float c = fmaxf(fabsf(sc), 1e-37f);
-    X8 qf[D / 16];
-    {
-        const E *qp = (const E *)a.q + (int64_t)(sq.q0 + t) * a.q_token + (int64_t)qhead * a.q_head;
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) {
-            X8 x = {};
-            if (view.alive) {
-                if (a.q_wide) x = *(const X8 *)(qp + s * 16 + half * 8);
-                else
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = qp[s * 16 + half * 8 + i];
-            }
-            if (sc < 0)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = -x[i];
-            qf[s] = x;
-        }
-    }
-
-    // rows of this wavefront: between which positions they lie (for a tile that all of them see whole)
-    int wave_first = base + (rt * C::ROWS + wr * 32) / a.group, wave_last = base + (rt * C::ROWS + wr * 32 + 31) / a.group;
-    if (tree) { wave_first = base - 1; wave_last = sq.len; }
-
-    constexpr int KEYS_LANE = KT / 64;
-    auto start_of = [&](int tile) { return (tile < ex.sink_tiles ? tile : tile - ex.sink_tiles + ex.lo_tile) * KT; };
-    // the page of the key that lane l stands for, -1 where there is nothing to see
-    auto page_of = [&](int tile, int j) {
-        const int y = start_of(tile) + j * 64 + lane;
-        int page = -1;
-        if (tile < tile1 && y < ex.hi && (y >= ex.lo || y < a.n_sink)) page = sq.table[y >> kv.shift];
-        if (page >= kv.n_pages) { hx_raise(kv.status, HX_ERR_INDEX); page = -1; }
-        return page;
-    };
-
-    uint4 rk[LOADS], rv[LOADS];
-    int pages[KEYS_LANE];
-    unsigned long long there[KEYS_LANE];
-    constexpr int ROW_BYTES = FP8 ? D : 2 * D, PER_ROW = ROW_BYTES / 16;
-    const int64_t page_bytes = ((int64_t)kv.n_heads << kv.shift) * ROW_BYTES;
-    const int64_t here = (int64_t)a.layer * kv.n_pages * page_bytes + ((int64_t)head << kv.shift) * ROW_BYTES;
-    const char *k_at = (const char *)kv.k + here, *v_at = (const char *)kv.v + here;
-    const int in_page = (1 << kv.shift) - 1;
-    const int my_key = tid / PER_ROW, my_off = tid % PER_ROW * 16;
-    auto fetch = [&](int tile) {
-        const int y0 = start_of(tile);
-        bool whole = PAGE16;
-#pragma unroll
-        for (int j = 0; j < KEYS_LANE; ++j) whole = whole && there[j] == ~0ull;
-        if (whole) {
-            const int first = wave * 64 / PER_ROW;                // this wavefront's first key of each load
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int key = i * AT_THREADS / PER_ROW + first;
-                const int page = __builtin_amdgcn_readlane(pages[KEYS_LANE > 1 ? i * AT_THREADS / PER_ROW / 64 : 0], key & 63);
-                const int64_t at = page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES;       // a scalar
-                const int off = lane * 16;
-                rk[i] = *(const uint4 *)(k_at + at + off);
-                rv[i] = *(const uint4 *)(v_at + at + off);
-            }
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int key = i * AT_THREADS / PER_ROW + my_key;
-            const int page = __shfl(pages[KEYS_LANE > 1 ? i * AT_THREADS / PER_ROW / 64 : 0], key & 63);
-            const int64_t at = page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES + my_off;
-            rk[i] = rv[i] = make_uint4(0, 0, 0, 0);
-            if (page >= 0) {
-                rk[i] = *(const uint4 *)(k_at + at);
-                rv[i] = *(const uint4 *)(v_at + at);
-            }
-        }
-    };
-    // (a whole tile's thread has key my_key at my_off of each load, too: 64 lanes x 16 bytes are rows beside each other)
-    auto store = [&](uint4 *sk, uint4 *sv) {
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int key = i * AT_THREADS / PER_ROW + my_key, part = tid % PER_ROW;
-            if constexpr (FP8) {
-                union { X2 x[8]; uint4 u[2]; } wk_, wv_;
-                const uint32_t kk[4] = {rk[i].x, rk[i].y, rk[i].z, rk[i].w}, vv[4] = {rv[i].x, rv[i].y, rv[i].z, rv[i].w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) { widen(kk[j], wk_.x[2 * j], wk_.x[2 * j + 1]); widen(vv[j], wv_.x[2 * j], wv_.x[2 * j + 1]); }
-                sk[k_piece<CH>(key, 2 * part)] = wk_.u[0]; sk[k_piece<CH>(key, 2 * part + 1)] = wk_.u[1];
-                sv[v_piece<CH>(key, 2 * part)] = wv_.u[0]; sv[v_piece<CH>(key, 2 * part + 1)] = wv_.u[1];
-            } else {
-                sk[k_piece<CH>(key, part)] = rk[i];
-                sv[v_piece<CH>(key, part)] = rv[i];
-            }
-        }
-    };
-    auto look = [&](int tile) {
-#pragma unroll
-        for (int j = 0; j < KEYS_LANE; ++j) pages[j] = page_of(tile, j);
-    };
-    auto seen_keys = [&]() {
-#pragma unroll
-        for (int j = 0; j < KEYS_LANE; ++j) there[j] = __builtin_amdgcn_ballot_w64(pages[j] >= 0);
-    };
-
-    f32x16 o[D / 32] = {};
-    float m = NEG_INF, l = 0.0f;
-    // this lane's place in the values: 4 keys x 16 numbers a group of 16 lanes, of which lane j reads 4 numbers of key j / 4 and gets
-    // number j of the 4 keys
-    const int v_key = 4 * half + ((lane & 15) >> 2), v_sub = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-
-    if (tile0 < tile1) {
-        look(tile0);
-        seen_keys();
-        fetch(tile0);
-        look(tile0 + 1);
-    }
-    for (int tile = tile0; tile < tile1; ++tile) {
-        uint4 *sk = (uint4 *)(smem + (C::BUFS == 2 ? (tile & 1) * C::BUF : 0)), *sv = sk + KT * CH;
-        unsigned long long now[KEYS_LANE];
-#pragma unroll
-        for (int j = 0; j < KEYS_LANE; ++j) now[j] = there[j];
-        if (C::BUFS == 1) __syncthreads();
-        store(sk, sv);
-        if (tile + 1 < tile1) {
-            seen_keys();
-            fetch(tile + 1);
-            look(tile + 2);
-        }
-        __syncthreads();
-
-        const int y0 = start_of(tile);
-        f32x16 s[NK];
-#pragma unroll
-        for (int b = 0; b < NK; ++b) {
-            const int key = (wk * NK + b) * 32 + col;
-            f32x16 acc = {};
-#pragma unroll
-            for (int x = 0; x < D / 16; ++x) {
-                const uint4 kf = sk[k_piece<CH>(key, 2 * x + half)];
-                acc = mfma32(__builtin_bit_cast(X8, kf), qf[x], acc);
-            }
-            s[b] = acc;
-        }
-        // a lane's register i of block b is the score of key y0 + (wk NK + b) 32 + 8 (i / 4) + 4 half + i % 4
-#pragma unroll
-        for (int b = 0; b < NK; ++b) {
-            const int blk = (wk * NK + b) * 32, yb = y0 + blk;
-            const uint32_t seen = (uint32_t)(now[blk / 64] >> (blk & 32));
-            const bool all = seen == 0xffffffffu && (tree ? yb + 31 < base : yb + 31 <= wave_first) &&
-                             (a.window <= 0 || yb + 31 < a.n_sink || wave_last - yb < a.window);
-            if (!all) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int k = 8 * (i / 4) + 4 * half + i % 4;
-                    s[b][i] = ((seen >> k) & 1) && view.sees(yb + k) ? s[b][i] : NEG_INF;
-                }
-            }
-        }
-        float top = NEG_INF;
-#pragma unroll
-        for (int b = 0; b < NK; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-        top = fmaxf(top, other_half(top)) * c;
-        if (__builtin_amdgcn_ballot_w64(top > m + MAX_SLACK)) {
-            const float m_new = fmaxf(m, top);
-            const float shrink = __builtin_amdgcn_exp2f(m - (m_new == NEG_INF ? 0.0f : m_new));
-            m = m_new;
-            l *= shrink;
-#pragma unroll
-            for (int x = 0; x < D / 32; ++x) o[x] *= shrink;
-        }
-        const float m_use = m == NEG_INF ? 0.0f : m;
-#pragma unroll
-        for (int b = 0; b < NK; ++b) {
-            union { X8 x8[2]; X2 x2[8]; } p;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float w0 = __builtin_amdgcn_exp2f(fmaf(s[b][2 * i], c, -m_use)), w1 = __builtin_amdgcn_exp2f(fmaf(s[b][2 * i + 1], c, -m_use));
-                p.x2[i][0] = (E)w0;
-                p.x2[i][1] = (E)w1;
-                l += w0 + w1;
-            }
-            const int blk = (wk * NK + b) * 32;
-#pragma unroll
-            for (int st = 0; st < 2; ++st) {
-#pragma unroll
-                for (int x = 0; x < D / 32; ++x) {
-                    const int key = blk + st * 16 + v_key, piece = x * 4 + v_sub;
-                    using LdsPtr = __attribute__((address_space(3))) i16x4 *;
-                    const char *at0 = (const char *)(sv + v_piece<CH>(key, piece)) + (lane & 1) * 8;
-                    const char *at1 = at0 + 8 * CH * 16;
-                    union { i16x4 h[2]; X8 x; } vf;
-                    vf.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at0);
-                    vf.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at1);
-                    o[x] = mfma32(vf.x, p.x8[st], o[x]);
-                }
-            }
-        }
-    }
-
-    l += other_half(l);
-    if (!view.alive) { m = NEG_INF; l = 0.0f; }
-    if constexpr (WK > 1) {
-        // the wavefronts that shared the keys: common maximum, then the first of them adds the others' sums up
-        if (half == 0) { s_ml[wave][0][col] = m; s_ml[wave][1][col] = l; }
-        __syncthreads();
-        float top = NEG_INF;
-#pragma unroll
-        for (int w = 0; w < WK; ++w) top = fmaxf(top, s_ml[w * WR + wr][0][col]);
-        const float use = top == NEG_INF ? 0.0f : top;
-        float sum = 0.0f;
-#pragma unroll
-        for (int w = 0; w < WK; ++w) sum += s_ml[w * WR + wr][1][col] * __builtin_amdgcn_exp2f(s_ml[w * WR + wr][0][col] - use);
-        const float f = __builtin_amdgcn_exp2f(m - use);
-        float *s_o = (float *)smem;
-        if (wk > 0)
-#pragma unroll
-            for (int x = 0; x < D / 32; ++x)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s_o[(((wk - 1) * WR + wr) * (D / 2) + x * 16 + i) * 64 + lane] = o[x][i] * f;
-        __syncthreads();
-        if (wk == 0)
-#pragma unroll
-            for (int x = 0; x < D / 32; ++x)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float y = o[x][i] * f;
-#pragma unroll
-                    for (int w = 0; w < WK - 1; ++w) y += s_o[((w * WR + wr) * (D / 2) + x * 16 + i) * 64 + lane];
-                    o[x][i] = y;
-                }
-        m = top;
-        l = sum;
-    }
-    const bool mine = wk == 0 && t < sq.nq;
-    if (parts > 1) {
-        if (!mine) return;
-        const int64_t slot = (((int64_t)pair * a.row_tiles + rt) * a.splits + split) * C::ROWS + wr * 32 + col;
-        float *to = a.part + slot * D;
-#pragma unroll
-        for (int x = 0; x < D / 32; ++x)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *(float4 *)(to + x * 32 + 8 * i + 4 * half) = make_float4(o[x][4 * i], o[x][4 * i + 1], o[x][4 * i + 2], o[x][4 * i + 3]);
-        if (half == 0) a.part_ml[slot] = make_float2(m, l);
-        return;
-    }
-    if (!mine) return;
-    const float v_unit = a.v_scale ? a.v_scale[a.layer * kv.n_heads + head] : 1.0f;
-    const float f = l > 0.0f ? v_unit / l : 0.0f;
-    E *to = (E *)a.out + (int64_t)(sq.q0 + t) * a.out_token + (int64_t)qhead * a.out_head;
-#pragma unroll
-    for (int x = 0; x < D / 32; ++x)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float y[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) y[j] = l > 0.0f ? o[x][4 * i + j] * f : 0.0f;
-            put(to + x * 32 + 8 * i + 4 * half, a.out_wide, y[0], y[1], y[2], y[3]);
-        }
-    if (a.lse && half == 0) a.lse[(int64_t)(sq.q0 + t) * a.n_heads + qhead] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * LN2 : NEG_INF;
-}
-
-// The parts of rows put together, by D / 4 lanes a row: each has 4 of its numbers, and the maximum and sum of some of its parts.
-template <typename E, int D, int KT, int ROWS>
-__global__ __launch_bounds__(AT_THREADS) void hx_attend_join_kernel(AttendArgs a)
-{
-    constexpr int G = D / 4, TOGETHER = AT_THREADS / G, KEEP = (MAX_SPLITS + G - 1) / G;
-    const int per_tile = ROWS / TOGETHER, pair = blockIdx.x / (a.row_tiles * per_tile), rt = blockIdx.x / per_tile % a.row_tiles;
-    const int r = blockIdx.x % per_tile * TOGETHER + threadIdx.x / G, g = threadIdx.x % G, row = rt * ROWS + r;
-    const Seq sq = sequence(a, pair / a.kv.n_heads);
-    if (!sq.ok || rt * ROWS >= sq.nq * (int64_t)a.group) return;
-    int t_last = (rt * ROWS + ROWS - 1) / a.group;
-    t_last = t_last < sq.nq ? t_last : sq.nq - 1;
-    const int parts = parts_of(a, extent<KT>(a, sq, rt * ROWS / a.group, t_last).n), t = row / a.group, head = pair % a.kv.n_heads;
-    if (parts == 1 || t >= sq.nq) return;                        // (rows beside each other in a wavefront may end here)
-    const int64_t slot0 = ((int64_t)pair * a.row_tiles + rt) * a.splits * ROWS + r;
-    float2 ml[KEEP];
-    float top = NEG_INF;
-#pragma unroll
-    for (int k = 0; k < KEEP; ++k) {
-        const int p = k * G + g;
-        ml[k] = p < parts ? a.part_ml[slot0 + (int64_t)p * ROWS] : make_float2(NEG_INF, 0.0f);
-        top = fmaxf(top, ml[k].x);
-    }
-#pragma unroll
-    for (int d = G / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, G));
-    const float use = top == NEG_INF ? 0.0f : top;
-    float f[KEEP], l = 0.0f;
-#pragma unroll
-    for (int k = 0; k < KEEP; ++k) {
-        f[k] = ml[k].y > 0.0f ? __builtin_amdgcn_exp2f(ml[k].x - use) : 0.0f;
-        l += ml[k].y * f[k];
-    }
-#pragma unroll
-    for (int d = G / 2; d > 0; d >>= 1) l += __shfl_xor(l, d, G);
-    float4 o = make_float4(0, 0, 0, 0);
-    for (int p0 = 0; p0 < parts; p0 += 8) {
-        float4 x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = *(const float4 *)(a.part + (slot0 + (int64_t)(p0 + i < parts ? p0 + i : parts - 1) * ROWS) * D + 4 * g);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int p = p0 + i;
-            float w = __shfl(f[0], p % G, G);
-#pragma unroll
-            for (int k = 1; k < KEEP; ++k) {
-                const float v = __shfl(f[k], p % G, G);
-                w = p / G == k ? v : w;
-            }
-            if (p < parts && w > 0.0f) { o.x += x[i].x * w; o.y += x[i].y * w; o.z += x[i].z * w; o.w += x[i].w * w; }
-        }
-    }
-    const float v_unit = a.v_scale ? a.v_scale[a.layer * a.kv.n_heads + head] : 1.0f, unit = l > 0.0f ? v_unit / l : 0.0f;
-    const int qhead = head * a.group + row % a.group;
-    put((E *)a.out + (int64_t)(sq.q0 + t) * a.out_token + (int64_t)qhead * a.out_head + 4 * g, a.out_wide, o.x * unit, o.y * unit, o.z * unit, o.w * unit);
-    if (a.lse && g == 0) a.lse[(int64_t)(sq.q0 + t) * a.n_heads + qhead] = l > 0.0f ? (top + __builtin_amdgcn_logf(l)) * LN2 : NEG_INF;
-}
-
-// ---- few rows ----------------------------------------------------------------
-
-// value of the lane 16 away
-__device__ __forceinline__ float lane_16_away(float x)
-{
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(threadIdx.x & 16 ? r[0] : r[1]);
-}
-
-template <int CH> __device__ __forceinline__ int few_v_piece(int r, int c) { return r * CH + (c ^ (CH >= 16 ? (r & 7) << 1 : ((r >> 1) & 3) << 1)); }
-
-constexpr int FEW_KEYS = 32;
-
-// LDS of a wavefront: a tile's values, and at the end its sums
-constexpr int few_wave_lds(int dim, int cols) { return FEW_KEYS * dim * 2 > 16 * cols * dim * 4 ? FEW_KEYS * dim * 2 : 16 * cols * dim * 4; }
-
-// Up to 16 COLS rows of a KV head, as single tokens bring them: bound by the reads of keys and values.  Each wavefront takes every fourth tile
-// of 32 keys by itself, with nothing shared until the end: the keys go from memory into the registers of the matrix product, the values
-// through its own piece of LDS, which transposes them; what it asks for next is under way all the time.
-template <typename E, bool FP8, int D, int COLS, bool PAGE16>
-__global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && (D == 64 || FP8) ? 3 : 2) void hx_attend_few_kernel(AttendArgs a)
-{
-    using X8 = typename Types<E>::x8;
-    using X2 = typename Types<E>::x2;
-    constexpr int CH = D / 8, ROW_BYTES = FP8 ? D : 2 * D;
-    constexpr int K_LOADS = ROW_BYTES / 64;                     // of a lane for 16 keys
-    constexpr int V_LOADS = FEW_KEYS * ROW_BYTES / 1024;        // of a lane for the tile
-    constexpr int PER_ROW = ROW_BYTES / 16;
-    constexpr int WAVE_LDS = few_wave_lds(D, COLS), ROWS = 16 * COLS;
-    extern __shared__ __align__(16) char smem[];
-    int *s_depth = (int *)(smem + 4 * WAVE_LDS);
-    uint32_t *s_anc = (uint32_t *)(s_depth + HX_MAX_DRAFTS);
-    __shared__ float s_ml[4][2][ROWS];
-
-    const KvView &kv = a.kv;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), quad = lane >> 4, col = lane & 15;
-    const int nh = a.n * kv.n_heads;
-    const int pair = blockIdx.x % nh, split = blockIdx.x / nh, head = pair % kv.n_heads;
-    const Seq sq = sequence(a, pair / kv.n_heads);
-    if (!sq.there) { if (tid == 0) hx_raise(kv.status, HX_ERR_INDEX); return; }
-    if (sq.nq == 0) return;
-    if (!sq.ok && tid == 0) hx_raise(kv.status, HX_ERR_INDEX);
-    const int base = sq.base;
-    const bool tree = a.parent != nullptr;
-    const Extent ex = extent<FEW_KEYS>(a, sq, 0, sq.nq - 1);
-    const int parts = parts_of(a, ex.n);
-    if (split >= parts) return;
-    const int tile0 = split * a.chunk, tile1 = split == parts - 1 ? ex.n : tile0 + a.chunk;
-    if (tree && sq.ok) plant(a, sq, (int *)smem, s_depth, s_anc);
-
-    const float k_unit = a.k_scale ? a.k_scale[a.layer * kv.n_heads + head] : 1.0f;
-    const float sc = a.scale * k_unit * LOG2E;
-    const float c = fmaxf(fabsf(sc), 1e-37f);
-    // this lane's rows, one of each block of 16
-    int t[COLS], qhead[COLS];
-    Sight view[COLS];
-    X8 qf[COLS][D / 32];
-#pragma unroll
-    for (int w = 0; w < COLS; ++w) {
-        t[w] = (16 * w + col) / a.group;
-        qhead[w] = head * a.group + (16 * w + col) % a.group;
-        view[w] = sight(a, sq, t[w], s_depth, s_anc);
-        const E *qp = (const E *)a.q + (int64_t)(sq.q0 + t[w]) * a.q_token + (int64_t)qhead[w] * a.q_head;
-#pragma unroll
-        for (int s = 0; s < D / 32; ++s) {
-            // which 8 numbers of a row a lane's s-th piece of a key holds
-            const int d = FP8 ? (s >> 1) * 64 + quad * 16 + (s & 1) * 8 : s * 32 + quad * 8;
-            X8 x = {};
-            if (view[w].alive) {
-                if (a.q_wide) x = *(const X8 *)(qp + d);
-                else
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = qp[d + i];
-            }
-            if (sc < 0)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = -x[i];
-            qf[w][s] = x;
-        }
-    }
-    int all_last = base + sq.nq - 1;
-    if (tree) all_last = sq.len;
-
-    auto start_of = [&](int tile) { return (tile < ex.sink_tiles ? tile : tile - ex.sink_tiles + ex.lo_tile) * FEW_KEYS; };
-    auto page_of = [&](int tile) {
-        const int y = start_of(tile) + (lane & 31);
-        int page = -1;
-        if (tile < tile1 && y < ex.hi && (y >= ex.lo || y < a.n_sink)) page = sq.table[y >> kv.shift];
-        if (page >= kv.n_pages) { hx_raise(kv.status, HX_ERR_INDEX); page = -1; }
-        return page;
-    };
-    const int64_t page_bytes = ((int64_t)kv.n_heads << kv.shift) * ROW_BYTES;
-    const int64_t here = (int64_t)a.layer * kv.n_pages * page_bytes + ((int64_t)head << kv.shift) * ROW_BYTES;
-    const char *k_at = (const char *)kv.k + here, *v_at = (const char *)kv.v + here;
-    const int in_page = (1 << kv.shift) - 1;
-    uint4 rk[2][K_LOADS], rv[V_LOADS];
-    auto fetch_k = [&](int tile, int pages, bool whole) {
-        const int y0 = start_of(tile), off = col * ROW_BYTES + quad * 16;
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            if (whole) {
-                const int page = __builtin_amdgcn_readlane(pages, b * 16);
-                const char *at = k_at + (page * page_bytes + ((y0 + b * 16) & in_page) * ROW_BYTES);
-#pragma unroll
-                for (int i = 0; i < K_LOADS; ++i) rk[b][i] = *(const uint4 *)(at + off + i * 64);
-            } else {
-                const int key = b * 16 + col, page = __shfl(pages, key);
-                const char *at = k_at + (page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES + quad * 16);
-#pragma unroll
-                for (int i = 0; i < K_LOADS; ++i) {
-                    rk[b][i] = make_uint4(0, 0, 0, 0);
-                    if (page >= 0) rk[b][i] = *(const uint4 *)(at + i * 64);
-                }
-            }
-        }
-    };
-    auto fetch_v = [&](int tile, int pages, bool whole) {
-        const int y0 = start_of(tile);
-#pragma unroll
-        for (int i = 0; i < V_LOADS; ++i) {
-            if (whole) {
-                const int key = i * 64 / PER_ROW, page = __builtin_amdgcn_readlane(pages, key);
-                const char *at = v_at + (page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES);
-                rv[i] = *(const uint4 *)(at + lane * 16);
-            } else {
-                const int key = (i * 64 + lane) / PER_ROW, page = __shfl(pages, key);
-                rv[i] = make_uint4(0, 0, 0, 0);
-                if (page >= 0) rv[i] = *(const uint4 *)(v_at + (page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES + lane % PER_ROW * 16));
-            }
-        }
-    };
-
-    uint4 *sv = (uint4 *)(smem + wave * WAVE_LDS);
-    f32x4 o[COLS][D / 16] = {};
-    float m[COLS], l[COLS];
-#pragma unroll
-    for (int w = 0; w < COLS; ++w) { m[w] = NEG_INF; l[w] = 0.0f; }
-    int pages = page_of(tile0 + wave), next = page_of(tile0 + wave + 4);
-    uint32_t there = (uint32_t)__builtin_amdgcn_ballot_w64(pages >= 0);
-    if (tile0 + wave < tile1) {
-        const bool whole = PAGE16 && there == 0xffffffffu;
-        fetch_k(tile0 + wave, pages, whole);
-        fetch_v(tile0 + wave, pages, whole);
-    }
-    for (int tile = tile0 + wave; tile < tile1; tile += 4) {
-        const uint32_t now = there;
-        const int y0 = start_of(tile);
-        pages = next;
-        there = (uint32_t)__builtin_amdgcn_ballot_w64(pages >= 0);
-        const bool whole = PAGE16 && there == 0xffffffffu, more = tile + 4 < tile1;
-        next = page_of(tile + 8);
-        f32x4 s[COLS][2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            f32x4 acc[COLS] = {};
-#pragma unroll
-            for (int i = 0; i < K_LOADS; ++i) {
-                if constexpr (FP8) {
-                    union { X2 x2[8]; X8 x8[2]; } kw;
-                    const uint32_t kk[4] = {rk[b][i].x, rk[b][i].y, rk[b][i].z, rk[b][i].w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) widen(kk[j], kw.x2[2 * j], kw.x2[2 * j + 1]);
-#pragma unroll
-                    for (int w = 0; w < COLS; ++w) {
-                        acc[w] = mfma16(kw.x8[0], qf[w][2 * i], acc[w]);
-                        acc[w] = mfma16(kw.x8[1], qf[w][2 * i + 1], acc[w]);
-                    }
-                } else
-#pragma unroll
-                    for (int w = 0; w < COLS; ++w) acc[w] = mfma16(__builtin_bit_cast(X8, rk[b][i]), qf[w][i], acc[w]);
-            }
-#pragma unroll
-            for (int w = 0; w < COLS; ++w) s[w][b] = acc[w];
-        }
-        if (more) fetch_k(tile + 4, pages, whole);
-#pragma unroll
-        for (int i = 0; i < V_LOADS; ++i) {
-            const int key = (i * 64 + lane) / PER_ROW, part = lane % PER_ROW;
-            if constexpr (FP8) {
-                union { X2 x[8]; uint4 u[2]; } w;
-                const uint32_t vv[4] = {rv[i].x, rv[i].y, rv[i].z, rv[i].w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) widen(vv[j], w.x[2 * j], w.x[2 * j + 1]);
-                sv[few_v_piece<CH>(key, 2 * part)] = w.u[0]; sv[few_v_piece<CH>(key, 2 * part + 1)] = w.u[1];
-            } else sv[few_v_piece<CH>(key, part)] = rv[i];
-        }
-        if (more) fetch_v(tile + 4, pages, whole);
-        // a lane's register i of block b is the score of key y0 + 16 b + 4 quad + i
-        const bool all = now == 0xffffffffu && (tree ? y0 + 31 < base : y0 + 31 <= base) &&
-                         (a.window <= 0 || y0 + 31 < a.n_sink || all_last - y0 < a.window);
-        union { X8 x8; X2 x2[4]; } p[COLS];
-#pragma unroll
-        for (int w = 0; w < COLS; ++w) {
-            if (!all) {
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int k = 16 * b + 4 * quad + i;
-                        s[w][b][i] = ((now >> k) & 1) && view[w].sees(y0 + k) ? s[w][b][i] : NEG_INF;
-                    }
-            }
-            float top = fmaxf(fmaxf(fmaxf(s[w][0][0], s[w][0][1]), fmaxf(s[w][0][2], s[w][0][3])),
-                              fmaxf(fmaxf(s[w][1][0], s[w][1][1]), fmaxf(s[w][1][2], s[w][1][3])));
-            top = fmaxf(top, lane_16_away(top));
-            top = fmaxf(top, other_half(top)) * c;
-            if (__builtin_amdgcn_ballot_w64(top > m[w] + MAX_SLACK)) {
-                const float m_new = fmaxf(m[w], top);
-                const float shrink = __builtin_amdgcn_exp2f(m[w] - (m_new == NEG_INF ? 0.0f : m_new));
-                m[w] = m_new;
-                l[w] *= shrink;
-#pragma unroll
-                for (int x = 0; x < D / 16; ++x) o[w][x] *= shrink;
-            }
-            const float m_use = m[w] == NEG_INF ? 0.0f : m[w];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float w0 = __builtin_amdgcn_exp2f(fmaf(s[w][i / 2][2 * (i & 1)], c, -m_use)), w1 = __builtin_amdgcn_exp2f(fmaf(s[w][i / 2][2 * (i & 1) + 1], c, -m_use));
-                p[w].x2[i][0] = (E)w0;
-                p[w].x2[i][1] = (E)w1;
-                l[w] += w0 + w1;
-            }
-        }
-        // the values were written by other lanes of this wavefront: LDS works in order, the compiler has to as well
-        __builtin_amdgcn_wave_barrier();
-        asm volatile("" ::: "memory");
-#pragma unroll
-        for (int x = 0; x < D / 16; ++x) {
-            const int key = 4 * quad + (col >> 2), piece = x * 2 + ((col & 3) >> 1);
-            using LdsPtr = __attribute__((address_space(3))) i16x4 *;
-            const char *at0 = (const char *)(sv + few_v_piece<CH>(key, piece)) + (col & 1) * 8;
-            const char *at1 = at0 + 16 * CH * 16;
-            union { i16x4 h[2]; X8 x; } vf;
-            vf.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at0);
-            vf.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at1);
-#pragma unroll
-            for (int w = 0; w < COLS; ++w) o[w][x] = mfma16(vf.x, p[w].x8, o[w][x]);
-        }
-        __builtin_amdgcn_wave_barrier();
-        asm volatile("" ::: "memory");
-    }
-    // the four wavefronts' sums: each adds up a quarter of the numbers
-#pragma unroll
-    for (int w = 0; w < COLS; ++w) {
-        l[w] += lane_16_away(l[w]);
-        l[w] += other_half(l[w]);
-        if (!view[w].alive) { m[w] = NEG_INF; l[w] = 0.0f; }
-        if (quad == 0) { s_ml[wave][0][16 * w + col] = m[w]; s_ml[wave][1][16 * w + col] = l[w]; }
-    }
-    __syncthreads();
-    const float v_unit = a.v_scale ? a.v_scale[a.layer * kv.n_heads + head] : 1.0f;
-    f32x4 *s_o = (f32x4 *)smem;                                  // [wave][COLS][D / 16][64]
-    float top[COLS], sum[COLS];
-#pragma unroll
-    for (int w = 0; w < COLS; ++w) {
-        top[w] = NEG_INF;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) top[w] = fmaxf(top[w], s_ml[v][0][16 * w + col]);
-        const float use = top[w] == NEG_INF ? 0.0f : top[w], f = __builtin_amdgcn_exp2f(m[w] - use);
-        sum[w] = 0.0f;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) sum[w] += s_ml[v][1][16 * w + col] * __builtin_amdgcn_exp2f(s_ml[v][0][16 * w + col] - use);
-#pragma unroll
-        for (int x = 0; x < D / 16; ++x) s_o[((wave * COLS + w) * (D / 16) + x) * 64 + lane] = o[w][x] * f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < COLS; ++w) {
-        if (t[w] >= sq.nq) continue;
-        const int64_t slot = ((int64_t)pair * a.splits + split) * ROWS + 16 * w + col;
-        const float unit = sum[w] > 0.0f ? v_unit / sum[w] : 0.0f;
-#pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
-            const int x = wave * (D / 64) + i, d = x * 16 + 4 * quad;
-            f32x4 y = s_o[(w * (D / 16) + x) * 64 + lane];
-#pragma unroll
-            for (int v = 1; v < 4; ++v) y += s_o[((v * COLS + w) * (D / 16) + x) * 64 + lane];
-            if (parts > 1) {
-                leave(a.part + slot * D + d, y[0], y[1]);
-                leave(a.part + slot * D + d + 2, y[2], y[3]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) y[j] = sum[w] > 0.0f ? y[j] * unit : 0.0f;
-                put((E *)a.out + (int64_t)(sq.q0 + t[w]) * a.out_token + (int64_t)qhead[w] * a.out_head + d, a.out_wide, y[0], y[1], y[2], y[3]);
-            }
-        }
-        if (wave == 0 && quad == 0) {
-            if (parts > 1) leave((float *)(a.part_ml + slot), top[w], sum[w]);
-            else if (a.lse) a.lse[(int64_t)(sq.q0 + t[w]) * a.n_heads + qhead[w]] = sum[w] > 0.0f ? (top[w] + __builtin_amdgcn_logf(sum[w])) * LN2 : NEG_INF;
-        }
-    }
-    if (parts > 1) join<E, D, ROWS>(a, sq, pair, 0, parts, (float *)smem);
-}
-
-__global__ __launch_bounds__(AT_THREADS) void hx_attend_clear_kernel(int *done, int64_t n)
-{
-    const int64_t i = (int64_t)blockIdx.x * AT_THREADS + threadIdx.x;
-    if (i < n) done[i] = 0;
-}
-
-// Room for the parts, and where the workgroups themselves put them together, for counters, which are 0 whenever no launch is under way.
-int parts_room(hx_ctx *ctx, AttendArgs &a, int64_t tiles, int rows, int dim, bool counted, hipStream_t stream)
-{
-    const int64_t slots = tiles * a.splits * rows;
-    if (counted) {
-        const void *was = ctx->att_done.p;
-        if (int rc = hx_scratch(ctx, ctx->att_done, (size_t)tiles * sizeof(int))) return rc;
-        if (ctx->att_done.p != was) {
-            const int64_t n = ctx->att_done.cap / sizeof(int);
-            hx_attend_clear_kernel<<<(int)((n + AT_THREADS - 1) / AT_THREADS), AT_THREADS, 0, stream>>>((int *)ctx->att_done.p, n);
-        }
-        a.done = (int *)ctx->att_done.p;
-    }
-    if (int rc = hx_scratch(ctx, ctx->att, (size_t)slots * (dim * sizeof(float) + sizeof(float2)))) return rc;
-    a.part = (float *)ctx->att.p;
-    a.part_ml = (float2 *)(a.part + slots * dim);
-    return HX_OK;
-}
-
-template <typename E, bool FP8, int D, int WR>
-int launch(hx_ctx *ctx, AttendArgs &a, hipStream_t stream)
-{
-    using C = Tile<FP8, D, WR>;
-    const int lds = C::LDS + (a.parent ? TREE_BYTES : 0);
-    const int64_t tiles = (int64_t)a.n * a.kv.n_heads * a.row_tiles, grid = tiles * a.splits, join_grid = tiles * (C::ROWS / (AT_THREADS / (D / 4)));
-    HX_REQUIRE(ctx, grid <= INT32_MAX && join_grid <= INT32_MAX, HX_ERR_SHAPE, "%lld workgroups", (long long)grid);
-    if (a.splits > 1)
-        if (int rc = parts_room(ctx, a, tiles, C::ROWS, D, false, stream)) return rc;
-    if (a.kv.shift >= 4) hx_attend_kernel<E, FP8, D, WR, true><<<(int)grid, AT_THREADS, lds, stream>>>(a);
-    else hx_attend_kernel<E, FP8, D, WR, false><<<(int)grid, AT_THREADS, lds, stream>>>(a);
-    if (a.splits > 1) hx_attend_join_kernel<E, D, C::KT, C::ROWS><<<(int)join_grid, AT_THREADS, 0, stream>>>(a);
-    return hx_check_launch(ctx, "hx_attend_kernel");
-}
-
-// Parts of the keys where there are few workgroups otherwise: as many as make `want` workgroups if all sequences had the longest's
-// length, of `least` tiles at least.
-void divide(AttendArgs &a, int64_t groups, int64_t want, int max_len, int tile_keys, int least)
-{
-    int64_t reach = max_len;
-    if (a.window > 0 && reach > (int64_t)a.window + a.n_sink + a.max_q) reach = (int64_t)a.window + a.n_sink + a.max_q;
-    const int64_t tiles = (reach + tile_keys - 1) / tile_keys + 1;
-    int64_t chunk = (groups * tiles + want - 1) / want;
-    chunk = chunk > least ? chunk : least;
-    if (chunk * MAX_SPLITS < tiles) chunk = (tiles + MAX_SPLITS - 1) / MAX_SPLITS;
-    a.chunk = (int)chunk;
-    a.splits = (int)((tiles + chunk - 1) / chunk);
-}
-
-template <typename E, bool FP8, int D, int COLS>
-int launch_few(hx_ctx *ctx, AttendArgs &a, hipStream_t stream)
-{
-    const int lds = 4 * few_wave_lds(D, COLS) + (a.parent ? TREE_BYTES : 0);
-    const int64_t tiles = (int64_t)a.n * a.kv.n_heads, grid = tiles * a.splits;
-    HX_REQUIRE(ctx, grid <= INT32_MAX, HX_ERR_SHAPE, "%lld workgroups", (long long)grid);
-    if (a.splits > 1)
-        if (int rc = parts_room(ctx, a, tiles, 16 * COLS, D, true, stream)) return rc;
-    if (a.kv.shift >= 4) hx_attend_few_kernel<E, FP8, D, COLS, true><<<(int)grid, AT_THREADS, lds, stream>>>(a);
-    else hx_attend_few_kernel<E, FP8, D, COLS, false><<<(int)grid, AT_THREADS, lds, stream>>>(a);
-    return hx_check_launch(ctx, "hx_attend_few_kernel");
-}
-
-template <typename E, bool FP8, int D>
-int plan(hx_ctx *ctx, AttendArgs &a, int max_len, hipStream_t stream)
-{
-    const int64_t rows = (int64_t)a.max_q * a.group, pairs = (int64_t)a.n * a.kv.n_heads;
-    if (rows <= 32) {
-        a.row_tiles = 1;
-        divide(a, pairs, 16 * ctx->num_cu, max_len, FEW_KEYS, 8);
-        return rows <= 16 ? launch_few<E, FP8, D, 1>(ctx, a, stream) : launch_few<E, FP8, D, 2>(ctx, a, stream);
-    }
-    const int wr = rows <= 64 ? 2 : 4;
-    a.row_tiles = (int)((rows + 32 * wr - 1) / (32 * wr));
-    divide(a, pairs * a.row_tiles, 8 * ctx->num_cu, max_len, 64, 4);
-    return wr == 2 ? launch<E, FP8, D, 2>(ctx, a, stream) : launch<E, FP8, D, 4>(ctx, a, stream);
-}
-
-template <typename E, bool FP8>
-int by_dim(hx_ctx *ctx, AttendArgs &a, int max_len, hipStream_t stream)
-{
-    if (a.kv.dim == 64) return plan<E, FP8, 64>(ctx, a, max_len, stream);
-    if (a.kv.dim == 128) return plan<E, FP8, 128>(ctx, a, max_len, stream);
-    return plan<E, FP8, 256>(ctx, a, max_len, stream);
-}
-
-template <typename E, bool FP8, int D, int WR>
-bool allow()
-{
-    using C = Tile<FP8, D, WR>;
-    return hipFuncSetAttribute((const void *)hx_attend_kernel<E, FP8, D, WR, false>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS + TREE_BYTES) == hipSuccess &&
-           hipFuncSetAttribute((const void *)hx_attend_kernel<E, FP8, D, WR, true>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS + TREE_BYTES) == hipSuccess;
-}
-template <typename E, bool FP8, int D, int COLS>
-bool allow_few()
-{
-    const int lds = 4 * few_wave_lds(D, COLS) + TREE_BYTES;
-    return hipFuncSetAttribute((const void *)hx_attend_few_kernel<E, FP8, D, COLS, false>, hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess &&
-           hipFuncSetAttribute((const void *)hx_attend_few_kernel<E, FP8, D, COLS, true>, hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
-}
-template <typename E, bool FP8, int D>
-bool allow_dim() { return allow<E, FP8, D, 2>() && allow<E, FP8, D, 4>() && allow_few<E, FP8, D, 1>() && allow_few<E, FP8, D, 2>(); }
-template <typename E, bool FP8>
-bool allow_all() { return allow_dim<E, FP8, 64>() && allow_dim<E, FP8, 128>() && allow_dim<E, FP8, 256>(); }
-
-}  // namespace
+// Attention over cached pages: the entry point.  The kernels are hx_attend.hpp's, compiled for a pair of types in each of hx_attend_*.hip.
+#include "hx_attend_args.hpp"
 
 // more LDS a workgroup than the 64 KB that need no asking
 int hx_attend_init()
 {
-    return allow_all<__bf16, false>() && allow_all<__bf16, true>() && allow_all<_Float16, false>() && allow_all<_Float16, true>() ? HX_OK : HX_ERR_DEVICE;
+    return hx_attend_init_bf16() && hx_attend_init_bf16_e4m3() && hx_attend_init_f16() && hx_attend_init_f16_e4m3() ? HX_OK : HX_ERR_DEVICE;
 }
 
 extern "C" int hx_attend(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_kv_seqs *seqs,
@@ -1103,7 +34,7 @@ extern "C" int hx_attend(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, con
     HxDeviceGuard guard(ctx->device);
     HX_REQUIRE(ctx, guard.ok, HX_ERR_DEVICE, "cannot select device %d", ctx->device);
     hipStream_t stream = (hipStream_t)stream_;
-    AttendArgs a{};
+    HxAttend a{};
     a.kv = kv;
     a.layer = layer; a.n = g.n; a.row = g.row; a.q_ptr = g.q_ptr; a.n_q = g.n_q;
     a.max_q = g.max_q < g.n_q ? g.max_q : g.n_q;
@@ -1115,6 +46,6 @@ extern "C" int hx_attend(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, con
     a.q_wide = ((uintptr_t)g.q & 15) == 0 && g.q_token % 8 == 0 && g.q_head % 8 == 0;
     a.out_wide = ((uintptr_t)g.out & 7) == 0 && g.out_token % 4 == 0 && g.out_head % 4 == 0;
     const bool fp8 = pool->dtype == HX_E4M3;
-    if (g.dtype == HX_BF16) return fp8 ? by_dim<__bf16, true>(ctx, a, g.max_len, stream) : by_dim<__bf16, false>(ctx, a, g.max_len, stream);
-    return fp8 ? by_dim<_Float16, true>(ctx, a, g.max_len, stream) : by_dim<_Float16, false>(ctx, a, g.max_len, stream);
+    if (g.dtype == HX_BF16) return fp8 ? hx_attend_bf16_e4m3(ctx, a, g.max_len, stream) : hx_attend_bf16(ctx, a, g.max_len, stream);
+    return fp8 ? hx_attend_f16_e4m3(ctx, a, g.max_len, stream) : hx_attend_f16(ctx, a, g.max_len, stream);
 }
