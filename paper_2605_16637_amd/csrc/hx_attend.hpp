@@ -90,10 +90,9 @@ constexpr int TREE_BYTES = HX_MAX_DRAFTS * 4 * (1 + ANC_WORDS);
 // Every draft's depth (-1: left out) and the bits of the drafts above it; s_parent: HX_MAX_DRAFTS words that are free yet.
 __device__ __forceinline__ void plant(const AttendArgs &a, const Seq &q, int *s_parent, int *s_depth, uint32_t *s_anc)
 {
-    const int tid = threadIdx.x;
-    if (tid < q.nq) s_parent[tid] = a.parent[q.q0 + tid];
+    for (int i = threadIdx.x; i < q.nq; i += blockDim.x) s_parent[i] = a.parent[q.q0 + i];
     __syncthreads();
-    if (tid < q.nq) {
+    for (int tid = threadIdx.x; tid < q.nq; tid += blockDim.x) {
         uint32_t mine[ANC_WORDS] = {};
         int depth = 0, at = tid;
         while (at >= 0) {
@@ -111,17 +110,17 @@ __device__ __forceinline__ void plant(const AttendArgs &a, const Seq &q, int *s_
     __syncthreads();
 }
 
-// The tiles of KT keys that some of the queries t_first .. t_last may see: the first sink_tiles, then those from lo_tile on.
+// The tiles of KEYS keys that some of the queries t_first .. t_last may see: the first sink_tiles, then those from lo_tile on.
 struct Extent {
     int lo, hi, sink_tiles, lo_tile, n;
 };
 
-template <int KT>
+template <int KEYS>
 __device__ __forceinline__ Extent extent(const AttendArgs &a, const Seq &q, int t_first, int t_last)
 {
     const bool tree = a.parent != nullptr;
     Extent x{0, 0, 0, 0, 0};
-    if (!q.ok) return x;
+    if (!q.ok || a.kv.n_pages == 0) return x;
     x.hi = tree ? q.len : q.base + t_last + 1;
     if (a.window > 0) {
         const int first_pos = tree ? q.base - 1 : q.base + t_first;         // the least position of a query
@@ -129,13 +128,13 @@ __device__ __forceinline__ Extent extent(const AttendArgs &a, const Seq &q, int 
         x.lo = x.lo > 0 ? x.lo : 0;
         if (tree && x.lo > q.base) x.lo = q.base;
     }
-    x.lo_tile = x.lo / KT;
+    x.lo_tile = x.lo / KEYS;
     if (x.lo > 0) {
         const int sinks = a.n_sink < x.lo ? a.n_sink : x.lo;
-        x.sink_tiles = (sinks + KT - 1) / KT;
+        x.sink_tiles = (sinks + KEYS - 1) / KEYS;
         if (x.sink_tiles >= x.lo_tile) { x.sink_tiles = 0; x.lo_tile = 0; }
     }
-    x.n = x.hi > 0 ? x.sink_tiles + (x.hi + KT - 1) / KT - x.lo_tile : 0;
+    x.n = x.hi > 0 ? x.sink_tiles + (x.hi + KEYS - 1) / KEYS - x.lo_tile : 0;
     return x;
 }
 
@@ -279,21 +278,37 @@ __device__ __forceinline__ void join(const AttendArgs &a, const Seq &q, int pair
 
 // ---- many rows ---------------------------------------------------------------
 
-// WR wavefronts beside each other take 32 rows each (a row: one query and query head of the KV head), and where those are fewer than
-// four, WK of them share a tile's keys.
-template <bool FP8, int D, int WR>
+constexpr int KT = 32;                                   // keys of a tile
+__device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p; }
+
+// 16 bytes a lane straight to LDS, a wavefront's beside each other from `to` on (the same for all lanes).  The compiler knows neither that the
+// load is under way nor when it has come: that is waited for by count.
+__device__ __forceinline__ void to_lds(uint32_t to, int off, const char *from)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(from) : "memory");
+}
+__device__ __forceinline__ void to_lds(uint32_t to, const char *from)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+}
+
+constexpr int PAGES = 1024;                              // of a part, looked up at its start
+
+// WR wavefronts beside each other take 32 rows each (a row: one query and query head of the KV head).
+template <bool FP8, int D, int WR, bool PAGE16>
 struct Tile {
-    static constexpr int WK = WR < 4 ? 4 / WR : 1;
-    static constexpr int THREADS = 64 * WR * WK;
-    static constexpr int NK = WR >= 4 ? 2 : 1;           // blocks of 32 keys a wavefront takes of a tile
-    static constexpr int KT = WK * NK * 32;              // keys of a tile
+    static constexpr int THREADS = 64 * WR;
     static constexpr int ROWS = 32 * WR;
     static constexpr int CH = D / 8;                     // 16-byte pieces of a row in LDS
-    static constexpr int LOADS = KT * CH / THREADS / (FP8 ? 2 : 1);   // of a thread, 16 bytes each, keys or values
+    static constexpr int ROW_BYTES = FP8 ? D : 2 * D, PER_ROW = ROW_BYTES / 16;
+    static constexpr int PIECES = KT * PER_ROW;          // of a tile's keys, or values
+    static constexpr int LOADS = (PIECES + THREADS - 1) / THREADS;
     static constexpr int BUF = 2 * KT * D * 2;           // keys and values of a tile
-    static constexpr int BUFS = BUF <= 32768 ? 2 : 1;    // two tiles where two workgroups' fit a compute unit
-    static constexpr int LDS = BUF * BUFS;
-    static constexpr int DEPTH = LOADS * (D / 64) <= 8 ? 2 : 1;      // tiles under way to a thread's registers, as many as fit
+    // Tiles in LDS.  What is stored in 16 bits goes there straight from memory; 8 bits pass through registers, where RING more are
+    // under way.
+    static constexpr bool DIRECT = !FP8 && PAGE16;
+    static constexpr int RING = DIRECT && D < 256 ? 4 : 3;
+    static constexpr int LDS = BUF * RING + PAGES * 4;
 };
 
 // Where 16-byte piece c of key row r lies in LDS.  Keys are read 32 rows at a time at one piece; the pieces of 8 rows and more fall in
@@ -302,21 +317,22 @@ template <int CH> __device__ __forceinline__ int k_piece(int r, int c) { return 
 template <int CH> __device__ __forceinline__ int v_piece(int r, int c) { return r * CH + (c ^ (CH >= 16 ? (r & 3) << 2 : ((r >> 1) & 1) << 2)); }
 
 // PAGE16: pages of 16 tokens and more, so that what a wavefront loads at once lies in one page, and its address is a scalar.
+//
+// While a tile's weights are worked out the next tile's scores are: the matrix unit and the others are both busy within a wavefront, not
+// only between two.
 template <typename E, bool FP8, int D, int WR, bool PAGE16>
-__global__ __launch_bounds__(WR < 4 ? 256 : 64 * WR, D == 256 ? 1 : 2) void hx_attend_kernel(AttendArgs a)
+__global__ __launch_bounds__(64 * WR, D == 256 ? 1 : 2) void hx_attend_kernel(AttendArgs a)
 {
     using X8 = typename Types<E>::x8;
     using X2 = typename Types<E>::x2;
-    using C = Tile<FP8, D, WR>;
-    constexpr int KT = C::KT, CH = C::CH, LOADS = C::LOADS, NK = C::NK, WK = C::WK, DEPTH = C::DEPTH, THREADS = C::THREADS;
+    using C = Tile<FP8, D, WR, PAGE16>;
+    constexpr int RING = C::RING, CH = C::CH, LOADS = C::LOADS, THREADS = C::THREADS, ROW_BYTES = C::ROW_BYTES, PER_ROW = C::PER_ROW;
     extern __shared__ __align__(16) char smem[];
-    int *s_depth = (int *)(smem + C::LDS);
+    int *s_page = (int *)(smem + C::BUF * RING), *s_depth = (int *)(smem + C::LDS);
     uint32_t *s_anc = (uint32_t *)(s_depth + HX_MAX_DRAFTS);     // [HX_MAX_DRAFTS][ANC_WORDS]
-    __shared__ float s_ml[WR * WK][2][32];
 
     const KvView &kv = a.kv;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, col = lane & 31;
-    const int wr = wave % WR, wk = wave / WR;
     const int nh = a.n * kv.n_heads;
     const int pair = blockIdx.x % nh, rest = blockIdx.x / nh;
     // row tiles of the same keys beside each other: they meet in the XCD's cache
@@ -339,7 +355,7 @@ __global__ __launch_bounds__(WR < 4 ? 256 : 64 * WR, D == 256 ? 1 : 2) void hx_a
     if (tree && sq.ok) plant(a, sq, (int *)smem, s_depth, s_anc);
 
     // this lane's row
-    const int row = rt * C::ROWS + wr * 32 + col, t = row / a.group, qhead = head * a.group + row % a.group;
+    const int row = rt * C::ROWS + wave * 32 + col, t = row / a.group, qhead = head * a.group + row % a.group;
     const Sight view = sight(a, sq, t, s_depth, s_anc);
 
     const float k_unit = a.k_scale ? a.k_scale[a.layer * kv.n_heads + head] : 1.0f;
@@ -366,143 +382,175 @@ __global__ __launch_bounds__(WR < 4 ? 256 : 64 * WR, D == 256 ? 1 : 2) void hx_a
     }
 
     // rows of this wavefront: between which positions they lie (for a tile that all of them see whole)
-    int wave_first = base + (rt * C::ROWS + wr * 32) / a.group, wave_last = base + (rt * C::ROWS + wr * 32 + 31) / a.group;
+    int wave_first = base + (rt * C::ROWS + wave * 32) / a.group, wave_last = base + (rt * C::ROWS + wave * 32 + 31) / a.group;
     if (tree) { wave_first = base - 1; wave_last = sq.len; }
 
-    constexpr int KEYS_LANE = KT / 64;
-    using First = std::integral_constant<int, 0>;
-    using Last = std::integral_constant<int, DEPTH - 1>;
     auto start_of = [&](int tile) { return (tile < ex.sink_tiles ? tile : tile - ex.sink_tiles + ex.lo_tile) * KT; };
-    // the page of the key that lane l stands for, -1 where there is nothing to see
-    auto page_of = [&](int tile, int j) {
-        const int y = start_of(tile) + j * 64 + lane;
-        int page = -1;
-        if (tile < tile1 && y < ex.hi && (y >= ex.lo || y < a.n_sink)) page = sq.table[y >> kv.shift];
-        return page;
+    // PAGE16: a tile has its keys in one page, or in two of 16
+    const int per_tile = kv.shift == 4 ? 2 : 1;
+    auto page_at = [&](int y) {
+        const int page = y < ex.hi ? sq.table[y >> kv.shift] : -1;
+        if (page >= kv.n_pages) hx_raise(kv.status, HX_ERR_INDEX);
+        return page < kv.n_pages ? page : -1;
     };
+    if constexpr (PAGE16) {
+        // what is looked up now need not be waited for among the keys
+        const int n = (tile1 - tile0) * per_tile;
+        for (int i = tid; i < n && i < PAGES; i += THREADS) s_page[i] = page_at(start_of(tile0 + i / per_tile) + i % per_tile * 16);
+        __syncthreads();
+    }
+    auto listed = [&](int i, int y) { return i < PAGES ? s_page[i] : page_at(y); };
 
-    uint4 rk[DEPTH][LOADS], rv[DEPTH][LOADS];
-    int pages[KEYS_LANE];                                // of the tile that is asked for next
-    unsigned long long there[DEPTH][KEYS_LANE];          // which keys of the tiles under way are there
-    constexpr int ROW_BYTES = FP8 ? D : 2 * D, PER_ROW = ROW_BYTES / 16;
+    uint4 rk[C::DIRECT ? 1 : RING][LOADS], rv[C::DIRECT ? 1 : RING][LOADS];
+    uint32_t there[RING], now = 0;                       // which keys of the tiles under way are there, and of the one whose scores are next
     const int64_t page_bytes = ((int64_t)kv.n_heads << kv.shift) * ROW_BYTES;
     const int64_t here = (int64_t)a.layer * kv.n_pages * page_bytes + ((int64_t)head << kv.shift) * ROW_BYTES;
     const char *k_at = (const char *)kv.k + here, *v_at = (const char *)kv.v + here;
     const int in_page = (1 << kv.shift) - 1;
-    const int my_key = tid / PER_ROW, my_off = tid % PER_ROW * 16;
-    auto fetch = [&](int tile, auto set) {
+    const int my_key = tid / PER_ROW, my_part = tid % PER_ROW;
+    const bool loads = C::PIECES % THREADS == 0 || wave * 64 < C::PIECES;
+    // A tile's keys and values are asked for, by the same number of loads whatever the tile, so that it is known how many are under way.
+    // Through registers what is not there is read from the pool's start and cleared on its way to LDS.  Straight to LDS a lane's 16 bytes
+    // lie in the order of the lanes: each asks for the piece that belongs there, zeros where nothing is.
+    int k_off[LOADS], v_off[LOADS];
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+        const int key = j * THREADS / PER_ROW + my_key, in_group = key - (j * THREADS / PER_ROW + wave * 64 / PER_ROW);
+        k_off[j] = C::DIRECT ? in_group * ROW_BYTES + (k_piece<CH>(key, my_part) - key * CH) * 16 : lane * 16;
+        v_off[j] = C::DIRECT ? in_group * ROW_BYTES + (v_piece<CH>(key, my_part) - key * CH) * 16 : lane * 16;
+    }
+    auto ask = [&](int tile, auto set) {
         constexpr int S = decltype(set)::value;
+        int64_t at[LOADS], off[LOADS];
+        there[S] = 0;
+        bool whole = false;
         const int y0 = start_of(tile);
-        bool whole = PAGE16;
-#pragma unroll
-        for (int j = 0; j < KEYS_LANE; ++j) {
-            pages[j] = in_pool(kv, pages[j]);
-            there[S][j] = __builtin_amdgcn_ballot_w64(pages[j] >= 0);
-            whole = whole && there[S][j] == ~0ull;
-        }
-        if (whole) {
-            const int first = wave * 64 / PER_ROW;                // this wavefront's first key of each load
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int key = i * THREADS / PER_ROW + first;
-                const int page = __builtin_amdgcn_readlane(pages[KEYS_LANE > 1 ? i * THREADS / PER_ROW / 64 : 0], key & 63);
-                const int64_t at = page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES;       // a scalar
-                const int off = lane * 16;
-                rk[S][i] = *(const uint4 *)(k_at + at + off);
-                rv[S][i] = *(const uint4 *)(v_at + at + off);
+        int p0 = -1, p1 = -1;
+        if constexpr (PAGE16)
+            if (tile < tile1) {
+                const int i = (tile - tile0) * per_tile;
+                p0 = __builtin_amdgcn_readfirstlane(listed(i, y0));
+                p1 = per_tile == 2 ? __builtin_amdgcn_readfirstlane(listed(i + 1, y0 + 16)) : p0;
+                whole = p0 >= 0 && p1 >= 0 && y0 + KT <= ex.hi && (y0 >= ex.lo || y0 + KT <= a.n_sink);
             }
-            return;
+        auto page_of = [&](int key) {
+            const int y = y0 + key;
+            if (tile >= tile1 || y >= ex.hi || (y < ex.lo && y >= a.n_sink)) return -1;
+            return PAGE16 ? (key < 16 ? p0 : p1) : page_at(y);
+        };
+        if (whole) {
+            there[S] = 0xffffffffu;
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) {
+                const int key = (j * THREADS / PER_ROW + wave * 64 / PER_ROW) & 31;              // this wavefront's first key
+                at[j] = (key < 16 ? p0 : p1) * page_bytes + ((y0 + key) & in_page) * ROW_BYTES;    // a scalar
+            }
+        } else there[S] = (uint32_t)__builtin_amdgcn_ballot_w64(page_of(col) >= 0);
+        if constexpr (C::DIRECT) {
+            if (loads)
+#pragma unroll
+                for (int j = 0; j < LOADS; ++j) {
+                    const int key = j * THREADS / PER_ROW + my_key;
+                    const uint32_t to = lds_address(smem) + S * C::BUF + (j * THREADS + wave * 64) * 16, to_v = to + KT * CH * 16;
+                    if (whole) {
+                        to_lds(to, k_off[j], k_at + at[j]);
+                        to_lds(to_v, v_off[j], v_at + at[j]);
+                    } else {
+                        const int page = page_of(key);
+                        const int64_t o = page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES;
+                        to_lds(to, page >= 0 ? k_at + o + (k_piece<CH>(key, my_part) - key * CH) * 16 : (const char *)a.zeros);
+                        to_lds(to_v, page >= 0 ? v_at + o + (v_piece<CH>(key, my_part) - key * CH) * 16 : (const char *)a.zeros);
+                    }
+                }
+        } else {
+            if (whole)
+#pragma unroll
+                for (int j = 0; j < LOADS; ++j) off[j] = at[j] + lane * 16;
+            else
+#pragma unroll
+                for (int j = 0; j < LOADS; ++j) {
+                    const int key = j * THREADS / PER_ROW + my_key, page = key < KT ? page_of(key) : -1;
+                    off[j] = page >= 0 ? page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES + my_part * 16 : 0;
+                }
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) {
+                rk[S][j] = *(const uint4 *)(k_at + off[j]);
+                rv[S][j] = *(const uint4 *)(v_at + off[j]);
+            }
         }
+    };
+    auto store = [&](auto set) {
+        constexpr int S = decltype(set)::value;
+        uint4 *sk = (uint4 *)(smem + S * C::BUF), *sv = sk + KT * CH;
+        if (!loads) return;
+        if (there[S] != 0xffffffffu)
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i)
+                if (!((there[S] >> (i * THREADS / PER_ROW + my_key)) & 1)) rk[S][i] = rv[S][i] = make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int key = i * THREADS / PER_ROW + my_key;
-            const int page = __shfl(pages[KEYS_LANE > 1 ? i * THREADS / PER_ROW / 64 : 0], key & 63);
-            const int64_t at = page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES + my_off;
-            rk[S][i] = rv[S][i] = make_uint4(0, 0, 0, 0);
-            if (page >= 0) {
-                rk[S][i] = *(const uint4 *)(k_at + at);
-                rv[S][i] = *(const uint4 *)(v_at + at);
-            }
-        }
-    };
-    // (a whole tile's thread has key my_key at my_off of each load, too: 64 lanes x 16 bytes are rows beside each other)
-    auto store = [&](uint4 *sk, uint4 *sv, auto set) {
-        constexpr int S = decltype(set)::value;
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int key = i * THREADS / PER_ROW + my_key, part = tid % PER_ROW;
             if constexpr (FP8) {
-                union { X2 x[8]; uint4 u[2]; } wk_, wv_;
+                union { X2 x[8]; uint4 u[2]; } wk, wv;
                 const uint32_t kk[4] = {rk[S][i].x, rk[S][i].y, rk[S][i].z, rk[S][i].w}, vv[4] = {rv[S][i].x, rv[S][i].y, rv[S][i].z, rv[S][i].w};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) { widen(kk[j], wk_.x[2 * j], wk_.x[2 * j + 1]); widen(vv[j], wv_.x[2 * j], wv_.x[2 * j + 1]); }
-                sk[k_piece<CH>(key, 2 * part)] = wk_.u[0]; sk[k_piece<CH>(key, 2 * part + 1)] = wk_.u[1];
-                sv[v_piece<CH>(key, 2 * part)] = wv_.u[0]; sv[v_piece<CH>(key, 2 * part + 1)] = wv_.u[1];
+                for (int j = 0; j < 4; ++j) { widen(kk[j], wk.x[2 * j], wk.x[2 * j + 1]); widen(vv[j], wv.x[2 * j], wv.x[2 * j + 1]); }
+                sk[k_piece<CH>(key, 2 * my_part)] = wk.u[0]; sk[k_piece<CH>(key, 2 * my_part + 1)] = wk.u[1];
+                sv[v_piece<CH>(key, 2 * my_part)] = wv.u[0]; sv[v_piece<CH>(key, 2 * my_part + 1)] = wv.u[1];
             } else {
-                sk[k_piece<CH>(key, part)] = rk[S][i];
-                sv[v_piece<CH>(key, part)] = rv[S][i];
+                sk[k_piece<CH>(key, my_part)] = rk[S][i];
+                sv[v_piece<CH>(key, my_part)] = rv[S][i];
             }
         }
     };
-    // tile's keys and values are asked for, and before that the pages of the one after it: what is asked for later is there later
-    auto ask = [&](int tile, auto set) {
-        int next[KEYS_LANE];
-#pragma unroll
-        for (int j = 0; j < KEYS_LANE; ++j) next[j] = page_of(tile + 1, j);
-        fetch(tile, set);
-#pragma unroll
-        for (int j = 0; j < KEYS_LANE; ++j) pages[j] = next[j];
-    };
-    f32x16 o[D / 32] = {};
+
+    const bool rows_here = rt * C::ROWS + wave * 32 < sq.nq * a.group;           // else the wavefront only loads
+    f32x16 o[D / 32] = {}, s = {};
     float m = NEG_INF, l = 0.0f;
     // this lane's place in the values: 4 keys x 16 numbers a group of 16 lanes, of which lane j reads 4 numbers of key j / 4 and gets
     // number j of the 4 keys
     const int v_key = 4 * half + ((lane & 15) >> 2), v_sub = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+    auto scores = [&](auto set) {
+        constexpr int S = decltype(set)::value;
+        const uint4 *sk = (const uint4 *)(smem + S * C::BUF);
+        f32x16 acc = {};
+#pragma unroll
+        for (int x = 0; x < D / 16; ++x) acc = mfma32(__builtin_bit_cast(X8, sk[k_piece<CH>(col, 2 * x + half)]), qf[x], acc);
+        return acc;
+    };
 
     auto one_tile = [&](int tile, auto set) {
-        constexpr int S = decltype(set)::value;
-        uint4 *sk = (uint4 *)(smem + (C::BUFS == 2 ? (tile & 1) * C::BUF : 0)), *sv = sk + KT * CH;
-        unsigned long long now[KEYS_LANE];
-#pragma unroll
-        for (int j = 0; j < KEYS_LANE; ++j) now[j] = there[S][j];
-        if (C::BUFS == 1) __syncthreads();
-        store(sk, sv, set);
-        if (tile + DEPTH < tile1) ask(tile + DEPTH, set);
-        __syncthreads();
-
+        constexpr int S = decltype(set)::value, NEXT = (S + 1) % RING;
+        using Next = std::integral_constant<int, NEXT>;
+        const uint32_t seen = now;
+        now = there[NEXT];
+        if constexpr (C::DIRECT) {
+            // the next tile has come, those after it may be under way; the place of the one before this is free once all are here
+            if (tile + RING - 2 < tile1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS * (RING - 3)) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (tile + RING - 1 < tile1) ask(tile + RING - 1, std::integral_constant<int, (S + RING - 1) % RING>{});
+        } else {
+            // the next tile's registers go to LDS and are free for the one RING further on
+            store(Next{});
+            ask(tile + 1 + RING, Next{});
+            __syncthreads();
+        }
+        if (!rows_here || tile >= tile1) return;
+        // a lane's register i is the score of key y0 + 8 (i / 4) + 4 half + i % 4
         const int y0 = start_of(tile);
-        f32x16 s[NK];
+        const bool all = seen == 0xffffffffu && (tree ? y0 + 31 < base : y0 + 31 <= wave_first) &&
+                         (a.window <= 0 || y0 + 31 < a.n_sink || wave_last - y0 < a.window);
+        if (!all) {
 #pragma unroll
-        for (int b = 0; b < NK; ++b) {
-            const int key = (wk * NK + b) * 32 + col;
-            f32x16 acc = {};
-#pragma unroll
-            for (int x = 0; x < D / 16; ++x) {
-                const uint4 kf = sk[k_piece<CH>(key, 2 * x + half)];
-                acc = mfma32(__builtin_bit_cast(X8, kf), qf[x], acc);
-            }
-            s[b] = acc;
-        }
-        // a lane's register i of block b is the score of key y0 + (wk NK + b) 32 + 8 (i / 4) + 4 half + i % 4
-#pragma unroll
-        for (int b = 0; b < NK; ++b) {
-            const int blk = (wk * NK + b) * 32, yb = y0 + blk;
-            const uint32_t seen = (uint32_t)(now[blk / 64] >> (blk & 32));
-            const bool all = seen == 0xffffffffu && (tree ? yb + 31 < base : yb + 31 <= wave_first) &&
-                             (a.window <= 0 || yb + 31 < a.n_sink || wave_last - yb < a.window);
-            if (!all) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int k = 8 * (i / 4) + 4 * half + i % 4;
-                    s[b][i] = ((seen >> k) & 1) && view.sees(yb + k) ? s[b][i] : NEG_INF;
-                }
+            for (int i = 0; i < 16; ++i) {
+                const int k = 8 * (i / 4) + 4 * half + i % 4;
+                s[i] = ((seen >> k) & 1) && view.sees(y0 + k) ? s[i] : NEG_INF;
             }
         }
-        float top = NEG_INF;
+        float top = s[0];
 #pragma unroll
-        for (int b = 0; b < NK; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
         top = fmaxf(top, other_half(top)) * c;
         if (__builtin_amdgcn_ballot_w64(top > m + MAX_SLACK)) {
             const float m_new = fmaxf(m, top);
@@ -513,82 +561,62 @@ __global__ __launch_bounds__(WR < 4 ? 256 : 64 * WR, D == 256 ? 1 : 2) void hx_a
             for (int x = 0; x < D / 32; ++x) o[x] *= shrink;
         }
         const float m_use = m == NEG_INF ? 0.0f : m;
+        // (after the last tile the scores of what happens to lie in LDS, which nobody asks for)
+        const f32x16 next = scores(Next{});
+        union { X8 x8[2]; X2 x2[8]; } p;
 #pragma unroll
-        for (int b = 0; b < NK; ++b) {
-            union { X8 x8[2]; X2 x2[8]; } p;
+        for (int i = 0; i < 8; ++i) {
+            const float w0 = __builtin_amdgcn_exp2f(fmaf(s[2 * i], c, -m_use)), w1 = __builtin_amdgcn_exp2f(fmaf(s[2 * i + 1], c, -m_use));
+            p.x2[i][0] = (E)w0;
+            p.x2[i][1] = (E)w1;
+            l += w0 + w1;
+        }
+        const uint4 *sv = (const uint4 *)(smem + S * C::BUF) + KT * CH;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float w0 = __builtin_amdgcn_exp2f(fmaf(s[b][2 * i], c, -m_use)), w1 = __builtin_amdgcn_exp2f(fmaf(s[b][2 * i + 1], c, -m_use));
-                p.x2[i][0] = (E)w0;
-                p.x2[i][1] = (E)w1;
-                l += w0 + w1;
-            }
-            const int blk = (wk * NK + b) * 32;
+        for (int st = 0; st < 2; ++st) {
 #pragma unroll
-            for (int st = 0; st < 2; ++st) {
-#pragma unroll
-                for (int x = 0; x < D / 32; ++x) {
-                    const int key = blk + st * 16 + v_key, piece = x * 4 + v_sub;
-                    using LdsPtr = __attribute__((address_space(3))) i16x4 *;
-                    const char *at0 = (const char *)(sv + v_piece<CH>(key, piece)) + (lane & 1) * 8;
-                    const char *at1 = at0 + 8 * CH * 16;
-                    union { i16x4 h[2]; X8 x; } vf;
-                    vf.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at0);
-                    vf.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at1);
-                    o[x] = mfma32(vf.x, p.x8[st], o[x]);
-                }
+            for (int x = 0; x < D / 32; ++x) {
+                const int key = st * 16 + v_key, piece = x * 4 + v_sub;
+                using LdsPtr = __attribute__((address_space(3))) i16x4 *;
+                const char *at0 = (const char *)(sv + v_piece<CH>(key, piece)) + (lane & 1) * 8;
+                const char *at1 = at0 + 8 * CH * 16;
+                union { i16x4 h[2]; X8 x; } vf;
+                vf.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at0);
+                vf.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at1);
+                o[x] = mfma32(vf.x, p.x8[st], o[x]);
             }
         }
+        s = next;
     };
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
+    using I2 = std::integral_constant<int, 2>;
+    using I3 = std::integral_constant<int, RING == 4 ? 3 : 0>;
     if (tile0 < tile1) {
-#pragma unroll
-        for (int j = 0; j < KEYS_LANE; ++j) pages[j] = page_of(tile0, j);
-        ask(tile0, First{});
+        ask(tile0, I0{});
+        if (!C::DIRECT || tile0 + 1 < tile1) ask(tile0 + 1, I1{});
+        if (!C::DIRECT || (RING == 4 && tile0 + 2 < tile1)) ask(tile0 + 2, I2{});
+        now = there[0];
+        if constexpr (C::DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        else {
+            store(I0{});
+            ask(tile0 + 3, I0{});
+        }
+        __syncthreads();
+        s = scores(I0{});
     }
-    if (DEPTH == 2 && tile0 + 1 < tile1) ask(tile0 + 1, Last{});
-    for (int tile = tile0; tile < tile1; tile += DEPTH) {
-        one_tile(tile, First{});
-        if (DEPTH == 2 && tile + 1 < tile1) one_tile(tile + 1, Last{});
+    for (int tile = tile0; tile < tile1; tile += RING) {
+        one_tile(tile, I0{});
+        one_tile(tile + 1, I1{});
+        one_tile(tile + 2, I2{});
+        if constexpr (RING == 4) one_tile(tile + 3, I3{});
     }
 
     l += other_half(l);
     if (!view.alive) { m = NEG_INF; l = 0.0f; }
-    if constexpr (WK > 1) {
-        // the wavefronts that shared the keys: common maximum, then the first of them adds the others' sums up
-        if (half == 0) { s_ml[wave][0][col] = m; s_ml[wave][1][col] = l; }
-        __syncthreads();
-        float top = NEG_INF;
-#pragma unroll
-        for (int w = 0; w < WK; ++w) top = fmaxf(top, s_ml[w * WR + wr][0][col]);
-        const float use = top == NEG_INF ? 0.0f : top;
-        float sum = 0.0f;
-#pragma unroll
-        for (int w = 0; w < WK; ++w) sum += s_ml[w * WR + wr][1][col] * __builtin_amdgcn_exp2f(s_ml[w * WR + wr][0][col] - use);
-        const float f = __builtin_amdgcn_exp2f(m - use);
-        float *s_o = (float *)smem;
-        if (wk > 0)
-#pragma unroll
-            for (int x = 0; x < D / 32; ++x)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s_o[(((wk - 1) * WR + wr) * (D / 2) + x * 16 + i) * 64 + lane] = o[x][i] * f;
-        __syncthreads();
-        if (wk == 0)
-#pragma unroll
-            for (int x = 0; x < D / 32; ++x)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float y = o[x][i] * f;
-#pragma unroll
-                    for (int w = 0; w < WK - 1; ++w) y += s_o[((w * WR + wr) * (D / 2) + x * 16 + i) * 64 + lane];
-                    o[x][i] = y;
-                }
-        m = top;
-        l = sum;
-    }
-    const bool mine = wk == 0 && t < sq.nq;
+    if (t >= sq.nq) return;
     if (parts > 1) {
-        if (!mine) return;
-        const int64_t slot = (((int64_t)pair * a.row_tiles + rt) * a.splits + split) * C::ROWS + wr * 32 + col;
+        const int64_t slot = (((int64_t)pair * a.row_tiles + rt) * a.splits + split) * C::ROWS + wave * 32 + col;
         float *to = a.part + slot * D;
 #pragma unroll
         for (int x = 0; x < D / 32; ++x)
@@ -598,7 +626,6 @@ __global__ __launch_bounds__(WR < 4 ? 256 : 64 * WR, D == 256 ? 1 : 2) void hx_a
         if (half == 0) a.part_ml[slot] = make_float2(m, l);
         return;
     }
-    if (!mine) return;
     const float v_unit = a.v_scale ? a.v_scale[a.layer * kv.n_heads + head] : 1.0f;
     const float f = l > 0.0f ? v_unit / l : 0.0f;
     E *to = (E *)a.out + (int64_t)(sq.q0 + t) * a.out_token + (int64_t)qhead * a.out_head;
@@ -615,7 +642,7 @@ __global__ __launch_bounds__(WR < 4 ? 256 : 64 * WR, D == 256 ? 1 : 2) void hx_a
 }
 
 // The parts of rows put together, by D / 4 lanes a row: each has 4 of its numbers, and the maximum and sum of some of its parts.
-template <typename E, int D, int KT, int ROWS>
+template <typename E, int D, int KEYS, int ROWS>
 __global__ __launch_bounds__(AT_THREADS) void hx_attend_join_kernel(AttendArgs a)
 {
     constexpr int G = D / 4, TOGETHER = AT_THREADS / G, KEEP = (MAX_SPLITS + G - 1) / G;
@@ -625,7 +652,7 @@ __global__ __launch_bounds__(AT_THREADS) void hx_attend_join_kernel(AttendArgs a
     if (!sq.ok || rt * ROWS >= sq.nq * (int64_t)a.group) return;
     int t_last = (rt * ROWS + ROWS - 1) / a.group;
     t_last = t_last < sq.nq ? t_last : sq.nq - 1;
-    const int parts = parts_of(a, extent<KT>(a, sq, rt * ROWS / a.group, t_last).n), t = row / a.group, head = pair % a.kv.n_heads;
+    const int parts = parts_of(a, extent<KEYS>(a, sq, rt * ROWS / a.group, t_last).n), t = row / a.group, head = pair % a.kv.n_heads;
     if (parts == 1 || t >= sq.nq) return;                        // (rows beside each other in a wavefront may end here)
     const int64_t slot0 = ((int64_t)pair * a.row_tiles + rt) * a.splits * ROWS + r;
     float2 ml[KEEP];
@@ -989,18 +1016,17 @@ int parts_room(hx_ctx *ctx, AttendArgs &a, int64_t tiles, int rows, int dim, boo
     return HX_OK;
 }
 
-template <typename E, bool FP8, int D, int WR>
+template <typename E, bool FP8, int D, bool PAGE16>
 int launch(hx_ctx *ctx, AttendArgs &a, hipStream_t stream)
 {
-    using C = Tile<FP8, D, WR>;
+    using C = Tile<FP8, D, 4, PAGE16>;
     const int lds = C::LDS + (a.parent ? TREE_BYTES : 0);
     const int64_t tiles = (int64_t)a.n * a.kv.n_heads * a.row_tiles, grid = tiles * a.splits, join_grid = tiles * (C::ROWS / (AT_THREADS / (D / 4)));
     HX_REQUIRE(ctx, grid <= INT32_MAX && join_grid <= INT32_MAX, HX_ERR_SHAPE, "%lld workgroups", (long long)grid);
     if (a.splits > 1)
         if (int rc = parts_room(ctx, a, tiles, C::ROWS, D, false, stream)) return rc;
-    if (a.kv.shift >= 4) hx_attend_kernel<E, FP8, D, WR, true><<<(int)grid, C::THREADS, lds, stream>>>(a);
-    else hx_attend_kernel<E, FP8, D, WR, false><<<(int)grid, C::THREADS, lds, stream>>>(a);
-    if (a.splits > 1) hx_attend_join_kernel<E, D, C::KT, C::ROWS><<<(int)join_grid, AT_THREADS, 0, stream>>>(a);
+    hx_attend_kernel<E, FP8, D, 4, PAGE16><<<(int)grid, C::THREADS, lds, stream>>>(a);
+    if (a.splits > 1) hx_attend_join_kernel<E, D, KT, C::ROWS><<<(int)join_grid, AT_THREADS, 0, stream>>>(a);
     return hx_check_launch(ctx, "hx_attend_kernel");
 }
 
@@ -1040,13 +1066,9 @@ int plan(hx_ctx *ctx, AttendArgs &a, int max_len, hipStream_t stream)
         divide(a, pairs, 16 * ctx->num_cu, max_len, FEW_KEYS, 8);
         return rows <= 16 ? launch_few<E, FP8, D, 1>(ctx, a, stream) : launch_few<E, FP8, D, 2>(ctx, a, stream);
     }
-    const int wr = rows <= 64 ? 2 : rows <= 128 || D == 256 ? 4 : 8;
-    a.row_tiles = (int)((rows + 32 * wr - 1) / (32 * wr));
-    divide(a, pairs * a.row_tiles, (wr == 8 ? 4 : 8) * ctx->num_cu, max_len, 64, 4);
-    if (wr == 2) return launch<E, FP8, D, 2>(ctx, a, stream);
-    if constexpr (D < 256)
-        if (wr == 8) return launch<E, FP8, D, 8>(ctx, a, stream);
-    return launch<E, FP8, D, 4>(ctx, a, stream);
+    a.row_tiles = (int)((rows + 127) / 128);
+    divide(a, pairs * a.row_tiles, 8 * ctx->num_cu, max_len, KT, 8);
+    return a.kv.shift >= 4 ? launch<E, FP8, D, true>(ctx, a, stream) : launch<E, FP8, D, false>(ctx, a, stream);
 }
 
 template <typename E, bool FP8>
@@ -1057,12 +1079,11 @@ int by_dim(hx_ctx *ctx, AttendArgs &a, int max_len, hipStream_t stream)
     return plan<E, FP8, 256>(ctx, a, max_len, stream);
 }
 
-template <typename E, bool FP8, int D, int WR>
+template <typename E, bool FP8, int D, bool PAGE16>
 bool allow()
 {
-    using C = Tile<FP8, D, WR>;
-    return hipFuncSetAttribute((const void *)hx_attend_kernel<E, FP8, D, WR, false>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS + TREE_BYTES) == hipSuccess &&
-           hipFuncSetAttribute((const void *)hx_attend_kernel<E, FP8, D, WR, true>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS + TREE_BYTES) == hipSuccess;
+    return hipFuncSetAttribute((const void *)hx_attend_kernel<E, FP8, D, 4, PAGE16>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                               Tile<FP8, D, 4, PAGE16>::LDS + TREE_BYTES) == hipSuccess;
 }
 template <typename E, bool FP8, int D, int COLS>
 bool allow_few()
@@ -1072,7 +1093,7 @@ bool allow_few()
            hipFuncSetAttribute((const void *)hx_attend_few_kernel<E, FP8, D, COLS, true>, hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
 }
 template <typename E, bool FP8, int D>
-bool allow_dim() { return allow<E, FP8, D, 2>() && allow<E, FP8, D, 4>() && allow<E, FP8, D, D == 256 ? 4 : 8>() && allow_few<E, FP8, D, 1>() && allow_few<E, FP8, D, 2>(); }
+bool allow_dim() { return allow<E, FP8, D, false>() && allow<E, FP8, D, true>() && allow_few<E, FP8, D, 1>() && allow_few<E, FP8, D, 2>(); }
 template <typename E, bool FP8>
 bool allow_all() { return allow_dim<E, FP8, 64>() && allow_dim<E, FP8, 128>() && allow_dim<E, FP8, 256>(); }
 

@@ -18,6 +18,7 @@ struct HxAttend {
     int window, n_sink;
     const int32_t *parent;
     const float *k_scale, *v_scale;
+    const void *zeros;           // 16 bytes of them, aligned
     bool q_wide, out_wide;       // q can be read 16 bytes at a time, out written 8
     int row_tiles, splits;       // parts of a row tile's keys, at most
     int chunk;                   // tiles of keys of a part

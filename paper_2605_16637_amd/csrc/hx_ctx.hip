@@ -396,6 +396,7 @@ extern "C" int hx_ctx_create(hx_ctx **out, int device)
     if (e == hipSuccess) { what = "hipHostMalloc(status)"; e = hipHostMalloc((void **)&ctx->h_status, sizeof(int32_t), hipHostMallocDefault); }
     if (e == hipSuccess) { what = "hipMalloc(report)"; e = hipMalloc((void **)&ctx->d_report, HX_VALIDATE_FIELDS * sizeof(int32_t)); }
     if (e == hipSuccess) { what = "hipMalloc(sync)"; e = hipMalloc((void **)&ctx->d_sync, HX_SYNC_WORDS * sizeof(int32_t)); }
+    if (e == hipSuccess) { what = "hipMalloc(zeros)"; e = hipMalloc((void **)&ctx->d_zeros, 64 * sizeof(int32_t)); }
     if (e == hipSuccess) { what = "hipMalloc(ticket)"; e = hipMalloc((void **)&ctx->d_ticket, sizeof(int32_t)); }
     if (e == hipSuccess) { what = "hipMalloc(accumulators)"; e = hipMalloc((void **)&ctx->d_acc, 3 * HX_MAX_INSTANCES * sizeof(unsigned long long)); }
     if (e == hipSuccess && device < HX_MAX_DEVICES) {     // set-up for hx_commit_static on this device
@@ -412,6 +413,7 @@ extern "C" int hx_ctx_create(hx_ctx **out, int device)
         hx_clear_status_kernel<<<1, 1, 0, nullptr>>>(ctx->d_status);
         hx_clear_status_kernel<<<1, 1, 0, nullptr>>>(ctx->d_ticket);
         hx_clear_status_kernel<<<1, HX_SYNC_WORDS, 0, nullptr>>>(ctx->d_sync);
+        hx_clear_status_kernel<<<1, 64, 0, nullptr>>>(ctx->d_zeros);
         e = hipGetLastError();
     }
     if (e == hipSuccess) { what = "hipStreamSynchronize"; e = hipStreamSynchronize(nullptr); }
@@ -433,6 +435,7 @@ extern "C" int hx_ctx_destroy(hx_ctx *ctx)
     if (ctx->d_report) (void)hipFree(ctx->d_report);
     if (ctx->d_sync) (void)hipFree(ctx->d_sync);
     if (ctx->d_ticket) (void)hipFree(ctx->d_ticket);
+    if (ctx->d_zeros) (void)hipFree(ctx->d_zeros);
     if (ctx->d_acc) (void)hipFree(ctx->d_acc);
     if (ctx->d_dpart) (void)hipFree(ctx->d_dpart);
     if (ctx->d_dtl) (void)hipFree(ctx->d_dtl);
