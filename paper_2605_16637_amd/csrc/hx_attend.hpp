@@ -279,6 +279,11 @@ __device__ __forceinline__ void join(const AttendArgs &a, const Seq &q, int pair
 // ---- many rows ---------------------------------------------------------------
 
 constexpr int KT = 32;                                   // keys of a tile
+__device__ __forceinline__ int64_t uniform(int64_t x)
+{
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
+
 __device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p; }
 
 // 16 bytes a lane straight to LDS, a wavefront's beside each other from `to` on (the same for all lanes).  The compiler knows neither that the
@@ -292,7 +297,7 @@ __device__ __forceinline__ void to_lds(uint32_t to, const char *from)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
 }
 
-constexpr int PAGES = 1024;                              // of a part, looked up at its start
+constexpr int SPAN = 256;                                // tiles whose pages are looked up at once
 
 // WR wavefronts beside each other take 32 rows each (a row: one query and query head of the KV head).
 template <bool FP8, int D, int WR, bool PAGE16>
@@ -308,7 +313,7 @@ struct Tile {
     // under way.
     static constexpr bool DIRECT = !FP8 && PAGE16;
     static constexpr int RING = DIRECT && D < 256 ? 4 : 3;
-    static constexpr int LDS = BUF * RING + PAGES * 4;
+    static constexpr int LDS = BUF * RING + SPAN * 16;
 };
 
 // Where 16-byte piece c of key row r lies in LDS.  Keys are read 32 rows at a time at one piece; the pieces of 8 rows and more fall in
@@ -321,14 +326,15 @@ template <int CH> __device__ __forceinline__ int v_piece(int r, int c) { return 
 // While a tile's weights are worked out the next tile's scores are: the matrix unit and the others are both busy within a wavefront, not
 // only between two.
 template <typename E, bool FP8, int D, int WR, bool PAGE16>
-__global__ __launch_bounds__(64 * WR, D == 256 ? 1 : 2) void hx_attend_kernel(AttendArgs a)
+__global__ __launch_bounds__(64 * WR, D == 256 ? 1 : D == 64 && !FP8 && PAGE16 ? 3 : 2) void hx_attend_kernel(AttendArgs a)
 {
     using X8 = typename Types<E>::x8;
     using X2 = typename Types<E>::x2;
     using C = Tile<FP8, D, WR, PAGE16>;
     constexpr int RING = C::RING, CH = C::CH, LOADS = C::LOADS, THREADS = C::THREADS, ROW_BYTES = C::ROW_BYTES, PER_ROW = C::PER_ROW;
     extern __shared__ __align__(16) char smem[];
-    int *s_page = (int *)(smem + C::BUF * RING), *s_depth = (int *)(smem + C::LDS);
+    longlong2 *s_off = (longlong2 *)(smem + C::BUF * RING);
+    int *s_depth = (int *)(smem + C::LDS);
     uint32_t *s_anc = (uint32_t *)(s_depth + HX_MAX_DRAFTS);     // [HX_MAX_DRAFTS][ANC_WORDS]
 
     const KvView &kv = a.kv;
@@ -381,25 +387,20 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : 2) void hx_attend_kernel(At
         }
     }
 
-    // rows of this wavefront: between which positions they lie (for a tile that all of them see whole)
-    int wave_first = base + (rt * C::ROWS + wave * 32) / a.group, wave_last = base + (rt * C::ROWS + wave * 32 + 31) / a.group;
-    if (tree) { wave_first = base - 1; wave_last = sq.len; }
+    // Tiles that all rows of this wavefront see whole: their first key is at most whole_to, and at least whole_from or at most whole_sink.
+    const int wave_first = tree ? base - 1 : base + (rt * C::ROWS + wave * 32) / a.group;
+    const int wave_last = tree ? sq.len : base + (rt * C::ROWS + wave * 32 + 31) / a.group;
+    const int whole_to = wave_first + 1 - KT, whole_from = a.window > 0 ? wave_last - a.window + 1 : 0, whole_sink = a.n_sink - KT;
+    const bool rows_here = rt * C::ROWS + wave * 32 < sq.nq * a.group;           // else the wavefront only loads
 
-    auto start_of = [&](int tile) { return (tile < ex.sink_tiles ? tile : tile - ex.sink_tiles + ex.lo_tile) * KT; };
-    // PAGE16: a tile has its keys in one page, or in two of 16
-    const int per_tile = kv.shift == 4 ? 2 : 1;
+    const int beyond_sinks = (ex.lo_tile - ex.sink_tiles) * KT;
+    auto start_of = [&](int tile) { return tile * KT + (tile < ex.sink_tiles ? 0 : beyond_sinks); };
     auto page_at = [&](int y) {
         const int page = y < ex.hi ? sq.table[y >> kv.shift] : -1;
         if (page >= kv.n_pages) hx_raise(kv.status, HX_ERR_INDEX);
         return page < kv.n_pages ? page : -1;
     };
-    if constexpr (PAGE16) {
-        // what is looked up now need not be waited for among the keys
-        const int n = (tile1 - tile0) * per_tile;
-        for (int i = tid; i < n && i < PAGES; i += THREADS) s_page[i] = page_at(start_of(tile0 + i / per_tile) + i % per_tile * 16);
-        __syncthreads();
-    }
-    auto listed = [&](int i, int y) { return i < PAGES ? s_page[i] : page_at(y); };
+    auto in_sight = [&](int y) { return y < ex.hi && (y >= ex.lo || y < a.n_sink); };       // of some row of the tile of rows
 
     uint4 rk[C::DIRECT ? 1 : RING][LOADS], rv[C::DIRECT ? 1 : RING][LOADS];
     uint32_t there[RING], now = 0;                       // which keys of the tiles under way are there, and of the one whose scores are next
@@ -419,63 +420,59 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : 2) void hx_attend_kernel(At
         k_off[j] = C::DIRECT ? in_group * ROW_BYTES + (k_piece<CH>(key, my_part) - key * CH) * 16 : lane * 16;
         v_off[j] = C::DIRECT ? in_group * ROW_BYTES + (v_piece<CH>(key, my_part) - key * CH) * 16 : lane * 16;
     }
-    auto ask = [&](int tile, auto set) {
+    const uint32_t lds0 = lds_address(smem);
+    // two: where the tile's first and second 16 keys lie, the lowest bit set where some key of the tile is not there, -1 where no page is
+    auto ask = [&](int tile, longlong2 two, auto set) {
         constexpr int S = decltype(set)::value;
-        int64_t at[LOADS], off[LOADS];
-        there[S] = 0;
-        bool whole = false;
+        const int64_t o0 = uniform(two.x), o1 = uniform(two.y);
         const int y0 = start_of(tile);
-        int p0 = -1, p1 = -1;
-        if constexpr (PAGE16)
-            if (tile < tile1) {
-                const int i = (tile - tile0) * per_tile;
-                p0 = __builtin_amdgcn_readfirstlane(listed(i, y0));
-                p1 = per_tile == 2 ? __builtin_amdgcn_readfirstlane(listed(i + 1, y0 + 16)) : p0;
-                whole = p0 >= 0 && p1 >= 0 && y0 + KT <= ex.hi && (y0 >= ex.lo || y0 + KT <= a.n_sink);
-            }
-        auto page_of = [&](int key) {
+        const bool whole = PAGE16 && !((o0 | o1) & 1);
+        auto place_of = [&](int key) -> int64_t {
             const int y = y0 + key;
-            if (tile >= tile1 || y >= ex.hi || (y < ex.lo && y >= a.n_sink)) return -1;
-            return PAGE16 ? (key < 16 ? p0 : p1) : page_at(y);
-        };
-        if (whole) {
-            there[S] = 0xffffffffu;
-#pragma unroll
-            for (int j = 0; j < LOADS; ++j) {
-                const int key = (j * THREADS / PER_ROW + wave * 64 / PER_ROW) & 31;              // this wavefront's first key
-                at[j] = (key < 16 ? p0 : p1) * page_bytes + ((y0 + key) & in_page) * ROW_BYTES;    // a scalar
+            if (tile >= tile1 || key >= KT || !in_sight(y)) return -1;
+            if constexpr (PAGE16) {
+                const int64_t o = key < 16 ? o0 : o1;
+                return o < 0 ? -1 : (o & ~(int64_t)15) + (key & 15) * ROW_BYTES;
             }
-        } else there[S] = (uint32_t)__builtin_amdgcn_ballot_w64(page_of(col) >= 0);
+            const int page = page_at(y);
+            return page < 0 ? -1 : page * page_bytes + (y & in_page) * ROW_BYTES;
+        };
+        there[S] = 0xffffffffu;
+        if (!whole) there[S] = (uint32_t)__builtin_amdgcn_ballot_w64(place_of(col) >= 0);
         if constexpr (C::DIRECT) {
             if (loads)
 #pragma unroll
                 for (int j = 0; j < LOADS; ++j) {
-                    const int key = j * THREADS / PER_ROW + my_key;
-                    const uint32_t to = lds_address(smem) + S * C::BUF + (j * THREADS + wave * 64) * 16, to_v = to + KT * CH * 16;
+                    const int key = j * THREADS / PER_ROW + my_key, first = (j * THREADS / PER_ROW + wave * 64 / PER_ROW) & 31;
+                    const uint32_t to = lds0 + S * C::BUF + (j * THREADS + wave * 64) * 16, to_v = to + KT * CH * 16;
                     if (whole) {
-                        to_lds(to, k_off[j], k_at + at[j]);
-                        to_lds(to_v, v_off[j], v_at + at[j]);
+                        const int64_t at = (first < 16 ? o0 : o1) + (first & 15) * ROW_BYTES;
+                        to_lds(to, k_off[j], k_at + at);
+                        to_lds(to_v, v_off[j], v_at + at);
                     } else {
-                        const int page = page_of(key);
-                        const int64_t o = page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES;
-                        to_lds(to, page >= 0 ? k_at + o + (k_piece<CH>(key, my_part) - key * CH) * 16 : (const char *)a.zeros);
-                        to_lds(to_v, page >= 0 ? v_at + o + (v_piece<CH>(key, my_part) - key * CH) * 16 : (const char *)a.zeros);
+                        const int64_t at = place_of(key);
+                        to_lds(to, at >= 0 ? k_at + at + (k_piece<CH>(key, my_part) - key * CH) * 16 : (const char *)a.zeros);
+                        to_lds(to_v, at >= 0 ? v_at + at + (v_piece<CH>(key, my_part) - key * CH) * 16 : (const char *)a.zeros);
                     }
                 }
         } else {
+            int64_t at[LOADS];
             if (whole)
 #pragma unroll
-                for (int j = 0; j < LOADS; ++j) off[j] = at[j] + lane * 16;
+                for (int j = 0; j < LOADS; ++j) {
+                    const int first = (j * THREADS / PER_ROW + wave * 64 / PER_ROW) & 31;
+                    at[j] = (first < 16 ? o0 : o1) + (first & 15) * ROW_BYTES + lane * 16;
+                }
             else
 #pragma unroll
                 for (int j = 0; j < LOADS; ++j) {
-                    const int key = j * THREADS / PER_ROW + my_key, page = key < KT ? page_of(key) : -1;
-                    off[j] = page >= 0 ? page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES + my_part * 16 : 0;
+                    const int64_t x = place_of(j * THREADS / PER_ROW + my_key);
+                    at[j] = x >= 0 ? x + my_part * 16 : 0;
                 }
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) {
-                rk[S][j] = *(const uint4 *)(k_at + off[j]);
-                rv[S][j] = *(const uint4 *)(v_at + off[j]);
+                rk[S][j] = *(const uint4 *)(k_at + at[j]);
+                rv[S][j] = *(const uint4 *)(v_at + at[j]);
             }
         }
     };
@@ -504,44 +501,51 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : 2) void hx_attend_kernel(At
         }
     };
 
-    const bool rows_here = rt * C::ROWS + wave * 32 < sq.nq * a.group;           // else the wavefront only loads
     f32x16 o[D / 32] = {}, s = {};
-    float m = NEG_INF, l = 0.0f;
-    // this lane's place in the values: 4 keys x 16 numbers a group of 16 lanes, of which lane j reads 4 numbers of key j / 4 and gets
-    // number j of the 4 keys
-    const int v_key = 4 * half + ((lane & 15) >> 2), v_sub = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+    float m = NEG_INF, l = 0.0f, l1 = 0.0f;
+    // This lane's places in a tile of the first ring place.  A key's pieces 2 x + half are one x apart in the bits that x has; its values: 4 keys
+    // x 16 numbers a group of 16 lanes, of which lane j reads 4 numbers of key j / 4 and gets number j of the 4 keys.
+    uint32_t k_lane[D / 16], v_lane[D / 32];
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x) k_lane[x] = lds0 + k_piece<CH>(col, 2 * x + half) * 16;
+#pragma unroll
+    for (int x = 0; x < D / 32; ++x)
+        v_lane[x] = lds0 + KT * CH * 16 + v_piece<CH>(4 * half + ((lane & 15) >> 2), x * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) * 16 + (lane & 1) * 8;
     auto scores = [&](auto set) {
         constexpr int S = decltype(set)::value;
-        const uint4 *sk = (const uint4 *)(smem + S * C::BUF);
         f32x16 acc = {};
 #pragma unroll
-        for (int x = 0; x < D / 16; ++x) acc = mfma32(__builtin_bit_cast(X8, sk[k_piece<CH>(col, 2 * x + half)]), qf[x], acc);
+        for (int x = 0; x < D / 16; ++x) {
+            using LdsPtr = __attribute__((address_space(3))) const X8 *;
+            acc = mfma32(*(LdsPtr)(uintptr_t)(k_lane[x] + S * C::BUF), qf[x], acc);
+        }
         return acc;
     };
 
+    int seg0 = tile0, seg1 = tile0;                      // tiles whose places are in s_off
+    auto place = [&](int tile) { return PAGE16 && tile < seg1 ? s_off[tile - seg0] : longlong2{-1, -1}; };
     auto one_tile = [&](int tile, auto set) {
         constexpr int S = decltype(set)::value, NEXT = (S + 1) % RING;
         using Next = std::integral_constant<int, NEXT>;
         const uint32_t seen = now;
         now = there[NEXT];
+        const longlong2 two = place(C::DIRECT ? tile + RING - 1 : tile + 1 + RING);
         if constexpr (C::DIRECT) {
             // the next tile has come, those after it may be under way; the place of the one before this is free once all are here
-            if (tile + RING - 2 < tile1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS * (RING - 3)) : "memory");
+            if (tile + RING - 2 < seg1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS * (RING - 3)) : "memory");
             else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
-            if (tile + RING - 1 < tile1) ask(tile + RING - 1, std::integral_constant<int, (S + RING - 1) % RING>{});
+            if (tile + RING - 1 < seg1) ask(tile + RING - 1, two, std::integral_constant<int, (S + RING - 1) % RING>{});
         } else {
             // the next tile's registers go to LDS and are free for the one RING further on
             store(Next{});
-            ask(tile + 1 + RING, Next{});
+            ask(tile + 1 + RING, two, Next{});
             __syncthreads();
         }
-        if (!rows_here || tile >= tile1) return;
+        if (!rows_here || tile >= seg1) return;
         // a lane's register i is the score of key y0 + 8 (i / 4) + 4 half + i % 4
         const int y0 = start_of(tile);
-        const bool all = seen == 0xffffffffu && (tree ? y0 + 31 < base : y0 + 31 <= wave_first) &&
-                         (a.window <= 0 || y0 + 31 < a.n_sink || wave_last - y0 < a.window);
-        if (!all) {
+        if (seen != 0xffffffffu || y0 > whole_to || (y0 < whole_from && y0 > whole_sink)) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int k = 8 * (i / 4) + 4 * half + i % 4;
@@ -557,6 +561,7 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : 2) void hx_attend_kernel(At
             const float shrink = __builtin_amdgcn_exp2f(m - (m_new == NEG_INF ? 0.0f : m_new));
             m = m_new;
             l *= shrink;
+            l1 *= shrink;
 #pragma unroll
             for (int x = 0; x < D / 32; ++x) o[x] *= shrink;
         }
@@ -569,20 +574,17 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : 2) void hx_attend_kernel(At
             const float w0 = __builtin_amdgcn_exp2f(fmaf(s[2 * i], c, -m_use)), w1 = __builtin_amdgcn_exp2f(fmaf(s[2 * i + 1], c, -m_use));
             p.x2[i][0] = (E)w0;
             p.x2[i][1] = (E)w1;
-            l += w0 + w1;
+            l += w0;
+            l1 += w1;
         }
-        const uint4 *sv = (const uint4 *)(smem + S * C::BUF) + KT * CH;
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
 #pragma unroll
             for (int x = 0; x < D / 32; ++x) {
-                const int key = st * 16 + v_key, piece = x * 4 + v_sub;
                 using LdsPtr = __attribute__((address_space(3))) i16x4 *;
-                const char *at0 = (const char *)(sv + v_piece<CH>(key, piece)) + (lane & 1) * 8;
-                const char *at1 = at0 + 8 * CH * 16;
                 union { i16x4 h[2]; X8 x; } vf;
-                vf.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at0);
-                vf.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at1);
+                vf.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(uintptr_t)(v_lane[x] + S * C::BUF + st * 16 * CH * 16));
+                vf.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(uintptr_t)(v_lane[x] + S * C::BUF + (st * 16 + 8) * CH * 16));
                 o[x] = mfma32(vf.x, p.x8[st], o[x]);
             }
         }
@@ -592,26 +594,38 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : 2) void hx_attend_kernel(At
     using I1 = std::integral_constant<int, 1>;
     using I2 = std::integral_constant<int, 2>;
     using I3 = std::integral_constant<int, RING == 4 ? 3 : 0>;
-    if (tile0 < tile1) {
-        ask(tile0, I0{});
-        if (!C::DIRECT || tile0 + 1 < tile1) ask(tile0 + 1, I1{});
-        if (!C::DIRECT || (RING == 4 && tile0 + 2 < tile1)) ask(tile0 + 2, I2{});
+    for (seg0 = tile0; seg0 < tile1; seg0 = seg1) {
+        // the places of the next SPAN tiles, which then need not be waited for among the keys
+        seg1 = seg0 + SPAN < tile1 ? seg0 + SPAN : tile1;
+        if constexpr (PAGE16) {
+            if (seg0 > tile0) __syncthreads();
+            for (int i = tid; i < 2 * (seg1 - seg0); i += THREADS) {
+                const int y0 = start_of(seg0 + i / 2), y = y0 + (i & 1) * 16, page = page_at(y);
+                const bool all = y0 + KT <= ex.hi && (y0 >= ex.lo || y0 + KT <= a.n_sink);
+                ((int64_t *)s_off)[i] = page < 0 ? -1 : (page * page_bytes + (y & in_page) * ROW_BYTES) | (all ? 0 : 1);
+            }
+        }
+        __syncthreads();
+        ask(seg0, place(seg0), I0{});
+        if (!C::DIRECT || seg0 + 1 < seg1) ask(seg0 + 1, place(seg0 + 1), I1{});
+        if (!C::DIRECT || (RING == 4 && seg0 + 2 < seg1)) ask(seg0 + 2, place(seg0 + 2), I2{});
         now = there[0];
         if constexpr (C::DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         else {
             store(I0{});
-            ask(tile0 + 3, I0{});
+            ask(seg0 + 3, place(seg0 + 3), I0{});
         }
         __syncthreads();
         s = scores(I0{});
-    }
-    for (int tile = tile0; tile < tile1; tile += RING) {
-        one_tile(tile, I0{});
-        one_tile(tile + 1, I1{});
-        one_tile(tile + 2, I2{});
-        if constexpr (RING == 4) one_tile(tile + 3, I3{});
+        for (int tile = seg0; tile < seg1; tile += RING) {
+            one_tile(tile, I0{});
+            one_tile(tile + 1, I1{});
+            one_tile(tile + 2, I2{});
+            if constexpr (RING == 4) one_tile(tile + 3, I3{});
+        }
     }
 
+    l += l1;
     l += other_half(l);
     if (!view.alive) { m = NEG_INF; l = 0.0f; }
     if (t >= sq.nq) return;
@@ -1030,18 +1044,24 @@ int launch(hx_ctx *ctx, AttendArgs &a, hipStream_t stream)
     return hx_check_launch(ctx, "hx_attend_kernel");
 }
 
-// Parts of the keys where there are few workgroups otherwise: as many as make `want` workgroups if all sequences had the longest's
-// length, of `least` tiles at least.
-void divide(AttendArgs &a, int64_t groups, int64_t want, int max_len, int tile_keys, int least)
+// Parts of the keys where there are few workgroups otherwise: `many` workgroups if all sequences had the longest's length, but no part
+// shorter than `part` tiles unless there were not even `few` workgroups then, and none shorter than `least`.
+struct Division {
+    int64_t many, few;
+    int part, least;
+};
+void divide(AttendArgs &a, int64_t groups, const Division &d, int max_len, int tile_keys)
 {
     int64_t reach = max_len;
     if (a.window > 0 && reach > (int64_t)a.window + a.n_sink + a.max_q) reach = (int64_t)a.window + a.n_sink + a.max_q;
-    const int64_t tiles = (reach + tile_keys - 1) / tile_keys + 1;
-    int64_t chunk = (groups * tiles + want - 1) / want;
-    chunk = chunk > least ? chunk : least;
+    const int64_t tiles = (reach + tile_keys - 1) / tile_keys + 1, all = groups * tiles;
+    int64_t chunk = (all + d.many - 1) / d.many, fill = (all + d.few - 1) / d.few;
+    fill = fill < d.part ? fill : d.part;
+    chunk = chunk > fill ? chunk : fill;
+    chunk = chunk > d.least ? chunk : d.least;
     if (chunk * MAX_SPLITS < tiles) chunk = (tiles + MAX_SPLITS - 1) / MAX_SPLITS;
     a.chunk = (int)chunk;
-    a.splits = (int)((tiles + chunk - 1) / chunk);
+    a.splits = groups >= d.many / 2 ? 1 : (int)((tiles + chunk - 1) / chunk);
 }
 
 template <typename E, bool FP8, int D, int COLS>
@@ -1063,11 +1083,11 @@ int plan(hx_ctx *ctx, AttendArgs &a, int max_len, hipStream_t stream)
     const int64_t rows = (int64_t)a.max_q * a.group, pairs = (int64_t)a.n * a.kv.n_heads;
     if (rows <= 32) {
         a.row_tiles = 1;
-        divide(a, pairs, 16 * ctx->num_cu, max_len, FEW_KEYS, 8);
+        divide(a, pairs, {16 * ctx->num_cu, 16 * ctx->num_cu, 8, 8}, max_len, FEW_KEYS);
         return rows <= 16 ? launch_few<E, FP8, D, 1>(ctx, a, stream) : launch_few<E, FP8, D, 2>(ctx, a, stream);
     }
     a.row_tiles = (int)((rows + 127) / 128);
-    divide(a, pairs * a.row_tiles, 8 * ctx->num_cu, max_len, KT, 8);
+    divide(a, pairs * a.row_tiles, {16 * ctx->num_cu, 2 * ctx->num_cu, 32, 4}, max_len, KT);
     return a.kv.shift >= 4 ? launch<E, FP8, D, true>(ctx, a, stream) : launch<E, FP8, D, false>(ctx, a, stream);
 }
 
