@@ -606,13 +606,15 @@ int hx_decode_plan_greedy(hx_ctx *ctx, const hx_model *model, const hx_calls *qu
  * every ref 0 and a table of -1 with lengths 0 is the empty cache.
  *
  * Pages are taken lowest number first, in the order of the rows in the call.
- * Rows in error (out of range, listed twice -- the first counts --, lengths or
- * pages out of range) are left as they are and raise HX_ERR_INDEX in the stream
- * status; rows for which no page is left raise HX_ERR_CAPACITY and are left as
- * they are too.  Scratch: these calls allocate the first time they meet a
+ * Rows in error (out of range, listed twice -- the first counts --, lengths out
+ * of range) are left as they are and raise HX_ERR_INDEX in the stream status;
+ * rows for which no page is left raise HX_ERR_CAPACITY and are left as they are
+ * too.  An entry of a table that is no page of the pool raises HX_ERR_INDEX and
+ * is taken for -1.  Scratch: these calls allocate the first time they meet a
  * larger problem than before, in bytes that follow n_pages and the rows of the
  * call; what they allocated before stays until the context ends, so graphs
- * captured earlier stay valid.
+ * captured earlier stay valid.  A call that would have to allocate while its
+ * stream is being captured returns HX_ERR_CAPACITY: make it once before.
  */
 #define HX_F32   1     /* types of stored numbers */
 #define HX_BF16  2
@@ -718,7 +720,8 @@ int hx_kv_compact(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs *seqs, i
  *     most HX_MAX_DRAFTS queries of a sequence;
  * of those, with window > 0, the positions below n_sink and the last `window`
  * positions up to the query's own; and only where the table holds a page.
- * What is not visible to a query has no part in its result, whatever its bits.
+ * What is not visible to a query has no part in its result, whatever its bits;
+ * where values or scores that it sees are infinite or NaN, so is its result.
  * Sums, maxima and outputs are held in 32 bits; the weights exp(s - max) are
  * rounded to q's type for their product with the values.
  * A row, q_ptr, page or parent out of range raises HX_ERR_INDEX; its queries

@@ -31,6 +31,7 @@ extern "C" int hx_attend(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, con
     HX_REQUIRE(ctx, kv.rows > 0, HX_ERR_INVALID_ARG, "%d sequences asked for of none", g.n);
     HX_REQUIRE(ctx, (int64_t)g.max_q * g.n_heads <= INT32_MAX / 2 && (int64_t)g.n * kv.n_heads <= INT32_MAX, HX_ERR_SHAPE,
                "%d queries of %d heads, %d sequences", g.max_q, g.n_heads, g.n);
+    HX_REQUIRE(ctx, (int64_t)kv.max_pages << kv.shift <= INT32_MAX / 2, HX_ERR_SHAPE, "%d pages of %d tokens a row", kv.max_pages, 1 << kv.shift);
     HxDeviceGuard guard(ctx->device);
     HX_REQUIRE(ctx, guard.ok, HX_ERR_DEVICE, "cannot select device %d", ctx->device);
     hipStream_t stream = (hipStream_t)stream_;

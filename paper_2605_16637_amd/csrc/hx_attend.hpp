@@ -51,6 +51,41 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float MAX_SLACK = 8.0f;            // a running maximum is raised when a score exceeds it by this many powers of 2
 
 
+// Whether a sum of weights holds any: 0 where nothing was visible.  (By the bits: a NaN among the visible has to reach the outputs.)
+__device__ __forceinline__ bool holds_any(float l) { return hx_bits(l) << 1 != 0; }
+
+// Whether a lane's sums hold an infinity or a NaN.
+template <int N, typename F>
+__device__ __forceinline__ bool any_odd(const F *o)
+{
+    uint32_t worst = 0;
+#pragma unroll
+    for (int x = 0; x < N; ++x)
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(F) / sizeof(float)); ++i) {
+            const uint32_t size = hx_bits(o[x][i]) & 0x7fffffffu;
+            worst = size > worst ? size : worst;
+        }
+    return worst >= 0x7f800000u;
+}
+
+// N stored numbers
+template <typename E, bool FP8, int N>
+__device__ __forceinline__ void numbers(const char *from, float *to)
+{
+    if constexpr (FP8) {
+        using X2 = typename Types<E>::x2;
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            X2 a, b;
+            widen(((const uint32_t *)from)[i], a, b);
+            to[4 * i] = (float)a[0]; to[4 * i + 1] = (float)a[1]; to[4 * i + 2] = (float)b[0]; to[4 * i + 3] = (float)b[1];
+        }
+    } else
+#pragma unroll
+        for (int i = 0; i < N; ++i) to[i] = (float)((const E *)from)[i];
+}
+
 constexpr int AT_THREADS = 256;
 constexpr int MAX_SPLITS = 64;
 
@@ -249,14 +284,14 @@ __device__ __forceinline__ void join(const AttendArgs &a, const Seq &q, int pair
         for (int p = 0; p < parts; ++p) top = fmaxf(top, s[p * ROWS + r]);
         const float use = top == NEG_INF ? 0.0f : top;
         for (int p = 0; p < parts; ++p) {
-            const float y = s_l[p * ROWS + r], f = y > 0.0f ? __builtin_amdgcn_exp2f(s[p * ROWS + r] - use) : 0.0f;
+            const float y = s_l[p * ROWS + r], f = holds_any(y) ? __builtin_amdgcn_exp2f(s[p * ROWS + r] - use) : 0.0f;
             s[p * ROWS + r] = f;
             l += y * f;
         }
-        s[parts * ROWS + r] = l > 0.0f ? v_unit / l : 0.0f;
+        s[parts * ROWS + r] = holds_any(l) ? v_unit / l : 0.0f;
         if (a.lse) {
             const int row = rt * ROWS + r;
-            a.lse[(int64_t)(q.q0 + row / a.group) * a.n_heads + head * a.group + row % a.group] = l > 0.0f ? (top + __builtin_amdgcn_logf(l)) * LN2 : NEG_INF;
+            a.lse[(int64_t)(q.q0 + row / a.group) * a.n_heads + head * a.group + row % a.group] = holds_any(l) ? (top + __builtin_amdgcn_logf(l)) * LN2 : NEG_INF;
         }
     }
     __syncthreads();
@@ -268,7 +303,7 @@ __device__ __forceinline__ void join(const AttendArgs &a, const Seq &q, int pair
             const float *from = a.part + (slot0 + (int64_t)p * ROWS + r) * D + d;
             const float2 x = find(from), y = find(from + 2);
             const float f = s[p * ROWS + r];
-            if (f > 0.0f) { o.x += x.x * f; o.y += x.y * f; o.z += y.x * f; o.w += y.y * f; }
+            if (holds_any(f)) { o.x += x.x * f; o.y += x.y * f; o.z += y.x * f; o.w += y.y * f; }
         }
         const float f = s[parts * ROWS + r];
         put((E *)a.out + (int64_t)(q.q0 + row / a.group) * a.out_token + (int64_t)(head * a.group + row % a.group) * a.out_head + d, a.out_wide,
@@ -627,6 +662,39 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : D == 64 && !FP8 && PAGE16 ?
 
     l += l1;
     l += other_half(l);
+    // A weight of 0 times an infinite or NaN value is no 0: where a row's sums are not finite they are taken again key by key, from what it
+    // sees alone.
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(any_odd<D / 32>(o)) != 0 && sq.nq > 1, false)) {
+        const float m_use = m == NEG_INF ? 0.0f : m;
+#pragma unroll
+        for (int x = 0; x < D / 32; ++x) o[x] = f32x16{};
+#pragma unroll 1
+        for (int key = tile0 * KT; key < tile1 * KT; ++key) {
+            const int y = start_of(key / KT) + key % KT, page = in_sight(y) ? page_at(y) : -1;
+            if (page < 0) continue;
+            const int64_t at = page * page_bytes + (y & in_page) * ROW_BYTES;
+            float dot = 0.0f;
+#pragma unroll
+            for (int x = 0; x < D / 16; ++x) {
+                float k[8];
+                numbers<E, FP8, 8>(k_at + at + (x * 16 + half * 8) * (ROW_BYTES / D), k);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dot = fmaf((float)qf[x][i], k[i], dot);
+            }
+            dot += other_half(dot);
+            const bool see = view.sees(y);
+            const float weight = __builtin_amdgcn_exp2f(fmaf(dot, c, -m_use));
+#pragma unroll
+            for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float v[4];
+                    numbers<E, FP8, 4>(v_at + at + (x * 32 + 8 * i + 4 * half) * (ROW_BYTES / D), v);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[x][4 * i + j] += see ? weight * v[j] : 0.0f;
+                }
+        }
+    }
     if (!view.alive) { m = NEG_INF; l = 0.0f; }
     if (t >= sq.nq) return;
     if (parts > 1) {
@@ -641,7 +709,7 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : D == 64 && !FP8 && PAGE16 ?
         return;
     }
     const float v_unit = a.v_scale ? a.v_scale[a.layer * kv.n_heads + head] : 1.0f;
-    const float f = l > 0.0f ? v_unit / l : 0.0f;
+    const float f = holds_any(l) ? v_unit / l : 0.0f;
     E *to = (E *)a.out + (int64_t)(sq.q0 + t) * a.out_token + (int64_t)qhead * a.out_head;
 #pragma unroll
     for (int x = 0; x < D / 32; ++x)
@@ -649,10 +717,10 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : D == 64 && !FP8 && PAGE16 ?
         for (int i = 0; i < 4; ++i) {
             float y[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) y[j] = l > 0.0f ? o[x][4 * i + j] * f : 0.0f;
+            for (int j = 0; j < 4; ++j) y[j] = holds_any(l) ? o[x][4 * i + j] * f : 0.0f;
             put(to + x * 32 + 8 * i + 4 * half, a.out_wide, y[0], y[1], y[2], y[3]);
         }
-    if (a.lse && half == 0) a.lse[(int64_t)(sq.q0 + t) * a.n_heads + qhead] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * LN2 : NEG_INF;
+    if (a.lse && half == 0) a.lse[(int64_t)(sq.q0 + t) * a.n_heads + qhead] = holds_any(l) ? (m + __builtin_amdgcn_logf(l)) * LN2 : NEG_INF;
 }
 
 // The parts of rows put together, by D / 4 lanes a row: each has 4 of its numbers, and the maximum and sum of some of its parts.
@@ -683,7 +751,7 @@ __global__ __launch_bounds__(AT_THREADS) void hx_attend_join_kernel(AttendArgs a
     float f[KEEP], l = 0.0f;
 #pragma unroll
     for (int k = 0; k < KEEP; ++k) {
-        f[k] = ml[k].y > 0.0f ? __builtin_amdgcn_exp2f(ml[k].x - use) : 0.0f;
+        f[k] = holds_any(ml[k].y) ? __builtin_amdgcn_exp2f(ml[k].x - use) : 0.0f;
         l += ml[k].y * f[k];
     }
 #pragma unroll
@@ -702,13 +770,13 @@ __global__ __launch_bounds__(AT_THREADS) void hx_attend_join_kernel(AttendArgs a
                 const float v = __shfl(f[k], p % G, G);
                 w = p / G == k ? v : w;
             }
-            if (p < parts && w > 0.0f) { o.x += x[i].x * w; o.y += x[i].y * w; o.z += x[i].z * w; o.w += x[i].w * w; }
+            if (p < parts && holds_any(w)) { o.x += x[i].x * w; o.y += x[i].y * w; o.z += x[i].z * w; o.w += x[i].w * w; }
         }
     }
-    const float v_unit = a.v_scale ? a.v_scale[a.layer * a.kv.n_heads + head] : 1.0f, unit = l > 0.0f ? v_unit / l : 0.0f;
+    const float v_unit = a.v_scale ? a.v_scale[a.layer * a.kv.n_heads + head] : 1.0f, unit = holds_any(l) ? v_unit / l : 0.0f;
     const int qhead = head * a.group + row % a.group;
     put((E *)a.out + (int64_t)(sq.q0 + t) * a.out_token + (int64_t)qhead * a.out_head + 4 * g, a.out_wide, o.x * unit, o.y * unit, o.z * unit, o.w * unit);
-    if (a.lse && g == 0) a.lse[(int64_t)(sq.q0 + t) * a.n_heads + qhead] = l > 0.0f ? (top + __builtin_amdgcn_logf(l)) * LN2 : NEG_INF;
+    if (a.lse && g == 0) a.lse[(int64_t)(sq.q0 + t) * a.n_heads + qhead] = holds_any(l) ? (top + __builtin_amdgcn_logf(l)) * LN2 : NEG_INF;
 }
 
 // ---- few rows ----------------------------------------------------------------
@@ -952,6 +1020,46 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && (D == 64 ||
         __builtin_amdgcn_wave_barrier();
         asm volatile("" ::: "memory");
     }
+    // sums that are not finite, as above (a single query's heads all see the same keys)
+    bool odd = false;
+#pragma unroll
+    for (int w = 0; w < COLS; ++w) odd |= sq.nq > 1 && any_odd<D / 16>(o[w]);
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, false)) {
+#pragma unroll
+        for (int w = 0; w < COLS; ++w)
+#pragma unroll
+            for (int x = 0; x < D / 16; ++x) o[w][x] = f32x4{};
+#pragma unroll 1
+        for (int key = (tile0 + wave) * FEW_KEYS; key < tile1 * FEW_KEYS; key += key % FEW_KEYS == FEW_KEYS - 1 ? 3 * FEW_KEYS + 1 : 1) {
+            const int y = start_of(key / FEW_KEYS) + key % FEW_KEYS;
+            if (y >= ex.hi || (y < ex.lo && y >= a.n_sink)) continue;
+            const int page = in_pool(kv, sq.table[y >> kv.shift]);
+            if (page < 0) continue;
+            const int64_t at = page * page_bytes + (y & in_page) * ROW_BYTES;
+#pragma unroll
+            for (int w = 0; w < COLS; ++w) {
+                float dot = 0.0f;
+#pragma unroll
+                for (int x = 0; x < D / 32; ++x) {
+                    float k[8];
+                    numbers<E, FP8, 8>(k_at + at + (FP8 ? (x >> 1) * 64 + quad * 16 + (x & 1) * 8 : (x * 32 + quad * 8) * 2), k);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) dot = fmaf((float)qf[w][x][i], k[i], dot);
+                }
+                dot += lane_16_away(dot);
+                dot += other_half(dot);
+                const bool see = view[w].sees(y);
+                const float weight = __builtin_amdgcn_exp2f(fmaf(dot, c, -(m[w] == NEG_INF ? 0.0f : m[w])));
+#pragma unroll
+                for (int x = 0; x < D / 16; ++x) {
+                    float v[4];
+                    numbers<E, FP8, 4>(v_at + at + (x * 16 + 4 * quad) * (ROW_BYTES / D), v);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[w][x][j] += see ? weight * v[j] : 0.0f;
+                }
+            }
+        }
+    }
     // the four wavefronts' sums: each adds up a quarter of the numbers
 #pragma unroll
     for (int w = 0; w < COLS; ++w) {
@@ -981,7 +1089,7 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && (D == 64 ||
     for (int w = 0; w < COLS; ++w) {
         if (t[w] >= sq.nq) continue;
         const int64_t slot = ((int64_t)pair * a.splits + split) * ROWS + 16 * w + col;
-        const float unit = sum[w] > 0.0f ? v_unit / sum[w] : 0.0f;
+        const float unit = holds_any(sum[w]) ? v_unit / sum[w] : 0.0f;
 #pragma unroll
         for (int i = 0; i < D / 64; ++i) {
             const int x = wave * (D / 64) + i, d = x * 16 + 4 * quad;
@@ -993,13 +1101,13 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && (D == 64 ||
                 leave(a.part + slot * D + d + 2, y[2], y[3]);
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) y[j] = sum[w] > 0.0f ? y[j] * unit : 0.0f;
+                for (int j = 0; j < 4; ++j) y[j] = holds_any(sum[w]) ? y[j] * unit : 0.0f;
                 put((E *)a.out + (int64_t)(sq.q0 + t[w]) * a.out_token + (int64_t)qhead[w] * a.out_head + d, a.out_wide, y[0], y[1], y[2], y[3]);
             }
         }
         if (wave == 0 && quad == 0) {
             if (parts > 1) leave((float *)(a.part_ml + slot), top[w], sum[w]);
-            else if (a.lse) a.lse[(int64_t)(sq.q0 + t[w]) * a.n_heads + qhead[w]] = sum[w] > 0.0f ? (top[w] + __builtin_amdgcn_logf(sum[w])) * LN2 : NEG_INF;
+            else if (a.lse) a.lse[(int64_t)(sq.q0 + t[w]) * a.n_heads + qhead[w]] = holds_any(sum[w]) ? (top[w] + __builtin_amdgcn_logf(sum[w])) * LN2 : NEG_INF;
         }
     }
     if (parts > 1) join<E, D, ROWS>(a, sq, pair, 0, parts, (float *)smem);
@@ -1017,14 +1125,14 @@ int parts_room(hx_ctx *ctx, AttendArgs &a, int64_t tiles, int rows, int dim, boo
     const int64_t slots = tiles * a.splits * rows;
     if (counted) {
         const void *was = ctx->att_done.p;
-        if (int rc = hx_scratch(ctx, ctx->att_done, (size_t)tiles * sizeof(int))) return rc;
+        if (int rc = hx_scratch(ctx, ctx->att_done, (size_t)tiles * sizeof(int), stream)) return rc;
         if (ctx->att_done.p != was) {
             const int64_t n = ctx->att_done.cap / sizeof(int);
             hx_attend_clear_kernel<<<(int)((n + AT_THREADS - 1) / AT_THREADS), AT_THREADS, 0, stream>>>((int *)ctx->att_done.p, n);
         }
         a.done = (int *)ctx->att_done.p;
     }
-    if (int rc = hx_scratch(ctx, ctx->att, (size_t)slots * (dim * sizeof(float) + sizeof(float2)))) return rc;
+    if (int rc = hx_scratch(ctx, ctx->att, (size_t)slots * (dim * sizeof(float) + sizeof(float2)), stream)) return rc;
     a.part = (float *)ctx->att.p;
     a.part_ml = (float2 *)(a.part + slots * dim);
     return HX_OK;
@@ -1036,7 +1144,7 @@ int launch(hx_ctx *ctx, AttendArgs &a, hipStream_t stream)
     using C = Tile<FP8, D, 4, PAGE16>;
     const int lds = C::LDS + (a.parent ? TREE_BYTES : 0);
     const int64_t tiles = (int64_t)a.n * a.kv.n_heads * a.row_tiles, grid = tiles * a.splits, join_grid = tiles * (C::ROWS / (AT_THREADS / (D / 4)));
-    HX_REQUIRE(ctx, grid <= INT32_MAX && join_grid <= INT32_MAX, HX_ERR_SHAPE, "%lld workgroups", (long long)grid);
+    HX_REQUIRE(ctx, grid <= hx_most_groups(C::THREADS) && join_grid <= hx_most_groups(AT_THREADS), HX_ERR_SHAPE, "%lld workgroups", (long long)grid);
     if (a.splits > 1)
         if (int rc = parts_room(ctx, a, tiles, C::ROWS, D, false, stream)) return rc;
     hx_attend_kernel<E, FP8, D, 4, PAGE16><<<(int)grid, C::THREADS, lds, stream>>>(a);
@@ -1069,7 +1177,7 @@ int launch_few(hx_ctx *ctx, AttendArgs &a, hipStream_t stream)
 {
     const int lds = 4 * few_wave_lds(D, COLS) + (a.parent ? TREE_BYTES : 0);
     const int64_t tiles = (int64_t)a.n * a.kv.n_heads, grid = tiles * a.splits;
-    HX_REQUIRE(ctx, grid <= INT32_MAX, HX_ERR_SHAPE, "%lld workgroups", (long long)grid);
+    HX_REQUIRE(ctx, grid <= hx_most_groups(AT_THREADS), HX_ERR_SHAPE, "%lld workgroups", (long long)grid);
     if (a.splits > 1)
         if (int rc = parts_room(ctx, a, tiles, 16 * COLS, D, true, stream)) return rc;
     if (a.kv.shift >= 4) hx_attend_few_kernel<E, FP8, D, COLS, true><<<(int)grid, AT_THREADS, lds, stream>>>(a);

@@ -57,7 +57,7 @@ struct hx_ctx {
     size_t dtl_cap = 0;
     float *d_dtab = nullptr;               // decode-stage first-room tables, dtab_cap instances
     int dtab_cap = 0;
-    HxScratch kv, att, att_done, smp;      // the serving step: pages (hx_kv.hip), attention (hx_attend.hip; its counters, 0 between launches), sampling (hx_sample.hip)
+    HxScratch kv, att, att_done;           // the serving step: pages (hx_kv.hip), attention (hx_attend.hip), and its counters, which are 0 between launches
     int32_t *d_zeros = nullptr;            // 64 words that stay 0
     int num_cu = 256;
     HxDagStore dag;
@@ -86,14 +86,24 @@ inline int hx_fail(hx_ctx *ctx, int code, const char *fmt, ...)
         if (!(cond)) return hx_fail((ctx), (code), __VA_ARGS__); \
     } while (0)
 
-inline int hx_scratch(hx_ctx *ctx, HxScratch &s, size_t bytes)
+// Workgroups of `threads` that a launch may have: the runtime counts threads in 32 bits.
+constexpr int64_t hx_most_groups(int threads) { return UINT32_MAX / threads; }
+
+inline int hx_scratch(hx_ctx *ctx, HxScratch &s, size_t bytes, hipStream_t stream)
 {
     if (bytes <= s.cap) return HX_OK;
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    HX_HIP(ctx, hipStreamIsCapturing(stream, &capture));
+    HX_REQUIRE(ctx, capture == hipStreamCaptureStatusNone, HX_ERR_CAPACITY, "scratch would grow by a call that is being captured: make the call once before");
     size_t want = 2 * s.cap > ((size_t)1 << 20) ? 2 * s.cap : (size_t)1 << 20;
     want = bytes > want ? bytes : want;
     HX_REQUIRE(ctx, s.n_old < 48, HX_ERR_CAPACITY, "scratch has grown too often");
     void *p = nullptr;
-    HX_HIP(ctx, hipMalloc(&p, want));
+    const hipError_t e = hipMalloc(&p, want);
+    if (e != hipSuccess) {
+        (void)hipGetLastError();                   // not the next launch's
+        return hx_fail(ctx, HX_ERR_DEVICE, "%zu bytes of scratch: %s", want, hipGetErrorString(e));
+    }
     if (s.p) s.old[s.n_old++] = s.p;
     s.p = p;
     s.cap = want;

@@ -444,7 +444,6 @@ extern "C" int hx_ctx_destroy(hx_ctx *ctx)
     hx_scratch_release(ctx->kv);
     hx_scratch_release(ctx->att);
     hx_scratch_release(ctx->att_done);
-    hx_scratch_release(ctx->smp);
     delete ctx;
     return HX_OK;
 }

@@ -36,7 +36,7 @@ __device__ __forceinline__ int64_t block_before(int64_t x, int64_t *s, int64_t *
     return before + sum - x;
 }
 
-// The first `want` pages with ref == 0 (USED: > 0) from page `from` on and before `to`, into list; returns how many there are, at most `want`.
+// The first `want` pages that are free, ref <= 0 (USED: in use), from page `from` on and before `to`, into list; returns how many there are, at most `want`.
 // A wavefront looks at 8 x 64 neighbouring pages at a time, the workgroup at 8192.
 constexpr int SCAN_EACH = 8;
 template <bool USED>
@@ -53,7 +53,7 @@ __device__ int first_pages(const int32_t *ref, int from, int to, int want, int32
         int count = 0;
 #pragma unroll
         for (int j = 0; j < SCAN_EACH; ++j) {
-            m[j] = __builtin_amdgcn_ballot_w64(USED ? r[j] > 0 : r[j] == 0);
+            m[j] = __builtin_amdgcn_ballot_w64((r[j] > 0) == USED);
             count += __builtin_popcountll(m[j]);
         }
         int64_t all;
@@ -117,7 +117,7 @@ __global__ __launch_bounds__(PL_THREADS) void hx_kv_fork_plan_kernel(ForkArgs a)
             if (t < 0) bad = true;
             if (t > 0 && (t & ((1 << kv.shift) - 1))) {
                 page = hx_row(kv, r)[t >> kv.shift];
-                if (page >= kv.n_pages) { bad = true; t = -1; }
+                if (page >= kv.n_pages) { bad = true; page = -1; }
             }
         }
         int64_t all;
@@ -262,7 +262,7 @@ __device__ __forceinline__ uint32_t to_e4m3(const float *x, float scale)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         y[i] = x[i] / scale;
-        nan[i] = (__float_as_uint(y[i]) & 0x7fffffffu) > 0x7f800000u;
+        nan[i] = (hx_bits(y[i]) & 0x7fffffffu) > 0x7f800000u;
         y[i] = fminf(fmaxf(y[i], -448.0f), 448.0f);
     }
     uint32_t w = 0;
@@ -349,8 +349,10 @@ __device__ bool keep_check(const KeepArgs &a, int i, int *s_bad)
     const KvView &kv = a.kv;
     if (threadIdx.x == 0) *s_bad = 0;
     __syncthreads();
-    const int r = a.row[i], nd = a.n_draft[i], k0 = a.keep_ptr[i], k1 = a.keep_ptr[i + 1], m = k1 - k0;
-    bool bad = r < 0 || r >= kv.rows || nd < 0 || k0 < 0 || m < 0 || m > nd || k1 > a.n_keep;
+    const int r = a.row[i], nd = a.n_draft[i], k0 = a.keep_ptr[i], k1 = a.keep_ptr[i + 1];
+    bool bad = r < 0 || r >= kv.rows || nd < 0 || k0 < 0 || k1 < k0 || k1 > a.n_keep;
+    const int m = bad ? 0 : k1 - k0;
+    bad |= m > nd;
     int len = 0;
     if (!bad) {
         len = kv.len[r];
@@ -544,7 +546,7 @@ int blocks_for(int64_t items, int threads, int64_t most)
     if (n == 0) return HX_OK;                                                                       \
     HX_REQUIRE(ctx, what_ok, HX_ERR_INVALID_ARG, "NULL array");                                     \
     HX_REQUIRE(ctx, kv.rows > 0, HX_ERR_INVALID_ARG, "%d rows asked for of no sequences", n);       \
-    HX_REQUIRE(ctx, (int64_t)n * (groups) <= INT32_MAX, HX_ERR_SHAPE, "%d rows of %d layers in one call", n, kv.n_layers); \
+    HX_REQUIRE(ctx, (int64_t)n * (groups) <= hx_most_groups(CP_THREADS), HX_ERR_SHAPE, "%d rows of %d layers in one call", n, kv.n_layers); \
     hipStream_t stream = (hipStream_t)stream_
 
 #define HX_KV_DEVICE(ctx)                                                                           \
@@ -558,7 +560,7 @@ extern "C" int hx_kv_fork(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs 
     HX_KV_BEGIN(ctx, src && dst, 1 + 2 * kv.n_layers);
     const int parts = 1 + 2 * kv.n_layers;
     HX_KV_DEVICE(ctx);
-    if (int rc = hx_scratch(ctx, ctx->kv, ((size_t)kv.rows + 4 * (size_t)n) * sizeof(int32_t))) return rc;
+    if (int rc = hx_scratch(ctx, ctx->kv, ((size_t)kv.rows + 4 * (size_t)n) * sizeof(int32_t), stream)) return rc;
     int32_t *w = (int32_t *)ctx->kv.p;
     ForkArgs a{kv, n, src, dst, n_tok, w, w + kv.rows, w + kv.rows + n, w + kv.rows + 2 * (size_t)n, w + kv.rows + 3 * (size_t)n,
                pool->head_dim * hx_type_size(pool->dtype)};
@@ -573,7 +575,7 @@ extern "C" int hx_kv_grow(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs 
     if (!ctx) return HX_ERR_INVALID_ARG;
     HX_KV_BEGIN(ctx, row && n_new, 1);
     HX_KV_DEVICE(ctx);
-    if (int rc = hx_scratch(ctx, ctx->kv, ((size_t)kv.rows + 2 * (size_t)n + kv.n_pages) * sizeof(int32_t))) return rc;
+    if (int rc = hx_scratch(ctx, ctx->kv, ((size_t)kv.rows + 2 * (size_t)n + kv.n_pages) * sizeof(int32_t), stream)) return rc;
     int32_t *w = (int32_t *)ctx->kv.p;
     GrowArgs a{kv, n, row, n_new, w, w + kv.rows, w + kv.rows + n, w + kv.rows + 2 * (size_t)n};
     hx_kv_grow_kernel<<<1, PL_THREADS, 0, stream>>>(a);
@@ -595,7 +597,7 @@ extern "C" int hx_kv_write(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, c
     const bool aligned = (((uintptr_t)k | (uintptr_t)v) & 15) == 0 && token_stride % 8 == 0 && head_stride % 8 == 0;
     WriteArgs a{kv, layer, n, n_tok, row, tok_ptr, k, v, token_stride, head_stride, pool->k_scale, pool->v_scale, aligned};
     const int64_t blocks = ((int64_t)n_tok * (kv.dim / 8) * kv.n_heads + CP_THREADS - 1) / CP_THREADS;
-    HX_REQUIRE(ctx, blocks <= INT32_MAX, HX_ERR_SHAPE, "%d tokens in one call", n_tok);
+    HX_REQUIRE(ctx, blocks <= hx_most_groups(CP_THREADS), HX_ERR_SHAPE, "%d tokens in one call", n_tok);
     const int grid = (int)blocks;
     HX_KV_DEVICE(ctx);
 #define HX_WRITE(S)                                                                                              \
@@ -618,7 +620,7 @@ extern "C" int hx_kv_keep(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs 
     HX_REQUIRE(ctx, n_keep == 0 || keep, HX_ERR_INVALID_ARG, "NULL array");
     const int parts = 2 * kv.n_layers;
     HX_KV_DEVICE(ctx);
-    if (int rc = hx_scratch(ctx, ctx->kv, (size_t)n * sizeof(int32_t))) return rc;
+    if (int rc = hx_scratch(ctx, ctx->kv, (size_t)n * sizeof(int32_t), stream)) return rc;
     KeepArgs a{kv, n, n_keep, row, n_draft, keep_ptr, keep, (int32_t *)ctx->kv.p, pool->head_dim * hx_type_size(pool->dtype)};
     hx_kv_keep_move_kernel<<<n * parts, CP_THREADS, 0, stream>>>(a);
     hx_kv_keep_apply_kernel<<<n, CP_THREADS, 0, stream>>>(a);
@@ -646,7 +648,7 @@ extern "C" int hx_kv_compact(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_se
     HX_REQUIRE(ctx, guard.ok, HX_ERR_DEVICE, "cannot select device %d", ctx->device);
     hipStream_t stream = (hipStream_t)stream_;
     const size_t P = kv.n_pages;
-    if (int rc = hx_scratch(ctx, ctx->kv, (4 + 3 * P) * sizeof(int32_t))) return rc;
+    if (int rc = hx_scratch(ctx, ctx->kv, (4 + 3 * P) * sizeof(int32_t), stream)) return rc;
     int32_t *w = (int32_t *)ctx->kv.p;
     const int64_t page_bytes = ((int64_t)kv.n_heads << kv.shift) * kv.dim * hx_type_size(pool->dtype);
     CompactArgs a{kv, w, w + 4, w + 4 + P, moved ? moved : w + 4 + 2 * P, n_used, page_bytes};

@@ -34,7 +34,7 @@ __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__bf16 x) { return (float)x; }
 __device__ __forceinline__ float to_float(_Float16 x) { return (float)x; }
 
-__device__ __forceinline__ bool is_nan(float x) { return (__float_as_uint(x) & 0x7fffffffu) > 0x7f800000u; }
+__device__ __forceinline__ bool is_nan(float x) { return (hx_bits(x) & 0x7fffffffu) > 0x7f800000u; }
 
 // unsigned keys in the order of the numbers; the two zeros are one
 __device__ __forceinline__ uint32_t key_of(float x)
@@ -49,7 +49,7 @@ constexpr uint32_t KEY_BARRED = 0x007fffffu;       // of -infinity; a NaN's is m
 // floor(f * w) for 0 <= f < 1; *rest: whether something was cut off
 __device__ __forceinline__ uint64_t scaled(float f, uint64_t w, bool *rest)
 {
-    const uint32_t b = __float_as_uint(f), e = b >> 23;
+    const uint32_t b = __float_as_uint(f) & 0x7fffffffu, e = b >> 23;         // (f may be -0)
     const uint64_t m = (b & 0x7fffffu) | (e ? 0x800000u : 0u);
     const int shift = 150 - (int)(e ? e : 1);               // f = m 2^-shift, shift >= 24
     const uint64_t lo = m * w, hi = __umul64hi(m, w);
@@ -672,6 +672,7 @@ extern "C" int hx_sample(hx_ctx *ctx, int32_t n_rows, int32_t n_vocab, int32_t d
     HX_REQUIRE(ctx, n_vocab > 0, HX_ERR_INVALID_ARG, "rows without a logit");
     HX_REQUIRE(ctx, logits && u && token, HX_ERR_INVALID_ARG, "NULL array");
     HX_REQUIRE(ctx, ((uintptr_t)logits & (hx_type_size(dtype) - 1)) == 0, HX_ERR_INVALID_ARG, "logits are not aligned to their type");
+    HX_REQUIRE(ctx, n_rows <= hx_most_groups(SA_THREADS), HX_ERR_SHAPE, "%d rows in one call", n_rows);
     HxDeviceGuard guard(ctx->device);
     HX_REQUIRE(ctx, guard.ok, HX_ERR_DEVICE, "cannot select device %d", ctx->device);
     hipStream_t stream = (hipStream_t)stream_;

@@ -146,6 +146,27 @@ def test_write_rounds_to_the_pools_type(ctx, src, type_, wide):
     same(model, pool, seqs)
 
 
+@pytest.mark.parametrize("src", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("type_", ["bf16", "f16", "e4m3"])
+def test_write_of_infinities_and_nan(ctx, src, type_):
+    import torch
+    model, pool, seqs = make_cache(16, [8], 8, layers=1, heads=1, dim=16, type_=type_)
+    x = torch.zeros(8, 1, 16)
+    x[0, 0, :6] = torch.tensor([float("inf"), -float("inf"), float("nan"), 1.0, -1.0, 0.0])
+    x[1, 0, 5], x[7, 0, 15], x[7, 0, 3] = float("nan"), -float("inf"), 2.0
+    x = x.to(sh.torch_type(src)).cuda()
+    x[2, 0, 4] = -x[0, 0, 2]
+    ctx.hx_kv_write(pool, 0, seqs, sh.i32([0]), sh.i32([0, 8]), x, -x)
+    assert status(ctx) == 0
+    page = int(model.table[0, 0])
+    for mine, given in ((pool["k"], x), (pool["v"], -x)):
+        want = given.float()
+        if type_ == "e4m3":
+            want = torch.where(want.isnan(), want, want.clamp(-448, 448))
+        got = mine[0, page, 0].float()
+        assert torch.equal(got.isnan(), want[:, 0].isnan()) and torch.equal(got.nan_to_num(9, 8, -8), want[:, 0].nan_to_num(9, 8, -8))
+
+
 def test_write_does_not_touch_what_others_hold_or_what_is_not_there(ctx):
     import torch
     model, pool, seqs = make_cache(8, [16, 12], 8, heads=1, dim=16)
@@ -222,6 +243,36 @@ def test_compact_moves_pages_down(ctx, n, spare, T):
     same(model, pool, seqs)
     ctx.hx_kv_compact(pool, seqs)
     assert status(ctx) == 0
+    same(model, pool, seqs)
+
+
+def test_keep_of_bounds_that_are_none(ctx):
+    """Ends of a row's list that lie before its start, by so much that their difference passes 32 bits."""
+    model, pool, seqs = make_cache(13, [24, 30], 8)
+    for ptr in ([2147483647, -2147483647, -2147483647], [2, 0, 1], [-5, 1, 1], [0, 2147483647, -2147483648], [-2147483648, 2147483647, 3]):
+        ctx.hx_kv_keep(pool, seqs, sh.i32([0, 1]), sh.i32([0, 0]), sh.i32(ptr), sh.i32([0, 1, 2]))
+        assert status(ctx) == -6
+    same(model, pool, seqs)
+
+
+def test_counts_below_none_are_free_pages(ctx):
+    model, pool, seqs = make_cache(14, [24, 30, 5], 8, spare=6)
+    low = np.nonzero(model.ref == 0)[0][:3]
+    pool["ref"][sh.i32(low).long()] = -7
+    model.compact()
+    ctx.hx_kv_compact(pool, seqs)
+    assert status(ctx) == 0
+    assert np.array_equal(seqs["table"].cpu().numpy(), model.table) and np.array_equal(np.maximum(pool["ref"].cpu().numpy(), 0), model.ref)
+
+
+def test_fork_of_entries_that_are_no_pages(ctx):
+    model, pool, seqs = make_cache(15, [30, 16], 8, rows=6)
+    seqs["table"][0, 1] = seqs["table"][0, 3] = len(model.ref)
+    ctx.hx_kv_fork(pool, seqs, sh.i32([0, 1]), sh.i32([4, 5]))
+    assert status(ctx) == -6
+    model.table[0, 1] = model.table[0, 3] = -1
+    model.fork([0, 1], [4, 5])
+    model.table[0, 1] = model.table[0, 3] = len(model.ref)
     same(model, pool, seqs)
 
 
@@ -461,6 +512,101 @@ def test_nothing_to_do(ctx):
     assert status(ctx) == 0
 
 
+def attend_out(ctx, k, v, table, length, ptr, q, T, **more):
+    """(out, lse) in 64 bits of one call over layer 0 of a bf16 or fp16 cache."""
+    import torch
+    out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda:0")
+    ctx.hx_attend(dict(k=k, v=v, ref=sh.i32(np.ones(k.shape[1]))), 0, dict(table=table, len=length), ptr, q, out, max_q=int(ptr.diff().max()), lse=lse, **more)
+    return out.float().cpu().numpy().astype(np.float64), lse.cpu().numpy().astype(np.float64)
+
+
+@pytest.mark.parametrize("type_", ["bf16", "f16"])
+@pytest.mark.parametrize("dim,group,nq,T,is_tree", [(64, 1, 9, 16, False), (64, 4, 60, 16, False), (128, 2, 16, 8, False), (128, 4, 70, 32, False), (128, 3, 5, 16, True),
+                                                    (128, 4, 40, 16, True), (256, 2, 14, 16, True), (256, 4, 33, 4, False), (64, 2, 300, 16, False)])
+def test_infinite_and_nan_values_that_some_queries_do_not_see(ctx, type_, dim, group, nq, T, is_tree):
+    """Keys and values of some positions are replaced; rows that do not see these keep their results, the others' follow the formula."""
+    import torch
+    n = nq + 700
+    rng = np.random.default_rng(nq)
+    g = torch.Generator().manual_seed(nq)
+    t = sh.torch_type(type_)
+    pages = -(-n // T)
+    k, v = (torch.randn(1, pages, 1, T, dim, generator=g).to(t).cuda() for _ in range(2))
+    q = torch.randn(nq, group, dim, generator=g).to(t).cuda()
+    table, length, ptr = sh.i32(rng.permutation(pages)[None]), sh.i32([n]), sh.i32([0, nq])
+    parent = tree(rng, nq, 5, 2) if is_tree else None
+    window, sinks = 600, 3
+    more = dict(window=window, n_sink=sinks, parent=None if parent is None else sh.i32(parent))
+    see = sh.visible(n, nq, parent, window, sinks)
+    was, was_lse = attend_out(ctx, k, v, table, length, ptr, q, T, **more)
+    # each within (half a step of the weights + of the output, and sums in 32 bits) of the exact result, at most the largest |value|
+    near = 2 * (2 * sh.HALF_STEP[type_] + 2.0 ** -12) * float(v.float().abs().max())
+    place = table[0].cpu().numpy()
+    seen_by_some = np.nonzero(see.any(0) & ~see[see.any(1)].all(0))[0]
+    assert len(seen_by_some)
+    unseen = np.nonzero(~see.any(0))[0][-1:].tolist()
+    odd = sorted(set([int(seen_by_some[0]), int(seen_by_some[len(seen_by_some) // 4]), int(seen_by_some[-1])] + [int(x) for x in unseen]))
+    for what in (float("inf"), float("-inf"), float("nan")):
+        v2 = v.clone()
+        for y in odd:
+            v2[0, place[y // T], 0, y % T, 1::3] = what
+        got, lse = attend_out(ctx, k, v2, table, length, ptr, q, T, **more)
+        hit = see[:, odd].any(1)
+        assert (~hit).any() or is_tree
+        assert np.array_equal(lse, was_lse)
+        assert (np.abs(got - was)[~hit] <= near).all()
+        plain = np.ones(dim, bool)
+        plain[1::3] = False
+        assert (np.abs(got - was)[hit][..., plain] <= near).all()
+        x = got[hit][..., ~plain]
+        assert np.isnan(x).all() if what != what else (x == what).all()
+    k2 = k.clone()
+    for y in odd:
+        k2[0, place[y // T], 0, y % T] = float("nan")
+        v2[0, place[y // T], 0, y % T] = float("nan")
+    got, lse = attend_out(ctx, k2, v2, table, length, ptr, q, T, **more)
+    assert np.isnan(got[hit]).all() and np.isnan(lse[hit]).all()
+    # (how far a maximum has been raised goes by the rows beside it: sums of n weights in 32 bits, twice)
+    sums = 2 * (n + 64) * 2.0 ** -24 * np.maximum(1.0, np.abs(was_lse[~hit], where=np.isfinite(was_lse[~hit]), out=np.zeros_like(was_lse[~hit])))
+    near_lse = (lse[~hit] == was_lse[~hit]) | (np.abs(np.where(np.isfinite(lse[~hit]), lse[~hit], 0) - np.where(np.isfinite(was_lse[~hit]), was_lse[~hit], 0)) <= sums)
+    assert (np.abs(got - was)[~hit] <= near).all() and near_lse.all() and np.array_equal(np.isinf(lse[~hit]), np.isinf(was_lse[~hit]))
+    assert status(ctx) == 0
+
+
+def test_a_single_token_that_sees_no_number(ctx):
+    import torch
+    g = torch.Generator().manual_seed(1)
+    for n in (5, 3000):
+        k, v = (torch.randn(1, -(-n // 16), 2, 16, 64, generator=g).to(torch.bfloat16).cuda() for _ in range(2))
+        q = torch.randn(1, 4, 64, generator=g).to(torch.bfloat16).cuda()
+        k[0, 0, 1, 2] = float("nan")
+        got, lse = attend_out(ctx, k, v, sh.i32(np.arange(-(-n // 16))[None]), sh.i32([n]), sh.i32([0, 1]), q, 16)
+        assert np.isfinite(got[0, :2]).all() and np.isfinite(lse[0, :2]).all() and np.isnan(got[0, 2:]).all() and np.isnan(lse[0, 2:]).all()
+
+
+def test_scratch_does_not_grow_while_a_stream_is_captured():
+    import torch
+    from paper_2605_16637_amd import binding
+    c = binding.Context(0)
+    model, pool, seqs = make_cache(31, [9, 4], 8, rows=4)
+    begin = [x.clone() for x in (seqs["table"], seqs["len"], pool["ref"])]
+    row, one = sh.i32([0, 1]), sh.i32([1, 9])
+    graph, x = torch.cuda.CUDAGraph(), torch.zeros(8, device="cuda:0")
+    with torch.cuda.graph(graph):
+        x += 1
+        with pytest.raises(binding.HxError) as e:
+            c.hx_kv_grow(pool, seqs, row, one)
+    assert e.value.code == -4
+    graph.replay()
+    torch.cuda.synchronize()
+    assert float(x[0]) == 1 and all(torch.equal(a, b) for a, b in zip(begin, (seqs["table"], seqs["len"], pool["ref"])))
+    c.hx_kv_grow(pool, seqs, row, one)
+    model.grow([0, 1], [1, 9])
+    assert status(c) == 0
+    same(model, pool, seqs)
+    c.close()
+
+
 # ---- sampling ------------------------------------------------------------------------------------------------------------
 
 def check_sample(ctx, x, u, type_="f32", T=None, k=None, p=None, mp=None, pad=0):
@@ -557,6 +703,15 @@ def test_sample_no_numbers_and_settings_out_of_range(ctx):
         ctx.hx_sample(sh.dev(x.astype(np.float32)), f("u", 0.5), token, temperature=f("T", 1.0), top_p=f("p", 1.0), min_p=f("mp", 0.0), logprob=logprob, n_kept=kept)
         assert status(ctx) == -1
         assert int(token[0]) == -1 and int(kept[0]) == 0 and float(logprob[0]) == -np.inf and int(token[1]) >= 0 and int(kept[1]) == 700
+
+
+def test_sample_of_a_negative_zero(ctx):
+    rng = np.random.default_rng(9)
+    x = rng.normal(0, 2, (3, 900))
+    x[:, :4] = -np.inf
+    for type_ in ("f32", "bf16"):
+        assert check_sample(ctx, x, [-0.0] * 3, type_, p=[-0.0, 0.9, 1.0], mp=[-0.0] * 3)[0] == 0
+        assert check_sample(ctx, x, [-0.0] * 3, type_, T=[-0.0, 1.0, 0.5])[0] == 0
 
 
 def test_sample_many_rows_and_a_large_vocabulary(ctx):

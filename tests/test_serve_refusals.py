@@ -130,6 +130,18 @@ def test_sampling_that_is_refused(lib):
     assert b"aligned" in (call(logits=a + 2) and lib.hx_last_error(ctx))
 
 
+def test_calls_too_large_to_launch_and_rows_too_long(lib):
+    """Launches count threads in 32 bits; nothing of such a call is begun."""
+    lib, ctx = lib
+    a = 4096
+    big = C.byref(pool(n_layers=32)), C.byref(seqs())
+    assert lib.hx_kv_fork(ctx, *big, 300000, a, a, None, None) == SHAPE                       # 65 workgroups of 256 each
+    assert lib.hx_kv_keep(ctx, *big, 300000, a, a, a, a, 3, None) == SHAPE
+    assert lib.hx_kv_free(ctx, *big, 1 << 24, a, None, None, None) == SHAPE
+    assert lib.hx_sample(ctx, 1 << 22, 100, binding.HX_F32, a, C.c_int64(100), None, None, None, None, a, a, None, None, None) == SHAPE
+    assert lib.hx_attend(ctx, C.byref(pool(page_tokens=1024)), 0, C.byref(seqs(max_pages=1 << 20)), C.byref(attend_args()), None) == SHAPE
+
+
 def test_structures_match_the_header(tmp_path):
     import os
     import subprocess
