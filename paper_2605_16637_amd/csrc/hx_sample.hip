@@ -11,11 +11,12 @@ namespace {
 
 constexpr int SA_THREADS = 1024;
 constexpr int SA_WAVES = SA_THREADS / HX_WAVE;
-constexpr int SA_UNROLL = 4;                      // pieces of 16 bytes a lane adds up before the wavefront does
+constexpr int SA_UNROLL = 4;                      // pieces of 16 bytes a lane has under way, and adds up before the wavefront does
 constexpr int SA_STEP = SA_UNROLL * HX_WAVE;
 constexpr int SA_BINS = 1408, SA_COLS = 4;        // 32 bins to a factor of 2 in weight, 44 factors; a bin's sum lies in 4 places, a lane's by its number
 constexpr int SA_LIST = 1792;                     // elements of the limit's bin that are looked at in LDS
 constexpr int SA_FEW = 128;                       // of them, those that are compared with each other
+constexpr int SA_SHORT = 512;                     // elements that are all that can stay: what follows looks at them alone
 
 struct SampleArgs {
     int n_rows, n_vocab, qbits;
@@ -67,6 +68,7 @@ struct Shared {
     uint64_t hist[SA_BINS * SA_COLS];          // and the sums of locate()
     uint32_t lkey[SA_LIST];
     int lidx[SA_LIST];
+    uint4 edge[2];                             // the row's first and last 16 bytes, without what is not of the row
     double tab[32];                            // 2^(j / 32)
     uint64_t wave[SA_WAVES];
     int wmin[SA_WAVES], wmax[SA_WAVES];
@@ -127,68 +129,84 @@ struct Row {
     using R = Raw<E>;
     static constexpr int EACH = R::EACH;
     const E *p;
+    const uint4 *base, *edge;
     int n, skip;              // elements; those of the first piece that lie before the row
     int per, pieces;
     bool nans;                // some element is no number
 
-    __device__ void set(const E *at, int count)
+    __device__ void set(const E *at, int count, uint4 *s_edge)
     {
         p = at;
         n = count;
         nans = false;
         skip = (int)(((uintptr_t)at & 15) / sizeof(E));
+        base = (const uint4 *)(p - skip);
+        edge = s_edge;
         pieces = (int)(((int64_t)n + skip + EACH - 1) / EACH);
         const int64_t w = ((int64_t)pieces + SA_WAVES - 1) / SA_WAVES;
         per = (int)((w + SA_STEP - 1) / SA_STEP * SA_STEP);
+        if (threadIdx.x % HX_WAVE == 0 && threadIdx.x < 2 * HX_WAVE) s_edge[threadIdx.x / HX_WAVE] = by_element(threadIdx.x ? pieces - 1 : 0);
+        __syncthreads();
     }
-    // piece c as it is stored; -infinity for what is not of the row, and for a NaN
-    __device__ __forceinline__ void load_any(int c, uint32_t *w) const
+    // piece c, -infinity for what is not of the row
+    __device__ __forceinline__ uint4 by_element(int c) const
     {
         const int64_t first = (int64_t)c * EACH - skip;
+        uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = R::BARRED;
 #pragma unroll
         for (int j = 0; j < EACH; ++j)
             if (first + j >= 0 && first + j < n) {
                 const E x = p[first + j];
-                if (is_nan(to_float(x)) && nans) continue;
                 if constexpr (sizeof(E) == 4) w[j] = __float_as_uint(x);
                 else {
                     const uint32_t y = __builtin_bit_cast(uint16_t, x);
                     w[j / 2] = j & 1 ? (w[j / 2] & 0xffffu) | y << 16 : (w[j / 2] & 0xffff0000u) | y;
                 }
             }
-    }
-    // piece at + lane
-    __device__ __forceinline__ uint4 load(int at) const
-    {
-        const int lane = threadIdx.x & 63;
-        if ((int64_t)at * EACH >= skip && (int64_t)(at + HX_WAVE) * EACH - skip <= n && !nans)      // the same for all lanes
-            return *((const uint4 *)(p - skip) + at + lane);
-        uint32_t w[4];
-        load_any(at + lane, w);
         return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    // piece c; -infinity for what is not of the row, and for a NaN
+    __device__ __forceinline__ uint4 load(int c) const
+    {
+        uint4 v = make_uint4(R::BARRED, R::BARRED, R::BARRED, R::BARRED);
+        if (c > 0 && c < pieces - 1) v = base[c];
+        else if (c == 0 || c == pieces - 1) v = edge[c != 0];
+        if (nans) {
+            uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int j = 0; j < EACH; ++j)
+                if (is_nan(R::get(w, j))) {
+                    if constexpr (sizeof(E) == 4) w[j] = R::BARRED;
+                    else w[j / 2] = j & 1 ? (w[j / 2] & 0xffffu) | (R::BARRED & 0xffff0000u) : (w[j / 2] & 0xffff0000u) | (R::BARRED & 0xffffu);
+                }
+            v = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        return v;
     }
     static __device__ __forceinline__ uint32_t key(const uint32_t *w, int j) { return key_of(R::get(w, j)); }
     __device__ __forceinline__ int index(int c, int j) const { return c * EACH - skip + j; }
-    // f(number of the piece, piece) for all pieces of this wavefront, a lane's next two being asked for meanwhile; done(step) after
+    // f(number of the piece, piece) for all pieces of this wavefront, a lane's next SA_UNROLL being asked for meanwhile; done(step) after
     // each SA_UNROLL of them
     template <typename F, typename D>
     __device__ __forceinline__ void each(F f, D done) const
     {
         const int lane = threadIdx.x & 63, c0 = (threadIdx.x >> 6) * per, end = c0 + per < pieces ? c0 + per : pieces;
-        uint4 now = make_uint4(0, 0, 0, 0), next = now;
-        if (c0 < end) now = load(c0);
-        if (c0 + HX_WAVE < end) next = load(c0 + HX_WAVE);
+        uint4 v[SA_UNROLL];
+#pragma unroll
+        for (int i = 0; i < SA_UNROLL; ++i)
+            if (c0 + i * HX_WAVE < end) v[i] = load(c0 + i * HX_WAVE + lane);
 #pragma unroll 1
-        for (int at = c0; at < c0 + per; at += HX_WAVE) {
-            if (at < end) {
-                const uint32_t w[4] = {now.x, now.y, now.z, now.w};
-                now = next;
-                if (at + 2 * HX_WAVE < end) next = load(at + 2 * HX_WAVE);
-                f(at + lane, w);
-            }
-            if ((at - c0) % SA_STEP == SA_STEP - HX_WAVE) done((at - c0) / SA_STEP);
+        for (int at = c0; at < c0 + per; at += SA_STEP) {
+#pragma unroll
+            for (int i = 0; i < SA_UNROLL; ++i)
+                if (at + i * HX_WAVE < end) {
+                    const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                    f(at + i * HX_WAVE + lane, w);
+                    if (at + SA_STEP + i * HX_WAVE < end) v[i] = load(at + SA_STEP + i * HX_WAVE + lane);
+                }
+            done((at - c0) / SA_STEP);
         }
     }
     template <typename F>
@@ -221,29 +239,30 @@ struct Limit {
 };
 
 // Weights of a row: 2^q exp((x - top) / T) = 2^q 2^(z / 32).  z's whole part picks a number of the table and the exponent, the rest,
-// |f| <= 1/2, goes through the series of exp(f ln 2 / 32) up to f^5: 2^-48 of the weight.
+// |f| <= 1/2, goes through the series of exp(f ln 2 / 32) up to f^5: 2^-48 of the weight.  Without branches, so that several elements' steps
+// lie beside each other.
 struct Weights {
     double top, inv;          // 32 log2(e) / T
     const double *tab;
     int q;
-    bool boundless;           // the largest is +infinity, which takes all the weight
+    bool boundless;           // the largest is +infinity, which takes all the weight: top 0 and inv 1, and all others as if -infinity
     uint32_t hi;
 
-    __device__ __forceinline__ double reach(uint32_t k) const { return fmax(((double)of_key(k) - top) * inv, -1.0e6); }
-    __device__ __forceinline__ int bin(uint32_t k) const
+    // a logit as the functions below take it
+    __device__ __forceinline__ float logit(float x) const { return boundless ? (x == __builtin_inff() ? 0.0f : -__builtin_inff()) : x; }
+    // z; weights of 2^-1000 and less are one
+    __device__ __forceinline__ double reach(float x) const { return fmax(((double)x - top) * inv, -32000.0); }
+    __device__ __forceinline__ int bin(float x) const
     {
-        if (boundless) return k == hi ? 0 : SA_BINS - 1;
-        const int b = -(int)__builtin_bit_cast(uint64_t, reach(k) + 6755399441055744.0);     // 1.5 2^52: the nearest whole number in the low bits
+        const int b = -(int)__builtin_bit_cast(uint64_t, reach(x) + 6755399441055744.0);     // 1.5 2^52: the nearest whole number in the low bits
         return b < SA_BINS - 1 ? b : SA_BINS - 1;
     }
+    __device__ __forceinline__ int bin(uint32_t k) const { return bin(logit(of_key(k))); }
     // the weight, and its bin
-    __device__ __forceinline__ double scaled(uint32_t k, int *b) const
+    __device__ __forceinline__ double scaled(uint32_t k, int *b) const { return scaled(logit(of_key(k)), b); }
+    __device__ __forceinline__ double scaled(float x, int *b) const
     {
-        if (boundless) {
-            *b = k == hi ? 0 : SA_BINS - 1;
-            return k == hi ? __builtin_ldexp(1.0, q) : 0.0;
-        }
-        const double z = reach(k), t = z + 6755399441055744.0, f = z - (t - 6755399441055744.0);
+        const double z = reach(x), t = z + 6755399441055744.0, f = z - (t - 6755399441055744.0);
         const int n = (int)__builtin_bit_cast(uint64_t, t);
         double p = 3.9737099845494154e-11;                    // (ln 2 / 32)^5 / 5!
         p = __builtin_fma(p, f, 9.172562701824643e-09);
@@ -252,17 +271,53 @@ struct Weights {
         p = __builtin_fma(p, f, 2.166084939249829e-02);
         p = __builtin_fma(p, f, 1.0);
         *b = -n < SA_BINS - 1 ? -n : SA_BINS - 1;
-        return __builtin_ldexp(p * tab[n & 31], (n >> 5) + q);
+        // 2^(n / 32 + q): the exponent goes into the table's number
+        const uint64_t power = __builtin_bit_cast(uint64_t, tab[n & 31]) + ((uint64_t)(uint32_t)((n >> 5) + q) << 52);
+        return p * __builtin_bit_cast(double, power);
     }
     // to the nearest whole number; it is below 2^51
     static __device__ __forceinline__ uint64_t whole(double w) { return __builtin_bit_cast(uint64_t, w + 4503599627370496.0) & 0xfffffffffffffull; }
     __device__ __forceinline__ uint64_t mass(uint32_t k) const { int b; return whole(scaled(k, &b)); }
 };
 
-// The lowest element at which the sum of `mass` in the order of the numbers exceeds target(total); -1: nowhere.  mass(key,
-// number, &in) says whether the element counts, *count how many do.
+// Which elements a limit leaves, by one comparison each: up to the limit's piece those from its logit on, after it those beyond.  Only the
+// piece itself is looked at number by number.
+template <typename E>
+struct Cut {
+    Limit lim;
+    float from, beyond;
+    int piece;
+    __device__ __forceinline__ Cut(const Row<E> &row, const Limit &l)
+        : lim(l), from(of_key(l.key)), beyond(of_key(l.key + 1)), piece(l.idx == 0x7fffffff ? l.idx : (l.idx + row.skip) / Row<E>::EACH) {}
+    // a piece's logits, -infinity for what does not stay; whether any of the wavefront's does
+    __device__ __forceinline__ bool stay(const Row<E> &row, const Weights &wt, int c, const uint32_t *p, float *x, bool *held) const
+    {
+        const float least = c <= piece ? from : beyond;
+        bool some = false;
+#pragma unroll
+        for (int j = 0; j < Row<E>::EACH; ++j) {
+            x[j] = Row<E>::R::get(p, j);
+            held[j] = x[j] >= least;
+        }
+        if (__builtin_amdgcn_ballot_w64(c == piece))
+#pragma unroll
+            for (int j = 0; j < Row<E>::EACH; ++j) held[j] = lim.holds(row.key(p, j), row.index(c, j));
+#pragma unroll
+        for (int j = 0; j < Row<E>::EACH; ++j) {
+            some |= held[j];
+            x[j] = held[j] ? x[j] : -__builtin_inff();
+        }
+        if (wt.boundless)
+#pragma unroll
+            for (int j = 0; j < Row<E>::EACH; ++j) x[j] = wt.logit(x[j]);
+        return __builtin_amdgcn_ballot_w64(some);
+    }
+};
+
+// The lowest element at which the sum of their masses in the order of the numbers exceeds target(total); -1: nowhere.  masses(number of the
+// piece, piece, out) gives those of a piece's elements and returns how many of them count; *count = how many do in all.
 template <typename E, typename M, typename W>
-__device__ __forceinline__ int locate(const Row<E> &row, Shared &s, M mass, W target, uint64_t *total, int *count)
+__device__ __forceinline__ int locate(const Row<E> &row, Shared &s, M masses, W target, uint64_t *total, int *count)
 {
     constexpr int EACH = Row<E>::EACH;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, steps = row.per / SA_STEP;
@@ -270,12 +325,10 @@ __device__ __forceinline__ int locate(const Row<E> &row, Shared &s, M mass, W ta
     uint64_t x = 0;
     __syncthreads();
     row.each([&](int c, const uint32_t *p) {
+        uint64_t q[EACH];
+        mine += masses(c, p, q);
 #pragma unroll
-        for (int j = 0; j < EACH; ++j) {
-            bool in;
-            x += mass(row.key(p, j), row.index(c, j), &in);
-            mine += in;
-        }
+        for (int j = 0; j < EACH; ++j) x += q[j];
     }, [&](int step) {
         x = wave_sum(x);
         if (lane == 0) s.hist[w * steps + step] = x;
@@ -309,15 +362,12 @@ __device__ __forceinline__ int locate(const Row<E> &row, Shared &s, M mass, W ta
 #pragma unroll 1
             for (int i = 0; i < SA_UNROLL && found < 0; ++i) {
                 const int c = c0 + i * HX_WAVE + lane;
-                uint32_t p[4];
+                const uint4 v = row.load(c);
+                const uint32_t p[4] = {v.x, v.y, v.z, v.w};
                 uint64_t q[EACH], y = 0;
-                row.load_any(c, p);
+                (void)masses(c, p, q);
 #pragma unroll
-                for (int j = 0; j < EACH; ++j) {
-                    bool in;
-                    q[j] = mass(row.key(p, j), row.index(c, j), &in);
-                    y += q[j];
-                }
+                for (int j = 0; j < EACH; ++j) y += q[j];
                 const uint64_t sum = wave_scan(y);
                 uint64_t run = before + sum - y;
                 int here = -1;
@@ -372,6 +422,22 @@ __device__ __forceinline__ void crossing(Shared &s, const uint64_t *x, uint64_t 
     __syncthreads();
 }
 
+// The lowest key of lo .. hi for which f holds, which holds for all keys above one for which it does; hi if for none.  By 64 at a time.
+template <typename F>
+__device__ __forceinline__ uint32_t first_where(uint32_t lo, uint32_t hi, F f)
+{
+    while (lo < hi) {
+        const uint32_t step = (hi - lo) / HX_WAVE + 1;
+        const uint64_t at = (uint64_t)lo + (uint64_t)(threadIdx.x & 63) * step;
+        const unsigned long long m = __builtin_amdgcn_ballot_w64(at >= hi || f((uint32_t)at));
+        const int l = m ? __builtin_ctzll(m) : HX_WAVE;
+        const uint64_t end = (uint64_t)lo + (uint64_t)l * step;
+        if (l > 0) lo = (uint32_t)(end - step) + 1;
+        hi = l == 0 ? lo : end < hi ? (uint32_t)end : hi;
+    }
+    return lo;
+}
+
 // The last element that stays of those for which `in` holds, in the order (logit falling, number rising): the one at which the sum of
 // their weights (count_them: their number) reaches want(total).  EQUALS: the first *stay of those with the key are the last ones that stay.
 enum Found { ALL_STAY, LAST_FOUND, EQUALS };
@@ -389,20 +455,48 @@ __device__ __forceinline__ Found find_limit(const Row<E> &row, Shared &s, const 
         for (int i = tid; i < SA_BINS * SA_COLS; i += SA_THREADS) s.hist[i] = 0;
         if (tid == 0) s.r32[2] = 0;
         __syncthreads();
-        row.each([&](int c, const uint32_t *p) {
+        const Cut<E> cut(row, in);
+        if (shift < 0 && count_them)
+            row.each([&](int c, const uint32_t *p) {
+                float x[EACH];
+                bool held[EACH];
+                if (!cut.stay(row, wt, c, p, x, held)) return;
+                int b[EACH];
+#pragma unroll
+                for (int j = 0; j < EACH; ++j) b[j] = wt.bin(x[j]);
+#pragma unroll
+                for (int j = 0; j < EACH; ++j)
+                    if (held[j]) atomicAdd((unsigned long long *)&s.hist[b[j] * SA_COLS + (lane & (SA_COLS - 1))], 1ull);
+            });
+        else if (shift < 0)
+            row.each([&](int c, const uint32_t *p) {
+                float x[EACH];
+                bool held[EACH];
+                if (!cut.stay(row, wt, c, p, x, held)) return;
+                int b[EACH];
+                uint64_t m[EACH];
+#pragma unroll
+                for (int j = 0; j < EACH; ++j) m[j] = Weights::whole(wt.scaled(x[j], &b[j]));
+#pragma unroll
+                for (int j = 0; j < EACH; ++j)
+                    if (m[j]) atomicAdd((unsigned long long *)&s.hist[b[j] * SA_COLS + (lane & (SA_COLS - 1))], (unsigned long long)m[j]);
+            });
+        else row.each([&](int c, const uint32_t *p) {
+            bool mine[EACH], some = false;
 #pragma unroll
             for (int j = 0; j < EACH; ++j) {
                 const uint32_t k = row.key(p, j);
-                const bool mine = k >= k_low && k <= k_high && in.holds(k, row.index(c, j));
-                if (__builtin_amdgcn_ballot_w64(mine)) {
-                    int b;
-                    uint64_t x = 1;
-                    if (count_them) b = wt.bin(k);
-                    else x = Weights::whole(wt.scaled(k, &b));
-                    if (shift >= 0) b = (int)((k_high - k) >> shift);
-                    if (mine && x) atomicAdd((unsigned long long *)&s.hist[b * SA_COLS + (lane & (SA_COLS - 1))], (unsigned long long)x);
-                }
+                mine[j] = k >= k_low && k <= k_high && in.holds(k, row.index(c, j));
+                some |= mine[j];
             }
+            if (!__builtin_amdgcn_ballot_w64(some)) return;
+#pragma unroll
+            for (int j = 0; j < EACH; ++j)
+                if (mine[j]) {
+                    const uint32_t k = row.key(p, j);
+                    const uint64_t m = mass(k);
+                    if (m) atomicAdd((unsigned long long *)&s.hist[((k_high - k) >> shift) * SA_COLS + (lane & (SA_COLS - 1))], (unsigned long long)m);
+                }
         });
         __syncthreads();
         {
@@ -417,13 +511,24 @@ __device__ __forceinline__ Found find_limit(const Row<E> &row, Shared &s, const 
         const int bin = s.r32[1];
         if (bin < 0) return ALL_STAY;
         before = s.r64[0];
-        // the elements of that bin
+        // the elements of that bin: their keys lie beside each other
+        uint32_t first_key, last_key;
+        if (shift >= 0) {
+            const uint64_t below = (uint64_t)(bin + 1) << shift;
+            last_key = k_high - ((uint32_t)bin << shift);
+            first_key = k_high - k_low >= below ? k_high - (uint32_t)below + 1 : k_low;
+        } else {
+            const uint32_t most = k_high < wt.hi ? k_high : wt.hi;
+            first_key = first_where(k_low, most, [&](uint32_t k) { return wt.bin(k) <= bin; });
+            last_key = first_where(first_key, most, [&](uint32_t k) { return wt.bin(k) < bin; });
+            if (wt.bin(last_key) < bin) --last_key;                 // (else none is nearer the top)
+        }
         uint32_t lo = 0xffffffffu, hi = 0;
         row.each([&](int c, const uint32_t *p) {
 #pragma unroll
             for (int j = 0; j < EACH; ++j) {
                 const uint32_t k = row.key(p, j);
-                if (k >= k_low && k <= k_high && (shift >= 0 ? (int)((k_high - k) >> shift) : wt.bin(k)) == bin && in.holds(k, row.index(c, j))) {
+                if (k >= first_key && k <= last_key && in.holds(k, row.index(c, j))) {
                     lo = k < lo ? k : lo;
                     hi = k > hi ? k : hi;
                     const int at = atomicAdd(&s.r32[2], 1);
@@ -517,6 +622,104 @@ __device__ __forceinline__ Found find_limit(const Row<E> &row, Shared &s, const 
     }
 }
 
+struct Settings {
+    int k;
+    float p, u;
+    double min_w;
+};
+
+// Sum over the workgroup's threads.
+__device__ __forceinline__ uint64_t block_sum(Shared &s, uint64_t x)
+{
+    x = wave_sum(x);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) s.wave[threadIdx.x >> 6] = x;
+    __syncthreads();
+    uint64_t all = 0;
+#pragma unroll
+    for (int i = 0; i < SA_WAVES; ++i) all += s.wave[i];
+    return all;
+}
+
+// The rest of the way where only the elements with keys from `least` on can stay and they are few: an element a thread, each compared with
+// all others.  False: they are more.
+template <typename E>
+__device__ __forceinline__ bool finish_short(const Row<E> &row, Shared &s, const Weights &wt, const Settings &g, uint32_t least, int *token, int *kept, uint64_t *total)
+{
+    const int tid = threadIdx.x;
+    __syncthreads();
+    if (tid == 0) s.r32[2] = 0;
+    __syncthreads();
+    row.each([&](int c, const uint32_t *p) {
+        uint32_t most = 0;
+#pragma unroll
+        for (int j = 0; j < Row<E>::EACH; ++j) {
+            const uint32_t k = row.key(p, j);
+            most = k > most ? k : most;
+        }
+        if (!__builtin_amdgcn_ballot_w64(most >= least)) return;
+#pragma unroll
+        for (int j = 0; j < Row<E>::EACH; ++j) {
+            const uint32_t k = row.key(p, j);
+            if (k >= least) {
+                const int at = atomicAdd(&s.r32[2], 1);
+                if (at < SA_SHORT) { s.lkey[at] = k; s.lidx[at] = row.index(c, j); }
+            }
+        }
+    });
+    __syncthreads();
+    const int n = s.r32[2];
+    if (n > SA_SHORT) return false;
+    const bool mine = tid < n;
+    const uint32_t k = mine ? s.lkey[tid] : 0;
+    const int idx = mine ? s.lidx[tid] : 0;
+    int b;
+    const double y = wt.scaled(k, &b);
+    uint64_t x = mine ? Weights::whole(y) : 0;
+    uint4 *all = (uint4 *)s.hist;
+    if (tid < SA_SHORT) all[tid] = make_uint4(k, (uint32_t)idx, (uint32_t)x, (uint32_t)(x >> 32));
+    __syncthreads();
+    int rank = 0;
+    uint64_t before = 0;
+    if (mine)
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) {
+            const uint4 o = all[j];
+            const bool earlier = o.x > k || (o.x == k && (int)o.y < idx);
+            rank += earlier;
+            before += earlier ? (uint64_t)o.w << 32 | o.z : 0;
+        }
+    bool stays = mine && (g.k <= 0 || rank < g.k);
+    if (g.p < 1.0f) {
+        uint64_t limit = 1;
+        const uint64_t sum = block_sum(s, stays ? x : 0);
+        if (g.p > 0.0f) {
+            bool rest;
+            limit = scaled(g.p, sum, &rest) + rest;
+            limit = limit ? limit : 1;
+        }
+        stays = stays && before < limit;
+    }
+    stays = stays && y >= g.min_w;
+    x = stays ? x : 0;
+    *total = block_sum(s, x);
+    if (tid < SA_SHORT) { all[tid].z = (uint32_t)x; all[tid].w = (uint32_t)(x >> 32); }
+    *kept = (int)block_sum(s, stays);
+    bool rest;
+    const uint64_t want = scaled(g.u, *total, &rest);
+    before = 0;
+    if (mine)
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) {
+            const uint4 o = all[j];
+            before += (int)o.y < idx ? (uint64_t)o.w << 32 | o.z : 0;
+        }
+    if (stays && before <= want && want < before + x) s.r32[0] = idx;
+    __syncthreads();
+    *token = s.r32[0];
+    return true;
+}
+
 template <typename E>
 __global__ __launch_bounds__(SA_THREADS) void hx_sample_kernel(SampleArgs a)
 {
@@ -524,7 +727,7 @@ __global__ __launch_bounds__(SA_THREADS) void hx_sample_kernel(SampleArgs a)
     __shared__ Shared s;
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     Row<E> row;
-    row.set((const E *)a.logits + (int64_t)r * a.row_stride, a.n_vocab);
+    row.set((const E *)a.logits + (int64_t)r * a.row_stride, a.n_vocab, s.edge);
 
     const float T = a.temperature ? a.temperature[r] : 1.0f, p = a.top_p ? a.top_p[r] : 1.0f, mp = a.min_p ? a.min_p[r] : 0.0f, u = a.u[r];
     const int k = a.top_k ? a.top_k[r] : 0;
@@ -541,6 +744,7 @@ __global__ __launch_bounds__(SA_THREADS) void hx_sample_kernel(SampleArgs a)
         hi = h0 > h1 ? h0 : h1;
         lo = l0 < l1 ? l0 : l1;
     }
+    const int own_hi = hi;
     auto over_all = [&](int &most, int &least) {
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) {
@@ -595,12 +799,66 @@ __global__ __launch_bounds__(SA_THREADS) void hx_sample_kernel(SampleArgs a)
         }
         return;
     }
-    const Weights wt{(double)of_key(top_key), 46.16624130844683 / (double)T, s.tab, a.qbits, top_key == 0xff800000u, top_key};
+    const bool boundless = top_key == 0xff800000u;
+    const Weights wt{boundless ? 0.0 : (double)of_key(top_key), boundless ? 1.0 : 46.16624130844683 / (double)T, s.tab, a.qbits, boundless, top_key};
     const double min_w = __builtin_ldexp((double)mp, a.qbits);
     Limit lim{KEY_BARRED + 1, 0x7fffffff};                 // all that are not barred
     uint64_t all;
     int kept, t = -1;
+    auto answer = [&] {
+        if (tid != 0) return;
+        a.token[r] = t;
+        if (a.n_kept) a.n_kept[r] = kept;
+        if (a.logprob) {
+            const double d = wt.boundless ? 0.0 : ((double)to_float(row.p[t]) - wt.top) / (double)T;
+            a.logprob[r] = (float)(d - (log((double)all) - a.qbits * 0.6931471805599453));
+        }
+    };
+    // Where few elements can stay, a key below which none does, and those from it on alone.  top-k: 1024 threads have each seen the largest
+    // of their part; none of the first k of all is below the k-th of these, and not many others are above it (k = 320: 383 are expected).  min-p alone: its weight, and
+    // 1 / 32 of a power of 2 less.
+    if (T != 0.0f && ((k > 0 && k < a.n_vocab && k <= SA_SHORT * 5 / 8 && !row.nans) || (k <= 0 && p >= 1.0f && mp > 0.0f))) {
+        uint32_t least = 0;
+        if (k > 0) {
+            const uint32_t own = key_of(R::of_order(own_hi));
+            for (int i = tid; i < SA_BINS * SA_COLS; i += SA_THREADS) s.hist[i] = 0;
+            __syncthreads();
+            const bool some = own > KEY_BARRED && own <= top_key;          // the thread has an element that is not barred
+            const int b = some ? wt.bin(own) : 0;
+            if (some) atomicAdd((unsigned long long *)&s.hist[b * SA_COLS + (lane & (SA_COLS - 1))], 1ull);
+            __syncthreads();
+            uint64_t x[2] = {0, 0}, limit = 0;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (2 * tid + i < SA_BINS)
+#pragma unroll
+                    for (int j = 0; j < SA_COLS; ++j) x[i] += s.hist[(2 * tid + i) * SA_COLS + j];
+            crossing<2>(s, x, 0, &limit, true, [&](uint64_t) { return (uint64_t)k; });
+            const int bin = s.r32[1];
+            if (bin >= 0) {
+                uint32_t mine = some && b <= bin ? own : 0xffffffffu;
+#pragma unroll
+                for (int d = 32; d > 0; d >>= 1) {
+                    const uint32_t x2 = __shfl_xor(mine, d);
+                    mine = x2 < mine ? x2 : mine;
+                }
+                if (lane == 0) s.wmin[w] = (int)mine;
+                __syncthreads();
+                least = 0xffffffffu;
+                for (int i = 0; i < SA_WAVES; ++i) least = (uint32_t)s.wmin[i] < least ? (uint32_t)s.wmin[i] : least;
+            }
+        } else {
+            const int bin = (int)(-32.0 * log2((double)mp)) + 2;
+            if (bin < SA_BINS - 1) least = first_where(KEY_BARRED + 1, top_key, [&](uint32_t kk) { return wt.bin(kk) <= bin; });
+        }
+        if (least && finish_short(row, s, wt, {k, p, u, min_w}, least, &t, &kept, &all)) {
+            answer();
+            return;
+        }
+    }
     enum { TOP_K, TOP_P, TOKEN };
+    // the least logit that min-p leaves
+    const uint32_t least_mp = mp > 0.0f && T != 0.0f ? first_where(KEY_BARRED + 1, top_key, [&](uint32_t kk) { int b; return wt.scaled(kk, &b) >= min_w; }) : 0;
     for (int step = T == 0.0f ? TOKEN : TOP_K;; ++step) {
         // equal_key: elements of this key count 1 and no others; else the weights of all that stay
         bool equal = step == TOKEN && T == 0.0f;
@@ -620,18 +878,28 @@ __global__ __launch_bounds__(SA_THREADS) void hx_sample_kernel(SampleArgs a)
             equal = true;
             equal_key = lim.key;
         }
-        t = locate(row, s, [&](uint32_t kk, int i, bool *in) -> uint64_t {
-            if (equal) { *in = kk == equal_key; return *in; }
-            const bool held = kk > KEY_BARRED && lim.holds(kk, i);
-            *in = false;
-            uint64_t x = 0;
-            if (__builtin_amdgcn_ballot_w64(held)) {
-                int b;
-                const double y = wt.scaled(kk, &b);
-                *in = held && y >= min_w;
-                x = *in ? Weights::whole(y) : 0;
+        if (step == TOKEN && least_mp > lim.key) lim = {least_mp, 0x7fffffff};
+        const Cut<E> cut(row, lim);
+        t = locate(row, s, [&](int c, const uint32_t *piece, uint64_t *q) -> int {
+            constexpr int EACH = R::EACH;
+            int count = 0;
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) q[j] = 0;
+            if (equal) {
+#pragma unroll
+                for (int j = 0; j < EACH; ++j) { q[j] = row.key(piece, j) == equal_key; count += (int)q[j]; }
+                return count;
             }
-            return x;
+            float x[EACH];
+            bool held[EACH];
+            if (!cut.stay(row, wt, c, piece, x, held)) return 0;
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+                int b;
+                q[j] = Weights::whole(wt.scaled(x[j], &b));
+                count += held[j];
+            }
+            return count;
         }, [&](uint64_t n) -> uint64_t {
             if (equal) return stay - 1;
             bool rest;
@@ -648,14 +916,7 @@ __global__ __launch_bounds__(SA_THREADS) void hx_sample_kernel(SampleArgs a)
         }
         return;
     }
-    if (tid == 0) {
-        a.token[r] = t;
-        if (a.n_kept) a.n_kept[r] = kept;
-        if (a.logprob) {
-            const double d = wt.boundless ? 0.0 : ((double)to_float(row.p[t]) - wt.top) / (double)T;
-            a.logprob[r] = (float)(d - (log((double)all) - a.qbits * 0.6931471805599453));
-        }
-    }
+    answer();
 }
 
 }  // namespace

@@ -196,6 +196,70 @@ def test_keep_moves_the_accepted_together(ctx, T, type_):
     same(model, pool, seqs)
 
 
+def test_keep_of_long_lists(ctx):
+    rng = np.random.default_rng(3)
+    lens = [700, 420, 900]
+    model, pool, seqs = make_cache(19, lens, 16, layers=2, heads=2, dim=16)
+    drafts = [600, 400, 900]
+    kept = [sorted(rng.permutation(n)[:m].tolist()) for n, m in ((600, 391), (400, 129), (900, 128))]
+    ptr = np.concatenate([[0], np.cumsum([len(x) for x in kept])])
+    model.keep([0, 1, 2], drafts, kept)
+    ctx.hx_kv_keep(pool, seqs, sh.i32([0, 1, 2]), sh.i32(drafts), sh.i32(ptr), sh.i32(sum(kept, [])))
+    assert status(ctx) == 0
+    same(model, pool, seqs)
+
+
+def test_keep_of_tokens_whose_pages_are_gone(ctx):
+    """What stays where it is needs no page; a pool of no pages has none to look at."""
+    import torch
+    x = torch.zeros(1, 0, 1, 8, 16, dtype=torch.bfloat16, device="cuda:0")
+    seqs = dict(table=sh.i32([[-1, -1], [-1, -1]]), len=sh.i32([9, 4]))
+    ctx.hx_kv_keep(dict(k=x, v=x, ref=sh.i32([])), seqs, sh.i32([0, 1]), sh.i32([5, 2]), sh.i32([0, 3, 4]), sh.i32([0, 1, 2, 0]))
+    assert status(ctx) == 0
+    assert seqs["len"].tolist() == [7, 3]
+
+
+@pytest.mark.parametrize("n", [1, 3, 64, 65, 300, 5000])
+@pytest.mark.parametrize("dim,heads", [(16, 1), (128, 4)])
+def test_write_of_many_sequences(ctx, n, dim, heads):
+    import torch
+    rng = np.random.default_rng(n)
+    T = 4
+    lens = rng.integers(0, 3 * T, n)
+    model, pool, seqs = make_cache(17, lens.tolist(), T, layers=1, heads=heads, dim=dim, rows=n + 1)
+    row = rng.permutation(n)
+    new = np.where(rng.random(n) < 0.5, 0, rng.integers(0, lens[row] + 1))
+    ptr = np.concatenate([[0], np.cumsum(new)])
+    x = torch.as_tensor(rng.integers(-15, 16, (int(ptr[-1]), 2 * heads, dim))).to(torch.bfloat16).cuda()
+    k, v = x[:, :heads], x[:, heads:]
+    model.write(0, row, ptr, k.float().cpu().numpy().astype(np.float64), v.float().cpu().numpy().astype(np.float64))
+    ctx.hx_kv_write(pool, 0, seqs, sh.i32(row), sh.i32(ptr), k, v)
+    assert status(ctx) == 0
+    same(model, pool, seqs)
+
+
+@pytest.mark.parametrize("n", [16, 17, 255, 1024, 1030, 2100])
+def test_forks_and_growth_of_many_rows(ctx, n):
+    """Around the number of rows that are compared in one place and the one that is planned at once; some rows are listed twice."""
+    rng = np.random.default_rng(n)
+    T, parents = 8, 20
+    lens = rng.integers(0, 5 * T, parents).tolist()
+    model, pool, seqs = make_cache(18, lens, T, layers=1, heads=1, dim=16, rows=parents + n, max_pages=12, spare=6 * n)
+    src, dst = rng.integers(0, parents, n), parents + rng.permutation(n)
+    twice = rng.permutation(n)[:8]
+    dst[twice[:4]] = dst[twice[4:]]
+    assert model.fork(src, dst) == {-6}
+    ctx.hx_kv_fork(pool, seqs, sh.i32(src), sh.i32(dst))
+    assert status(ctx) == -6
+    same(model, pool, seqs)
+    row, new = rng.permutation(parents + n)[:n], rng.integers(0, 2 * T, n)
+    row[twice[:4]] = row[twice[4:]]
+    assert model.grow(row, new) == {-6}
+    ctx.hx_kv_grow(pool, seqs, sh.i32(row), sh.i32(new))
+    assert status(ctx) == -6
+    same(model, pool, seqs, numbers=False)
+
+
 def test_keep_refuses_numbers_out_of_order_and_shared_pages(ctx):
     model, pool, seqs = make_cache(10, [24, 30, 40, 12], 8, rows=8)
     model.fork([2], [5])
@@ -703,6 +767,35 @@ def test_sample_no_numbers_and_settings_out_of_range(ctx):
         ctx.hx_sample(sh.dev(x.astype(np.float32)), f("u", 0.5), token, temperature=f("T", 1.0), top_p=f("p", 1.0), min_p=f("mp", 0.0), logprob=logprob, n_kept=kept)
         assert status(ctx) == -1
         assert int(token[0]) == -1 and int(kept[0]) == 0 and float(logprob[0]) == -np.inf and int(token[1]) >= 0 and int(kept[1]) == 700
+
+
+@pytest.mark.parametrize("type_", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("v", [9, 700, 5000, 40001])
+def test_sample_where_few_can_stay(ctx, type_, v):
+    """top-k around what is looked at in one place, ties across its end, barred and infinite logits, min-p alone."""
+    rng = np.random.default_rng(v + 1)
+    n = 16
+    x = rng.normal(0, 3, (n, v))
+    x[1] = np.round(x[1])                                      # many equal
+    x[2] = 1.5
+    x[3, rng.random(v) < 0.97] = -np.inf                       # fewer than k are left
+    x[4, : v // 2] = -np.inf
+    x[5, rng.integers(0, v, 4)] = np.inf
+    x[6] = np.linspace(-9, 9, v)
+    x[7] = -np.abs(x[7]) - 1000.0
+    k = np.array([1, 30, 320, 50, 200, 3, 319, 64, 321, 511, 512, 2, 320, 100, 7, 40])
+    p = np.where(np.arange(n) % 3 == 0, 1.0, rng.uniform(0.1, 0.99, n))
+    mp = np.where(np.arange(n) % 2 == 0, 0.0, rng.uniform(0.0, 0.3, n))
+    u = rng.random(n)
+    T = rng.uniform(0.4, 2.0, n)
+    for pad in (0, 1):
+        assert check_sample(ctx, x, u, type_, T=T, k=k, p=p, mp=mp, pad=pad)[0] == 0
+    assert check_sample(ctx, x, u, type_, k=k)[0] == 0
+    assert check_sample(ctx, x, u, type_, T=T, mp=np.full(n, 0.02))[0] == 0
+    assert check_sample(ctx, x, u, type_, T=T, mp=rng.uniform(0, 1e-12, n))[0] == 0
+    y = x.copy()
+    y[:, v // 3] = np.nan
+    assert check_sample(ctx, y, u, type_, T=T, k=k, p=p)[0] == -1
 
 
 def test_sample_of_a_negative_zero(ctx):
