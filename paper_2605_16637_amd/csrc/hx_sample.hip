@@ -15,7 +15,7 @@ constexpr int SA_UNROLL = 4;                      // pieces of 16 bytes a lane h
 constexpr int SA_STEP = SA_UNROLL * HX_WAVE;
 constexpr int SA_BINS = 1408, SA_COLS = 4;        // 32 bins to a factor of 2 in weight, 44 factors; a bin's sum lies in 4 places, a lane's by its number
 constexpr int SA_LIST = 1792;                     // elements of the limit's bin that are looked at in LDS
-constexpr int SA_FEW = 128;                       // of them, those that are compared with each other
+constexpr int SA_FEW = 256;                       // of them, those that are compared with each other
 constexpr int SA_SHORT = 512;                     // elements that are all that can stay: what follows looks at them alone
 
 struct SampleArgs {
@@ -356,33 +356,37 @@ __device__ __forceinline__ int locate(const Row<E> &row, Shared &s, M masses, W 
                 before += __shfl(sum - y, l);
             } else before += __shfl(sum, 63);
         }
-        if (at >= 0) {
-            const int c0 = (at / steps) * row.per + (at % steps) * SA_STEP;
-            int found = -1;
-#pragma unroll 1
-            for (int i = 0; i < SA_UNROLL && found < 0; ++i) {
-                const int c = c0 + i * HX_WAVE + lane;
-                const uint4 v = row.load(c);
-                const uint32_t p[4] = {v.x, v.y, v.z, v.w};
-                uint64_t q[EACH], y = 0;
-                (void)masses(c, p, q);
-#pragma unroll
-                for (int j = 0; j < EACH; ++j) y += q[j];
-                const uint64_t sum = wave_scan(y);
-                uint64_t run = before + sum - y;
-                int here = -1;
-#pragma unroll
-                for (int j = 0; j < EACH; ++j) {
-                    run += q[j];
-                    if (here < 0 && run > want) here = row.index(c, j);
-                }
-                const unsigned long long m = __builtin_amdgcn_ballot_w64(here >= 0);
-                if (m) found = __shfl(here, __builtin_ctzll(m));
-                before += __shfl(sum, 63);
-            }
-            if (lane == 0) s.r32[0] = found;
+        if (lane == 0) {
+            s.r32[1] = at;
+            s.r64[0] = all;
+            s.r64[1] = want - before;
         }
-        if (lane == 0) s.r64[0] = all;
+    }
+    __syncthreads();
+    // the pieces of that step: a wavefront each
+    const int at = s.r32[1];
+    const uint64_t want = s.r64[1];
+    uint64_t q[EACH], sum = 0, own = 0;
+    const int c = at < 0 ? 0 : (at / steps) * row.per + (at % steps) * SA_STEP + w * HX_WAVE + lane;
+    if (at >= 0 && w < SA_UNROLL) {
+        const uint4 v = row.load(c);
+        const uint32_t p[4] = {v.x, v.y, v.z, v.w};
+        (void)masses(c, p, q);
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) own += q[j];
+        sum = wave_scan(own);
+        if (lane == 63) s.wave[w] = sum;
+    }
+    __syncthreads();
+    if (at >= 0 && w < SA_UNROLL) {
+        uint64_t run = sum - own;
+        for (int i = 0; i < w; ++i) run += s.wave[i];
+        if (run <= want && want < run + own)
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+                if (run <= want && want < run + q[j]) s.r32[0] = row.index(c, j);
+                run += q[j];
+            }
     }
     __syncthreads();
     const int got = s.r32[0];
@@ -584,23 +588,25 @@ __device__ __forceinline__ Found find_limit(const Row<E> &row, Shared &s, const 
                 __syncthreads();
                 if (tid == 0) s.r32[2] = 0;
                 __syncthreads();
-                uint64_t *fm = s.hist;
-                uint32_t *fk = (uint32_t *)(s.hist + SA_FEW);
-                int *fi = (int *)(s.hist + 2 * SA_FEW);
+                uint4 *few = (uint4 *)s.hist;
                 for (int i = tid; i < n; i += SA_THREADS) {
                     const uint32_t k = s.lkey[i];
                     if (k >= lo && k <= hi) {
-                        const int at = atomicAdd(&s.r32[2], 1);
-                        fk[at] = k; fi[at] = s.lidx[i]; fm[at] = mass(k);
+                        const uint64_t x = mass(k);
+                        few[atomicAdd(&s.r32[2], 1)] = make_uint4(k, (uint32_t)s.lidx[i], (uint32_t)x, (uint32_t)(x >> 32));
                     }
                 }
                 __syncthreads();
                 if (tid < count) {
-                    const uint32_t k = fk[tid];
-                    const int i = fi[tid];
+                    const uint4 own = few[tid];
+                    const uint64_t x = (uint64_t)own.w << 32 | own.z;
                     uint64_t b = before;
-                    for (int j = 0; j < count; ++j) b += fk[j] > k || (fk[j] == k && fi[j] < i) ? fm[j] : 0;
-                    if (b < limit && limit <= b + fm[tid]) { s.r32[3] = i; s.r64[1] = k; }
+#pragma unroll 8
+                    for (int j = 0; j < count; ++j) {
+                        const uint4 o = few[j];
+                        b += o.x > own.x || (o.x == own.x && (int)o.y < (int)own.y) ? (uint64_t)o.w << 32 | o.z : 0;
+                    }
+                    if (b < limit && limit <= b + x) { s.r32[3] = (int)own.y; s.r64[1] = own.x; }
                 }
                 __syncthreads();
                 out->key = (uint32_t)s.r64[1];

@@ -866,3 +866,20 @@ def test_calls_on_a_stream_of_their_own_and_captured(ctx):
             assert torch.equal(a, b)
         torch.randn(1000, device="cuda:0").sum()             # the program's own work in between
     assert status(ctx) == 0
+
+
+def test_the_example_runs(monkeypatch, capsys):
+    import os
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    monkeypatch.syspath_prepend(os.path.join(root, "examples"))
+    import decode_instance
+    inst, answers = decode_instance.main(["--steps", "4", "--prompt", "300", "--window", "64"])
+    assert [len(x) for x in answers] == [5] * 4 and all(0 <= t < decode_instance.VOCAB for x in answers for t in x)
+    # four rows of their own pages now, the prompt's gone from all windows: what is in use is what the tables hold, at the pool's start
+    table, ref = inst.seqs["table"].cpu().numpy(), inst.pool["ref"].cpu().numpy()
+    held = np.bincount(table[table >= 0], minlength=len(ref))
+    assert np.array_equal(held, ref) and (ref[:int((ref > 0).sum())] > 0).all()
+    assert (inst.seqs["len"][1:5].cpu().numpy() >= 304).all() and int(inst.seqs["len"][0]) == 0
+    inst.ctx.close()
+    del sys.modules["decode_instance"]
