@@ -295,19 +295,48 @@ __device__ __forceinline__ void join(const AttendArgs &a, const Seq &q, int pair
         }
     }
     __syncthreads();
-    for (int u = tid; u < rows * (D / 4); u += AT_THREADS) {
-        const int r = u / (D / 4), d = u % (D / 4) * 4, row = rt * ROWS + r;
-        float4 o = make_float4(0, 0, 0, 0);
-#pragma unroll 4
-        for (int p = 0; p < parts; ++p) {
-            const float *from = a.part + (slot0 + (int64_t)p * ROWS + r) * D + d;
-            const float2 x = find(from), y = find(from + 2);
-            const float f = s[p * ROWS + r];
-            if (holds_any(f)) { o.x += x.x * f; o.y += x.y * f; o.z += y.x * f; o.w += y.y * f; }
+    // four numbers of EACH rows a thread, AHEAD parts of each under way: a trip to the others' parts takes longer than all else here
+    constexpr int EACH = 4, AHEAD = 4;
+    const int all = rows * (D / 4);
+    for (int u0 = tid; u0 < all; u0 += AT_THREADS * EACH) {
+        float4 o[EACH];
+        const float *from[EACH];
+        int row[EACH];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int u = u0 + i * AT_THREADS < all ? u0 + i * AT_THREADS : u0;
+            row[i] = u / (D / 4);
+            from[i] = a.part + (slot0 + row[i]) * D + u % (D / 4) * 4;
+            o[i] = make_float4(0, 0, 0, 0);
         }
-        const float f = s[parts * ROWS + r];
-        put((E *)a.out + (int64_t)(q.q0 + row / a.group) * a.out_token + (int64_t)(head * a.group + row % a.group) * a.out_head + d, a.out_wide,
-            o.x * f, o.y * f, o.z * f, o.w * f);
+        for (int p0 = 0; p0 < parts; p0 += AHEAD) {
+            float2 x[EACH][AHEAD], y[EACH][AHEAD];
+#pragma unroll
+            for (int i = 0; i < EACH; ++i)
+                if (u0 + i * AT_THREADS < all)
+#pragma unroll
+                    for (int k = 0; k < AHEAD; ++k) {
+                        const int p = p0 + k < parts ? p0 + k : parts - 1;
+                        x[i][k] = find(from[i] + (int64_t)p * ROWS * D);
+                        y[i][k] = find(from[i] + (int64_t)p * ROWS * D + 2);
+                    }
+#pragma unroll
+            for (int i = 0; i < EACH; ++i)
+                if (u0 + i * AT_THREADS < all)
+#pragma unroll
+                    for (int k = 0; k < AHEAD; ++k) {
+                        const float f = p0 + k < parts ? s[(p0 + k) * ROWS + row[i]] : 0.0f;
+                        if (holds_any(f)) { o[i].x += x[i][k].x * f; o[i].y += x[i][k].y * f; o[i].z += y[i][k].x * f; o[i].w += y[i][k].y * f; }
+                    }
+        }
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+            if (u0 + i * AT_THREADS < all) {
+                const int u = u0 + i * AT_THREADS, at = rt * ROWS + row[i];
+                const float f = s[parts * ROWS + row[i]];
+                put((E *)a.out + (int64_t)(q.q0 + at / a.group) * a.out_token + (int64_t)(head * a.group + at % a.group) * a.out_head + u % (D / 4) * 4, a.out_wide,
+                    o[i].x * f, o[i].y * f, o[i].z * f, o[i].w * f);
+            }
     }
 }
 
@@ -1021,10 +1050,9 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && (D == 64 ||
         asm volatile("" ::: "memory");
     }
     // sums that are not finite, as above (a single query's heads all see the same keys)
-    bool odd = false;
-#pragma unroll
-    for (int w = 0; w < COLS; ++w) odd |= sq.nq > 1 && any_odd<D / 16>(o[w]);
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, false)) {
+    bool odd = any_odd<D / 16>(o[0]);
+    if constexpr (COLS == 2) odd |= any_odd<D / 16>(o[1]);
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0 && sq.nq > 1, false)) {
 #pragma unroll
         for (int w = 0; w < COLS; ++w)
 #pragma unroll
