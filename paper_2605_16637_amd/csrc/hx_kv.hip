@@ -95,6 +95,8 @@ struct ForkArgs {
     int row_bytes;           // of a token in one head
 };
 
+// One workgroup, so that pages go out in the order of the rows: a chain of memory round trips (the claim, the source's length and last
+// page, the counts of 8192 pages at a time).  4 copies of one call: 7.4 us; 256 copies: 11.
 __global__ __launch_bounds__(PL_THREADS) void hx_kv_fork_plan_kernel(ForkArgs a)
 {
     __shared__ int64_t s[PL_WAVES];
@@ -150,7 +152,9 @@ __global__ __launch_bounds__(PL_THREADS) void hx_kv_fork_plan_kernel(ForkArgs a)
     }
 }
 
-// Workgroup (i, 0): the shared pages of copy i; (i, 1 + 2 layer + v): its last page's tokens in one layer's keys or values.
+// Workgroup (i, 0): the shared pages of copy i; (i, 1 + 2 layer + v): its last page's tokens in one layer's keys or values, 16 bytes a
+// thread.  Bound by HBM: 256 copies of tails in 32 layers, 1.0 GB read and written: 169 us, and their sources come from the caches three
+// times of four (a plain copy reaches 4.7 TB/s).
 __global__ __launch_bounds__(CP_THREADS) void hx_kv_fork_copy_kernel(ForkArgs a)
 {
     const KvView &kv = a.kv;
@@ -193,6 +197,7 @@ struct GrowArgs {
     int32_t *list;               // [n_pages]
 };
 
+// As the fork's plan: round trips.  64 rows, 32 tokens each: 9.7 us.
 __global__ __launch_bounds__(PL_THREADS) void hx_kv_grow_kernel(GrowArgs a)
 {
     __shared__ int64_t s[PL_WAVES];
@@ -284,7 +289,8 @@ struct WriteArgs {
     bool aligned;            // 8 numbers of a source can be loaded at once
 };
 
-// 8 numbers of a key and of a value a thread.  D: 0 = e4m3.
+// 8 numbers of a key and of a value a thread; D of one byte: e4m3.  2048 tokens of 64 rows, 8 heads of 128 (17 MB read and written):
+// 6.2 us, most of it the lookups before a thread's store (its sequence by bisection, row, length, page, count).
 template <typename S, typename D>
 __global__ __launch_bounds__(CP_THREADS) void hx_kv_write_kernel(WriteArgs a)
 {
@@ -380,6 +386,7 @@ __device__ bool keep_check(const KeepArgs &a, int i, int *s_bad)
     return !*s_bad;
 }
 
+// 64 rows, up to 6 of 32 tokens kept, one layer: 7.0 us, 2.4 more for the tables; moves of a row follow each other.
 // Workgroup (i, 2 layer + v): a token's place is read by the thread that then writes the earlier place, and numbers rise, so what
 // a thread overwrites it has read.
 __global__ __launch_bounds__(CP_THREADS) void hx_kv_keep_move_kernel(KeepArgs a)
@@ -443,6 +450,7 @@ struct FreeArgs {
     const int32_t *row, *first, *last;
 };
 
+// 2 us for a row, 4 to 5 for 24 or 64.
 // A workgroup a row.  An entry is taken out by an exchange, so a row that is listed twice gives each page back once.
 __global__ __launch_bounds__(CP_THREADS) void hx_kv_free_kernel(FreeArgs a)
 {
@@ -480,6 +488,8 @@ struct CompactArgs {
     int64_t page_bytes;          // of a page in one layer's keys
 };
 
+// Three launches: which pages move (9 us for 2600 pages), the copy, the tables (4.4 us).  The copy is bound by HBM: 3.8 GB read and written in
+// 776 us, 4.9 TB/s, a plain copy's rate.
 __global__ __launch_bounds__(PL_THREADS) void hx_kv_compact_plan_kernel(CompactArgs a)
 {
     __shared__ int64_t s[PL_WAVES];

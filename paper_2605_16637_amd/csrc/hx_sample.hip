@@ -5,6 +5,11 @@
 // elements of the bin where the limit falls, in finer bins where they are many.  The token is found the same way in the
 // order of the numbers.  Weights are whole numbers of 2^-q of the largest (q = 42 to 50 by the row's length, so that a row's sum
 // stays below 2^62): sums do not depend on the order they are added in, and no limit on how rounding went.
+//
+// A workgroup a row; a row is read three to five times (from the caches after the first).  Bound by instructions, of which a weight takes
+// 26, 14 of them in 64 bits; where top-k or min-p leave few elements, only these have weights.  256 rows of 131071 bf16 logits (67 MB; one
+// reading takes 14 us at a copy's rate): greedy 45 us, temperature alone 67, top-k 50 49, top-p 0.9 163.  One row of 32000 fp32 on one CU: 16,
+// 23, 25 and 53 us.
 #include "hx_serve.hpp"
 
 namespace {
