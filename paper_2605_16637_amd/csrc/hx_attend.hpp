@@ -390,10 +390,13 @@ template <int CH> __device__ __forceinline__ int v_piece(int r, int c) { return 
 // While a tile's weights are worked out the next tile's scores are: the matrix unit and the others are both busy within a wavefront, not
 // only between two.
 //
-// Bound by the matrix units and LDS alike: a tile is 16 products of 32 cycles a wavefront, and 16 KB that it reads from LDS at 128 bytes a
-// cycle and CU, with 8 wavefronts on a CU 1024 cycles either way.  Prompts of 3 sequences, 6144 queries and fewer, window 2048, 32 heads of 128:
-// 219 us, 0.79 PFLOP/s (a bf16 product of 8192^3 here: 1.18).  24 trees of 25 drafts over some 1500 tokens: 75 us + 10 to join, and 16 trees of
-// 64 over 8 bits and some 16384 tokens 0.42 PFLOP/s: 8 bits pass through registers and are widened on their way to LDS.
+// A tile is 16 products of 32 cycles a wavefront, 16 KB that it reads from LDS at 128 bytes a cycle and CU, and some 130 other instructions, 16
+// of them exponentials of 16 cycles: for the 8 wavefronts of a CU 1024 cycles of the matrix units, 1024 of LDS, some 1300 of the rest.
+// They take 2800, so two wavefronts a SIMD fill half of each other's waits.  Prompts of 3 sequences, 6144 queries and fewer, window 2048, 32 heads of 128:
+// 220 us, 0.78 PFLOP/s (a bf16 product of 8192^3 here: 1.18).  24 trees of 25 drafts over some 1500 tokens: 75 us + 10 to join, and 16 trees of
+// 64 over 8 bits and some 16384 tokens 473 us, 0.42 PFLOP/s: 8 bits pass through registers and are widened on their way to LDS.  Measured and
+// not taken: 64 rows a wavefront at one wavefront a SIMD, which halves what is read from LDS (495 and 882 us); operands read a stage ahead
+// (221 and 490).
 template <typename E, bool FP8, int D, int WR, bool PAGE16>
 __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : D == 64 && !FP8 && PAGE16 ? 3 : 2) void hx_attend_kernel(AttendArgs a)
 {
