@@ -630,7 +630,7 @@ typedef struct {
     int32_t page_tokens;      /* a power of two, 1..HX_MAX_PAGE_TOKENS                          */
     int32_t head_dim;         /* hx_attend: 64, 128 or 256; the others: any multiple of 16      */
     int32_t dtype;            /* HX_BF16, HX_F16 or HX_E4M3                                     */
-    void *k, *v;              /* device [n_layers][n_pages][n_heads][page_tokens][head_dim], 16-byte aligned */
+    void *k, *v;              /* device [n_layers][n_pages][n_heads][page_tokens][head_dim], 16-byte aligned; a page (n_heads * page_tokens * head_dim numbers) under 2 GiB */
     int32_t *ref;             /* device [n_pages]                                               */
     const float *k_scale;     /* device [n_layers][n_heads], HX_E4M3 only: a stored number times*/
     const float *v_scale;     /*   this is the key's (value's); > 0; NULL = 1                   */

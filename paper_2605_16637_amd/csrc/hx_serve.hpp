@@ -27,6 +27,8 @@ inline int hx_kv_view(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs *seq
                "page_tokens %d is no power of two up to %d", T, HX_MAX_PAGE_TOKENS);
     HX_REQUIRE(ctx, pool->head_dim % 16 == 0 && pool->head_dim <= 1024, HX_ERR_SHAPE, "head_dim %d is no multiple of 16 up to 1024", pool->head_dim);
     HX_REQUIRE(ctx, pool->n_heads <= 65536 && pool->n_layers <= 65536, HX_ERR_SHAPE, "%d layers of %d heads", pool->n_layers, pool->n_heads);
+    HX_REQUIRE(ctx, (int64_t)pool->n_heads * T * pool->head_dim * hx_type_size(pool->dtype) <= INT32_MAX, HX_ERR_SHAPE,
+               "a page of %d heads, %d tokens and %d numbers is beyond int32", pool->n_heads, T, pool->head_dim);
     HX_REQUIRE(ctx, pool->n_pages == 0 || (pool->k && pool->v && pool->ref), HX_ERR_INVALID_ARG, "NULL member in pool");
     HX_REQUIRE(ctx, (((uintptr_t)pool->k | (uintptr_t)pool->v) & 15) == 0, HX_ERR_INVALID_ARG, "the pool's k and v have to be 16-byte aligned");
     HX_REQUIRE(ctx, pool->dtype == HX_E4M3 || (!pool->k_scale && !pool->v_scale), HX_ERR_INVALID_ARG, "scales are for a pool of HX_E4M3");

@@ -130,6 +130,12 @@ def test_sampling_that_is_refused(lib):
     assert b"aligned" in (call(logits=a + 2) and lib.hx_last_error(ctx))
 
 
+def test_pages_of_2_gib_and_more(lib):
+    lib, ctx = lib
+    big = pool(n_heads=65536, page_tokens=64, head_dim=256)
+    assert list(entry_points(lib, ctx, big, seqs())) == [SHAPE] * 7
+
+
 def test_calls_too_large_to_launch_and_rows_too_long(lib):
     """Launches count threads in 32 bits; nothing of such a call is begun."""
     lib, ctx = lib
