@@ -394,7 +394,7 @@ template <int CH> __device__ __forceinline__ int v_piece(int r, int c) { return 
 // of them exponentials of 16 cycles: for the 8 wavefronts of a CU 1024 cycles of the matrix units, 1024 of LDS, some 1300 of the rest.
 // They take 2800, so two wavefronts a SIMD fill half of each other's waits.  Prompts of 3 sequences, 6144 queries and fewer, window 2048, 32 heads of 128:
 // 220 us, 0.78 PFLOP/s (a bf16 product of 8192^3 here: 1.18).  24 trees of 25 drafts over some 1500 tokens: 75 us + 10 to join, and 16 trees of
-// 64 over 8 bits and some 16384 tokens 473 us, 0.42 PFLOP/s: 8 bits pass through registers and are widened on their way to LDS.  Measured and
+// 64 over 8 bits and some 16384 tokens 466 us, 0.42 PFLOP/s: 8 bits pass through registers and are widened on their way to LDS.  Measured and
 // not taken: 64 rows a wavefront at one wavefront a SIMD, which halves what is read from LDS (495 and 882 us); operands read a stage ahead
 // (221 and 490).
 template <typename E, bool FP8, int D, int WR, bool PAGE16>
@@ -564,8 +564,13 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : D == 64 && !FP8 && PAGE16 ?
                 const uint32_t kk[4] = {rk[S][i].x, rk[S][i].y, rk[S][i].z, rk[S][i].w}, vv[4] = {rv[S][i].x, rv[S][i].y, rv[S][i].z, rv[S][i].w};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) { widen(kk[j], wk.x[2 * j], wk.x[2 * j + 1]); widen(vv[j], wv.x[2 * j], wv.x[2 * j + 1]); }
-                sk[k_piece<CH>(key, 2 * my_part)] = wk.u[0]; sk[k_piece<CH>(key, 2 * my_part + 1)] = wk.u[1];
-                sv[v_piece<CH>(key, 2 * my_part)] = wv.u[0]; sv[v_piece<CH>(key, 2 * my_part + 1)] = wv.u[1];
+                // half of a row's lanes begin with their second piece: 8 lanes beside each other fill all banks
+                const bool second = my_part & 4;
+                const int at0 = 2 * my_part + second, at1 = at0 ^ 1;
+                auto either = [&](const uint4 &x, const uint4 &y) { return make_uint4(second ? y.x : x.x, second ? y.y : x.y, second ? y.z : x.z, second ? y.w : x.w); };
+                const uint4 k0 = wk.u[0], k1 = wk.u[1], v0 = wv.u[0], v1 = wv.u[1];
+                sk[k_piece<CH>(key, at0)] = either(k0, k1); sk[k_piece<CH>(key, at1)] = either(k1, k0);
+                sv[v_piece<CH>(key, at0)] = either(v0, v1); sv[v_piece<CH>(key, at1)] = either(v1, v0);
             } else {
                 sk[k_piece<CH>(key, my_part)] = rk[S][i];
                 sv[v_piece<CH>(key, my_part)] = rv[S][i];

@@ -488,7 +488,7 @@ struct CompactArgs {
     int64_t page_bytes;          // of a page in one layer's keys
 };
 
-// Three launches: which pages move (9 us for 2600 pages), the copy, the tables (4.4 us).  The copy is bound by HBM: 3.8 GB read and written in
+// Three launches: which pages move (9 us for 3882 pages), the copy, the tables (4.4 us).  The copy is bound by HBM: 3.8 GB read and written in
 // 776 us, 4.9 TB/s, a plain copy's rate.
 __global__ __launch_bounds__(PL_THREADS) void hx_kv_compact_plan_kernel(CompactArgs a)
 {
