@@ -17,8 +17,8 @@
  *    on, owned by the caller, valid until the work enqueued on `stream` has
  *    finished.  "host" pointers are ordinary host memory read during the
  *    call.  The structs hx_model / hx_calls / hx_prefill_tab / hx_decode_tab /
- *    hx_links / hx_intervals themselves live in host memory; their pointer members are
- *    device pointers.  The library never returns memory the caller must free
+ *    hx_links / hx_intervals / hx_kv_pool / hx_kv_seqs / hx_attend_args themselves
+ *    live in host memory; their pointer members are device pointers.  The library never returns memory the caller must free
  *    (hx_dag_view returns borrowed pointers into the context).
  *  - `stream` is a hipStream_t (NULL = the default stream).  Work is enqueued
  *    on it and the call returns without waiting.  Conditions that only the

@@ -393,10 +393,10 @@ template <int CH> __device__ __forceinline__ int v_piece(int r, int c) { return 
 // A tile is 16 products of 32 cycles a wavefront, 16 KB that it reads from LDS at 128 bytes a cycle and CU, and some 130 other instructions, 16
 // of them exponentials of 16 cycles: for the 8 wavefronts of a CU 1024 cycles of the matrix units, 1024 of LDS, some 1300 of the rest.
 // They take 2800, so two wavefronts a SIMD fill half of each other's waits.  Prompts of 3 sequences, 6144 queries and fewer, window 2048, 32 heads of 128:
-// 220 us, 0.78 PFLOP/s (a bf16 product of 8192^3 here: 1.18).  24 trees of 25 drafts over some 1500 tokens: 75 us + 10 to join, and 16 trees of
+// 216 us, 0.80 PFLOP/s (a bf16 product of 8192^3 here: 1.18).  24 trees of 25 drafts over some 1500 tokens: 75 us + 10 to join, and 16 trees of
 // 64 over 8 bits and some 16384 tokens 466 us, 0.42 PFLOP/s: 8 bits pass through registers and are widened on their way to LDS.  Measured and
 // not taken: 64 rows a wavefront at one wavefront a SIMD, which halves what is read from LDS (495 and 882 us); operands read a stage ahead
-// (221 and 490).
+// (221 and 490, where what is here took 220 and 473).
 template <typename E, bool FP8, int D, int WR, bool PAGE16>
 __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : D == 64 && !FP8 && PAGE16 ? 3 : 2) void hx_attend_kernel(AttendArgs a)
 {
@@ -1166,6 +1166,7 @@ __global__ __launch_bounds__(AT_THREADS) void hx_attend_clear_kernel(int *done, 
 int parts_room(hx_ctx *ctx, AttendArgs &a, int64_t tiles, int rows, int dim, bool counted, hipStream_t stream)
 {
     const int64_t slots = tiles * a.splits * rows;
+    if (int rc = hx_scratch(ctx, ctx->att, (size_t)slots * (dim * sizeof(float) + sizeof(float2)), stream)) return rc;
     if (counted) {
         const void *was = ctx->att_done.p;
         if (int rc = hx_scratch(ctx, ctx->att_done, (size_t)tiles * sizeof(int), stream)) return rc;
@@ -1175,7 +1176,6 @@ int parts_room(hx_ctx *ctx, AttendArgs &a, int64_t tiles, int rows, int dim, boo
         }
         a.done = (int *)ctx->att_done.p;
     }
-    if (int rc = hx_scratch(ctx, ctx->att, (size_t)slots * (dim * sizeof(float) + sizeof(float2)), stream)) return rc;
     a.part = (float *)ctx->att.p;
     a.part_ml = (float2 *)(a.part + slots * dim);
     return HX_OK;
