@@ -459,16 +459,9 @@ __global__ __launch_bounds__(CP_THREADS) void hx_kv_free_kernel(FreeArgs a)
     if (r < 0 || r >= kv.rows) { if (threadIdx.x == 0) hx_raise(kv.status, HX_ERR_INDEX); return; }
     const int len = hx_sync_load(kv.len + r);
     if (!hx_row_ok(kv, r, len)) { if (threadIdx.x == 0) hx_raise(kv.status, HX_ERR_INDEX); return; }
-    int b0 = 0, b1 = hx_pages_of(len, kv.shift);
-    if (a.first) {
-        int lo = a.first[i], hi = a.last[i];
-        lo = lo > 0 ? lo : 0;
-        hi = hi < len ? hi : len;
-        b0 = hx_pages_of(lo, kv.shift);
-        b1 = hi > 0 ? hi >> kv.shift : 0;
-    }
+    const HxSpan span = a.first ? hx_filled_within(a.first[i], a.last[i], len, kv.shift) : HxSpan{0, (uint32_t)hx_pages_of(len, kv.shift)};
     int32_t *table = hx_row(kv, r);
-    for (int b = b0 + threadIdx.x; b < b1; b += CP_THREADS) {
+    for (uint32_t b = span.lo + threadIdx.x; b < span.hi; b += CP_THREADS) {
         const int page = atomicExch(table + b, -1);
         if (page >= 0) give_back(kv, page);
     }

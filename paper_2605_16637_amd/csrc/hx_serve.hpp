@@ -2,6 +2,7 @@
 #pragma once
 
 #include "hx_common.hpp"
+#include "hx_kv_span.hpp"
 
 // The pool and the tables as kernels take them.  T = 1 << shift tokens a page.
 struct KvView {
@@ -41,8 +42,6 @@ inline int hx_kv_view(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs *seq
                   pool->head_dim, seqs->n, seqs->max_pages};
     return HX_OK;
 }
-
-__host__ __device__ inline int hx_pages_of(int tokens, int shift) { return (int)(((int64_t)tokens + (1 << shift) - 1) >> shift); }
 
 // a row of the tables whose length its entries can hold
 __device__ __forceinline__ bool hx_row_ok(const KvView &kv, int r, int len) { return len >= 0 && len <= (int64_t)kv.max_pages << kv.shift; }

@@ -293,6 +293,21 @@ def test_free_whole_rows_and_what_a_window_left(ctx):
     same(model, pool, seqs)
 
 
+def test_free_of_what_lies_beyond_a_row(ctx):
+    """Pages of one token, and bounds up to the ends of an int: what they leave out stays."""
+    low, high = -2 ** 31, 2 ** 31 - 1
+    lens = [40, 0, 7, 300, 1]
+    for T in (1, 8):
+        model, pool, seqs = make_cache(21, lens, T, rows=9)
+        row = [0, 1, 2, 3, 4, 0, 2, 3, 3, 2]
+        first = [high, high, high - 255, 300, 1, low, 7, 257, high - 256, low]
+        last = [high, 0, high, high, low, low, high, high, low, 3]
+        model.give(row, first, last)
+        ctx.hx_kv_free(pool, seqs, sh.i32(row), sh.i32(first), sh.i32(last))
+        assert status(ctx) == 0
+        same(model, pool, seqs)
+
+
 @pytest.mark.parametrize("n,spare,T", [(0, 5, 8), (3, 0, 8), (12, 40, 4), (200, 900, 1), (3000, 20000, 1)])
 def test_compact_moves_pages_down(ctx, n, spare, T):
     rng = np.random.default_rng(n)
