@@ -158,10 +158,10 @@ __device__ __forceinline__ Extent extent(const AttendArgs &a, const Seq &q, int 
     if (!q.ok || a.kv.n_pages == 0) return x;
     x.hi = tree ? q.len : q.base + t_last + 1;
     if (a.window > 0) {
-        const int first_pos = tree ? q.base - 1 : q.base + t_first;         // the least position of a query
+        // the least position of a query: in a tree that of a draft without another above it, the first after the tokens before the drafts
+        const int first_pos = tree ? q.base : q.base + t_first;
         x.lo = first_pos - a.window + 1;
         x.lo = x.lo > 0 ? x.lo : 0;
-        if (tree && x.lo > q.base) x.lo = q.base;
     }
     x.lo_tile = x.lo / KEYS;
     if (x.lo > 0) {
@@ -705,7 +705,8 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : D == 64 && !FP8 && PAGE16 ?
     l += l1;
     l += other_half(l);
     // A weight of 0 times an infinite or NaN value is no 0: where a row's sums are not finite they are taken again key by key, from what it
-    // sees alone.
+    // sees alone.  (A single query's heads all see the same keys, those that the extent holds and a page has, and none else is loaded; a
+    // single draft that is left out sees none, and its sums go nowhere.)
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(any_odd<D / 32>(o)) != 0 && sq.nq > 1, false)) {
         const float m_use = m == NEG_INF ? 0.0f : m;
 #pragma unroll
@@ -1064,7 +1065,7 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && (D == 64 ||
         __builtin_amdgcn_wave_barrier();
         asm volatile("" ::: "memory");
     }
-    // sums that are not finite, as above (a single query's heads all see the same keys)
+    // sums that are not finite, as above
     bool odd = any_odd<D / 16>(o[0]);
     if constexpr (COLS == 2) odd |= any_odd<D / 16>(o[1]);
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0 && sq.nq > 1, false)) {

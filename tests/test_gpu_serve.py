@@ -663,6 +663,46 @@ def test_a_single_token_that_sees_no_number(ctx):
         assert np.isfinite(got[0, :2]).all() and np.isfinite(lse[0, :2]).all() and np.isnan(got[0, 2:]).all() and np.isnan(lse[0, 2:]).all()
 
 
+@pytest.mark.parametrize("type_", ["bf16", "f16"])
+@pytest.mark.parametrize("dim,group,T,context,window,sinks,others", [
+    (64, 1, 16, 700, 100, 0, []), (64, 4, 16, 700, 96, 4, []), (128, 4, 8, 300, 33, 3, [5, 2]), (128, 3, 32, 6000, 5000, 1, []),
+    (64, 40, 16, 700, 100, 0, []), (128, 48, 8, 333, 64, 7, []), (128, 4, 16, 500, 64, 2, [40, 12]), (256, 4, 16, 90, 1, 0, []), (256, 33, 4, 90, 17, 2, [3])])
+def test_a_tree_of_one_draft_does_not_see_what_lies_before_its_window(ctx, type_, dim, group, T, context, window, sinks, others):
+    """One draft, alone and beside larger trees; the values of the last position before the window, and of all that no window holds, are replaced."""
+    import torch
+    nq = [1] + others
+    lens = [context + m for m in nq]
+    g = torch.Generator().manual_seed(context)
+    t = sh.torch_type(type_)
+    per = [-(-n // T) for n in lens]
+    table = np.full((len(lens), max(per)), -1)
+    at = 0
+    for i, k in enumerate(per):
+        table[i, :k] = np.arange(at, at + k)
+        at += k
+    k, v = (torch.randn(1, at, 1, T, dim, generator=g).to(t).cuda() for _ in range(2))
+    q = torch.randn(sum(nq), group, dim, generator=g).to(t).cuda()
+    parent = sh.i32(np.concatenate([np.arange(-1, m - 1) for m in nq]))
+    more = dict(window=window, n_sink=sinks, parent=parent)
+    args = (sh.i32(table), sh.i32(lens), sh.i32(np.concatenate([[0], np.cumsum(nq)])), q, T)
+    was, was_lse = attend_out(ctx, k, v, *args, **more)
+    see = sh.visible(lens[0], 1, [-1], window, sinks)[0]
+    assert not see[context - window] and see[context - window + 1:].all()
+    for what in (float("inf"), float("-inf"), float("nan")):
+        for which in ([context - window], np.nonzero(~see)[0]):
+            k2, v2 = k.clone(), v.clone()
+            for y in which:
+                v2[0, table[0, y // T], 0, y % T] = what
+                if what != what:
+                    k2[0, table[0, y // T], 0, y % T] = what
+            got, lse = attend_out(ctx, k2, v2, *args, **more)
+            assert np.isfinite(got).all() and np.array_equal(got, was) and np.array_equal(lse, was_lse), (what, len(which))
+        v2[0, table[0, (context - window + 1) // T], 0, (context - window + 1) % T, 5] = what        # the first that it sees
+        got, _ = attend_out(ctx, k, v2, *args, **more)
+        assert not np.isfinite(got[0, :, 5]).any() and np.isfinite(got[0][:, np.arange(dim) != 5]).all()
+    assert status(ctx) == 0
+
+
 def test_scratch_does_not_grow_while_a_stream_is_captured():
     import torch
     from paper_2605_16637_amd import binding
