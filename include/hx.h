@@ -667,7 +667,9 @@ int hx_kv_grow(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs *seqs, int3
  * of type src_dtype: HX_F32, HX_BF16 or HX_F16; strides in numbers; n_tok =
  * tokens in all).  Rounded to the pool's type, to nearest even; HX_E4M3 holds
  * number / scale, and what lies beyond +-448 becomes +-448 (NaN stays NaN).  A
- * page that other rows hold too is not written to (HX_ERR_INDEX).
+ * page that other rows hold too is not written to (HX_ERR_INDEX).  Of an entry
+ * in error -- among them one with more tokens than its row has -- no token is
+ * written.  Every entry looks through the rows listed before it.
  */
 int hx_kv_write(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_kv_seqs *seqs, int32_t n,
                 const int32_t *row, const int32_t *tok_ptr, int32_t n_tok, int32_t src_dtype,

@@ -289,8 +289,43 @@ struct WriteArgs {
     bool aligned;            // 8 numbers of a source can be loaded at once
 };
 
+// Of a row listed twice the first entry counts.  A wavefront looks for the rows of its lanes' entries among those listed before, 256 at a time
+// in registers, the next 256 under way; entries rise with the lanes.
+constexpr int LISTED_EACH = 4;
+__device__ __forceinline__ void listed_ask(const int32_t *row, int from, int to, int *x)
+{
+#pragma unroll
+    for (int k = 0; k < LISTED_EACH; ++k) {
+        const int j = from + k * HX_WAVE + (threadIdx.x & (HX_WAVE - 1));
+        x[k] = j < to ? row[j] : 0;
+    }
+}
+// x: the call's first rows; all lanes take part
+__device__ __forceinline__ bool listed_before(const int32_t *row, int *x, int entry, int mine)
+{
+    const int lane = threadIdx.x & (HX_WAVE - 1), most = __builtin_amdgcn_readlane(entry, HX_WAVE - 1);
+    bool listed = false;
+    for (int j0 = 0; j0 < most; j0 += LISTED_EACH * HX_WAVE) {
+        int next[LISTED_EACH];
+        listed_ask(row, j0 + LISTED_EACH * HX_WAVE, most, next);
+        for (unsigned long long left = ~0ull; left;) {
+            const int from = __builtin_ctzll(left), e = __builtin_amdgcn_readlane(entry, from), r = __builtin_amdgcn_readlane(mine, from);
+            bool hit = false;
+#pragma unroll
+            for (int k = 0; k < LISTED_EACH; ++k) hit |= x[k] == r && j0 + k * HX_WAVE + lane < e;
+            const bool any = __builtin_amdgcn_ballot_w64(hit) != 0;
+            listed |= any && entry == e;
+            left &= ~__builtin_amdgcn_ballot_w64(entry == e);
+        }
+#pragma unroll
+        for (int k = 0; k < LISTED_EACH; ++k) x[k] = next[k];
+    }
+    return listed;
+}
+
 // 8 numbers of a key and of a value a thread; D of one byte: e4m3.  2048 tokens of 64 rows, 8 heads of 128 (17 MB read and written):
-// 6.2 us, most of it the lookups before a thread's store (its sequence by bisection, row, length, page, count).
+// 5.2 us in a graph of such calls, most of it the lookups before a thread's store (its sequence by bisection, row, length, page, count).  One
+// token each of 256 rows 3.8, of 1024 5.6; of these the look for rows listed twice takes 0.2, 0.3 and 1.1.
 template <typename S, typename D>
 __global__ __launch_bounds__(CP_THREADS) void hx_kv_write_kernel(WriteArgs a)
 {
@@ -299,19 +334,24 @@ __global__ __launch_bounds__(CP_THREADS) void hx_kv_write_kernel(WriteArgs a)
     const int64_t u = (int64_t)blockIdx.x * CP_THREADS + threadIdx.x;
     const int64_t q = u / per;
     const int c = (int)(u % per), h = c / per_head, d = (c % per_head) * 8;
-    if (q >= a.n_tok) return;
+    int rows[LISTED_EACH];
+    listed_ask(a.row, 0, a.n, rows);
     int lo = 0, hi = a.n - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (a.tok_ptr[mid] <= q) lo = mid; else hi = mid - 1;
     }
     const int first = a.tok_ptr[lo], last = a.tok_ptr[lo + 1], r = a.row[lo];
-    if (q < first || q >= last || r < 0 || r >= kv.rows) { if (c == 0) hx_raise(kv.status, HX_ERR_INDEX); return; }
-    const int len = kv.len[r];
+    // an entry is written as a whole or not at all
+    bool ok = first >= 0 && first <= q && q < last && last <= a.n_tok && r >= 0 && r < kv.rows;
+    const int len = ok ? kv.len[r] : 0;
+    ok = ok && hx_row_ok(kv, r, len) && last - first <= len;
     const int64_t pos = (int64_t)len - last + q;
-    if (!hx_row_ok(kv, r, len) || pos < 0) { if (c == 0) hx_raise(kv.status, HX_ERR_INDEX); return; }
-    const int page = hx_row(kv, r)[pos >> kv.shift];
-    if (page < 0 || page >= kv.n_pages || kv.ref[page] > 1) { if (c == 0) hx_raise(kv.status, HX_ERR_INDEX); return; }
+    const int page = ok ? hx_row(kv, r)[pos >> kv.shift] : -1;
+    ok = page >= 0 && page < kv.n_pages && kv.ref[page] <= 1;
+    const bool again = listed_before(a.row, rows, lo, r);
+    if (q >= a.n_tok) return;
+    if (!ok || again) { if (c == 0) hx_raise(kv.status, HX_ERR_INDEX); return; }
     const int64_t from = q * a.token_stride + h * a.head_stride + d;
     const int64_t to = hx_kv_at(kv, a.layer, page, h, (int)(pos & ((1 << kv.shift) - 1))) + d;
 #pragma unroll

@@ -181,6 +181,45 @@ def test_write_does_not_touch_what_others_hold_or_what_is_not_there(ctx):
     assert np.array_equal(pool_k[:, model.table[0, :2]], model.k[:, model.table[0, :2]])
 
 
+@pytest.mark.parametrize("heads,dim", [(1, 16), (2, 48), (8, 128)])
+@pytest.mark.parametrize("n", [2, 9, 200])
+def test_write_of_rows_listed_twice(ctx, n, heads, dim):
+    """Of a row's entries the first is written, with other tokens in the others, which are as many or more or fewer; the rest of the call is carried out."""
+    import torch
+    rng = np.random.default_rng(n + dim)
+    T, rows = 4, max(2, n // 3)
+    lens = (8 + rng.integers(0, 20, rows)).tolist()
+    model, pool, seqs = make_cache(22, lens, T, layers=1, heads=heads, dim=dim)
+    row = rng.integers(0, rows, n)
+    row[n // 2] = row[0]
+    new = rng.integers(0, 9, n)
+    new[0] = new[n // 2] = 5
+    ptr = np.concatenate([[0], np.cumsum(new)])
+    x = torch.as_tensor(rng.integers(-15, 16, (int(ptr[-1]), 2 * heads, dim))).to(torch.bfloat16).cuda()
+    k, v = x[:, :heads], x[:, heads:]
+    kf, vf = (y.float().cpu().numpy().astype(np.float64) for y in (k, v))
+    for i in range(n):
+        if row[i] not in row[:i]:
+            model.write(0, [row[i]], [0, int(new[i])], kf[ptr[i]:ptr[i + 1]], vf[ptr[i]:ptr[i + 1]])
+    ctx.hx_kv_write(pool, 0, seqs, sh.i32(row), sh.i32(ptr), k, v)
+    assert status(ctx) == -6
+    same(model, pool, seqs)
+
+
+def test_write_of_entries_in_error_writes_none_of_their_tokens(ctx):
+    import torch
+    model, pool, seqs = make_cache(23, [12, 20, 9, 16], 8, heads=2, dim=32)
+    x = torch.ones(40, 2, 32, dtype=torch.bfloat16, device="cuda:0")
+    one = np.ones((40, 2, 32))
+    # more tokens than the row has; an end beyond the tokens given; a row that is not there: the others are written
+    for row, ptr, fine in (([0, 1], [0, 13, 17], [1]), ([2, 0], [0, 3, 41], [0]), ([9, 3, -1], [0, 4, 8, 10], [1])):
+        ctx.hx_kv_write(pool, 0, seqs, sh.i32(row), sh.i32(ptr), x, x)
+        assert status(ctx) == -6
+        for i in fine:
+            model.write(0, [row[i]], [0, ptr[i + 1] - ptr[i]], one[:ptr[i + 1] - ptr[i]], one[:ptr[i + 1] - ptr[i]])
+        same(model, pool, seqs)
+
+
 @pytest.mark.parametrize("T", [1, 8, 32])
 @pytest.mark.parametrize("type_", ["bf16", "e4m3"])
 def test_keep_moves_the_accepted_together(ctx, T, type_):
