@@ -51,6 +51,7 @@ __device__ __forceinline__ uint32_t key_of(float x)
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 constexpr uint32_t KEY_BARRED = 0x007fffffu;       // of -infinity; a NaN's is made the same
+constexpr uint32_t KEY_INF = 0xff800000u;          // of +infinity; the keys beyond are no numbers
 
 // floor(f * w) for 0 <= f < 1; *rest: whether something was cut off
 __device__ __forceinline__ uint64_t scaled(float f, uint64_t w, bool *rest)
@@ -286,14 +287,15 @@ struct Weights {
 };
 
 // Which elements a limit leaves, by one comparison each: up to the limit's piece those from its logit on, after it those beyond.  Only the
-// piece itself is looked at number by number.
+// piece itself is looked at number by number, and all of them where the limit is +infinity: no number lies beyond it, and a comparison with
+// none is not to be relied on in this build.
 template <typename E>
 struct Cut {
     Limit lim;
     float from, beyond;
     int piece;
     __device__ __forceinline__ Cut(const Row<E> &row, const Limit &l)
-        : lim(l), from(of_key(l.key)), beyond(of_key(l.key + 1)), piece(l.idx == 0x7fffffff ? l.idx : (l.idx + row.skip) / Row<E>::EACH) {}
+        : lim(l), from(of_key(l.key)), beyond(of_key(l.key < KEY_INF ? l.key + 1 : l.key)), piece(l.idx == 0x7fffffff ? l.idx : (l.idx + row.skip) / Row<E>::EACH) {}
     // a piece's logits, -infinity for what does not stay; whether any of the wavefront's does
     __device__ __forceinline__ bool stay(const Row<E> &row, const Weights &wt, int c, const uint32_t *p, float *x, bool *held) const
     {
@@ -304,7 +306,7 @@ struct Cut {
             x[j] = Row<E>::R::get(p, j);
             held[j] = x[j] >= least;
         }
-        if (__builtin_amdgcn_ballot_w64(c == piece))
+        if (lim.key >= KEY_INF || __builtin_amdgcn_ballot_w64(c == piece))
 #pragma unroll
             for (int j = 0; j < Row<E>::EACH; ++j) held[j] = lim.holds(row.key(p, j), row.index(c, j));
 #pragma unroll
@@ -682,7 +684,7 @@ __device__ __forceinline__ bool finish_short(const Row<E> &row, Shared &s, const
     const int n = s.r32[2];
     if (n > SA_SHORT) return false;
     const bool mine = tid < n;
-    const uint32_t k = mine ? s.lkey[tid] : 0;
+    const uint32_t k = mine ? s.lkey[tid] : wt.hi;
     const int idx = mine ? s.lidx[tid] : 0;
     int b;
     const double y = wt.scaled(k, &b);
@@ -810,7 +812,7 @@ __global__ __launch_bounds__(SA_THREADS) void hx_sample_kernel(SampleArgs a)
         }
         return;
     }
-    const bool boundless = top_key == 0xff800000u;
+    const bool boundless = top_key == KEY_INF;
     const Weights wt{boundless ? 0.0 : (double)of_key(top_key), boundless ? 1.0 : 46.16624130844683 / (double)T, s.tab, a.qbits, boundless, top_key};
     const double min_w = __builtin_ldexp((double)mp, a.qbits);
     Limit lim{KEY_BARRED + 1, 0x7fffffff};                 // all that are not barred

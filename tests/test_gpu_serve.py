@@ -845,6 +845,24 @@ def test_sample_ends_of_the_range(ctx):
     assert check_sample(ctx, x, u, "f32", T=[1e30] * 8, p=[0.5] * 8)[0] == 0
 
 
+@pytest.mark.parametrize("type_", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("v", [40, 3000, 50021])
+def test_sample_limits_among_infinite_logits(ctx, type_, v):
+    """Several logits of +infinity, of which top-p or top-k leaves the first ones: none beyond the last that stays counts."""
+    rng = np.random.default_rng(v)
+    n = 12
+    x = rng.normal(0, 3, (n, v))
+    for i in range(n):
+        x[i, rng.permutation(v)[:(2, 5, v // 3, v - 1)[i % 4]]] = np.inf
+    x[3, 0] = -np.inf
+    u = rng.random(n)
+    p = np.array([0.4, 0.3, 0.7, 0.5, 0.999, 0.01, 0.25, 0.9, 0.6, 0.8, 0.35, 0.0])
+    assert check_sample(ctx, x, u, type_, p=p)[0] == 0
+    assert check_sample(ctx, x, u, type_, T=rng.uniform(0.4, 2, n), k=np.minimum(v - 1, 400) + np.arange(n), p=p)[0] == 0
+    assert check_sample(ctx, x, u, type_, k=[1, 3, v // 4, 2, 1, 4, 1, v // 2, 1, 2, 7, v - 2], mp=[0.0, 0.1, 1.0] * 4)[0] == 0
+    assert check_sample(ctx, x, u, type_, mp=[0.5] * n, T=[0.0, 1.0] * 6)[0] == 0
+
+
 def test_sample_no_numbers_and_settings_out_of_range(ctx):
     rng = np.random.default_rng(5)
     x = rng.normal(0, 2, (4, 700))
