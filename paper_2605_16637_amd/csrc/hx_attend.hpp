@@ -49,7 +49,9 @@ __device__ __forceinline__ void widen(uint32_t w, f16x2 &a, f16x2 &b)
 constexpr float NEG_INF = -__builtin_inff();
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float MAX_SLACK = 8.0f;            // a running maximum is raised when a score exceeds it by this many powers of 2
-
+// Weights are taken this many powers of 2 up, in the products and the sums alike: the largest lie between 2^LIFT and 2^(LIFT + MAX_SLACK).
+// fp16 ends at 2^-24 (a normal number at 2^-14): without it 32768 weights of 2^-25 of the largest were lost, 2^-10 together.  bf16 has fp32's range.
+template <typename E> constexpr float LIFT = std::is_same_v<E, _Float16> ? 7.0f : 0.0f;
 
 // Whether a sum of weights holds any: 0 where nothing was visible.  (By the bits: a NaN among the visible has to reach the outputs.)
 __device__ __forceinline__ bool holds_any(float l) { return hx_bits(l) << 1 != 0; }
@@ -633,8 +635,8 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : D == 64 && !FP8 && PAGE16 ?
 #pragma unroll
         for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
         top = fmaxf(top, other_half(top)) * c;
-        if (__builtin_amdgcn_ballot_w64(top > m + MAX_SLACK)) {
-            const float m_new = fmaxf(m, top);
+        if (__builtin_amdgcn_ballot_w64(top > m + (MAX_SLACK + LIFT<E>))) {
+            const float m_new = fmaxf(m, top - LIFT<E>);
             const float shrink = __builtin_amdgcn_exp2f(m - (m_new == NEG_INF ? 0.0f : m_new));
             m = m_new;
             l *= shrink;
@@ -1030,8 +1032,8 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && (D == 64 ||
                               fmaxf(fmaxf(s[w][1][0], s[w][1][1]), fmaxf(s[w][1][2], s[w][1][3])));
             top = fmaxf(top, lane_16_away(top));
             top = fmaxf(top, other_half(top)) * c;
-            if (__builtin_amdgcn_ballot_w64(top > m[w] + MAX_SLACK)) {
-                const float m_new = fmaxf(m[w], top);
+            if (__builtin_amdgcn_ballot_w64(top > m[w] + (MAX_SLACK + LIFT<E>))) {
+                const float m_new = fmaxf(m[w], top - LIFT<E>);
                 const float shrink = __builtin_amdgcn_exp2f(m[w] - (m_new == NEG_INF ? 0.0f : m_new));
                 m[w] = m_new;
                 l[w] *= shrink;

@@ -1,4 +1,6 @@
 """The serving step's operators against their plain forms in whole numbers and 64 bits."""
+import math
+
 import numpy as np
 import pytest
 
@@ -589,6 +591,36 @@ def test_scores_far_apart(ctx):
     """Maxima that keep moving, and weights that vanish."""
     for type_ in ("bf16", "f16"):
         assert check_attend(ctx, [700, 900], [1, 60], peaks=12.0, type_=type_, dim=128)[0] == 0
+
+
+@pytest.mark.parametrize("type_,cache", [("f16", "f16"), ("bf16", "bf16"), ("f16", "e4m3")])
+@pytest.mark.parametrize("n,nq,group,far", [(32768, 1, 1, 25.2), (32768, 1, 4, 26.9), (20000, 3, 2, 22.0), (6000, 20, 4, 24.9), (3000, 40, 1, 25.5), (700, 1, 2, 28.0)])
+def test_many_small_weights_beside_a_large_one(ctx, type_, cache, n, nq, group, far):
+    """One key's weight is 2^far of the others', whose values alone are not 0: together they are the result."""
+    import torch
+    T, dim = 32, 64
+    t, step = sh.torch_type(type_), sh.HALF_STEP[type_]
+    pages = -(-n // T)
+    g = torch.Generator().manual_seed(n)
+    k = torch.zeros(1, pages, 1, T, dim)
+    k[0, (n - nq) // 2 // T, 0, (n - nq) // 2 % T, 0] = 12.0
+    v = 1 + torch.rand(1, pages, 1, T, dim, generator=g)
+    v[0, (n - nq) // 2 // T, 0, (n - nq) // 2 % T] = 0
+    k, v = k.to(sh.torch_type(cache)).cuda(), v.to(sh.torch_type(cache)).cuda()
+    q = torch.zeros(nq, group, dim)
+    q[:, :, 0] = far * math.log(2) * dim ** 0.5 / 12.0
+    q = q.to(t).cuda()
+    out, lse = attend_out(ctx, k, v, sh.i32(np.arange(pages)[None]), sh.i32([n]), sh.i32([0, nq]), q, T)
+    kf, vf = (x[0, :, 0].float().reshape(-1, 1, dim)[:n].cpu().numpy().astype(np.float64) for x in (k, v))
+    o, l, size, plain, reach = sh.attend(q.double().cpu().numpy(), kf, vf, sh.visible(n, nq, None, 0, 0), dim ** -0.5, group)
+    ds = (dim + 8) * 2.0 ** -24 * reach + 2.0 ** -21
+    sums = (n + 16) * 2.0 ** -24
+    near = (step + 2 * ds[..., None] + sums) * size + step * np.abs(o)
+    if type_ == "f16":
+        near = near + 2.0 ** -32 * plain + 2.0 ** -25     # weights below the least normal number, 2^7 up; outputs below it
+    assert (np.abs(out - o) <= near).all(), (np.abs(out - o) / near).max()
+    assert (np.abs(lse - l) <= ds + sums + 2.0 ** -22 * np.abs(l)).all()
+    assert status(ctx) == 0
 
 
 def test_how_the_work_is_divided_does_not_go_by_the_real_lengths(ctx):
