@@ -2,7 +2,7 @@
 //
 // Everything here is integers and copies; results depend on the arguments alone.  Which pages a call takes is decided by one
 // workgroup that looks through `ref` from its start (the free pages of lowest number, in the order of the call's rows), and the
-// copying is spread over the chip.
+// copying is spread over the chip.  Counters of entries and pages have no sign: they pass a limit of INT32_MAX by a workgroup's threads.
 #include "hx_serve.hpp"
 
 namespace {
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(CP_THREADS) void hx_kv_fork_copy_kernel(ForkArgs a)
     if (part == 0) {
         const int32_t *from = hx_row(kv, a.src[i]);
         int32_t *to = hx_row(kv, a.dst[i]);
-        for (int b = threadIdx.x; b < t >> kv.shift; b += CP_THREADS) {
+        for (uint32_t b = threadIdx.x; b < (uint32_t)t >> kv.shift; b += CP_THREADS) {
             int page = from[b];
             if (page >= kv.n_pages) { hx_raise(kv.status, HX_ERR_INDEX); page = -1; }
             to[b] = page;
@@ -231,18 +231,18 @@ __global__ __launch_bounds__(PL_THREADS) void hx_kv_grow_kernel(GrowArgs a)
     if (bad) hx_raise(kv.status, HX_ERR_INDEX);
     const int found = first_pages<false>(kv.ref, 0, kv.n_pages, want < kv.n_pages ? (int)want : kv.n_pages, a.list, s);
     // a page a thread: the row that wanted it is found by bisection
-    for (int j = threadIdx.x; j < found; j += PL_THREADS) {
+    for (uint32_t j = threadIdx.x; j < (uint32_t)found; j += PL_THREADS) {
         int lo = 0, hi = a.n - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if (a.first[mid] <= j) lo = mid; else hi = mid - 1;
+            if ((uint32_t)a.first[mid] <= j) lo = mid; else hi = mid - 1;
         }
         // `lo` is the last row before whom at most j pages are wanted: j is its own
         const int r = a.row[lo], need = hx_pages_of(kv.len[r] + a.n_new[lo], kv.shift) - a.have[lo];
         if ((int64_t)a.first[lo] + need > found) continue;       // it does not get all it needs
         const int page = a.list[j];
         kv.ref[page] = 1;
-        hx_row(kv, r)[a.have[lo] + j - a.first[lo]] = page;
+        hx_row(kv, r)[a.have[lo] + (int)j - a.first[lo]] = page;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < a.n; i += PL_THREADS) {
@@ -408,10 +408,10 @@ __device__ bool keep_check(const KeepArgs &a, int i, int *s_bad)
         const int base = len - nd;
         const int32_t *table = hx_row(kv, r);
         for (int j = threadIdx.x; j < i; j += CP_THREADS) bad |= a.row[j] == r;
-        for (int j = threadIdx.x; j < m; j += CP_THREADS) {
+        for (uint32_t j = threadIdx.x; j < (uint32_t)m; j += CP_THREADS) {
             const int k = a.keep[k0 + j];
             if (k < 0 || k >= nd || (j > 0 && a.keep[k0 + j - 1] >= k)) { bad = true; continue; }
-            if (k == j) continue;
+            if ((uint32_t)k == j) continue;
             const int from = table[(base + k) >> kv.shift], to = table[(base + j) >> kv.shift];
             bad |= from < 0 || from >= kv.n_pages || to < 0 || to >= kv.n_pages || kv.ref[to] > 1;
         }
@@ -473,7 +473,7 @@ __global__ __launch_bounds__(CP_THREADS) void hx_kv_keep_apply_kernel(KeepArgs a
     if (!a.ok[i]) return;
     const int r = a.row[i], len = kv.len[r], left = len - a.n_draft[i] + a.keep_ptr[i + 1] - a.keep_ptr[i];
     int32_t *table = hx_row(kv, r);
-    for (int b = hx_pages_of(left, kv.shift) + threadIdx.x; b < hx_pages_of(len, kv.shift); b += CP_THREADS) {
+    for (uint32_t b = hx_pages_of(left, kv.shift) + threadIdx.x; b < (uint32_t)hx_pages_of(len, kv.shift); b += CP_THREADS) {
         const int page = table[b];
         table[b] = -1;
         if (page >= 0) give_back(kv, page);
@@ -528,10 +528,10 @@ __global__ __launch_bounds__(PL_THREADS) void hx_kv_compact_plan_kernel(CompactA
     __shared__ int64_t s[PL_WAVES];
     const KvView &kv = a.kv;
     int mine = 0;
-    for (int p = threadIdx.x; p < kv.n_pages; p += PL_THREADS) {
+    for (uint32_t p = threadIdx.x; p < (uint32_t)kv.n_pages; p += PL_THREADS) {
         const bool used = kv.ref[p] > 0;
         mine += used;
-        a.moved[p] = used ? p : -1;
+        a.moved[p] = used ? (int)p : -1;
     }
     int64_t all;
     (void)block_before(mine, s, &all);

@@ -385,6 +385,34 @@ def test_counts_below_none_are_free_pages(ctx):
     assert np.array_equal(seqs["table"].cpu().numpy(), model.table) and np.array_equal(np.maximum(pool["ref"].cpu().numpy(), 0), model.ref)
 
 
+def test_a_row_of_as_many_entries_as_an_int_counts(ctx):
+    """Pages of one token, and a row's last ones: taken, filled, dropped again, given back, moved."""
+    import torch
+    n, new = 2 ** 31 - 1, 300
+    table = torch.full((1, n), -1, dtype=torch.int32, device="cuda:0")
+    seqs = dict(table=table, len=sh.i32([n - new]))
+    k, v = (torch.zeros(1, 2 * new, 1, 1, 16, dtype=torch.bfloat16, device="cuda:0") for _ in range(2))
+    pool = dict(k=k, v=v, ref=sh.i32([1, 0] * new))               # every second page is someone else's
+    x = torch.arange(new, device="cuda:0").remainder(200).to(torch.bfloat16)[:, None, None].expand(new, 1, 16).contiguous()
+
+    def end():
+        assert status(ctx) == 0
+        assert bool((table[0, :n - new] == -1).all())
+        return table[0, n - new:].tolist(), pool["ref"].tolist(), int(seqs["len"])
+    ctx.hx_kv_grow(pool, seqs, sh.i32([0]), sh.i32([new]))
+    assert end() == (list(range(1, 2 * new, 2)), [1, 1] * new, n)
+    ctx.hx_kv_write(pool, 0, seqs, sh.i32([0]), sh.i32([0, new]), x, -x)
+    ctx.hx_kv_keep(pool, seqs, sh.i32([0]), sh.i32([new]), sh.i32([0, 3]), sh.i32([0, 7, 299]))
+    assert end() == ([1, 3, 5] + [-1] * (new - 3), [1, 1] * 3 + [1, 0] * (new - 3), n - new + 3)
+    assert [k[0, p, 0, 0, 5].item() for p in (1, 3, 5)] == [0, 7, 99] and torch.equal(k, -v)
+    ctx.hx_kv_grow(pool, seqs, sh.i32([0]), sh.i32([new - 3]))
+    ctx.hx_kv_free(pool, seqs, sh.i32([0, 0, 0]), sh.i32([n - 260, n, n]), sh.i32([n, n, 2 ** 31 - 1]))
+    assert end() == (list(range(1, 81, 2)) + [-1] * 260, [1, 1] * 40 + [1, 0] * 260, n)
+    ctx.hx_kv_compact(pool, seqs)
+    got, ref, _ = end()
+    assert ref == [1] * 340 + [0] * 260 and got[:40] == list(range(1, 81, 2)) and got[40:] == [-1] * 260
+
+
 def test_fork_of_entries_that_are_no_pages(ctx):
     model, pool, seqs = make_cache(15, [30, 16], 8, rows=6)
     seqs["table"][0, 1] = seqs["table"][0, 3] = len(model.ref)
