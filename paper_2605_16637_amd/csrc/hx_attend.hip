@@ -1,12 +1,6 @@
 // Attention over cached pages: the entry point.  The kernels are hx_attend.hpp's, compiled for a pair of types in each of hx_attend_*.hip.
 #include "hx_attend_args.hpp"
 
-// more LDS a workgroup than the 64 KB that need no asking
-int hx_attend_init()
-{
-    return hx_attend_init_bf16() && hx_attend_init_bf16_e4m3() && hx_attend_init_f16() && hx_attend_init_f16_e4m3() ? HX_OK : HX_ERR_DEVICE;
-}
-
 extern "C" int hx_attend(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_kv_seqs *seqs,
                          const hx_attend_args *args, void *stream_)
 {

@@ -1231,9 +1231,39 @@ int launch_few(hx_ctx *ctx, AttendArgs &a, hipStream_t stream)
     return hx_check_launch(ctx, "hx_attend_few_kernel");
 }
 
+// More LDS a workgroup than the 64 KB that need no asking, for the kernels of a pair of types and a head_dim, the first time that a context
+// meets them.  (When it is created this took 5 ms, most of it the loading of code that a planner never runs.)
+template <typename E, bool FP8, int D, bool PAGE16>
+hipError_t allow_many()
+{
+    return hipFuncSetAttribute((const void *)hx_attend_kernel<E, FP8, D, 4, PAGE16>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                               Tile<FP8, D, 4, PAGE16>::LDS + TREE_BYTES);
+}
+template <typename E, bool FP8, int D, int COLS, bool PAGE16>
+hipError_t allow_few()
+{
+    return hipFuncSetAttribute((const void *)hx_attend_few_kernel<E, FP8, D, COLS, PAGE16>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                               4 * few_wave_lds(D, COLS) + TREE_BYTES);
+}
+template <typename E, bool FP8, int D>
+int allow(hx_ctx *ctx)
+{
+    constexpr int kind = (std::is_same_v<E, _Float16> ? 6 : 0) + (FP8 ? 3 : 0) + (D == 64 ? 0 : D == 128 ? 1 : 2);
+    if (ctx->att_allowed >> kind & 1) return HX_OK;
+    for (const hipError_t e : {allow_many<E, FP8, D, false>(), allow_many<E, FP8, D, true>(), allow_few<E, FP8, D, 1, false>(), allow_few<E, FP8, D, 1, true>(),
+                               allow_few<E, FP8, D, 2, false>(), allow_few<E, FP8, D, 2, true>()}) {
+        if (e == hipSuccess) continue;
+        (void)hipGetLastError();                   // not the next launch's
+        return hx_fail(ctx, HX_ERR_DEVICE, "hipFuncSetAttribute(LDS size): %s", hipGetErrorString(e));
+    }
+    ctx->att_allowed |= 1u << kind;
+    return HX_OK;
+}
+
 template <typename E, bool FP8, int D>
 int plan(hx_ctx *ctx, AttendArgs &a, int max_len, hipStream_t stream)
 {
+    if (int rc = allow<E, FP8, D>(ctx)) return rc;
     const int64_t rows = (int64_t)a.max_q * a.group, pairs = (int64_t)a.n * a.kv.n_heads;
     if (rows <= 32) {
         a.row_tiles = 1;
@@ -1253,27 +1283,8 @@ int by_dim(hx_ctx *ctx, AttendArgs &a, int max_len, hipStream_t stream)
     return plan<E, FP8, 256>(ctx, a, max_len, stream);
 }
 
-template <typename E, bool FP8, int D, bool PAGE16>
-bool allow()
-{
-    return hipFuncSetAttribute((const void *)hx_attend_kernel<E, FP8, D, 4, PAGE16>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                               Tile<FP8, D, 4, PAGE16>::LDS + TREE_BYTES) == hipSuccess;
-}
-template <typename E, bool FP8, int D, int COLS>
-bool allow_few()
-{
-    const int lds = 4 * few_wave_lds(D, COLS) + TREE_BYTES;
-    return hipFuncSetAttribute((const void *)hx_attend_few_kernel<E, FP8, D, COLS, false>, hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess &&
-           hipFuncSetAttribute((const void *)hx_attend_few_kernel<E, FP8, D, COLS, true>, hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
-}
-template <typename E, bool FP8, int D>
-bool allow_dim() { return allow<E, FP8, D, false>() && allow<E, FP8, D, true>() && allow_few<E, FP8, D, 1>() && allow_few<E, FP8, D, 2>(); }
-template <typename E, bool FP8>
-bool allow_all() { return allow_dim<E, FP8, 64>() && allow_dim<E, FP8, 128>() && allow_dim<E, FP8, 256>(); }
-
 }  // namespace
 
-// One source file for each pair of types, queries' and cache's: HX_ATTEND_TYPES(name, E, FP8) defines its two functions.
+// One source file for each pair of types, queries' and cache's: HX_ATTEND_TYPES(name, E, FP8) defines its function.
 #define HX_ATTEND_TYPES(name, E, FP8)                                                                                    \
-    int hx_attend_##name(hx_ctx *ctx, HxAttend &a, int max_len, hipStream_t stream) { return by_dim<E, FP8>(ctx, a, max_len, stream); } \
-    bool hx_attend_init_##name() { return allow_all<E, FP8>(); }
+    int hx_attend_##name(hx_ctx *ctx, HxAttend &a, int max_len, hipStream_t stream) { return by_dim<E, FP8>(ctx, a, max_len, stream); }

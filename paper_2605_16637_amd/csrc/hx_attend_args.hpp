@@ -27,12 +27,8 @@ struct HxAttend {
     float2 *part_ml;             // [workgroup][rows] maximum (of s log2 e) and sum
 };
 
-// hx_attend_*.hip: queries' type, and a cache of 8 bits where the name says so.  The init functions allow their kernels more LDS.
+// hx_attend_*.hip: queries' type, and a cache of 8 bits where the name says so.
 int hx_attend_bf16(hx_ctx *ctx, HxAttend &a, int max_len, hipStream_t stream);
 int hx_attend_f16(hx_ctx *ctx, HxAttend &a, int max_len, hipStream_t stream);
 int hx_attend_bf16_e4m3(hx_ctx *ctx, HxAttend &a, int max_len, hipStream_t stream);
 int hx_attend_f16_e4m3(hx_ctx *ctx, HxAttend &a, int max_len, hipStream_t stream);
-bool hx_attend_init_bf16();
-bool hx_attend_init_f16();
-bool hx_attend_init_bf16_e4m3();
-bool hx_attend_init_f16_e4m3();

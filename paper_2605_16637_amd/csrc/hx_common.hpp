@@ -58,6 +58,7 @@ struct hx_ctx {
     float *d_dtab = nullptr;               // decode-stage first-room tables, dtab_cap instances
     int dtab_cap = 0;
     HxScratch kv, att, att_done;           // the serving step: pages (hx_kv.hip), attention (hx_attend.hip), and its counters, which are 0 between launches
+    unsigned att_allowed = 0;              // pairs of types and head_dims whose kernels have been allowed their LDS (hx_attend.hpp)
     int32_t *d_zeros = nullptr;            // 64 words that stay 0
     int num_cu = 256;
     HxDagStore dag;

@@ -17,7 +17,6 @@ int hx_relax_search(hx_ctx *ctx, const hx_model *model, const hx_calls *calls,
                     const HxAppendPlan *walks, bool *merged, void *stream);         // hx_score.hip
 int hx_plan_init();                 // hx_plan.hip
 int hx_decode_init();               // hx_decode.hip
-int hx_attend_init();               // hx_attend.hip
 
 namespace {
 
@@ -404,7 +403,7 @@ extern "C" int hx_ctx_create(hx_ctx **out, int device)
         unsigned long long *p = nullptr;
         e = hx_static_scratch(device, &p);
     }
-    if (e == hipSuccess && (hx_plan_init() != HX_OK || hx_decode_init() != HX_OK || hx_attend_init() != HX_OK)) { what = "hipFuncSetAttribute(LDS size)"; e = hipErrorInvalidValue; }
+    if (e == hipSuccess && (hx_plan_init() != HX_OK || hx_decode_init() != HX_OK)) { what = "hipFuncSetAttribute(LDS size)"; e = hipErrorInvalidValue; }
     if (e == hipSuccess) {
         what = "launch of hx_clear_status_kernel";
         CommitArgs z{};

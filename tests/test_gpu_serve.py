@@ -802,6 +802,33 @@ def test_a_tree_of_one_draft_does_not_see_what_lies_before_its_window(ctx, type_
     assert status(ctx) == 0
 
 
+@pytest.mark.parametrize("type_,cache,dim", [("bf16", "bf16", 256), ("f16", "e4m3", 128), ("bf16", "e4m3", 64)])
+@pytest.mark.parametrize("nq", [1, 30])
+def test_the_first_call_of_a_context_may_be_captured(type_, cache, dim, nq):
+    import torch
+    from paper_2605_16637_amd import binding
+    g = torch.Generator().manual_seed(dim)
+    n, T, t = 60, 16, sh.torch_type(type_)
+    k, v = (torch.randn(1, 4, 2, T, dim, generator=g).to(sh.torch_type(cache)).cuda() for _ in range(2))
+    q = torch.randn(nq, 4, dim, generator=g).to(t).cuda()
+    pool, seqs = dict(k=k, v=v, ref=sh.i32(np.ones(4))), dict(table=sh.i32([[2, 0, 3, 1]]), len=sh.i32([n]))
+    ptr, parent = sh.i32([0, nq]), sh.i32(np.arange(-1, nq - 1))
+    out, want = torch.zeros_like(q), torch.zeros_like(q)
+    c, other = binding.Context(0), binding.Context(0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.hx_attend(pool, 0, seqs, ptr, q, out, max_q=nq, max_len=n, parent=parent)
+    other.hx_attend(pool, 0, seqs, ptr, q, want, max_q=nq, max_len=n, parent=parent)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and bool(want.float().abs().sum() > 0)
+    assert status(c) == 0 and status(other) == 0
+    c.close()
+    other.close()
+
+
 def test_scratch_does_not_grow_while_a_stream_is_captured():
     import torch
     from paper_2605_16637_amd import binding
