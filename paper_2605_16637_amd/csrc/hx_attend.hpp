@@ -1200,22 +1200,43 @@ int launch(hx_ctx *ctx, AttendArgs &a, hipStream_t stream)
 
 // Parts of the keys where there are few workgroups otherwise: `many` workgroups if all sequences had the longest's length, but no part
 // shorter than `part` tiles unless there were not even `few` workgroups then, and none shorter than `least`.
+//
+// Where tiles of rows alone are two workgroups a CU and more, `full` of them, parts cost their joining and gain only that a long sequence
+// among short ones is not one workgroup's: none is shorter than `full_part` tiles then, more with more tiles of rows, up to twice that.
+// Divided as before that, with these longer parts, and not at all, 32 heads of 128 over 8 KV heads: 2 prompts of 3000 tokens 249, 177
+// and 177 us; 64 trees of 32 drafts over 1500 134, 97 and 97, over 500 but one over 32768 182, 181 and 818; 256 sequences' tokens over 500 to
+// 32768 1485, 1460 and 1580, over 500 but one over 32768 375, 366 and 580, over 1000 195, 183 and 185.  What this loses: 100 trees of 16 over
+// some 1500 tokens, 40 to 8192, take 199 divided further and 238 as here.
 struct Division {
     int64_t many, few;
     int part, least;
+    int64_t full;
+    int full_part;
 };
-void divide(AttendArgs &a, int64_t groups, const Division &d, int max_len, int tile_keys)
+void divide(AttendArgs &a, int64_t groups, const Division &d, int max_len, int tile_keys, int tile_rows)
 {
+    // what one tile of rows may see: its own queries, or all drafts of a tree, and the window and the sinks before them
+    const int64_t own = a.parent || a.max_q < tile_rows / a.group + 2 ? a.max_q : tile_rows / a.group + 2;
     int64_t reach = max_len;
-    if (a.window > 0 && reach > (int64_t)a.window + a.n_sink + a.max_q) reach = (int64_t)a.window + a.n_sink + a.max_q;
+    if (a.window > 0 && reach > (int64_t)a.window + a.n_sink + own) reach = (int64_t)a.window + a.n_sink + own;
     const int64_t tiles = (reach + tile_keys - 1) / tile_keys + 1, all = groups * tiles;
     int64_t chunk = (all + d.many - 1) / d.many, fill = (all + d.few - 1) / d.few;
     fill = fill < d.part ? fill : d.part;
     chunk = chunk > fill ? chunk : fill;
     chunk = chunk > d.least ? chunk : d.least;
-    if (chunk * MAX_SPLITS < tiles) chunk = (tiles + MAX_SPLITS - 1) / MAX_SPLITS;
+    int64_t parts = (tiles + chunk - 1) / chunk;
+    if (groups >= d.full) {
+        const int64_t more = d.full_part * groups / d.full, long_part = more < 2 * d.full_part ? more : 2 * d.full_part;
+        chunk = chunk > long_part ? chunk : long_part;
+        parts = (tiles + chunk / 2) / chunk;                 // the last one up to half as long again
+        parts = parts > 1 ? parts : 1;
+    }
+    if (parts > MAX_SPLITS) {
+        parts = MAX_SPLITS;
+        chunk = (tiles + MAX_SPLITS - 1) / MAX_SPLITS;
+    }
     a.chunk = (int)chunk;
-    a.splits = groups >= d.many / 2 ? 1 : (int)((tiles + chunk - 1) / chunk);
+    a.splits = (int)parts;
 }
 
 template <typename E, bool FP8, int D, int COLS>
@@ -1267,11 +1288,11 @@ int plan(hx_ctx *ctx, AttendArgs &a, int max_len, hipStream_t stream)
     const int64_t rows = (int64_t)a.max_q * a.group, pairs = (int64_t)a.n * a.kv.n_heads;
     if (rows <= 32) {
         a.row_tiles = 1;
-        divide(a, pairs, {16 * ctx->num_cu, 16 * ctx->num_cu, 8, 8}, max_len, FEW_KEYS);
+        divide(a, pairs, {16 * ctx->num_cu, 16 * ctx->num_cu, 8, 8, 2 * ctx->num_cu, 64}, max_len, FEW_KEYS, 32);
         return rows <= 16 ? launch_few<E, FP8, D, 1>(ctx, a, stream) : launch_few<E, FP8, D, 2>(ctx, a, stream);
     }
     a.row_tiles = (int)((rows + 127) / 128);
-    divide(a, pairs * a.row_tiles, {16 * ctx->num_cu, 2 * ctx->num_cu, 32, 4}, max_len, KT);
+    divide(a, pairs * a.row_tiles, {16 * ctx->num_cu, 2 * ctx->num_cu, 32, 4, 2 * ctx->num_cu, 128}, max_len, KT, 128);
     return a.kv.shift >= 4 ? launch<E, FP8, D, true>(ctx, a, stream) : launch<E, FP8, D, false>(ctx, a, stream);
 }
 
