@@ -17,7 +17,7 @@ SOURCES = ["hx_ctx.hip", "hx_score.hip", "hx_dag.hip", "hx_plan.hip", "hx_decode
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     "-ffp-contract=off",                       # every fused multiply-add is an explicit fmaf
-    # no arithmetic ever sees a NaN, so min/max need no quieting: the one NaN the library writes (the ratio of a call
+    # the search's arithmetic never sees a NaN, so min/max need no quieting: the one NaN it writes (the ratio of a call
     # whose node or workflow index is out of range) is chosen among integers and stored as bits, never computed with
     "-fno-honor-nans",
     # no packed fp32 instructions.  A device feature; the flag cannot be routed to the device pass alone (-Xarch_device
@@ -25,6 +25,11 @@ FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-command-line-argument",
 ]
+
+
+# a user's keys, values and logits may hold NaNs, and what becomes of them is part of the serving step's contract.  (Attention's
+# kernels take 0 to 1 % longer for it.)
+SERVING = ("hx_kv", "hx_attend", "hx_sample")
 
 
 # host-side AddressSanitizer + UndefinedBehaviorSanitizer (device code cannot be sanitized here): each option
@@ -66,7 +71,8 @@ def _compile(cmd, verbose, out=None) -> str:
             rest = [x for x in cmd if x not in sources and x != "-shared"]
             at = rest.index("-o")
             objects = [os.path.join(tmp, os.path.basename(x) + ".o") for x in sources]
-            list(pool.map(lambda so: _compile([*rest[:at], "-c", "-o", so[1], so[0]], verbose), zip(sources, objects)))
+            more = [["-fhonor-nans"] if os.path.basename(x).startswith(SERVING) else [] for x in sources]
+            list(pool.map(lambda som: _compile([*rest[:at], *som[2], "-c", "-o", som[1], som[0]], verbose), zip(sources, objects, more)))
             return _compile([*rest[:at], "-shared", "-o", rest[at + 1], *objects], verbose, out)
     if verbose:
         print(" ".join(cmd))

@@ -1,6 +1,8 @@
 // Attention over cached pages: the entry point.  The kernels are hx_attend.hpp's, compiled for a pair of types in each of hx_attend_*.hip.
 #include "hx_attend_args.hpp"
 
+#include <cmath>
+
 extern "C" int hx_attend(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_kv_seqs *seqs,
                          const hx_attend_args *args, void *stream_)
 {
@@ -16,9 +18,7 @@ extern "C" int hx_attend(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, con
     HX_REQUIRE(ctx, pool->dtype == HX_E4M3 || pool->dtype == g.dtype, HX_ERR_INVALID_ARG, "queries of type %d over a pool of type %d", g.dtype, pool->dtype);
     HX_REQUIRE(ctx, g.n_heads > 0 && g.n_heads % kv.n_heads == 0, HX_ERR_SHAPE, "%d query heads over %d KV heads", g.n_heads, kv.n_heads);
     HX_REQUIRE(ctx, !g.parent || g.max_q <= HX_MAX_DRAFTS, HX_ERR_SHAPE, "a tree of up to %d drafts, beyond %d", g.max_q, HX_MAX_DRAFTS);
-    uint32_t scale_bits;                       // (this build's arithmetic tells no NaN)
-    memcpy(&scale_bits, &g.scale, sizeof(scale_bits));
-    HX_REQUIRE(ctx, (scale_bits & 0x7f800000u) != 0x7f800000u, HX_ERR_INVALID_ARG, "scale is not finite");
+    HX_REQUIRE(ctx, std::isfinite(g.scale), HX_ERR_INVALID_ARG, "scale is not finite");
     if (g.n == 0 || g.n_q == 0 || g.max_q == 0) return HX_OK;
     HX_REQUIRE(ctx, g.q_ptr && g.q && g.out, HX_ERR_INVALID_ARG, "NULL array");
     HX_REQUIRE(ctx, (((uintptr_t)g.q | (uintptr_t)g.out) & 1) == 0, HX_ERR_INVALID_ARG, "q or out is not aligned to its type");

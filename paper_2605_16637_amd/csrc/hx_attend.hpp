@@ -53,8 +53,8 @@ constexpr float MAX_SLACK = 8.0f;            // a running maximum is raised when
 // fp16 ends at 2^-24 (a normal number at 2^-14): without it 32768 weights of 2^-25 of the largest were lost, 2^-10 together.  bf16 has fp32's range.
 template <typename E> constexpr float LIFT = std::is_same_v<E, _Float16> ? 7.0f : 0.0f;
 
-// Whether a sum of weights holds any: 0 where nothing was visible.  (By the bits: a NaN among the visible has to reach the outputs.)
-__device__ __forceinline__ bool holds_any(float l) { return hx_bits(l) << 1 != 0; }
+// Whether a sum of weights holds any: 0 where nothing was visible.  (A NaN among the visible has to reach the outputs.)
+__device__ __forceinline__ bool holds_any(float l) { return l != 0.0f; }
 
 // Whether a lane's sums hold an infinity or a NaN.
 template <int N, typename F>
@@ -65,7 +65,7 @@ __device__ __forceinline__ bool any_odd(const F *o)
     for (int x = 0; x < N; ++x)
 #pragma unroll
         for (int i = 0; i < (int)(sizeof(F) / sizeof(float)); ++i) {
-            const uint32_t size = hx_bits(o[x][i]) & 0x7fffffffu;
+            const uint32_t size = __float_as_uint(o[x][i]) & 0x7fffffffu;
             worst = size > worst ? size : worst;
         }
     return worst >= 0x7f800000u;

@@ -259,7 +259,7 @@ __device__ __forceinline__ float load_number(const float *p) { return *p; }
 __device__ __forceinline__ float load_number(const __bf16 *p) { return (float)*p; }
 __device__ __forceinline__ float load_number(const _Float16 *p) { return (float)*p; }
 
-// 4 numbers as 8 bits each.  The clamp would lose a NaN, which the sign and the exponent's bits tell (this build's arithmetic sees none).
+// 4 numbers as 8 bits each.  The clamp would lose a NaN.
 __device__ __forceinline__ uint32_t to_e4m3(const float *x, float scale)
 {
     float y[4];
@@ -267,7 +267,7 @@ __device__ __forceinline__ uint32_t to_e4m3(const float *x, float scale)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         y[i] = x[i] / scale;
-        nan[i] = (hx_bits(y[i]) & 0x7fffffffu) > 0x7f800000u;
+        nan[i] = y[i] != y[i];
         y[i] = fminf(fmaxf(y[i], -448.0f), 448.0f);
     }
     uint32_t w = 0;

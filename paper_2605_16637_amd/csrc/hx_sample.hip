@@ -40,7 +40,7 @@ __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__bf16 x) { return (float)x; }
 __device__ __forceinline__ float to_float(_Float16 x) { return (float)x; }
 
-__device__ __forceinline__ bool is_nan(float x) { return (hx_bits(x) & 0x7fffffffu) > 0x7f800000u; }
+__device__ __forceinline__ bool is_nan(float x) { return x != x; }
 
 // unsigned keys in the order of the numbers; the two zeros are one
 __device__ __forceinline__ uint32_t key_of(float x)
@@ -287,8 +287,7 @@ struct Weights {
 };
 
 // Which elements a limit leaves, by one comparison each: up to the limit's piece those from its logit on, after it those beyond.  Only the
-// piece itself is looked at number by number, and all of them where the limit is +infinity: no number lies beyond it, and a comparison with
-// none is not to be relied on in this build.
+// piece itself is looked at number by number, and all of them where the limit is +infinity, as no number lies beyond it.
 template <typename E>
 struct Cut {
     Limit lim;

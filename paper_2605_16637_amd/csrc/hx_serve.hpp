@@ -54,13 +54,4 @@ __device__ __forceinline__ int64_t hx_kv_at(const KvView &kv, int layer, int pag
     return ((((int64_t)layer * kv.n_pages + page) * kv.n_heads + head) << kv.shift) * kv.dim + (int64_t)tok * kv.dim;
 }
 
-// A number's bits, past what the compiler takes for granted: this build's arithmetic knows no NaN, and a test of bits that it recognises
-// as a comparison of numbers would know none either.
-__device__ __forceinline__ uint32_t hx_bits(float x)
-{
-    uint32_t b = __float_as_uint(x);
-    asm("" : "+v"(b));
-    return b;
-}
-
 __device__ __forceinline__ int hx_sync_load(const int32_t *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
