@@ -1201,11 +1201,11 @@ int launch(hx_ctx *ctx, AttendArgs &a, hipStream_t stream)
 // Parts of the keys where there are few workgroups otherwise: `many` workgroups if all sequences had the longest's length, but no part
 // shorter than `part` tiles unless there were not even `few` workgroups then, and none shorter than `least`.
 //
-// Where tiles of rows alone are two workgroups a CU and more, `full` of them, parts cost their joining and gain only that a long sequence
+// Where tiles of rows alone are two workgroups a CU and more (four of single tokens), `full` of them, parts cost their joining and gain only that a long sequence
 // among short ones is not one workgroup's: none is shorter than `full_part` tiles then, more with more tiles of rows, up to twice that.
 // Divided as before that, with these longer parts, and not at all, 32 heads of 128 over 8 KV heads: 2 prompts of 3000 tokens 249, 177
 // and 177 us; 64 trees of 32 drafts over 1500 134, 97 and 97, over 500 but one over 32768 182, 181 and 818; 256 sequences' tokens over 500 to
-// 32768 1485, 1460 and 1580, over 500 but one over 32768 375, 366 and 580, over 1000 195, 183 and 185.  What this loses: 100 trees of 16 over
+// 32768 1485, 1509 and 1584, over 500 but one over 32768 375, 369 and 589, over 1000 195, 189 and 185.  What this loses: 100 trees of 16 over
 // some 1500 tokens, 40 to 8192, take 199 divided further and 238 as here.
 struct Division {
     int64_t many, few;
@@ -1288,7 +1288,7 @@ int plan(hx_ctx *ctx, AttendArgs &a, int max_len, hipStream_t stream)
     const int64_t rows = (int64_t)a.max_q * a.group, pairs = (int64_t)a.n * a.kv.n_heads;
     if (rows <= 32) {
         a.row_tiles = 1;
-        divide(a, pairs, {16 * ctx->num_cu, 16 * ctx->num_cu, 8, 8, 2 * ctx->num_cu, 64}, max_len, FEW_KEYS, 32);
+        divide(a, pairs, {16 * ctx->num_cu, 16 * ctx->num_cu, 8, 8, 4 * ctx->num_cu, 64}, max_len, FEW_KEYS, 32);
         return rows <= 16 ? launch_few<E, FP8, D, 1>(ctx, a, stream) : launch_few<E, FP8, D, 2>(ctx, a, stream);
     }
     a.row_tiles = (int)((rows + 127) / 128);

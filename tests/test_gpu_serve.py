@@ -555,10 +555,10 @@ def test_long_contexts_are_divided_and_joined(ctx, rows):
         assert check_attend(ctx, lens, [rows, 1], heads=1, group=4, dim=128, window=window, sinks=4)[0] == 0
 
 
-@pytest.mark.parametrize("nq", [[1] * 8, [33, 2, 1, 1, 7, 1, 1, 1]])
+@pytest.mark.parametrize("nq", [[1] * 16, [33, 2, 1, 1, 7, 1, 1, 1]])
 def test_few_long_parts_where_the_rows_fill_the_chip(ctx, nq):
-    """512 tiles of rows: parts of 64 tiles of keys and more, or 128, the last one longer; lengths around their ends."""
-    lens = [6500, 4200, 2500, 1, 700, 64, 2049, 4097]
+    """1024 and 512 tiles of rows: parts of 64 tiles of keys and more, or 128, the last one longer; lengths around their ends."""
+    lens = ([6500, 4200, 2500, 1, 700, 64, 2049, 4097] * 2)[:len(nq)]
     for window in (0, 4500):
         assert check_attend(ctx, lens, nq, heads=64, group=1, window=window, sinks=3, layers=1, layer=0)[0] == 0
 
