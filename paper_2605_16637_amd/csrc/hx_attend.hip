@@ -37,7 +37,7 @@ extern "C" int hx_attend(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, con
     a.q = g.q; a.q_token = g.q_token; a.q_head = g.q_head;
     a.out = g.out; a.out_token = g.out_token; a.out_head = g.out_head;
     a.lse = g.lse; a.scale = g.scale; a.window = g.window; a.n_sink = g.n_sink; a.parent = g.parent;
-    a.zeros = ctx->d_zeros;
+    a.zeros = hx_serve(ctx)->d_zeros;
     a.k_scale = pool->k_scale; a.v_scale = pool->v_scale;
     a.q_wide = ((uintptr_t)g.q & 15) == 0 && g.q_token % 8 == 0 && g.q_head % 8 == 0;
     a.out_wide = ((uintptr_t)g.out & 7) == 0 && g.out_token % 4 == 0 && g.out_head % 4 == 0;

@@ -1168,18 +1168,19 @@ __global__ __launch_bounds__(AT_THREADS) void hx_attend_clear_kernel(int *done, 
 // Room for the parts, and where the workgroups themselves put them together, for counters, which are 0 whenever no launch is under way.
 int parts_room(hx_ctx *ctx, AttendArgs &a, int64_t tiles, int rows, int dim, bool counted, hipStream_t stream)
 {
+    HxScratch &parts = hx_serve(ctx)->att, &done = hx_serve(ctx)->att_done;
     const int64_t slots = tiles * a.splits * rows;
-    if (int rc = hx_scratch(ctx, ctx->att, (size_t)slots * (dim * sizeof(float) + sizeof(float2)), stream)) return rc;
+    if (int rc = hx_scratch(ctx, parts, (size_t)slots * (dim * sizeof(float) + sizeof(float2)), stream)) return rc;
     if (counted) {
-        const void *was = ctx->att_done.p;
-        if (int rc = hx_scratch(ctx, ctx->att_done, (size_t)tiles * sizeof(int), stream)) return rc;
-        if (ctx->att_done.p != was) {
-            const int64_t n = ctx->att_done.cap / sizeof(int);
-            hx_attend_clear_kernel<<<(int)((n + AT_THREADS - 1) / AT_THREADS), AT_THREADS, 0, stream>>>((int *)ctx->att_done.p, n);
+        const void *was = done.p;
+        if (int rc = hx_scratch(ctx, done, (size_t)tiles * sizeof(int), stream)) return rc;
+        if (done.p != was) {
+            const int64_t n = done.cap / sizeof(int);
+            hx_attend_clear_kernel<<<(int)((n + AT_THREADS - 1) / AT_THREADS), AT_THREADS, 0, stream>>>((int *)done.p, n);
         }
-        a.done = (int *)ctx->att_done.p;
+        a.done = (int *)done.p;
     }
-    a.part = (float *)ctx->att.p;
+    a.part = (float *)parts.p;
     a.part_ml = (float2 *)(a.part + slots * dim);
     return HX_OK;
 }
@@ -1270,14 +1271,14 @@ template <typename E, bool FP8, int D>
 int allow(hx_ctx *ctx)
 {
     constexpr int kind = (std::is_same_v<E, _Float16> ? 6 : 0) + (FP8 ? 3 : 0) + (D == 64 ? 0 : D == 128 ? 1 : 2);
-    if (ctx->att_allowed >> kind & 1) return HX_OK;
+    if (hx_serve(ctx)->att_allowed >> kind & 1) return HX_OK;
     for (const hipError_t e : {allow_many<E, FP8, D, false>(), allow_many<E, FP8, D, true>(), allow_few<E, FP8, D, 1, false>(), allow_few<E, FP8, D, 1, true>(),
                                allow_few<E, FP8, D, 2, false>(), allow_few<E, FP8, D, 2, true>()}) {
         if (e == hipSuccess) continue;
         (void)hipGetLastError();                   // not the next launch's
         return hx_fail(ctx, HX_ERR_DEVICE, "hipFuncSetAttribute(LDS size): %s", hipGetErrorString(e));
     }
-    ctx->att_allowed |= 1u << kind;
+    hx_serve(ctx)->att_allowed |= 1u << kind;
     return HX_OK;
 }
 

@@ -30,15 +30,6 @@ constexpr int HX_SWEEP_LIMIT = 4096;      // max_sweeps is below it
 constexpr int HX_SYNC_WORDS = 66;
 constexpr int HX_SWEEP_POLLS = 1 << 18;   // a workgroup waits for the others some 0.2 s
 
-// Scratch that grows and never shrinks.  What it was before stays allocated until the context ends: a captured graph may still use
-// it, and the sizes double, so all of it together is at most as much again.
-struct HxScratch {
-    void *p = nullptr;
-    size_t cap = 0;
-    void *old[48] = {};
-    int n_old = 0;
-};
-
 struct hx_ctx {
     int device = 0;
     char err[256] = "no error";
@@ -57,9 +48,6 @@ struct hx_ctx {
     size_t dtl_cap = 0;
     float *d_dtab = nullptr;               // decode-stage first-room tables, dtab_cap instances
     int dtab_cap = 0;
-    HxScratch kv, att, att_done;           // the serving step: pages (hx_kv.hip), attention (hx_attend.hip), and its counters, which are 0 between launches
-    unsigned att_allowed = 0;              // pairs of types and head_dims whose kernels have been allowed their LDS (hx_attend.hpp)
-    int32_t *d_zeros = nullptr;            // 64 words that stay 0
     int num_cu = 256;
     HxDagStore dag;
 };
@@ -86,37 +74,6 @@ inline int hx_fail(hx_ctx *ctx, int code, const char *fmt, ...)
     do {                                                \
         if (!(cond)) return hx_fail((ctx), (code), __VA_ARGS__); \
     } while (0)
-
-// Workgroups of `threads` that a launch may have: the runtime counts threads in 32 bits.
-constexpr int64_t hx_most_groups(int threads) { return UINT32_MAX / threads; }
-
-inline int hx_scratch(hx_ctx *ctx, HxScratch &s, size_t bytes, hipStream_t stream)
-{
-    if (bytes <= s.cap) return HX_OK;
-    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-    HX_HIP(ctx, hipStreamIsCapturing(stream, &capture));
-    HX_REQUIRE(ctx, capture == hipStreamCaptureStatusNone, HX_ERR_CAPACITY, "scratch would grow by a call that is being captured: make the call once before");
-    size_t want = 2 * s.cap > ((size_t)1 << 20) ? 2 * s.cap : (size_t)1 << 20;
-    want = bytes > want ? bytes : want;
-    HX_REQUIRE(ctx, s.n_old < 48, HX_ERR_CAPACITY, "scratch has grown too often");
-    void *p = nullptr;
-    const hipError_t e = hipMalloc(&p, want);
-    if (e != hipSuccess) {
-        (void)hipGetLastError();                   // not the next launch's
-        return hx_fail(ctx, HX_ERR_DEVICE, "%zu bytes of scratch: %s", want, hipGetErrorString(e));
-    }
-    if (s.p) s.old[s.n_old++] = s.p;
-    s.p = p;
-    s.cap = want;
-    return HX_OK;
-}
-
-inline void hx_scratch_release(HxScratch &s)
-{
-    if (s.p) (void)hipFree(s.p);
-    for (int i = 0; i < s.n_old; ++i) (void)hipFree(s.old[i]);
-    s = HxScratch{};
-}
 
 // Every kernel that can meet a bad element records the first error here.
 __device__ inline void hx_raise(int32_t *status, int32_t code)

@@ -3,6 +3,7 @@
 #include "hx_search.hpp"
 #include "hx_cp.hpp"
 #include "hx_append.hpp"
+#include "hx_serve.hpp"
 
 void hx_dag_release(hx_ctx *ctx);   // hx_dag.hip
 int hx_reveal_search(hx_ctx *ctx, const hx_model *model, const hx_calls *calls,
@@ -384,7 +385,7 @@ extern "C" int hx_ctx_create(hx_ctx **out, int device)
     if (device < 0 || device >= count) return create_fail("no such device", hipErrorInvalidDevice);
     HxDeviceGuard guard(device);
     if (!guard.ok) return create_fail("hipSetDevice", hipErrorInvalidDevice);
-    hx_ctx *ctx = new (std::nothrow) hx_ctx();
+    HxServe *ctx = new (std::nothrow) HxServe();
     if (!ctx) return create_fail("out of host memory", hipErrorOutOfMemory);
     ctx->device = device;
     hipDeviceProp_t prop;
@@ -434,16 +435,17 @@ extern "C" int hx_ctx_destroy(hx_ctx *ctx)
     if (ctx->d_report) (void)hipFree(ctx->d_report);
     if (ctx->d_sync) (void)hipFree(ctx->d_sync);
     if (ctx->d_ticket) (void)hipFree(ctx->d_ticket);
-    if (ctx->d_zeros) (void)hipFree(ctx->d_zeros);
     if (ctx->d_acc) (void)hipFree(ctx->d_acc);
     if (ctx->d_dpart) (void)hipFree(ctx->d_dpart);
     if (ctx->d_dtl) (void)hipFree(ctx->d_dtl);
     if (ctx->d_dtab) (void)hipFree(ctx->d_dtab);
     if (ctx->d_rkey) (void)hipFree(ctx->d_rkey);
-    hx_scratch_release(ctx->kv);
-    hx_scratch_release(ctx->att);
-    hx_scratch_release(ctx->att_done);
-    delete ctx;
+    HxServe *serve = hx_serve(ctx);
+    if (serve->d_zeros) (void)hipFree(serve->d_zeros);
+    hx_scratch_release(serve->kv);
+    hx_scratch_release(serve->att);
+    hx_scratch_release(serve->att_done);
+    delete serve;
     return HX_OK;
 }
 

@@ -603,8 +603,8 @@ extern "C" int hx_kv_fork(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs 
     HX_KV_BEGIN(ctx, src && dst, 1 + 2 * kv.n_layers);
     const int parts = 1 + 2 * kv.n_layers;
     HX_KV_DEVICE(ctx);
-    if (int rc = hx_scratch(ctx, ctx->kv, ((size_t)kv.rows + 4 * (size_t)n) * sizeof(int32_t), stream)) return rc;
-    int32_t *w = (int32_t *)ctx->kv.p;
+    if (int rc = hx_scratch(ctx, hx_serve(ctx)->kv, ((size_t)kv.rows + 4 * (size_t)n) * sizeof(int32_t), stream)) return rc;
+    int32_t *w = (int32_t *)hx_serve(ctx)->kv.p;
     ForkArgs a{kv, n, src, dst, n_tok, w, w + kv.rows, w + kv.rows + n, w + kv.rows + 2 * (size_t)n, w + kv.rows + 3 * (size_t)n,
                pool->head_dim * hx_type_size(pool->dtype)};
     hx_kv_fork_plan_kernel<<<1, PL_THREADS, 0, stream>>>(a);
@@ -618,8 +618,8 @@ extern "C" int hx_kv_grow(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs 
     if (!ctx) return HX_ERR_INVALID_ARG;
     HX_KV_BEGIN(ctx, row && n_new, 1);
     HX_KV_DEVICE(ctx);
-    if (int rc = hx_scratch(ctx, ctx->kv, ((size_t)kv.rows + 2 * (size_t)n + kv.n_pages) * sizeof(int32_t), stream)) return rc;
-    int32_t *w = (int32_t *)ctx->kv.p;
+    if (int rc = hx_scratch(ctx, hx_serve(ctx)->kv, ((size_t)kv.rows + 2 * (size_t)n + kv.n_pages) * sizeof(int32_t), stream)) return rc;
+    int32_t *w = (int32_t *)hx_serve(ctx)->kv.p;
     GrowArgs a{kv, n, row, n_new, w, w + kv.rows, w + kv.rows + n, w + kv.rows + 2 * (size_t)n};
     hx_kv_grow_kernel<<<1, PL_THREADS, 0, stream>>>(a);
     return hx_check_launch(ctx, "hx_kv_grow_kernel");
@@ -663,8 +663,8 @@ extern "C" int hx_kv_keep(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs 
     HX_REQUIRE(ctx, n_keep == 0 || keep, HX_ERR_INVALID_ARG, "NULL array");
     const int parts = 2 * kv.n_layers;
     HX_KV_DEVICE(ctx);
-    if (int rc = hx_scratch(ctx, ctx->kv, (size_t)n * sizeof(int32_t), stream)) return rc;
-    KeepArgs a{kv, n, n_keep, row, n_draft, keep_ptr, keep, (int32_t *)ctx->kv.p, pool->head_dim * hx_type_size(pool->dtype)};
+    if (int rc = hx_scratch(ctx, hx_serve(ctx)->kv, (size_t)n * sizeof(int32_t), stream)) return rc;
+    KeepArgs a{kv, n, n_keep, row, n_draft, keep_ptr, keep, (int32_t *)hx_serve(ctx)->kv.p, pool->head_dim * hx_type_size(pool->dtype)};
     hx_kv_keep_move_kernel<<<n * parts, CP_THREADS, 0, stream>>>(a);
     hx_kv_keep_apply_kernel<<<n, CP_THREADS, 0, stream>>>(a);
     return hx_check_launch(ctx, "hx_kv_keep_apply_kernel");
@@ -691,8 +691,8 @@ extern "C" int hx_kv_compact(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_se
     HX_REQUIRE(ctx, guard.ok, HX_ERR_DEVICE, "cannot select device %d", ctx->device);
     hipStream_t stream = (hipStream_t)stream_;
     const size_t P = kv.n_pages;
-    if (int rc = hx_scratch(ctx, ctx->kv, (4 + 3 * P) * sizeof(int32_t), stream)) return rc;
-    int32_t *w = (int32_t *)ctx->kv.p;
+    if (int rc = hx_scratch(ctx, hx_serve(ctx)->kv, (4 + 3 * P) * sizeof(int32_t), stream)) return rc;
+    int32_t *w = (int32_t *)hx_serve(ctx)->kv.p;
     const int64_t page_bytes = ((int64_t)kv.n_heads << kv.shift) * kv.dim * hx_type_size(pool->dtype);
     CompactArgs a{kv, w, w + 4, w + 4 + P, moved ? moved : w + 4 + 2 * P, n_used, page_bytes};
     hx_kv_compact_plan_kernel<<<1, PL_THREADS, 0, stream>>>(a);
