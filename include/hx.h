@@ -724,9 +724,10 @@ int hx_kv_compact(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs *seqs, i
  * positions up to the query's own; and only where the table holds a page.
  * What is not visible to a query has no part in its result, whatever its bits;
  * where values or scores that it sees are infinite or NaN, so is its result.
- * Sums, maxima and outputs are held in 32 bits; the weights exp(s - max) are
- * rounded to q's type for their product with the values (HX_F16: to multiples of
- * 2^-31 of the largest, below 2^-21 of it).
+ * Sums, maxima and outputs are held in 32 bits; for their product with the values
+ * the weights exp(s - max) are rounded to q's type, where max_q * n_heads is more
+ * than 32 times the KV heads, and else to the sum of two numbers of that type
+ * (HX_F16: to multiples of 2^-31 of the largest, below 2^-21 of it).
  * A row, q_ptr, page or parent out of range raises HX_ERR_INDEX; its queries
  * then get out = 0, lse = -infinity, or are not written.
  */

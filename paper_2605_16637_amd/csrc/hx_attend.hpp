@@ -845,8 +845,14 @@ constexpr int few_wave_lds(int dim, int cols) { return FEW_KEYS * dim * 2 > 16 *
 // through its own piece of LDS, which transposes them; what it asks for next is under way all the time.  256 sequences, window 4096, one token each,
 // 8 KV heads of 128: 598 us, 5.8 TB/s (a plain copy: 4.7).  One sequence is launch, lookups and three round trips: a token of 777 10 us, 8
 // drafts over some 1500 18 us, of which the parts' joining some 4.
+//
+// A weight is two numbers of q's type, its rounding and what that leaves, in a product each: what remains of its rounding is 2^-16 of it (fp16
+// 2^-22), so that the result is as near the exact one as its own rounding lets it be.  With one number a result of 16 bits was off by 1.3 to 1.4
+// times as much.  What the second product costs: 0 to 2 % in most cases, up to 7 where an 8-bit cache or heads of 64 bring fewer bytes a weight
+// and rows are more than 16.  (The kernel for many rows, which the matrix units and the weights' arithmetic bound, has one number: two
+// took 9 to 29 % longer, 24 trees of 25 drafts 84 -> 94 us, the prompts above 213 -> 262.)
 template <typename E, bool FP8, int D, int COLS, bool PAGE16>
-__global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && (D == 64 || FP8) ? 3 : 2) void hx_attend_few_kernel(AttendArgs a)
+__global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4 : COLS == 1 && FP8 ? 3 : 2) void hx_attend_few_kernel(AttendArgs a)
 {
     using X8 = typename Types<E>::x8;
     using X2 = typename Types<E>::x2;
@@ -1016,7 +1022,7 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && (D == 64 ||
         // a lane's register i of block b is the score of key y0 + 16 b + 4 quad + i
         const bool all = now == 0xffffffffu && (tree ? y0 + 31 < base : y0 + 31 <= base) &&
                          (a.window <= 0 || y0 + 31 < a.n_sink || all_last - y0 < a.window);
-        union { X8 x8; X2 x2[4]; } p[COLS];
+        union { X8 x8; X2 x2[4]; } p[COLS], rest[COLS];
 #pragma unroll
         for (int w = 0; w < COLS; ++w) {
             if (!all) {
@@ -1046,6 +1052,8 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && (D == 64 ||
                 const float w0 = __builtin_amdgcn_exp2f(fmaf(s[w][i / 2][2 * (i & 1)], c, -m_use)), w1 = __builtin_amdgcn_exp2f(fmaf(s[w][i / 2][2 * (i & 1) + 1], c, -m_use));
                 p[w].x2[i][0] = (E)w0;
                 p[w].x2[i][1] = (E)w1;
+                rest[w].x2[i][0] = (E)(w0 - (float)p[w].x2[i][0]);
+                rest[w].x2[i][1] = (E)(w1 - (float)p[w].x2[i][1]);
                 l[w] += w0 + w1;
             }
         }
@@ -1062,7 +1070,7 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && (D == 64 ||
             vf.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at0);
             vf.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at1);
 #pragma unroll
-            for (int w = 0; w < COLS; ++w) o[w][x] = mfma16(vf.x, p[w].x8, o[w][x]);
+            for (int w = 0; w < COLS; ++w) o[w][x] = mfma16(vf.x, rest[w].x8, mfma16(vf.x, p[w].x8, o[w][x]));
         }
         __builtin_amdgcn_wave_barrier();
         asm volatile("" ::: "memory");

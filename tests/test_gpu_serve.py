@@ -659,6 +659,31 @@ def test_many_small_weights_beside_a_large_one(ctx, type_, cache, n, nq, group, 
     assert status(ctx) == 0
 
 
+@pytest.mark.parametrize("type_,cache", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "e4m3"), ("f16", "e4m3")])
+@pytest.mark.parametrize("dim,nq,group", [(64, 1, 4), (128, 3, 8), (128, 1, 1), (256, 8, 2)])
+@pytest.mark.parametrize("n", [90, 5000])
+def test_few_rows_are_off_by_their_own_rounding(ctx, type_, cache, dim, nq, group, n):
+    """Up to 32 rows a KV head: weights as two numbers, so that hardly more than the rounding of the result remains."""
+    import torch
+    T, heads = 16, 2
+    g = torch.Generator().manual_seed(n + dim)
+    pages = -(-n // T)
+    k, v = (torch.randn(1, pages, heads, T, dim, generator=g).to(sh.torch_type(cache)).cuda() for _ in range(2))
+    q = torch.randn(nq, heads * group, dim, generator=g).to(sh.torch_type(type_)).cuda()
+    out, _ = attend_out(ctx, k, v, sh.i32(np.arange(pages)[None]), sh.i32([n]), sh.i32([0, nq]), q, T)
+    kf, vf = (x[0].float().cpu().numpy().transpose(0, 2, 1, 3).reshape(-1, heads, dim)[:n].astype(np.float64) for x in (k, v))
+    o, _, size, plain, reach = sh.attend(q.double().cpu().numpy(), kf, vf, sh.visible(n, nq, None, 0, 0), dim ** -0.5, group)
+    bits = 8 if type_ == "bf16" else 11
+    ds = (dim + 8) * 2.0 ** -24 * reach + 2.0 ** -21
+    near = (2.0 ** (-2 * bits) + 2 * ds + (n + 16) * 2.0 ** -24)[..., None] * size
+    if type_ == "f16":
+        near = near + 2.0 ** -32 * plain + 2.0 ** -25
+    # half a step of the result, or of the one above where the sums take it there
+    near = near + 2.0 ** (np.floor(np.log2(np.abs(o) + near)) - bits)
+    assert (np.abs(out - o) <= near).all(), (np.abs(out - o) / near).max()
+    assert status(ctx) == 0
+
+
 def test_how_the_work_is_divided_does_not_go_by_the_real_lengths(ctx):
     for most in (0, 1, 100, 100000):
         assert check_attend(ctx, [700, 30, 4000], [1, 2, 5], max_len=most, heads=1, dim=128)[0] == 0
