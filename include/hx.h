@@ -38,8 +38,9 @@
  *    but the status word, which kernels update atomically).  A context is not
  *    thread-safe.
  *  - Device memory is allocated by hx_ctx_create and hx_dag_reserve, and by
- *    hx_decode_score, hx_rank (beyond 28672 calls), hx_kv_*, hx_attend and
- *    hx_sample the first time they meet a larger problem than before; every other call only launches kernels and
+ *    hx_decode_score, hx_rank (beyond 28672 calls), hx_kv_fork, hx_kv_grow,
+ *    hx_kv_keep, hx_kv_compact and hx_attend the first time they meet a larger
+ *    problem than before; every other call only launches kernels and
  *    can be captured in a HIP graph (hx_validate_round and hx_stream_status
  *    wait for the stream and cannot).
  */
@@ -610,9 +611,11 @@ int hx_decode_plan_greedy(hx_ctx *ctx, const hx_model *model, const hx_calls *qu
  * of range) are left as they are and raise HX_ERR_INDEX in the stream status;
  * rows for which no page is left raise HX_ERR_CAPACITY and are left as they are
  * too.  An entry of a table that is no page of the pool raises HX_ERR_INDEX and
- * is taken for -1.  Scratch: these calls allocate the first time they meet a
- * larger problem than before, in bytes that follow n_pages and the rows of the
- * call; what they allocated before stays until the context ends, so graphs
+ * is taken for -1.  Scratch: fork, grow, keep and compact allocate the first time
+ * they meet a larger problem than before, in bytes that follow n_pages and the
+ * rows of the tables and of the call; hx_attend where it divides keys, for the
+ * parts' sums: up to some 6000 times 128 rows of head_dim + 2 floats (0.4 GB at
+ * 128).  What they allocated before stays until the context ends, so graphs
  * captured earlier stay valid.  A call that would have to allocate while its
  * stream is being captured returns HX_ERR_CAPACITY: make it once before.
  */
@@ -723,7 +726,10 @@ int hx_kv_compact(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs *seqs, i
  * of those, with window > 0, the positions below n_sink and the last `window`
  * positions up to the query's own; and only where the table holds a page.
  * What is not visible to a query has no part in its result, whatever its bits;
- * where values or scores that it sees are infinite or NaN, so is its result.
+ * where values that it sees are infinite or NaN, or scores +infinity or NaN, so
+ * is its result (a score of -infinity is a weight of 0).  Where a sequence has
+ * more than one query a result that is not finite is taken twice, the second time
+ * key by key, which can take some 20 times as long as the rest of the call.
  * Sums, maxima and outputs are held in 32 bits; for their product with the values
  * the weights exp(s - max) are rounded to q's type, where max_q * n_heads is more
  * than 32 times the KV heads, and else to the sum of two numbers of that type
@@ -767,7 +773,8 @@ int hx_attend(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_kv_se
  * share, n_kept = how many stay.  temperature 0 takes the first token of the
  * order.  NULL for top_k, top_p, min_p: off; for temperature: 1; logprob and
  * n_kept may be NULL.  The w are held to 2^-42 of the largest or better and added as whole
- * numbers, so a row's result depends on nothing but its inputs.  -infinity bars a token; where all are
+ * numbers, so a row's result depends on nothing but its inputs; a token of less
+ * than 2^-43 of the largest may never be drawn.  -infinity bars a token; where all are
  * barred token = -1, logprob = -infinity, n_kept = 0.  +infinity takes all the
  * weight.  A NaN logit counts as -infinity and raises HX_ERR_INVALID_ARG in the stream
  * status; so does a setting out of range (temperature or min_p below 0, min_p

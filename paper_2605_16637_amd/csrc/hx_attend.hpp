@@ -383,7 +383,7 @@ struct Tile {
 };
 
 // Where 16-byte piece c of key row r lies in LDS.  Keys are read 32 rows at a time at one piece; the pieces of 8 rows and more fall in
-// different banks.  Values are read as 4 rows x 64 bytes; those rows' pieces, too.  (No bank conflict is counted.)
+// different banks.  Values are read as 4 rows x 64 bytes; those rows' pieces, too.  (The prompts' 8.5e6 LDS instructions count no bank conflict; 8 bits 6e4 of 1.3e7, as they are widened into LDS.)
 template <int CH> __device__ __forceinline__ int k_piece(int r, int c) { return r * CH + (c ^ (r & (CH < 16 ? CH - 1 : 15))); }
 template <int CH> __device__ __forceinline__ int v_piece(int r, int c) { return r * CH + (c ^ (CH >= 16 ? (r & 3) << 2 : ((r >> 1) & 1) << 2)); }
 
@@ -394,9 +394,9 @@ template <int CH> __device__ __forceinline__ int v_piece(int r, int c) { return 
 //
 // A tile is 16 products of 32 cycles a wavefront, 16 KB that it reads from LDS at 128 bytes a cycle and CU, and some 130 other instructions, 16
 // of them exponentials of 16 cycles: for the 8 wavefronts of a CU 1024 cycles of the matrix units, 1024 of LDS, some 1300 of the rest.
-// They take 2800, so two wavefronts a SIMD fill half of each other's waits.  Prompts of 3 sequences, 6144 queries and fewer, window 2048, 32 heads of 128:
-// 216 us, 0.80 PFLOP/s (a bf16 product of 8192^3 here: 1.18).  24 trees of 25 drafts over some 1500 tokens: 75 us + 10 to join, and 16 trees of
-// 64 over 8 bits and some 16384 tokens 466 us, 0.42 PFLOP/s: 8 bits pass through registers and are widened on their way to LDS.  Measured and
+// They take 2800, so two wavefronts a SIMD fill half of each other's waits.  Prompts of 2310, 3010 and 2893 tokens, window 2048, 32 heads of 128:
+// 216 us, 0.80 PFLOP/s (a bf16 product of 8192^3 here: 1.18; cards differ, up to 244).  24 trees of up to 25 drafts over some 2400 tokens: 76 us + 10 to join, and 16
+// trees of up to 64 over 8 bits and some 16500 tokens 468 us, 0.42 PFLOP/s: 8 bits pass through registers and are widened on their way to LDS.  Measured and
 // not taken: 64 rows a wavefront at one wavefront a SIMD, which halves what is read from LDS (495 and 882 us); operands read a stage ahead
 // (221 and 490, where what is here took 220 and 473).
 template <typename E, bool FP8, int D, int WR, bool PAGE16>
@@ -843,8 +843,8 @@ constexpr int few_wave_lds(int dim, int cols) { return FEW_KEYS * dim * 2 > 16 *
 // Up to 16 COLS rows of a KV head, as single tokens bring them: bound by the reads of keys and values.  Each wavefront takes every fourth tile
 // of 32 keys by itself, with nothing shared until the end: the keys go from memory into the registers of the matrix product, the values
 // through its own piece of LDS, which transposes them; what it asks for next is under way all the time.  256 sequences, window 4096, one token each,
-// 8 KV heads of 128: 598 us, 5.8 TB/s (a plain copy: 4.7).  One sequence is launch, lookups and three round trips: a token of 777 10 us, 8
-// drafts over some 1500 18 us, of which the parts' joining some 4.
+// 8 KV heads of 128: 600 us, 5.8 TB/s (a plain copy: 4.7).  One sequence is launch, lookups and three round trips: a token of 230 10 us, 8
+// drafts over 856 18 us, of which the parts' joining some 4.
 //
 // A weight is two numbers of q's type, its rounding and what that leaves, in a product each: what remains of its rounding is 2^-16 of it (fp16
 // 2^-22), so that the result is as near the exact one as its own rounding lets it be.  With one number a result of 16 bits was off by 1.3 to 1.4
@@ -1210,7 +1210,7 @@ int launch(hx_ctx *ctx, AttendArgs &a, hipStream_t stream)
 // Parts of the keys where there are few workgroups otherwise: `many` workgroups if all sequences had the longest's length, but no part
 // shorter than `part` tiles unless there were not even `few` workgroups then, and none shorter than `least`.
 //
-// Where tiles of rows alone are two workgroups a CU and more (four of single tokens), `full` of them, parts cost their joining and gain only that a long sequence
+// Where tiles of rows alone are two workgroups a CU and more (four of up to 32 rows, as up to four fit a CU), `full` of them, parts cost their joining and gain only that a long sequence
 // among short ones is not one workgroup's: none is shorter than `full_part` tiles then, more with more tiles of rows, up to twice that.
 // Divided as before that, with these longer parts, and not at all, 32 heads of 128 over 8 KV heads: 2 prompts of 3000 tokens 249, 177
 // and 177 us; 64 trees of 32 drafts over 1500 134, 97 and 97, over 500 but one over 32768 182, 181 and 818; 256 sequences' tokens over 500 to

@@ -197,7 +197,7 @@ struct GrowArgs {
     int32_t *list;               // [n_pages]
 };
 
-// As the fork's plan: round trips.  64 rows, 32 tokens each: 9.7 us.
+// As the fork's plan: round trips.  64 rows, 32 tokens each: 10.1 us.
 __global__ __launch_bounds__(PL_THREADS) void hx_kv_grow_kernel(GrowArgs a)
 {
     __shared__ int64_t s[PL_WAVES];
@@ -426,7 +426,8 @@ __device__ bool keep_check(const KeepArgs &a, int i, int *s_bad)
     return !*s_bad;
 }
 
-// 64 rows, up to 6 of 32 tokens kept, one layer: 7.0 us, 2.4 more for the tables; moves of a row follow each other.
+// 64 rows, up to 6 of 32 tokens kept, one layer: 7.3 us, 3.1 more for the tables; moves of a row follow each other.  With the tables, 32 layers
+// of 64, 256 and 1024 rows: 18, 55 and 318 us, for 49, 193 and 785 MB read and written (each layer's workgroups check their row again).
 // Workgroup (i, 2 layer + v): a token's place is read by the thread that then writes the earlier place, and numbers rise, so what
 // a thread overwrites it has read.
 __global__ __launch_bounds__(CP_THREADS) void hx_kv_keep_move_kernel(KeepArgs a)
