@@ -727,9 +727,9 @@ int hx_kv_compact(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs *seqs, i
  * positions up to the query's own; and only where the table holds a page.
  * What is not visible to a query has no part in its result, whatever its bits;
  * where values that it sees are infinite or NaN, or scores +infinity or NaN, so
- * is its result (a score of -infinity is a weight of 0).  Where a sequence has
- * more than one query a result that is not finite is taken twice, the second time
- * key by key, which can take some 20 times as long as the rest of the call.
+ * is its result (a score of -infinity is a weight of 0).  A result that is not
+ * finite is taken twice, the second time key by key, which can take some 20 times
+ * as long as the rest of the call.
  * Sums, maxima and outputs are held in 32 bits; for their product with the values
  * the weights exp(s - max) are rounded to q's type, where max_q * n_heads is more
  * than 32 times the KV heads, and else to the sum of two numbers of that type

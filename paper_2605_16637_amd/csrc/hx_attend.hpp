@@ -707,9 +707,8 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : D == 64 && !FP8 && PAGE16 ?
     l += l1;
     l += other_half(l);
     // A weight of 0 times an infinite or NaN value is no 0: where a row's sums are not finite they are taken again key by key, from what it
-    // sees alone.  (A single query's heads all see the same keys, those that the extent holds and a page has, and none else is loaded; a
-    // single draft that is left out sees none, and its sums go nowhere.)
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(any_odd<D / 32>(o)) != 0 && sq.nq > 1, false)) {
+    // sees alone, with weights of 32 bits, which an infinite value leaves infinite.
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(any_odd<D / 32>(o)) != 0, false)) {
         const float m_use = m == NEG_INF ? 0.0f : m;
 #pragma unroll
         for (int x = 0; x < D / 32; ++x) o[x] = f32x16{};
@@ -1078,7 +1077,7 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4
     // sums that are not finite, as above
     bool odd = any_odd<D / 16>(o[0]);
     if constexpr (COLS == 2) odd |= any_odd<D / 16>(o[1]);
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0 && sq.nq > 1, false)) {
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, false)) {
 #pragma unroll
         for (int w = 0; w < COLS; ++w)
 #pragma unroll

@@ -784,6 +784,31 @@ def test_infinite_and_nan_values_that_some_queries_do_not_see(ctx, type_, dim, g
     assert status(ctx) == 0
 
 
+@pytest.mark.parametrize("type_,cache", [("bf16", "bf16"), ("f16", "f16")])
+@pytest.mark.parametrize("dim,group,n", [(64, 1, 5), (128, 4, 3000), (128, 20, 700), (256, 2, 90), (64, 40, 700), (128, 40, 6000)])
+def test_a_single_token_that_sees_infinite_values(ctx, type_, cache, dim, group, n):
+    """Weights are above 0: an infinite value leaves its sum infinite, two of opposite signs leave none, and other numbers stay as they are."""
+    import torch
+    T = 16
+    g = torch.Generator().manual_seed(n)
+    k, v = (torch.randn(1, -(-n // T), 1, T, dim, generator=g).to(sh.torch_type(cache)).cuda() for _ in range(2))
+    q = torch.randn(1, group, dim, generator=g).to(sh.torch_type(type_)).cuda()
+    args = (sh.i32(np.arange(-(-n // T))[None]), sh.i32([n]), sh.i32([0, 1]), q, T)
+    was, was_lse = attend_out(ctx, k, v, *args)
+    at = [1, n // 2, n - 1]
+    for y in at:
+        v[0, y // T, 0, y % T, 1] = float("inf")
+        v[0, y // T, 0, y % T, 2] = float("-inf")
+        v[0, y // T, 0, y % T, 3] = float("inf") if y == at[0] else float("-inf")
+    got, lse = attend_out(ctx, k, v, *args)
+    assert (got[..., 1] == np.inf).all() and (got[..., 2] == -np.inf).all() and np.isnan(got[..., 3]).all()
+    assert np.array_equal(lse, was_lse)
+    rest = np.arange(dim) > 3
+    near = 2 * (2 * sh.HALF_STEP[type_] + 2.0 ** -12) * float(v.float().abs()[..., 4:].max())
+    assert (np.abs(got - was)[..., rest] <= near).all()
+    assert status(ctx) == 0
+
+
 def test_a_single_token_that_sees_no_number(ctx):
     import torch
     g = torch.Generator().manual_seed(1)
