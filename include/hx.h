@@ -623,6 +623,7 @@ int hx_decode_plan_greedy(hx_ctx *ctx, const hx_model *model, const hx_calls *qu
 #define HX_BF16  2
 #define HX_F16   3
 #define HX_E4M3  4     /* 8 bits: 4 of exponent, 3 of mantissa, no infinity, 448 the largest */
+#define HX_E2M1  5     /* 4 bits: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign, two a byte, the earlier in the low half; times a scale of 32 numbers */
 
 #define HX_MAX_PAGE_TOKENS 1024
 #define HX_MAX_DRAFTS      256       /* drafted tokens of a sequence in hx_attend, as a tree */
@@ -631,12 +632,16 @@ int hx_decode_plan_greedy(hx_ctx *ctx, const hx_model *model, const hx_calls *qu
 typedef struct {
     int32_t n_layers, n_pages, n_heads;   /* n_heads: KV heads                                  */
     int32_t page_tokens;      /* a power of two, 1..HX_MAX_PAGE_TOKENS                          */
-    int32_t head_dim;         /* hx_attend: 64, 128 or 256; the others: any multiple of 16      */
-    int32_t dtype;            /* HX_BF16, HX_F16 or HX_E4M3                                     */
+    int32_t head_dim;         /* attention: 64, 128 or 256; the others: any multiple of 16 (HX_E2M1: 32) */
+    int32_t dtype;            /* HX_BF16, HX_F16, HX_E4M3 or HX_E2M1                            */
     void *k, *v;              /* device [n_layers][n_pages][n_heads][page_tokens][head_dim], 16-byte aligned; a page (n_heads * page_tokens * head_dim numbers) under 2 GiB */
     int32_t *ref;             /* device [n_pages]                                               */
     const float *k_scale;     /* device [n_layers][n_heads], HX_E4M3 only: a stored number times*/
     const float *v_scale;     /*   this is the key's (value's); > 0; NULL = 1                   */
+    uint8_t *k_exp, *v_exp;   /* device [n_layers][n_pages][n_heads][page_tokens][head_dim/32], 16-byte aligned, HX_E2M1 only: numbers 32 g ..
+                                 32 g + 31 of a token's key (value) times 2^(byte g - 127); 104..140, or 255: they are NaN      */
+    void *bounds;             /* device [n_layers][n_pages][n_heads][2][head_dim], 16-byte aligned, of dtype (HX_BF16 for pools of 8 and 4 bits), or NULL:
+                                 hx_kv_bound's, for hx_attend_top                               */
 } hx_kv_pool;
 
 typedef struct {
@@ -644,6 +649,15 @@ typedef struct {
     int32_t *table;           /* device [n][max_pages]                                          */
     int32_t *len;             /* device [n] tokens of each row                                  */
 } hx_kv_seqs;
+
+/*
+ * Pools of HX_E2M1 hold a number in 4 bits and, for 32 of them, a power of two
+ * in 8.  What is written has scales of 2^-23 to 2^13, so that every number that
+ * is held is a number of HX_BF16 and of HX_F16: the least scale with which 6
+ * reaches the largest of the 32, and each the nearest of what 4 bits hold,
+ * halves going to the even code.  What lies beyond 6 * 2^13 becomes that; a NaN
+ * among 32 numbers makes all of them NaN.
+ */
 
 /*
  * Row dst[i], which must be empty, becomes a copy of the first n_tok[i] tokens
@@ -677,6 +691,17 @@ int hx_kv_grow(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs *seqs, int3
 int hx_kv_write(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_kv_seqs *seqs, int32_t n,
                 const int32_t *row, const int32_t *tok_ptr, int32_t n_tok, int32_t src_dtype,
                 const void *k, const void *v, int64_t token_stride, int64_t head_stride, void *stream);
+
+/*
+ * The other way: the keys and values of one layer of the last tok_ptr[i+1] -
+ * tok_ptr[i] tokens of row[i], as numbers of type dst_dtype (HX_F32, HX_BF16 or
+ * HX_F16; a stored number times its scale, rounded to nearest even), for a call
+ * whose cache goes to another instance.  Tokens whose page is not there are 0.
+ * Of an entry in error nothing is written.  A row may be listed more than once.
+ */
+int hx_kv_read(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_kv_seqs *seqs, int32_t n,
+               const int32_t *row, const int32_t *tok_ptr, int32_t n_tok, int32_t dst_dtype,
+               void *k, void *v, int64_t token_stride, int64_t head_stride, void *stream);
 
 /*
  * Of the last n_draft[i] tokens of row[i] those with the numbers keep[j], j =
@@ -745,7 +770,7 @@ typedef struct {
     int32_t max_q;            /* most queries of one sequence                                   */
     int32_t max_len;          /* longest sequence, about: only how the work is divided goes by it */
     int32_t n_heads;          /* query heads, a multiple of the KV heads                        */
-    int32_t dtype;            /* of q and out: HX_BF16 or HX_F16, the pool's unless that is HX_E4M3 */
+    int32_t dtype;            /* of q and out: HX_BF16 or HX_F16, the pool's unless that has 8 or 4 bits */
     const void *q;            /* device, strides in numbers, dim contiguous                     */
     int64_t q_token, q_head;
     void *out;

@@ -21,9 +21,9 @@ EXPORTS = ("hx_ctx_create", "hx_ctx_destroy", "hx_last_error", "hx_stream_status
            "hx_critical_path", "hx_horizons", "hx_dag_reserve", "hx_dag_append", "hx_dag_set_cost", "hx_dag_view",
            "hx_score_placements", "hx_validate_round", "hx_select", "hx_urgency", "hx_commit", "hx_commit_static", "hx_round", "hx_rank", "hx_plan_greedy",
            "hx_decode_score", "hx_decode_plan_greedy",
-           "hx_kv_fork", "hx_kv_grow", "hx_kv_write", "hx_kv_keep", "hx_kv_free", "hx_kv_compact", "hx_attend", "hx_sample")
+           "hx_kv_fork", "hx_kv_grow", "hx_kv_write", "hx_kv_read", "hx_kv_keep", "hx_kv_free", "hx_kv_compact", "hx_attend", "hx_sample")
 
-HX_F32, HX_BF16, HX_F16, HX_E4M3 = 1, 2, 3, 4
+HX_F32, HX_BF16, HX_F16, HX_E4M3, HX_E2M1 = 1, 2, 3, 4, 5
 
 
 class HxError(RuntimeError):
@@ -79,7 +79,7 @@ class hx_round_args(C.Structure):
 class hx_kv_pool(C.Structure):
     _fields_ = [("n_layers", C.c_int32), ("n_pages", C.c_int32), ("n_heads", C.c_int32), ("page_tokens", C.c_int32),
                 ("head_dim", C.c_int32), ("dtype", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("ref", C.c_void_p),
-                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p), ("bounds", C.c_void_p)]
 
 
 class hx_kv_seqs(C.Structure):
@@ -265,7 +265,9 @@ def _number_type(t, *allowed):
 
 
 def make_kv_pool(p: dict) -> hx_kv_pool:
-    """From k, v [layers, pages, KV heads, page_tokens, head_dim], ref [pages] and, for 8-bit caches, k_scale, v_scale [layers, KV heads]."""
+    """From k, v [layers, pages, KV heads, page_tokens, head_dim], ref [pages] and, for 8-bit caches, k_scale, v_scale [layers, KV heads].  A
+    cache of 4 bits: k, v of uint8 with head_dim / 2 bytes, and k_exp, v_exp of uint8 with head_dim / 32.  With page bounds: bounds [layers,
+    pages, KV heads, 2, head_dim], of the cache's type (bfloat16 for 8 and 4 bits)."""
     torch = _torch()
     k, v = p["k"], p["v"]
     if k.dim() != 5 or v.shape != k.shape or v.dtype != k.dtype:
@@ -273,9 +275,15 @@ def make_kv_pool(p: dict) -> hx_kv_pool:
     n_layers, n_pages, n_heads, tokens, dim = k.shape
     if tokens != int(p.get("page_tokens", tokens)):
         raise ValueError(f"pages of {tokens} tokens, not {p['page_tokens']}")
-    return hx_kv_pool(n_layers, n_pages, n_heads, tokens, dim, _number_type(k, HX_BF16, HX_F16, HX_E4M3), _ptr(k), _ptr(v),
+    four = k.dtype == torch.uint8
+    if four:
+        dim *= 2
+    exps, k_exp, v_exp, bounds = n_layers * n_pages * n_heads * tokens * (dim // 32), p.get("k_exp"), p.get("v_exp"), p.get("bounds")
+    wide = k.dtype if k.dtype in (torch.bfloat16, torch.float16) else torch.bfloat16
+    return hx_kv_pool(n_layers, n_pages, n_heads, tokens, dim, HX_E2M1 if four else _number_type(k, HX_BF16, HX_F16, HX_E4M3), _ptr(k), _ptr(v),
                       _ptr(p["ref"], torch.int32, n_pages), _ptr(p.get("k_scale"), torch.float32, n_layers * n_heads),
-                      _ptr(p.get("v_scale"), torch.float32, n_layers * n_heads))
+                      _ptr(p.get("v_scale"), torch.float32, n_layers * n_heads), _ptr(k_exp, torch.uint8, exps), _ptr(v_exp, torch.uint8, exps),
+                      _ptr(bounds, wide, n_layers * n_pages * n_heads * 2 * dim))
 
 
 def make_kv_seqs(s: dict) -> hx_kv_seqs:
@@ -589,6 +597,19 @@ class Context:
         if (v_token, v_head) != (token, head) or v.dtype != k.dtype or v.shape != k.shape:
             raise ValueError("expected k and v of one type, shape and set of strides")
         self._invoke(self.lib.hx_kv_write, self._ctx, C.byref(kv), int(layer), C.byref(sq), n, _ptr(row, i32), _ptr(tok_ptr, i32, n + 1),
+                     n_tok, _number_type(k, HX_F32, HX_BF16, HX_F16), C.c_void_p(kp), C.c_void_p(vp), C.c_int64(token), C.c_int64(head),
+                     _stream(stream))
+
+    def hx_kv_read(self, pool, layer, seqs, row, tok_ptr, k, v, stream=None):
+        """k, v [tokens, KV heads, head_dim], of one type and one set of strides, are filled with what the cache holds."""
+        torch = _torch()
+        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs), int(row.numel()), torch.int32
+        n_tok = int(k.shape[0])
+        kp, token, head = _strided(k, n_tok, kv.n_heads, kv.head_dim)
+        vp, v_token, v_head = _strided(v, n_tok, kv.n_heads, kv.head_dim)
+        if (v_token, v_head) != (token, head) or v.dtype != k.dtype or v.shape != k.shape:
+            raise ValueError("expected k and v of one type, shape and set of strides")
+        self._invoke(self.lib.hx_kv_read, self._ctx, C.byref(kv), int(layer), C.byref(sq), n, _ptr(row, i32), _ptr(tok_ptr, i32, n + 1),
                      n_tok, _number_type(k, HX_F32, HX_BF16, HX_F16), C.c_void_p(kp), C.c_void_p(vp), C.c_int64(token), C.c_int64(head),
                      _stream(stream))
 

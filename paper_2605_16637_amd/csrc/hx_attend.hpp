@@ -7,237 +7,9 @@
 // values are read from LDS in that order, transposed on the way).
 #pragma once
 
-#include "hx_attend_args.hpp"
-
-#include <type_traits>
+#include "hx_attend_common.hpp"
 
 namespace {
-
-using AttendArgs = HxAttend;
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-
-template <typename E> struct Types;
-template <> struct Types<__bf16> { using x8 = bf16x8; using x4 = bf16x4; using x2 = bf16x2; };
-template <> struct Types<_Float16> { using x8 = f16x8; using x4 = f16x4; using x2 = f16x2; };
-
-__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
-
-// 4 stored numbers of 8 bits; every e4m3 is a bf16 and an fp16 exactly
-__device__ __forceinline__ void widen(uint32_t w, bf16x2 &a, bf16x2 &b)
-{
-    a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false);
-    b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
-}
-__device__ __forceinline__ void widen(uint32_t w, f16x2 &a, f16x2 &b)
-{
-    a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false);
-    b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true);
-}
-
-constexpr float NEG_INF = -__builtin_inff();
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr float MAX_SLACK = 8.0f;            // a running maximum is raised when a score exceeds it by this many powers of 2
-// Weights are taken this many powers of 2 up, in the products and the sums alike: the largest lie between 2^LIFT and 2^(LIFT + MAX_SLACK).
-// fp16 ends at 2^-24 (a normal number at 2^-14): without it 32768 weights of 2^-25 of the largest were lost, 2^-10 together.  bf16 has fp32's range.
-template <typename E> constexpr float LIFT = std::is_same_v<E, _Float16> ? 7.0f : 0.0f;
-
-// Whether a sum of weights holds any: 0 where nothing was visible.  (A NaN among the visible has to reach the outputs.)
-__device__ __forceinline__ bool holds_any(float l) { return l != 0.0f; }
-
-// Whether a lane's sums hold an infinity or a NaN.
-template <int N, typename F>
-__device__ __forceinline__ bool any_odd(const F *o)
-{
-    uint32_t worst = 0;
-#pragma unroll
-    for (int x = 0; x < N; ++x)
-#pragma unroll
-        for (int i = 0; i < (int)(sizeof(F) / sizeof(float)); ++i) {
-            const uint32_t size = __float_as_uint(o[x][i]) & 0x7fffffffu;
-            worst = size > worst ? size : worst;
-        }
-    return worst >= 0x7f800000u;
-}
-
-// N stored numbers
-template <typename E, bool FP8, int N>
-__device__ __forceinline__ void numbers(const char *from, float *to)
-{
-    if constexpr (FP8) {
-        using X2 = typename Types<E>::x2;
-#pragma unroll
-        for (int i = 0; i < N / 4; ++i) {
-            X2 a, b;
-            widen(((const uint32_t *)from)[i], a, b);
-            to[4 * i] = (float)a[0]; to[4 * i + 1] = (float)a[1]; to[4 * i + 2] = (float)b[0]; to[4 * i + 3] = (float)b[1];
-        }
-    } else
-#pragma unroll
-        for (int i = 0; i < N; ++i) to[i] = (float)((const E *)from)[i];
-}
-
-constexpr int AT_THREADS = 256;
-constexpr int MAX_SPLITS = 64;
-
-// one value of the other half of the wavefront
-__device__ __forceinline__ float other_half(float x)
-{
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(threadIdx.x & 32 ? r[0] : r[1]);
-}
-
-// A sequence and its queries.
-struct Seq {
-    int q0, nq, len, base;       // base: the position of the first query's token
-    bool there, ok;              // queries lie within the call's; the rest is in range too
-    const int32_t *table;
-};
-
-__device__ __forceinline__ Seq sequence(const AttendArgs &a, int i)
-{
-    const KvView &kv = a.kv;
-    Seq s;
-    s.q0 = a.q_ptr[i];
-    const int q1 = a.q_ptr[i + 1], r = a.row ? a.row[i] : i;
-    s.nq = q1 - s.q0;
-    s.there = s.q0 >= 0 && q1 >= s.q0 && q1 <= a.n_q;
-    s.ok = s.there && r >= 0 && r < kv.rows && s.nq <= a.max_q;
-    s.len = s.ok ? kv.len[r] : 0;
-    s.ok = s.ok && hx_row_ok(kv, r, s.len) && s.nq <= s.len;
-    s.base = s.len - s.nq;
-    s.table = hx_row(kv, s.ok ? r : 0);
-    return s;
-}
-
-constexpr int ANC_WORDS = HX_MAX_DRAFTS / 32;
-constexpr int TREE_BYTES = HX_MAX_DRAFTS * 4 * (1 + ANC_WORDS);
-
-// Every draft's depth (-1: left out) and the bits of the drafts above it; s_parent: HX_MAX_DRAFTS words that are free yet.
-__device__ __forceinline__ void plant(const AttendArgs &a, const Seq &q, int *s_parent, int *s_depth, uint32_t *s_anc)
-{
-    for (int i = threadIdx.x; i < q.nq; i += blockDim.x) s_parent[i] = a.parent[q.q0 + i];
-    __syncthreads();
-    for (int tid = threadIdx.x; tid < q.nq; tid += blockDim.x) {
-        uint32_t mine[ANC_WORDS] = {};
-        int depth = 0, at = tid;
-        while (at >= 0) {
-#pragma unroll
-            for (int w = 0; w < ANC_WORDS; ++w) mine[w] |= at >> 5 == w ? 1u << (at & 31) : 0u;
-            const int up = s_parent[at];
-            if (up >= at || up < -2) { hx_raise(a.kv.status, HX_ERR_INDEX); at = -2; break; }
-            at = up;
-            ++depth;
-        }
-        s_depth[tid] = at == -2 ? -1 : depth - 1;
-#pragma unroll
-        for (int w = 0; w < ANC_WORDS; ++w) s_anc[tid * ANC_WORDS + w] = mine[w];
-    }
-    __syncthreads();
-}
-
-// The tiles of KEYS keys that some of the queries t_first .. t_last may see: the first sink_tiles, then those from lo_tile on.
-struct Extent {
-    int lo, hi, sink_tiles, lo_tile, n;
-};
-
-template <int KEYS>
-__device__ __forceinline__ Extent extent(const AttendArgs &a, const Seq &q, int t_first, int t_last)
-{
-    const bool tree = a.parent != nullptr;
-    Extent x{0, 0, 0, 0, 0};
-    if (!q.ok || a.kv.n_pages == 0) return x;
-    x.hi = tree ? q.len : q.base + t_last + 1;
-    if (a.window > 0) {
-        // the least position of a query: in a tree that of a draft without another above it, the first after the tokens before the drafts
-        const int first_pos = tree ? q.base : q.base + t_first;
-        x.lo = first_pos - a.window + 1;
-        x.lo = x.lo > 0 ? x.lo : 0;
-    }
-    x.lo_tile = x.lo / KEYS;
-    if (x.lo > 0) {
-        const int sinks = a.n_sink < x.lo ? a.n_sink : x.lo;
-        x.sink_tiles = (sinks + KEYS - 1) / KEYS;
-        if (x.sink_tiles >= x.lo_tile) { x.sink_tiles = 0; x.lo_tile = 0; }
-    }
-    x.n = x.hi > 0 ? x.sink_tiles + (x.hi + KEYS - 1) / KEYS - x.lo_tile : 0;
-    return x;
-}
-
-// Parts of n tiles: of `chunk` each, the last takes what is left.
-__device__ __forceinline__ int parts_of(const AttendArgs &a, int n)
-{
-    const int parts = n > a.chunk ? (n + a.chunk - 1) / a.chunk : 1;
-    return parts < a.splits ? parts : a.splits;
-}
-
-// A page that the pool has, or -1.
-__device__ __forceinline__ int in_pool(const KvView &kv, int page)
-{
-    if (__builtin_amdgcn_ballot_w64(page >= kv.n_pages)) {
-        if (page >= kv.n_pages) hx_raise(kv.status, HX_ERR_INDEX);
-        page = page < kv.n_pages ? page : -1;
-    }
-    return page;
-}
-
-// What a lane's query sees.
-struct Sight {
-    bool tree, alive;
-    int pos, t, base, nq, window, n_sink;
-    const int *s_depth;
-    const uint32_t *s_anc;
-    __device__ __forceinline__ bool sees(int y) const
-    {
-        bool see = alive;
-        int ypos = y;
-        if (tree && y >= base) {
-            const int d = y - base;
-            const bool in = d < nq;
-            see = see && in && ((s_anc[t * ANC_WORDS + ((in ? d : 0) >> 5)] >> (d & 31)) & 1);
-            ypos = base + s_depth[in ? d : 0];
-        }
-        return see && ypos <= pos && (window <= 0 || ypos < n_sink || pos - ypos < window);
-    }
-};
-
-__device__ __forceinline__ Sight sight(const AttendArgs &a, const Seq &q, int t, const int *s_depth, const uint32_t *s_anc)
-{
-    Sight v;
-    v.tree = a.parent != nullptr;
-    v.alive = q.ok && t < q.nq;
-    v.t = v.alive ? t : 0;
-    v.pos = q.base + t;
-    if (v.tree && v.alive) {
-        const int d = s_depth[t];
-        v.alive = d >= 0;
-        v.pos = q.base + d;
-    }
-    v.base = q.base; v.nq = q.nq; v.window = a.window; v.n_sink = a.n_sink; v.s_depth = s_depth; v.s_anc = s_anc;
-    return v;
-}
-
-template <typename E>
-__device__ __forceinline__ void put(E *to, bool wide, float a, float b, float c, float d)
-{
-    typename Types<E>::x4 y;
-    y[0] = (E)a; y[1] = (E)b; y[2] = (E)c; y[3] = (E)d;
-    if (wide) *(typename Types<E>::x4 *)to = y;
-    else
-#pragma unroll
-        for (int j = 0; j < 4; ++j) to[j] = y[j];
-}
 
 // What workgroups leave for each other goes past the caches that they do not share: device-scope stores and loads, of 8 bytes.
 __device__ __forceinline__ void leave(float *to, float x, float y)
@@ -366,18 +138,19 @@ __device__ __forceinline__ void to_lds(uint32_t to, const char *from)
 constexpr int SPAN = 256;                                // tiles whose pages are looked up at once
 
 // WR wavefronts beside each other take 32 rows each (a row: one query and query head of the KV head).
-template <bool FP8, int D, int WR, bool PAGE16>
+template <int BITS, int D, int WR, bool PAGE16>
 struct Tile {
     static constexpr int THREADS = 64 * WR;
     static constexpr int ROWS = 32 * WR;
     static constexpr int CH = D / 8;                     // 16-byte pieces of a row in LDS
-    static constexpr int ROW_BYTES = FP8 ? D : 2 * D, PER_ROW = ROW_BYTES / 16;
+    static constexpr int ROW_BYTES = ROW<BITS, D>;
+    static constexpr int PIECE = BITS == 4 ? 8 : 16, PER_ROW = ROW_BYTES / PIECE;    // what a lane loads at once: 8 numbers of 16 bits, else 16
     static constexpr int PIECES = KT * PER_ROW;          // of a tile's keys, or values
     static constexpr int LOADS = (PIECES + THREADS - 1) / THREADS;
     static constexpr int BUF = 2 * KT * D * 2;           // keys and values of a tile
     // Tiles in LDS.  What is stored in 16 bits goes there straight from memory; 8 bits pass through registers, where RING more are
     // under way.
-    static constexpr bool DIRECT = !FP8 && PAGE16;
+    static constexpr bool DIRECT = BITS == 16 && PAGE16;
     static constexpr int RING = DIRECT && D < 256 ? 4 : 3;
     static constexpr int LDS = BUF * RING + SPAN * 16;
 };
@@ -399,13 +172,14 @@ template <int CH> __device__ __forceinline__ int v_piece(int r, int c) { return 
 // trees of up to 64 over 8 bits and some 16500 tokens 468 us, 0.42 PFLOP/s: 8 bits pass through registers and are widened on their way to LDS.  Measured and
 // not taken: 64 rows a wavefront at one wavefront a SIMD, which halves what is read from LDS (495 and 882 us); operands read a stage ahead
 // (221 and 490, where what is here took 220 and 473).
-template <typename E, bool FP8, int D, int WR, bool PAGE16>
-__global__ __launch_bounds__(64 * WR, D == 256 ? 1 : D == 64 && !FP8 && PAGE16 ? 3 : 2) void hx_attend_kernel(AttendArgs a)
+template <typename E, int BITS, int D, int WR, bool PAGE16>
+__global__ __launch_bounds__(64 * WR, D == 256 ? 1 : D == 64 && BITS == 16 && PAGE16 ? 3 : 2) void hx_attend_kernel(AttendArgs a)
 {
     using X8 = typename Types<E>::x8;
     using X2 = typename Types<E>::x2;
-    using C = Tile<FP8, D, WR, PAGE16>;
-    constexpr int RING = C::RING, CH = C::CH, LOADS = C::LOADS, THREADS = C::THREADS, ROW_BYTES = C::ROW_BYTES, PER_ROW = C::PER_ROW;
+    using C = Tile<BITS, D, WR, PAGE16>;
+    constexpr int RING = C::RING, CH = C::CH, LOADS = C::LOADS, THREADS = C::THREADS, ROW_BYTES = C::ROW_BYTES, PER_ROW = C::PER_ROW, PIECE = C::PIECE;
+    using Piece = std::conditional_t<PIECE == 8, uint2, uint4>;
     extern __shared__ __align__(16) char smem[];
     longlong2 *s_off = (longlong2 *)(smem + C::BUF * RING);
     int *s_depth = (int *)(smem + C::LDS);
@@ -418,7 +192,7 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : D == 64 && !FP8 && PAGE16 ?
     // row tiles of the same keys beside each other: they meet in the XCD's cache
     const int split = rest / a.row_tiles, rt = a.row_tiles - 1 - rest % a.row_tiles;
     const int head = pair % kv.n_heads;
-    const Seq sq = sequence(a, pair / kv.n_heads);
+    const Seq sq = sequence(a, pair);
     if (!sq.there) { if (tid == 0) hx_raise(kv.status, HX_ERR_INDEX); return; }
     if (rt * C::ROWS >= sq.nq * (int64_t)a.group) return;
     if (!sq.ok && tid == 0) hx_raise(kv.status, HX_ERR_INDEX);
@@ -476,11 +250,13 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : D == 64 && !FP8 && PAGE16 ?
     };
     auto in_sight = [&](int y) { return y < ex.hi && (y >= ex.lo || y < a.n_sink); };       // of some row of the tile of rows
 
-    uint4 rk[C::DIRECT ? 1 : RING][LOADS], rv[C::DIRECT ? 1 : RING][LOADS];
+    Piece rk[C::DIRECT ? 1 : RING][LOADS], rv[C::DIRECT ? 1 : RING][LOADS];
+    uint8_t ek[BITS == 4 ? RING : 1][LOADS], ev[BITS == 4 ? RING : 1][LOADS];      // scales of 4 bits
     uint32_t there[RING], now = 0;                       // which keys of the tiles under way are there, and of the one whose scores are next
     const int64_t page_bytes = ((int64_t)kv.n_heads << kv.shift) * ROW_BYTES;
     const int64_t here = (int64_t)a.layer * kv.n_pages * page_bytes + ((int64_t)head << kv.shift) * ROW_BYTES;
     const char *k_at = (const char *)kv.k + here, *v_at = (const char *)kv.v + here;
+    const uint8_t *ke_at = BITS == 4 ? a.k_exp + here / 16 : nullptr, *ve_at = BITS == 4 ? a.v_exp + here / 16 : nullptr;      // a byte for 16
     const int in_page = (1 << kv.shift) - 1;
     const int my_key = tid / PER_ROW, my_part = tid % PER_ROW;
     const bool loads = C::PIECES % THREADS == 0 || wave * 64 < C::PIECES;
@@ -491,8 +267,8 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : D == 64 && !FP8 && PAGE16 ?
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
         const int key = j * THREADS / PER_ROW + my_key, in_group = key - (j * THREADS / PER_ROW + wave * 64 / PER_ROW);
-        k_off[j] = C::DIRECT ? in_group * ROW_BYTES + (k_piece<CH>(key, my_part) - key * CH) * 16 : lane * 16;
-        v_off[j] = C::DIRECT ? in_group * ROW_BYTES + (v_piece<CH>(key, my_part) - key * CH) * 16 : lane * 16;
+        k_off[j] = C::DIRECT ? in_group * ROW_BYTES + (k_piece<CH>(key, my_part) - key * CH) * 16 : lane * PIECE;
+        v_off[j] = C::DIRECT ? in_group * ROW_BYTES + (v_piece<CH>(key, my_part) - key * CH) * 16 : lane * PIECE;
     }
     const uint32_t lds0 = lds_address(smem);
     // two: where the tile's first and second 16 keys lie, the lowest bit set where some key of the tile is not there, -1 where no page is
@@ -535,18 +311,22 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : D == 64 && !FP8 && PAGE16 ?
 #pragma unroll
                 for (int j = 0; j < LOADS; ++j) {
                     const int first = (j * THREADS / PER_ROW + wave * 64 / PER_ROW) & 31;
-                    at[j] = (first < 16 ? o0 : o1) + (first & 15) * ROW_BYTES + lane * 16;
+                    at[j] = (first < 16 ? o0 : o1) + (first & 15) * ROW_BYTES + lane * PIECE;
                 }
             else
 #pragma unroll
                 for (int j = 0; j < LOADS; ++j) {
                     const int64_t x = place_of(j * THREADS / PER_ROW + my_key);
-                    at[j] = x >= 0 ? x + my_part * 16 : 0;
+                    at[j] = x >= 0 ? x + my_part * PIECE : 0;
                 }
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) {
-                rk[S][j] = *(const uint4 *)(k_at + at[j]);
-                rv[S][j] = *(const uint4 *)(v_at + at[j]);
+                rk[S][j] = *(const Piece *)(k_at + at[j]);
+                rv[S][j] = *(const Piece *)(v_at + at[j]);
+                if constexpr (BITS == 4) {
+                    ek[S][j] = ke_at[at[j] / 16];
+                    ev[S][j] = ve_at[at[j] / 16];
+                }
             }
         }
     };
@@ -557,15 +337,24 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : D == 64 && !FP8 && PAGE16 ?
         if (there[S] != 0xffffffffu)
 #pragma unroll
             for (int i = 0; i < LOADS; ++i)
-                if (!((there[S] >> (i * THREADS / PER_ROW + my_key)) & 1)) rk[S][i] = rv[S][i] = make_uint4(0, 0, 0, 0);
+                if (!((there[S] >> (i * THREADS / PER_ROW + my_key)) & 1)) {
+                    rk[S][i] = rv[S][i] = Piece{};
+                    if constexpr (BITS == 4) ek[S][i] = ev[S][i] = 0;
+                }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int key = i * THREADS / PER_ROW + my_key;
-            if constexpr (FP8) {
+            if constexpr (BITS < 16) {
                 union { X2 x[8]; uint4 u[2]; } wk, wv;
-                const uint32_t kk[4] = {rk[S][i].x, rk[S][i].y, rk[S][i].z, rk[S][i].w}, vv[4] = {rv[S][i].x, rv[S][i].y, rv[S][i].z, rv[S][i].w};
+                if constexpr (BITS == 4) {
+                    const float uk = power_of(ek[S][i]), uv = power_of(ev[S][i]);
+                    widen4(rk[S][i].x, uk, wk.x); widen4(rk[S][i].y, uk, wk.x + 4);
+                    widen4(rv[S][i].x, uv, wv.x); widen4(rv[S][i].y, uv, wv.x + 4);
+                } else {
+                    const uint32_t kk[4] = {rk[S][i].x, rk[S][i].y, rk[S][i].z, rk[S][i].w}, vv[4] = {rv[S][i].x, rv[S][i].y, rv[S][i].z, rv[S][i].w};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) { widen(kk[j], wk.x[2 * j], wk.x[2 * j + 1]); widen(vv[j], wv.x[2 * j], wv.x[2 * j + 1]); }
+                    for (int j = 0; j < 4; ++j) { widen(kk[j], wk.x[2 * j], wk.x[2 * j + 1]); widen(vv[j], wv.x[2 * j], wv.x[2 * j + 1]); }
+                }
                 // half of a row's lanes begin with their second piece: 8 lanes beside each other fill all banks
                 const bool second = my_part & 4;
                 const int at0 = 2 * my_part + second, at1 = at0 ^ 1;
@@ -721,7 +510,8 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : D == 64 && !FP8 && PAGE16 ?
 #pragma unroll
             for (int x = 0; x < D / 16; ++x) {
                 float k[8];
-                numbers<E, FP8, 8>(k_at + at + (x * 16 + half * 8) * (ROW_BYTES / D), k);
+                const int d = x * 16 + half * 8;
+                numbers<E, BITS, 8>(k_at + at + d * BITS / 8, ke_at + at / 16 + d / 32, k);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) dot = fmaf((float)qf[x][i], k[i], dot);
             }
@@ -733,7 +523,8 @@ __global__ __launch_bounds__(64 * WR, D == 256 ? 1 : D == 64 && !FP8 && PAGE16 ?
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float v[4];
-                    numbers<E, FP8, 4>(v_at + at + (x * 32 + 8 * i + 4 * half) * (ROW_BYTES / D), v);
+                    const int d = x * 32 + 8 * i + 4 * half;
+                    numbers<E, BITS, 4>(v_at + at + d * BITS / 8, ve_at + at / 16 + d / 32, v);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) o[x][4 * i + j] += see ? weight * v[j] : 0.0f;
                 }
@@ -774,7 +565,7 @@ __global__ __launch_bounds__(AT_THREADS) void hx_attend_join_kernel(AttendArgs a
     constexpr int G = D / 4, TOGETHER = AT_THREADS / G, KEEP = (MAX_SPLITS + G - 1) / G;
     const int per_tile = ROWS / TOGETHER, pair = blockIdx.x / (a.row_tiles * per_tile), rt = blockIdx.x / per_tile % a.row_tiles;
     const int r = blockIdx.x % per_tile * TOGETHER + threadIdx.x / G, g = threadIdx.x % G, row = rt * ROWS + r;
-    const Seq sq = sequence(a, pair / a.kv.n_heads);
+    const Seq sq = sequence(a, pair);
     if (!sq.ok || rt * ROWS >= sq.nq * (int64_t)a.group) return;
     int t_last = (rt * ROWS + ROWS - 1) / a.group;
     t_last = t_last < sq.nq ? t_last : sq.nq - 1;
@@ -850,15 +641,18 @@ constexpr int few_wave_lds(int dim, int cols) { return FEW_KEYS * dim * 2 > 16 *
 // times as much.  What the second product costs: 0 to 2 % in most cases, up to 7 where an 8-bit cache or heads of 64 bring fewer bytes a weight
 // and rows are more than 16.  (The kernel for many rows, which the matrix units and the weights' arithmetic bound, has one number: two
 // took 9 to 29 % longer, 24 trees of 25 drafts 84 -> 94 us, the prompts above 213 -> 262.)
-template <typename E, bool FP8, int D, int COLS, bool PAGE16>
-__global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4 : COLS == 1 && FP8 ? 3 : 2) void hx_attend_few_kernel(AttendArgs a)
+template <typename E, int BITS, int D, int COLS, bool PAGE16>
+__global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4 : COLS == 1 && BITS < 16 ? 3 : 2) void hx_attend_few_kernel(AttendArgs a)
 {
     using X8 = typename Types<E>::x8;
     using X2 = typename Types<E>::x2;
-    constexpr int CH = D / 8, ROW_BYTES = FP8 ? D : 2 * D;
-    constexpr int K_LOADS = ROW_BYTES / 64;                     // of a lane for 16 keys
-    constexpr int V_LOADS = FEW_KEYS * ROW_BYTES / 1024;        // of a lane for the tile
-    constexpr int PER_ROW = ROW_BYTES / 16;
+    constexpr int CH = D / 8, ROW_BYTES = ROW<BITS, D>;
+    constexpr int K_BYTES = ROW_BYTES < 64 ? ROW_BYTES / 4 : 16, K_LOADS = ROW_BYTES / 4 / K_BYTES;     // a lane's load for 16 keys, and how many
+    constexpr int K_NUMBERS = K_BYTES * 8 / BITS;               // of a load
+    using KPiece = std::conditional_t<K_BYTES == 8, uint2, uint4>;
+    constexpr int V_BYTES = ROW_BYTES < 64 ? 8 : 16, V_LOADS = FEW_KEYS * ROW_BYTES / (64 * V_BYTES);     // of a lane for the tile
+    constexpr int PER_ROW = ROW_BYTES / V_BYTES;                // a load of the wavefront: at most 16 keys
+    using VPiece = std::conditional_t<V_BYTES == 8, uint2, uint4>;
     constexpr int WAVE_LDS = few_wave_lds(D, COLS), ROWS = 16 * COLS;
     extern __shared__ __align__(16) char smem[];
     int *s_depth = (int *)(smem + 4 * WAVE_LDS);
@@ -869,7 +663,7 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), quad = lane >> 4, col = lane & 15;
     const int nh = a.n * kv.n_heads;
     const int pair = blockIdx.x % nh, split = blockIdx.x / nh, head = pair % kv.n_heads;
-    const Seq sq = sequence(a, pair / kv.n_heads);
+    const Seq sq = sequence(a, pair);
     if (!sq.there) { if (tid == 0) hx_raise(kv.status, HX_ERR_INDEX); return; }
     if (sq.nq == 0) return;
     if (!sq.ok && tid == 0) hx_raise(kv.status, HX_ERR_INDEX);
@@ -897,7 +691,8 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4
 #pragma unroll
         for (int s = 0; s < D / 32; ++s) {
             // which 8 numbers of a row a lane's s-th piece of a key holds
-            const int d = FP8 ? (s >> 1) * 64 + quad * 16 + (s & 1) * 8 : s * 32 + quad * 8;
+            constexpr int EACH = K_NUMBERS / 8;
+            const int d = (s / EACH) * (4 * K_NUMBERS) + quad * K_NUMBERS + (s % EACH) * 8;
             X8 x = {};
             if (view[w].alive) {
                 if (a.q_wide) x = *(const X8 *)(qp + d);
@@ -924,24 +719,34 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4
     const int64_t page_bytes = ((int64_t)kv.n_heads << kv.shift) * ROW_BYTES;
     const int64_t here = (int64_t)a.layer * kv.n_pages * page_bytes + ((int64_t)head << kv.shift) * ROW_BYTES;
     const char *k_at = (const char *)kv.k + here, *v_at = (const char *)kv.v + here;
+    const uint8_t *ke_at = BITS == 4 ? a.k_exp + here / 16 : nullptr, *ve_at = BITS == 4 ? a.v_exp + here / 16 : nullptr;      // a byte for 16
     const int in_page = (1 << kv.shift) - 1;
-    uint4 rk[2][K_LOADS], rv[V_LOADS];
+    KPiece rk[2][K_LOADS];
+    VPiece rv[V_LOADS];
+    uint8_t ek[BITS == 4 ? 2 : 1][K_LOADS], ev[V_LOADS];         // scales of 4 bits
     auto fetch_k = [&](int tile, int pages, bool whole) {
-        const int y0 = start_of(tile), off = col * ROW_BYTES + quad * 16;
+        const int y0 = start_of(tile), off = col * ROW_BYTES + quad * K_BYTES;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             if (whole) {
                 const int page = __builtin_amdgcn_readlane(pages, b * 16);
-                const char *at = k_at + (page * page_bytes + ((y0 + b * 16) & in_page) * ROW_BYTES);
-#pragma unroll
-                for (int i = 0; i < K_LOADS; ++i) rk[b][i] = *(const uint4 *)(at + off + i * 64);
-            } else {
-                const int key = b * 16 + col, page = __shfl(pages, key);
-                const char *at = k_at + (page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES + quad * 16);
+                const int64_t at = page * page_bytes + ((y0 + b * 16) & in_page) * ROW_BYTES;
 #pragma unroll
                 for (int i = 0; i < K_LOADS; ++i) {
-                    rk[b][i] = make_uint4(0, 0, 0, 0);
-                    if (page >= 0) rk[b][i] = *(const uint4 *)(at + i * 64);
+                    rk[b][i] = *(const KPiece *)(k_at + at + off + i * 64);
+                    if constexpr (BITS == 4) ek[b][i] = (ke_at + at / 16)[(off + i * 64) / 16];
+                }
+            } else {
+                const int key = b * 16 + col, page = __shfl(pages, key);
+                const int64_t at = page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES + quad * K_BYTES;
+#pragma unroll
+                for (int i = 0; i < K_LOADS; ++i) {
+                    rk[b][i] = KPiece{};
+                    if (page >= 0) rk[b][i] = *(const KPiece *)(k_at + at + i * 64);
+                    if constexpr (BITS == 4) {
+                        ek[b][i] = 0;
+                        if (page >= 0) ek[b][i] = ke_at[(at + i * 64) / 16];
+                    }
                 }
             }
         }
@@ -952,12 +757,18 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4
         for (int i = 0; i < V_LOADS; ++i) {
             if (whole) {
                 const int key = i * 64 / PER_ROW, page = __builtin_amdgcn_readlane(pages, key);
-                const char *at = v_at + (page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES);
-                rv[i] = *(const uint4 *)(at + lane * 16);
+                const int64_t at = page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES;
+                rv[i] = *(const VPiece *)(v_at + at + lane * V_BYTES);
+                if constexpr (BITS == 4) ev[i] = (ve_at + at / 16)[lane * V_BYTES / 16];
             } else {
                 const int key = (i * 64 + lane) / PER_ROW, page = __shfl(pages, key);
-                rv[i] = make_uint4(0, 0, 0, 0);
-                if (page >= 0) rv[i] = *(const uint4 *)(v_at + (page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES + lane % PER_ROW * 16));
+                const int64_t at = page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES + lane % PER_ROW * V_BYTES;
+                rv[i] = VPiece{};
+                if (page >= 0) rv[i] = *(const VPiece *)(v_at + at);
+                if constexpr (BITS == 4) {
+                    ev[i] = 0;
+                    if (page >= 0) ev[i] = ve_at[at / 16];
+                }
             }
         }
     };
@@ -988,7 +799,17 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4
             f32x4 acc[COLS] = {};
 #pragma unroll
             for (int i = 0; i < K_LOADS; ++i) {
-                if constexpr (FP8) {
+                if constexpr (BITS == 4) {
+                    const float unit = power_of(ek[b][i]);
+                    const uint32_t *kk = (const uint32_t *)&rk[b][i];
+#pragma unroll
+                    for (int j = 0; j < K_NUMBERS / 8; ++j) {
+                        union { X2 x2[4]; X8 x8; } kw;
+                        widen4(kk[j], unit, kw.x2);
+#pragma unroll
+                        for (int w = 0; w < COLS; ++w) acc[w] = mfma16(kw.x8, qf[w][K_NUMBERS / 8 * i + j], acc[w]);
+                    }
+                } else if constexpr (BITS == 8) {
                     union { X2 x2[8]; X8 x8[2]; } kw;
                     const uint32_t kk[4] = {rk[b][i].x, rk[b][i].y, rk[b][i].z, rk[b][i].w};
 #pragma unroll
@@ -1009,7 +830,16 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4
 #pragma unroll
         for (int i = 0; i < V_LOADS; ++i) {
             const int key = (i * 64 + lane) / PER_ROW, part = lane % PER_ROW;
-            if constexpr (FP8) {
+            if constexpr (BITS == 4) {
+                const float unit = power_of(ev[i]);
+                const uint32_t *vv = (const uint32_t *)&rv[i];
+#pragma unroll
+                for (int j = 0; j < V_BYTES / 4; ++j) {
+                    union { X2 x[4]; uint4 u; } w;
+                    widen4(vv[j], unit, w.x);
+                    sv[few_v_piece<CH>(key, V_BYTES / 4 * part + j)] = w.u;
+                }
+            } else if constexpr (BITS == 8) {
                 union { X2 x[8]; uint4 u[2]; } w;
                 const uint32_t vv[4] = {rv[i].x, rv[i].y, rv[i].z, rv[i].w};
 #pragma unroll
@@ -1095,7 +925,9 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4
 #pragma unroll
                 for (int x = 0; x < D / 32; ++x) {
                     float k[8];
-                    numbers<E, FP8, 8>(k_at + at + (FP8 ? (x >> 1) * 64 + quad * 16 + (x & 1) * 8 : (x * 32 + quad * 8) * 2), k);
+                    constexpr int EACH = K_NUMBERS / 8;
+                    const int d = (x / EACH) * (4 * K_NUMBERS) + quad * K_NUMBERS + (x % EACH) * 8;
+                    numbers<E, BITS, 8>(k_at + at + d * BITS / 8, ke_at + at / 16 + d / 32, k);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) dot = fmaf((float)qf[w][x][i], k[i], dot);
                 }
@@ -1106,7 +938,8 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4
 #pragma unroll
                 for (int x = 0; x < D / 16; ++x) {
                     float v[4];
-                    numbers<E, FP8, 4>(v_at + at + (x * 16 + 4 * quad) * (ROW_BYTES / D), v);
+                    const int d = x * 16 + 4 * quad;
+                    numbers<E, BITS, 4>(v_at + at + d * BITS / 8, ve_at + at / 16 + d / 32, v);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) o[w][x][j] += see ? weight * v[j] : 0.0f;
                 }
@@ -1192,16 +1025,16 @@ int parts_room(hx_ctx *ctx, AttendArgs &a, int64_t tiles, int rows, int dim, boo
     return HX_OK;
 }
 
-template <typename E, bool FP8, int D, bool PAGE16>
+template <typename E, int BITS, int D, bool PAGE16>
 int launch(hx_ctx *ctx, AttendArgs &a, hipStream_t stream)
 {
-    using C = Tile<FP8, D, 4, PAGE16>;
+    using C = Tile<BITS, D, 4, PAGE16>;
     const int lds = C::LDS + (a.parent ? TREE_BYTES : 0);
     const int64_t tiles = (int64_t)a.n * a.kv.n_heads * a.row_tiles, grid = tiles * a.splits, join_grid = tiles * (C::ROWS / (AT_THREADS / (D / 4)));
     HX_REQUIRE(ctx, grid <= hx_most_groups(C::THREADS) && join_grid <= hx_most_groups(AT_THREADS), HX_ERR_SHAPE, "%lld workgroups", (long long)grid);
     if (a.splits > 1)
         if (int rc = parts_room(ctx, a, tiles, C::ROWS, D, false, stream)) return rc;
-    hx_attend_kernel<E, FP8, D, 4, PAGE16><<<(int)grid, C::THREADS, lds, stream>>>(a);
+    hx_attend_kernel<E, BITS, D, 4, PAGE16><<<(int)grid, C::THREADS, lds, stream>>>(a);
     if (a.splits > 1) hx_attend_join_kernel<E, D, KT, C::ROWS><<<(int)join_grid, AT_THREADS, 0, stream>>>(a);
     return hx_check_launch(ctx, "hx_attend_kernel");
 }
@@ -1247,7 +1080,7 @@ void divide(AttendArgs &a, int64_t groups, const Division &d, int max_len, int t
     a.splits = (int)parts;
 }
 
-template <typename E, bool FP8, int D, int COLS>
+template <typename E, int BITS, int D, int COLS>
 int launch_few(hx_ctx *ctx, AttendArgs &a, hipStream_t stream)
 {
     const int lds = 4 * few_wave_lds(D, COLS) + (a.parent ? TREE_BYTES : 0);
@@ -1255,32 +1088,32 @@ int launch_few(hx_ctx *ctx, AttendArgs &a, hipStream_t stream)
     HX_REQUIRE(ctx, grid <= hx_most_groups(AT_THREADS), HX_ERR_SHAPE, "%lld workgroups", (long long)grid);
     if (a.splits > 1)
         if (int rc = parts_room(ctx, a, tiles, 16 * COLS, D, true, stream)) return rc;
-    if (a.kv.shift >= 4) hx_attend_few_kernel<E, FP8, D, COLS, true><<<(int)grid, AT_THREADS, lds, stream>>>(a);
-    else hx_attend_few_kernel<E, FP8, D, COLS, false><<<(int)grid, AT_THREADS, lds, stream>>>(a);
+    if (a.kv.shift >= 4) hx_attend_few_kernel<E, BITS, D, COLS, true><<<(int)grid, AT_THREADS, lds, stream>>>(a);
+    else hx_attend_few_kernel<E, BITS, D, COLS, false><<<(int)grid, AT_THREADS, lds, stream>>>(a);
     return hx_check_launch(ctx, "hx_attend_few_kernel");
 }
 
 // More LDS a workgroup than the 64 KB that need no asking, for the kernels of a pair of types and a head_dim, the first time that a context
 // meets them.  (When it is created this took 5 ms, most of it the loading of code that a planner never runs.)
-template <typename E, bool FP8, int D, bool PAGE16>
+template <typename E, int BITS, int D, bool PAGE16>
 hipError_t allow_many()
 {
-    return hipFuncSetAttribute((const void *)hx_attend_kernel<E, FP8, D, 4, PAGE16>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                               Tile<FP8, D, 4, PAGE16>::LDS + TREE_BYTES);
+    return hipFuncSetAttribute((const void *)hx_attend_kernel<E, BITS, D, 4, PAGE16>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                               Tile<BITS, D, 4, PAGE16>::LDS + TREE_BYTES);
 }
-template <typename E, bool FP8, int D, int COLS, bool PAGE16>
+template <typename E, int BITS, int D, int COLS, bool PAGE16>
 hipError_t allow_few()
 {
-    return hipFuncSetAttribute((const void *)hx_attend_few_kernel<E, FP8, D, COLS, PAGE16>, hipFuncAttributeMaxDynamicSharedMemorySize,
+    return hipFuncSetAttribute((const void *)hx_attend_few_kernel<E, BITS, D, COLS, PAGE16>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                4 * few_wave_lds(D, COLS) + TREE_BYTES);
 }
-template <typename E, bool FP8, int D>
+template <typename E, int BITS, int D>
 int allow(hx_ctx *ctx)
 {
-    constexpr int kind = (std::is_same_v<E, _Float16> ? 6 : 0) + (FP8 ? 3 : 0) + (D == 64 ? 0 : D == 128 ? 1 : 2);
+    constexpr int kind = (std::is_same_v<E, _Float16> ? 9 : 0) + (BITS == 16 ? 0 : BITS == 8 ? 3 : 6) + (D == 64 ? 0 : D == 128 ? 1 : 2);
     if (hx_serve(ctx)->att_allowed >> kind & 1) return HX_OK;
-    for (const hipError_t e : {allow_many<E, FP8, D, false>(), allow_many<E, FP8, D, true>(), allow_few<E, FP8, D, 1, false>(), allow_few<E, FP8, D, 1, true>(),
-                               allow_few<E, FP8, D, 2, false>(), allow_few<E, FP8, D, 2, true>()}) {
+    for (const hipError_t e : {allow_many<E, BITS, D, false>(), allow_many<E, BITS, D, true>(), allow_few<E, BITS, D, 1, false>(), allow_few<E, BITS, D, 1, true>(),
+                               allow_few<E, BITS, D, 2, false>(), allow_few<E, BITS, D, 2, true>()}) {
         if (e == hipSuccess) continue;
         (void)hipGetLastError();                   // not the next launch's
         return hx_fail(ctx, HX_ERR_DEVICE, "hipFuncSetAttribute(LDS size): %s", hipGetErrorString(e));
@@ -1289,31 +1122,31 @@ int allow(hx_ctx *ctx)
     return HX_OK;
 }
 
-template <typename E, bool FP8, int D>
+template <typename E, int BITS, int D>
 int plan(hx_ctx *ctx, AttendArgs &a, int max_len, hipStream_t stream)
 {
-    if (int rc = allow<E, FP8, D>(ctx)) return rc;
+    if (int rc = allow<E, BITS, D>(ctx)) return rc;
     const int64_t rows = (int64_t)a.max_q * a.group, pairs = (int64_t)a.n * a.kv.n_heads;
     if (rows <= 32) {
         a.row_tiles = 1;
         divide(a, pairs, {16 * ctx->num_cu, 16 * ctx->num_cu, 8, 8, 4 * ctx->num_cu, 64}, max_len, FEW_KEYS, 32);
-        return rows <= 16 ? launch_few<E, FP8, D, 1>(ctx, a, stream) : launch_few<E, FP8, D, 2>(ctx, a, stream);
+        return rows <= 16 ? launch_few<E, BITS, D, 1>(ctx, a, stream) : launch_few<E, BITS, D, 2>(ctx, a, stream);
     }
     a.row_tiles = (int)((rows + 127) / 128);
     divide(a, pairs * a.row_tiles, {16 * ctx->num_cu, 2 * ctx->num_cu, 32, 4, 2 * ctx->num_cu, 128}, max_len, KT, 128);
-    return a.kv.shift >= 4 ? launch<E, FP8, D, true>(ctx, a, stream) : launch<E, FP8, D, false>(ctx, a, stream);
+    return a.kv.shift >= 4 ? launch<E, BITS, D, true>(ctx, a, stream) : launch<E, BITS, D, false>(ctx, a, stream);
 }
 
-template <typename E, bool FP8>
+template <typename E, int BITS>
 int by_dim(hx_ctx *ctx, AttendArgs &a, int max_len, hipStream_t stream)
 {
-    if (a.kv.dim == 64) return plan<E, FP8, 64>(ctx, a, max_len, stream);
-    if (a.kv.dim == 128) return plan<E, FP8, 128>(ctx, a, max_len, stream);
-    return plan<E, FP8, 256>(ctx, a, max_len, stream);
+    if (a.kv.dim == 64) return plan<E, BITS, 64>(ctx, a, max_len, stream);
+    if (a.kv.dim == 128) return plan<E, BITS, 128>(ctx, a, max_len, stream);
+    return plan<E, BITS, 256>(ctx, a, max_len, stream);
 }
 
 }  // namespace
 
-// One source file for each pair of types, queries' and cache's: HX_ATTEND_TYPES(name, E, FP8) defines its function.
-#define HX_ATTEND_TYPES(name, E, FP8)                                                                                    \
-    int hx_attend_##name(hx_ctx *ctx, HxAttend &a, int max_len, hipStream_t stream) { return by_dim<E, FP8>(ctx, a, max_len, stream); }
+// One source file for each pair of types, queries' and cache's: HX_ATTEND_TYPES(name, E, BITS) defines its function.
+#define HX_ATTEND_TYPES(name, E, BITS)                                                                                   \
+    int hx_attend_##name(hx_ctx *ctx, HxAttend &a, int max_len, hipStream_t stream) { return by_dim<E, BITS>(ctx, a, max_len, stream); }

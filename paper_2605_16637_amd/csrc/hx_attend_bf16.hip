@@ -1,4 +1,4 @@
 // Attention's kernels: queries of bf16, a cache of the same.
 #include "hx_attend.hpp"
 
-HX_ATTEND_TYPES(bf16, __bf16, false)
+HX_ATTEND_TYPES(bf16, __bf16, 16)

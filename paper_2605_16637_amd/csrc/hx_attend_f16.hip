@@ -1,4 +1,4 @@
 // Attention's kernels: queries of f16, a cache of the same.
 #include "hx_attend.hpp"
 
-HX_ATTEND_TYPES(f16, _Float16, false)
+HX_ATTEND_TYPES(f16, _Float16, 16)

@@ -445,6 +445,7 @@ extern "C" int hx_ctx_destroy(hx_ctx *ctx)
     hx_scratch_release(serve->kv);
     hx_scratch_release(serve->att);
     hx_scratch_release(serve->att_done);
+    hx_scratch_release(serve->top);
     delete serve;
     return HX_OK;
 }

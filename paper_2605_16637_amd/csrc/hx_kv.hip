@@ -5,6 +5,8 @@
 // copying is spread over the chip.  Counters of entries and pages have no sign: they pass a limit of INT32_MAX by a workgroup's threads.
 #include "hx_serve.hpp"
 
+#include <type_traits>
+
 namespace {
 
 constexpr int PL_THREADS = 1024;           // the planning workgroup
@@ -84,6 +86,26 @@ __device__ void claim_rows(const int32_t *row, int n, int rows, int32_t *claim)
     __syncthreads();
 }
 
+// One of a pool's arrays, by a number that is the same for all threads.
+struct Plane {
+    char *at;
+    int row_bytes;           // of a token in one head
+};
+__device__ __forceinline__ Plane plane(const KvPlanes &p, int i)
+{
+    return Plane{i == 0 ? p.at[0] : i == 1 ? p.at[1] : i == 2 ? p.at[2] : p.at[3], i < 2 ? p.row_bytes[0] : p.row_bytes[2]};
+}
+
+// f(U{}) with the widest type that rows of so many bytes consist of.
+template <typename F>
+__device__ __forceinline__ void by_width(int row_bytes, F f)
+{
+    if (row_bytes % 16 == 0) f(uint4{});
+    else if (row_bytes % 4 == 0) f(uint32_t{});
+    else if (row_bytes % 2 == 0) f(uint16_t{});
+    else f(uint8_t{});
+}
+
 struct ForkArgs {
     KvView kv;
     int n;
@@ -92,7 +114,9 @@ struct ForkArgs {
     int32_t *tok;            // [n] tokens of the copy, -1: none is made
     int32_t *from, *to;      // [n] the last page's, -1: none is copied
     int32_t *list;           // [n] free pages
-    int row_bytes;           // of a token in one head
+    KvPlanes planes;
+    char *bounds;            // or NULL
+    int64_t bounds_bytes;    // of a page in one layer
 };
 
 // One workgroup, so that pages go out in the order of the rows: a chain of memory round trips (the claim, the source's length and last
@@ -152,13 +176,13 @@ __global__ __launch_bounds__(PL_THREADS) void hx_kv_fork_plan_kernel(ForkArgs a)
     }
 }
 
-// Workgroup (i, 0): the shared pages of copy i; (i, 1 + 2 layer + v): its last page's tokens in one layer's keys or values, 16 bytes a
-// thread.  Bound by HBM: 256 copies of tails in 32 layers, 1.0 GB read and written: 169 us, and their sources come from the caches three
+// Workgroup (i, 0): the shared pages of copy i; (i, 1 + planes layer + v): its last page's tokens in one layer's keys or values, 16 bytes a
+// thread (the page's bounds, by the keys' workgroup).  Bound by HBM: 256 copies of tails in 32 layers, 1.0 GB read and written: 169 us, and their sources come from the caches three
 // times of four (a plain copy reaches 4.7 TB/s).
 __global__ __launch_bounds__(CP_THREADS) void hx_kv_fork_copy_kernel(ForkArgs a)
 {
     const KvView &kv = a.kv;
-    const int parts = 1 + 2 * kv.n_layers, i = blockIdx.x / parts, part = blockIdx.x % parts;
+    const int parts = 1 + a.planes.n * kv.n_layers, i = blockIdx.x / parts, part = blockIdx.x % parts;
     const int t = a.tok[i];
     if (t <= 0) return;
     if (part == 0) {
@@ -175,16 +199,23 @@ __global__ __launch_bounds__(CP_THREADS) void hx_kv_fork_copy_kernel(ForkArgs a)
         return;
     }
     if (a.from[i] < 0) return;
-    const int layer = (part - 1) >> 1, toks = t & ((1 << kv.shift) - 1);
-    char *base = (char *)(((part - 1) & 1) ? kv.v : kv.k);
-    const int64_t head_bytes = (int64_t)a.row_bytes << kv.shift;
-    const char *from = base + ((int64_t)layer * kv.n_pages + a.from[i]) * kv.n_heads * head_bytes;
-    char *to = base + ((int64_t)layer * kv.n_pages + a.to[i]) * kv.n_heads * head_bytes;
-    const int per = toks * a.row_bytes / 16;                   // 16-byte pieces of a head
-    for (int c = threadIdx.x; c < per * kv.n_heads; c += CP_THREADS) {
-        const int64_t at = (c / per) * head_bytes + (int64_t)(c % per) * 16;
-        *(uint4 *)(to + at) = *(const uint4 *)(from + at);
-    }
+    const int layer = (part - 1) / a.planes.n, which = (part - 1) % a.planes.n, toks = t & ((1 << kv.shift) - 1);
+    const Plane x = plane(a.planes, which);
+    const int64_t head_bytes = (int64_t)x.row_bytes << kv.shift;
+    const int64_t page_from = (int64_t)layer * kv.n_pages + a.from[i], page_to = (int64_t)layer * kv.n_pages + a.to[i];
+    const char *from = x.at + page_from * kv.n_heads * head_bytes;
+    char *to = x.at + page_to * kv.n_heads * head_bytes;
+    by_width(x.row_bytes, [&](auto unit) {
+        using U = decltype(unit);
+        const int per = toks * x.row_bytes / (int)sizeof(U);   // pieces of a head
+        for (int c = threadIdx.x; c < per * kv.n_heads; c += CP_THREADS) {
+            const int64_t at = (c / per) * head_bytes + (int64_t)(c % per) * sizeof(U);
+            *(U *)(to + at) = *(const U *)(from + at);
+        }
+    });
+    if (a.bounds && which == 0)
+        for (int64_t c = (int64_t)threadIdx.x * 16; c < a.bounds_bytes; c += CP_THREADS * 16)
+            *(uint4 *)(a.bounds + page_to * a.bounds_bytes + c) = *(const uint4 *)(a.bounds + page_from * a.bounds_bytes + c);
 }
 
 struct GrowArgs {
@@ -279,6 +310,42 @@ __device__ __forceinline__ uint32_t to_e4m3(const float *x, float scale)
     return w;
 }
 
+// A pool of 4 bits.
+struct E2m1 {};
+constexpr int E2M1_LEAST = 127 - 23, E2M1_MOST = 127 + 13, E2M1_NAN = 255;       // bytes of its scales
+
+// 8 of 32 numbers, of which 4 lanes beside each other have a quarter each, as codes of 4 bits; *exp: their scale's byte.
+// 2^e is the least that 6 of it reach the largest with: 6 is 1.5 * 4, so the largest's own exponent decides, and whether its fraction is more than 1.5.
+// A number over a power of 2 is exact, and so are comparisons with the middles between codes; a middle goes to the even code.
+__device__ __forceinline__ uint32_t to_e2m1(const float *x, int *exp)
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t size = __float_as_uint(x[i]) & 0x7fffffffu;
+        top = size > top ? size : top;
+    }
+#pragma unroll
+    for (int d = 1; d < 4; d <<= 1) {
+        const uint32_t y = __shfl_xor(top, d);
+        top = y > top ? y : top;
+    }
+    // (a NaN's bits are the largest)
+    int e = (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x400000u ? 1 : 0);
+    e = e < E2M1_LEAST ? E2M1_LEAST : e > E2M1_MOST ? E2M1_MOST : e;
+    const bool nan = top > 0x7f800000u;
+    const float down = __uint_as_float((uint32_t)(254 - e) << 23);
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float y = fabsf(x[i]) * down;
+        const uint32_t code = (y > 0.25f) + (y >= 0.75f) + (y > 1.25f) + (y >= 1.75f) + (y > 2.5f) + (y >= 3.5f) + (y > 5.0f);
+        w |= (code | (__float_as_uint(x[i]) >> 31 << 3)) << (4 * i);
+    }
+    *exp = nan ? E2M1_NAN : e;
+    return nan ? 0 : w;
+}
+
 struct WriteArgs {
     KvView kv;
     int layer, n, n_tok;
@@ -286,6 +353,7 @@ struct WriteArgs {
     const void *k, *v;
     int64_t token_stride, head_stride;
     const float *k_scale, *v_scale;
+    uint8_t *k_exp, *v_exp;
     bool aligned;            // 8 numbers of a source can be loaded at once
 };
 
@@ -323,7 +391,7 @@ __device__ __forceinline__ bool listed_before(const int32_t *row, int *x, int en
     return listed;
 }
 
-// 8 numbers of a key and of a value a thread; D of one byte: e4m3.  2048 tokens of 64 rows, 8 heads of 128 (17 MB read and written):
+// 8 numbers of a key and of a value a thread; D of one byte: e4m3, or two numbers of 4 bits.  2048 tokens of 64 rows, 8 heads of 128 (17 MB read and written):
 // 5.2 us in a graph of such calls, most of it the lookups before a thread's store (its sequence by bisection, row, length, page, count).  One
 // token each of 256 rows 3.8, of 1024 5.6; of these the look for rows listed twice takes 0.2, 0.3 and 1.1.
 template <typename S, typename D>
@@ -362,7 +430,14 @@ __global__ __launch_bounds__(CP_THREADS) void hx_kv_write_kernel(WriteArgs a)
         else
 #pragma unroll
             for (int i = 0; i < 8; ++i) e.x[i] = src[i];
-        if constexpr (sizeof(D) == 1) {
+        if constexpr (std::is_same_v<D, E2m1>) {
+            float x[8];
+            int exp;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = load_number(&e.x[i]);
+            *(uint32_t *)((char *)(which ? kv.v : kv.k) + to / 2) = to_e2m1(x, &exp);
+            if (c % 4 == 0) (which ? a.v_exp : a.k_exp)[to / E2M1_GROUP] = (uint8_t)exp;
+        } else if constexpr (sizeof(D) == 1) {
             const float *scales = which ? a.v_scale : a.k_scale;
             const float scale = scales ? scales[a.layer * kv.n_heads + h] : 1.0f;
             float x[8];
@@ -378,6 +453,91 @@ __global__ __launch_bounds__(CP_THREADS) void hx_kv_write_kernel(WriteArgs a)
     }
 }
 
+// ---- read --------------------------------------------------------------------
+
+struct ReadArgs {
+    KvView kv;
+    int layer, n, n_tok;
+    const int32_t *row, *tok_ptr;
+    void *k, *v;
+    int64_t token_stride, head_stride;
+    const float *k_scale, *v_scale;
+    const uint8_t *k_exp, *v_exp;
+    bool aligned;            // 8 numbers can be stored at once
+};
+
+// 8 stored numbers from number `at` of the pool on, times their scale.
+template <typename S>
+__device__ __forceinline__ void stored(const void *pool, const uint8_t *exps, float scale, int64_t at, float *x)
+{
+    if constexpr (std::is_same_v<S, E2m1>) {
+        const uint32_t w = *(const uint32_t *)((const char *)pool + at / 2);
+        const int byte = exps[at / E2M1_GROUP];
+        const float unit = byte == E2M1_NAN ? __builtin_nanf("") : __uint_as_float((uint32_t)byte << 23);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t code = w >> (4 * i) & 7;
+            // 1 to 6: codes 2 to 7 are one bit of exponent over one of fraction more each; 0 and 0.5 beside them
+            const float size = code < 2 ? 0.5f * code : __uint_as_float((code << 22) + (126u << 23));
+            x[i] = (w >> (4 * i) & 8 ? -size : size) * unit;
+        }
+    } else if constexpr (sizeof(S) == 1) {
+        const uint2 w = *(const uint2 *)((const char *)pool + at);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int word = i < 4 ? w.x : w.y;
+            const float y = i % 4 == 0 ? __builtin_amdgcn_cvt_f32_fp8(word, 0) : i % 4 == 1 ? __builtin_amdgcn_cvt_f32_fp8(word, 1)
+                          : i % 4 == 2 ? __builtin_amdgcn_cvt_f32_fp8(word, 2) : __builtin_amdgcn_cvt_f32_fp8(word, 3);
+            x[i] = y * scale;
+        }
+    } else {
+        struct alignas(16) Eight { S x[8]; } e = *(const Eight *)((const S *)pool + at);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = (float)e.x[i];
+    }
+}
+
+// 8 numbers of a key and of a value a thread, as the write.
+template <typename S, typename D>
+__global__ __launch_bounds__(CP_THREADS) void hx_kv_read_kernel(ReadArgs a)
+{
+    const KvView &kv = a.kv;
+    const int per_head = kv.dim / 8, per = per_head * kv.n_heads;
+    const int64_t u = (int64_t)blockIdx.x * CP_THREADS + threadIdx.x;
+    const int64_t q = u / per;
+    if (q >= a.n_tok) return;
+    const int c = (int)(u % per), h = c / per_head, d = (c % per_head) * 8;
+    int lo = 0, hi = a.n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.tok_ptr[mid] <= q) lo = mid; else hi = mid - 1;
+    }
+    const int first = a.tok_ptr[lo], last = a.tok_ptr[lo + 1], r = a.row[lo];
+    bool ok = first >= 0 && first <= q && q < last && last <= a.n_tok && r >= 0 && r < kv.rows;
+    const int len = ok ? kv.len[r] : 0;
+    ok = ok && hx_row_ok(kv, r, len) && last - first <= len;
+    if (!ok) { if (c == 0) hx_raise(kv.status, HX_ERR_INDEX); return; }
+    const int64_t pos = (int64_t)len - last + q;
+    int page = hx_row(kv, r)[pos >> kv.shift];
+    if (page >= kv.n_pages) { if (c == 0) hx_raise(kv.status, HX_ERR_INDEX); page = -1; }
+    const int64_t from = page < 0 ? 0 : hx_kv_at(kv, a.layer, page, h, (int)(pos & ((1 << kv.shift) - 1))) + d;
+    const int64_t to = q * a.token_stride + h * a.head_stride + d;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        const float *scales = which ? a.v_scale : a.k_scale;
+        float x[8] = {};
+        if (page >= 0) stored<S>(which ? kv.v : kv.k, which ? a.v_exp : a.k_exp, scales ? scales[a.layer * kv.n_heads + h] : 1.0f, from, x);
+        D *at = (D *)(which ? a.v : a.k) + to;
+        struct alignas(8 * sizeof(D) < 16 ? 8 * sizeof(D) : 16) Eight { D x[8]; } e;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e.x[i] = (D)x[i];
+        if (a.aligned) *(Eight *)at = e;
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) at[i] = e.x[i];
+    }
+}
+
 // ---- keep --------------------------------------------------------------------
 
 struct KeepArgs {
@@ -385,7 +545,7 @@ struct KeepArgs {
     int n, n_keep;
     const int32_t *row, *n_draft, *keep_ptr, *keep;
     int32_t *ok;             // [n] whether the row is changed
-    int row_bytes;
+    KvPlanes planes;
 };
 
 // Whether entry i of the call can be carried out; the same for all threads.  Its answer is taken before anything of the call
@@ -428,13 +588,13 @@ __device__ bool keep_check(const KeepArgs &a, int i, int *s_bad)
 
 // 64 rows, up to 6 of 32 tokens kept, one layer: 7.3 us, 3.1 more for the tables; moves of a row follow each other.  With the tables, 32 layers
 // of 64, 256 and 1024 rows: 18, 55 and 318 us, for 49, 193 and 785 MB read and written (each layer's workgroups check their row again).
-// Workgroup (i, 2 layer + v): a token's place is read by the thread that then writes the earlier place, and numbers rise, so what
+// Workgroup (i, planes layer + v): a token's place is read by the thread that then writes the earlier place, and numbers rise, so what
 // a thread overwrites it has read.
 __global__ __launch_bounds__(CP_THREADS) void hx_kv_keep_move_kernel(KeepArgs a)
 {
     __shared__ int s_bad;
     const KvView &kv = a.kv;
-    const int parts = 2 * kv.n_layers, i = blockIdx.x / parts, part = blockIdx.x % parts;
+    const int parts = a.planes.n * kv.n_layers, i = blockIdx.x / parts, part = blockIdx.x % parts;
     const bool ok = keep_check(a, i, &s_bad);
     if (part == 0 && threadIdx.x == 0) {
         a.ok[i] = ok;
@@ -443,21 +603,24 @@ __global__ __launch_bounds__(CP_THREADS) void hx_kv_keep_move_kernel(KeepArgs a)
     if (!ok) return;
     const int r = a.row[i], k0 = a.keep_ptr[i], m = a.keep_ptr[i + 1] - k0, base = kv.len[r] - a.n_draft[i];
     const int32_t *table = hx_row(kv, r);
-    char *store = (char *)((part & 1) ? kv.v : kv.k);
-    const int64_t head_bytes = (int64_t)a.row_bytes << kv.shift;
-    const int64_t layer_page = (int64_t)(part >> 1) * kv.n_pages;
-    const int per_head = a.row_bytes / 16, in_page = (1 << kv.shift) - 1;
-    for (int c = threadIdx.x; c < per_head * kv.n_heads; c += CP_THREADS) {
-        char *at = store + (c / per_head) * head_bytes + (c % per_head) * 16;
-        for (int j = 0; j < m; ++j) {
-            const int k = a.keep[k0 + j];
-            if (k == j) continue;
-            const int from = base + k, to = base + j;
-            const char *x = at + (layer_page + table[from >> kv.shift]) * kv.n_heads * head_bytes + (int64_t)(from & in_page) * a.row_bytes;
-            char *y = at + (layer_page + table[to >> kv.shift]) * kv.n_heads * head_bytes + (int64_t)(to & in_page) * a.row_bytes;
-            *(uint4 *)y = *(const uint4 *)x;
+    const Plane store = plane(a.planes, part % a.planes.n);
+    const int64_t head_bytes = (int64_t)store.row_bytes << kv.shift;
+    const int64_t layer_page = (int64_t)(part / a.planes.n) * kv.n_pages;
+    by_width(store.row_bytes, [&](auto unit) {
+        using U = decltype(unit);
+        const int per_head = store.row_bytes / (int)sizeof(U), in_page = (1 << kv.shift) - 1;
+        for (int c = threadIdx.x; c < per_head * kv.n_heads; c += CP_THREADS) {
+            char *at = store.at + (c / per_head) * head_bytes + (c % per_head) * sizeof(U);
+            for (int j = 0; j < m; ++j) {
+                const int k = a.keep[k0 + j];
+                if (k == j) continue;
+                const int from = base + k, to = base + j;
+                const char *x = at + (layer_page + table[from >> kv.shift]) * kv.n_heads * head_bytes + (int64_t)(from & in_page) * store.row_bytes;
+                char *y = at + (layer_page + table[to >> kv.shift]) * kv.n_heads * head_bytes + (int64_t)(to & in_page) * store.row_bytes;
+                *(U *)y = *(const U *)x;
+            }
         }
-    }
+    });
 }
 
 // A page is held by one table less.  Counts that would go below 0 stay.
@@ -519,7 +682,9 @@ struct CompactArgs {
     int32_t *high, *hole;        // [n_pages / 2] which, and where to
     int32_t *moved;              // [n_pages]
     int32_t *n_used;             // or NULL
-    int64_t page_bytes;          // of a page in one layer's keys
+    KvPlanes planes;
+    char *bounds;                // or NULL
+    int64_t bounds_bytes;        // of a page in one layer
 };
 
 // Three launches: which pages move (9 us for 3882 pages), the copy, the tables (4.4 us).  The copy is bound by HBM: 3.8 GB read and written in
@@ -549,13 +714,21 @@ __global__ __launch_bounds__(PL_THREADS) void hx_kv_compact_plan_kernel(CompactA
 __global__ __launch_bounds__(CP_THREADS) void hx_kv_compact_copy_kernel(CompactArgs a)
 {
     const KvView &kv = a.kv;
-    const int n = *a.count, parts = 2 * kv.n_layers;
+    const int n = *a.count, each = a.planes.n + (a.bounds != nullptr), parts = each * kv.n_layers;
     for (int64_t u = blockIdx.x; u < (int64_t)n * parts; u += gridDim.x) {
-        const int j = (int)(u / parts), part = (int)(u % parts);
-        char *store = (char *)((part & 1) ? kv.v : kv.k) + (int64_t)(part >> 1) * kv.n_pages * a.page_bytes;
-        const uint4 *from = (const uint4 *)(store + a.high[j] * a.page_bytes);
-        uint4 *to = (uint4 *)(store + a.hole[j] * a.page_bytes);
-        for (int64_t c = threadIdx.x; c < a.page_bytes / 16; c += CP_THREADS) to[c] = from[c];
+        const int j = (int)(u / parts), part = (int)(u % parts), which = part % each;
+        const Plane x = plane(a.planes, which);
+        const int64_t bytes = which == a.planes.n ? a.bounds_bytes : ((int64_t)kv.n_heads << kv.shift) * x.row_bytes;
+        char *store = (which == a.planes.n ? a.bounds : x.at) + (int64_t)(part / each) * kv.n_pages * bytes;
+        if (bytes % 16 == 0) {
+            const uint4 *from = (const uint4 *)(store + a.high[j] * bytes);
+            uint4 *to = (uint4 *)(store + a.hole[j] * bytes);
+            for (int64_t c = threadIdx.x; c < bytes / 16; c += CP_THREADS) to[c] = from[c];
+        } else {
+            const char *from = store + a.high[j] * bytes;          // scales of a small page
+            char *to = store + a.hole[j] * bytes;
+            for (int64_t c = threadIdx.x; c < bytes; c += CP_THREADS) to[c] = from[c];
+        }
     }
 }
 
@@ -601,13 +774,14 @@ extern "C" int hx_kv_fork(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs 
                           const int32_t *src, const int32_t *dst, const int32_t *n_tok, void *stream_)
 {
     if (!ctx) return HX_ERR_INVALID_ARG;
-    HX_KV_BEGIN(ctx, src && dst, 1 + 2 * kv.n_layers);
-    const int parts = 1 + 2 * kv.n_layers;
+    HX_KV_BEGIN(ctx, src && dst, 1 + hx_kv_planes(pool).n * kv.n_layers);
+    const KvPlanes planes = hx_kv_planes(pool);
+    const int parts = 1 + planes.n * kv.n_layers;
     HX_KV_DEVICE(ctx);
     if (int rc = hx_scratch(ctx, hx_serve(ctx)->kv, ((size_t)kv.rows + 4 * (size_t)n) * sizeof(int32_t), stream)) return rc;
     int32_t *w = (int32_t *)hx_serve(ctx)->kv.p;
     ForkArgs a{kv, n, src, dst, n_tok, w, w + kv.rows, w + kv.rows + n, w + kv.rows + 2 * (size_t)n, w + kv.rows + 3 * (size_t)n,
-               pool->head_dim * hx_type_size(pool->dtype)};
+               planes, (char *)pool->bounds, hx_bounds_bytes(pool)};
     hx_kv_fork_plan_kernel<<<1, PL_THREADS, 0, stream>>>(a);
     hx_kv_fork_copy_kernel<<<n * parts, CP_THREADS, 0, stream>>>(a);
     return hx_check_launch(ctx, "hx_kv_fork_copy_kernel");
@@ -639,7 +813,7 @@ extern "C" int hx_kv_write(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, c
     HX_REQUIRE(ctx, k && v, HX_ERR_INVALID_ARG, "NULL keys or values");
     HX_REQUIRE(ctx, (((uintptr_t)k | (uintptr_t)v) & (hx_type_size(src_dtype) - 1)) == 0, HX_ERR_INVALID_ARG, "keys or values are not aligned to their type");
     const bool aligned = (((uintptr_t)k | (uintptr_t)v) & 15) == 0 && token_stride % 8 == 0 && head_stride % 8 == 0;
-    WriteArgs a{kv, layer, n, n_tok, row, tok_ptr, k, v, token_stride, head_stride, pool->k_scale, pool->v_scale, aligned};
+    WriteArgs a{kv, layer, n, n_tok, row, tok_ptr, k, v, token_stride, head_stride, pool->k_scale, pool->v_scale, pool->k_exp, pool->v_exp, aligned};
     const int64_t blocks = ((int64_t)n_tok * (kv.dim / 8) * kv.n_heads + CP_THREADS - 1) / CP_THREADS;
     HX_REQUIRE(ctx, blocks <= hx_most_groups(CP_THREADS), HX_ERR_SHAPE, "%d tokens in one call", n_tok);
     const int grid = (int)blocks;
@@ -647,7 +821,8 @@ extern "C" int hx_kv_write(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, c
 #define HX_WRITE(S)                                                                                              \
     (pool->dtype == HX_BF16 ? hx_kv_write_kernel<S, __bf16><<<grid, CP_THREADS, 0, stream>>>(a)                  \
      : pool->dtype == HX_F16 ? hx_kv_write_kernel<S, _Float16><<<grid, CP_THREADS, 0, stream>>>(a)               \
-                             : hx_kv_write_kernel<S, uint8_t><<<grid, CP_THREADS, 0, stream>>>(a))
+     : pool->dtype == HX_E4M3 ? hx_kv_write_kernel<S, uint8_t><<<grid, CP_THREADS, 0, stream>>>(a)               \
+                              : hx_kv_write_kernel<S, E2m1><<<grid, CP_THREADS, 0, stream>>>(a))
     if (src_dtype == HX_F32) HX_WRITE(float);
     else if (src_dtype == HX_BF16) HX_WRITE(__bf16);
     else HX_WRITE(_Float16);
@@ -655,17 +830,48 @@ extern "C" int hx_kv_write(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, c
     return hx_check_launch(ctx, "hx_kv_write_kernel");
 }
 
+extern "C" int hx_kv_read(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_kv_seqs *seqs, int32_t n,
+                          const int32_t *row, const int32_t *tok_ptr, int32_t n_tok, int32_t dst_dtype,
+                          void *k, void *v, int64_t token_stride, int64_t head_stride, void *stream_)
+{
+    if (!ctx) return HX_ERR_INVALID_ARG;
+    HX_KV_BEGIN(ctx, row && tok_ptr, 1);
+    HX_REQUIRE(ctx, layer >= 0 && layer < kv.n_layers, HX_ERR_INVALID_ARG, "layer %d of %d", layer, kv.n_layers);
+    HX_REQUIRE(ctx, n_tok >= 0, HX_ERR_INVALID_ARG, "negative size");
+    HX_REQUIRE(ctx, dst_dtype == HX_F32 || dst_dtype == HX_BF16 || dst_dtype == HX_F16, HX_ERR_INVALID_ARG, "numbers of type %d", dst_dtype);
+    if (n_tok == 0) return HX_OK;
+    HX_REQUIRE(ctx, k && v, HX_ERR_INVALID_ARG, "NULL keys or values");
+    HX_REQUIRE(ctx, (((uintptr_t)k | (uintptr_t)v) & (hx_type_size(dst_dtype) - 1)) == 0, HX_ERR_INVALID_ARG, "keys or values are not aligned to their type");
+    const bool aligned = (((uintptr_t)k | (uintptr_t)v) & 15) == 0 && token_stride % 8 == 0 && head_stride % 8 == 0;
+    ReadArgs a{kv, layer, n, n_tok, row, tok_ptr, k, v, token_stride, head_stride, pool->k_scale, pool->v_scale, pool->k_exp, pool->v_exp, aligned};
+    const int64_t blocks = ((int64_t)n_tok * (kv.dim / 8) * kv.n_heads + CP_THREADS - 1) / CP_THREADS;
+    HX_REQUIRE(ctx, blocks <= hx_most_groups(CP_THREADS), HX_ERR_SHAPE, "%d tokens in one call", n_tok);
+    const int grid = (int)blocks;
+    HX_KV_DEVICE(ctx);
+#define HX_READ(D)                                                                                               \
+    (pool->dtype == HX_BF16 ? hx_kv_read_kernel<__bf16, D><<<grid, CP_THREADS, 0, stream>>>(a)                   \
+     : pool->dtype == HX_F16 ? hx_kv_read_kernel<_Float16, D><<<grid, CP_THREADS, 0, stream>>>(a)                \
+     : pool->dtype == HX_E4M3 ? hx_kv_read_kernel<uint8_t, D><<<grid, CP_THREADS, 0, stream>>>(a)                \
+                              : hx_kv_read_kernel<E2m1, D><<<grid, CP_THREADS, 0, stream>>>(a))
+    if (dst_dtype == HX_F32) HX_READ(float);
+    else if (dst_dtype == HX_BF16) HX_READ(__bf16);
+    else HX_READ(_Float16);
+#undef HX_READ
+    return hx_check_launch(ctx, "hx_kv_read_kernel");
+}
+
 extern "C" int hx_kv_keep(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs *seqs, int32_t n, const int32_t *row,
                           const int32_t *n_draft, const int32_t *keep_ptr, const int32_t *keep, int32_t n_keep, void *stream_)
 {
     if (!ctx) return HX_ERR_INVALID_ARG;
-    HX_KV_BEGIN(ctx, row && n_draft && keep_ptr, 2 * kv.n_layers);
+    HX_KV_BEGIN(ctx, row && n_draft && keep_ptr, hx_kv_planes(pool).n * kv.n_layers);
     HX_REQUIRE(ctx, n_keep >= 0, HX_ERR_INVALID_ARG, "negative size");
     HX_REQUIRE(ctx, n_keep == 0 || keep, HX_ERR_INVALID_ARG, "NULL array");
-    const int parts = 2 * kv.n_layers;
+    const KvPlanes planes = hx_kv_planes(pool);
+    const int parts = planes.n * kv.n_layers;
     HX_KV_DEVICE(ctx);
     if (int rc = hx_scratch(ctx, hx_serve(ctx)->kv, (size_t)n * sizeof(int32_t), stream)) return rc;
-    KeepArgs a{kv, n, n_keep, row, n_draft, keep_ptr, keep, (int32_t *)hx_serve(ctx)->kv.p, pool->head_dim * hx_type_size(pool->dtype)};
+    KeepArgs a{kv, n, n_keep, row, n_draft, keep_ptr, keep, (int32_t *)hx_serve(ctx)->kv.p, planes};
     hx_kv_keep_move_kernel<<<n * parts, CP_THREADS, 0, stream>>>(a);
     hx_kv_keep_apply_kernel<<<n, CP_THREADS, 0, stream>>>(a);
     return hx_check_launch(ctx, "hx_kv_keep_apply_kernel");
@@ -694,12 +900,12 @@ extern "C" int hx_kv_compact(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_se
     const size_t P = kv.n_pages;
     if (int rc = hx_scratch(ctx, hx_serve(ctx)->kv, (4 + 3 * P) * sizeof(int32_t), stream)) return rc;
     int32_t *w = (int32_t *)hx_serve(ctx)->kv.p;
-    const int64_t page_bytes = ((int64_t)kv.n_heads << kv.shift) * kv.dim * hx_type_size(pool->dtype);
-    CompactArgs a{kv, w, w + 4, w + 4 + P, moved ? moved : w + 4 + 2 * P, n_used, page_bytes};
+    const KvPlanes planes = hx_kv_planes(pool);
+    CompactArgs a{kv, w, w + 4, w + 4 + P, moved ? moved : w + 4 + 2 * P, n_used, planes, (char *)pool->bounds, hx_bounds_bytes(pool)};
     hx_kv_compact_plan_kernel<<<1, PL_THREADS, 0, stream>>>(a);
     if (P > 0) {
         // how many pages move only the GPU knows: at most half of them
-        const int64_t most = (int64_t)(P / 2 + 1) * 2 * kv.n_layers;
+        const int64_t most = (int64_t)(P / 2 + 1) * (planes.n + (pool->bounds != nullptr)) * kv.n_layers;
         hx_kv_compact_copy_kernel<<<(int)(most < 16 * ctx->num_cu ? most : 16 * ctx->num_cu), CP_THREADS, 0, stream>>>(a);
         const int64_t entries = (int64_t)kv.rows * kv.max_pages;
         hx_kv_compact_apply_kernel<<<blocks_for(entries > (int64_t)P ? entries : P, CP_THREADS, 8 * ctx->num_cu), CP_THREADS, 0, stream>>>(a);

@@ -15,7 +15,8 @@ struct HxScratch {
 
 // Every context is one of these; the planner's files, which do without, know its first part alone.
 struct HxServe : hx_ctx {
-    HxScratch kv, att, att_done;           // pages (hx_kv.hip), attention (hx_attend.hip), and its counters, which are 0 between launches
+    HxScratch kv, att, att_done;           // pages (hx_kv*.hip), attention (hx_attend.hip), and its counters, which are 0 between launches
+    HxScratch top;                         // the pages that queries choose (hx_attend_top.hip)
     unsigned att_allowed = 0;              // pairs of types and head_dims whose kernels have been allowed their LDS (hx_attend.hpp)
     int32_t *d_zeros = nullptr;            // 64 words that stay 0
 };
@@ -64,23 +65,49 @@ struct KvView {
 
 inline int hx_type_size(int dtype) { return dtype == HX_F32 ? 4 : dtype == HX_E4M3 ? 1 : 2; }
 
+// Of a token's key in one head, without its scales.
+inline int hx_row_bytes(int dtype, int dim) { return dtype == HX_E2M1 ? dim / 2 : dim * hx_type_size(dtype); }
+
+constexpr int E2M1_GROUP = 32;             // numbers under one scale
+
+// What a pool holds of tokens, each [layers][pages][heads][tokens] rows of `row_bytes`: keys, values and, of HX_E2M1, their scales.
+struct KvPlanes {
+    char *at[4];
+    int row_bytes[4];
+    int n;
+};
+inline KvPlanes hx_kv_planes(const hx_kv_pool *pool)
+{
+    const int row = hx_row_bytes(pool->dtype, pool->head_dim), exps = pool->head_dim / E2M1_GROUP;
+    if (pool->dtype != HX_E2M1) return KvPlanes{{(char *)pool->k, (char *)pool->v}, {row, row}, 2};
+    return KvPlanes{{(char *)pool->k, (char *)pool->v, (char *)pool->k_exp, (char *)pool->v_exp}, {row, row, exps, exps}, 4};
+}
+// of a page's bounds in one layer; they are in 16 bits
+inline int64_t hx_bounds_bytes(const hx_kv_pool *pool) { return (int64_t)pool->n_heads * 2 * pool->head_dim * 2; }
+
 // Fills a view after the checks every call makes.
 inline int hx_kv_view(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs *seqs, KvView *out)
 {
     HX_REQUIRE(ctx, pool && seqs, HX_ERR_INVALID_ARG, "NULL pool or sequences");
     HX_REQUIRE(ctx, pool->n_layers > 0 && pool->n_pages >= 0 && pool->n_heads > 0 && pool->head_dim > 0, HX_ERR_INVALID_ARG,
                "pool of %d layers, %d pages, %d heads of %d", pool->n_layers, pool->n_pages, pool->n_heads, pool->head_dim);
-    HX_REQUIRE(ctx, pool->dtype == HX_BF16 || pool->dtype == HX_F16 || pool->dtype == HX_E4M3, HX_ERR_INVALID_ARG, "pool of type %d", pool->dtype);
+    HX_REQUIRE(ctx, pool->dtype == HX_BF16 || pool->dtype == HX_F16 || pool->dtype == HX_E4M3 || pool->dtype == HX_E2M1, HX_ERR_INVALID_ARG, "pool of type %d", pool->dtype);
     const int T = pool->page_tokens;
     HX_REQUIRE(ctx, T >= 1 && T <= HX_MAX_PAGE_TOKENS && (T & (T - 1)) == 0, HX_ERR_SHAPE,
                "page_tokens %d is no power of two up to %d", T, HX_MAX_PAGE_TOKENS);
     HX_REQUIRE(ctx, pool->head_dim % 16 == 0 && pool->head_dim <= 1024, HX_ERR_SHAPE, "head_dim %d is no multiple of 16 up to 1024", pool->head_dim);
+    HX_REQUIRE(ctx, pool->dtype != HX_E2M1 || pool->head_dim % E2M1_GROUP == 0, HX_ERR_SHAPE, "head_dim %d of 4 bits is no multiple of %d", pool->head_dim, E2M1_GROUP);
     HX_REQUIRE(ctx, pool->n_heads <= 65536 && pool->n_layers <= 65536, HX_ERR_SHAPE, "%d layers of %d heads", pool->n_layers, pool->n_heads);
-    HX_REQUIRE(ctx, (int64_t)pool->n_heads * T * pool->head_dim * hx_type_size(pool->dtype) <= INT32_MAX, HX_ERR_SHAPE,
+    HX_REQUIRE(ctx, (int64_t)pool->n_heads * T * hx_row_bytes(pool->dtype, pool->head_dim) <= INT32_MAX, HX_ERR_SHAPE,
                "a page of %d heads, %d tokens and %d numbers is beyond int32", pool->n_heads, T, pool->head_dim);
     HX_REQUIRE(ctx, pool->n_pages == 0 || (pool->k && pool->v && pool->ref), HX_ERR_INVALID_ARG, "NULL member in pool");
     HX_REQUIRE(ctx, (((uintptr_t)pool->k | (uintptr_t)pool->v) & 15) == 0, HX_ERR_INVALID_ARG, "the pool's k and v have to be 16-byte aligned");
     HX_REQUIRE(ctx, pool->dtype == HX_E4M3 || (!pool->k_scale && !pool->v_scale), HX_ERR_INVALID_ARG, "scales are for a pool of HX_E4M3");
+    if (pool->dtype == HX_E2M1) {
+        HX_REQUIRE(ctx, pool->n_pages == 0 || (pool->k_exp && pool->v_exp), HX_ERR_INVALID_ARG, "a pool of HX_E2M1 without k_exp and v_exp");
+        HX_REQUIRE(ctx, (((uintptr_t)pool->k_exp | (uintptr_t)pool->v_exp) & 15) == 0, HX_ERR_INVALID_ARG, "the pool's k_exp and v_exp have to be 16-byte aligned");
+    } else HX_REQUIRE(ctx, !pool->k_exp && !pool->v_exp, HX_ERR_INVALID_ARG, "k_exp and v_exp are for a pool of HX_E2M1");
+    HX_REQUIRE(ctx, ((uintptr_t)pool->bounds & 15) == 0, HX_ERR_INVALID_ARG, "the pool's bounds have to be 16-byte aligned");
     HX_REQUIRE(ctx, seqs->n >= 0 && seqs->max_pages >= 0, HX_ERR_INVALID_ARG, "negative size of sequences");
     HX_REQUIRE(ctx, (int64_t)seqs->max_pages * T <= INT32_MAX, HX_ERR_SHAPE, "%d pages of %d tokens a row are beyond int32", seqs->max_pages, T);
     HX_REQUIRE(ctx, seqs->n == 0 || (seqs->len && (seqs->table || seqs->max_pages == 0)), HX_ERR_INVALID_ARG, "NULL member in sequences");
