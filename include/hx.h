@@ -17,7 +17,7 @@
  *    on, owned by the caller, valid until the work enqueued on `stream` has
  *    finished.  "host" pointers are ordinary host memory read during the
  *    call.  The structs hx_model / hx_calls / hx_prefill_tab / hx_decode_tab /
- *    hx_links / hx_intervals / hx_kv_pool / hx_kv_seqs / hx_attend_args themselves
+ *    hx_links / hx_intervals / hx_kv_pool / hx_kv_seqs / hx_attend_args / hx_top themselves
  *    live in host memory; their pointer members are device pointers.  The library never returns memory the caller must free
  *    (hx_dag_view returns borrowed pointers into the context).
  *  - `stream` is a hipStream_t (NULL = the default stream).  Work is enqueued
@@ -39,7 +39,7 @@
  *    thread-safe.
  *  - Device memory is allocated by hx_ctx_create and hx_dag_reserve, and by
  *    hx_decode_score, hx_rank (beyond 28672 calls), hx_kv_fork, hx_kv_grow,
- *    hx_kv_keep, hx_kv_compact and hx_attend the first time they meet a larger
+ *    hx_kv_keep, hx_kv_compact, hx_attend and hx_attend_top the first time they meet a larger
  *    problem than before; every other call only launches kernels and
  *    can be captured in a HIP graph (hx_validate_round and hx_stream_status
  *    wait for the stream and cannot).
@@ -783,6 +783,46 @@ typedef struct {
 } hx_attend_args;
 int hx_attend(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_kv_seqs *seqs,
               const hx_attend_args *args, void *stream);
+
+/*
+ * Bounds of keys: for every page of the pool, layer and KV head, the least and
+ * the largest number of its tokens' keys in each of the head_dim places, as the
+ * pool holds them (of HX_E4M3 without k_scale).  The call sets those of the
+ * pages that hold any of the last n_new[i] tokens of row[i] (n_new NULL: all its
+ * pages) from the tokens that are filled, in one layer, or in all (layer -1).
+ * NaNs count in no bound; a place with nothing else has bounds of +infinity and
+ * -infinity, in this order.  Call it when tokens have been written, or moved by
+ * hx_kv_keep or hx_kv_evict; hx_kv_fork and hx_kv_compact take bounds along (a
+ * fork's last page has those of the page that it is copied from).
+ */
+int hx_kv_bound(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_kv_seqs *seqs, int32_t n,
+                const int32_t *row, const int32_t *n_new, void *stream);
+
+/*
+ * Attention over some pages of each sequence, which every query chooses for
+ * every KV head by the bounds of what their keys can score:
+ *   bound of page b = max over the KV head's query heads of sum_d q_d (q_d < 0 ? lo_bd : hi_bd)
+ * with -q for q where scale < 0; held in 64 bits.  A query sees n_pages pages up
+ * to the one of its own token: the first n_first, the last n_last, and of the
+ * others those of the largest bounds, equal ones in rising order; all of them
+ * where there are no more.  Of its own page it sees the tokens up to its own.
+ * Pages that are not there are not chosen, nor are pages whose bound is
+ * -infinity, whose keys have no weight; a bound that is NaN is taken for
+ * +infinity.  What is not chosen has no part in the result; what is has the part
+ * that it has in hx_attend.  chosen: the numbers of the pages in their row,
+ * rising, then -1.
+ * args->parent must be NULL and args->window 0; pool->bounds must hold the pages'
+ * bounds.  Scratch: 8 bytes for each page of a row, query and KV head, up to 256 MB
+ * (more queries are taken in several parts), 4 for each page that is chosen.
+ */
+typedef struct {
+    int32_t n_pages;          /* 1 .. HX_MAX_TOP                                                */
+    int32_t n_first, n_last;  /* n_first >= 0, n_last >= 1, together at most n_pages            */
+    int32_t *chosen;          /* device [n_q][KV heads][n_pages] out, or NULL                   */
+} hx_top;
+#define HX_MAX_TOP 4096
+int hx_attend_top(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_kv_seqs *seqs,
+                  const hx_attend_args *args, const hx_top *top, void *stream);
 
 /*
  * One token a row from its logits (dtype HX_F32, HX_BF16 or HX_F16; row_stride

@@ -21,7 +21,8 @@ EXPORTS = ("hx_ctx_create", "hx_ctx_destroy", "hx_last_error", "hx_stream_status
            "hx_critical_path", "hx_horizons", "hx_dag_reserve", "hx_dag_append", "hx_dag_set_cost", "hx_dag_view",
            "hx_score_placements", "hx_validate_round", "hx_select", "hx_urgency", "hx_commit", "hx_commit_static", "hx_round", "hx_rank", "hx_plan_greedy",
            "hx_decode_score", "hx_decode_plan_greedy",
-           "hx_kv_fork", "hx_kv_grow", "hx_kv_write", "hx_kv_read", "hx_kv_keep", "hx_kv_free", "hx_kv_compact", "hx_attend", "hx_sample")
+           "hx_kv_fork", "hx_kv_grow", "hx_kv_write", "hx_kv_read", "hx_kv_keep", "hx_kv_free", "hx_kv_compact", "hx_kv_bound", "hx_attend", "hx_attend_top",
+           "hx_sample")
 
 HX_F32, HX_BF16, HX_F16, HX_E4M3, HX_E2M1 = 1, 2, 3, 4, 5
 
@@ -92,6 +93,10 @@ class hx_attend_args(C.Structure):
                 ("q_token", C.c_int64), ("q_head", C.c_int64), ("out", C.c_void_p), ("out_token", C.c_int64),
                 ("out_head", C.c_int64), ("lse", C.c_void_p), ("scale", C.c_float), ("window", C.c_int32),
                 ("n_sink", C.c_int32), ("parent", C.c_void_p)]
+
+
+class hx_top(C.Structure):
+    _fields_ = [("n_pages", C.c_int32), ("n_first", C.c_int32), ("n_last", C.c_int32), ("chosen", C.c_void_p)]
 
 
 _lib = None
@@ -300,6 +305,23 @@ def _strided(t, n, heads, dim):
     if not t.is_cuda or (dim > 1 and t.stride(2) != 1):
         raise ValueError("expected a tensor in device memory whose last dimension is contiguous")
     return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _attend_args(kv, sq, q_ptr, q, out, max_q, max_len, row, scale, lse):
+    """What attention's calls share; out may be None where there is none."""
+    torch = _torch()
+    n, n_q, heads = int(q_ptr.numel()) - 1, int(q.shape[0]), int(q.shape[1])
+    if out is not None and out.dtype != q.dtype:
+        raise ValueError(f"out of type {out.dtype} for queries of type {q.dtype}")
+    a = hx_attend_args()
+    a.n, a.row, a.q_ptr, a.n_q, a.max_q = n, _ptr(row, torch.int32, n), _ptr(q_ptr, torch.int32), n_q, int(max_q)
+    a.max_len = sq.max_pages * kv.page_tokens if max_len is None else int(max_len)
+    a.n_heads, a.dtype = heads, _number_type(q, HX_BF16, HX_F16)
+    a.q, a.q_token, a.q_head = _strided(q, n_q, heads, kv.head_dim)
+    if out is not None:
+        a.out, a.out_token, a.out_head = _strided(out, n_q, heads, kv.head_dim)
+    a.lse, a.scale = _ptr(lse, torch.float32, n_q * heads), kv.head_dim ** -0.5 if scale is None else float(scale)
+    return a
 
 
 class Context:
@@ -635,20 +657,24 @@ class Context:
                   lse=None, stream=None):
         """q, out [queries, query heads, head_dim] (any strides before the last dimension); scale None: head_dim ** -0.5; max_len None:
         what the table can hold."""
-        torch = _torch()
-        kv, sq, i32 = make_kv_pool(pool), make_kv_seqs(seqs), torch.int32
-        n, n_q, heads = int(q_ptr.numel()) - 1, int(q.shape[0]), int(q.shape[1])
-        if out.dtype != q.dtype:
-            raise ValueError(f"out of type {out.dtype} for queries of type {q.dtype}")
-        a = hx_attend_args()
-        a.n, a.row, a.q_ptr, a.n_q, a.max_q = n, _ptr(row, i32, n), _ptr(q_ptr, i32), n_q, int(max_q)
-        a.max_len = sq.max_pages * kv.page_tokens if max_len is None else int(max_len)
-        a.n_heads, a.dtype = heads, _number_type(q, HX_BF16, HX_F16)
-        a.q, a.q_token, a.q_head = _strided(q, n_q, heads, kv.head_dim)
-        a.out, a.out_token, a.out_head = _strided(out, n_q, heads, kv.head_dim)
-        a.lse, a.scale = _ptr(lse, torch.float32, n_q * heads), kv.head_dim ** -0.5 if scale is None else float(scale)
-        a.window, a.n_sink, a.parent = int(window), int(n_sink), _ptr(parent, i32, n_q)
+        kv, sq = make_kv_pool(pool), make_kv_seqs(seqs)
+        a = _attend_args(kv, sq, q_ptr, q, out, max_q, max_len, row, scale, lse)
+        a.window, a.n_sink, a.parent = int(window), int(n_sink), _ptr(parent, _torch().int32, a.n_q)
         self._invoke(self.lib.hx_attend, self._ctx, C.byref(kv), int(layer), C.byref(sq), C.byref(a), _stream(stream))
+
+    def hx_kv_bound(self, pool, layer, seqs, row, n_new=None, stream=None):
+        """Of the pages with the rows' last n_new tokens (None: all); layer -1: in all layers."""
+        torch = _torch()
+        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs), int(row.numel()), torch.int32
+        self._invoke(self.lib.hx_kv_bound, self._ctx, C.byref(kv), int(layer), C.byref(sq), n, _ptr(row, i32), _ptr(n_new, i32, n), _stream(stream))
+
+    def hx_attend_top(self, pool, layer, seqs, q_ptr, q, out, max_q, n_pages, n_first=0, n_last=1, max_len=None, row=None, scale=None, chosen=None,
+                      lse=None, stream=None):
+        """As hx_attend over n_pages pages for each query and KV head; chosen [queries, KV heads, n_pages]."""
+        kv, sq = make_kv_pool(pool), make_kv_seqs(seqs)
+        a = _attend_args(kv, sq, q_ptr, q, out, max_q, max_len, row, scale, lse)
+        t = hx_top(int(n_pages), int(n_first), int(n_last), _ptr(chosen, _torch().int32, a.n_q * kv.n_heads * int(n_pages)))
+        self._invoke(self.lib.hx_attend_top, self._ctx, C.byref(kv), int(layer), C.byref(sq), C.byref(a), C.byref(t), _stream(stream))
 
     def hx_sample(self, logits, u, token, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, n_kept=None, stream=None):
         """logits [rows, vocabulary], the rows any stride apart."""

@@ -1034,6 +1034,7 @@ int launch(hx_ctx *ctx, AttendArgs &a, hipStream_t stream)
     HX_REQUIRE(ctx, grid <= hx_most_groups(C::THREADS) && join_grid <= hx_most_groups(AT_THREADS), HX_ERR_SHAPE, "%lld workgroups", (long long)grid);
     if (a.splits > 1)
         if (int rc = parts_room(ctx, a, tiles, C::ROWS, D, false, stream)) return rc;
+    if (a.room_only) return HX_OK;
     hx_attend_kernel<E, BITS, D, 4, PAGE16><<<(int)grid, C::THREADS, lds, stream>>>(a);
     if (a.splits > 1) hx_attend_join_kernel<E, D, KT, C::ROWS><<<(int)join_grid, AT_THREADS, 0, stream>>>(a);
     return hx_check_launch(ctx, "hx_attend_kernel");
@@ -1088,6 +1089,7 @@ int launch_few(hx_ctx *ctx, AttendArgs &a, hipStream_t stream)
     HX_REQUIRE(ctx, grid <= hx_most_groups(AT_THREADS), HX_ERR_SHAPE, "%lld workgroups", (long long)grid);
     if (a.splits > 1)
         if (int rc = parts_room(ctx, a, tiles, 16 * COLS, D, true, stream)) return rc;
+    if (a.room_only) return HX_OK;
     if (a.kv.shift >= 4) hx_attend_few_kernel<E, BITS, D, COLS, true><<<(int)grid, AT_THREADS, lds, stream>>>(a);
     else hx_attend_few_kernel<E, BITS, D, COLS, false><<<(int)grid, AT_THREADS, lds, stream>>>(a);
     return hx_check_launch(ctx, "hx_attend_few_kernel");

@@ -22,6 +22,7 @@ struct HxAttend {
     const int32_t *picked;       // [query][KV head][picked_pages] pages chosen for each, or NULL: then n = n_q, and each is a sequence
     const int32_t *picked_len;   // [query][KV head] the place of the query's own token among the chosen pages' + 1
     int picked_pages;
+    bool room_only;              // scratch is asked for, nothing launched
     const void *zeros;           // 16 bytes of them, aligned
     bool q_wide, out_wide;       // q can be read 16 bytes at a time, out written 8
     int row_tiles, splits;       // parts of a row tile's keys, at most

@@ -3,9 +3,7 @@
 // Everything here is integers and copies; results depend on the arguments alone.  Which pages a call takes is decided by one
 // workgroup that looks through `ref` from its start (the free pages of lowest number, in the order of the call's rows), and the
 // copying is spread over the chip.  Counters of entries and pages have no sign: they pass a limit of INT32_MAX by a workgroup's threads.
-#include "hx_serve.hpp"
-
-#include <type_traits>
+#include "hx_kv_numbers.hpp"
 
 namespace {
 
@@ -310,10 +308,6 @@ __device__ __forceinline__ uint32_t to_e4m3(const float *x, float scale)
     return w;
 }
 
-// A pool of 4 bits.
-struct E2m1 {};
-constexpr int E2M1_LEAST = 127 - 23, E2M1_MOST = 127 + 13, E2M1_NAN = 255;       // bytes of its scales
-
 // 8 of 32 numbers, of which 4 lanes beside each other have a quarter each, as codes of 4 bits; *exp: their scale's byte.
 // 2^e is the least that 6 of it reach the largest with: 6 is 1.5 * 4, so the largest's own exponent decides, and whether its fraction is more than 1.5.
 // A number over a power of 2 is exact, and so are comparisons with the middles between codes; a middle goes to the even code.
@@ -466,37 +460,6 @@ struct ReadArgs {
     bool aligned;            // 8 numbers can be stored at once
 };
 
-// 8 stored numbers from number `at` of the pool on, times their scale.
-template <typename S>
-__device__ __forceinline__ void stored(const void *pool, const uint8_t *exps, float scale, int64_t at, float *x)
-{
-    if constexpr (std::is_same_v<S, E2m1>) {
-        const uint32_t w = *(const uint32_t *)((const char *)pool + at / 2);
-        const int byte = exps[at / E2M1_GROUP];
-        const float unit = byte == E2M1_NAN ? __builtin_nanf("") : __uint_as_float((uint32_t)byte << 23);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t code = w >> (4 * i) & 7;
-            // 1 to 6: codes 2 to 7 are one bit of exponent over one of fraction more each; 0 and 0.5 beside them
-            const float size = code < 2 ? 0.5f * code : __uint_as_float((code << 22) + (126u << 23));
-            x[i] = (w >> (4 * i) & 8 ? -size : size) * unit;
-        }
-    } else if constexpr (sizeof(S) == 1) {
-        const uint2 w = *(const uint2 *)((const char *)pool + at);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int word = i < 4 ? w.x : w.y;
-            const float y = i % 4 == 0 ? __builtin_amdgcn_cvt_f32_fp8(word, 0) : i % 4 == 1 ? __builtin_amdgcn_cvt_f32_fp8(word, 1)
-                          : i % 4 == 2 ? __builtin_amdgcn_cvt_f32_fp8(word, 2) : __builtin_amdgcn_cvt_f32_fp8(word, 3);
-            x[i] = y * scale;
-        }
-    } else {
-        struct alignas(16) Eight { S x[8]; } e = *(const Eight *)((const S *)pool + at);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = (float)e.x[i];
-    }
-}
-
 // 8 numbers of a key and of a value a thread, as the write.
 template <typename S, typename D>
 __global__ __launch_bounds__(CP_THREADS) void hx_kv_read_kernel(ReadArgs a)
@@ -526,7 +489,7 @@ __global__ __launch_bounds__(CP_THREADS) void hx_kv_read_kernel(ReadArgs a)
     for (int which = 0; which < 2; ++which) {
         const float *scales = which ? a.v_scale : a.k_scale;
         float x[8] = {};
-        if (page >= 0) stored<S>(which ? kv.v : kv.k, which ? a.v_exp : a.k_exp, scales ? scales[a.layer * kv.n_heads + h] : 1.0f, from, x);
+        if (page >= 0) stored<S, 8>(which ? kv.v : kv.k, which ? a.v_exp : a.k_exp, scales ? scales[a.layer * kv.n_heads + h] : 1.0f, from, x);
         D *at = (D *)(which ? a.v : a.k) + to;
         struct alignas(8 * sizeof(D) < 16 ? 8 * sizeof(D) : 16) Eight { D x[8]; } e;
 #pragma unroll

@@ -142,7 +142,8 @@ def compare(mine, mine_lse, q, k, v, see, scale, group, type_):
         near = near + 2.0 ** -25 * plain + 2.0 ** -25     # weights and outputs below the least normal number
     none = np.isinf(l)
     assert np.array_equal(none, np.isinf(mine_lse)) and (mine_lse[none] < 0).all()
-    assert (np.abs(mine_lse - l)[~none] <= (ds + sums + 2.0 ** -22 * np.abs(np.where(none, 0, l)))[~none]).all()
+    mine_lse, l = np.where(none, 0, mine_lse), np.where(none, 0, l)
+    assert (np.abs(mine_lse - l) <= ds + sums + 2.0 ** -22 * np.abs(l))[~none].all()
     assert (mine[none] == 0).all()
     far = np.abs(mine - o) - near
     assert (far <= 0).all(), (np.unravel_index(far.argmax(), far.shape), far.max())
@@ -155,3 +156,28 @@ def status(ctx):
     except binding.HxError as e:
         return e.code
     return 0
+
+
+def bounds_of(stored, filled):
+    """[.., T, dim] numbers and how many of T are filled -> [.., 2, dim] bounds; NaNs count in none."""
+    y = stored[..., :filled, :]
+    lo, hi = np.where(np.isnan(y), np.inf, y).min(-2), np.where(np.isnan(y), -np.inf, y).max(-2)
+    return np.stack([lo, hi], -2)
+
+
+def choose(bounds, there, own, q, sign, n_pages, n_first, n_last):
+    """Pages 0 .. own of one KV head that one query sees: bounds [own + 1, 2, dim], there [own + 1], q [group, dim]."""
+    pages = [b for b in range(own + 1) if there[b]]
+    if own + 1 <= n_pages:
+        return pages
+    fixed = [b for b in pages if b < n_first or b > own - n_last]
+    score = {}
+    with np.errstate(invalid="ignore"):
+        for b in pages:
+            if b in fixed:
+                continue
+            x = q * sign
+            s = (x * np.where(x < 0, bounds[b, 0], bounds[b, 1])).sum(1)
+            score[b] = max(np.inf if np.isnan(y) else y for y in s)
+    best = sorted((b for b in score if score[b] > -np.inf), key=lambda b: (-score[b], b))
+    return sorted(fixed + best[:n_pages - len(fixed)])

@@ -1,0 +1,351 @@
+"""Bounds of pages, and attention over the pages that they choose, against plain forms in 64 bits."""
+import numpy as np
+import pytest
+
+from tests import long_helpers as lh
+from tests import serve_helpers as sh
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from paper_2605_16637_amd import binding
+    c = binding.Context(0)
+    yield c
+    c.close()
+
+
+def bounds64(c):
+    return lh.f64(c.pool["bounds"])
+
+
+def want_bounds(c, layer, i, block, was):
+    """Of one page of a sequence, or what was there."""
+    p = c.table[c.where[i], block]
+    return was[layer, p] if p < 0 else lh.bounds_of(c.stored["k"][layer, p], min(c.T, c.lens[i] - block * c.T))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "f16", "e4m3", "e2m1"])
+@pytest.mark.parametrize("T,heads,dim", [(1, 1, 32), (4, 3, 96), (16, 8, 128), (64, 2, 256), (1024, 1, 64)])
+@pytest.mark.parametrize("part", [False, True])
+def test_bounds_of_every_page_and_of_the_last_tokens(ctx, cache, T, heads, dim, part):
+    lens = [1, 0, T, T + 1, 3 * T + (T + 1) // 2, 40]
+    c = lh.Cache(T + dim, lens, T, heads, dim, cache, missing=[(4, 1)], bounds=True)
+    was = bounds64(c)
+    new = [min(n, x) for n, x in zip(lens, (1, 0, 0, 1, T + 2, 7))] if part else lens
+    rows = [5, 3, 0, 1, 4, 2]
+    ctx.hx_kv_bound(c.pool, 1, c.seqs, sh.i32(c.where[rows]), sh.i32([new[i] for i in rows]) if part else None)
+    assert lh.status(ctx) == 0
+    want = was.copy()
+    for i in range(6):
+        for b in range(c.need[i]):
+            if (b + 1) * T > lens[i] - new[i] and c.table[c.where[i], b] >= 0:
+                want[1, c.table[c.where[i], b]] = want_bounds(c, 1, i, b, was)
+    assert np.array_equal(bounds64(c), want, equal_nan=True)
+    ctx.hx_kv_bound(c.pool, -1, c.seqs, sh.i32(c.where))                       # all pages, in all layers
+    for l in range(2):
+        for i in range(6):
+            for b in range(c.need[i]):
+                p = c.table[c.where[i], b]
+                if p >= 0:
+                    assert np.array_equal(bounds64(c)[l, p], want_bounds(c, l, i, b, was))
+
+
+def test_bounds_of_infinities_and_nan(ctx):
+    c = lh.Cache(3, [20, 8], 8, 2, 64, "f16", bounds=True, garbage=False)
+    k = c.pool["k"]
+    p, r = int(c.table[c.where[0], 0]), int(c.table[c.where[0], 2])
+    k[0, p, 0, 3, 5], k[0, p, 0, 4, 6], k[0, p, 1, 0, 0] = float("nan"), float("inf"), -float("inf")
+    k[0, p, 0, :, 9] = float("nan")
+    k[0, r, :, 4:] = float("inf")                                             # behind the sequence's end
+    c.stored["k"] = lh.numbers(c.pool, "k")
+    ctx.hx_kv_bound(c.pool, 0, c.seqs, sh.i32(c.where))
+    got = bounds64(c)
+    for b in range(3):
+        assert np.array_equal(got[0, c.table[c.where[0], b]], want_bounds(c, 0, 0, b, got))
+    assert got[0, p, 0, 0, 9] == np.inf and got[0, p, 0, 1, 9] == -np.inf and np.isfinite(got[0, r]).all()
+
+
+def test_bounds_of_rows_in_error(ctx):
+    c = lh.Cache(4, [20, 9, 30], 8, 2, 64, "bf16", bounds=True)
+    was = bounds64(c)
+    r0, r1, r2 = (int(x) for x in c.where)
+    seqs = dict(table=c.seqs["table"].clone(), len=c.seqs["len"])
+    seqs["table"][r2, 1] = c.n_pages
+    ctx.hx_kv_bound(c.pool, 0, seqs, sh.i32([r0, -1, 99, r1, r2]), sh.i32([21, 1, 1, -1, 30]))
+    assert lh.status(ctx) == -6
+    want = was.copy()
+    for b in (0, 2, 3):
+        want[0, c.table[r2, b]] = want_bounds(c, 0, 2, b, was)
+    assert np.array_equal(bounds64(c), want, equal_nan=True)
+    ctx.hx_kv_bound(c.pool, 0, c.seqs, sh.i32([]))
+    assert lh.status(ctx) == 0
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e2m1"])
+def test_bounds_go_with_their_pages(ctx, cache):
+    c = lh.Cache(5, [20, 33], 8, 2, 64, cache, bounds=True, extra_rows=2)
+    ctx.hx_kv_bound(c.pool, -1, c.seqs, sh.i32(c.where))
+    before = bounds64(c)
+    empty = int(np.setdiff1d(np.arange(c.rows), c.where)[0])
+    ctx.hx_kv_fork(c.pool, c.seqs, sh.i32([c.where[1]]), sh.i32([empty]))
+    table = c.seqs["table"].cpu().numpy()
+    assert np.array_equal(bounds64(c)[:, table[empty, 4]], before[:, table[c.where[1], 4]])
+    ctx.hx_kv_free(c.pool, c.seqs, sh.i32([c.where[1]]))
+    held = [(r, b) for r in range(c.rows) for b in range(table.shape[1]) if table[r, b] >= 0 and r != c.where[1]]
+    was = {x: bounds64(c)[:, table[x]] for x in held}
+    ctx.hx_kv_compact(c.pool, c.seqs)
+    assert lh.status(ctx) == 0
+    table = c.seqs["table"].cpu().numpy()
+    assert all(np.array_equal(bounds64(c)[:, table[x]], was[x]) for x in held)
+
+
+def check_top(ctx, lens, nq, n_pages, n_first=0, n_last=1, heads=2, group=2, dim=64, T=8, type_="bf16", cache=None, missing=(), scale=None, wide=True,
+              seed=0, max_len=None, alike=0.7, change=None, with_chosen=True):
+    import torch
+    c = lh.Cache(seed, lens, T, heads, dim, cache or type_, missing=missing, alike=alike, bounds=True)
+    if change:
+        change(c)
+    ctx.hx_kv_bound(c.pool, 1, c.seqs, sh.i32(c.where))
+    ptr = np.concatenate([[0], np.cumsum(nq)])
+    total = int(ptr[-1])
+    q = lh.queries(total, heads * group, dim, type_, seed, wide)
+    out = torch.full_like(q, 7.0)
+    lse = torch.full((total, heads * group), 7.0, device="cuda:0")
+    chosen = torch.full((total, heads, n_pages), 7, dtype=torch.int32, device="cuda:0") if with_chosen else None
+    ctx.hx_attend_top(c.pool, 1, c.seqs, sh.i32(ptr), q, out, max_q=max(nq), max_len=max_len, n_pages=n_pages, n_first=n_first, n_last=n_last,
+                      row=sh.i32(c.where), scale=scale, chosen=chosen, lse=lse)
+    assert lh.status(ctx) == 0
+    qf, got, got_lse, bounds = lh.f64(q), lh.f64(out), lh.f64(lse), bounds64(c)
+    scale = dim ** -0.5 if scale is None else scale
+    for i in range(len(lens)):
+        k, v = c.of(c.k, 1, i), c.of(c.v, 1, i)
+        pages = c.table[c.where[i], :c.need[i]]
+        for x in range(nq[i]):
+            j, pos = int(ptr[i]) + x, lens[i] - nq[i] + x
+            own = pos // T
+            for h in range(heads):
+                want = lh.choose(bounds[1, np.maximum(pages, 0), h], pages >= 0, own, qf[j, h * group:(h + 1) * group], -1.0 if scale < 0 else 1.0, n_pages,
+                                 n_first, n_last)
+                if with_chosen:
+                    assert chosen[j, h].tolist() == want + [-1] * (n_pages - len(want)), (i, x, h)
+                see = np.isin(np.arange(lens[i]) // T, want) & (np.arange(lens[i]) <= pos)
+                part = slice(h * group, (h + 1) * group)
+                lh.compare(got[j:j + 1, part], got_lse[j:j + 1, part], qf[j:j + 1, part], k[:, h:h + 1], v[:, h:h + 1], see[None], scale, group, type_)
+
+
+@pytest.mark.parametrize("type_,cache", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "e4m3"), ("f16", "e4m3"), ("bf16", "e2m1"), ("f16", "e2m1")])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_types(ctx, type_, cache, dim):
+    check_top(ctx, [1, 7, 8, 9, 64, 65, 300, 511], [1] * 8, n_pages=6, n_first=1, n_last=2, dim=dim, type_=type_, cache=cache)
+
+
+@pytest.mark.parametrize("T", [1, 2, 16, 64, 256])
+@pytest.mark.parametrize("n_pages,n_first,n_last", [(1, 0, 1), (2, 0, 1), (5, 0, 5), (9, 4, 1), (40, 1, 2)])
+def test_page_sizes_and_what_is_seen_in_any_case(ctx, T, n_pages, n_first, n_last):
+    check_top(ctx, [3, 5 * T, 20 * T + 1, 41 * T - 1 if T < 64 else 700], [1, 1, 1, 1], n_pages=n_pages, n_first=n_first, n_last=n_last, T=T)
+
+
+@pytest.mark.parametrize("heads,group", [(1, 1), (3, 3), (2, 5), (1, 8), (2, 16), (1, 33), (1, 130)])
+def test_head_layouts(ctx, heads, group):
+    check_top(ctx, [90, 333], [1, 2], n_pages=7, n_first=1, heads=heads, group=group)
+
+
+@pytest.mark.parametrize("wide", [True, False])
+def test_prompts(ctx, wide):
+    """Every query chooses for itself, up to its own page."""
+    check_top(ctx, [40, 100, 70], [40, 33, 1], n_pages=4, n_first=1, n_last=2, wide=wide, dim=128)
+
+
+@pytest.mark.parametrize("n", [2500, 9000])
+@pytest.mark.parametrize("max_len", [None, 1])
+def test_many_pages(ctx, n, max_len):
+    """Thousands of bounds: dealt into bins more than once; whatever is said of the lengths."""
+    check_top(ctx, [n, n - 1], [1, 1], n_pages=300, n_first=2, n_last=3, T=1, heads=1, max_len=max_len)
+    check_top(ctx, [n, 17], [1, 1], n_pages=64, T=4, heads=2, max_len=max_len, with_chosen=False, seed=1)
+
+
+def test_scales(ctx):
+    for scale in (-0.3, 0.0, 2.0):
+        check_top(ctx, [200], [3], n_pages=5, scale=scale)
+
+
+def test_pages_that_are_not_there(ctx):
+    """Not among the first, the last, the others, nor the query's own; the others take their places."""
+    check_top(ctx, [100, 104, 99, 16, 5], [1] * 5, n_pages=5, n_first=2, n_last=2, missing=[(0, 0), (0, 5), (1, 11), (1, 12), (2, 12), (2, 3), (3, 0), (3, 1), (4, 0)])
+    gone = [(0, b) for b in range(12) if b not in (3, 9)]
+    check_top(ctx, [100], [1], n_pages=5, n_first=1, missing=gone)
+
+
+def test_equal_bounds_go_to_the_lowest_pages(ctx):
+    def few(c):
+        """Keys of few whole numbers: hundreds of pages with the same bound, between others."""
+        import torch
+        g = torch.Generator("cuda:0").manual_seed(1)
+        x = torch.randint(0, 2, c.pool["k"].shape, generator=g, device="cuda:0").float()
+        c.pool["k"].copy_(torch.where(c.pool["k"].isnan(), c.pool["k"].float(), x * (torch.arange(x.shape[1], device="cuda:0") % 3 == 0)[None, :, None, None, None]))
+        c.stored["k"] = lh.numbers(c.pool, "k")
+        c.k = c.stored["k"]
+    for seed in range(3):
+        check_top(ctx, [1500, 800], [1, 2], n_pages=50, n_first=1, n_last=1, T=2, heads=1, group=1, change=few, seed=seed)
+
+    def same(c):
+        c.pool["k"].fill_(1.0)
+        c.stored["k"] = lh.numbers(c.pool, "k")
+        c.k = c.stored["k"]
+    check_top(ctx, [1500, 40], [1, 2], n_pages=9, n_first=1, n_last=2, T=2, change=same)
+
+
+def test_bounds_that_are_infinite_or_no_number(ctx):
+    def odd(c):
+        """Keys of +-infinity in places where the query has a part or none, and NaN: of pages that may be chosen, or not."""
+        k = c.pool["k"]
+        pages = c.table[c.where[0]]
+        k[1, pages[3], 0, 2, 5], k[1, pages[4], 0, 1, 6] = -float("inf"), -float("inf")
+        k[1, pages[6], :, :, 7] = -float("inf")
+        k[1, pages[8], 0, 0, 9] = float("nan")
+        c.stored["k"] = lh.numbers(c.pool, "k")
+        c.k = c.stored["k"]
+    import torch
+    lens, T, dim, n_pages = [100], 8, 64, 5
+    c = lh.Cache(9, lens, T, 1, dim, "bf16", bounds=True)
+    odd(c)
+    ctx.hx_kv_bound(c.pool, 1, c.seqs, sh.i32(c.where))
+    bounds = bounds64(c)
+    pages = c.table[c.where[0], :13]
+    for seed in range(4):
+        q = lh.queries(1, 2, dim, "bf16", seed).clone()
+        if seed == 3:
+            q[:, :, 7] = 0.0
+        out, chosen = torch.zeros_like(q), torch.zeros(1, 1, n_pages, dtype=torch.int32, device="cuda:0")
+        ctx.hx_attend_top(c.pool, 1, c.seqs, sh.i32([0, 1]), q, out, max_q=1, n_pages=n_pages, n_first=1, row=sh.i32(c.where), chosen=chosen)
+        want = lh.choose(bounds[1, pages, 0], pages >= 0, 12, lh.f64(q)[0], 1.0, n_pages, 1, 1)
+        assert chosen[0, 0].tolist() == want + [-1] * (n_pages - len(want))
+    assert lh.status(ctx) == 0
+
+
+def test_what_is_not_chosen_has_no_part(ctx):
+    """Values and keys of pages that are not chosen may be anything; the bounds alone decide."""
+    import torch
+    c = lh.Cache(11, [400], 8, 1, 64, "bf16", bounds=True, alike=1.0)
+    ctx.hx_kv_bound(c.pool, 1, c.seqs, sh.i32(c.where))
+    q = lh.queries(1, 2, 64, "bf16", 0).clone()
+    call = dict(max_q=1, n_pages=6, n_first=1, n_last=2, row=sh.i32(c.where))
+    a, b, chosen = torch.zeros_like(q), torch.zeros_like(q), torch.zeros(1, 1, 6, dtype=torch.int32, device="cuda:0")
+    ctx.hx_attend_top(c.pool, 1, c.seqs, sh.i32([0, 1]), q, a, chosen=chosen, **call)
+    others = np.setdiff1d(np.arange(50), chosen.cpu().numpy())
+    for name in ("k", "v"):
+        c.pool[name][:, c.table[c.where[0], others]] = float("nan")
+    ctx.hx_attend_top(c.pool, 1, c.seqs, sh.i32([0, 1]), q, b, **call)
+    assert torch.equal(a, b) and lh.status(ctx) == 0 and bool(a.isfinite().all())
+
+
+def test_all_pages_are_what_attention_sees(ctx):
+    """As many pages as there are: the same as hx_attend, bit for bit (the work is divided alike)."""
+    import torch
+    c = lh.Cache(12, [60, 33, 7], 8, 2, 64, "bf16", bounds=True)
+    q = lh.queries(3, 4, 64, "bf16", 0)
+    a, b = torch.zeros(2, 3, 4, 64, dtype=torch.bfloat16, device="cuda:0")
+    ctx.hx_attend_top(c.pool, 1, c.seqs, sh.i32([0, 1, 2, 3]), q, a, max_q=1, n_pages=20, row=sh.i32(c.where))
+    ctx.hx_attend(c.pool, 1, c.seqs, sh.i32([0, 1, 2, 3]), q, b, max_q=1, row=sh.i32(c.where))
+    assert torch.equal(a, b) and lh.status(ctx) == 0
+
+
+def test_queries_and_rows_out_of_range(ctx):
+    import torch
+    c = lh.Cache(13, [60, 33, 7, 20], 8, 2, 64, "bf16", bounds=True)
+    ctx.hx_kv_bound(c.pool, 1, c.seqs, sh.i32(c.where))
+    q = lh.queries(8, 4, 64, "bf16", 0)
+    out, lse = torch.full((8, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda:0"), torch.full((8, 4), 7.0, device="cuda:0")
+    good, good_lse = torch.zeros_like(out), torch.zeros_like(lse)
+    call = dict(max_q=2, n_pages=3, n_first=1)
+    rows = [int(c.where[0]), 99, int(c.where[2]), int(c.where[3])]
+    ctx.hx_attend_top(c.pool, 1, c.seqs, sh.i32([0, 2, 4, 7, 8]), q, out, row=sh.i32(rows), lse=lse, **call)      # no such row; three queries where two are said
+    assert lh.status(ctx) == -6
+    assert bool((out[2:7] == 0).all()) and bool((lse[2:7] == -float("inf")).all())
+    ctx.hx_attend_top(c.pool, 1, c.seqs, sh.i32([0, 2]), q[:2], good[:2], row=sh.i32(rows[:1]), lse=good_lse[:2], **call)
+    ctx.hx_attend_top(c.pool, 1, c.seqs, sh.i32([0, 1]), q[7:], good[7:], row=sh.i32(rows[3:]), lse=good_lse[7:], **call)
+    assert lh.status(ctx) == 0
+    assert torch.equal(out[[0, 1, 7]], good[[0, 1, 7]]) and torch.equal(lse[[0, 1, 7]], good_lse[[0, 1, 7]])
+    seqs = dict(table=c.seqs["table"].clone(), len=c.seqs["len"])
+    seqs["table"][rows[0], 3] = c.n_pages + 7                                  # no page of the pool: taken for one that is not there
+    chosen = torch.zeros(1, 2, 3, dtype=torch.int32, device="cuda:0")
+    ctx.hx_attend_top(c.pool, 1, seqs, sh.i32([0, 1]), q[:1], out[:1], row=sh.i32(rows[:1]), chosen=chosen, **call)
+    assert lh.status(ctx) == -6 and not bool((chosen == 3).any())
+    ctx.hx_attend_top(c.pool, 1, c.seqs, sh.i32([0]), q[:0], out[:0], max_q=0, n_pages=3)
+    assert lh.status(ctx) == 0
+
+
+def test_queries_in_several_parts(ctx):
+    """Rows of so many entries that the scores of all queries are not held at once: the same as one query after the other."""
+    import torch
+    T, heads, n_q, wide_rows = 1, 1, 40, 1 << 20
+    c = lh.Cache(14, [300], T, heads, 64, "bf16", bounds=True, extra_rows=0)
+    table = torch.full((1, wide_rows), -1, dtype=torch.int32, device="cuda:0")
+    table[:, :c.seqs["table"].shape[1]] = c.seqs["table"]
+    seqs = dict(table=table, len=c.seqs["len"])
+    ctx.hx_kv_bound(c.pool, 1, c.seqs, sh.i32([0]))
+    q = lh.queries(n_q, 2, 64, "bf16", 0)
+    out, want = torch.zeros(2, n_q, 2, 64, dtype=torch.bfloat16, device="cuda:0")
+    lse, want_lse = torch.zeros(2, n_q, 2, device="cuda:0")
+    chosen, want_chosen = torch.zeros(2, n_q, 1, 9, dtype=torch.int32, device="cuda:0")
+    ctx.hx_attend_top(c.pool, 1, seqs, sh.i32([0, n_q]), q, out, max_q=n_q, n_pages=9, max_len=300, chosen=chosen, lse=lse)      # 32 queries' scores are 256 MB
+    ctx.hx_attend_top(c.pool, 1, c.seqs, sh.i32([0, n_q]), q, want, max_q=n_q, n_pages=9, max_len=300, chosen=want_chosen, lse=want_lse)
+    assert lh.status(ctx) == 0
+    assert torch.equal(chosen, want_chosen) and torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+def test_captured_and_on_another_stream(ctx):
+    import torch
+    c = lh.Cache(15, [500, 130], 8, 2, 64, "bf16", bounds=True)
+    q = torch.zeros(2, 4, 64, dtype=torch.bfloat16, device="cuda:0")
+    out, chosen = torch.zeros_like(q), torch.zeros(2, 2, 7, dtype=torch.int32, device="cuda:0")
+    row, ptr = sh.i32(c.where), sh.i32([0, 1, 2])
+
+    def calls(s):
+        ctx.hx_kv_bound(c.pool, 1, c.seqs, row, stream=s)
+        ctx.hx_attend_top(c.pool, 1, c.seqs, ptr, q, out, max_q=1, n_pages=7, n_first=1, row=row, chosen=chosen, stream=s)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    calls(s)
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        calls(s)
+    for seed in range(3):
+        q.copy_(torch.randn(q.shape, generator=torch.Generator("cuda:0").manual_seed(seed), device="cuda:0"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        a, b = out.clone(), chosen.clone()
+        out.zero_(); chosen.zero_()
+        calls(None)
+        torch.cuda.synchronize()
+        assert torch.equal(a, out) and torch.equal(b, chosen)
+
+
+def test_scratch_does_not_grow_while_a_stream_is_captured():
+    """The call that would have to allocate is refused before it launches anything; the same call later is fine."""
+    import torch
+    from paper_2605_16637_amd import binding
+    fresh = binding.Context(0)
+    c = lh.Cache(16, [900], 8, 2, 64, "bf16", bounds=True)
+    row, ptr, q = sh.i32(c.where), sh.i32([0, 1]), lh.queries(1, 4, 64, "bf16", 0)
+    out = torch.full((1, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda:0")
+    fresh.hx_kv_bound(c.pool, 1, c.seqs, row)
+    call = lambda s=None: fresh.hx_attend_top(c.pool, 1, c.seqs, ptr, q, out, max_q=1, n_pages=40, row=row, stream=s)  # noqa: E731
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph, other = torch.cuda.CUDAGraph(), torch.zeros(1, device="cuda:0")
+    with torch.cuda.graph(graph, stream=s):
+        other.add_(1)
+        with pytest.raises(binding.HxError, match="captured"):
+            call(s)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert bool((out == 7.0).all()) and int(other) == 1
+    call()
+    fresh.hx_stream_status()
+    assert not bool((out == 7.0).all())
+    fresh.close()
