@@ -39,7 +39,7 @@
  *    thread-safe.
  *  - Device memory is allocated by hx_ctx_create and hx_dag_reserve, and by
  *    hx_decode_score, hx_rank (beyond 28672 calls), hx_kv_fork, hx_kv_grow,
- *    hx_kv_keep, hx_kv_compact, hx_attend and hx_attend_top the first time they meet a larger
+ *    hx_kv_keep, hx_kv_compact, hx_kv_evict, hx_attend and hx_attend_top the first time they meet a larger
  *    problem than before; every other call only launches kernels and
  *    can be captured in a HIP graph (hx_validate_round and hx_stream_status
  *    wait for the stream and cannot).
@@ -823,6 +823,33 @@ typedef struct {
 #define HX_MAX_TOP 4096
 int hx_attend_top(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_kv_seqs *seqs,
                   const hx_attend_args *args, const hx_top *top, void *stream);
+
+/*
+ * What hx_attend with the same args gave each token, summed: for every sequence
+ * and position y of its row
+ *   weight[row][y] += sum over its queries j that see y and their heads a of exp(s - lse[j][a])
+ * weight: device [seqs n][max_pages * page_tokens].  args->lse is hx_attend's;
+ * where it is not finite a query's head adds nothing.  args->out is not used.  A
+ * row listed twice counts once, for its first entry.  Sums are held in 32 bits
+ * and added in an order that the arguments alone determine.
+ */
+int hx_kv_weigh(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_kv_seqs *seqs,
+                const hx_attend_args *args, float *weight, void *stream);
+
+/*
+ * Every row[i] of more than n_keep tokens is cut to n_keep: the first n_first,
+ * the last n_last, and of the others those of the largest weight[row][y], of equal
+ * ones the earlier (what is not above 0 counts as 0).  Tokens whose page is not
+ * there go.  The others move together in every layer, in order, and their weights
+ * with them (those behind them become 0); pages past them are given back.  A page
+ * that other rows hold too, or that is not there, is replaced by a free one where
+ * something in it would change or where the row goes on in it; rows for which no
+ * page is left are left as they are (HX_ERR_CAPACITY).  kept: device [n][n_keep]
+ * out, the positions that the tokens had, then -1 (all -1: the row is as it was), or
+ * NULL.  A position is the token's place in its row: windows count what has stayed.
+ */
+int hx_kv_evict(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs *seqs, int32_t n, const int32_t *row,
+                float *weight, int32_t n_keep, int32_t n_first, int32_t n_last, int32_t *kept, void *stream);
 
 /*
  * One token a row from its logits (dtype HX_F32, HX_BF16 or HX_F16; row_stride

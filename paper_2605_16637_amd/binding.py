@@ -22,7 +22,7 @@ EXPORTS = ("hx_ctx_create", "hx_ctx_destroy", "hx_last_error", "hx_stream_status
            "hx_score_placements", "hx_validate_round", "hx_select", "hx_urgency", "hx_commit", "hx_commit_static", "hx_round", "hx_rank", "hx_plan_greedy",
            "hx_decode_score", "hx_decode_plan_greedy",
            "hx_kv_fork", "hx_kv_grow", "hx_kv_write", "hx_kv_read", "hx_kv_keep", "hx_kv_free", "hx_kv_compact", "hx_kv_bound", "hx_attend", "hx_attend_top",
-           "hx_sample")
+           "hx_kv_weigh", "hx_kv_evict", "hx_sample")
 
 HX_F32, HX_BF16, HX_F16, HX_E4M3, HX_E2M1 = 1, 2, 3, 4, 5
 
@@ -322,6 +322,10 @@ def _attend_args(kv, sq, q_ptr, q, out, max_q, max_len, row, scale, lse):
         a.out, a.out_token, a.out_head = _strided(out, n_q, heads, kv.head_dim)
     a.lse, a.scale = _ptr(lse, torch.float32, n_q * heads), kv.head_dim ** -0.5 if scale is None else float(scale)
     return a
+
+
+def _weights(weight, kv, sq):
+    return _ptr(weight, _torch().float32, sq.n * sq.max_pages * kv.page_tokens)
 
 
 class Context:
@@ -675,6 +679,20 @@ class Context:
         a = _attend_args(kv, sq, q_ptr, q, out, max_q, max_len, row, scale, lse)
         t = hx_top(int(n_pages), int(n_first), int(n_last), _ptr(chosen, _torch().int32, a.n_q * kv.n_heads * int(n_pages)))
         self._invoke(self.lib.hx_attend_top, self._ctx, C.byref(kv), int(layer), C.byref(sq), C.byref(a), C.byref(t), _stream(stream))
+
+    def hx_kv_weigh(self, pool, layer, seqs, q_ptr, q, lse, weight, max_q, max_len=None, row=None, scale=None, window=0, n_sink=0, parent=None, stream=None):
+        """The arguments of an hx_attend call and the lse that it left; weight [rows of the tables, entries of a row * page_tokens]."""
+        kv, sq = make_kv_pool(pool), make_kv_seqs(seqs)
+        a = _attend_args(kv, sq, q_ptr, q, None, max_q, max_len, row, scale, lse)
+        a.window, a.n_sink, a.parent = int(window), int(n_sink), _ptr(parent, _torch().int32, a.n_q)
+        self._invoke(self.lib.hx_kv_weigh, self._ctx, C.byref(kv), int(layer), C.byref(sq), C.byref(a), _weights(weight, kv, sq), _stream(stream))
+
+    def hx_kv_evict(self, pool, seqs, row, weight, n_keep, n_first=0, n_last=0, kept=None, stream=None):
+        """weight as in hx_kv_weigh; kept [rows in the call, n_keep]."""
+        torch = _torch()
+        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs), int(row.numel()), torch.int32
+        self._invoke(self.lib.hx_kv_evict, self._ctx, C.byref(kv), C.byref(sq), n, _ptr(row, i32), _weights(weight, kv, sq), int(n_keep), int(n_first),
+                     int(n_last), _ptr(kept, i32, n * max(int(n_keep), 0)), _stream(stream))
 
     def hx_sample(self, logits, u, token, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, n_kept=None, stream=None):
         """logits [rows, vocabulary], the rows any stride apart."""

@@ -12,7 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhx.so")
 CALIB_LIB = os.path.join(HERE, "libhx_calib.so")      # the benchmark's calibration kernels, a library of their own
 MARSHAL_LIB = os.path.join(HERE, "hx_marshal.so")     # host code of the binding (hx_marshal.cpp), a Python module
-SOURCES = ["hx_ctx.hip", "hx_score.hip", "hx_dag.hip", "hx_plan.hip", "hx_decode.hip", "hx_kv.hip", "hx_kv_bound.hip", "hx_attend.hip", "hx_attend_top.hip", "hx_sample.hip",
+SOURCES = ["hx_ctx.hip", "hx_score.hip", "hx_dag.hip", "hx_plan.hip", "hx_decode.hip", "hx_kv.hip", "hx_kv_bound.hip", "hx_kv_evict.hip",
+           "hx_attend.hip", "hx_attend_top.hip", "hx_attend_weigh.hip", "hx_sample.hip",
            "hx_attend_bf16.hip", "hx_attend_f16.hip", "hx_attend_bf16_e4m3.hip", "hx_attend_f16_e4m3.hip",
            "hx_attend_bf16_e2m1.hip", "hx_attend_f16_e2m1.hip"]
 FLAGS = [

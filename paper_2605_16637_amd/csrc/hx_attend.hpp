@@ -647,9 +647,9 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4
     using X8 = typename Types<E>::x8;
     using X2 = typename Types<E>::x2;
     constexpr int CH = D / 8, ROW_BYTES = ROW<BITS, D>;
-    constexpr int K_BYTES = ROW_BYTES < 64 ? ROW_BYTES / 4 : 16, K_LOADS = ROW_BYTES / 4 / K_BYTES;     // a lane's load for 16 keys, and how many
-    constexpr int K_NUMBERS = K_BYTES * 8 / BITS;               // of a load
-    using KPiece = std::conditional_t<K_BYTES == 8, uint2, uint4>;
+    using Keys = KeyPieces<BITS, D>;
+    using KPiece = typename Keys::Piece;
+    constexpr int K_BYTES = Keys::BYTES, K_LOADS = Keys::LOADS;
     constexpr int V_BYTES = ROW_BYTES < 64 ? 8 : 16, V_LOADS = FEW_KEYS * ROW_BYTES / (64 * V_BYTES);     // of a lane for the tile
     constexpr int PER_ROW = ROW_BYTES / V_BYTES;                // a load of the wavefront: at most 16 keys
     using VPiece = std::conditional_t<V_BYTES == 8, uint2, uint4>;
@@ -691,8 +691,7 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4
 #pragma unroll
         for (int s = 0; s < D / 32; ++s) {
             // which 8 numbers of a row a lane's s-th piece of a key holds
-            constexpr int EACH = K_NUMBERS / 8;
-            const int d = (s / EACH) * (4 * K_NUMBERS) + quad * K_NUMBERS + (s % EACH) * 8;
+            const int d = Keys::place(s, quad);
             X8 x = {};
             if (view[w].alive) {
                 if (a.q_wide) x = *(const X8 *)(qp + d);
@@ -799,29 +798,12 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4
             f32x4 acc[COLS] = {};
 #pragma unroll
             for (int i = 0; i < K_LOADS; ++i) {
-                if constexpr (BITS == 4) {
-                    const float unit = power_of(ek[b][i]);
-                    const uint32_t *kk = (const uint32_t *)&rk[b][i];
 #pragma unroll
-                    for (int j = 0; j < K_NUMBERS / 8; ++j) {
-                        union { X2 x2[4]; X8 x8; } kw;
-                        widen4(kk[j], unit, kw.x2);
+                for (int j = 0; j < Keys::EACH; ++j) {
+                    const X8 k = Keys::template operand<E>(rk[b][i], BITS == 4 ? ek[b][i] : 0, j);
 #pragma unroll
-                        for (int w = 0; w < COLS; ++w) acc[w] = mfma16(kw.x8, qf[w][K_NUMBERS / 8 * i + j], acc[w]);
-                    }
-                } else if constexpr (BITS == 8) {
-                    union { X2 x2[8]; X8 x8[2]; } kw;
-                    const uint32_t kk[4] = {rk[b][i].x, rk[b][i].y, rk[b][i].z, rk[b][i].w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) widen(kk[j], kw.x2[2 * j], kw.x2[2 * j + 1]);
-#pragma unroll
-                    for (int w = 0; w < COLS; ++w) {
-                        acc[w] = mfma16(kw.x8[0], qf[w][2 * i], acc[w]);
-                        acc[w] = mfma16(kw.x8[1], qf[w][2 * i + 1], acc[w]);
-                    }
-                } else
-#pragma unroll
-                    for (int w = 0; w < COLS; ++w) acc[w] = mfma16(__builtin_bit_cast(X8, rk[b][i]), qf[w][i], acc[w]);
+                    for (int w = 0; w < COLS; ++w) acc[w] = mfma16(k, qf[w][Keys::EACH * i + j], acc[w]);
+                }
             }
 #pragma unroll
             for (int w = 0; w < COLS; ++w) s[w][b] = acc[w];
@@ -925,8 +907,7 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4
 #pragma unroll
                 for (int x = 0; x < D / 32; ++x) {
                     float k[8];
-                    constexpr int EACH = K_NUMBERS / 8;
-                    const int d = (x / EACH) * (4 * K_NUMBERS) + quad * K_NUMBERS + (x % EACH) * 8;
+                    const int d = Keys::place(x, quad);
                     numbers<E, BITS, 8>(k_at + at + d * BITS / 8, ke_at + at / 16 + d / 32, k);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) dot = fmaf((float)qf[w][x][i], k[i], dot);

@@ -79,6 +79,29 @@ __device__ __forceinline__ bool any_odd(const F *o)
 // Bytes of a row of D numbers, without its scales.
 template <int BITS, int D> constexpr int ROW = D * BITS / 8;
 
+// How the keys of 16 rows go from memory into a matrix product: a lane's load, how many, and the place of the 8 numbers of the s-th of D / 32 operands.
+template <int BITS, int D>
+struct KeyPieces {
+    static constexpr int BYTES = ROW<BITS, D> < 64 ? ROW<BITS, D> / 4 : 16, LOADS = ROW<BITS, D> / 4 / BYTES;
+    static constexpr int NUMBERS = BYTES * 8 / BITS, EACH = NUMBERS / 8;         // of a load: numbers, operands
+    using Piece = std::conditional_t<BYTES == 8, uint2, uint4>;
+    static __device__ __forceinline__ int place(int s, int quad) { return (s / EACH) * (4 * NUMBERS) + quad * NUMBERS + (s % EACH) * 8; }
+    // operand j of a load; exp: its scale's byte, of 4 bits
+    template <typename E>
+    static __device__ __forceinline__ typename Types<E>::x8 operand(const Piece &piece, uint32_t exp, int j)
+    {
+        using X8 = typename Types<E>::x8;
+        if constexpr (BITS == 16) return __builtin_bit_cast(X8, piece);
+        else {
+            union { typename Types<E>::x2 x2[4]; X8 x8; } k;
+            struct Words { uint32_t w[BYTES / 4]; } w = __builtin_bit_cast(Words, piece);
+            if constexpr (BITS == 4) widen4(w.w[j], power_of(exp), k.x2);
+            else { widen(w.w[2 * j], k.x2[0], k.x2[1]); widen(w.w[2 * j + 1], k.x2[2], k.x2[3]); }
+            return k.x8;
+        }
+    }
+};
+
 // N stored numbers (N 4 or 8, of one group); exp: their scale's byte, of 4 bits only
 template <typename E, int BITS, int N>
 __device__ __forceinline__ void numbers(const char *from, const uint8_t *exp, float *to)

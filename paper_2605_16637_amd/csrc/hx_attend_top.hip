@@ -1,6 +1,7 @@
 // Attention over the pages that every query chooses for every KV head: what a page's keys can score at most, the pages of the largest of these,
 // and hx_attend's kernels over them, for which each query and KV head is a sequence with a table of its own.
 #include "hx_attend_common.hpp"
+#include "hx_nth.hpp"
 
 namespace {
 
@@ -158,131 +159,15 @@ __global__ __launch_bounds__(TOP_THREADS) void hx_top_score_kernel(TopArgs t)
 
 // ---- the pages of the largest ------------------------------------------------
 
-constexpr int BINS = 512, LIST = 256;
 constexpr int PICK_WAVES = TOP_THREADS / 64;
 
-struct Picking {
-    int bins[BINS];
-    double list[LIST];
-    double least[PICK_WAVES], most[PICK_WAVES];
-    int count[2][PICK_WAVES];
-    int above, n_list, bin;
-    double edge;
-    int equals;
-};
-
-// The n-th largest of the scores of pages from .. to-1 (pages there are more than n), and how many equal to it are among the first n.  Scores are
-// dealt into bins between the least and the largest of those that are left, and the bin that holds the n-th is looked at again, until few
-// enough are left to compare each with each.  -infinity counts for nothing and is the edge where there are no n others.
-__device__ __forceinline__ void nth_largest(const double *score, int from, int to, int n, Picking &s)
-{
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    double lo = -__builtin_inf(), hi = __builtin_inf();        // those that are left: lo <= score <= hi, and n of them are wanted
-    for (bool first = true;; first = false) {
-        // the least and the largest finite one, and how many are infinite
-        double least = __builtin_inf(), most = -__builtin_inf();
-        int infinite = 0, left = 0;
-        for (int b = from + tid; b < to; b += TOP_THREADS) {
-            const double x = score[b];
-            if (!(x >= lo && x <= hi) || x == -__builtin_inf()) continue;
-            ++left;
-            if (x == __builtin_inf()) { ++infinite; continue; }
-            least = fmin(least, x);
-            most = fmax(most, x);
-        }
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) {
-            least = fmin(least, across(least, d));
-            most = fmax(most, across(most, d));
-            infinite += __shfl_xor(infinite, d);
-            left += __shfl_xor(left, d);
-        }
-        if (lane == 0) { s.least[wave] = least; s.most[wave] = most; s.count[0][wave] = infinite; s.count[1][wave] = left; }
-        for (int i = tid; i < BINS; i += TOP_THREADS) s.bins[i] = 0;
-        if (tid == 0) s.n_list = 0;
-        __syncthreads();
-        infinite = left = 0;
-#pragma unroll
-        for (int w = 0; w < PICK_WAVES; ++w) {
-            least = w == 0 ? s.least[0] : fmin(least, s.least[w]);
-            most = w == 0 ? s.most[0] : fmax(most, s.most[w]);
-            infinite += s.count[0][w];
-            left += s.count[1][w];
-        }
-        if (left <= n) {                                       // all that are left
-            if (tid == 0) { s.edge = first ? -__builtin_inf() : least; s.equals = INT32_MAX; }
-            __syncthreads();
-            return;
-        }
-        if (infinite >= n) { if (tid == 0) { s.edge = __builtin_inf(); s.equals = n; } __syncthreads(); return; }
-        n -= infinite;
-        if (least == most) { if (tid == 0) { s.edge = least; s.equals = n; } __syncthreads(); return; }
-        if (left - infinite > LIST) {
-            // (rounding is monotonous: a larger score is in no lower bin)
-            const double unit = (BINS - 1) / (most - least);
-            auto bin_of = [&](double x) { const double y = (x - least) * unit; return y < BINS - 1 ? (int)y : BINS - 1; };
-            for (int b = from + tid; b < to; b += TOP_THREADS) {
-                const double x = score[b];
-                if (x >= least && x <= most) atomicAdd(s.bins + bin_of(x), 1);
-            }
-            __syncthreads();
-            if (wave == 0) {
-                // a lane's bins, the highest first; how many lie in those of the lanes before it
-                int mine = 0;
-#pragma unroll
-                for (int i = 0; i < BINS / 64; ++i) mine += s.bins[BINS - 1 - lane * (BINS / 64) - i];
-                int before = mine;
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) { const int y = __shfl_up(before, d); if (lane >= d) before += y; }
-                before -= mine;
-                if (before < n && before + mine >= n) {
-                    for (int i = 0; i < BINS / 64; ++i) {
-                        const int at = BINS - 1 - lane * (BINS / 64) - i, c = s.bins[at];
-                        if (before + c >= n) { s.bin = at; s.above = before; break; }
-                        before += c;
-                    }
-                }
-            }
-            __syncthreads();
-            const int bin = s.bin;
-            n -= s.above;
-            // the bin's own least and largest are the next range
-            double l = __builtin_inf(), h = -__builtin_inf();
-            for (int b = from + tid; b < to; b += TOP_THREADS) {
-                const double x = score[b];
-                if (x >= least && x <= most && bin_of(x) == bin) { l = fmin(l, x); h = fmax(h, x); }
-            }
-#pragma unroll
-            for (int d = 32; d > 0; d >>= 1) { l = fmin(l, across(l, d)); h = fmax(h, across(h, d)); }
-            if (lane == 0) { s.least[wave] = l; s.most[wave] = h; }
-            __syncthreads();
-            lo = s.least[0]; hi = s.most[0];
-#pragma unroll
-            for (int w = 1; w < PICK_WAVES; ++w) { lo = fmin(lo, s.least[w]); hi = fmax(hi, s.most[w]); }
-            __syncthreads();
-            continue;
-        }
-        for (int b = from + tid; b < to; b += TOP_THREADS) {
-            const double x = score[b];
-            if (x >= least && x <= most) s.list[atomicAdd(&s.n_list, 1)] = x;
-        }
-        __syncthreads();
-        const int m = s.n_list;
-        if (tid < m) {
-            const double x = s.list[tid];
-            int larger = 0, equal = 0;
-            for (int i = 0; i < m; ++i) { larger += s.list[i] > x; equal += s.list[i] == x; }
-            if (larger < n && larger + equal >= n) { s.edge = x; s.equals = n - larger; }          // (all that are equal write the same)
-        }
-        __syncthreads();
-        return;
-    }
-}
+// A score's key, 0 where it is -infinity (-0 and 0 are the same number).
+__device__ __forceinline__ uint64_t key_of(double x) { return x == -__builtin_inf() ? 0 : nth_key(x + 0.0); }
 
 // A workgroup a query and KV head.
 __global__ __launch_bounds__(TOP_THREADS) void hx_top_pick_kernel(TopArgs t)
 {
-    __shared__ Picking s;
+    __shared__ NthState<uint64_t, TOP_THREADS> s;
     __shared__ int s_before[2][PICK_WAVES];
     const AttendArgs &a = t.a;
     const KvView &kv = a.kv;
@@ -300,7 +185,7 @@ __global__ __launch_bounds__(TOP_THREADS) void hx_top_pick_kernel(TopArgs t)
     const bool all = p.own < t.n_pages || kv.n_pages == 0;
     const int from = t.n_first, to = p.own - t.n_last + 1;         // the pages between those that are seen in any case
     const double *score = t.score + (int64_t)pair * t.stride;
-    double edge = -__builtin_inf();
+    uint64_t edge = 0;
     int equals = 0;
     if (!all) {
         int want = t.n_pages;
@@ -317,10 +202,10 @@ __global__ __launch_bounds__(TOP_THREADS) void hx_top_pick_kernel(TopArgs t)
         for (int w = 0; w < PICK_WAVES; ++w) want -= s_before[0][w];
         __syncthreads();
         if (want > 0) {
-            nth_largest(score, from, to, want, s);
+            nth_largest([&](int b) { return key_of(score[b]); }, from, to, want, s);
             edge = s.edge;
             equals = s.equals;
-        } else edge = __builtin_inf();
+        } else edge = ~0ull;
     }
     // the pages in rising order
     int n = 0, seen_equal = 0;
@@ -328,8 +213,8 @@ __global__ __launch_bounds__(TOP_THREADS) void hx_top_pick_kernel(TopArgs t)
         const int b = b0 + tid;
         const int page = in_pool(kv, b <= p.own ? p.table[b] : -1);
         const bool between = !all && b >= from && b < to;
-        const double x = between && page >= 0 ? score[b] : 0.0;
-        const bool equal = between && page >= 0 && x == edge && x > -__builtin_inf();
+        const uint64_t x = between && page >= 0 ? key_of(score[b]) : 0;
+        const bool equal = x == edge && x > 0;
         const unsigned long long e = __builtin_amdgcn_ballot_w64(equal);
         if (lane == 0) s_before[0][wave] = __builtin_popcountll(e);
         __syncthreads();

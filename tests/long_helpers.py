@@ -181,3 +181,58 @@ def choose(bounds, there, own, q, sign, n_pages, n_first, n_last):
             score[b] = max(np.inf if np.isnan(y) else y for y in s)
     best = sorted((b for b in score if score[b] > -np.inf), key=lambda b: (-score[b], b))
     return sorted(fixed + best[:n_pages - len(fixed)])
+
+
+def evict(c, weight, rows, n_keep, n_first, n_last):
+    """The rules of eviction on a cache's tables and pages (c: table, length, ref, T; pages: {name: [layers, pages, heads, T, ..]}); returns errors and
+    the positions kept, for each row None where it is left."""
+    T, errors, kept, seen = c.T, set(), [], set()
+    plans, free = [], [p for p in range(len(c.ref)) if c.ref[p] == 0]
+    first_ref = c.ref.copy()
+    out = False
+    for r in rows:
+        twice = r in seen
+        seen.add(r)
+        if not 0 <= r < len(c.length) or twice or not 0 <= c.length[r] <= c.table.shape[1] * T:
+            errors.add(-6)
+            kept.append(None)
+            continue
+        n = int(c.length[r])
+        if n <= n_keep:
+            kept.append(None)
+            continue
+        page = lambda b: c.table[r][b] if 0 <= c.table[r][b] < len(c.ref) else -1  # noqa: E731
+        there = [y for y in range(n) if page(y // T) >= 0]
+        fixed = [y for y in there if y < n_first or y >= n - n_last]
+        w = lambda y: weight[r][y] if weight[r][y] > 0 else 0.0  # noqa: E731
+        others = sorted((y for y in there if n_first <= y < n - n_last), key=lambda y: (-w(y), y))
+        stay = sorted(fixed + others[:n_keep - len(fixed)])
+        m = len(stay)
+        changed = {j // T for j in range(m) if stay[j] != j} | ({m // T} if m % T else set())
+        new = sorted(b for b in changed if page(b) < 0 or first_ref[page(b)] > 1)
+        if new and (out or len(new) > len(free)):
+            out = True
+            errors.add(-4)
+            kept.append(None)
+            continue
+        plans.append((r, stay, {b: free.pop(0) for b in new}))
+        kept.append(stay)
+    for r, stay, new in plans:
+        n, m, old = int(c.length[r]), len(stay), c.table[r].copy()
+        target = [new.get(b, old[b]) for b in range(-(-m // T))]
+        for x in c.pages.values():
+            y = [x[:, old[s // T], :, s % T].copy() for s in stay]
+            for j in range(m):
+                x[:, target[j // T], :, j % T] = y[j]
+        weight[r][:m] = weight[r][stay]
+        weight[r][m:n] = 0.0
+        for b in range(-(-n // T)):
+            now = target[b] if b < len(target) else -1
+            if now != old[b]:
+                c.table[r][b] = now
+                if 0 <= old[b] < len(c.ref):
+                    c.ref[old[b]] -= 1
+        for p in new.values():
+            c.ref[p] = 1
+        c.length[r] = m
+    return errors, kept

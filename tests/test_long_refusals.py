@@ -85,3 +85,29 @@ def test_structures_match_the_header(tmp_path):
     subprocess.check_call(["gcc", "-std=c99", "-I", os.path.join(root, "include"), "-o", str(tmp_path / "a"), str(tmp_path / "a.c")])
     got = [int(x) for x in subprocess.check_output([str(tmp_path / "a")], text=True).split()]
     assert got == [C.sizeof(cls)] + [getattr(cls, f).offset for f, _ in cls._fields_]
+
+
+def test_weighing_that_is_refused(lib):  # noqa: F811
+    lib, ctx = lib
+
+    def call(p=pool(), layer=0, w=4096, **over):
+        return lib.hx_kv_weigh(ctx, C.byref(p), layer, C.byref(seqs()), C.byref(attend_args(**{**dict(lse=4096, out=None), **over})), w, None)
+    assert call(w=None) == INVALID and call(lse=None) == INVALID and call(w=4097) == INVALID and call(lse=4098) == INVALID
+    assert call(layer=2) == INVALID and call(q=None) == INVALID and call(n_heads=3) == SHAPE and call(max_q=257, parent=4096) == SHAPE
+    assert call(p=pool(head_dim=96)) == SHAPE and call(dtype=binding.HX_F16) == INVALID and call(n_q=0, lse=None, w=None) == 0
+    assert lib.hx_kv_weigh(ctx, C.byref(pool()), 0, C.byref(seqs()), None, 4096, None) == INVALID
+
+
+@pytest.mark.parametrize("n_keep,n_first,n_last,code", [(0, 0, 0, INVALID), (-1, 0, 0, INVALID), (4, -1, 0, INVALID), (4, 0, -1, INVALID), (4, 3, 2, INVALID),
+                                                        (2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1, INVALID)])
+def test_budgets_that_are_refused(lib, n_keep, n_first, n_last, code):  # noqa: F811
+    lib, ctx = lib
+    assert lib.hx_kv_evict(ctx, C.byref(pool()), C.byref(seqs()), 1, 4096, 4096, n_keep, n_first, n_last, None, None) == code
+
+
+def test_evictions_that_are_refused(lib):  # noqa: F811
+    lib, ctx = lib
+    call = lambda n=1, row=4096, w=4096, p=pool(), s=seqs(): lib.hx_kv_evict(ctx, C.byref(p), C.byref(s), n, row, w, 4, 1, 1, None, None)  # noqa: E731
+    assert call(n=-1) == INVALID and call(row=None) == INVALID and call(w=None) == INVALID and call(w=4098) == INVALID
+    assert call(n=0, row=None, w=None) == 0 and call(s=seqs(n=0, table=None, len=None)) == INVALID
+    assert call(n=1 << 20, p=pool(n_layers=1000)) == SHAPE and call(p=pool(dtype=0)) == INVALID and call(s=seqs(len=None)) == INVALID
