@@ -625,6 +625,9 @@ __device__ __forceinline__ float lane_16_away(float x)
 
 template <int CH> __device__ __forceinline__ int few_v_piece(int r, int c) { return r * CH + (c ^ (CH >= 16 ? (r & 7) << 1 : ((r >> 1) & 3) << 1)); }
 
+// As that, for values of 4 bits, of which a lane writes 2 or 4 pieces beside each other: 8 lanes' fall in different banks.
+template <int CH> __device__ __forceinline__ int four_v_piece(int r, int c) { return few_v_piece<CH>(r, c ^ ((c >> 3) & 3)) ^ (CH == 8 ? r & 1 : 0); }
+
 constexpr int FEW_KEYS = 32;
 
 // LDS of a wavefront: a tile's values, and at the end its sums
@@ -642,7 +645,7 @@ constexpr int few_wave_lds(int dim, int cols) { return FEW_KEYS * dim * 2 > 16 *
 // and rows are more than 16.  (The kernel for many rows, which the matrix units and the weights' arithmetic bound, has one number: two
 // took 9 to 29 % longer, 24 trees of 25 drafts 84 -> 94 us, the prompts above 213 -> 262.)
 template <typename E, int BITS, int D, int COLS, bool PAGE16>
-__global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4 : COLS == 1 && BITS < 16 ? 3 : 2) void hx_attend_few_kernel(AttendArgs a)
+__global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? (BITS == 4 ? 3 : 4) : COLS == 1 && BITS == 8 ? 3 : 2) void hx_attend_few_kernel(AttendArgs a)
 {
     using X8 = typename Types<E>::x8;
     using X2 = typename Types<E>::x2;
@@ -720,32 +723,23 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4
     const char *k_at = (const char *)kv.k + here, *v_at = (const char *)kv.v + here;
     const uint8_t *ke_at = BITS == 4 ? a.k_exp + here / 16 : nullptr, *ve_at = BITS == 4 ? a.v_exp + here / 16 : nullptr;      // a byte for 16
     const int in_page = (1 << kv.shift) - 1;
-    KPiece rk[2][K_LOADS];
-    VPiece rv[V_LOADS];
-    uint8_t ek[BITS == 4 ? 2 : 1][K_LOADS], ev[V_LOADS];         // scales of 4 bits
+    uint4 rk[2][K_LOADS], rv[V_LOADS];
     auto fetch_k = [&](int tile, int pages, bool whole) {
-        const int y0 = start_of(tile), off = col * ROW_BYTES + quad * K_BYTES;
+        const int y0 = start_of(tile), off = col * ROW_BYTES + quad * 16;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             if (whole) {
                 const int page = __builtin_amdgcn_readlane(pages, b * 16);
-                const int64_t at = page * page_bytes + ((y0 + b * 16) & in_page) * ROW_BYTES;
+                const char *at = k_at + (page * page_bytes + ((y0 + b * 16) & in_page) * ROW_BYTES);
 #pragma unroll
-                for (int i = 0; i < K_LOADS; ++i) {
-                    rk[b][i] = *(const KPiece *)(k_at + at + off + i * 64);
-                    if constexpr (BITS == 4) ek[b][i] = (ke_at + at / 16)[(off + i * 64) / 16];
-                }
+                for (int i = 0; i < K_LOADS; ++i) rk[b][i] = *(const uint4 *)(at + off + i * 64);
             } else {
                 const int key = b * 16 + col, page = __shfl(pages, key);
-                const int64_t at = page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES + quad * K_BYTES;
+                const char *at = k_at + (page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES + quad * 16);
 #pragma unroll
                 for (int i = 0; i < K_LOADS; ++i) {
-                    rk[b][i] = KPiece{};
-                    if (page >= 0) rk[b][i] = *(const KPiece *)(k_at + at + i * 64);
-                    if constexpr (BITS == 4) {
-                        ek[b][i] = 0;
-                        if (page >= 0) ek[b][i] = ke_at[(at + i * 64) / 16];
-                    }
+                    rk[b][i] = make_uint4(0, 0, 0, 0);
+                    if (page >= 0) rk[b][i] = *(const uint4 *)(at + i * 64);
                 }
             }
         }
@@ -756,18 +750,12 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4
         for (int i = 0; i < V_LOADS; ++i) {
             if (whole) {
                 const int key = i * 64 / PER_ROW, page = __builtin_amdgcn_readlane(pages, key);
-                const int64_t at = page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES;
-                rv[i] = *(const VPiece *)(v_at + at + lane * V_BYTES);
-                if constexpr (BITS == 4) ev[i] = (ve_at + at / 16)[lane * V_BYTES / 16];
+                const char *at = v_at + (page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES);
+                rv[i] = *(const uint4 *)(at + lane * 16);
             } else {
                 const int key = (i * 64 + lane) / PER_ROW, page = __shfl(pages, key);
-                const int64_t at = page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES + lane % PER_ROW * V_BYTES;
-                rv[i] = VPiece{};
-                if (page >= 0) rv[i] = *(const VPiece *)(v_at + at);
-                if constexpr (BITS == 4) {
-                    ev[i] = 0;
-                    if (page >= 0) ev[i] = ve_at[at / 16];
-                }
+                rv[i] = make_uint4(0, 0, 0, 0);
+                if (page >= 0) rv[i] = *(const uint4 *)(v_at + (page * page_bytes + ((y0 + key) & in_page) * ROW_BYTES + lane % PER_ROW * 16));
             }
         }
     };
@@ -777,63 +765,11 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4
     float m[COLS], l[COLS];
 #pragma unroll
     for (int w = 0; w < COLS; ++w) { m[w] = NEG_INF; l[w] = 0.0f; }
-    int pages = page_of(tile0 + wave), next = page_of(tile0 + wave + 4);
-    pages = in_pool(kv, pages);
-    uint32_t there = (uint32_t)__builtin_amdgcn_ballot_w64(pages >= 0);
-    if (tile0 + wave < tile1) {
-        const bool whole = PAGE16 && there == 0xffffffffu;
-        fetch_k(tile0 + wave, pages, whole);
-        fetch_v(tile0 + wave, pages, whole);
-    }
-    for (int tile = tile0 + wave; tile < tile1; tile += 4) {
-        const uint32_t now = there;
-        const int y0 = start_of(tile);
-        pages = in_pool(kv, next);
-        there = (uint32_t)__builtin_amdgcn_ballot_w64(pages >= 0);
-        const bool whole = PAGE16 && there == 0xffffffffu, more = tile + 4 < tile1;
-        next = page_of(tile + 8);
-        f32x4 s[COLS][2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            f32x4 acc[COLS] = {};
-#pragma unroll
-            for (int i = 0; i < K_LOADS; ++i) {
-#pragma unroll
-                for (int j = 0; j < Keys::EACH; ++j) {
-                    const X8 k = Keys::template operand<E>(rk[b][i], BITS == 4 ? ek[b][i] : 0, j);
-#pragma unroll
-                    for (int w = 0; w < COLS; ++w) acc[w] = mfma16(k, qf[w][Keys::EACH * i + j], acc[w]);
-                }
-            }
-#pragma unroll
-            for (int w = 0; w < COLS; ++w) s[w][b] = acc[w];
-        }
-        if (more) fetch_k(tile + 4, pages, whole);
-#pragma unroll
-        for (int i = 0; i < V_LOADS; ++i) {
-            const int key = (i * 64 + lane) / PER_ROW, part = lane % PER_ROW;
-            if constexpr (BITS == 4) {
-                const float unit = power_of(ev[i]);
-                const uint32_t *vv = (const uint32_t *)&rv[i];
-#pragma unroll
-                for (int j = 0; j < V_BYTES / 4; ++j) {
-                    union { X2 x[4]; uint4 u; } w;
-                    widen4(vv[j], unit, w.x);
-                    sv[few_v_piece<CH>(key, V_BYTES / 4 * part + j)] = w.u;
-                }
-            } else if constexpr (BITS == 8) {
-                union { X2 x[8]; uint4 u[2]; } w;
-                const uint32_t vv[4] = {rv[i].x, rv[i].y, rv[i].z, rv[i].w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) widen(vv[j], w.x[2 * j], w.x[2 * j + 1]);
-                sv[few_v_piece<CH>(key, 2 * part)] = w.u[0]; sv[few_v_piece<CH>(key, 2 * part + 1)] = w.u[1];
-            } else sv[few_v_piece<CH>(key, part)] = rv[i];
-        }
-        if (more) fetch_v(tile + 4, pages, whole);
-        // a lane's register i of block b is the score of key y0 + 16 b + 4 quad + i
+    // a lane's register i of block b is the score of key y0 + 16 b + 4 quad + i; `now`: which keys of the tile are there
+    union Weights { X8 x8; X2 x2[4]; };
+    auto weigh = [&](f32x4 (&s)[COLS][2], uint32_t now, int y0, Weights (&p)[COLS], Weights (&rest)[COLS]) {
         const bool all = now == 0xffffffffu && (tree ? y0 + 31 < base : y0 + 31 <= base) &&
                          (a.window <= 0 || y0 + 31 < a.n_sink || all_last - y0 < a.window);
-        union { X8 x8; X2 x2[4]; } p[COLS], rest[COLS];
 #pragma unroll
         for (int w = 0; w < COLS; ++w) {
             if (!all) {
@@ -847,9 +783,10 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4
             }
             float top = fmaxf(fmaxf(fmaxf(s[w][0][0], s[w][0][1]), fmaxf(s[w][0][2], s[w][0][3])),
                               fmaxf(fmaxf(s[w][1][0], s[w][1][1]), fmaxf(s[w][1][2], s[w][1][3])));
-            top = fmaxf(top, lane_16_away(top));
-            top = fmaxf(top, other_half(top)) * c;
-            if (__builtin_amdgcn_ballot_w64(top > m[w] + (MAX_SLACK + LIFT<E>))) {
+            // (the other lanes' scores of the same row are looked at only where some score is far above the maximum)
+            if (__builtin_amdgcn_ballot_w64(top * c > m[w] + (MAX_SLACK + LIFT<E>))) {
+                top = fmaxf(top, lane_16_away(top));
+                top = fmaxf(top, other_half(top)) * c;
                 const float m_new = fmaxf(m[w], top - LIFT<E>);
                 const float shrink = __builtin_amdgcn_exp2f(m[w] - (m_new == NEG_INF ? 0.0f : m_new));
                 m[w] = m_new;
@@ -863,28 +800,231 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? 4
                 const float w0 = __builtin_amdgcn_exp2f(fmaf(s[w][i / 2][2 * (i & 1)], c, -m_use)), w1 = __builtin_amdgcn_exp2f(fmaf(s[w][i / 2][2 * (i & 1) + 1], c, -m_use));
                 p[w].x2[i][0] = (E)w0;
                 p[w].x2[i][1] = (E)w1;
-                rest[w].x2[i][0] = (E)(w0 - (float)p[w].x2[i][0]);
-                rest[w].x2[i][1] = (E)(w1 - (float)p[w].x2[i][1]);
+                float r0, r1;
+                if constexpr (std::is_same_v<E, __bf16>) {
+                    const uint32_t both = __builtin_bit_cast(uint32_t, p[w].x2[i]);
+                    r0 = w0 - __uint_as_float(both << 16);
+                    r1 = w1 - __uint_as_float(both & 0xffff0000u);
+                } else {
+                    r0 = w0 - (float)p[w].x2[i][0];
+                    r1 = w1 - (float)p[w].x2[i][1];
+                }
+                rest[w].x2[i][0] = (E)r0;
+                rest[w].x2[i][1] = (E)r1;
                 l[w] += w0 + w1;
             }
         }
-        // the values were written by other lanes of this wavefront: LDS works in order, the compiler has to as well
+    };
+    // the values were written by other lanes of this wavefront: LDS works in order, the compiler has to as well
+    auto in_order = [] {
         __builtin_amdgcn_wave_barrier();
         asm volatile("" ::: "memory");
+    };
+    // dims 16 x .. of the tile's values, keys in the weights' order
+    auto values = [&](int x) {
+        const int key = 4 * quad + (col >> 2), piece = x * 2 + ((col & 3) >> 1);
+        using LdsPtr = __attribute__((address_space(3))) i16x4 *;
+        const char *at0 = (const char *)(sv + (BITS == 4 ? four_v_piece<CH>(key, piece) : few_v_piece<CH>(key, piece))) + (col & 1) * 8;
+        const char *at1 = at0 + 16 * CH * 16;
+        union { i16x4 h[2]; X8 x; } vf;
+        vf.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at0);
+        vf.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at1);
+        return vf.x;
+    };
+    if constexpr (BITS == 4) {
+        // A tile of 4 bits is a quarter of the bytes of one of 16: two are under way, and their pages are looked up a tile earlier still.  Every
+        // tile asks for the same number of loads, of the pool's first page where there is none, so that what is waited for is known by count (with
+        // loads that depend on a page's being there all of them were waited for at every tile, the next pages' too).  128 sequences over some 4000 tokens,
+        // 32 heads of 128: 175 us, 4.0 TB/s (219 with the loop for 16 bits); two wavefronts a SIMD that keep a tile's values in registers took
+        // less than three with an eighth to a half of them (181 to 194).
+        struct Ahead {
+            KPiece k[2][K_LOADS];
+            VPiece v[V_LOADS];
+            uint32_t ke[2][K_LOADS], ve[V_LOADS];
+            uint32_t there;
+        };
+        struct Looked {
+            int page;
+            bool any;
+        };
+        const uint32_t page_16 = (uint32_t)(page_bytes / 16);
+        auto look = [&](int tile) {
+            const int y = start_of(tile) + (lane & 31);
+            const bool any = tile < tile1 && y < ex.hi && (y >= ex.lo || y < a.n_sink);
+            return Looked{sq.table[any ? y >> kv.shift : 0], any};
+        };
+        auto ask = [&](Ahead &r, int tile, Looked looked) {
+            const int page = in_pool(kv, looked.any ? looked.page : -1), y0 = start_of(tile);
+            r.there = (uint32_t)__builtin_amdgcn_ballot_w64(page >= 0);
+            if constexpr (PAGE16) {
+                // in 16 bytes: a data piece, and its scale's place
+                uint64_t at[2];
 #pragma unroll
-        for (int x = 0; x < D / 16; ++x) {
-            const int key = 4 * quad + (col >> 2), piece = x * 2 + ((col & 3) >> 1);
-            using LdsPtr = __attribute__((address_space(3))) i16x4 *;
-            const char *at0 = (const char *)(sv + few_v_piece<CH>(key, piece)) + (col & 1) * 8;
-            const char *at1 = at0 + 16 * CH * 16;
-            union { i16x4 h[2]; X8 x; } vf;
-            vf.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at0);
-            vf.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)at1);
+                for (int b = 0; b < 2; ++b) {
+                    // (of these keys the first may lie before a window)
+                    const uint32_t some = r.there >> (b * 16) & 0xffffu;
+                    const int p = __builtin_amdgcn_readlane(page, b * 16 + __builtin_ctz(some | 0x10000u) % 16);
+                    at[b] = (uint64_t)(uint32_t)(p < 0 ? 0 : p) * page_16 + (uint32_t)(((y0 + b * 16) & in_page) * (ROW_BYTES / 16));
+                }
 #pragma unroll
-            for (int w = 0; w < COLS; ++w) o[w][x] = mfma16(vf.x, rest[w].x8, mfma16(vf.x, p[w].x8, o[w][x]));
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < K_LOADS; ++i) {
+                        const int off = col * ROW_BYTES + quad * K_BYTES + i * 64;
+                        r.k[b][i] = *(const KPiece *)(k_at + at[b] * 16 + off);
+                        r.ke[b][i] = (ke_at + at[b])[off / 16];
+                    }
+#pragma unroll
+                for (int i = 0; i < V_LOADS; ++i) {
+                    constexpr int HALF = 16 * PER_ROW / 64;              // loads of 16 keys
+                    const int off = (i % HALF) * 64 * V_BYTES + lane * V_BYTES;
+                    r.v[i] = *(const VPiece *)(v_at + at[i / HALF] * 16 + off);
+                    r.ve[i] = (ve_at + at[i / HALF])[off / 16];
+                }
+            } else {
+                auto place = [&](int key) {
+                    const int p = __shfl(page, key);
+                    return (p < 0 ? 0 : p) * page_bytes + ((y0 + key) & in_page) * ROW_BYTES;
+                };
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const int64_t at = place(b * 16 + col) + quad * K_BYTES;
+#pragma unroll
+                    for (int i = 0; i < K_LOADS; ++i) {
+                        r.k[b][i] = *(const KPiece *)(k_at + at + i * 64);
+                        r.ke[b][i] = ke_at[(at + i * 64) / 16];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < V_LOADS; ++i) {
+                    const int64_t at = place((i * 64 + lane) / PER_ROW) + lane % PER_ROW * V_BYTES;
+                    r.v[i] = *(const VPiece *)(v_at + at);
+                    r.ve[i] = ve_at[at / 16];
+                }
+            }
+        };
+        Looked next;
+        auto step = [&](Ahead &r, int tile) {
+            if (tile >= tile1) return;
+            const uint32_t now = r.there;
+            if (now != 0xffffffffu) {
+                // what is not there may be NaN by its scale, which 0 makes a number
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < K_LOADS; ++i) r.ke[b][i] = (now >> (b * 16 + col)) & 1 ? r.ke[b][i] : 0;
+#pragma unroll
+                for (int i = 0; i < V_LOADS; ++i) r.ve[i] = (now >> ((i * 64 + lane) / PER_ROW)) & 1 ? r.ve[i] : 0;
+            }
+            f32x4 s[COLS][2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                for (int w = 0; w < COLS; ++w) s[w][b] = f32x4{};
+#pragma unroll
+                for (int i = 0; i < K_LOADS; ++i)
+#pragma unroll
+                    for (int j = 0; j < Keys::EACH; ++j) {
+                        const X8 k = Keys::template operand<E>(r.k[b][i], r.ke[b][i], j);
+#pragma unroll
+                        for (int w = 0; w < COLS; ++w) s[w][b] = mfma16(k, qf[w][Keys::EACH * i + j], s[w][b]);
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < V_LOADS; ++i) {
+                const int key = (i * 64 + lane) / PER_ROW, part = lane % PER_ROW;
+                const float unit = power_of(r.ve[i]);
+                struct Words { uint32_t w[V_BYTES / 4]; } v = __builtin_bit_cast(Words, r.v[i]);
+#pragma unroll
+                for (int j = 0; j < V_BYTES / 4; ++j) {
+                    union { X2 x[4]; uint4 u; } w;
+                    widen4(v.w[j], unit, w.x);
+                    sv[four_v_piece<CH>(key, V_BYTES / 4 * part + j)] = w.u;
+                }
+            }
+            const Looked then = look(tile + 12);
+            ask(r, tile + 8, next);
+            next = then;
+            in_order();
+            // the values are on their way from LDS while the weights are worked out
+            X8 vf[D / 16];
+#pragma unroll
+            for (int x = 0; x < D / 16; ++x) vf[x] = values(x);
+            Weights p[COLS], rest[COLS];
+            weigh(s, now, start_of(tile), p, rest);
+#pragma unroll
+            for (int x = 0; x < D / 16; ++x)
+#pragma unroll
+                for (int w = 0; w < COLS; ++w) o[w][x] = mfma16(vf[x], rest[w].x8, mfma16(vf[x], p[w].x8, o[w][x]));
+            in_order();
+        };
+        Ahead r0, r1;
+        {
+            const Looked l0 = look(tile0 + wave), l1 = look(tile0 + wave + 4);
+            next = look(tile0 + wave + 8);
+            ask(r0, tile0 + wave, l0);
+            ask(r1, tile0 + wave + 4, l1);
         }
-        __builtin_amdgcn_wave_barrier();
-        asm volatile("" ::: "memory");
+        for (int tile = tile0 + wave; tile < tile1; tile += 8) {
+            step(r0, tile);
+            step(r1, tile + 4);
+        }
+    } else {
+        int pages = page_of(tile0 + wave), next = page_of(tile0 + wave + 4);
+        pages = in_pool(kv, pages);
+        uint32_t there = (uint32_t)__builtin_amdgcn_ballot_w64(pages >= 0);
+        if (tile0 + wave < tile1) {
+            const bool whole = PAGE16 && there == 0xffffffffu;
+            fetch_k(tile0 + wave, pages, whole);
+            fetch_v(tile0 + wave, pages, whole);
+        }
+        for (int tile = tile0 + wave; tile < tile1; tile += 4) {
+            const uint32_t now = there;
+            const int y0 = start_of(tile);
+            pages = in_pool(kv, next);
+            there = (uint32_t)__builtin_amdgcn_ballot_w64(pages >= 0);
+            const bool whole = PAGE16 && there == 0xffffffffu, more = tile + 4 < tile1;
+            next = page_of(tile + 8);
+            f32x4 s[COLS][2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                f32x4 acc[COLS] = {};
+#pragma unroll
+                for (int i = 0; i < K_LOADS; ++i) {
+#pragma unroll
+                    for (int j = 0; j < Keys::EACH; ++j) {
+                        const X8 k = Keys::template operand<E>(rk[b][i], 0, j);
+#pragma unroll
+                        for (int w = 0; w < COLS; ++w) acc[w] = mfma16(k, qf[w][Keys::EACH * i + j], acc[w]);
+                    }
+                }
+#pragma unroll
+                for (int w = 0; w < COLS; ++w) s[w][b] = acc[w];
+            }
+            if (more) fetch_k(tile + 4, pages, whole);
+#pragma unroll
+            for (int i = 0; i < V_LOADS; ++i) {
+                const int key = (i * 64 + lane) / PER_ROW, part = lane % PER_ROW;
+                if constexpr (BITS == 8) {
+                    union { X2 x[8]; uint4 u[2]; } w;
+                    const uint32_t vv[4] = {rv[i].x, rv[i].y, rv[i].z, rv[i].w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) widen(vv[j], w.x[2 * j], w.x[2 * j + 1]);
+                    sv[few_v_piece<CH>(key, 2 * part)] = w.u[0]; sv[few_v_piece<CH>(key, 2 * part + 1)] = w.u[1];
+                } else sv[few_v_piece<CH>(key, part)] = rv[i];
+            }
+            if (more) fetch_v(tile + 4, pages, whole);
+            Weights p[COLS], rest[COLS];
+            weigh(s, now, y0, p, rest);
+            in_order();
+#pragma unroll
+            for (int x = 0; x < D / 16; ++x) {
+                const X8 vf = values(x);
+#pragma unroll
+                for (int w = 0; w < COLS; ++w) o[w][x] = mfma16(vf, rest[w].x8, mfma16(vf, p[w].x8, o[w][x]));
+            }
+            in_order();
+        }
     }
     // sums that are not finite, as above
     bool odd = any_odd<D / 16>(o[0]);
