@@ -616,13 +616,6 @@ __global__ __launch_bounds__(AT_THREADS) void hx_attend_join_kernel(AttendArgs a
 
 // ---- few rows ----------------------------------------------------------------
 
-// value of the lane 16 away
-__device__ __forceinline__ float lane_16_away(float x)
-{
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(threadIdx.x & 16 ? r[0] : r[1]);
-}
-
 template <int CH> __device__ __forceinline__ int few_v_piece(int r, int c) { return r * CH + (c ^ (CH >= 16 ? (r & 7) << 1 : ((r >> 1) & 3) << 1)); }
 
 // As that, for values of 4 bits, of which a lane writes 2 or 4 pieces beside each other: 8 lanes' fall in different banks.

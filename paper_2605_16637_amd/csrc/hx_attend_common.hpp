@@ -135,6 +135,13 @@ __device__ __forceinline__ float other_half(float x)
     return __uint_as_float(threadIdx.x & 32 ? r[0] : r[1]);
 }
 
+// value of the lane 16 away
+__device__ __forceinline__ float lane_16_away(float x)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(threadIdx.x & 16 ? r[0] : r[1]);
+}
+
 // A sequence and its queries.
 struct Seq {
     int q0, nq, len, base;       // base: the position of the first query's token

@@ -5,7 +5,7 @@
 
 namespace {
 
-constexpr int TOP_THREADS = 256;
+constexpr int TOP_THREADS = 256, TOP_WAVES = TOP_THREADS / 64;
 constexpr int64_t TOP_SCORES = (int64_t)1 << 28;         // bytes of scores at once
 
 struct TopArgs {
@@ -13,11 +13,13 @@ struct TopArgs {
     const void *bounds;              // of the layer
     int first_query, n_queries;      // of this part of the call
     int n_pages, n_first, n_last;
-    int stride;                      // entries of a row
-    double *score;                   // [query][KV head][stride], NULL where no row has more than n_pages entries
+    int stride;                      // entries of a row, up to a multiple of 16; 0 where no row has more than n_pages entries
+    float *score;                    // [query][KV head][stride]
+    float *off;                      // [query][KV head][stride / 16] what a score of these 16 pages may be off by
+    double *exact;                   // [query][KV head][stride] of those pages for which that matters
     int32_t *picked, *picked_len;    // what hx_attend's kernels read
     int32_t *chosen;                 // of the call's first query, or NULL
-    int chunks;                      // workgroups that look at the pages of one query and KV head
+    int q_tiles, chunks;             // of a sequence; workgroups that look at the pages of a tile of queries and a KV head
 };
 
 // A query's row: its pages up to its own, `own`.
@@ -44,6 +46,138 @@ __device__ __forceinline__ Place place(const AttendArgs &a, int j)
 
 // ---- what a page can score ---------------------------------------------------
 
+constexpr float INF = __builtin_inff();
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+// bounds as numbers of the queries' type; those of 8 and 4 bits are bf16, and fp16 exactly
+template <typename Q, typename E>
+__device__ __forceinline__ typename Types<Q>::x8 as_query(typename Types<E>::x8 x)
+{
+    if constexpr (std::is_same_v<Q, E>) return x;
+    else {
+        typename Types<Q>::x8 y;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = (Q)(float)x[i];
+        return y;
+    }
+}
+
+// What pages can score, by the matrix units: a query's numbers that are not below 0 times the upper bounds, and the others times the lower ones.  Products
+// of 16-bit numbers are exact and their sums are held in 32 bits, so a score is off by at most 2 D 2^-23 of the sum of its terms' sizes, which |q|
+// times the larger bound's size sums to: where that could change which pages are chosen, they are scored again in 64 bits.
+//
+// ONE: a single query a sequence, whose heads are the columns; else 16 queries beside each other are, and the heads follow each other.  A wavefront has 16
+// pages at once and asks for the next 16.
+template <typename Q, typename E, int D, bool ONE>
+__global__ __launch_bounds__(TOP_THREADS) void hx_top_score_kernel(TopArgs t)
+{
+    using Q8 = typename Types<Q>::x8;
+    using E8 = typename Types<E>::x8;
+    constexpr int PARTS = D / 32;
+    const AttendArgs &a = t.a;
+    const KvView &kv = a.kv;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = lane >> 4, col = lane & 15;
+    const int pairs = a.n * kv.n_heads, pair = blockIdx.x % pairs, rest = blockIdx.x / pairs, head = pair % kv.n_heads;
+    const int qt = rest % t.q_tiles, part = rest / t.q_tiles;
+    const Seq sq = sequence(a, pair);
+    if (!sq.ok) return;
+    // the tile's queries that are of this part of the call
+    int t0 = ONE ? qt : qt * 16, t1 = ONE ? qt + 1 : qt * 16 + 16;
+    t1 = t1 < sq.nq ? t1 : sq.nq;
+    const int from = t.first_query - sq.q0, until = from + t.n_queries;
+    if (t0 >= t1 || t1 <= from || t0 >= until) return;
+    const int last_seen = t1 <= until ? t1 - 1 : until - 1, own = (sq.base + last_seen) >> kv.shift, last = own - t.n_last;
+    if (own < t.n_pages) return;                                  // (no more pages than they may see)
+    const int mine = ONE ? t0 : t0 + col;                         // this column's query
+    const bool real = mine >= from && mine < until && mine < sq.nq;
+    const int64_t line = real ? (int64_t)(mine - from) * kv.n_heads + head : 0;
+    const int rounds = ONE ? (a.group + 15) / 16 : a.group;
+    constexpr float UNIT = 2.0f * D * 1.1920929e-07f * 1.02f;
+
+    const int steps = (last + 16) / 16 - t.n_first / 16;          // 16 pages each, from the one with the first that is not seen in any case
+    const int stride = t.chunks * TOP_WAVES;
+    auto look = [&](int step) {
+        const int b = (t.n_first / 16 + step) * 16 + col;
+        return step < steps && b <= last && b >= t.n_first ? sq.table[b] : -1;
+    };
+    E8 lo[PARTS], hi[PARTS];
+    unsigned here = 0;                                            // which of the 16 pages are there
+    auto fetch = [&](int page) {
+        page = in_pool(kv, page);
+        here = (unsigned)__builtin_amdgcn_ballot_w64(page >= 0) & 0xffffu;
+        const E *at = (const E *)t.bounds + ((int64_t)(page < 0 ? 0 : page) * kv.n_heads + head) * (2 * D) + quad * 8;
+#pragma unroll
+        for (int s = 0; s < PARTS; ++s) { lo[s] = *(const E8 *)(at + s * 32); hi[s] = *(const E8 *)(at + D + s * 32); }
+    };
+    int step = part * TOP_WAVES + wave;
+    if (step >= steps) return;
+    int next = look(step + stride);
+    fetch(look(step));
+    for (; step < steps; step += stride) {
+        const unsigned now = here;
+        Q8 l[PARTS], h[PARTS];
+        s16x8 m[PARTS];
+#pragma unroll
+        for (int s = 0; s < PARTS; ++s) {
+            l[s] = as_query<Q, E>(lo[s]);
+            h[s] = as_query<Q, E>(hi[s]);
+            const s16x8 x = __builtin_bit_cast(s16x8, l[s]) & (short)0x7fff, y = __builtin_bit_cast(s16x8, h[s]) & (short)0x7fff;
+            m[s] = __builtin_elementwise_max(x, y);
+        }
+        if (step + stride < steps) {
+            fetch(next);
+            next = look(step + 2 * stride);
+        }
+        float best[4] = {-INF, -INF, -INF, -INF}, off = 0.0f;
+        for (int r = 0; r < rounds; ++r) {
+            const int g = ONE ? r * 16 + col : r;
+            const bool in = real && g < a.group;
+            const Q *q = (const Q *)a.q + (int64_t)(sq.q0 + (in ? mine : t0)) * a.q_token + (int64_t)(head * a.group + (in ? g : 0)) * a.q_head + quad * 8;
+            f32x4 acc = {}, size = {};
+#pragma unroll
+            for (int s = 0; s < PARTS; ++s) {
+                Q8 x = {};
+                if (in) {
+                    if (a.q_wide) x = *(const Q8 *)(q + s * 32);
+                    else
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) x[i] = q[s * 32 + i];
+                }
+                s16x8 bits = __builtin_bit_cast(s16x8, x);
+                if (a.scale < 0) bits ^= (short)0x8000;
+                const s16x8 under = bits >> 15;                   // all bits set where it is below 0 (or -0, times anything)
+                acc = mfma16(h[s], __builtin_bit_cast(Q8, (s16x8)(bits & ~under)), acc);
+                acc = mfma16(l[s], __builtin_bit_cast(Q8, (s16x8)(bits & under)), acc);
+                size = mfma16(__builtin_bit_cast(Q8, m[s]), __builtin_bit_cast(Q8, (s16x8)(bits & (short)0x7fff)), size);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (!in || !((now >> (quad * 4 + i)) & 1)) continue;
+                best[i] = fmaxf(best[i], acc[i]);
+                // (an infinity or NaN in a score makes it worth nothing)
+                const float by = __builtin_fabsf(acc[i]) < INF ? size[i] : INF;
+                off = by < off ? off : by == by ? by : INF;
+            }
+        }
+        if constexpr (ONE)
+#pragma unroll
+            for (int d = 1; d < 16; d <<= 1) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) best[i] = fmaxf(best[i], __shfl_xor(best[i], d));
+                off = fmaxf(off, __shfl_xor(off, d));
+            }
+        off = fmaxf(off, lane_16_away(off));
+        off = fmaxf(off, other_half(off));
+        const int block = t.n_first / 16 + step;
+        if (real && (!ONE || col == 0)) {
+            *(float4 *)(t.score + line * t.stride + block * 16 + quad * 4) = make_float4(best[0], best[1], best[2], best[3]);
+            if (quad == 0) t.off[line * (t.stride / 16) + block] = off * UNIT + 1e-37f;
+        }
+    }
+}
+
+// ---- the pages of the largest ------------------------------------------------
+
 __device__ __forceinline__ double across(double x, int d)
 {
     const uint64_t v = __builtin_bit_cast(uint64_t, x);
@@ -51,124 +185,53 @@ __device__ __forceinline__ double across(double x, int d)
     return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 
-// Four heads' sums over LANES lanes, and the largest: half of the heads is given away for each of the first two steps.  Heads from `heads` on have
-// none.  *odd: whether any of them is NaN.
-template <int LANES>
-__device__ __forceinline__ double largest_sum(const double *v, int sub, int heads, bool *odd)
-{
-    const bool up = sub & (LANES / 2), up2 = sub & (LANES / 4);
-    double x0 = up ? v[2] : v[0], x1 = up ? v[3] : v[1];
-    x0 += across(up ? v[0] : v[2], LANES / 2);
-    x1 += across(up ? v[1] : v[3], LANES / 2);
-    double x = (up2 ? x1 : x0) + across(up2 ? x0 : x1, LANES / 4);
-#pragma unroll
-    for (int d = LANES / 8; d > 0; d >>= 1) x += across(x, d);
-    if ((up ? 2 : 0) + (up2 ? 1 : 0) >= heads) x = -__builtin_inf();
-    *odd = x != x;
-    x = fmax(x, across(x, LANES / 4));
-    return fmax(x, across(x, LANES / 2));
-}
-
-// Bounds of E, queries of Q.  A page's bounds lie over D / 8 lanes, 8 places each.  A product of two 16-bit numbers is exact in 64 bits, and the sums are off by some 2^-50 of
-// their terms: which of two pages comes first does not go by how they are added, but for differences below that.
+// A page's score in 64 bits by D / 8 lanes beside each other, of which each has 8 places: the same products, whose sums are off by some 2^-50 of their terms.
 template <typename Q, typename E, int D>
-__global__ __launch_bounds__(TOP_THREADS) void hx_top_score_kernel(TopArgs t)
+__device__ __forceinline__ double exact_score(const TopArgs &t, int j, int head, int page, int sub)
 {
-    using Q8 = typename Types<Q>::x8;
     using E8 = typename Types<E>::x8;
-    constexpr int LANES = D / 8, PER = 64 / LANES, STEPS = 4, WAVES = TOP_THREADS / 64;      // pages a wavefront has at once, how many times
     const AttendArgs &a = t.a;
-    const KvView &kv = a.kv;
-    const int pairs = t.n_queries * kv.n_heads, pair = blockIdx.x % pairs, head = pair % kv.n_heads, j = t.first_query + pair / kv.n_heads;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane % LANES, slot = lane / LANES;
-    const Place p = place(a, j);
-    if (!p.ok || p.own < t.n_pages) return;                       // (no more pages than it may see)
-    const int last = p.own - t.n_last;
-    for (int chunk = blockIdx.x / pairs;; chunk += t.chunks) {
-        const int b0 = t.n_first + (chunk * WAVES + wave) * (STEPS * PER) + slot;
-        if (t.n_first + chunk * WAVES * (STEPS * PER) > last) break;
-        E8 lo[STEPS], hi[STEPS];
-        int page[STEPS];
-        double best[STEPS];
+    const E *at = (const E *)t.bounds + ((int64_t)page * a.kv.n_heads + head) * (2 * D) + sub * 8;
+    const E8 lo = *(const E8 *)at, hi = *(const E8 *)(at + D);
+    double best = -__builtin_inf();
+#pragma unroll 1
+    for (int g = 0; g < a.group; ++g) {
+        const Q *q = (const Q *)a.q + (int64_t)j * a.q_token + (int64_t)(head * a.group + g) * a.q_head + sub * 8;
+        double v = 0;
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            const int b = b0 + s * PER;
-            page[s] = in_pool(kv, b <= last ? p.table[b] : -1);
-            const E *at = (const E *)t.bounds + ((int64_t)(page[s] < 0 ? 0 : page[s]) * kv.n_heads + head) * (2 * D) + sub * 8;
-            lo[s] = *(const E8 *)at;
-            hi[s] = *(const E8 *)(at + D);
-            best[s] = -__builtin_inf();
+        for (int i = 0; i < 8; ++i) {
+            const float x = a.scale < 0 ? -(float)q[i] : (float)q[i];
+            v = fma((double)x, (double)(float)(x < 0 ? lo[i] : hi[i]), v);
         }
-        for (int g0 = 0; g0 < a.group; g0 += 4) {
-            double above[4][8], below[4][8];                      // the query's numbers where they are not below 0, and where they are
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int qhead = head * a.group + (g0 + g < a.group ? g0 + g : g0);
-                const Q *q = (const Q *)a.q + (int64_t)j * a.q_token + (int64_t)qhead * a.q_head + sub * 8;
-                Q8 x;
-                if (a.q_wide) x = *(const Q8 *)q;
-                else
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = q[i];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const double y = a.scale < 0 ? -(double)(float)x[i] : (double)(float)x[i];
-                    above[g][i] = y >= 0 ? y : y < 0 ? 0.0 : y;
-                    below[g][i] = y < 0 ? y : 0.0;
-                }
-            }
-#pragma unroll
-            for (int s = 0; s < STEPS; ++s) {
-                double v[4] = {};
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const double l = (double)(float)lo[s][i], h = (double)(float)hi[s][i];
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) v[g] = fma(below[g][i], l, fma(above[g][i], h, v[g]));
-                }
-                bool odd;
-                double x = largest_sum<LANES>(v, sub, a.group - g0, &odd);
-                if (__builtin_amdgcn_ballot_w64(odd)) {
-                    // 0 times an infinite bound is NaN; the bound that does not count is left out then
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) v[g] = 0;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            const bool under = below[g][i] < 0;
-                            v[g] = fma(under ? below[g][i] : above[g][i], (double)(float)(under ? lo[s][i] : hi[s][i]), v[g]);
-                        }
-                    x = largest_sum<LANES>(v, sub, a.group - g0, &odd);
-                    // a bound that is NaN is taken for +infinity, whichever of the lanes has seen it
-                    const unsigned long long any = __builtin_amdgcn_ballot_w64(odd);
-                    const unsigned long long mine = LANES == 64 ? ~0ull : ((1ull << LANES) - 1) << (slot * LANES);
-                    if (any & mine) x = __builtin_inf();
-                }
-                best[s] = fmax(best[s], x);
-            }
-        }
-        if (sub == 0)
-#pragma unroll
-            for (int s = 0; s < STEPS; ++s) {
-                const int b = b0 + s * PER;
-                if (b <= last) t.score[(int64_t)pair * t.stride + b] = page[s] < 0 ? -__builtin_inf() : best[s];
-            }
+        for (int d = D / 16; d > 0; d >>= 1) v += across(v, d);
+        best = fmax(best, v == v ? v : __builtin_inf());          // a bound that is no number is taken for +infinity
     }
+    return best;
 }
 
-// ---- the pages of the largest ------------------------------------------------
-
-constexpr int PICK_WAVES = TOP_THREADS / 64;
-
-// A score's key, 0 where it is -infinity (-0 and 0 are the same number).
+// Keys of scores, 0 where they are -infinity (-0 and 0 are the same number).
 __device__ __forceinline__ uint64_t key_of(double x) { return x == -__builtin_inf() ? 0 : nth_key(x + 0.0); }
-
-// A workgroup a query and KV head.
-__global__ __launch_bounds__(TOP_THREADS) void hx_top_pick_kernel(TopArgs t)
+__device__ __forceinline__ uint32_t key_of(float x)
 {
-    __shared__ NthState<uint64_t, TOP_THREADS> s;
-    __shared__ int s_before[2][PICK_WAVES];
+    const int32_t v = __builtin_bit_cast(int32_t, x + 0.0f);
+    return x == -INF ? 0 : (uint32_t)(v ^ (v >> 31 | INT32_MIN));
+}
+__device__ __forceinline__ float of_key(uint32_t k)
+{
+    const int32_t v = (int32_t)k;
+    return __builtin_bit_cast(float, v < 0 ? v ^ INT32_MIN : ~v);
+}
+
+// A workgroup a query and KV head: of few pages a wavefront.
+template <typename Q, typename E, int D, int THREADS>
+__global__ __launch_bounds__(THREADS) void hx_top_pick_kernel(TopArgs t)
+{
+    constexpr int WAVES = THREADS / 64, CACHE = 4 * THREADS, LANES = D / 8, LIST = NTH_LIST;
+    __shared__ union { NthState<uint32_t, THREADS> near; NthState<uint64_t, THREADS> exact; } s;
+    __shared__ float s_score[CACHE];
+    __shared__ int s_list[LIST], s_n_list, s_count[2][WAVES];
+    __shared__ float s_off[WAVES];
     const AttendArgs &a = t.a;
     const KvView &kv = a.kv;
     const int pair = blockIdx.x, head = pair % kv.n_heads, j = t.first_query + pair / kv.n_heads;
@@ -179,55 +242,119 @@ __global__ __launch_bounds__(TOP_THREADS) void hx_top_pick_kernel(TopArgs t)
     if (!p.ok) {
         if (tid == 0) { hx_raise(kv.status, HX_ERR_INDEX); picked[0] = -1; t.picked_len[pair] = 1; }
         if (chosen)
-            for (int i = tid; i < t.n_pages; i += TOP_THREADS) chosen[i] = -1;
+            for (int i = tid; i < t.n_pages; i += THREADS) chosen[i] = -1;
         return;
     }
+    // how many threads say so
+    auto count = [&](bool x) {
+        const unsigned long long m = __builtin_amdgcn_ballot_w64(x);
+        if (lane == 0) s_count[0][wave] = __builtin_popcountll(m);
+        __syncthreads();
+        int all = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) all += s_count[0][w];
+        __syncthreads();
+        return all;
+    };
     const bool all = p.own < t.n_pages || kv.n_pages == 0;
     const int from = t.n_first, to = p.own - t.n_last + 1;         // the pages between those that are seen in any case
-    const double *score = t.score + (int64_t)pair * t.stride;
+    const float *score = t.score + (int64_t)pair * t.stride;
+    double *exact = t.exact + (int64_t)pair * t.stride;
+    const bool cached = to - from <= CACHE;
+    auto score_of = [&](int b) { return cached ? s_score[b - from] : score[b]; };
+    auto page_at = [&](int b) { const int page = p.table[b]; return page < kv.n_pages ? page : -1; };
+    // which of the pages between are taken
+    enum { NONE, LEFT, NEAR, EXACT, BLIND } how = NONE;            // none; all that are there; scores from `under` on; scores above `over`, and from
+    float over = INF, under = INF;                                 // `under` on the largest exact ones; all by their exact ones
     uint64_t edge = 0;
     int equals = 0;
-    if (!all) {
-        int want = t.n_pages;
-        int fixed = 0;
-        for (int i = tid; i < t.n_first + t.n_last; i += TOP_THREADS) {
-            const int page = p.table[i < t.n_first ? i : p.own - t.n_last + 1 + i - t.n_first];
-            fixed += page >= 0 && page < kv.n_pages;
+    auto unsure = [&](int b) { return how == BLIND ? page_at(b) >= 0 : score_of(b) <= over && score_of(b) >= under; };
+    int want = t.n_pages;
+    if (!all)
+        for (int i0 = 0; i0 < t.n_first + t.n_last; i0 += THREADS) {
+            const int i = i0 + tid;
+            want -= count(i < t.n_first + t.n_last && page_at(i < t.n_first ? i : to + i - t.n_first) >= 0);
         }
+    if (!all && want > 0) {
+        float off = 0.0f;
+        for (int i = from / 16 + tid; i <= (to - 1) / 16; i += THREADS) off = fmaxf(off, t.off[(int64_t)pair * (t.stride / 16) + i]);
+        if (cached)
+            for (int b = from + tid; b < to; b += THREADS) s_score[b - from] = score[b];
 #pragma unroll
-        for (int d = 32; d > 0; d >>= 1) fixed += __shfl_xor(fixed, d);
-        if (lane == 0) s_before[0][wave] = fixed;
+        for (int d = 32; d > 0; d >>= 1) off = fmaxf(off, __shfl_xor(off, d));
+        if (lane == 0) s_off[wave] = off;
+        if (tid == 0) s_n_list = 0;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < PICK_WAVES; ++w) want -= s_before[0][w];
-        __syncthreads();
-        if (want > 0) {
-            nth_largest([&](int b) { return key_of(score[b]); }, from, to, want, s);
-            edge = s.edge;
-            equals = s.equals;
-        } else edge = ~0ull;
+        for (int w = 0; w < WAVES; ++w) off = fmaxf(off, s_off[w]);
+        if (off < INF) {
+            nth_largest([&](int b) { return key_of(score_of(b)); }, from, to, want, s.near);
+            how = s.near.edge ? EXACT : LEFT;
+            const float near = of_key(s.near.edge);
+            over = near + 2.1f * off;
+            under = near - 2.1f * off;
+        } else how = BLIND;
+        int unsures = 0, sure = 0;
+        if (how != LEFT)
+            for (int b0 = from; b0 < to; b0 += THREADS) {
+                const int b = b0 + tid;
+                const bool u = b < to && unsure(b);
+                sure += count(b < to && how == EXACT && score_of(b) > over);
+                unsures += count(u);
+                if (u) {
+                    const int at = atomicAdd(&s_n_list, 1);
+                    if (at < LIST) s_list[at] = b;
+                }
+            }
+        if (how == EXACT && sure + unsures == want) how = NEAR;
+        if (how >= EXACT) {
+            __syncthreads();
+            const int groups = THREADS / LANES, sub = tid % LANES;
+            if (unsures <= LIST) {
+                for (int i0 = 0; i0 < unsures; i0 += groups) {
+                    const int i = i0 + tid / LANES, b = s_list[i < unsures ? i : 0];
+                    const double x = exact_score<Q, E, D>(t, j, head, page_at(b), sub);
+                    if (i < unsures && sub == 0) exact[b] = x;
+                }
+                __syncthreads();
+                nth_largest([&](int i) { return key_of(exact[s_list[i]]); }, 0, unsures, want - sure, s.exact);
+            } else {
+                for (int b0 = from; b0 < to; b0 += groups) {
+                    const int b = b0 + tid / LANES, page = b < to && unsure(b) ? page_at(b) : -1;
+                    const double x = exact_score<Q, E, D>(t, j, head, page < 0 ? 0 : page, sub);
+                    if (page >= 0 && sub == 0) exact[b] = x;
+                }
+                __syncthreads();
+                nth_largest([&](int b) { return unsure(b) ? key_of(exact[b]) : (uint64_t)0; }, from, to, want - sure, s.exact);
+            }
+            edge = s.exact.edge;
+            equals = s.exact.equals;
+        }
     }
     // the pages in rising order
     int n = 0, seen_equal = 0;
-    for (int b0 = 0; b0 <= p.own; b0 += TOP_THREADS) {
+    for (int b0 = 0; b0 <= p.own; b0 += THREADS) {
         const int b = b0 + tid;
         const int page = in_pool(kv, b <= p.own ? p.table[b] : -1);
-        const bool between = !all && b >= from && b < to;
-        const uint64_t x = between && page >= 0 ? key_of(score[b]) : 0;
-        const bool equal = x == edge && x > 0;
+        const bool between = !all && b >= from && b < to && page >= 0;
+        const bool told = between && how >= EXACT && unsure(b);
+        const float x = between && how != NONE ? score_of(b) : 0.0f;
+        const uint64_t k = told ? key_of(exact[b]) : 0;
+        const bool equal = k == edge && k > 0;
         const unsigned long long e = __builtin_amdgcn_ballot_w64(equal);
-        if (lane == 0) s_before[0][wave] = __builtin_popcountll(e);
+        if (lane == 0) s_count[0][wave] = __builtin_popcountll(e);
         __syncthreads();
         int rank = seen_equal + __builtin_popcountll(e & ((1ull << lane) - 1)), all_equal = 0;
 #pragma unroll
-        for (int w = 0; w < PICK_WAVES; ++w) { rank += w < wave ? s_before[0][w] : 0; all_equal += s_before[0][w]; }
-        const bool take = page >= 0 && (!between || x > edge || (equal && rank < equals));
+        for (int w = 0; w < WAVES; ++w) { rank += w < wave ? s_count[0][w] : 0; all_equal += s_count[0][w]; }
+        const bool best = told ? k > edge || (equal && rank < equals) : how == LEFT ? x > -INF : how == NEAR ? x >= under : how == EXACT && x > over;
+        const bool take = page >= 0 && (!between || best);
         const unsigned long long m = __builtin_amdgcn_ballot_w64(take);
-        if (lane == 0) s_before[1][wave] = __builtin_popcountll(m);
+        if (lane == 0) s_count[1][wave] = __builtin_popcountll(m);
         __syncthreads();
         int at = n + __builtin_popcountll(m & ((1ull << lane) - 1));
 #pragma unroll
-        for (int w = 0; w < PICK_WAVES; ++w) { at += w < wave ? s_before[1][w] : 0; n += s_before[1][w]; }
+        for (int w = 0; w < WAVES; ++w) { at += w < wave ? s_count[1][w] : 0; n += s_count[1][w]; }
         seen_equal += all_equal;
         if (take) {
             picked[at] = page;
@@ -238,7 +365,7 @@ __global__ __launch_bounds__(TOP_THREADS) void hx_top_pick_kernel(TopArgs t)
         __syncthreads();
     }
     if (chosen)
-        for (int i = n + tid; i < t.n_pages; i += TOP_THREADS) chosen[i] = -1;
+        for (int i = n + tid; i < t.n_pages; i += THREADS) chosen[i] = -1;
     const int own_page = p.table[p.own];
     if (tid == 0 && (own_page < 0 || own_page >= kv.n_pages)) {
         if (n == 0) picked[0] = -1;
@@ -246,12 +373,25 @@ __global__ __launch_bounds__(TOP_THREADS) void hx_top_pick_kernel(TopArgs t)
     }
 }
 
-template <typename Q, typename E>
-void score(const TopArgs &t, int64_t grid, hipStream_t stream)
+template <typename Q, typename E, int D>
+void score_and_pick(const TopArgs &t, int64_t score_grid, int pages, hipStream_t stream)
 {
-    if (t.a.kv.dim == 64) hx_top_score_kernel<Q, E, 64><<<(int)grid, TOP_THREADS, 0, stream>>>(t);
-    else if (t.a.kv.dim == 128) hx_top_score_kernel<Q, E, 128><<<(int)grid, TOP_THREADS, 0, stream>>>(t);
-    else hx_top_score_kernel<Q, E, 256><<<(int)grid, TOP_THREADS, 0, stream>>>(t);
+    const int pick_grid = t.n_queries * t.a.kv.n_heads;
+    if (score_grid > 0) {
+        if (t.a.max_q == 1) hx_top_score_kernel<Q, E, D, true><<<(int)score_grid, TOP_THREADS, 0, stream>>>(t);
+        else hx_top_score_kernel<Q, E, D, false><<<(int)score_grid, TOP_THREADS, 0, stream>>>(t);
+    }
+    if (pages <= 384) hx_top_pick_kernel<Q, E, D, 64><<<pick_grid, 64, 0, stream>>>(t);
+    else if (pages <= 1536) hx_top_pick_kernel<Q, E, D, 256><<<pick_grid, 256, 0, stream>>>(t);
+    else hx_top_pick_kernel<Q, E, D, 1024><<<pick_grid, 1024, 0, stream>>>(t);
+}
+
+template <typename Q, typename E>
+void by_dim(const TopArgs &t, int64_t score_grid, int pages, hipStream_t stream)
+{
+    if (t.a.kv.dim == 64) score_and_pick<Q, E, 64>(t, score_grid, pages, stream);
+    else if (t.a.kv.dim == 128) score_and_pick<Q, E, 128>(t, score_grid, pages, stream);
+    else score_and_pick<Q, E, 256>(t, score_grid, pages, stream);
 }
 
 }  // namespace
@@ -272,22 +412,30 @@ extern "C" int hx_attend_top(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer,
     HX_REQUIRE(ctx, top->n_pages <= HX_MAX_TOP, HX_ERR_SHAPE, "%d pages for a query, beyond %d", top->n_pages, HX_MAX_TOP);
     HX_REQUIRE(ctx, pool->bounds || kv.n_pages == 0, HX_ERR_INVALID_ARG, "a pool without bounds");
     if (!any) return HX_OK;
-    const int H = kv.n_heads, n_q = args->n_q;
-    // more pages than any row has are never chosen
-    const int n_pages = top->n_pages;
-    const int64_t stride = kv.max_pages > n_pages ? kv.max_pages : 0;
-    // so many queries at once that scores stay below TOP_SCORES, and launches within their limits
+    const int H = kv.n_heads, n_q = args->n_q, n_pages = top->n_pages;
     const HxAttend whole = hx_attend_view(ctx, pool, layer, kv, *args);
-    int64_t at_once = stride ? TOP_SCORES / (stride * H * (int64_t)sizeof(double)) : n_q;
-    const int64_t tiles = (whole.group + 127) / 128, fits = hx_most_groups(TOP_THREADS) / (H * tiles * 64);
+    // no row has more pages than entries: no scores where all of them are seen
+    const int64_t stride = kv.max_pages > n_pages && kv.n_pages > 0 ? ((int64_t)kv.max_pages + 15) / 16 * 16 : 0;
+    const size_t line = (size_t)stride * (sizeof(double) + sizeof(float)) + (size_t)(stride / 16) * sizeof(float);
+    // so many queries at once that scores stay below TOP_SCORES, and launches within their limits
+    int64_t at_once = stride ? TOP_SCORES / (int64_t)(line * H) : n_q;
+    const int64_t tiles = (whole.group + 127) / 128, fits = hx_most_groups(1024) / (H * tiles * 64);
     HX_REQUIRE(ctx, fits > 0, HX_ERR_SHAPE, "%d query heads", whole.n_heads);
     at_once = at_once < fits ? at_once : fits;
     at_once = at_once < 1 ? 1 : at_once < n_q ? at_once : n_q;
+    const int64_t q_tiles = (whole.max_q + 15) / 16, score_tiles = (int64_t)args->n * H * q_tiles;
+    HX_REQUIRE(ctx, score_tiles <= hx_most_groups(TOP_THREADS), HX_ERR_SHAPE, "%d sequences of %d queries", args->n, whole.max_q);
+    // Workgroups look at 64 pages at once, and again; as many of them for a tile of queries as there are pages for, up to 8 a CU in all.
+    int64_t about = ((int64_t)args->max_len >> kv.shift) + 1;
+    about = about < stride ? about : stride;
+    const int64_t useful = (about + 63) / 64, wanted = 8 * ctx->num_cu / score_tiles, most_chunks = hx_most_groups(TOP_THREADS) / score_tiles;
+    int64_t chunks = useful < wanted ? useful : wanted;
+    chunks = chunks < 1 ? 1 : chunks < most_chunks ? chunks : most_chunks;
     HxDeviceGuard guard(ctx->device);
     HX_REQUIRE(ctx, guard.ok, HX_ERR_DEVICE, "cannot select device %d", ctx->device);
     const hipStream_t stream = (hipStream_t)stream_;
     const int64_t pairs = at_once * H;
-    const size_t bytes = (size_t)pairs * (stride * sizeof(double) + ((size_t)n_pages + 1) * sizeof(int32_t));
+    const size_t bytes = (size_t)pairs * (line + ((size_t)n_pages + 1) * sizeof(int32_t));
     if (int rc = hx_scratch(ctx, hx_serve(ctx)->top, bytes, stream)) return rc;
     const int64_t seen = (int64_t)n_pages << kv.shift, most = args->max_len < seen ? args->max_len : seen;
     auto part_of = [&](int64_t j, int64_t n) {
@@ -312,26 +460,21 @@ extern "C" int hx_attend_top(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer,
     t.bounds = (const char *)pool->bounds + (int64_t)layer * kv.n_pages * hx_bounds_bytes(pool);
     t.n_pages = n_pages; t.n_first = top->n_first; t.n_last = top->n_last;
     t.stride = (int)stride;
-    t.score = (double *)hx_serve(ctx)->top.p;
-    t.picked = (int32_t *)(t.score + pairs * stride);
+    t.exact = (double *)hx_serve(ctx)->top.p;
+    t.score = (float *)(t.exact + pairs * stride);
+    t.off = t.score + pairs * stride;
+    t.picked = (int32_t *)(t.off + pairs * (stride / 16));
     t.picked_len = t.picked + pairs * n_pages;
     t.chosen = top->chosen;
-    const int per = TOP_THREADS / (kv.dim / 8) * 4;                 // pages that a workgroup looks at at once
-    const int64_t about = ((int64_t)args->max_len >> kv.shift) + 1, chunks = ((about < stride ? about : stride) + per - 1) / per;
-    t.chunks = (int)(chunks < 1 ? 1 : chunks < 64 ? chunks : 64);
+    t.q_tiles = (int)q_tiles;
+    t.chunks = (int)chunks;
     for (int64_t j = 0; j < n_q; j += at_once) {
         t.first_query = (int)j;
         t.n_queries = (int)(n_q - j < at_once ? n_q - j : at_once);
-        const int64_t now = (int64_t)t.n_queries * H;
-        if (stride && kv.n_pages > 0) {
-            const int64_t grid = now * t.chunks;
-            const bool bf16 = args->dtype == HX_BF16;
-            if (bf16) score<__bf16, __bf16>(t, grid, stream);
-            else if (pool->dtype == HX_F16) score<_Float16, _Float16>(t, grid, stream);
-            else score<_Float16, __bf16>(t, grid, stream);
-            if (int rc = hx_check_launch(ctx, "hx_top_score_kernel")) return rc;
-        }
-        hx_top_pick_kernel<<<(int)now, TOP_THREADS, 0, stream>>>(t);
+        const int64_t grid = stride ? score_tiles * chunks : 0;
+        if (args->dtype == HX_BF16) by_dim<__bf16, __bf16>(t, grid, (int)about, stream);
+        else if (pool->dtype == HX_F16) by_dim<_Float16, _Float16>(t, grid, (int)about, stream);
+        else by_dim<_Float16, __bf16>(t, grid, (int)about, stream);
         if (int rc = hx_check_launch(ctx, "hx_top_pick_kernel")) return rc;
         HxAttend a = part_of(j, t.n_queries);
         a.picked = t.picked; a.picked_len = t.picked_len;

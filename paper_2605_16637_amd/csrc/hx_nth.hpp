@@ -79,8 +79,8 @@ __device__ __forceinline__ void nth_largest(F key, int from, int to, int n, NthS
                 if (x >= least && x <= most) s.list[atomicAdd(&s.n_list, 1)] = x;
             }
             __syncthreads();
-            if (tid < left) {
-                const K x = s.list[tid];
+            for (int k = tid; k < left; k += THREADS) {
+                const K x = s.list[k];
                 int larger = 0, equal = 0;
                 for (int i = 0; i < left; ++i) { larger += s.list[i] > x; equal += s.list[i] == x; }
                 if (larger < n && larger + equal >= n) { s.edge = x; s.equals = n - larger; }          // (all that are equal write the same)
