@@ -31,6 +31,9 @@ struct Place {
 __device__ __forceinline__ Place place(const AttendArgs &a, int j)
 {
     int lo = 0, hi = a.n - 1;
+    // with one query a sequence it is the j-th
+    const int guess = j < hi ? j : hi;
+    if (a.q_ptr[guess] <= j && a.q_ptr[guess + 1] > j) lo = hi = guess;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (a.q_ptr[mid] <= j) lo = mid; else hi = mid - 1;
@@ -189,23 +192,35 @@ __device__ __forceinline__ double across(double x, int d)
 template <typename Q, typename E, int D>
 __device__ __forceinline__ double exact_score(const TopArgs &t, int j, int head, int page, int sub)
 {
+    using Q8 = typename Types<Q>::x8;
     using E8 = typename Types<E>::x8;
     const AttendArgs &a = t.a;
     const E *at = (const E *)t.bounds + ((int64_t)page * a.kv.n_heads + head) * (2 * D) + sub * 8;
     const E8 lo = *(const E8 *)at, hi = *(const E8 *)(at + D);
     double best = -__builtin_inf();
 #pragma unroll 1
-    for (int g = 0; g < a.group; ++g) {
-        const Q *q = (const Q *)a.q + (int64_t)j * a.q_token + (int64_t)(head * a.group + g) * a.q_head + sub * 8;
-        double v = 0;
+    for (int g0 = 0; g0 < a.group; g0 += 4) {
+        Q8 x[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float x = a.scale < 0 ? -(float)q[i] : (float)q[i];
-            v = fma((double)x, (double)(float)(x < 0 ? lo[i] : hi[i]), v);
+        for (int k = 0; k < 4; ++k) {
+            const Q *q = (const Q *)a.q + (int64_t)j * a.q_token + (int64_t)(head * a.group + (g0 + k < a.group ? g0 + k : g0)) * a.q_head + sub * 8;
+            if (a.q_wide) x[k] = *(const Q8 *)q;
+            else
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[k][i] = q[i];
         }
 #pragma unroll
-        for (int d = D / 16; d > 0; d >>= 1) v += across(v, d);
-        best = fmax(best, v == v ? v : __builtin_inf());          // a bound that is no number is taken for +infinity
+        for (int k = 0; k < 4; ++k) {
+            double v = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float y = a.scale < 0 ? -(float)x[k][i] : (float)x[k][i];
+                v = fma((double)y, (double)(float)(y < 0 ? lo[i] : hi[i]), v);
+            }
+#pragma unroll
+            for (int d = D / 16; d > 0; d >>= 1) v += across(v, d);
+            best = fmax(best, v == v ? v : __builtin_inf());      // a bound that is no number is taken for +infinity
+        }
     }
     return best;
 }
@@ -223,15 +238,20 @@ __device__ __forceinline__ float of_key(uint32_t k)
     return __builtin_bit_cast(float, v < 0 ? v ^ INT32_MIN : ~v);
 }
 
-// A workgroup a query and KV head: of few pages a wavefront.
+// A workgroup a query and KV head, of up to 256 pages a single wavefront, which needs no barriers: a chain of round trips (the query's row, its length, its
+// pages and their scores, all of which are kept in LDS) and of passes over the scores.  cache: pages that fit there.
 template <typename Q, typename E, int D, int THREADS>
-__global__ __launch_bounds__(THREADS) void hx_top_pick_kernel(TopArgs t)
+__global__ __launch_bounds__(THREADS) void hx_top_pick_kernel(TopArgs t, int cache)
 {
-    constexpr int WAVES = THREADS / 64, CACHE = 4 * THREADS, LANES = D / 8, LIST = NTH_LIST;
-    __shared__ union { NthState<uint32_t, THREADS> near; NthState<uint64_t, THREADS> exact; } s;
-    __shared__ float s_score[CACHE];
+    constexpr int WAVES = THREADS / 64, LANES = D / 8, LIST = 64, EACH = 4;      // EACH: scores that a thread holds
+    __shared__ NthHeld<uint32_t, THREADS> s_near;
+    __shared__ NthHeld<uint64_t, THREADS> s_far;
+    __shared__ NthState<uint64_t, THREADS> s_many;
+    __shared__ double s_exact[LIST];
     __shared__ int s_list[LIST], s_n_list, s_count[2][WAVES];
     __shared__ float s_off[WAVES];
+    extern __shared__ int s_pages[];                               // [cache] entries of the row, then their scores
+    float *s_score = (float *)(s_pages + cache);
     const AttendArgs &a = t.a;
     const KvView &kv = a.kv;
     const int pair = blockIdx.x, head = pair % kv.n_heads, j = t.first_query + pair / kv.n_heads;
@@ -245,41 +265,55 @@ __global__ __launch_bounds__(THREADS) void hx_top_pick_kernel(TopArgs t)
             for (int i = tid; i < t.n_pages; i += THREADS) chosen[i] = -1;
         return;
     }
-    // how many threads say so
-    auto count = [&](bool x) {
-        const unsigned long long m = __builtin_amdgcn_ballot_w64(x);
-        if (lane == 0) s_count[0][wave] = __builtin_popcountll(m);
-        __syncthreads();
-        int all = 0;
+    // sums of x and y over the wavefronts, each of which has one
+    auto add_up = [&](int &x, int &y) {
+        if constexpr (WAVES > 1) {
+            if (lane == 0) { s_count[0][wave] = x; s_count[1][wave] = y; }
+            __syncthreads();
+            x = y = 0;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) all += s_count[0][w];
-        __syncthreads();
-        return all;
+            for (int w = 0; w < WAVES; ++w) { x += s_count[0][w]; y += s_count[1][w]; }
+            __syncthreads();
+        }
     };
     const bool all = p.own < t.n_pages || kv.n_pages == 0;
     const int from = t.n_first, to = p.own - t.n_last + 1;         // the pages between those that are seen in any case
     const float *score = t.score + (int64_t)pair * t.stride;
     double *exact = t.exact + (int64_t)pair * t.stride;
-    const bool cached = to - from <= CACHE;
-    auto score_of = [&](int b) { return cached ? s_score[b - from] : score[b]; };
-    auto page_at = [&](int b) { const int page = p.table[b]; return page < kv.n_pages ? page : -1; };
+    const bool cached = p.own < cache;
+    float off = 0.0f;
+    if (!all)
+        for (int i = from / 16 + tid; i <= (to - 1) / 16; i += THREADS) off = fmaxf(off, t.off[(int64_t)pair * (t.stride / 16) + i]);
+    int fixed = 0, none = 0;                                       // pages that are there of those seen in any case
+    if (cached) {
+        for (int b0 = 0; b0 <= p.own; b0 += THREADS) {
+            const int b = b0 + tid;
+            const bool in = b <= p.own, between = !all && b >= from && b < to;
+            const int page = in_pool(kv, in ? p.table[b] : -1);
+            if (in) s_pages[b] = page;
+            if (between) s_score[b] = score[b];
+            fixed += __builtin_popcountll(__builtin_amdgcn_ballot_w64(!between && page >= 0));
+        }
+    } else
+        for (int i0 = 0; i0 < t.n_first + t.n_last; i0 += THREADS) {
+            const int i = i0 + tid, page = i < t.n_first + t.n_last ? p.table[i < t.n_first ? i : to + i - t.n_first] : -1;
+            fixed += __builtin_popcountll(__builtin_amdgcn_ballot_w64(page >= 0 && page < kv.n_pages));
+        }
+    add_up(fixed, none);
+    auto score_of = [&](int b) { return cached ? s_score[b] : score[b]; };
+    auto page_at = [&](int b) {
+        if (cached) return s_pages[b];
+        const int page = p.table[b];
+        return page < kv.n_pages ? page : -1;
+    };
     // which of the pages between are taken
     enum { NONE, LEFT, NEAR, EXACT, BLIND } how = NONE;            // none; all that are there; scores from `under` on; scores above `over`, and from
     float over = INF, under = INF;                                 // `under` on the largest exact ones; all by their exact ones
     uint64_t edge = 0;
-    int equals = 0;
+    int equals = 0, unsures = 0;
     auto unsure = [&](int b) { return how == BLIND ? page_at(b) >= 0 : score_of(b) <= over && score_of(b) >= under; };
-    int want = t.n_pages;
-    if (!all)
-        for (int i0 = 0; i0 < t.n_first + t.n_last; i0 += THREADS) {
-            const int i = i0 + tid;
-            want -= count(i < t.n_first + t.n_last && page_at(i < t.n_first ? i : to + i - t.n_first) >= 0);
-        }
+    const int want = t.n_pages - fixed;
     if (!all && want > 0) {
-        float off = 0.0f;
-        for (int i = from / 16 + tid; i <= (to - 1) / 16; i += THREADS) off = fmaxf(off, t.off[(int64_t)pair * (t.stride / 16) + i]);
-        if (cached)
-            for (int b = from + tid; b < to; b += THREADS) s_score[b - from] = score[b];
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) off = fmaxf(off, __shfl_xor(off, d));
         if (lane == 0) s_off[wave] = off;
@@ -288,24 +322,38 @@ __global__ __launch_bounds__(THREADS) void hx_top_pick_kernel(TopArgs t)
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) off = fmaxf(off, s_off[w]);
         if (off < INF) {
-            nth_largest([&](int b) { return key_of(score_of(b)); }, from, to, want, s.near);
-            how = s.near.edge ? EXACT : LEFT;
-            const float near = of_key(s.near.edge);
+            uint32_t k;
+            if (to - from <= EACH * THREADS) {
+                uint32_t x[EACH];
+#pragma unroll
+                for (int i = 0; i < EACH; ++i) {
+                    const int b = from + i * THREADS + tid;
+                    x[i] = b < to ? key_of(score_of(b)) : 0;
+                }
+                nth_largest_held(x, want, s_near, &k, &equals);
+            } else {
+                nth_largest([&](int b) { return (uint64_t)key_of(score_of(b)); }, from, to, want, s_many);
+                k = (uint32_t)s_many.edge;
+            }
+            how = k ? EXACT : LEFT;
+            const float near = of_key(k);
             over = near + 2.1f * off;
             under = near - 2.1f * off;
         } else how = BLIND;
-        int unsures = 0, sure = 0;
-        if (how != LEFT)
+        int sure = 0;
+        if (how != LEFT) {
             for (int b0 = from; b0 < to; b0 += THREADS) {
                 const int b = b0 + tid;
                 const bool u = b < to && unsure(b);
-                sure += count(b < to && how == EXACT && score_of(b) > over);
-                unsures += count(u);
+                sure += __builtin_popcountll(__builtin_amdgcn_ballot_w64(b < to && how == EXACT && score_of(b) > over));
+                unsures += __builtin_popcountll(__builtin_amdgcn_ballot_w64(u));
                 if (u) {
                     const int at = atomicAdd(&s_n_list, 1);
                     if (at < LIST) s_list[at] = b;
                 }
             }
+            add_up(sure, unsures);
+        }
         if (how == EXACT && sure + unsures == want) how = NEAR;
         if (how >= EXACT) {
             __syncthreads();
@@ -314,10 +362,11 @@ __global__ __launch_bounds__(THREADS) void hx_top_pick_kernel(TopArgs t)
                 for (int i0 = 0; i0 < unsures; i0 += groups) {
                     const int i = i0 + tid / LANES, b = s_list[i < unsures ? i : 0];
                     const double x = exact_score<Q, E, D>(t, j, head, page_at(b), sub);
-                    if (i < unsures && sub == 0) exact[b] = x;
+                    if (i < unsures && sub == 0) s_exact[i] = x;
                 }
                 __syncthreads();
-                nth_largest([&](int i) { return key_of(exact[s_list[i]]); }, 0, unsures, want - sure, s.exact);
+                const uint64_t x[1] = {tid < unsures ? key_of(s_exact[tid]) : 0};
+                nth_largest_held(x, want - sure, s_far, &edge, &equals);
             } else {
                 for (int b0 = from; b0 < to; b0 += groups) {
                     const int b = b0 + tid / LANES, page = b < to && unsure(b) ? page_at(b) : -1;
@@ -325,36 +374,50 @@ __global__ __launch_bounds__(THREADS) void hx_top_pick_kernel(TopArgs t)
                     if (page >= 0 && sub == 0) exact[b] = x;
                 }
                 __syncthreads();
-                nth_largest([&](int b) { return unsure(b) ? key_of(exact[b]) : (uint64_t)0; }, from, to, want - sure, s.exact);
+                nth_largest([&](int b) { return unsure(b) ? key_of(exact[b]) : (uint64_t)0; }, from, to, want - sure, s_many);
+                edge = s_many.edge;
+                equals = s_many.equals;
             }
-            edge = s.exact.edge;
-            equals = s.exact.equals;
         }
     }
+    auto exact_of = [&](int b) {
+        if (unsures > LIST) return exact[b];
+        int i = 0;
+        while (i < unsures - 1 && s_list[i] != b) ++i;
+        return s_exact[i];
+    };
     // the pages in rising order
     int n = 0, seen_equal = 0;
     for (int b0 = 0; b0 <= p.own; b0 += THREADS) {
         const int b = b0 + tid;
-        const int page = in_pool(kv, b <= p.own ? p.table[b] : -1);
+        const int page = cached ? (b <= p.own ? s_pages[b] : -1) : in_pool(kv, b <= p.own ? p.table[b] : -1);
         const bool between = !all && b >= from && b < to && page >= 0;
         const bool told = between && how >= EXACT && unsure(b);
         const float x = between && how != NONE ? score_of(b) : 0.0f;
-        const uint64_t k = told ? key_of(exact[b]) : 0;
+        const uint64_t k = told ? key_of(exact_of(b)) : 0;
         const bool equal = k == edge && k > 0;
         const unsigned long long e = __builtin_amdgcn_ballot_w64(equal);
-        if (lane == 0) s_count[0][wave] = __builtin_popcountll(e);
-        __syncthreads();
-        int rank = seen_equal + __builtin_popcountll(e & ((1ull << lane) - 1)), all_equal = 0;
+        int rank = seen_equal + __builtin_popcountll(e & ((1ull << lane) - 1)), all_equal = __builtin_popcountll(e);
+        if constexpr (WAVES > 1) {
+            if (lane == 0) s_count[0][wave] = all_equal;
+            __syncthreads();
+            all_equal = 0;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) { rank += w < wave ? s_count[0][w] : 0; all_equal += s_count[0][w]; }
+            for (int w = 0; w < WAVES; ++w) { rank += w < wave ? s_count[0][w] : 0; all_equal += s_count[0][w]; }
+        }
         const bool best = told ? k > edge || (equal && rank < equals) : how == LEFT ? x > -INF : how == NEAR ? x >= under : how == EXACT && x > over;
         const bool take = page >= 0 && (!between || best);
         const unsigned long long m = __builtin_amdgcn_ballot_w64(take);
-        if (lane == 0) s_count[1][wave] = __builtin_popcountll(m);
-        __syncthreads();
-        int at = n + __builtin_popcountll(m & ((1ull << lane) - 1));
+        int at = n + __builtin_popcountll(m & ((1ull << lane) - 1)), taken = __builtin_popcountll(m);
+        if constexpr (WAVES > 1) {
+            if (lane == 0) s_count[1][wave] = taken;
+            __syncthreads();
+            taken = 0;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) { at += w < wave ? s_count[1][w] : 0; n += s_count[1][w]; }
+            for (int w = 0; w < WAVES; ++w) { at += w < wave ? s_count[1][w] : 0; taken += s_count[1][w]; }
+            __syncthreads();
+        }
+        n += taken;
         seen_equal += all_equal;
         if (take) {
             picked[at] = page;
@@ -362,15 +425,13 @@ __global__ __launch_bounds__(THREADS) void hx_top_pick_kernel(TopArgs t)
             // where its own page is there it is the last of all; else all that are chosen are full
             if (b == p.own) t.picked_len[pair] = (at << kv.shift) + (p.pos & ((1 << kv.shift) - 1)) + 1;
         }
-        __syncthreads();
+        if (b == p.own && !take) {
+            if (at == 0) picked[0] = -1;
+            t.picked_len[pair] = at == 0 ? 1 : at << kv.shift;
+        }
     }
     if (chosen)
         for (int i = n + tid; i < t.n_pages; i += THREADS) chosen[i] = -1;
-    const int own_page = p.table[p.own];
-    if (tid == 0 && (own_page < 0 || own_page >= kv.n_pages)) {
-        if (n == 0) picked[0] = -1;
-        t.picked_len[pair] = n == 0 ? 1 : n << kv.shift;
-    }
 }
 
 template <typename Q, typename E, int D>
@@ -381,9 +442,9 @@ void score_and_pick(const TopArgs &t, int64_t score_grid, int pages, hipStream_t
         if (t.a.max_q == 1) hx_top_score_kernel<Q, E, D, true><<<(int)score_grid, TOP_THREADS, 0, stream>>>(t);
         else hx_top_score_kernel<Q, E, D, false><<<(int)score_grid, TOP_THREADS, 0, stream>>>(t);
     }
-    if (pages <= 384) hx_top_pick_kernel<Q, E, D, 64><<<pick_grid, 64, 0, stream>>>(t);
-    else if (pages <= 1536) hx_top_pick_kernel<Q, E, D, 256><<<pick_grid, 256, 0, stream>>>(t);
-    else hx_top_pick_kernel<Q, E, D, 1024><<<pick_grid, 1024, 0, stream>>>(t);
+    const int cache = pages < 1024 ? pages : pages <= 2048 ? 2048 : 4096, lds = cache * 8;
+    if (pages <= 256) hx_top_pick_kernel<Q, E, D, 64><<<pick_grid, 64, lds, stream>>>(t, cache);
+    else hx_top_pick_kernel<Q, E, D, 512><<<pick_grid, 512, lds, stream>>>(t, cache);
 }
 
 template <typename Q, typename E>

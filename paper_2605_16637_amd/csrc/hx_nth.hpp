@@ -5,7 +5,7 @@
 
 namespace {
 
-constexpr int NTH_BINS = 1024, NTH_LIST = 256;
+constexpr int NTH_BINS = 1024, NTH_LIST = 64;
 
 template <typename K, int THREADS>
 struct NthState {
@@ -122,6 +122,77 @@ __device__ __forceinline__ void nth_largest(F key, int from, int to, int n, NthS
         const K width = ((K)1 << shift) - 1;
         hi = most - lo < width ? most : lo + width;
     }
+}
+
+// The same of keys that the threads hold, EACH a thread (0: none): the range between the least and the largest is halved until as many lie above as are wanted,
+// by counts of the wavefronts, which meet once for each halving.
+template <typename K, int THREADS>
+struct NthHeld {
+    static constexpr int WAVES = THREADS / HX_WAVE;
+    K least[WAVES], most[WAVES], last[WAVES];
+    int count[2][WAVES];
+};
+template <typename K, int THREADS, int EACH>
+__device__ __forceinline__ void nth_largest_held(const K (&x)[EACH], int n, NthHeld<K, THREADS> &s, K *edge, int *equals)
+{
+    constexpr int WAVES = THREADS / HX_WAVE;
+    const int lane = threadIdx.x & (HX_WAVE - 1), wave = threadIdx.x / HX_WAVE;
+    auto extreme = [](K a, K b, bool largest) { return (b > a) == largest ? b : a; };
+    auto over_lanes = [&](K y, bool largest) {
+#pragma unroll
+        for (int d = HX_WAVE / 2; d > 0; d >>= 1) y = extreme(y, nth_across(y, d), largest);
+        return y;
+    };
+    auto over_waves = [&](K y, K *to, bool largest) {
+        if constexpr (WAVES > 1) {
+            if (lane == 0) to[wave] = y;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) y = extreme(y, to[w], largest);
+        }
+        return y;
+    };
+    int turn = 0;
+    auto at_least = [&](K y) {                              // how many keys are y or more
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) c += __builtin_popcountll(__builtin_amdgcn_ballot_w64(x[i] >= y));
+        if constexpr (WAVES > 1) {
+            if (lane == 0) s.count[turn][wave] = c;
+            __syncthreads();
+            c = 0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) c += s.count[turn][w];
+            turn ^= 1;                                      // (who is still reading the other has passed a barrier since)
+        }
+        return c;
+    };
+    K least = ~(K)0, most = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        least = x[i] != 0 && x[i] < least ? x[i] : least;
+        most = x[i] > most ? x[i] : most;
+    }
+    least = over_waves(over_lanes(least, false), s.least, false);
+    most = over_waves(over_lanes(most, true), s.most, true);
+    *edge = 0;
+    *equals = INT32_MAX;
+    if (at_least(1) <= n) return;
+    // more than n keys are `least` or more, fewer than n are more than `most`
+    while (least < most) {
+        const K mid = most - (most - least) / 2;
+        const int above = at_least(mid);
+        if (above == n) {                                   // the least of them is the n-th
+            K y = ~(K)0;
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) y = x[i] >= mid && x[i] < y ? x[i] : y;
+            *edge = over_waves(over_lanes(y, false), s.last, false);
+            return;
+        }
+        if (above > n) least = mid; else most = mid - 1;
+    }
+    *edge = least;
+    *equals = n - (least == ~(K)0 ? 0 : at_least(least + 1));
 }
 
 // Order of a number that is no NaN, as a key: larger numbers have larger keys, -infinity has the least.
