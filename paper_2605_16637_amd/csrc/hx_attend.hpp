@@ -828,7 +828,7 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? (
         // A tile of 4 bits is a quarter of the bytes of one of 16: two are under way, and their pages are looked up a tile earlier still.  Every
         // tile asks for the same number of loads, of the pool's first page where there is none, so that what is waited for is known by count (with
         // loads that depend on a page's being there all of them were waited for at every tile, the next pages' too).  128 sequences over some 4000 tokens,
-        // 32 heads of 128: 175 us, 4.0 TB/s (219 with the loop for 16 bits); two wavefronts a SIMD that keep a tile's values in registers took
+        // 32 heads of 128: 170 us, 4.1 TB/s (219 with the loop for 16 bits); two wavefronts a SIMD that keep a tile's values in registers took
         // less than three with an eighth to a half of them (181 to 194).
         struct Ahead {
             KPiece k[2][K_LOADS];
@@ -898,7 +898,6 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? (
         };
         Looked next;
         auto step = [&](Ahead &r, int tile) {
-            if (tile >= tile1) return;
             const uint32_t now = r.there;
             if (now != 0xffffffffu) {
                 // what is not there may be NaN by its scale, which 0 makes a number
@@ -951,16 +950,20 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : COLS == 1 && D == 64 ? (
                 for (int w = 0; w < COLS; ++w) o[w][x] = mfma16(vf[x], rest[w].x8, mfma16(vf[x], p[w].x8, o[w][x]));
             in_order();
         };
-        Ahead r0, r1;
-        {
-            const Looked l0 = look(tile0 + wave), l1 = look(tile0 + wave + 4);
-            next = look(tile0 + wave + 8);
-            ask(r0, tile0 + wave, l0);
-            ask(r1, tile0 + wave + 4, l1);
-        }
-        for (int tile = tile0 + wave; tile < tile1; tile += 8) {
-            step(r0, tile);
-            step(r1, tile + 4);
+        // (without a tile there may be no table and no page)
+        int tile = tile0 + wave;
+        if (tile < tile1) {
+            Ahead r0, r1;
+            const Looked l0 = look(tile), l1 = look(tile + 4);
+            next = look(tile + 8);
+            ask(r0, tile, l0);
+            ask(r1, tile + 4, l1);
+            // (a step that may be left out would have all loads waited for)
+            for (; tile + 4 < tile1; tile += 8) {
+                step(r0, tile);
+                step(r1, tile + 4);
+            }
+            if (tile < tile1) step(r0, tile);
         }
     } else {
         int pages = page_of(tile0 + wave), next = page_of(tile0 + wave + 4);

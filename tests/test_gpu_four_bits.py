@@ -352,3 +352,22 @@ def test_captured_and_on_another_stream(ctx):
         torch.cuda.synchronize()
         assert all(torch.equal(p, t) for p, t in zip(a, (k, v, out)))
         assert np.array_equal(lh.f64(k), lh.decode(*lh.encode(lh.f64(x))))
+
+
+@pytest.mark.parametrize("pages,entries", [(0, 0), (0, 3), (4, 0), (4, 3)])
+@pytest.mark.parametrize("rows", [1, 40])
+def test_queries_of_rows_that_hold_nothing(ctx, pages, entries, rows):
+    """Pools without pages, tables without entries, rows that the tables lack: zeros, and no page is read."""
+    import torch
+    heads, group, dim, T = 2, 2, 64, 16
+    pool = dict(empty_pool(1, pages, heads, T, dim), page_tokens=T)
+    seqs = dict(table=torch.full((2, entries), -1, dtype=torch.int32, device="cuda:0"), len=sh.i32([0, 0]))
+    q = torch.randn(2 * rows, heads * group, dim, device="cuda:0").bfloat16()
+    out, lse = torch.full_like(q, 7.0), torch.full((2 * rows, heads * group), 7.0, device="cuda:0")
+    ctx.hx_attend(pool, 0, seqs, sh.i32([0, rows, 2 * rows]), q, out, max_q=rows, row=sh.i32([1, 2]), max_len=max(1, entries * T), lse=lse)
+    assert lh.status(ctx) == -6                                                # more queries than tokens, and no row 2
+    assert (out == 0).all() and torch.isneginf(lse).all()
+    weight = torch.full((2, entries * T), 7.0, device="cuda:0")
+    if entries:
+        ctx.hx_kv_weigh(pool, 0, seqs, sh.i32([0, rows, 2 * rows]), q, lse, weight, max_q=rows, row=sh.i32([1, 2]), max_len=entries * T)
+        assert lh.status(ctx) == -6 and (weight == 7).all()
