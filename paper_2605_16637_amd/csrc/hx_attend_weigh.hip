@@ -4,6 +4,7 @@
 namespace {
 
 constexpr int WG_THREADS = 256, WG_WAVES = WG_THREADS / 64;
+constexpr int BLOCKS = 2, KEYS = 16 * BLOCKS;                  // blocks of 16 keys, and keys, that a wavefront has at once
 
 struct WeighArgs {
     AttendArgs a;
@@ -22,166 +23,285 @@ __device__ __forceinline__ bool row_before(const AttendArgs &a, int i)
     return __syncthreads_or(hit);
 }
 
-// A wavefront takes 16 BLOCKS keys of a sequence and all heads: its weights are its own, and their sums need no other's.  The keys of a head go from memory
-// into the registers of the product with 16 rows (queries x query heads of the KV head) at a time; the next head's are under way while
-// weights are worked out.
-template <typename E, int BITS, int D, int BLOCKS>
-__global__ __launch_bounds__(WG_THREADS) void hx_weigh_kernel(WeighArgs w)
+// 8 numbers of a query, which need not be aligned to more than their type
+template <typename E>
+__device__ __forceinline__ typename Types<E>::x8 eight(const E *q)
 {
-    using X8 = typename Types<E>::x8;
-    using Keys = KeyPieces<BITS, D>;
-    using KPiece = typename Keys::Piece;
-    constexpr int ROW_BYTES = ROW<BITS, D>, KEYS = 16 * BLOCKS, TILE = KEYS * WG_WAVES;
+    struct __attribute__((packed, aligned(2))) Loose { typename Types<E>::x8 x; };
+    return ((const Loose *)q)->x;
+}
+
+// KEYS keys of a sequence from y0 on: where they lie, and those of them that are there.
+struct Where {
+    int64_t at[BLOCKS];
+    uint32_t there;
+};
+template <int BITS, int D>
+__device__ __forceinline__ Where where(const AttendArgs &a, const Seq &sq, const Extent &ex, int y0, int64_t page_bytes)
+{
+    using Pieces = KeyPieces<BITS, D>;
+    const KvView &kv = a.kv;
+    const int lane = threadIdx.x & 63, quad = lane >> 4, col = lane & 15, mine = y0 + (lane & (KEYS - 1));
+    Where w;
+    int page = -1;
+    if (mine < ex.hi && (mine >= ex.lo || mine < a.n_sink)) page = sq.table[mine >> kv.shift];
+    page = in_pool(kv, page);
+    w.there = (uint32_t)__builtin_amdgcn_ballot_w64(page >= 0);
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+        const int p = __shfl(page, b * 16 + col), y = y0 + b * 16 + col;
+        // (what is not there reads the pool's first page, and counts for nothing)
+        w.at[b] = (p < 0 ? 0 : p * page_bytes + (y & ((1 << kv.shift) - 1)) * ROW<BITS, D>) + quad * Pieces::BYTES;
+    }
+    return w;
+}
+
+// What a step needs: the keys of a head, and 16 rows (queries x query heads of the KV head) of it.
+template <int BITS, int D>
+struct KeysOf {
+    typename KeyPieces<BITS, D>::Piece k[BLOCKS][KeyPieces<BITS, D>::LOADS];
+    uint32_t e[BLOCKS][KeyPieces<BITS, D>::LOADS];
+};
+template <typename E, int D>
+struct RowsOf {
+    typename Types<E>::x8 q[D / 32];
+    float lse, unit;                 // unit: of the head's keys, of 8 bits
+};
+
+template <typename E, int BITS, int D>
+struct Weigher {
+    using Pieces = KeyPieces<BITS, D>;
+    const AttendArgs &a;
+    const Seq &sq;
+    const char *k_at;
+    const uint8_t *ke_at;
+    int64_t head_bytes;
+    int rows;                        // of a KV head
+    const int *s_depth;
+    const uint32_t *s_anc;
+    float sum[BLOCKS][4];
+
+    // (without `in` the same number of loads, of one place)
+    __device__ __forceinline__ void ask_keys(KeysOf<BITS, D> &r, const Where &w, int head, bool in) const
+    {
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) {
+            const int64_t at = in ? w.at[b] + head * head_bytes : 0;
+#pragma unroll
+            for (int l = 0; l < Pieces::LOADS; ++l) {
+                r.k[b][l] = *(const typename Pieces::Piece *)(k_at + at + l * 64);
+                r.e[b][l] = BITS == 4 ? ke_at[(at + l * 64) / 16] : 0;
+            }
+        }
+    }
+    __device__ __forceinline__ void ask_rows(RowsOf<E, D> &r, int head, int rt) const
+    {
+        const int lane = threadIdx.x & 63, quad = lane >> 4, row = rt * 16 + (lane & 15), in = row < rows ? row : 0;
+        const int t = in / a.group, qhead = head * a.group + in % a.group;
+        const E *q = (const E *)a.q + (int64_t)(sq.q0 + t) * a.q_token + (int64_t)qhead * a.q_head;
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) r.q[s] = eight(q + Pieces::place(s, quad));
+        r.lse = a.lse[(int64_t)(sq.q0 + t) * a.n_heads + qhead];
+        r.unit = 1.0f;
+        if constexpr (BITS == 8) {
+            const float unit = (a.k_scale ? a.k_scale + a.layer * a.kv.n_heads : (const float *)a.zeros)[a.k_scale ? head : 0];
+            r.unit = a.k_scale ? unit : 1.0f;
+        }
+    }
+    // scores of the keys (a lane: keys 16 b + 4 quad + i) with the rows (its column)
+    __device__ __forceinline__ void scores(const KeysOf<BITS, D> &k, const RowsOf<E, D> &r, f32x4 (&s)[BLOCKS]) const
+    {
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) {
+            s[b] = f32x4{};
+#pragma unroll
+            for (int l = 0; l < Pieces::LOADS; ++l)
+#pragma unroll
+                for (int j = 0; j < Pieces::EACH; ++j) s[b] = mfma16(Pieces::template operand<E>(k.k[b][l], k.e[b][l], j), r.q[Pieces::EACH * l + j], s[b]);
+        }
+    }
+    __device__ __forceinline__ void add(const f32x4 (&s)[BLOCKS], float lse, float unit, int rt, int y0, uint32_t there)
+    {
+        const int lane = threadIdx.x & 63, quad = lane >> 4, row = rt * 16 + (lane & 15);
+        const bool tree = a.parent != nullptr;
+        const float sc = a.scale * unit;
+        // as in attention the factor is no 0: a score of -infinity stays one
+        const float c = copysignf(fmaxf(fabsf(sc), 1e-37f), sc);
+        const int t_first = rt * 16 / a.group, t_last = (rt * 16 + 15) / a.group, end = y0 + KEYS - 1;
+        const int first = tree ? sq.base - 1 : sq.base + t_first, last = tree ? sq.len : sq.base + (t_last < sq.nq ? t_last : sq.nq - 1);
+        const bool counts = row < rows && __builtin_fabsf(lse) < __builtin_inff();
+        if (there == 0xffffffffu && end <= first && (a.window <= 0 || end < a.n_sink || last - y0 < a.window)) {
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s[b][x], c, -lse) * LOG2E);
+                    sum[b][x] += counts ? p : 0.0f;
+                }
+        } else {
+            const Sight view = sight(a, sq, row / a.group, s_depth, s_anc);
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int k = b * 16 + quad * 4 + x;
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s[b][x], c, -lse) * LOG2E);
+                    sum[b][x] += counts && ((there >> k) & 1) && view.sees(y0 + k) ? p : 0.0f;
+                }
+        }
+    }
+    // over the 16 lanes that have a key's sums
+    __device__ __forceinline__ void add_up()
+    {
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int d = 8; d > 0; d >>= 1) sum[b][x] += __shfl_xor(sum[b][x], d);
+    }
+};
+
+// weight[row][y] += sum over the queries and heads that see key y of exp(score - lse): a query's softmax statistics are known, so a key's
+// weight needs no other key's, no maximum and no second pass, and only keys are read.  One wavefront has a key's sums in a fixed order, and a
+// sequence's row is another's to none: no atomics, the same sums every time.
+//
+// FEW: up to 16 rows a KV head, bound by the keys' bytes.  A wavefront takes 32 keys and all heads, so that its sums need no other's; two
+// heads' keys are under way.  128 sequences over some 4000 tokens, 8 KV heads of 128: 264 us, 3.9 TB/s of keys (with the workgroup's wavefronts on
+// a head each and their sums joined in LDS 303; at three wavefronts a SIMD 328, as the keys under way do not fit their registers).
+// Else the wavefronts have the same 32 keys and divide heads and rows, 16 rows under way while weights are worked out, and their sums are
+// added in LDS: there are rows for many steps, and as few keys as possible a workgroup fill the chip.  What it does is exponentials, 4 for 16
+// products of a lane and mask tests at sequences' ends.  The last 32 queries of 7 prompts of some 6000 tokens, 32 heads of 128: 75 us (95 with 128
+// keys a workgroup; 64 keys a wavefront 74, and 96 at three wavefronts a SIMD; this at two 78).
+template <typename E, int BITS, int D, bool FEW>
+__global__ __launch_bounds__(WG_THREADS, D == 256 ? 1 : FEW ? 2 : 3) void hx_weigh_kernel(WeighArgs w)
+{
+    constexpr int TILE = FEW ? KEYS * WG_WAVES : KEYS;
+    using Self = Weigher<E, BITS, D>;
     extern __shared__ __align__(16) char smem[];
     int *s_depth = (int *)smem + HX_MAX_DRAFTS;
     uint32_t *s_anc = (uint32_t *)(s_depth + HX_MAX_DRAFTS);
     const AttendArgs &a = w.a;
     const KvView &kv = a.kv;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), quad = lane >> 4, col = lane & 15;
-    const int i = blockIdx.x % a.n, part = blockIdx.x / a.n;
-    const Seq sq = sequence(a, i * kv.n_heads);
+    const int i = blockIdx.x % a.n, part = blockIdx.x / a.n, H = kv.n_heads;
+    const Seq sq = sequence(a, i * H);
     const Extent ex = extent<TILE>(a, sq, 0, sq.nq - 1);
     if (!sq.ok) { if (tid == 0 && part == 0 && (!sq.there || sq.nq > 0)) hx_raise(kv.status, HX_ERR_INDEX); return; }
     if (sq.nq == 0 || part >= ex.n) return;
     if (row_before(a, i)) { if (tid == 0 && part == 0) hx_raise(kv.status, HX_ERR_INDEX); return; }
-    const bool tree = a.parent != nullptr;
-    if (tree) plant(a, sq, (int *)smem, s_depth, s_anc);
-    const int r = a.row ? a.row[i] : i, rows = sq.nq * a.group, row_tiles = (rows + 15) / 16;
-    const int64_t page_bytes = ((int64_t)kv.n_heads << kv.shift) * ROW_BYTES, head_bytes = (int64_t)ROW_BYTES << kv.shift;
-    const int64_t here = (int64_t)a.layer * kv.n_pages * page_bytes;
-    const char *k_at = (const char *)kv.k + here;
-    const uint8_t *ke_at = BITS == 4 ? a.k_exp + here / 16 : nullptr;
+    if (a.parent) plant(a, sq, (int *)smem, s_depth, s_anc);
+    const int64_t page_bytes = ((int64_t)H << kv.shift) * ROW<BITS, D>, here = (int64_t)a.layer * kv.n_pages * page_bytes;
+    Self g{a, sq, (const char *)kv.k + here, BITS == 4 ? a.k_exp + here / 16 : nullptr, (int64_t)ROW<BITS, D> << kv.shift, sq.nq * a.group, s_depth, s_anc, {}};
+    float *to = w.weight + (a.row ? a.row[i] : i) * w.pitch;
     for (int tile = part; tile < ex.n; tile += w.each) {
-        const int y0 = (tile < ex.sink_tiles ? tile : tile - ex.sink_tiles + ex.lo_tile) * TILE + wave * KEYS;
-        // lane x looks up key x; what is not there reads the pool's first page, and counts for nothing
-        int page = -1;
-        {
-            const int y = y0 + (lane & (KEYS - 1));
-            if (y < ex.hi && (y >= ex.lo || y < a.n_sink)) page = sq.table[y >> kv.shift];
-            page = in_pool(kv, page);
-        }
-        const uint64_t there = __builtin_amdgcn_ballot_w64(page >= 0) & (KEYS == 64 ? ~0ull : (1ull << (KEYS & 63)) - 1);
-        if (there == 0) continue;
-        int64_t at[BLOCKS];
+        const int y0 = (tile < ex.sink_tiles ? tile : tile - ex.sink_tiles + ex.lo_tile) * TILE + (FEW ? wave * KEYS : 0);
+        const Where at = where<BITS, D>(a, sq, ex, y0, page_bytes);
+        if (at.there == 0) continue;
 #pragma unroll
-        for (int b = 0; b < BLOCKS; ++b) {
-            const int p = __shfl(page, b * 16 + col), y = y0 + b * 16 + col;
-            at[b] = (p < 0 ? 0 : p * page_bytes + (y & ((1 << kv.shift) - 1)) * ROW_BYTES) + quad * Keys::BYTES;
-        }
-        KPiece rk[BLOCKS][Keys::LOADS];
-        uint8_t ek[BLOCKS][Keys::LOADS];
-        auto fetch_k = [&](int head) {
+        for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
-            for (int b = 0; b < BLOCKS; ++b)
-#pragma unroll
-                for (int l = 0; l < Keys::LOADS; ++l) {
-                    rk[b][l] = *(const KPiece *)(k_at + at[b] + head * head_bytes + l * 64);
-                    if constexpr (BITS == 4) ek[b][l] = ke_at[(at[b] + head * head_bytes + l * 64) / 16];
-                }
-        };
-        X8 qf[D / 32];
-        float lse;
-        auto fetch_q = [&](int head, int rt) {
-            const int row = rt * 16 + col;
-            const bool in = row < rows;
-            const int t = in ? row / a.group : 0, qhead = head * a.group + (in ? row % a.group : 0);
-            const E *q = (const E *)a.q + (int64_t)(sq.q0 + t) * a.q_token + (int64_t)qhead * a.q_head;
-#pragma unroll
-            for (int s = 0; s < D / 32; ++s) {
-                const int d = Keys::place(s, quad);
-                X8 x = {};
-                if (in) {
-                    if (a.q_wide) x = *(const X8 *)(q + d);
-                    else
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) x[j] = q[d + j];
-                }
-                qf[s] = x;
+            for (int x = 0; x < 4; ++x) g.sum[b][x] = 0.0f;
+        if constexpr (FEW) {
+            KeysOf<BITS, D> k0, k1;
+            RowsOf<E, D> r0, r1;
+            g.ask_keys(k0, at, 0, true);
+            g.ask_rows(r0, 0, 0);
+            g.ask_keys(k1, at, 1, H > 1);
+            g.ask_rows(r1, H > 1 ? 1 : 0, 0);
+            auto step = [&](KeysOf<BITS, D> &k, RowsOf<E, D> &r, int head) {
+                f32x4 s[BLOCKS];
+                g.scores(k, r, s);
+                const float lse = r.lse, unit = r.unit;
+                g.ask_keys(k, at, head + 2, head + 2 < H);
+                g.ask_rows(r, head + 2 < H ? head + 2 : head, 0);
+                g.add(s, lse, unit, 0, y0, at.there);
+            };
+            // (a step that may be left out would have all loads waited for)
+            int head = 0;
+            for (; head + 1 < H; head += 2) {
+                step(k0, r0, head);
+                step(k1, r1, head + 1);
             }
-            lse = in ? a.lse[(int64_t)(sq.q0 + t) * a.n_heads + qhead] : __builtin_inff();
-        };
-        float sum[BLOCKS][4] = {};
-        fetch_k(0);
-        fetch_q(0, 0);
-        for (int head = 0; head < kv.n_heads; ++head) {
-            const float k_unit = a.k_scale ? a.k_scale[a.layer * kv.n_heads + head] : 1.0f, sc = a.scale * k_unit;
-            // as in attention the factor is no 0, and its sign the query's: a score of -infinity stays one
-            const float c = copysignf(fmaxf(fabsf(sc), 1e-37f), sc);
-            for (int rt = 0; rt < row_tiles; ++rt) {
-                f32x4 s[BLOCKS] = {};
+            if (head < H) step(k0, r0, head);
+            g.add_up();
+        } else {
+            const int row_tiles = (g.rows + 15) / 16, steps = H * row_tiles;
+            const int u0 = (int)((int64_t)steps * wave / WG_WAVES), u1 = (int)((int64_t)steps * (wave + 1) / WG_WAVES);
+            for (int u = u0; u < u1;) {
+                const int head = u / row_tiles, rt0 = u % row_tiles, rt1 = (head + 1) * row_tiles <= u1 ? row_tiles : rt0 + u1 - u;
+                KeysOf<BITS, D> k;
+                RowsOf<E, D> r0, r1;
+                g.ask_keys(k, at, head, true);
+                g.ask_rows(r0, head, rt0);
+                g.ask_rows(r1, head, rt0 + 1 < rt1 ? rt0 + 1 : rt0);
+                auto step = [&](RowsOf<E, D> &r, int rt) {
+                    f32x4 s[BLOCKS];
+                    g.scores(k, r, s);
+                    const float lse = r.lse, unit = r.unit;
+                    g.ask_rows(r, head, rt + 2 < rt1 ? rt + 2 : rt);
+                    g.add(s, lse, unit, rt, y0, at.there);
+                };
+                int rt = rt0;
+                for (; rt + 1 < rt1; rt += 2) {
+                    step(r0, rt);
+                    step(r1, rt + 1);
+                }
+                if (rt < rt1) step(r0, rt);
+                u += rt1 - rt0;
+            }
+            g.add_up();
+            __shared__ float s_sum[WG_WAVES][KEYS];
+            if (col == 0)
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
-                    for (int l = 0; l < Keys::LOADS; ++l)
+                    for (int x = 0; x < 4; ++x) s_sum[wave][b * 16 + quad * 4 + x] = g.sum[b][x];
+            __syncthreads();
+            if (tid < KEYS && ((at.there >> tid) & 1)) {
+                float all = s_sum[0][tid];
 #pragma unroll
-                        for (int j = 0; j < Keys::EACH; ++j) s[b] = mfma16(Keys::template operand<E>(rk[b][l], ek[b][l], j), qf[Keys::EACH * l + j], s[b]);
-                const float mine = lse;
-                if (rt + 1 < row_tiles) fetch_q(head, rt + 1);
-                else if (head + 1 < kv.n_heads) {
-                    fetch_k(head + 1);
-                    fetch_q(head + 1, 0);
-                }
-                const int t = (rt * 16 + col) / a.group, t_last = (rt * 16 + 15) / a.group, last = sq.base + (t_last < sq.nq ? t_last : sq.nq - 1);
-                const int first = tree ? sq.base - 1 : sq.base + rt * 16 / a.group, end = y0 + KEYS - 1;
-                const bool counts = rt * 16 + col < rows && __builtin_fabsf(mine) < __builtin_inff();
-                const bool whole = there == (KEYS == 64 ? ~0ull : (1ull << (KEYS & 63)) - 1) && end <= first &&
-                                   (a.window <= 0 || end < a.n_sink || (tree ? sq.len : last) - y0 < a.window);
-                if (whole) {
-#pragma unroll
-                    for (int b = 0; b < BLOCKS; ++b)
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const float p = __builtin_amdgcn_exp2f(fmaf(s[b][x], c, -mine) * LOG2E);
-                            sum[b][x] += counts ? p : 0.0f;
-                        }
-                } else {
-                    const Sight view = sight(a, sq, t, s_depth, s_anc);
-#pragma unroll
-                    for (int b = 0; b < BLOCKS; ++b)
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const int k = b * 16 + quad * 4 + x;
-                            const float p = __builtin_amdgcn_exp2f(fmaf(s[b][x], c, -mine) * LOG2E);
-                            sum[b][x] += counts && ((there >> k) & 1) && view.sees(y0 + k) ? p : 0.0f;
-                        }
-                }
+                for (int v = 1; v < WG_WAVES; ++v) all += s_sum[v][tid];
+                to[y0 + tid] += all;
             }
+            __syncthreads();
+            continue;
         }
-        // a key's sums lie over 16 lanes
-        float *to = w.weight + r * w.pitch;
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) {
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-#pragma unroll
-                for (int d = 8; d > 0; d >>= 1) sum[b][x] += __shfl_xor(sum[b][x], d);
             const int k = b * 16 + quad * 4 + col;
-            if (col < 4 && ((there >> k) & 1)) to[y0 + k] += col == 0 ? sum[b][0] : col == 1 ? sum[b][1] : col == 2 ? sum[b][2] : sum[b][3];
+            const float (&sum)[4] = g.sum[b];
+            if (col < 4 && ((at.there >> k) & 1)) to[y0 + k] += col == 0 ? sum[0] : col == 1 ? sum[1] : col == 2 ? sum[2] : sum[3];
         }
     }
 }
 
-template <typename E, int BITS, int D>
+template <typename E, int BITS, int D, bool FEW>
 int launch(hx_ctx *ctx, WeighArgs &w, int max_len, hipStream_t stream)
 {
-    constexpr int BLOCKS = 2;
-    const int TILE = 16 * BLOCKS * WG_WAVES;
+    const int tile = FEW ? KEYS * WG_WAVES : KEYS;
     int64_t reach = max_len;
     const HxAttend &a = w.a;
     if (a.window > 0 && reach > (int64_t)a.window + a.n_sink + a.max_q) reach = (int64_t)a.window + a.n_sink + a.max_q;
-    const int64_t tiles = (reach + TILE - 1) / TILE + 2, most = hx_most_groups(WG_THREADS) / a.n;
+    const int64_t tiles = (reach + tile - 1) / tile + 2, most = hx_most_groups(WG_THREADS) / a.n;
     w.each = (int)(tiles < most ? tiles : most);
     const int lds = a.parent ? HX_MAX_DRAFTS * 4 + TREE_BYTES : 0;
-    hx_weigh_kernel<E, BITS, D, BLOCKS><<<(int)((int64_t)w.each * a.n), WG_THREADS, lds, stream>>>(w);
+    hx_weigh_kernel<E, BITS, D, FEW><<<(int)((int64_t)w.each * a.n), WG_THREADS, lds, stream>>>(w);
     return hx_check_launch(ctx, "hx_weigh_kernel");
+}
+
+template <typename E, int BITS, int D>
+int by_rows(hx_ctx *ctx, WeighArgs &w, int max_len, hipStream_t stream)
+{
+    return (int64_t)w.a.max_q * w.a.group <= 16 ? launch<E, BITS, D, true>(ctx, w, max_len, stream) : launch<E, BITS, D, false>(ctx, w, max_len, stream);
 }
 
 template <typename E, int BITS>
 int by_dim(hx_ctx *ctx, WeighArgs &w, int max_len, hipStream_t stream)
 {
-    if (w.a.kv.dim == 64) return launch<E, BITS, 64>(ctx, w, max_len, stream);
-    if (w.a.kv.dim == 128) return launch<E, BITS, 128>(ctx, w, max_len, stream);
-    return launch<E, BITS, 256>(ctx, w, max_len, stream);
+    if (w.a.kv.dim == 64) return by_rows<E, BITS, 64>(ctx, w, max_len, stream);
+    if (w.a.kv.dim == 128) return by_rows<E, BITS, 128>(ctx, w, max_len, stream);
+    return by_rows<E, BITS, 256>(ctx, w, max_len, stream);
 }
 
 template <typename E>
