@@ -125,6 +125,30 @@ __device__ __forceinline__ void numbers(const char *from, const uint8_t *exp, fl
         for (int i = 0; i < N; ++i) to[i] = (float)((const E *)from)[i];
 }
 
+__device__ __forceinline__ int64_t uniform(int64_t x)
+{
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
+
+__device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p; }
+
+// 16 bytes a lane straight to LDS, a wavefront's beside each other from `to` on (the same for all lanes).  The compiler knows neither that the
+// load is under way nor when it has come: that is waited for by count.
+__device__ __forceinline__ void to_lds(uint32_t to, int off, const char *from)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(from) : "memory");
+}
+__device__ __forceinline__ void to_lds(uint32_t to, const char *from)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+}
+
+// the same of 4 bytes a lane
+__device__ __forceinline__ void to_lds_word(uint32_t to, int off, const char *from)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(off), "s"(from) : "memory");
+}
+
 constexpr int AT_THREADS = 256;
 constexpr int MAX_SPLITS = 64;
 

@@ -57,6 +57,29 @@ __device__ __forceinline__ Where where(const AttendArgs &a, const Seq &sq, const
 }
 
 // What a step needs: the keys of a head, and 16 rows (queries x query heads of the KV head) of it.
+// A head's rows 16 at a time: with up to 16 query heads a KV head as many tokens as fit, with more a part of one token's.  A lane's row then has
+// the same place in each, `at` behind the first: no division by the way.
+struct RowTiles {
+    int tokens, chunks, n;       // tokens of a row tile, or row tiles of a token; of a head
+    __device__ __forceinline__ RowTiles(int nq, int group)
+    {
+        tokens = group < 16 ? 16 / group : 1;
+        chunks = (group + 15) / 16;
+        n = (nq + tokens - 1) / tokens * chunks;
+    }
+};
+struct Place {
+    static constexpr int NO_RANK = INT_MAX;
+    int token, rank;             // of the row tile's; `rank` of those that may be missing, tokens or heads
+    int64_t at;                  // in numbers of a layout
+    __device__ __forceinline__ Place(int r, int group, const RowTiles &tiles, int64_t token_step, int64_t head_step)
+    {
+        token = r / group;                                        // (0 with 16 and more heads)
+        rank = group > 16 ? r : token < tiles.tokens ? token : NO_RANK;
+        at = rank < NO_RANK ? token * token_step + (r - token * group) * head_step : 0;
+    }
+};
+
 template <int BITS, int D>
 struct KeysOf {
     typename KeyPieces<BITS, D>::Piece k[BLOCKS][KeyPieces<BITS, D>::LOADS];
@@ -66,6 +89,14 @@ template <typename E, int D>
 struct RowsOf {
     typename Types<E>::x8 q[D / 32];
     float lse, unit;                 // unit: of the head's keys, of 8 bits
+};
+
+// 16 rows on their way to LDS, where each lane finds the pieces of its row.  They are asked for as rows lie in memory: a matrix operand's lanes beside
+// each other hold different rows, of which each load by itself is an access of its own.
+template <int D>
+struct RowsInLds {
+    static constexpr int CH = D / 8, LOADS = CH / 4, BYTES = 16 * CH * 16 + 256, RING = 3;
+    static __device__ __forceinline__ int piece(int r, int c) { return r * CH + (c ^ (r & (CH < 16 ? CH - 1 : 15))); }
 };
 
 template <typename E, int BITS, int D>
@@ -94,58 +125,72 @@ struct Weigher {
             }
         }
     }
-    __device__ __forceinline__ void ask_rows(RowsOf<E, D> &r, int head, int rt) const
+    // (few rows: all of a head; what is no row reads the first)
+    __device__ __forceinline__ void ask_rows(RowsOf<E, D> &r, int head, int64_t q_at, int64_t lse_at) const
     {
-        const int lane = threadIdx.x & 63, quad = lane >> 4, row = rt * 16 + (lane & 15), in = row < rows ? row : 0;
-        const int t = in / a.group, qhead = head * a.group + in % a.group;
-        const E *q = (const E *)a.q + (int64_t)(sq.q0 + t) * a.q_token + (int64_t)qhead * a.q_head;
+        const int quad = threadIdx.x >> 4 & 3;
+        const E *q = (const E *)a.q + (int64_t)sq.q0 * a.q_token + (int64_t)head * a.group * a.q_head + q_at;
 #pragma unroll
         for (int s = 0; s < D / 32; ++s) r.q[s] = eight(q + Pieces::place(s, quad));
-        r.lse = a.lse[(int64_t)(sq.q0 + t) * a.n_heads + qhead];
-        r.unit = 1.0f;
-        if constexpr (BITS == 8) {
-            const float unit = (a.k_scale ? a.k_scale + a.layer * a.kv.n_heads : (const float *)a.zeros)[a.k_scale ? head : 0];
-            r.unit = a.k_scale ? unit : 1.0f;
-        }
+        r.lse = a.lse[(int64_t)sq.q0 * a.n_heads + (int64_t)head * a.group + lse_at];
+        r.unit = unit_of(head);
+    }
+    __device__ __forceinline__ float unit_of(int head) const
+    {
+        if constexpr (BITS != 8) return 1.0f;
+        const float unit = (a.k_scale ? a.k_scale + a.layer * a.kv.n_heads : (const float *)a.zeros)[a.k_scale ? head : 0];
+        return a.k_scale ? unit : 1.0f;
+    }
+    struct Operands {
+        typedef uint32_t Words __attribute__((ext_vector_type(4)));
+        Words x[BLOCKS][D / 32];
+    };
+    __device__ __forceinline__ void operands(Operands &o, const KeysOf<BITS, D> &k) const
+    {
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int l = 0; l < Pieces::LOADS; ++l)
+#pragma unroll
+                for (int j = 0; j < Pieces::EACH; ++j)
+                    o.x[b][Pieces::EACH * l + j] = __builtin_bit_cast(typename Operands::Words, Pieces::template operand<E>(k.k[b][l], k.e[b][l], j));
     }
     // scores of the keys (a lane: keys 16 b + 4 quad + i) with the rows (its column)
-    __device__ __forceinline__ void scores(const KeysOf<BITS, D> &k, const RowsOf<E, D> &r, f32x4 (&s)[BLOCKS]) const
+    __device__ __forceinline__ void scores(const Operands &k, const RowsOf<E, D> &r, f32x4 (&s)[BLOCKS]) const
     {
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) {
             s[b] = f32x4{};
 #pragma unroll
-            for (int l = 0; l < Pieces::LOADS; ++l)
-#pragma unroll
-                for (int j = 0; j < Pieces::EACH; ++j) s[b] = mfma16(Pieces::template operand<E>(k.k[b][l], k.e[b][l], j), r.q[Pieces::EACH * l + j], s[b]);
+            for (int x = 0; x < D / 32; ++x) s[b] = mfma16(__builtin_bit_cast(typename Types<E>::x8, k.x[b][x]), r.q[x], s[b]);
         }
     }
-    __device__ __forceinline__ void add(const f32x4 (&s)[BLOCKS], float lse, float unit, int rt, int y0, uint32_t there)
+    // t: this lane's row's token, counts: whether there is such a row; t_first, t_last: those of all lanes
+    __device__ __forceinline__ void add(const f32x4 (&s)[BLOCKS], float lse, float unit, int t, bool counts, int t_first, int t_last, int y0, uint32_t there)
     {
-        const int lane = threadIdx.x & 63, quad = lane >> 4, row = rt * 16 + (lane & 15);
+        const int quad = threadIdx.x >> 4 & 3, end = y0 + KEYS - 1;
         const bool tree = a.parent != nullptr;
         const float sc = a.scale * unit;
         // as in attention the factor is no 0: a score of -infinity stays one
-        const float c = copysignf(fmaxf(fabsf(sc), 1e-37f), sc);
-        const int t_first = rt * 16 / a.group, t_last = (rt * 16 + 15) / a.group, end = y0 + KEYS - 1;
-        const int first = tree ? sq.base - 1 : sq.base + t_first, last = tree ? sq.len : sq.base + (t_last < sq.nq ? t_last : sq.nq - 1);
-        const bool counts = row < rows && __builtin_fabsf(lse) < __builtin_inff();
+        const float c = copysignf(fmaxf(fabsf(sc), 1e-37f), sc) * LOG2E, less = -lse * LOG2E;
+        const int first = tree ? sq.base - 1 : sq.base + t_first, last = tree ? sq.len : sq.base + t_last;
+        counts = counts && __builtin_fabsf(lse) < __builtin_inff();
         if (there == 0xffffffffu && end <= first && (a.window <= 0 || end < a.n_sink || last - y0 < a.window)) {
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(s[b][x], c, -lse) * LOG2E);
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s[b][x], c, less));
                     sum[b][x] += counts ? p : 0.0f;
                 }
         } else {
-            const Sight view = sight(a, sq, row / a.group, s_depth, s_anc);
+            const Sight view = sight(a, sq, t, s_depth, s_anc);
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     const int k = b * 16 + quad * 4 + x;
-                    const float p = __builtin_amdgcn_exp2f(fmaf(s[b][x], c, -lse) * LOG2E);
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s[b][x], c, less));
                     sum[b][x] += counts && ((there >> k) & 1) && view.sees(y0 + k) ? p : 0.0f;
                 }
         }
@@ -169,23 +214,48 @@ struct Weigher {
 // FEW: up to 16 rows a KV head, bound by the keys' bytes.  A wavefront takes 32 keys and all heads, so that its sums need no other's; two
 // heads' keys are under way.  128 sequences over some 4000 tokens, 8 KV heads of 128: 264 us, 3.9 TB/s of keys (with the workgroup's wavefronts on
 // a head each and their sums joined in LDS 303; at three wavefronts a SIMD 328, as the keys under way do not fit their registers).
-// Else the wavefronts have the same 32 keys and divide heads and rows, 16 rows under way while weights are worked out, and their sums are
-// added in LDS: there are rows for many steps, and as few keys as possible a workgroup fill the chip.  What it does is exponentials, 4 for 16
-// products of a lane and mask tests at sequences' ends.  The last 32 queries of 7 prompts of some 6000 tokens, 32 heads of 128: 75 us (95 with 128
-// keys a workgroup; 64 keys a wavefront 74, and 96 at three wavefronts a SIMD; this at two 78).
+// Else the wavefronts have the same 32 keys and divide heads and rows, 16 rows a step, and their sums are added in LDS: there are rows for many
+// steps, and as few keys as possible a workgroup fill the chip.  Rows come through LDS, two steps ahead, and a head's keys are made operands
+// once.  What it does is exponentials and what goes with them, 8 a lane for 8 matrix instructions, and the wait for a head's first keys.  The last 32 queries of 7
+// prompts of some 6000 tokens, 32 heads of 128: 58 us at three wavefronts a SIMD, 67 at two; 75 with rows straight to registers, of which a load is an
+// access for each of 64 lanes and every step waited for all loads; 95 with 128 keys a workgroup.
+// a head and one of its row tiles
+struct Step {
+    int head, t0, chunk;
+    __device__ __forceinline__ Step(int u, const RowTiles &tiles) : head(u / tiles.n), t0(u % tiles.n / tiles.chunks * tiles.tokens), chunk(u % tiles.chunks) {}
+    __device__ __forceinline__ bool first() const { return (t0 | chunk) == 0; }
+    // rows, or heads, that are left from here on
+    __device__ __forceinline__ int left(int nq, int group) const { return group > 16 ? group - chunk * 16 : nq - t0; }
+    // (behind the last one the first of the last head again)
+    __device__ __forceinline__ void next(const RowTiles &tiles, int nq, int heads)
+    {
+        if (++chunk < tiles.chunks) return;
+        chunk = 0;
+        t0 += tiles.tokens;
+        if (t0 < nq) return;
+        t0 = 0;
+        head += head + 1 < heads;
+    }
+};
+
 template <typename E, int BITS, int D, bool FEW>
 __global__ __launch_bounds__(WG_THREADS, D == 256 ? 1 : FEW ? 2 : 3) void hx_weigh_kernel(WeighArgs w)
 {
     constexpr int TILE = FEW ? KEYS * WG_WAVES : KEYS;
     using Self = Weigher<E, BITS, D>;
     extern __shared__ __align__(16) char smem[];
+    __shared__ __align__(16) char s_rows[FEW ? 1 : WG_WAVES][RowsInLds<D>::RING][FEW ? 16 : RowsInLds<D>::BYTES];
     int *s_depth = (int *)smem + HX_MAX_DRAFTS;
     uint32_t *s_anc = (uint32_t *)(s_depth + HX_MAX_DRAFTS);
     const AttendArgs &a = w.a;
     const KvView &kv = a.kv;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), quad = lane >> 4, col = lane & 15;
     const int i = blockIdx.x % a.n, part = blockIdx.x / a.n, H = kv.n_heads;
-    const Seq sq = sequence(a, i * H);
+    Seq sq = sequence(a, i * H);
+    sq.q0 = __builtin_amdgcn_readfirstlane(sq.q0);
+    sq.nq = __builtin_amdgcn_readfirstlane(sq.nq);
+    sq.len = __builtin_amdgcn_readfirstlane(sq.len);
+    sq.base = __builtin_amdgcn_readfirstlane(sq.base);
     const Extent ex = extent<TILE>(a, sq, 0, sq.nq - 1);
     if (!sq.ok) { if (tid == 0 && part == 0 && (!sq.there || sq.nq > 0)) hx_raise(kv.status, HX_ERR_INDEX); return; }
     if (sq.nq == 0 || part >= ex.n) return;
@@ -194,6 +264,19 @@ __global__ __launch_bounds__(WG_THREADS, D == 256 ? 1 : FEW ? 2 : 3) void hx_wei
     const int64_t page_bytes = ((int64_t)H << kv.shift) * ROW<BITS, D>, here = (int64_t)a.layer * kv.n_pages * page_bytes;
     Self g{a, sq, (const char *)kv.k + here, BITS == 4 ? a.k_exp + here / 16 : nullptr, (int64_t)ROW<BITS, D> << kv.shift, sq.nq * a.group, s_depth, s_anc, {}};
     float *to = w.weight + (a.row ? a.row[i] : i) * w.pitch;
+    // where the rows of a row tile lie that this lane asks for, in bytes, if they may be read 16 bytes at a time and are not far apart
+    const RowTiles tiles(sq.nq, a.group);
+    const Place mine(col, a.group, tiles, a.n_heads, 1);
+    const bool wide = a.q_wide && a.q_token >= 0 && a.q_head >= 0 && a.q_token < 1 << 24 && a.q_head < 1 << 24;
+    int near[RowsInLds<D>::LOADS], far[RowsInLds<D>::LOADS], rank[RowsInLds<D>::LOADS];
+#pragma unroll
+    for (int j = 0; j < RowsInLds<D>::LOADS; ++j) {
+        const int r = (j * 64 + lane) / RowsInLds<D>::CH;
+        const Place p(r, a.group, tiles, a.q_token, a.q_head);
+        near[j] = (RowsInLds<D>::piece(r, lane % RowsInLds<D>::CH) - r * RowsInLds<D>::CH) * 16;
+        far[j] = (int)p.at * 2;
+        rank[j] = p.rank;
+    }
     for (int tile = part; tile < ex.n; tile += w.each) {
         const int y0 = (tile < ex.sink_tiles ? tile : tile - ex.sink_tiles + ex.lo_tile) * TILE + (FEW ? wave * KEYS : 0);
         const Where at = where<BITS, D>(a, sq, ex, y0, page_bytes);
@@ -206,16 +289,21 @@ __global__ __launch_bounds__(WG_THREADS, D == 256 ? 1 : FEW ? 2 : 3) void hx_wei
             KeysOf<BITS, D> k0, k1;
             RowsOf<E, D> r0, r1;
             g.ask_keys(k0, at, 0, true);
-            g.ask_rows(r0, 0, 0);
+            const int t = col / a.group;
+            const bool is_row = col < g.rows;
+            const int64_t q_at = is_row ? t * a.q_token + (col - t * a.group) * a.q_head : 0, lse_at = is_row ? (int64_t)t * a.n_heads + (col - t * a.group) : 0;
+            g.ask_rows(r0, 0, q_at, lse_at);
             g.ask_keys(k1, at, 1, H > 1);
-            g.ask_rows(r1, H > 1 ? 1 : 0, 0);
+            g.ask_rows(r1, H > 1 ? 1 : 0, q_at, lse_at);
             auto step = [&](KeysOf<BITS, D> &k, RowsOf<E, D> &r, int head) {
                 f32x4 s[BLOCKS];
-                g.scores(k, r, s);
+                typename Self::Operands now;
+                g.operands(now, k);
+                g.scores(now, r, s);
                 const float lse = r.lse, unit = r.unit;
                 g.ask_keys(k, at, head + 2, head + 2 < H);
-                g.ask_rows(r, head + 2 < H ? head + 2 : head, 0);
-                g.add(s, lse, unit, 0, y0, at.there);
+                g.ask_rows(r, head + 2 < H ? head + 2 : head, q_at, lse_at);
+                g.add(s, lse, unit, t, is_row, 0, sq.nq - 1, y0, at.there);
             };
             // (a step that may be left out would have all loads waited for)
             int head = 0;
@@ -226,29 +314,66 @@ __global__ __launch_bounds__(WG_THREADS, D == 256 ? 1 : FEW ? 2 : 3) void hx_wei
             if (head < H) step(k0, r0, head);
             g.add_up();
         } else {
-            const int row_tiles = (g.rows + 15) / 16, steps = H * row_tiles;
-            const int u0 = (int)((int64_t)steps * wave / WG_WAVES), u1 = (int)((int64_t)steps * (wave + 1) / WG_WAVES);
-            for (int u = u0; u < u1;) {
-                const int head = u / row_tiles, rt0 = u % row_tiles, rt1 = (head + 1) * row_tiles <= u1 ? row_tiles : rt0 + u1 - u;
-                KeysOf<BITS, D> k;
-                RowsOf<E, D> r0, r1;
-                g.ask_keys(k, at, head, true);
-                g.ask_rows(r0, head, rt0);
-                g.ask_rows(r1, head, rt0 + 1 < rt1 ? rt0 + 1 : rt0);
-                auto step = [&](RowsOf<E, D> &r, int rt) {
-                    f32x4 s[BLOCKS];
-                    g.scores(k, r, s);
-                    const float lse = r.lse, unit = r.unit;
-                    g.ask_rows(r, head, rt + 2 < rt1 ? rt + 2 : rt);
-                    g.add(s, lse, unit, rt, y0, at.there);
+            using Q = RowsInLds<D>;
+            const int steps = H * tiles.n, u0 = (int)((int64_t)steps * wave / WG_WAVES), u1 = (int)((int64_t)steps * (wave + 1) / WG_WAVES);
+            if (u0 < u1) {
+                Step to(u0, tiles), from = to;
+                int put = 0, get = 0;
+                auto ask = [&] {
+                    char *slot = s_rows[wave][put];
+                    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(slot));
+                    const int left = to.left(sq.nq, a.group);
+                    const int64_t token = sq.q0 + to.t0, qhead = to.head * a.group + to.chunk * 16;
+                    const E *q = (const E *)a.q + token * a.q_token + qhead * a.q_head;
+                    if (wide)
+#pragma unroll
+                        for (int j = 0; j < Q::LOADS; ++j) to_lds(lds + j * 1024, near[j] + (rank[j] < left ? far[j] : 0), (const char *)q);
+                    else
+                        for (int j = 0; j < Q::LOADS; ++j) {
+                            const int r = (j * 64 + lane) / Q::CH, c = Q::piece(r, lane % Q::CH) - r * Q::CH;
+                            const Place p(r, a.group, tiles, a.q_token, a.q_head);
+                            *(typename Types<E>::x8 *)(slot + j * 1024 + lane * 16) = eight(q + (p.rank < left ? p.at : 0) + c * 8);
+                        }
+                    to_lds_word(lds + Q::LOADS * 1024, mine.rank < left ? (int)mine.at * 4 : 0, (const char *)(a.lse + token * a.n_heads + qhead));
+                    put = put + 1 < Q::RING ? put + 1 : 0;
+                    to.next(tiles, sq.nq, H);              // (always as many loads are under way)
                 };
-                int rt = rt0;
-                for (; rt + 1 < rt1; rt += 2) {
-                    step(r0, rt);
-                    step(r1, rt + 1);
+#pragma unroll
+                for (int x = 0; x < Q::RING - 1; ++x) ask();
+                for (int u = u0; u < u1;) {
+                    float unit = g.unit_of(from.head);
+                    typename Self::Operands k;
+                    {
+                        KeysOf<BITS, D> stored;
+                        g.ask_keys(stored, at, from.head, true);
+                        g.operands(k, stored);
+                    }
+                    // (waited for here, or the compiler would at every step, and for the rows under way)
+                    asm volatile("" : "+v"(unit));
+#pragma unroll
+                    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                        for (int x = 0; x < D / 32; ++x) asm volatile("" : "+v"(k.x[b][x]));
+#pragma unroll 1
+                    do {
+                        // these rows are there, and what was read where the next will be has come
+                        if (wide) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((Q::RING - 2) * (Q::LOADS + 1)) : "memory");
+                        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+                        ask();
+                        const char *slot = s_rows[wave][get];
+                        RowsOf<E, D> r;
+#pragma unroll
+                        for (int s = 0; s < D / 32; ++s) r.q[s] = *(const typename Types<E>::x8 *)(slot + Q::piece(col, KeyPieces<BITS, D>::place(s, quad) / 8) * 16);
+                        r.lse = *(const float *)(slot + Q::LOADS * 1024 + col * 4);
+                        f32x4 s[BLOCKS];
+                        g.scores(k, r, s);
+                        const int t_last = from.t0 + tiles.tokens < sq.nq ? from.t0 + tiles.tokens - 1 : sq.nq - 1;
+                        g.add(s, r.lse, unit, from.t0 + mine.token, mine.rank < from.left(sq.nq, a.group), from.t0, t_last, y0, at.there);
+                        get = get + 1 < Q::RING ? get + 1 : 0;
+                        from.next(tiles, sq.nq, H);
+                    } while (++u < u1 && !from.first());
                 }
-                if (rt < rt1) step(r0, rt);
-                u += rt1 - rt0;
+                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             }
             g.add_up();
             __shared__ float s_sum[WG_WAVES][KEYS];

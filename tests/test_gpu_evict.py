@@ -75,6 +75,14 @@ def test_weights_of_head_layouts(ctx, heads, group):
     check_weigh(ctx, [5, 90, 200], [1, 3, 2], heads=heads, group=group)
 
 
+@pytest.mark.parametrize("heads,group", [(1, 1), (5, 3), (2, 7), (3, 16), (1, 17), (2, 40)])
+@pytest.mark.parametrize("dim,cache", [(64, "e4m3"), (128, "bf16"), (256, "e2m1")])
+@pytest.mark.parametrize("wide", [True, False])
+def test_weights_of_many_rows_and_head_layouts(ctx, heads, group, dim, cache, wide):
+    """Rows that end inside a block of 16, heads that end inside one, fewer blocks than wavefronts, and queries that lie anyhow."""
+    check_weigh(ctx, [17, 100, 75], [17, 33, 20], heads=heads, group=group, dim=dim, cache=cache, wide=wide, seed=group)
+
+
 @pytest.mark.parametrize("window,sinks", [(1, 0), (2, 1), (17, 5), (64, 70), (65, 0), (500, 1000)])
 def test_weights_of_windows_and_sinks(ctx, window, sinks):
     check_weigh(ctx, [1, 40, 64, 129, 300, 411], [1] * 6, window=window, sinks=sinks)
