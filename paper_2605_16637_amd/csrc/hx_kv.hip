@@ -228,7 +228,7 @@ __device__ __forceinline__ uint32_t to_e4m3(const float *x, float scale)
 
 // 8 of 32 numbers, of which 4 lanes beside each other have a quarter each, as codes of 4 bits; *exp: their scale's byte.
 // 2^e is the least that 6 of it reach the largest with: 6 is 1.5 * 4, so the largest's own exponent decides, and whether its fraction is more than 1.5.
-// A number over a power of 2 is exact, and so are comparisons with the middles between codes; a middle goes to the even code.
+// The matrix unit's own conversion over a power of 2 rounds to the nearest code, a middle to the even one, and what lies beyond 6 to 6.
 __device__ __forceinline__ uint32_t to_e2m1(const float *x, int *exp)
 {
     uint32_t top = 0;
@@ -246,14 +246,12 @@ __device__ __forceinline__ uint32_t to_e2m1(const float *x, int *exp)
     int e = (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x400000u ? 1 : 0);
     e = e < E2M1_LEAST ? E2M1_LEAST : e > E2M1_MOST ? E2M1_MOST : e;
     const bool nan = top > 0x7f800000u;
-    const float down = __uint_as_float((uint32_t)(254 - e) << 23);
+    const float unit = __uint_as_float((uint32_t)e << 23);
     uint32_t w = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float y = fabsf(x[i]) * down;
-        const uint32_t code = (y > 0.25f) + (y >= 0.75f) + (y > 1.25f) + (y >= 1.75f) + (y > 2.5f) + (y >= 3.5f) + (y > 5.0f);
-        w |= (code | (__float_as_uint(x[i]) >> 31 << 3)) << (4 * i);
-    }
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], unit, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], unit, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], unit, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], unit, 3);
     *exp = nan ? E2M1_NAN : e;
     return nan ? 0 : w;
 }
@@ -268,6 +266,29 @@ struct WriteArgs {
     uint8_t *k_exp, *v_exp;
     bool aligned;            // 8 numbers of a source can be loaded at once
 };
+
+// The last entry that begins with token q or before it, the first if none does; all lanes of a wavefront take part, whose tokens rise.  The
+// first lane's is found 64 entries at a time, a wait for memory each; only where another's lies further on it goes on by halves.
+__device__ __forceinline__ int entry_of(const int32_t *tok_ptr, int n, int64_t q)
+{
+    const int lane = threadIdx.x & (HX_WAVE - 1), q0 = __builtin_amdgcn_readfirstlane((int)q);
+    int lo = 0, end = n;
+    while (end - lo > 1) {
+        const int step = (end - lo + HX_WAVE - 1) / HX_WAVE, at = lo + lane * step;
+        const unsigned long long up_to = __builtin_amdgcn_ballot_w64(at < end && tok_ptr[at < end ? at : lo] <= q0);
+        const int count = up_to == ~0ull ? HX_WAVE : __builtin_ctzll(~up_to);
+        if (count == 0) break;
+        lo += (count - 1) * step;
+        end = lo + step < end ? lo + step : end;
+    }
+    int mine = lo, hi = n - 1;
+    if (lo < hi && tok_ptr[lo + 1] <= q)
+        while (mine < hi) {
+            const int mid = (mine + hi + 1) >> 1;
+            if (tok_ptr[mid] <= q) mine = mid; else hi = mid - 1;
+        }
+    return mine;
+}
 
 // Of a row listed twice the first entry counts.  A wavefront looks for the rows of its lanes' entries among those listed before, 256 at a time
 // in registers, the next 256 under way; entries rise with the lanes.
@@ -303,24 +324,33 @@ __device__ __forceinline__ bool listed_before(const int32_t *row, int *x, int en
     return listed;
 }
 
-// 8 numbers of a key and of a value a thread; D of one byte: e4m3, or two numbers of 4 bits.  2048 tokens of 64 rows, 8 heads of 128 (17 MB read and written):
-// 5.2 us in a graph of such calls, most of it the lookups before a thread's store (its sequence by bisection, row, length, page, count).  One
-// token each of 256 rows 3.8, of 1024 5.6; of these the look for rows listed twice takes 0.2, 0.3 and 1.1.
+// 8 numbers of a key and of a value a thread; D of one byte: e4m3, or two numbers of 4 bits.  2048 tokens of 64 rows, 8 heads of 128 (17 MB read and
+// written): 4.8 us in a graph of such calls, most of it the lookups before a thread's store (its sequence, row, length, page, count), under which
+// its numbers are on their way; 5.2 with a bisection for the sequence and the numbers behind it.  One token each of 256 rows 3.3, of 1024 4.7; of these the look
+// for rows listed twice takes 0.2, 0.3 and 1.1.  To 4 bits, 14454 tokens of prompts (59 MB read, 16 written): 22 us, 3.4 TB/s, where a wavefront's some 520
+// instructions take as long; 31 with codes by comparison with the middles, twice the instructions.
 template <typename S, typename D>
 __global__ __launch_bounds__(CP_THREADS) void hx_kv_write_kernel(WriteArgs a)
 {
     const KvView &kv = a.kv;
     const int per_head = kv.dim / 8, per = per_head * kv.n_heads;
-    const int64_t u = (int64_t)blockIdx.x * CP_THREADS + threadIdx.x;
-    const int64_t q = u / per;
-    const int c = (int)(u % per), h = c / per_head, d = (c % per_head) * 8;
+    const uint32_t u = blockIdx.x * (uint32_t)CP_THREADS + threadIdx.x;      // (a grid has fewer than 2^32 threads)
+    const int64_t q = u / (uint32_t)per;
+    const int c = (int)(u % (uint32_t)per), h = c / per_head, d = (c % per_head) * 8;
+    // (the numbers come while their place is looked up; what is behind the last token reads the first)
+    const int64_t from = q < a.n_tok ? q * a.token_stride + h * a.head_stride + d : 0;
+    struct alignas(8 * sizeof(S) < 16 ? 8 * sizeof(S) : 16) Eight { S x[8]; } source[2];
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        const S *src = (const S *)(which ? a.v : a.k) + from;
+        if (a.aligned) source[which] = *(const Eight *)src;
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) source[which].x[i] = src[i];
+    }
     int rows[LISTED_EACH];
     listed_ask(a.row, 0, a.n, rows);
-    int lo = 0, hi = a.n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.tok_ptr[mid] <= q) lo = mid; else hi = mid - 1;
-    }
+    const int lo = entry_of(a.tok_ptr, a.n, q);
     const int first = a.tok_ptr[lo], last = a.tok_ptr[lo + 1], r = a.row[lo];
     // an entry is written as a whole or not at all
     bool ok = first >= 0 && first <= q && q < last && last <= a.n_tok && r >= 0 && r < kv.rows;
@@ -332,16 +362,10 @@ __global__ __launch_bounds__(CP_THREADS) void hx_kv_write_kernel(WriteArgs a)
     const bool again = listed_before(a.row, rows, lo, r);
     if (q >= a.n_tok) return;
     if (!ok || again) { if (c == 0) hx_raise(kv.status, HX_ERR_INDEX); return; }
-    const int64_t from = q * a.token_stride + h * a.head_stride + d;
     const int64_t to = hx_kv_at(kv, a.layer, page, h, (int)(pos & ((1 << kv.shift) - 1))) + d;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-        const S *src = (const S *)(which ? a.v : a.k) + from;
-        struct alignas(8 * sizeof(S) < 16 ? 8 * sizeof(S) : 16) Eight { S x[8]; } e;
-        if (a.aligned) e = *(const Eight *)src;
-        else
-#pragma unroll
-            for (int i = 0; i < 8; ++i) e.x[i] = src[i];
+        const Eight &e = source[which];
         if constexpr (std::is_same_v<D, E2m1>) {
             float x[8];
             int exp;
@@ -378,36 +402,38 @@ struct ReadArgs {
     bool aligned;            // 8 numbers can be stored at once
 };
 
-// 8 numbers of a key and of a value a thread, as the write.
+// 8 numbers of a key and of a value a thread, as the write.  From 4 bits, 14454 tokens (16 MB read, 59 written): 22 us, 3.4 TB/s; 24.4 with codes taken
+// apart bit by bit and the value asked for behind the key.
 template <typename S, typename D>
 __global__ __launch_bounds__(CP_THREADS) void hx_kv_read_kernel(ReadArgs a)
 {
     const KvView &kv = a.kv;
     const int per_head = kv.dim / 8, per = per_head * kv.n_heads;
-    const int64_t u = (int64_t)blockIdx.x * CP_THREADS + threadIdx.x;
-    const int64_t q = u / per;
-    if (q >= a.n_tok) return;
-    const int c = (int)(u % per), h = c / per_head, d = (c % per_head) * 8;
-    int lo = 0, hi = a.n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.tok_ptr[mid] <= q) lo = mid; else hi = mid - 1;
-    }
+    const uint32_t u = blockIdx.x * (uint32_t)CP_THREADS + threadIdx.x;      // (a grid has fewer than 2^32 threads)
+    const int64_t q = u / (uint32_t)per;
+    const int c = (int)(u % (uint32_t)per), h = c / per_head, d = (c % per_head) * 8;
+    const int lo = entry_of(a.tok_ptr, a.n, q);
     const int first = a.tok_ptr[lo], last = a.tok_ptr[lo + 1], r = a.row[lo];
     bool ok = first >= 0 && first <= q && q < last && last <= a.n_tok && r >= 0 && r < kv.rows;
     const int len = ok ? kv.len[r] : 0;
     ok = ok && hx_row_ok(kv, r, len) && last - first <= len;
+    if (q >= a.n_tok) return;
     if (!ok) { if (c == 0) hx_raise(kv.status, HX_ERR_INDEX); return; }
     const int64_t pos = (int64_t)len - last + q;
     int page = hx_row(kv, r)[pos >> kv.shift];
     if (page >= kv.n_pages) { if (c == 0) hx_raise(kv.status, HX_ERR_INDEX); page = -1; }
     const int64_t from = page < 0 ? 0 : hx_kv_at(kv, a.layer, page, h, (int)(pos & ((1 << kv.shift) - 1))) + d;
     const int64_t to = q * a.token_stride + h * a.head_stride + d;
+    float both[2][8] = {};
+    if (page >= 0)
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            const float *scales = which ? a.v_scale : a.k_scale;
+            stored<S, 8>(which ? kv.v : kv.k, which ? a.v_exp : a.k_exp, scales ? scales[a.layer * kv.n_heads + h] : 1.0f, from, both[which]);
+        }
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-        const float *scales = which ? a.v_scale : a.k_scale;
-        float x[8] = {};
-        if (page >= 0) stored<S, 8>(which ? kv.v : kv.k, which ? a.v_exp : a.k_exp, scales ? scales[a.layer * kv.n_heads + h] : 1.0f, from, x);
+        const float (&x)[8] = both[which];
         D *at = (D *)(which ? a.v : a.k) + to;
         struct alignas(8 * sizeof(D) < 16 ? 8 * sizeof(D) : 16) Eight { D x[8]; } e;
 #pragma unroll

@@ -19,12 +19,13 @@ __device__ __forceinline__ void stored(const void *pool, const uint8_t *exps, fl
         struct alignas(N / 2) Words { uint32_t w[N / 8]; } e = *(const Words *)((const char *)pool + at / 2);
         const int byte = exps[at / E2M1_GROUP];
         const float unit = byte == E2M1_NAN ? __builtin_nanf("") : __uint_as_float((uint32_t)byte << 23);
+        typedef float Two __attribute__((ext_vector_type(2)));
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const uint32_t w = e.w[i / 8] >> (4 * (i % 8)), code = w & 7;
-            // codes 2 to 7 are one bit of exponent over one of fraction more each: 1 to 6; 0 and 0.5 lie below
-            const float size = code < 2 ? 0.5f * code : __uint_as_float((code << 22) + (126u << 23));
-            x[i] = (w & 8 ? -size : size) * unit;
+        for (int i = 0; i < N / 8; ++i) {
+            const Two y[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(e.w[i], unit, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(e.w[i], unit, 1),
+                              __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(e.w[i], unit, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(e.w[i], unit, 3)};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[8 * i + j] = y[j / 2][j % 2];
         }
     } else if constexpr (sizeof(S) == 1) {
         struct alignas(N < 16 ? N : 16) Words { uint32_t w[N / 4]; } e = *(const Words *)((const char *)pool + at);
