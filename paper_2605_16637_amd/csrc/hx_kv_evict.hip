@@ -8,12 +8,14 @@
 namespace {
 
 constexpr int EV_THREADS = 512, EV_WAVES = EV_THREADS / HX_WAVE;
+constexpr int EV_FULL = 2;                 // workgroups a CU from which the move is not divided further
 constexpr int EV_AHEAD = 8;                // tokens that a thread moves at once
 
 struct EvictArgs {
     KvView kv;
     KvPlanes planes;
     int n, n_keep, n_first, n_last, keep_pages;
+    int slices;              // of a token's bytes, in the move
     const int32_t *row;
     float *weight;
     int64_t pitch;           // of a row's weights
@@ -158,12 +160,12 @@ __device__ __forceinline__ int page_after(const EvictArgs &a, int i, int b, cons
     return f < 0 ? table[b] : a.list[a.first[i] + f];
 }
 
-// Workgroup (i, part): a head of one array of a layer, or, first, the row's weights.  Tokens move to lower positions, in order: a round's tokens are all
+// Workgroup (i, part): a head of one array of a layer, of few such a slice of its tokens' bytes, or, first, the row's weights.  Tokens move to lower positions, in order: a round's tokens are all
 // loaded before any of them is stored, and later rounds load only what lies behind what has been stored.
 __global__ __launch_bounds__(EV_THREADS) void hx_kv_evict_move_kernel(EvictArgs a)
 {
     const KvView &kv = a.kv;
-    const int heads = kv.n_heads, parts = 1 + a.planes.n * kv.n_layers * heads, i = blockIdx.x / parts, part = blockIdx.x % parts, tid = threadIdx.x;
+    const int heads = kv.n_heads, parts = 1 + a.planes.n * kv.n_layers * heads * a.slices, i = blockIdx.x / parts, part = blockIdx.x % parts, tid = threadIdx.x;
     const int n = a.stay[i], r = a.row[i];
     if (n < 0) return;
     const int32_t *kept = a.kept + (int64_t)i * a.n_keep;
@@ -189,7 +191,7 @@ __global__ __launch_bounds__(EV_THREADS) void hx_kv_evict_move_kernel(EvictArgs 
         return;
     }
     const int32_t *table = hx_row(kv, r);
-    const int head = (part - 1) % heads, which = (part - 1) / heads % a.planes.n, layer = (part - 1) / heads / a.planes.n, in_page = (1 << kv.shift) - 1;
+    const int slice = (part - 1) % a.slices, p = (part - 1) / a.slices, head = p % heads, which = p / heads % a.planes.n, layer = p / heads / a.planes.n, in_page = (1 << kv.shift) - 1;
     const Plane x = plane(a.planes, which);
     const int64_t head_bytes = (int64_t)x.row_bytes << kv.shift;
     char *at = x.at + ((int64_t)layer * kv.n_pages * heads + head) * head_bytes;
@@ -197,7 +199,9 @@ __global__ __launch_bounds__(EV_THREADS) void hx_kv_evict_move_kernel(EvictArgs 
     const int start = begin & ~in_page;
     by_width(x.row_bytes, [&](auto unit) {
         using U = decltype(unit);
-        const int pieces = x.row_bytes / (int)sizeof(U), slots = EV_THREADS / pieces, slot = tid / pieces, c = tid % pieces;      // (at most 128 pieces)
+        const int all = x.row_bytes / (int)sizeof(U), c0 = all * slice / a.slices, pieces = all * (slice + 1) / a.slices - c0;       // (at most 128)
+        if (pieces == 0) return;
+        const int slots = EV_THREADS / pieces, slot = tid / pieces, c = c0 + tid % pieces;
         for (int j0 = start; j0 < n; j0 += slots * EV_AHEAD) {
             U y[EV_AHEAD];
             int64_t to[EV_AHEAD];
@@ -253,7 +257,10 @@ extern "C" int hx_kv_evict(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs
     HX_REQUIRE(ctx, ((uintptr_t)weight & 3) == 0, HX_ERR_INVALID_ARG, "weights are not aligned to their type");
     HX_REQUIRE(ctx, kv.rows > 0, HX_ERR_INVALID_ARG, "%d rows asked for of no sequences", n);
     const KvPlanes planes = hx_kv_planes(pool);
-    const int64_t parts = 1 + (int64_t)planes.n * kv.n_layers * kv.n_heads;
+    // a round is a chain of lookups, and a slice of half the bytes takes twice the tokens in one: slices until the chip is full, of no less than 64 bytes.
+    int slices = 1;
+    while (2 * (int64_t)n * planes.n * kv.n_layers * kv.n_heads * slices <= EV_FULL * ctx->num_cu && planes.row_bytes[0] >= 128 * slices) slices *= 2;
+    const int64_t parts = 1 + (int64_t)planes.n * kv.n_layers * kv.n_heads * slices;
     HX_REQUIRE(ctx, n * parts <= hx_most_groups(EV_THREADS), HX_ERR_SHAPE, "%d rows of %d layers of %d heads in one call", n, kv.n_layers, kv.n_heads);
     const int keep_pages = (int)(((int64_t)n_keep + (1 << kv.shift) - 1) >> kv.shift);
     HxDeviceGuard guard(ctx->device);
@@ -263,7 +270,7 @@ extern "C" int hx_kv_evict(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs
     if (int rc = hx_scratch(ctx, hx_serve(ctx)->kv, words * sizeof(int32_t), stream)) return rc;
     int32_t *w = (int32_t *)hx_serve(ctx)->kv.p;
     const size_t N = n;
-    EvictArgs a{kv, planes, n, n_keep, n_first, n_last, keep_pages, row, weight, (int64_t)kv.max_pages << kv.shift,
+    EvictArgs a{kv, planes, n, n_keep, n_first, n_last, keep_pages, slices, row, weight, (int64_t)kv.max_pages << kv.shift,
                 kept ? kept : w + N * (4 + (size_t)keep_pages) + kv.n_pages, w, w + N, w + 2 * N, w + 3 * N, w + 4 * N, w + N * (4 + (size_t)keep_pages)};
     hx_kv_evict_select_kernel<<<n, EV_THREADS, 0, stream>>>(a);
     hx_kv_evict_plan_kernel<<<1, PL_THREADS, 0, stream>>>(a);
