@@ -8,6 +8,7 @@
 namespace {
 
 constexpr int EV_THREADS = 512, EV_WAVES = EV_THREADS / HX_WAVE;
+constexpr int EV_CACHE = 8192;              // tokens of a row whose weights are kept in LDS
 constexpr int EV_FULL = 2;                 // workgroups a CU from which the move is not divided further
 constexpr int EV_AHEAD = 8;                // tokens that a thread moves at once
 
@@ -50,6 +51,7 @@ __global__ __launch_bounds__(EV_THREADS) void hx_kv_evict_select_kernel(EvictArg
 {
     __shared__ NthState<uint32_t, EV_THREADS> s;
     __shared__ int s_count[EV_WAVES], s_count2[EV_WAVES];
+    __shared__ uint32_t s_key[EV_CACHE];
     const KvView &kv = a.kv;
     const int i = blockIdx.x, tid = threadIdx.x, r = a.row[i];
     bool bad = r < 0 || r >= kv.rows;
@@ -67,18 +69,27 @@ __global__ __launch_bounds__(EV_THREADS) void hx_kv_evict_select_kernel(EvictArg
     const int32_t *table = hx_row(kv, r);
     const float *weight = a.weight + r * a.pitch;
     auto there = [&](int y) { const int page = table[y >> kv.shift]; return page >= 0 && page < kv.n_pages; };
+    // 0: no page is there
+    auto look = [&](int y) { return there(y) ? weight_key(weight[y]) : 0; };
+    const bool cached = len <= EV_CACHE;
+    if (cached) {
+#pragma unroll 4
+        for (int y = tid; y < len; y += EV_THREADS) s_key[y] = look(y);
+        __syncthreads();
+    }
+    auto key_at = [&](int y) { return cached ? s_key[y] : look(y); };
     const int from = a.n_first, to = len - a.n_last;              // n_first + n_last <= n_keep < len
     int fixed = 0, all;
     for (int y0 = 0; y0 < a.n_first + a.n_last; y0 += EV_THREADS) {
         const int y = y0 + tid;
-        count_before(y < a.n_first + a.n_last && there(y < a.n_first ? y : to + y - a.n_first), s_count, &all);
+        count_before(y < a.n_first + a.n_last && key_at(y < a.n_first ? y : to + y - a.n_first) != 0, s_count, &all);
         fixed += all;
     }
     const int want = a.n_keep - fixed;
     uint32_t edge = ~0u;
     int equals = 0;
     if (want > 0) {
-        nth_largest([&](int y) { return there(y) ? weight_key(weight[y]) : 0; }, from, to, want, s);
+        nth_largest(key_at, from, to, want, s);
         edge = s.edge;
         equals = s.equals;
     }
@@ -86,9 +97,9 @@ __global__ __launch_bounds__(EV_THREADS) void hx_kv_evict_select_kernel(EvictArg
     int n = 0, same = 0, moves = INT32_MAX;
     for (int y0 = 0; y0 < len; y0 += EV_THREADS) {
         const int y = y0 + tid;
-        const bool here = y < len && there(y), between = y >= from && y < to;
-        if (y < len && table[y >> kv.shift] >= kv.n_pages) hx_raise(kv.status, HX_ERR_INDEX);
-        const uint32_t x = here && between ? weight_key(weight[y]) : 0;
+        const uint32_t key = y < len ? key_at(y) : 0;
+        const bool here = key != 0, between = y >= from && y < to;
+        const uint32_t x = between ? key : 0;
         const bool equal = x == edge && x > 0;
         const int rank = same + count_before(equal, s_count, &all);
         same += all;
@@ -101,6 +112,8 @@ __global__ __launch_bounds__(EV_THREADS) void hx_kv_evict_select_kernel(EvictArg
         }
     }
     for (int j = n + tid; j < a.n_keep; j += EV_THREADS) kept[j] = -1;
+    for (int b = tid; b < hx_pages_of(len, kv.shift); b += EV_THREADS)
+        if (table[b] >= kv.n_pages) hx_raise(kv.status, HX_ERR_INDEX);
 #pragma unroll
     for (int d = HX_WAVE / 2; d > 0; d >>= 1) { const int o = __shfl_xor(moves, d); moves = o < moves ? o : moves; }
     __syncthreads();
