@@ -314,7 +314,12 @@ __global__ __launch_bounds__(THREADS) void hx_top_pick_kernel(TopArgs t, int cac
     float over = INF, under = INF;                                 // `under` on the largest exact ones; all by their exact ones
     uint64_t edge = 0;
     int equals = 0, unsures = 0;
-    auto unsure = [&](int b) { return how == BLIND ? page_at(b) >= 0 : score_of(b) <= over && score_of(b) >= under; };
+    // (a page that is not there has a score of -infinity, which `under` may be of numbers near the type's lowest)
+    auto unsure = [&](int b) {
+        if (how == BLIND) return page_at(b) >= 0;
+        const float x = score_of(b);
+        return x <= over && x >= under && x > -INF;
+    };
     const int want = t.n_pages - fixed;
     if (!all && want > 0) {
 #pragma unroll

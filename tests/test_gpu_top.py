@@ -197,6 +197,26 @@ def test_equal_bounds_go_to_the_lowest_pages(ctx):
     check_top(ctx, [1500, 40], [1, 2], n_pages=9, n_first=1, n_last=2, T=2, change=same)
 
 
+def test_bounds_near_the_lowest_number(ctx):
+    """A score less what it may be off by is -infinity, the score of a page that is not there."""
+    import torch
+    heads, dim, T, n = 1, 64, 4, 90
+    c = lh.Cache(21, [n * T], T, heads, dim, "bf16", missing=[(0, 3), (0, 7), (0, 50)], bounds=True)
+    lo = torch.finfo(torch.bfloat16).min
+    c.pool["k"].zero_()
+    c.pool["k"][..., 0] = lo
+    c.pool["k"][..., 1] = -(2.0 ** 120 - 2.0 ** 112)                           # together some 2^112 from the lowest number of 32 bits
+    best = [int(c.table[c.where[0], b]) for b in (20, 60)]
+    c.pool["k"][:, best, :, :, 1] = 0.0
+    ctx.hx_kv_bound(c.pool, 1, c.seqs, sh.i32(c.where))
+    q = torch.zeros(1, 2, dim, dtype=torch.bfloat16, device="cuda:0")
+    q[..., :2] = 1.0
+    chosen = torch.zeros(1, 1, 8, dtype=torch.int32, device="cuda:0")
+    ctx.hx_attend_top(c.pool, 1, c.seqs, sh.i32([0, 1]), q, torch.zeros_like(q), max_q=1, n_pages=8, n_first=1, row=sh.i32(c.where), chosen=chosen)
+    assert lh.status(ctx) == 0
+    assert chosen[0, 0].tolist() == [0, 1, 2, 4, 5, 20, 60, n - 1]
+
+
 def test_bounds_that_are_infinite_or_no_number(ctx):
     def odd(c):
         """Keys of +-infinity in places where the query has a part or none, and NaN: of pages that may be chosen, or not."""
