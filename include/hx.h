@@ -810,7 +810,7 @@ int hx_kv_bound(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_kv_
  * -infinity, whose keys have no weight; a bound that is NaN is taken for
  * +infinity.  What is not chosen has no part in the result; what is has the part
  * that it has in hx_attend.  chosen: the numbers of the pages in their row,
- * rising, then -1.
+ * rising, then -1.  Of queries that are no sequence's nothing is written.
  * args->parent must be NULL and args->window 0; pool->bounds must hold the pages'
  * bounds.  Scratch: 12.25 bytes for each entry of a row, query and KV head, up to 256 MB
  * (more queries are taken in several parts), 4 for each page that is chosen.

@@ -180,11 +180,12 @@ __device__ __forceinline__ Seq sequence(const AttendArgs &a, int pair)
     const int i = pair / kv.n_heads;
     Seq s;
     if (a.picked) {
+        const int len = a.picked_len[pair];                      // -1: the query is no sequence's
         s.q0 = i;
-        s.nq = 1;
+        s.nq = len < 0 ? 0 : 1;
         s.there = s.ok = true;
-        s.len = a.picked_len[pair];
-        s.base = s.len - 1;
+        s.len = len < 0 ? 0 : len;
+        s.base = s.len - s.nq;
         s.table = a.picked + (int64_t)pair * a.picked_pages;
         return s;
     }

@@ -24,7 +24,7 @@ struct TopArgs {
 
 // A query's row: its pages up to its own, `own`.
 struct Place {
-    bool ok;
+    bool ok, none;                   // none: no sequence has such a query
     int pos, own;
     const int32_t *table;
 };
@@ -41,6 +41,7 @@ __device__ __forceinline__ Place place(const AttendArgs &a, int j)
     const Seq s = sequence(a, lo * a.kv.n_heads);
     Place p;
     p.ok = s.ok && j >= s.q0 && j < s.q0 + s.nq;
+    p.none = j < a.q_ptr[0] || j >= a.q_ptr[a.n];
     p.pos = p.ok ? s.base + j - s.q0 : 0;
     p.own = p.pos >> a.kv.shift;
     p.table = s.table;
@@ -262,6 +263,10 @@ __global__ __launch_bounds__(THREADS) void hx_top_pick_kernel(TopArgs t, int cac
     const Place p = place(a, j);
     int32_t *picked = t.picked + (int64_t)pair * t.n_pages;
     int32_t *chosen = t.chosen ? t.chosen + ((int64_t)j * kv.n_heads + head) * t.n_pages : nullptr;
+    if (p.none) {
+        if (tid == 0) t.picked_len[pair] = -1;
+        return;
+    }
     if (!p.ok) {
         if (tid == 0) { hx_raise(kv.status, HX_ERR_INDEX); picked[0] = -1; t.picked_len[pair] = 1; }
         if (chosen)

@@ -224,8 +224,8 @@ __global__ __launch_bounds__(EV_THREADS) void hx_kv_evict_move_kernel(EvictArgs 
                 const int at_k = j0 + k * slots + slot, j = slot < slots && at_k < n ? at_k : j0;
                 const int from = kept[j], old = table[from >> kv.shift], page = page_after(a, i, j >> kv.shift, table);
                 const bool moves = at_k == j && (from != j || page != old);
-                to[k] = moves ? page * heads * head_bytes + (int64_t)(j & in_page) * x.row_bytes + c * sizeof(U) : -1;
-                y[k] = *(const U *)(at + old * heads * head_bytes + (int64_t)(from & in_page) * x.row_bytes + c * sizeof(U));
+                to[k] = moves ? (int64_t)page * heads * head_bytes + (int64_t)(j & in_page) * x.row_bytes + c * sizeof(U) : -1;
+                y[k] = *(const U *)(at + (int64_t)old * heads * head_bytes + (int64_t)(from & in_page) * x.row_bytes + c * sizeof(U));
             }
             __syncthreads();
 #pragma unroll

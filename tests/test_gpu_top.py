@@ -297,6 +297,32 @@ def test_queries_and_rows_out_of_range(ctx):
     assert lh.status(ctx) == 0
 
 
+@pytest.mark.parametrize("group", [2, 40])
+def test_queries_of_no_sequence_are_left_as_they_were(ctx, group):
+    """A batch padded to more queries than its sequences have, as hx_attend takes it."""
+    import torch
+    c = lh.Cache(15, [60, 33], 8, 2, 64, "bf16", bounds=True)
+    ctx.hx_kv_bound(c.pool, 1, c.seqs, sh.i32(c.where))
+    q = lh.queries(12, 2 * group, 64, "bf16", 0)
+    ptr, call = sh.i32([2, 4, 7]), dict(max_q=3, row=sh.i32(c.where))
+    got, lse = torch.full((12, 2 * group, 64), 7.0, dtype=torch.bfloat16, device="cuda:0"), torch.full((12, 2 * group), 7.0, device="cuda:0")
+    want, want_lse = got.clone(), lse.clone()
+    chosen = torch.full((12, 2, 3), 99, dtype=torch.int32, device="cuda:0")
+    ctx.hx_attend_top(c.pool, 1, c.seqs, ptr, q, got, n_pages=3, chosen=chosen, lse=lse, **call)
+    ctx.hx_attend_top(c.pool, 1, c.seqs, sh.i32([0, 2, 5]), q[2:7], want[2:7], n_pages=3, lse=want_lse[2:7], **call)
+    assert lh.status(ctx) == 0
+    assert torch.equal(got, want) and torch.equal(lse, want_lse)
+    assert bool((chosen[:2] == 99).all()) and bool((chosen[7:] == 99).all()) and not bool((chosen[2:7] == 99).any())
+    ctx.hx_attend(c.pool, 1, c.seqs, ptr, q, got, lse=lse, **call)
+    assert lh.status(ctx) == 0 and bool((got[:2] == 7).all()) and bool((got[7:] == 7).all())
+    weight = torch.zeros(c.rows, c.table.shape[1] * 8, device="cuda:0")
+    ctx.hx_kv_weigh(c.pool, 1, c.seqs, ptr, q, lse, weight, **call)
+    assert lh.status(ctx) == 0
+    part = torch.zeros_like(weight)
+    ctx.hx_kv_weigh(c.pool, 1, c.seqs, sh.i32([0, 2, 5]), q[2:7], lse[2:7].contiguous(), part, **call)
+    assert torch.equal(weight, part)
+
+
 def test_queries_in_several_parts(ctx):
     """Rows of so many entries that the scores of all queries are not held at once: the same as one query after the other."""
     import torch
