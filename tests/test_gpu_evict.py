@@ -100,6 +100,15 @@ def test_weights_of_trees(ctx, n, window, sinks):
     check_weigh(ctx, [n, n + 1, n + 333], [n] * 3, heads=1, group=3, dim=128, window=window, sinks=sinks, parents=parents)
 
 
+@pytest.mark.parametrize("dim,cache", [(64, "f16"), (256, "f16"), (256, "e4m3")])
+def test_weights_of_trees_over_head_sizes(ctx, dim, cache):
+    """The trees' words beside the most rows in LDS that there are."""
+    rng = np.random.default_rng(dim)
+    n = 40
+    parents = [[int(rng.integers(max(-1, i - 9), i)) for i in range(n)] for _ in range(2)]
+    check_weigh(ctx, [n, n + 210], [n] * 2, heads=2, group=5, dim=dim, type_="f16", cache=cache, parents=parents, wide=dim == 64)
+
+
 def test_weights_where_pages_are_not_there_strides_and_scales(ctx):
     check_weigh(ctx, [40, 64, 300, 16], [1, 1, 60, 1], missing=[(0, 0), (1, 1), (2, 5), (3, 0)])
     check_weigh(ctx, [40, 64, 300, 16], [3, 60, 20, 1], wide=False, T=8)
