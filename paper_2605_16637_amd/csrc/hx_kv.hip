@@ -226,35 +226,38 @@ __device__ __forceinline__ uint32_t to_e4m3(const float *x, float scale)
     return w;
 }
 
-// 8 of 32 numbers, of which 4 lanes beside each other have a quarter each, as codes of 4 bits; *exp: their scale's byte.
+// 16 of 32 numbers, of which 2 lanes beside each other have a half each, as codes of 4 bits; *exp: their scale's byte.
 // 2^e is the least that 6 of it reach the largest with: 6 is 1.5 * 4, so the largest's own exponent decides, and whether its fraction is more than 1.5.
 // The matrix unit's own conversion over a power of 2 rounds to the nearest code, a middle to the even one, and what lies beyond 6 to 6.
-__device__ __forceinline__ uint32_t to_e2m1(const float *x, int *exp)
+__device__ __forceinline__ uint2 to_e2m1(const float *x, int *exp)
 {
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 16; ++i) {
         const uint32_t size = __float_as_uint(x[i]) & 0x7fffffffu;
         top = size > top ? size : top;
     }
-#pragma unroll
-    for (int d = 1; d < 4; d <<= 1) {
-        const uint32_t y = __shfl_xor(top, d);
-        top = y > top ? y : top;
-    }
+    const uint32_t other = __shfl_xor(top, 1);
+    top = other > top ? other : top;
     // (a NaN's bits are the largest)
     int e = (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x400000u ? 1 : 0);
     e = e < E2M1_LEAST ? E2M1_LEAST : e > E2M1_MOST ? E2M1_MOST : e;
     const bool nan = top > 0x7f800000u;
     const float unit = __uint_as_float((uint32_t)e << 23);
-    uint32_t w = 0;
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], unit, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], unit, 1);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], unit, 2);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], unit, 3);
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        w[i] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w[i], x[8 * i], x[8 * i + 1], unit, 0);
+        w[i] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w[i], x[8 * i + 2], x[8 * i + 3], unit, 1);
+        w[i] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w[i], x[8 * i + 4], x[8 * i + 5], unit, 2);
+        w[i] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w[i], x[8 * i + 6], x[8 * i + 7], unit, 3);
+    }
     *exp = nan ? E2M1_NAN : e;
-    return nan ? 0 : w;
+    return nan ? make_uint2(0, 0) : make_uint2(w[0], w[1]);
 }
+
+// numbers of a key and of a value that a thread has, by the type of the pool
+template <typename P> constexpr int a_time = std::is_same_v<P, E2m1> ? 16 : 8;
 
 struct WriteArgs {
     KvView kv;
@@ -324,29 +327,30 @@ __device__ __forceinline__ bool listed_before(const int32_t *row, int *x, int en
     return listed;
 }
 
-// 8 numbers of a key and of a value a thread; D of one byte: e4m3, or two numbers of 4 bits.  2048 tokens of 64 rows, 8 heads of 128 (17 MB read and
+// 8 numbers of a key and of a value a thread, 16 to 4 bits; D of one byte: e4m3, or two numbers of 4 bits.  2048 tokens of 64 rows, 8 heads of 128 (17 MB read and
 // written): 4.8 us in a graph of such calls, most of it the lookups before a thread's store (its sequence, row, length, page, count), under which
 // its numbers are on their way; 5.2 with a bisection for the sequence and the numbers behind it.  One token each of 256 rows 3.3, of 1024 4.7; of these the look
-// for rows listed twice takes 0.2, 0.3 and 1.1.  To 4 bits, 14454 tokens of prompts (59 MB read, 16 written): 22 us, 3.4 TB/s, where a wavefront's some 520
-// instructions take as long; 31 with codes by comparison with the middles, twice the instructions.
+// for rows listed twice takes 0.2, 0.3 and 1.1.  To 4 bits, 14454 tokens of prompts (59 MB read, 16 written): 22 us, 3.4 TB/s, of which the first
+// lookups and the last stores are some 6; 31 with codes by comparison with the middles, twice the instructions; 0.3 more with 8 numbers a thread.
 template <typename S, typename D>
 __global__ __launch_bounds__(CP_THREADS) void hx_kv_write_kernel(WriteArgs a)
 {
     const KvView &kv = a.kv;
-    const int per_head = kv.dim / 8, per = per_head * kv.n_heads;
+    constexpr int N = a_time<D>;
+    const int per_head = kv.dim / N, per = per_head * kv.n_heads;
     const uint32_t u = blockIdx.x * (uint32_t)CP_THREADS + threadIdx.x;      // (a grid has fewer than 2^32 threads)
     const int64_t q = u / (uint32_t)per;
-    const int c = (int)(u % (uint32_t)per), h = c / per_head, d = (c % per_head) * 8;
+    const int c = (int)(u % (uint32_t)per), h = c / per_head, d = (c % per_head) * N;
     // (the numbers come while their place is looked up; what is behind the last token reads the first)
     const int64_t from = q < a.n_tok ? q * a.token_stride + h * a.head_stride + d : 0;
-    struct alignas(8 * sizeof(S) < 16 ? 8 * sizeof(S) : 16) Eight { S x[8]; } source[2];
+    struct alignas(16) Source { S x[N]; } source[2];
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         const S *src = (const S *)(which ? a.v : a.k) + from;
-        if (a.aligned) source[which] = *(const Eight *)src;
+        if (a.aligned) source[which] = *(const Source *)src;
         else
 #pragma unroll
-            for (int i = 0; i < 8; ++i) source[which].x[i] = src[i];
+            for (int i = 0; i < N; ++i) source[which].x[i] = src[i];
     }
     int rows[LISTED_EACH];
     listed_ask(a.row, 0, a.n, rows);
@@ -365,14 +369,14 @@ __global__ __launch_bounds__(CP_THREADS) void hx_kv_write_kernel(WriteArgs a)
     const int64_t to = hx_kv_at(kv, a.layer, page, h, (int)(pos & ((1 << kv.shift) - 1))) + d;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-        const Eight &e = source[which];
+        const Source &e = source[which];
         if constexpr (std::is_same_v<D, E2m1>) {
-            float x[8];
+            float x[N];
             int exp;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = load_number(&e.x[i]);
-            *(uint32_t *)((char *)(which ? kv.v : kv.k) + to / 2) = to_e2m1(x, &exp);
-            if (c % 4 == 0) (which ? a.v_exp : a.k_exp)[to / E2M1_GROUP] = (uint8_t)exp;
+            for (int i = 0; i < N; ++i) x[i] = load_number(&e.x[i]);
+            *(uint2 *)((char *)(which ? kv.v : kv.k) + to / 2) = to_e2m1(x, &exp);
+            if (c % 2 == 0) (which ? a.v_exp : a.k_exp)[to / E2M1_GROUP] = (uint8_t)exp;
         } else if constexpr (sizeof(D) == 1) {
             const float *scales = which ? a.v_scale : a.k_scale;
             const float scale = scales ? scales[a.layer * kv.n_heads + h] : 1.0f;
@@ -408,10 +412,11 @@ template <typename S, typename D>
 __global__ __launch_bounds__(CP_THREADS) void hx_kv_read_kernel(ReadArgs a)
 {
     const KvView &kv = a.kv;
-    const int per_head = kv.dim / 8, per = per_head * kv.n_heads;
+    constexpr int N = a_time<S>;
+    const int per_head = kv.dim / N, per = per_head * kv.n_heads;
     const uint32_t u = blockIdx.x * (uint32_t)CP_THREADS + threadIdx.x;      // (a grid has fewer than 2^32 threads)
     const int64_t q = u / (uint32_t)per;
-    const int c = (int)(u % (uint32_t)per), h = c / per_head, d = (c % per_head) * 8;
+    const int c = (int)(u % (uint32_t)per), h = c / per_head, d = (c % per_head) * N;
     const int lo = entry_of(a.tok_ptr, a.n, q);
     const int first = a.tok_ptr[lo], last = a.tok_ptr[lo + 1], r = a.row[lo];
     bool ok = first >= 0 && first <= q && q < last && last <= a.n_tok && r >= 0 && r < kv.rows;
@@ -424,24 +429,24 @@ __global__ __launch_bounds__(CP_THREADS) void hx_kv_read_kernel(ReadArgs a)
     if (page >= kv.n_pages) { if (c == 0) hx_raise(kv.status, HX_ERR_INDEX); page = -1; }
     const int64_t from = page < 0 ? 0 : hx_kv_at(kv, a.layer, page, h, (int)(pos & ((1 << kv.shift) - 1))) + d;
     const int64_t to = q * a.token_stride + h * a.head_stride + d;
-    float both[2][8] = {};
+    float both[2][N] = {};
     if (page >= 0)
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
             const float *scales = which ? a.v_scale : a.k_scale;
-            stored<S, 8>(which ? kv.v : kv.k, which ? a.v_exp : a.k_exp, scales ? scales[a.layer * kv.n_heads + h] : 1.0f, from, both[which]);
+            stored<S, N>(which ? kv.v : kv.k, which ? a.v_exp : a.k_exp, scales ? scales[a.layer * kv.n_heads + h] : 1.0f, from, both[which]);
         }
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-        const float (&x)[8] = both[which];
+        const float (&x)[N] = both[which];
         D *at = (D *)(which ? a.v : a.k) + to;
-        struct alignas(8 * sizeof(D) < 16 ? 8 * sizeof(D) : 16) Eight { D x[8]; } e;
+        struct alignas(16) Out { D x[N]; } e;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e.x[i] = (D)x[i];
-        if (a.aligned) *(Eight *)at = e;
+        for (int i = 0; i < N; ++i) e.x[i] = (D)x[i];
+        if (a.aligned) *(Out *)at = e;
         else
 #pragma unroll
-            for (int i = 0; i < 8; ++i) at[i] = e.x[i];
+            for (int i = 0; i < N; ++i) at[i] = e.x[i];
     }
 }
 
@@ -714,7 +719,7 @@ extern "C" int hx_kv_write(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, c
     HX_REQUIRE(ctx, (((uintptr_t)k | (uintptr_t)v) & (hx_type_size(src_dtype) - 1)) == 0, HX_ERR_INVALID_ARG, "keys or values are not aligned to their type");
     const bool aligned = (((uintptr_t)k | (uintptr_t)v) & 15) == 0 && token_stride % 8 == 0 && head_stride % 8 == 0;
     WriteArgs a{kv, layer, n, n_tok, row, tok_ptr, k, v, token_stride, head_stride, pool->k_scale, pool->v_scale, pool->k_exp, pool->v_exp, aligned};
-    const int64_t blocks = ((int64_t)n_tok * (kv.dim / 8) * kv.n_heads + CP_THREADS - 1) / CP_THREADS;
+    const int64_t blocks = ((int64_t)n_tok * (kv.dim / (pool->dtype == HX_E2M1 ? a_time<E2m1> : 8)) * kv.n_heads + CP_THREADS - 1) / CP_THREADS;
     HX_REQUIRE(ctx, blocks <= hx_most_groups(CP_THREADS), HX_ERR_SHAPE, "%d tokens in one call", n_tok);
     const int grid = (int)blocks;
     HX_KV_DEVICE(ctx);
@@ -744,7 +749,7 @@ extern "C" int hx_kv_read(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, co
     HX_REQUIRE(ctx, (((uintptr_t)k | (uintptr_t)v) & (hx_type_size(dst_dtype) - 1)) == 0, HX_ERR_INVALID_ARG, "keys or values are not aligned to their type");
     const bool aligned = (((uintptr_t)k | (uintptr_t)v) & 15) == 0 && token_stride % 8 == 0 && head_stride % 8 == 0;
     ReadArgs a{kv, layer, n, n_tok, row, tok_ptr, k, v, token_stride, head_stride, pool->k_scale, pool->v_scale, pool->k_exp, pool->v_exp, aligned};
-    const int64_t blocks = ((int64_t)n_tok * (kv.dim / 8) * kv.n_heads + CP_THREADS - 1) / CP_THREADS;
+    const int64_t blocks = ((int64_t)n_tok * (kv.dim / (pool->dtype == HX_E2M1 ? a_time<E2m1> : 8)) * kv.n_heads + CP_THREADS - 1) / CP_THREADS;
     HX_REQUIRE(ctx, blocks <= hx_most_groups(CP_THREADS), HX_ERR_SHAPE, "%d tokens in one call", n_tok);
     const int grid = (int)blocks;
     HX_KV_DEVICE(ctx);
