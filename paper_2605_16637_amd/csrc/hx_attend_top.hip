@@ -251,7 +251,7 @@ __global__ __launch_bounds__(THREADS) void hx_top_pick_kernel(TopArgs t, int cac
     __shared__ NthHeld<uint32_t, THREADS> s_near;
     __shared__ NthHeld<uint64_t, THREADS> s_far;
     __shared__ NthState<uint64_t, THREADS> s_many;
-    __shared__ double s_exact[LIST];
+    __shared__ uint64_t s_key[LIST];
     __shared__ int s_list[LIST], s_n_list, s_count[2][WAVES];
     __shared__ float s_off[WAVES];
     extern __shared__ int s_pages[];                               // [cache] entries of the row, then their scores
@@ -315,8 +315,8 @@ __global__ __launch_bounds__(THREADS) void hx_top_pick_kernel(TopArgs t, int cac
         return page < kv.n_pages ? page : -1;
     };
     // which of the pages between are taken
-    enum { NONE, LEFT, NEAR, EXACT, BLIND } how = NONE;            // none; all that are there; scores from `under` on; scores above `over`, and from
-    float over = INF, under = INF;                                 // `under` on the largest exact ones; all by their exact ones
+    enum { NONE, LEFT, NEAR, MARKED, EXACT, BLIND } how = NONE;    // none; all that are there; scores from `under` on; scores above `over` and infinite
+    float over = INF, under = INF;                                 // ones; above `over` and, from `under` on, the largest exact ones; all by their exact ones
     uint64_t edge = 0;
     int equals = 0, unsures = 0;
     // (a page that is not there has a score of -infinity, which `under` may be of numbers near the type's lowest)
@@ -375,11 +375,24 @@ __global__ __launch_bounds__(THREADS) void hx_top_pick_kernel(TopArgs t, int cac
                 for (int i0 = 0; i0 < unsures; i0 += groups) {
                     const int i = i0 + tid / LANES, b = s_list[i < unsures ? i : 0];
                     const double x = exact_score<Q, E, D>(t, j, head, page_at(b), sub);
-                    if (i < unsures && sub == 0) s_exact[i] = x;
+                    if (i < unsures && sub == 0) s_key[i] = key_of(x);
                 }
                 __syncthreads();
-                const uint64_t x[1] = {tid < unsures ? key_of(s_exact[tid]) : 0};
-                nth_largest_held(x, want - sure, s_far, &edge, &equals);
+                const uint64_t mine = tid < unsures ? s_key[tid] : 0;
+                if (cached) {
+                    // each counts those before it; scores say from here on whether their page is taken
+                    if (tid < unsures) {
+                        const int b = s_list[tid];
+                        int before = 0;
+                        for (int i = 0; i < unsures; ++i) before += s_key[i] > mine || (s_key[i] == mine && s_list[i] < b);
+                        s_score[b] = mine > 0 && before < want - sure ? INF : -INF;
+                    }
+                    __syncthreads();
+                    how = MARKED;
+                } else {
+                    const uint64_t x[1] = {mine};
+                    nth_largest_held(x, want - sure, s_far, &edge, &equals);
+                }
             } else {
                 for (int b0 = from; b0 < to; b0 += groups) {
                     const int b = b0 + tid / LANES, page = b < to && unsure(b) ? page_at(b) : -1;
@@ -393,45 +406,48 @@ __global__ __launch_bounds__(THREADS) void hx_top_pick_kernel(TopArgs t, int cac
             }
         }
     }
-    auto exact_of = [&](int b) {
-        if (unsures > LIST) return exact[b];
+    auto exact_key = [&](int b) {
+        if (unsures > LIST) return key_of(exact[b]);
         int i = 0;
         while (i < unsures - 1 && s_list[i] != b) ++i;
-        return s_exact[i];
+        return s_key[i];
     };
     // the pages in rising order
-    int n = 0, seen_equal = 0;
+    int n = 0, seen_equal = 0, turn = 0;
     for (int b0 = 0; b0 <= p.own; b0 += THREADS) {
         const int b = b0 + tid;
         const int page = cached ? (b <= p.own ? s_pages[b] : -1) : in_pool(kv, b <= p.own ? p.table[b] : -1);
         const bool between = !all && b >= from && b < to && page >= 0;
         const bool told = between && how >= EXACT && unsure(b);
         const float x = between && how != NONE ? score_of(b) : 0.0f;
-        const uint64_t k = told ? key_of(exact_of(b)) : 0;
+        const uint64_t k = told ? exact_key(b) : 0;
         const bool equal = k == edge && k > 0;
+        const bool best = told ? k > edge : how == LEFT ? x > -INF : how == NEAR ? x >= under : how == MARKED ? x > over || x == INF : how == EXACT && x > over;
+        const bool sure = page >= 0 && (!between || best);
+        // the wavefronts' counts, of which each adds up those before it: of equal ones the first are taken
         const unsigned long long e = __builtin_amdgcn_ballot_w64(equal);
-        int rank = seen_equal + __builtin_popcountll(e & ((1ull << lane) - 1)), all_equal = __builtin_popcountll(e);
+        int all_sure = __builtin_popcountll(__builtin_amdgcn_ballot_w64(sure)), all_equal = __builtin_popcountll(e);
+        int rank = seen_equal + __builtin_popcountll(e & ((1ull << lane) - 1)), at = n;
+        auto of_equal = [&](int before, int here) { const int left = equals - before; return left < 0 ? 0 : left < here ? left : here; };
         if constexpr (WAVES > 1) {
-            if (lane == 0) s_count[0][wave] = all_equal;
+            if (lane == 0) s_count[turn][wave] = all_sure << 16 | all_equal;
             __syncthreads();
-            all_equal = 0;
+            rank -= seen_equal;
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) { rank += w < wave ? s_count[0][w] : 0; all_equal += s_count[0][w]; }
+            for (int w = 0; w < WAVES; ++w) {
+                const int c = s_count[turn][w], taken = (c >> 16) + of_equal(seen_equal, c & 0xffff);
+                n += taken;
+                at += w < wave ? taken : 0;
+                rank += w == wave ? seen_equal : 0;
+                seen_equal += c & 0xffff;
+            }
+            turn ^= 1;                                             // (who is still reading the other has passed a barrier since)
+        } else {
+            n += all_sure + of_equal(seen_equal, all_equal);
+            seen_equal += all_equal;
         }
-        const bool best = told ? k > edge || (equal && rank < equals) : how == LEFT ? x > -INF : how == NEAR ? x >= under : how == EXACT && x > over;
-        const bool take = page >= 0 && (!between || best);
-        const unsigned long long m = __builtin_amdgcn_ballot_w64(take);
-        int at = n + __builtin_popcountll(m & ((1ull << lane) - 1)), taken = __builtin_popcountll(m);
-        if constexpr (WAVES > 1) {
-            if (lane == 0) s_count[1][wave] = taken;
-            __syncthreads();
-            taken = 0;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) { at += w < wave ? s_count[1][w] : 0; taken += s_count[1][w]; }
-            __syncthreads();
-        }
-        n += taken;
-        seen_equal += all_equal;
+        const bool take = sure || (equal && rank < equals);
+        at += __builtin_popcountll(__builtin_amdgcn_ballot_w64(take) & ((1ull << lane) - 1));
         if (take) {
             picked[at] = page;
             if (chosen) chosen[at] = b;
@@ -499,10 +515,11 @@ extern "C" int hx_attend_top(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer,
     at_once = at_once < 1 ? 1 : at_once < n_q ? at_once : n_q;
     const int64_t q_tiles = (whole.max_q + 15) / 16, score_tiles = (int64_t)args->n * H * q_tiles;
     HX_REQUIRE(ctx, score_tiles <= hx_most_groups(TOP_THREADS), HX_ERR_SHAPE, "%d sequences of %d queries", args->n, whole.max_q);
-    // Workgroups look at 64 pages at once, and again; as many of them for a tile of queries as there are pages for, up to 8 a CU in all.
+    // Workgroups look at 64 pages at once, and again; as many of them for a tile of queries as there are pages for, up to 16 a CU in all (48 sequences over some 16000
+    // tokens: 152 us, 156 with 8).
     int64_t about = ((int64_t)args->max_len >> kv.shift) + 1;
     about = about < stride ? about : stride;
-    const int64_t useful = (about + 63) / 64, wanted = 8 * ctx->num_cu / score_tiles, most_chunks = hx_most_groups(TOP_THREADS) / score_tiles;
+    const int64_t useful = (about + 63) / 64, wanted = 16 * ctx->num_cu / score_tiles, most_chunks = hx_most_groups(TOP_THREADS) / score_tiles;
     int64_t chunks = useful < wanted ? useful : wanted;
     chunks = chunks < 1 ? 1 : chunks < most_chunks ? chunks : most_chunks;
     HxDeviceGuard guard(ctx->device);
