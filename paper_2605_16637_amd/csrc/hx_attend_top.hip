@@ -72,7 +72,7 @@ __device__ __forceinline__ typename Types<Q>::x8 as_query(typename Types<E>::x8 
 //
 // ONE: a single query a sequence, whose heads are the columns; else 16 queries beside each other are, and the heads follow each other.  A wavefront has 16
 // pages at once and asks for the next 16.  Bound by the bounds' bytes with one query a sequence: 48 of them over some 16000 tokens, pages of 32, 8 heads of
-// 128: 126 MB in 42 us, 3.0 TB/s; 602 queries over some 8000: 16 us.  With all scores in 64 bits by the vector units the whole calls took 240 and 384 us where
+// 128: 126 MB in 39 us, 3.2 TB/s; 602 queries over some 8000: 16 us.  With all scores in 64 bits by the vector units the whole calls took 240 and 384 us where
 // they took 157 and 157 with these.
 template <typename Q, typename E, int D, bool ONE>
 __global__ __launch_bounds__(TOP_THREADS) void hx_top_score_kernel(TopArgs t)
@@ -243,7 +243,8 @@ __device__ __forceinline__ float of_key(uint32_t k)
 
 // A workgroup a query and KV head, of up to 256 pages a single wavefront, which needs no barriers: a chain of round trips (the query's row, its length, its
 // pages and their scores, all of which are kept in LDS) and of passes over the scores.  cache: pages that fit there.  One query over 30000 tokens, 64 pages of
-// 1875 for each of 8 heads: 19 us, of which the row and its scores take 5, the limit 4, the scores in 64 bits 5 and the pages' order 4; 384 such of 512: 22.
+// 1875 for each of 8 heads: 17 us, of which the row and its scores take 5, the limit 4 and the scores in 64 bits 5; 384 such of 512: 19.5.  (The limit found
+// by quarters, at half the meetings but three times the counts, takes as long.)
 template <typename Q, typename E, int D, int THREADS>
 __global__ __launch_bounds__(THREADS) void hx_top_pick_kernel(TopArgs t, int cache)
 {

@@ -256,9 +256,6 @@ __device__ __forceinline__ uint2 to_e2m1(const float *x, int *exp)
     return nan ? make_uint2(0, 0) : make_uint2(w[0], w[1]);
 }
 
-// numbers of a key and of a value that a thread has, by the type of the pool
-template <typename P> constexpr int a_time = std::is_same_v<P, E2m1> ? 16 : 8;
-
 struct WriteArgs {
     KvView kv;
     int layer, n, n_tok;
@@ -330,13 +327,13 @@ __device__ __forceinline__ bool listed_before(const int32_t *row, int *x, int en
 // 8 numbers of a key and of a value a thread, 16 to 4 bits; D of one byte: e4m3, or two numbers of 4 bits.  2048 tokens of 64 rows, 8 heads of 128 (17 MB read and
 // written): 4.8 us in a graph of such calls, most of it the lookups before a thread's store (its sequence, row, length, page, count), under which
 // its numbers are on their way; 5.2 with a bisection for the sequence and the numbers behind it.  One token each of 256 rows 3.3, of 1024 4.7; of these the look
-// for rows listed twice takes 0.2, 0.3 and 1.1.  To 4 bits, 14454 tokens of prompts (59 MB read, 16 written): 22 us, 3.4 TB/s, of which the first
-// lookups and the last stores are some 6; 31 with codes by comparison with the middles, twice the instructions; 0.3 more with 8 numbers a thread.
+// for rows listed twice takes 0.2, 0.3 and 1.1.  To 4 bits, 14454 tokens of prompts (59 MB read, 16 written): 18 us, 4.2 TB/s; 22 with 8 numbers a thread,
+// 31 with codes by comparison with the middles too, twice the instructions.
 template <typename S, typename D>
 __global__ __launch_bounds__(CP_THREADS) void hx_kv_write_kernel(WriteArgs a)
 {
     const KvView &kv = a.kv;
-    constexpr int N = a_time<D>;
+    constexpr int N = std::is_same_v<D, E2m1> ? 16 : 8;
     const int per_head = kv.dim / N, per = per_head * kv.n_heads;
     const uint32_t u = blockIdx.x * (uint32_t)CP_THREADS + threadIdx.x;      // (a grid has fewer than 2^32 threads)
     const int64_t q = u / (uint32_t)per;
@@ -406,13 +403,13 @@ struct ReadArgs {
     bool aligned;            // 8 numbers can be stored at once
 };
 
-// 8 numbers of a key and of a value a thread, as the write.  From 4 bits, 14454 tokens (16 MB read, 59 written): 22 us, 3.4 TB/s; 24.4 with codes taken
-// apart bit by bit and the value asked for behind the key.
+// 8 numbers of a key and of a value a thread, which a wavefront stores beside each other.  From 4 bits, 14454 tokens (16 MB read, 59 written): 22 us, 3.4 TB/s; 25
+// with 16 numbers a thread; 24.4 with codes taken apart bit by bit and the value asked for behind the key.
 template <typename S, typename D>
 __global__ __launch_bounds__(CP_THREADS) void hx_kv_read_kernel(ReadArgs a)
 {
     const KvView &kv = a.kv;
-    constexpr int N = a_time<S>;
+    constexpr int N = 8;
     const int per_head = kv.dim / N, per = per_head * kv.n_heads;
     const uint32_t u = blockIdx.x * (uint32_t)CP_THREADS + threadIdx.x;      // (a grid has fewer than 2^32 threads)
     const int64_t q = u / (uint32_t)per;
@@ -719,7 +716,7 @@ extern "C" int hx_kv_write(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, c
     HX_REQUIRE(ctx, (((uintptr_t)k | (uintptr_t)v) & (hx_type_size(src_dtype) - 1)) == 0, HX_ERR_INVALID_ARG, "keys or values are not aligned to their type");
     const bool aligned = (((uintptr_t)k | (uintptr_t)v) & 15) == 0 && token_stride % 8 == 0 && head_stride % 8 == 0;
     WriteArgs a{kv, layer, n, n_tok, row, tok_ptr, k, v, token_stride, head_stride, pool->k_scale, pool->v_scale, pool->k_exp, pool->v_exp, aligned};
-    const int64_t blocks = ((int64_t)n_tok * (kv.dim / (pool->dtype == HX_E2M1 ? a_time<E2m1> : 8)) * kv.n_heads + CP_THREADS - 1) / CP_THREADS;
+    const int64_t blocks = ((int64_t)n_tok * (kv.dim / (pool->dtype == HX_E2M1 ? 16 : 8)) * kv.n_heads + CP_THREADS - 1) / CP_THREADS;
     HX_REQUIRE(ctx, blocks <= hx_most_groups(CP_THREADS), HX_ERR_SHAPE, "%d tokens in one call", n_tok);
     const int grid = (int)blocks;
     HX_KV_DEVICE(ctx);
@@ -749,7 +746,7 @@ extern "C" int hx_kv_read(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, co
     HX_REQUIRE(ctx, (((uintptr_t)k | (uintptr_t)v) & (hx_type_size(dst_dtype) - 1)) == 0, HX_ERR_INVALID_ARG, "keys or values are not aligned to their type");
     const bool aligned = (((uintptr_t)k | (uintptr_t)v) & 15) == 0 && token_stride % 8 == 0 && head_stride % 8 == 0;
     ReadArgs a{kv, layer, n, n_tok, row, tok_ptr, k, v, token_stride, head_stride, pool->k_scale, pool->v_scale, pool->k_exp, pool->v_exp, aligned};
-    const int64_t blocks = ((int64_t)n_tok * (kv.dim / (pool->dtype == HX_E2M1 ? a_time<E2m1> : 8)) * kv.n_heads + CP_THREADS - 1) / CP_THREADS;
+    const int64_t blocks = ((int64_t)n_tok * (kv.dim / 8) * kv.n_heads + CP_THREADS - 1) / CP_THREADS;
     HX_REQUIRE(ctx, blocks <= hx_most_groups(CP_THREADS), HX_ERR_SHAPE, "%d tokens in one call", n_tok);
     const int grid = (int)blocks;
     HX_KV_DEVICE(ctx);
