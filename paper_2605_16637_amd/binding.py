@@ -283,12 +283,16 @@ def make_kv_pool(p: dict) -> hx_kv_pool:
     four = k.dtype == torch.uint8
     if four:
         dim *= 2
-    exps, k_exp, v_exp, bounds = n_layers * n_pages * n_heads * tokens * (dim // 32), p.get("k_exp"), p.get("v_exp"), p.get("bounds")
-    wide = k.dtype if k.dtype in (torch.bfloat16, torch.float16) else torch.bfloat16
-    return hx_kv_pool(n_layers, n_pages, n_heads, tokens, dim, HX_E2M1 if four else _number_type(k, HX_BF16, HX_F16, HX_E4M3), _ptr(k), _ptr(v),
+    pool = hx_kv_pool(n_layers, n_pages, n_heads, tokens, dim, HX_E2M1 if four else _number_type(k, HX_BF16, HX_F16, HX_E4M3), _ptr(k), _ptr(v),
                       _ptr(p["ref"], torch.int32, n_pages), _ptr(p.get("k_scale"), torch.float32, n_layers * n_heads),
-                      _ptr(p.get("v_scale"), torch.float32, n_layers * n_heads), _ptr(k_exp, torch.uint8, exps), _ptr(v_exp, torch.uint8, exps),
-                      _ptr(bounds, wide, n_layers * n_pages * n_heads * 2 * dim))
+                      _ptr(p.get("v_scale"), torch.float32, n_layers * n_heads))
+    if four or "k_exp" in p or "v_exp" in p:
+        exps = n_layers * n_pages * n_heads * tokens * (dim // 32)
+        pool.k_exp, pool.v_exp = _ptr(p.get("k_exp"), torch.uint8, exps), _ptr(p.get("v_exp"), torch.uint8, exps)
+    if "bounds" in p:
+        wide = k.dtype if k.dtype in (torch.bfloat16, torch.float16) else torch.bfloat16
+        pool.bounds = _ptr(p["bounds"], wide, n_layers * n_pages * n_heads * 2 * dim)
+    return pool
 
 
 def make_kv_seqs(s: dict) -> hx_kv_seqs:
