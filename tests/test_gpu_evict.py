@@ -370,3 +370,47 @@ def test_captured_and_on_another_stream(ctx):
             got.append([t.clone() for t in state])
         assert all(torch.equal(a, b) for a, b in zip(*got)) and lh.status(ctx) == 0
         assert c.seqs["len"][row.long()].tolist() == [90, 90]
+
+
+@pytest.mark.parametrize("cache,T,pages", [("bf16", 1, 1100000), ("e2m1", 32, 300000)])
+def test_pages_past_32_bits(ctx, cache, T, pages):
+    """All operators over rows whose pages lie at a pool's end, where bytes, of keys or bounds, pass 2^32: as over a small pool."""
+    import torch
+    heads, group, dim, lens, nq = 8, 2, 128, [40 * T // min(T, 4), 75], [1, 20]
+    c = lh.Cache(31, lens, T, heads, dim, cache, layers=1, extra_rows=0, bounds=True, garbage=False)
+    small, far = dict(c.pool), pages - c.n_pages
+    big = {}
+    for name, x in small.items():
+        if name == "page_tokens":
+            big[name] = x
+        elif name == "ref":
+            big[name] = torch.cat([torch.ones(far, dtype=torch.int32, device="cuda:0"), x])
+        else:
+            big[name] = torch.empty((1, pages) + tuple(x.shape[2:]), dtype=x.dtype, device="cuda:0")
+            big[name][:, far:] = x
+    assert max(x.numel() * x.element_size() for x in big.values() if torch.is_tensor(x)) > 2 ** 32
+    got = []
+    for pool, add in ((small, 0), (big, far)):
+        table = c.seqs["table"].clone()
+        table[table >= 0] += add
+        seqs = dict(table=table, len=c.seqs["len"].clone())
+        row, ptr = sh.i32(c.where), sh.i32([0, 1, 21])
+        x = torch.randn(2, 21, heads, dim, device="cuda:0", generator=torch.Generator("cuda:0").manual_seed(2))
+        ctx.hx_kv_write(pool, 0, seqs, row, ptr, x[0], x[1])
+        ctx.hx_kv_bound(pool, 0, seqs, row)
+        q = lh.queries(21, heads * group, dim, "bf16", 3)
+        out, lse = torch.zeros(2, 21, heads * group, dim, dtype=torch.bfloat16, device="cuda:0"), torch.zeros(2, 21, heads * group, device="cuda:0")
+        ctx.hx_attend(pool, 0, seqs, ptr, q, out[0], max_q=20, row=row, lse=lse[0])
+        ctx.hx_attend_top(pool, 0, seqs, ptr, q, out[1], max_q=20, n_pages=2, row=row, lse=lse[1])
+        weight = torch.zeros(c.rows, table.shape[1] * T, device="cuda:0")
+        ctx.hx_kv_weigh(pool, 0, seqs, ptr, q, lse[0], weight, max_q=20, row=row)
+        ctx.hx_kv_weigh(pool, 0, seqs, sh.i32([0, 1]), q, lse[0], weight, max_q=1, row=row[:1])
+        kept = torch.zeros(2, 33, dtype=torch.int32, device="cuda:0")
+        ctx.hx_kv_evict(pool, seqs, row, weight, 33, n_last=2, kept=kept)
+        assert lh.status(ctx) == 0
+        k, v = torch.zeros(2, 66, heads, dim, device="cuda:0")
+        ctx.hx_kv_read(pool, 0, seqs, row, sh.i32([0, 33, 66]), k, v)
+        assert lh.status(ctx) == 0 and seqs["len"][row.long()].tolist() == [33, 33]
+        got.append((out, lse, weight, kept, k, v))
+    for one, other in zip(*got):
+        assert torch.equal(one, other)
