@@ -285,8 +285,9 @@ __global__ __launch_bounds__(THREADS) void hx_top_pick_kernel(TopArgs t, int cac
             __syncthreads();
         }
     };
-    const bool all = p.own < t.n_pages || kv.n_pages == 0;
-    const int from = t.n_first, to = p.own - t.n_last + 1;         // the pages between those that are seen in any case
+    const HxSeen seen = hx_seen_in_any_case(p.own, t.n_pages, t.n_first, t.n_last);
+    const bool all = seen.all || kv.n_pages == 0;
+    const int from = seen.from, to = seen.to;                      // the pages between those that are seen in any case
     const float *score = t.score + (int64_t)pair * t.stride;
     double *exact = t.exact + (int64_t)pair * t.stride;
     const bool cached = p.own < cache;
@@ -303,9 +304,10 @@ __global__ __launch_bounds__(THREADS) void hx_top_pick_kernel(TopArgs t, int cac
             if (between) s_score[b] = score[b];
             fixed += __builtin_popcountll(__builtin_amdgcn_ballot_w64(!between && page >= 0));
         }
-    } else
-        for (int i0 = 0; i0 < t.n_first + t.n_last; i0 += THREADS) {
-            const int i = i0 + tid, page = i < t.n_first + t.n_last ? p.table[i < t.n_first ? i : to + i - t.n_first] : -1;
+    } else if (!all)
+        // (a row that all of is seen need not have as many entries)
+        for (int i0 = 0; i0 < seen.fixed; i0 += THREADS) {
+            const int i = i0 + tid, page = i < seen.fixed ? p.table[seen.entry(i)] : -1;
             fixed += __builtin_popcountll(__builtin_amdgcn_ballot_w64(page >= 0 && page < kv.n_pages));
         }
     add_up(fixed, none);
