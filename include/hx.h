@@ -847,6 +847,8 @@ int hx_kv_weigh(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_kv_
  * page is left are left as they are (HX_ERR_CAPACITY).  kept: device [n][n_keep]
  * out, the positions that the tokens had, then -1 (all -1: the row is as it was), or
  * NULL.  A position is the token's place in its row: windows count what has stayed.
+ * A row's max_pages * page_tokens is up to INT32_MAX / 2 here; n_keep may be more.  Scratch: 4 bytes for each page of the pool and, of every row, for each
+ * page that n_keep tokens or all that the row can have take, and for each of these tokens where kept is NULL.
  */
 int hx_kv_evict(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs *seqs, int32_t n, const int32_t *row,
                 float *weight, int32_t n_keep, int32_t n_first, int32_t n_last, int32_t *kept, void *stream);

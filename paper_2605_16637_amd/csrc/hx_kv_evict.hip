@@ -16,12 +16,13 @@ constexpr int EV_AHEAD = 8;                // tokens that a thread moves at once
 struct EvictArgs {
     KvView kv;
     KvPlanes planes;
-    int n, n_keep, n_first, n_last, keep_pages;
+    int n, n_keep, n_first, n_last, keep_pages;      // n_keep: no more than a row can have
     int slices;              // of a token's bytes, in the move
     const int32_t *row;
     float *weight;
     int64_t pitch;           // of a row's weights
-    int32_t *kept;           // [n][n_keep] positions of the tokens that stay
+    int32_t *kept;           // [n][kept_pitch] positions of the tokens that stay, then -1
+    uint32_t kept_pitch;     // what the caller said, where it has asked for them
     int32_t *stay;           // [n] how many, -1: the row is left as it is
     int32_t *moves;          // [n] the first of them that changes its place, or all
     int32_t *need;           // [n] pages that are replaced
@@ -29,6 +30,13 @@ struct EvictArgs {
     int32_t *fresh;          // [n][keep_pages] which of the row's new pages an entry gets, -1: it keeps its own
     int32_t *list;           // free pages
 };
+
+// Row i's kept positions from `from` on are none.  (No sign: the loop counts on past its end by a workgroup's threads, which may be near INT32_MAX.)
+__device__ __forceinline__ void kept_none(const EvictArgs &a, int i, uint32_t from)
+{
+    int32_t *kept = a.kept + (int64_t)i * a.kept_pitch;
+    for (uint32_t j = from + threadIdx.x; j < a.kept_pitch; j += EV_THREADS) kept[j] = -1;
+}
 
 // what is not above 0 counts as 0; keys of 0 are none, so that all are one up
 __device__ __forceinline__ uint32_t weight_key(float w) { return (w > 0.0f ? __float_as_uint(w) : 0) + 1; }
@@ -60,10 +68,10 @@ __global__ __launch_bounds__(EV_THREADS) void hx_kv_evict_select_kernel(EvictArg
     bad = __syncthreads_or(bad);
     const int len = bad ? 0 : kv.len[r];
     bad = bad || !hx_row_ok(kv, r, len);
-    int32_t *kept = a.kept + (int64_t)i * a.n_keep;
+    int32_t *kept = a.kept + (int64_t)i * a.kept_pitch;
     if (bad || len <= a.n_keep) {
         if (bad && tid == 0) hx_raise(kv.status, HX_ERR_INDEX);
-        for (int j = tid; j < a.n_keep; j += EV_THREADS) kept[j] = -1;
+        kept_none(a, i, 0);
         if (tid == 0) { a.stay[i] = -1; a.need[i] = 0; }
         return;
     }
@@ -112,7 +120,7 @@ __global__ __launch_bounds__(EV_THREADS) void hx_kv_evict_select_kernel(EvictArg
             if (y != at && at < moves) moves = at;
         }
     }
-    for (int j = n + tid; j < a.n_keep; j += EV_THREADS) kept[j] = -1;
+    kept_none(a, i, n);
     for (int b = tid; b < hx_pages_of(len, kv.shift); b += EV_THREADS)
         if (table[b] >= kv.n_pages) hx_raise(kv.status, HX_ERR_INDEX);
 #pragma unroll
@@ -182,7 +190,7 @@ __global__ __launch_bounds__(EV_THREADS) void hx_kv_evict_move_kernel(EvictArgs 
     const int heads = kv.n_heads, parts = 1 + a.planes.n * kv.n_layers * heads * a.slices, i = blockIdx.x / parts, part = blockIdx.x % parts, tid = threadIdx.x;
     const int n = a.stay[i], r = a.row[i];
     if (n < 0) return;
-    const int32_t *kept = a.kept + (int64_t)i * a.n_keep;
+    const int32_t *kept = a.kept + (int64_t)i * a.kept_pitch;
     const int begin = a.moves[i];
     if (part == 0) {
         float *w = a.weight + r * a.pitch;
@@ -240,7 +248,7 @@ __global__ __launch_bounds__(EV_THREADS) void hx_kv_evict_apply_kernel(EvictArgs
     const KvView &kv = a.kv;
     const int i = blockIdx.x, n = a.stay[i], r = a.row[i];
     if (n < 0) {
-        for (int j = threadIdx.x; j < a.n_keep; j += EV_THREADS) a.kept[(int64_t)i * a.n_keep + j] = -1;
+        kept_none(a, i, 0);
         return;
     }
     int32_t *table = hx_row(kv, r);
@@ -276,16 +284,18 @@ extern "C" int hx_kv_evict(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs
     while (2 * (int64_t)n * planes.n * kv.n_layers * kv.n_heads * slices <= EV_FULL * ctx->num_cu && planes.row_bytes[0] >= 128 * slices) slices *= 2;
     const int64_t parts = 1 + (int64_t)planes.n * kv.n_layers * kv.n_heads * slices;
     HX_REQUIRE(ctx, n * parts <= hx_most_groups(EV_THREADS), HX_ERR_SHAPE, "%d rows of %d layers of %d heads in one call", n, kv.n_layers, kv.n_heads);
-    const int keep_pages = (int)(((int64_t)n_keep + (1 << kv.shift) - 1) >> kv.shift);
+    HX_REQUIRE(ctx, (int64_t)kv.max_pages << kv.shift <= INT32_MAX / 2, HX_ERR_SHAPE, "%d pages of %d tokens a row", kv.max_pages, 1 << kv.shift);
+    // a budget beyond what a row can have needs no more room than that
+    const int pitch = kv.max_pages << kv.shift, most = n_keep < pitch ? n_keep : pitch, keep_pages = hx_pages_of(most, kv.shift);
     HxDeviceGuard guard(ctx->device);
     HX_REQUIRE(ctx, guard.ok, HX_ERR_DEVICE, "cannot select device %d", ctx->device);
     const hipStream_t stream = (hipStream_t)stream_;
-    const size_t words = (size_t)n * (4 + (size_t)keep_pages + (kept ? 0 : (size_t)n_keep)) + kv.n_pages;
+    const size_t words = (size_t)n * (4 + (size_t)keep_pages + (kept ? 0 : (size_t)most)) + kv.n_pages;
     if (int rc = hx_scratch(ctx, hx_serve(ctx)->kv, words * sizeof(int32_t), stream)) return rc;
     int32_t *w = (int32_t *)hx_serve(ctx)->kv.p;
     const size_t N = n;
-    EvictArgs a{kv, planes, n, n_keep, n_first, n_last, keep_pages, slices, row, weight, (int64_t)kv.max_pages << kv.shift,
-                kept ? kept : w + N * (4 + (size_t)keep_pages) + kv.n_pages, w, w + N, w + 2 * N, w + 3 * N, w + 4 * N, w + N * (4 + (size_t)keep_pages)};
+    EvictArgs a{kv, planes, n, most, n_first, n_last, keep_pages, slices, row, weight, pitch,
+                kept ? kept : w + N * (4 + (size_t)keep_pages) + kv.n_pages, (uint32_t)(kept ? n_keep : most), w, w + N, w + 2 * N, w + 3 * N, w + 4 * N, w + N * (4 + (size_t)keep_pages)};
     hx_kv_evict_select_kernel<<<n, EV_THREADS, 0, stream>>>(a);
     hx_kv_evict_plan_kernel<<<1, PL_THREADS, 0, stream>>>(a);
     hx_kv_evict_move_kernel<<<(int)(n * parts), EV_THREADS, 0, stream>>>(a);
