@@ -812,8 +812,8 @@ int hx_kv_bound(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_kv_
  * that it has in hx_attend.  chosen: the numbers of the pages in their row,
  * rising, then -1.  Of queries that are no sequence's nothing is written.
  * args->parent must be NULL and args->window 0; pool->bounds must hold the pages'
- * bounds.  Scratch: 12.25 bytes for each entry of a row, query and KV head, up to 256 MB
- * (more queries are taken in several parts), 4 for each page that is chosen.
+ * bounds.  Scratch: for each query and KV head 12.25 bytes for each entry of a row where rows have more than n_pages, and 4 for
+ * each page that is chosen (n_pages, or a row's entries), up to 256 MB in all: more queries are taken in several parts.
  */
 typedef struct {
     int32_t n_pages;          /* 1 .. HX_MAX_TOP                                                */

@@ -6,13 +6,14 @@
 namespace {
 
 constexpr int TOP_THREADS = 256, TOP_WAVES = TOP_THREADS / 64;
-constexpr int64_t TOP_SCORES = (int64_t)1 << 28;         // bytes of scores at once
+constexpr int64_t TOP_ROOM = (int64_t)1 << 28;           // bytes of scores and of chosen pages at once
 
 struct TopArgs {
     AttendArgs a;
     const void *bounds;              // of the layer
     int first_query, n_queries;      // of this part of the call
     int n_pages, n_first, n_last;
+    int picked_pages;                // n_pages, or a row's entries where they are fewer
     int stride;                      // entries of a row, up to a multiple of 16; 0 where no row has more than n_pages entries
     float *score;                    // [query][KV head][stride]
     float *off;                      // [query][KV head][stride / 16] what a score of these 16 pages may be off by
@@ -262,7 +263,7 @@ __global__ __launch_bounds__(THREADS) void hx_top_pick_kernel(TopArgs t, int cac
     const int pair = blockIdx.x, head = pair % kv.n_heads, j = t.first_query + pair / kv.n_heads;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const Place p = place(a, j);
-    int32_t *picked = t.picked + (int64_t)pair * t.n_pages;
+    int32_t *picked = t.picked + (int64_t)pair * t.picked_pages;
     int32_t *chosen = t.chosen ? t.chosen + ((int64_t)j * kv.n_heads + head) * t.n_pages : nullptr;
     if (p.none) {
         if (tid == 0) t.picked_len[pair] = -1;
@@ -509,9 +510,10 @@ extern "C" int hx_attend_top(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer,
     const HxAttend whole = hx_attend_view(ctx, pool, layer, kv, *args);
     // no row has more pages than entries: no scores where all of them are seen
     const int64_t stride = kv.max_pages > n_pages && kv.n_pages > 0 ? ((int64_t)kv.max_pages + 15) / 16 * 16 : 0;
-    const size_t line = (size_t)stride * (sizeof(double) + sizeof(float)) + (size_t)(stride / 16) * sizeof(float);
-    // so many queries at once that scores stay below TOP_SCORES, and launches within their limits
-    int64_t at_once = stride ? TOP_SCORES / (int64_t)(line * H) : n_q;
+    const int picked_pages = kv.max_pages < 1 ? 1 : kv.max_pages < n_pages ? kv.max_pages : n_pages;
+    const size_t line = (size_t)stride * (sizeof(double) + sizeof(float)) + (size_t)(stride / 16) * sizeof(float) + ((size_t)picked_pages + 1) * sizeof(int32_t);
+    // so many queries at once that they stay below TOP_ROOM, and launches within their limits
+    int64_t at_once = TOP_ROOM / (int64_t)(line * H);
     const int64_t tiles = (whole.group + 127) / 128, fits = hx_most_groups(1024) / (H * tiles * 64);
     HX_REQUIRE(ctx, fits > 0, HX_ERR_SHAPE, "%d query heads", whole.n_heads);
     at_once = at_once < fits ? at_once : fits;
@@ -529,14 +531,14 @@ extern "C" int hx_attend_top(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer,
     HX_REQUIRE(ctx, guard.ok, HX_ERR_DEVICE, "cannot select device %d", ctx->device);
     const hipStream_t stream = (hipStream_t)stream_;
     const int64_t pairs = at_once * H;
-    const size_t bytes = (size_t)pairs * (line + ((size_t)n_pages + 1) * sizeof(int32_t));
+    const size_t bytes = (size_t)pairs * line;
     if (int rc = hx_scratch(ctx, hx_serve(ctx)->top, bytes, stream)) return rc;
     const int64_t seen = (int64_t)n_pages << kv.shift, most = args->max_len < seen ? args->max_len : seen;
     auto part_of = [&](int64_t j, int64_t n) {
         HxAttend a = whole;
         a.n = a.n_q = (int)n;
         a.max_q = 1;
-        a.picked_pages = n_pages;
+        a.picked_pages = picked_pages;
         a.q = (const char *)a.q + j * a.q_token * 2;
         a.out = (char *)a.out + j * a.out_token * 2;
         if (a.lse) a.lse += j * a.n_heads;
@@ -552,13 +554,13 @@ extern "C" int hx_attend_top(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer,
     TopArgs t{};
     t.a = whole;
     t.bounds = (const char *)pool->bounds + (int64_t)layer * kv.n_pages * hx_bounds_bytes(pool);
-    t.n_pages = n_pages; t.n_first = top->n_first; t.n_last = top->n_last;
+    t.n_pages = n_pages; t.picked_pages = picked_pages; t.n_first = top->n_first; t.n_last = top->n_last;
     t.stride = (int)stride;
     t.exact = (double *)hx_serve(ctx)->top.p;
     t.score = (float *)(t.exact + pairs * stride);
     t.off = t.score + pairs * stride;
     t.picked = (int32_t *)(t.off + pairs * (stride / 16));
-    t.picked_len = t.picked + pairs * n_pages;
+    t.picked_len = t.picked + pairs * picked_pages;
     t.chosen = top->chosen;
     t.q_tiles = (int)q_tiles;
     t.chunks = (int)chunks;

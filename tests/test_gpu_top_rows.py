@@ -58,3 +58,54 @@ def test_short_rows_beside_long_ones_of_which_less_is_said(ctx, n_pages, n_first
     lens = [1, 2300, 9, 130, 96, 97]
     c = lh.Cache(n_pages, lens, 8, 2, 64, "bf16", bounds=True, extra_rows=0, room=0, missing=[(1, 0), (1, 200)])
     check(ctx, c, lens, n_pages, n_first, n_last, max_len, around=40)
+
+
+def test_pages_beyond_a_row_take_no_room():
+    """65536 queries and heads over rows of two entries: a budget of 4096 pages is one of two."""
+    import torch
+    from paper_2605_16637_amd import binding
+    fresh = binding.Context(0)
+    n = 8192
+    c = lh.Cache(51, [16, 9], 8, 8, 64, "bf16", bounds=True, extra_rows=0, room=0)
+    fresh.hx_kv_bound(c.pool, 1, c.seqs, sh.i32(c.where))
+    q = lh.queries(n, 8, 64, "bf16", 0)
+    out, want = torch.zeros(2, n, 8, 64, dtype=torch.bfloat16, device="cuda:0")
+    chosen = torch.full((n, 8, 4096), 7, dtype=torch.int32, device="cuda:0")
+    few = torch.full((n, 8, 2), 7, dtype=torch.int32, device="cuda:0")
+    call = dict(max_q=1, row=sh.i32(np.resize(c.where, n)))
+    ptr = sh.i32(range(n + 1))
+    torch.cuda.synchronize()
+    before = torch.cuda.mem_get_info()[0]
+    fresh.hx_attend_top(c.pool, 1, c.seqs, ptr, q, out, n_pages=4096, n_first=4000, n_last=90, chosen=chosen, **call)
+    torch.cuda.synchronize()
+    assert before - torch.cuda.mem_get_info()[0] < 128 << 20
+    fresh.hx_attend_top(c.pool, 1, c.seqs, ptr, q, want, n_pages=2, n_last=2, chosen=few, **call)
+    assert lh.status(fresh) == 0 and torch.equal(out, want)
+    assert torch.equal(chosen[:, :, :2], few) and bool((chosen[:, :, 2:] == -1).all()) and bool((few == sh.i32([0, 1])).all())
+    fresh.close()
+
+
+def test_queries_that_see_all_pages_in_several_parts():
+    """So many chosen pages that not all queries' are held at once, where there are no scores."""
+    import torch
+    from paper_2605_16637_amd import binding
+    fresh = binding.Context(0)
+    n, heads, n_q = 4096, 16, 1100                              # 1023 queries' pages are 256 MB
+    c = lh.Cache(52, [n], 1, heads, 64, "bf16", bounds=True, extra_rows=0, room=0, layers=1, spare=0)
+    q = lh.queries(n_q, heads, 64, "bf16", 0)
+    out, lse = torch.zeros_like(q), torch.zeros(n_q, heads, device="cuda:0")
+    chosen = torch.full((n_q, heads, n), 7, dtype=torch.int32, device="cuda:0")
+    torch.cuda.synchronize()
+    before = torch.cuda.mem_get_info()[0]
+    fresh.hx_attend_top(c.pool, 0, c.seqs, sh.i32([0, n_q]), q, out, max_q=n_q, n_pages=n, chosen=chosen, lse=lse)
+    torch.cuda.synchronize()
+    assert before - torch.cuda.mem_get_info()[0] < 1 << 30
+    assert lh.status(fresh) == 0
+    b = torch.arange(n, device="cuda:0", dtype=torch.int32)
+    for j in range(n_q):
+        assert bool((chosen[j] == torch.where(b <= n - n_q + j, b, -1)).all())
+    some = [0, 1, 1021, 1022, 1023, 1024, n_q - 1]
+    k, v = c.of(c.k, 0, 0), c.of(c.v, 0, 0)
+    see = np.arange(n) <= n - n_q + np.asarray(some)[:, None]
+    lh.compare(lh.f64(out)[some], lh.f64(lse)[some], lh.f64(q)[some], k, v, see, 64 ** -0.5, 1, "bf16")
+    fresh.close()
