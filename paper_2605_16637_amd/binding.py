@@ -275,12 +275,14 @@ def make_kv_pool(p: dict) -> hx_kv_pool:
     pages, KV heads, 2, head_dim], of the cache's type (bfloat16 for 8 and 4 bits)."""
     torch = _torch()
     k, v = p["k"], p["v"]
-    if k.dim() != 5 or v.shape != k.shape or v.dtype != k.dtype:
+    # (every call comes by here: an attribute of a tensor takes as long as a look into a dictionary three times)
+    shape, dtype = k.shape, k.dtype
+    if len(shape) != 5 or v.shape != shape or v.dtype != dtype:
         raise ValueError("expected k and v of one type, [layers, pages, KV heads, page_tokens, head_dim]")
-    n_layers, n_pages, n_heads, tokens, dim = k.shape
+    n_layers, n_pages, n_heads, tokens, dim = shape
     if tokens != int(p.get("page_tokens", tokens)):
         raise ValueError(f"pages of {tokens} tokens, not {p['page_tokens']}")
-    four = k.dtype == torch.uint8
+    four = dtype == torch.uint8
     if four:
         dim *= 2
     pool = hx_kv_pool(n_layers, n_pages, n_heads, tokens, dim, HX_E2M1 if four else _number_type(k, HX_BF16, HX_F16, HX_E4M3), _ptr(k), _ptr(v),
@@ -290,7 +292,7 @@ def make_kv_pool(p: dict) -> hx_kv_pool:
         exps = n_layers * n_pages * n_heads * tokens * (dim // 32)
         pool.k_exp, pool.v_exp = _ptr(p.get("k_exp"), torch.uint8, exps), _ptr(p.get("v_exp"), torch.uint8, exps)
     if "bounds" in p:
-        wide = k.dtype if k.dtype in (torch.bfloat16, torch.float16) else torch.bfloat16
+        wide = dtype if dtype in (torch.bfloat16, torch.float16) else torch.bfloat16
         pool.bounds = _ptr(p["bounds"], wide, n_layers * n_pages * n_heads * 2 * dim)
     return pool
 
