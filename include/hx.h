@@ -648,7 +648,17 @@ typedef struct {
     int32_t n, max_pages;     /* rows, entries of a row                                         */
     int32_t *table;           /* device [n][max_pages]                                          */
     int32_t *len;             /* device [n] tokens of each row                                  */
+    float *weight;            /* device [n][max_pages * page_tokens] what hx_kv_weigh has added to each token, or NULL: they are
+                                 not kept, or not looked at by this call                        */
 } hx_kv_seqs;
+
+/*
+ * Weights go with their tokens: those that hx_kv_grow lets in begin with 0, a copy
+ * (hx_kv_fork) has its source's, what hx_kv_keep and hx_kv_evict move takes its own along
+ * and leaves 0 behind the row's end.  A token that hx_kv_free takes the page of keeps its.
+ * What lies behind a row's end has no meaning.  A call that is given weight NULL
+ * leaves all of them as they are, in their old places.
+ */
 
 /*
  * Pools of HX_E2M1 hold a number in 4 bits and, for 32 of them, a power of two
@@ -828,8 +838,9 @@ int hx_attend_top(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_k
  * What hx_attend with the same args gave each token, summed: for every sequence
  * and position y of its row
  *   weight[row][y] += sum over its queries j that see y and their heads a of exp(s - lse[j][a])
- * weight: device [seqs n][max_pages * page_tokens].  args->lse is hx_attend's;
- * where it is not finite a query's head adds nothing.  args->out is not used.  A
+ * weight: device [seqs n][max_pages * page_tokens], as a rule seqs->weight, which the page calls
+ * take along with the tokens.  args->lse is hx_attend's (hx_attend_top's knows only of the pages that were chosen: the
+ * others' tokens would be given weights too); where it is not finite a query's head adds nothing.  args->out is not used.  A
  * row listed twice counts once, for its first entry.  Sums are held in 32 bits
  * and added in an order that the arguments alone determine.
  */
@@ -841,7 +852,7 @@ int hx_kv_weigh(hx_ctx *ctx, const hx_kv_pool *pool, int32_t layer, const hx_kv_
  * the last n_last, and of the others those of the largest weight[row][y], of equal
  * ones the earlier (what is not above 0 counts as 0).  Tokens whose page is not
  * there go.  The others move together in every layer, in order, and their weights
- * with them (those behind them become 0); pages past them are given back.  A page
+ * with them (those behind them become 0; weight is seqs->weight where that is given); pages past them are given back.  A page
  * that other rows hold too, or that is not there, is replaced by a free one where
  * something in it would change or where the row goes on in it; rows for which no
  * page is left are left as they are (HX_ERR_CAPACITY).  kept: device [n][n_keep]

@@ -84,7 +84,7 @@ class hx_kv_pool(C.Structure):
 
 
 class hx_kv_seqs(C.Structure):
-    _fields_ = [("n", C.c_int32), ("max_pages", C.c_int32), ("table", C.c_void_p), ("len", C.c_void_p)]
+    _fields_ = [("n", C.c_int32), ("max_pages", C.c_int32), ("table", C.c_void_p), ("len", C.c_void_p), ("weight", C.c_void_p)]
 
 
 class hx_attend_args(C.Structure):
@@ -297,11 +297,18 @@ def make_kv_pool(p: dict) -> hx_kv_pool:
     return pool
 
 
-def make_kv_seqs(s: dict) -> hx_kv_seqs:
+def make_kv_seqs(s: dict, pool=None) -> hx_kv_seqs:
+    """From table [rows, pages a row], len [rows] and, where the tokens' weights go with them, weight [rows, pages a row * page_tokens] of float32
+    (the pages are the pool's)."""
     torch = _torch()
     table = s["table"]
     n, max_pages = table.shape
-    return hx_kv_seqs(n, max_pages, _ptr(table, torch.int32), _ptr(s["len"], torch.int32, n))
+    seqs = hx_kv_seqs(n, max_pages, _ptr(table, torch.int32), _ptr(s["len"], torch.int32, n))
+    if "weight" in s:
+        if pool is None:
+            raise ValueError("weights of tokens without the pool whose pages they are in")
+        seqs.weight = _ptr(s["weight"], torch.float32, n * max_pages * pool["k"].shape[3])
+    return seqs
 
 
 def _strided(t, n, heads, dim):
@@ -610,19 +617,19 @@ class Context:
 
     def hx_kv_fork(self, pool, seqs, src, dst, n_tok=None, stream=None):
         torch = _torch()
-        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs), int(src.numel()), torch.int32
+        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs, pool), int(src.numel()), torch.int32
         self._invoke(self.lib.hx_kv_fork, self._ctx, C.byref(kv), C.byref(sq), n, _ptr(src, i32), _ptr(dst, i32, n),
                      _ptr(n_tok, i32, n), _stream(stream))
 
     def hx_kv_grow(self, pool, seqs, row, n_new, stream=None):
         torch = _torch()
-        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs), int(row.numel()), torch.int32
+        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs, pool), int(row.numel()), torch.int32
         self._invoke(self.lib.hx_kv_grow, self._ctx, C.byref(kv), C.byref(sq), n, _ptr(row, i32), _ptr(n_new, i32, n), _stream(stream))
 
     def hx_kv_write(self, pool, layer, seqs, row, tok_ptr, k, v, stream=None):
         """k, v [tokens, KV heads, head_dim], of one type and one set of strides."""
         torch = _torch()
-        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs), int(row.numel()), torch.int32
+        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs, pool), int(row.numel()), torch.int32
         n_tok = int(k.shape[0])
         kp, token, head = _strided(k, n_tok, kv.n_heads, kv.head_dim)
         vp, v_token, v_head = _strided(v, n_tok, kv.n_heads, kv.head_dim)
@@ -635,7 +642,7 @@ class Context:
     def hx_kv_read(self, pool, layer, seqs, row, tok_ptr, k, v, stream=None):
         """k, v [tokens, KV heads, head_dim], of one type and one set of strides, are filled with what the cache holds."""
         torch = _torch()
-        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs), int(row.numel()), torch.int32
+        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs, pool), int(row.numel()), torch.int32
         n_tok = int(k.shape[0])
         kp, token, head = _strided(k, n_tok, kv.n_heads, kv.head_dim)
         vp, v_token, v_head = _strided(v, n_tok, kv.n_heads, kv.head_dim)
@@ -647,19 +654,19 @@ class Context:
 
     def hx_kv_keep(self, pool, seqs, row, n_draft, keep_ptr, keep, stream=None):
         torch = _torch()
-        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs), int(row.numel()), torch.int32
+        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs, pool), int(row.numel()), torch.int32
         self._invoke(self.lib.hx_kv_keep, self._ctx, C.byref(kv), C.byref(sq), n, _ptr(row, i32), _ptr(n_draft, i32, n),
                      _ptr(keep_ptr, i32, n + 1), _ptr(keep, i32), int(keep.numel()), _stream(stream))
 
     def hx_kv_free(self, pool, seqs, row, first=None, last=None, stream=None):
         torch = _torch()
-        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs), int(row.numel()), torch.int32
+        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs, pool), int(row.numel()), torch.int32
         self._invoke(self.lib.hx_kv_free, self._ctx, C.byref(kv), C.byref(sq), n, _ptr(row, i32), _ptr(first, i32, n), _ptr(last, i32, n),
                      _stream(stream))
 
     def hx_kv_compact(self, pool, seqs, n_used=None, moved=None, stream=None):
         torch = _torch()
-        kv, sq, i32 = make_kv_pool(pool), make_kv_seqs(seqs), torch.int32
+        kv, sq, i32 = make_kv_pool(pool), make_kv_seqs(seqs, pool), torch.int32
         self._invoke(self.lib.hx_kv_compact, self._ctx, C.byref(kv), C.byref(sq), _ptr(n_used, i32, 1), _ptr(moved, i32, kv.n_pages),
                      _stream(stream))
 
@@ -667,7 +674,7 @@ class Context:
                   lse=None, stream=None):
         """q, out [queries, query heads, head_dim] (any strides before the last dimension); scale None: head_dim ** -0.5; max_len None:
         what the table can hold."""
-        kv, sq = make_kv_pool(pool), make_kv_seqs(seqs)
+        kv, sq = make_kv_pool(pool), make_kv_seqs(seqs, pool)
         a = _attend_args(kv, sq, q_ptr, q, out, max_q, max_len, row, scale, lse)
         a.window, a.n_sink, a.parent = int(window), int(n_sink), _ptr(parent, _torch().int32, a.n_q)
         self._invoke(self.lib.hx_attend, self._ctx, C.byref(kv), int(layer), C.byref(sq), C.byref(a), _stream(stream))
@@ -675,20 +682,21 @@ class Context:
     def hx_kv_bound(self, pool, layer, seqs, row, n_new=None, stream=None):
         """Of the pages with the rows' last n_new tokens (None: all); layer -1: in all layers."""
         torch = _torch()
-        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs), int(row.numel()), torch.int32
+        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs, pool), int(row.numel()), torch.int32
         self._invoke(self.lib.hx_kv_bound, self._ctx, C.byref(kv), int(layer), C.byref(sq), n, _ptr(row, i32), _ptr(n_new, i32, n), _stream(stream))
 
     def hx_attend_top(self, pool, layer, seqs, q_ptr, q, out, max_q, n_pages, n_first=0, n_last=1, max_len=None, row=None, scale=None, chosen=None,
                       lse=None, stream=None):
         """As hx_attend over n_pages pages for each query and KV head; chosen [queries, KV heads, n_pages]."""
-        kv, sq = make_kv_pool(pool), make_kv_seqs(seqs)
+        kv, sq = make_kv_pool(pool), make_kv_seqs(seqs, pool)
         a = _attend_args(kv, sq, q_ptr, q, out, max_q, max_len, row, scale, lse)
         t = hx_top(int(n_pages), int(n_first), int(n_last), _ptr(chosen, _torch().int32, a.n_q * kv.n_heads * int(n_pages)))
         self._invoke(self.lib.hx_attend_top, self._ctx, C.byref(kv), int(layer), C.byref(sq), C.byref(a), C.byref(t), _stream(stream))
 
     def hx_kv_weigh(self, pool, layer, seqs, q_ptr, q, lse, weight, max_q, max_len=None, row=None, scale=None, window=0, n_sink=0, parent=None, stream=None):
-        """The arguments of an hx_attend call and the lse that it left; weight [rows of the tables, entries of a row * page_tokens]."""
-        kv, sq = make_kv_pool(pool), make_kv_seqs(seqs)
+        """The arguments of an hx_attend call and the lse that it left; weight [rows of the tables, entries of a row * page_tokens], as a rule
+        seqs["weight"], which goes with the tokens."""
+        kv, sq = make_kv_pool(pool), make_kv_seqs(seqs, pool)
         a = _attend_args(kv, sq, q_ptr, q, None, max_q, max_len, row, scale, lse)
         a.window, a.n_sink, a.parent = int(window), int(n_sink), _ptr(parent, _torch().int32, a.n_q)
         self._invoke(self.lib.hx_kv_weigh, self._ctx, C.byref(kv), int(layer), C.byref(sq), C.byref(a), _weights(weight, kv, sq), _stream(stream))
@@ -696,7 +704,7 @@ class Context:
     def hx_kv_evict(self, pool, seqs, row, weight, n_keep, n_first=0, n_last=0, kept=None, stream=None):
         """weight as in hx_kv_weigh; kept [rows in the call, n_keep]."""
         torch = _torch()
-        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs), int(row.numel()), torch.int32
+        kv, sq, n, i32 = make_kv_pool(pool), make_kv_seqs(seqs, pool), int(row.numel()), torch.int32
         self._invoke(self.lib.hx_kv_evict, self._ctx, C.byref(kv), C.byref(sq), n, _ptr(row, i32), _weights(weight, kv, sq), int(n_keep), int(n_first),
                      int(n_last), _ptr(kept, i32, n * max(int(n_keep), 0)), _stream(stream))
 

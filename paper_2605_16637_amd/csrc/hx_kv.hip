@@ -9,6 +9,30 @@
 namespace {
 
 constexpr int CP_THREADS = 256;            // workgroups that copy
+constexpr int WT_EACH = 8;                 // weights of tokens that a thread moves at once
+
+// The tokens' weights, a row after the other; NULL where none are kept.
+struct Weights {
+    float *at;
+    int64_t pitch;
+    __device__ __forceinline__ float *row(int r) const { return at + r * pitch; }
+};
+// to[y] = from(y) for all y < n, by a workgroup.  A round's weights are all loaded before any is stored, as `to` may be where they lie: then from(y) has to
+// read places from y on, so that later rounds read what lies behind all that has been stored.
+template <typename F>
+__device__ __forceinline__ void move_weights(float *to, uint32_t n, F from)
+{
+    for (uint32_t y0 = threadIdx.x; y0 - threadIdx.x < n; y0 += CP_THREADS * WT_EACH) {
+        float x[WT_EACH];
+#pragma unroll
+        for (int k = 0; k < WT_EACH; ++k)
+            if (y0 + k * CP_THREADS < n) x[k] = from(y0 + k * CP_THREADS);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < WT_EACH; ++k)
+            if (y0 + k * CP_THREADS < n) to[y0 + k * CP_THREADS] = x[k];
+    }
+}
 constexpr int NO_CLAIM = 0x7fffffff;
 
 // Of several rows of a call with the same number the first counts.  claim: a word for each row of the tables.
@@ -33,6 +57,7 @@ struct ForkArgs {
     KvPlanes planes;
     char *bounds;            // or NULL
     int64_t bounds_bytes;    // of a page in one layer
+    Weights weights;
 };
 
 // One workgroup, so that pages go out in the order of the rows: a chain of memory round trips (the claim, the source's length and last
@@ -92,7 +117,7 @@ __global__ __launch_bounds__(PL_THREADS) void hx_kv_fork_plan_kernel(ForkArgs a)
     }
 }
 
-// Workgroup (i, 0): the shared pages of copy i; (i, 1 + planes layer + v): its last page's tokens in one layer's keys or values, 16 bytes a
+// Workgroup (i, 0): the shared pages of copy i, and its tokens' weights; (i, 1 + planes layer + v): its last page's tokens in one layer's keys or values, 16 bytes a
 // thread (the page's bounds, by the keys' workgroup).  Bound by HBM: 256 copies of tails in 32 layers, 1.0 GB read and written: 169 us, and their sources come from the caches three
 // times of four (a plain copy reaches 4.7 TB/s).
 __global__ __launch_bounds__(CP_THREADS) void hx_kv_fork_copy_kernel(ForkArgs a)
@@ -112,6 +137,10 @@ __global__ __launch_bounds__(CP_THREADS) void hx_kv_fork_copy_kernel(ForkArgs a)
         }
         // a last page that the source has given back is none of the copy's either
         if (threadIdx.x == 0 && (t & ((1 << kv.shift) - 1)) && a.from[i] < 0) to[t >> kv.shift] = -1;
+        if (a.weights.at) {
+            const float *theirs = a.weights.row(a.src[i]);
+            move_weights(a.weights.row(a.dst[i]), t, [&](uint32_t y) { return theirs[y]; });
+        }
         return;
     }
     if (a.from[i] < 0) return;
@@ -140,8 +169,9 @@ struct GrowArgs {
     const int32_t *row, *n_new;
     int32_t *claim;              // [rows]
     int32_t *first;              // [n] pages wanted by the rows before
-    int32_t *have;               // [n] pages the row has
+    int32_t *have;               // [n] pages the row has; after the call -1 where it has not grown
     int32_t *list;               // [n_pages]
+    Weights weights;
 };
 
 // As the fork's plan: round trips.  64 rows, 32 tokens each: 10.1 us.
@@ -195,9 +225,20 @@ __global__ __launch_bounds__(PL_THREADS) void hx_kv_grow_kernel(GrowArgs a)
     for (int i = threadIdx.x; i < a.n; i += PL_THREADS) {
         if (a.have[i] < 0) continue;
         const int r = a.row[i], len = kv.len[r] + a.n_new[i], need = hx_pages_of(len, kv.shift) - a.have[i];
-        if (need > 0 && (int64_t)a.first[i] + need > found) hx_raise(kv.status, HX_ERR_CAPACITY);
+        if (need > 0 && (int64_t)a.first[i] + need > found) { hx_raise(kv.status, HX_ERR_CAPACITY); a.have[i] = -1; }
         else kv.len[r] = len;
     }
+}
+
+// The tokens that have come in weigh nothing yet; a workgroup a row.
+__global__ __launch_bounds__(CP_THREADS) void hx_kv_grow_weights_kernel(GrowArgs a)
+{
+    const int i = blockIdx.x;
+    if (a.have[i] < 0) return;
+    const int r = a.row[i];
+    const uint32_t len = a.kv.len[r], from = len - a.n_new[i];
+    float *w = a.weights.row(r);
+    for (uint32_t y = from + threadIdx.x; y < len; y += CP_THREADS) w[y] = 0.0f;
 }
 
 // ---- write -------------------------------------------------------------------
@@ -455,6 +496,7 @@ struct KeepArgs {
     const int32_t *row, *n_draft, *keep_ptr, *keep;
     int32_t *ok;             // [n] whether the row is changed
     KvPlanes planes;
+    Weights weights;
 };
 
 // Whether entry i of the call can be carried out; the same for all threads.  Its answer is taken before anything of the call
@@ -543,6 +585,13 @@ __global__ __launch_bounds__(CP_THREADS) void hx_kv_keep_apply_kernel(KeepArgs a
         const int page = table[b];
         table[b] = -1;
         if (page >= 0) give_back(kv, page);
+    }
+    if (a.weights.at) {
+        const int base = len - a.n_draft[i], k0 = a.keep_ptr[i];
+        float *w = a.weights.row(r);
+        move_weights(w + base, left - base, [&](uint32_t j) { return w[base + a.keep[k0 + j]]; });       // (numbers rise: keep[k0 + j] >= j)
+        __syncthreads();
+        for (uint32_t y = left + threadIdx.x; y < (uint32_t)len; y += CP_THREADS) w[y] = 0.0f;
     }
     __syncthreads();
     if (threadIdx.x == 0) kv.len[r] = left;
@@ -650,6 +699,8 @@ __global__ __launch_bounds__(CP_THREADS) void hx_kv_compact_apply_kernel(Compact
     }
 }
 
+Weights weights_of(const KvView &kv, const hx_kv_seqs *seqs) { return Weights{seqs->weight, (int64_t)kv.max_pages << kv.shift}; }
+
 int blocks_for(int64_t items, int threads, int64_t most)
 {
     const int64_t b = (items + threads - 1) / threads;
@@ -683,7 +734,7 @@ extern "C" int hx_kv_fork(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs 
     if (int rc = hx_scratch(ctx, hx_serve(ctx)->kv, ((size_t)kv.rows + 4 * (size_t)n) * sizeof(int32_t), stream)) return rc;
     int32_t *w = (int32_t *)hx_serve(ctx)->kv.p;
     ForkArgs a{kv, n, src, dst, n_tok, w, w + kv.rows, w + kv.rows + n, w + kv.rows + 2 * (size_t)n, w + kv.rows + 3 * (size_t)n,
-               planes, (char *)pool->bounds, hx_bounds_bytes(pool)};
+               planes, (char *)pool->bounds, hx_bounds_bytes(pool), weights_of(kv, seqs)};
     hx_kv_fork_plan_kernel<<<1, PL_THREADS, 0, stream>>>(a);
     hx_kv_fork_copy_kernel<<<n * parts, CP_THREADS, 0, stream>>>(a);
     return hx_check_launch(ctx, "hx_kv_fork_copy_kernel");
@@ -697,8 +748,9 @@ extern "C" int hx_kv_grow(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs 
     HX_KV_DEVICE(ctx);
     if (int rc = hx_scratch(ctx, hx_serve(ctx)->kv, ((size_t)kv.rows + 2 * (size_t)n + kv.n_pages) * sizeof(int32_t), stream)) return rc;
     int32_t *w = (int32_t *)hx_serve(ctx)->kv.p;
-    GrowArgs a{kv, n, row, n_new, w, w + kv.rows, w + kv.rows + n, w + kv.rows + 2 * (size_t)n};
+    GrowArgs a{kv, n, row, n_new, w, w + kv.rows, w + kv.rows + n, w + kv.rows + 2 * (size_t)n, weights_of(kv, seqs)};
     hx_kv_grow_kernel<<<1, PL_THREADS, 0, stream>>>(a);
+    if (a.weights.at) hx_kv_grow_weights_kernel<<<n, CP_THREADS, 0, stream>>>(a);
     return hx_check_launch(ctx, "hx_kv_grow_kernel");
 }
 
@@ -773,7 +825,7 @@ extern "C" int hx_kv_keep(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs 
     const int parts = planes.n * kv.n_layers;
     HX_KV_DEVICE(ctx);
     if (int rc = hx_scratch(ctx, hx_serve(ctx)->kv, (size_t)n * sizeof(int32_t), stream)) return rc;
-    KeepArgs a{kv, n, n_keep, row, n_draft, keep_ptr, keep, (int32_t *)hx_serve(ctx)->kv.p, planes};
+    KeepArgs a{kv, n, n_keep, row, n_draft, keep_ptr, keep, (int32_t *)hx_serve(ctx)->kv.p, planes, weights_of(kv, seqs)};
     hx_kv_keep_move_kernel<<<n * parts, CP_THREADS, 0, stream>>>(a);
     hx_kv_keep_apply_kernel<<<n, CP_THREADS, 0, stream>>>(a);
     return hx_check_launch(ctx, "hx_kv_keep_apply_kernel");

@@ -277,6 +277,7 @@ extern "C" int hx_kv_evict(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs
     if (n == 0) return HX_OK;
     HX_REQUIRE(ctx, row && weight, HX_ERR_INVALID_ARG, "NULL array");
     HX_REQUIRE(ctx, ((uintptr_t)weight & 3) == 0, HX_ERR_INVALID_ARG, "weights are not aligned to their type");
+    HX_REQUIRE(ctx, !seqs->weight || seqs->weight == weight, HX_ERR_INVALID_ARG, "weights that are not the sequences' own, which would stay in their old places");
     HX_REQUIRE(ctx, kv.rows > 0, HX_ERR_INVALID_ARG, "%d rows asked for of no sequences", n);
     const KvPlanes planes = hx_kv_planes(pool);
     // a round is a chain of lookups, and a slice of half the bytes takes twice the tokens in one: slices until the chip is full, of no less than 64 bytes.

@@ -111,6 +111,7 @@ inline int hx_kv_view(hx_ctx *ctx, const hx_kv_pool *pool, const hx_kv_seqs *seq
     HX_REQUIRE(ctx, seqs->n >= 0 && seqs->max_pages >= 0, HX_ERR_INVALID_ARG, "negative size of sequences");
     HX_REQUIRE(ctx, (int64_t)seqs->max_pages * T <= INT32_MAX, HX_ERR_SHAPE, "%d pages of %d tokens a row are beyond int32", seqs->max_pages, T);
     HX_REQUIRE(ctx, seqs->n == 0 || (seqs->len && (seqs->table || seqs->max_pages == 0)), HX_ERR_INVALID_ARG, "NULL member in sequences");
+    HX_REQUIRE(ctx, ((uintptr_t)seqs->weight & 3) == 0, HX_ERR_INVALID_ARG, "the sequences' weights are not aligned to their type");
     int shift = 0;
     while ((1 << shift) < T) ++shift;
     *out = KvView{pool->k, pool->v, pool->ref, seqs->table, seqs->len, ctx->d_status, pool->n_layers, pool->n_pages, pool->n_heads, shift,
