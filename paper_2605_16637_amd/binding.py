@@ -313,11 +313,12 @@ def make_kv_seqs(s: dict, pool=None) -> hx_kv_seqs:
 
 def _strided(t, n, heads, dim):
     """Address, token and head stride of a [n, heads, dim] tensor whose last dimension is contiguous (any strides before it)."""
-    if t.dim() != 3 or t.shape[0] < n or t.shape[1] != heads or t.shape[2] != dim:
-        raise ValueError(f"expected [{n}, {heads}, {dim}], got {list(t.shape)}")
-    if not t.is_cuda or (dim > 1 and t.stride(2) != 1):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] < n or shape[1] != heads or shape[2] != dim:
+        raise ValueError(f"expected [{n}, {heads}, {dim}], got {list(shape)}")
+    if not t.is_cuda or (dim > 1 and stride[2] != 1):
         raise ValueError("expected a tensor in device memory whose last dimension is contiguous")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    return t.data_ptr(), stride[0], stride[1]
 
 
 def _attend_args(kv, sq, q_ptr, q, out, max_q, max_len, row, scale, lse):
