@@ -212,12 +212,13 @@ struct Weigher {
 // sequence's row is another's to none: no atomics, the same sums every time.
 //
 // FEW: up to 16 rows a KV head, bound by the keys' bytes.  A wavefront takes 32 keys and all heads, so that its sums need no other's; two
-// heads' keys are under way.  128 sequences over some 4000 tokens, 8 KV heads of 128: 264 us, 3.9 TB/s of keys (with the workgroup's wavefronts on
+// heads' keys are under way.  100 sequences over some 4000 tokens, 8 KV heads of 128: 264 us, 3.9 TB/s of keys (with the workgroup's wavefronts on
 // a head each and their sums joined in LDS 303; at three wavefronts a SIMD 328, as the keys under way do not fit their registers).
 // Else the wavefronts have the same 32 keys and divide heads and rows, 16 rows a step, and their sums are added in LDS: there are rows for many
 // steps, and as few keys as possible a workgroup fill the chip.  Rows come through LDS, two steps ahead, and a head's keys are made operands
-// once.  What it does is exponentials and what goes with them, 8 a lane for 8 matrix instructions, and the wait for a head's first keys.  The last 32 queries of 7
-// prompts of some 6000 tokens, 32 heads of 128: 58 us at three wavefronts a SIMD, 67 at two; 75 with rows straight to registers, of which a load is an
+// once.  It mostly waits: for a head's first keys nothing else is under way.  The last 32 queries of 7
+// prompts of some 6000 tokens, 32 heads of 128: 58 us, of which 9.5e6 vector instructions are some 15 of the chip's issue (their exponentials 4) and the
+// matrix instructions 4; some 1290 workgroups have work, 1.7 rounds of three a CU.  That is at three wavefronts a SIMD, 67 at two; 75 with rows straight to registers, of which a load is an
 // access for each of 64 lanes and every step waited for all loads; 95 with 128 keys a workgroup.
 // a head and one of its row tiles
 struct Step {
